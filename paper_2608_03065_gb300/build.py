@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libpsc_gb300.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 CXX_SOURCES = ["grammar.cpp", "lexer.cpp", "lalr.cpp", "classifier.cpp", "bottomup.cpp", "persist.cpp"]
-CU_SOURCES = ["psc_capi.cu"]
+CU_SOURCES = ["psc_capi.cu", "process.cu", "sample.cu", "head.cu"]
 GENCODE = "arch=compute_103a,code=sm_103a"
 
 
@@ -44,6 +44,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 def _build_locked(force: bool, verbose: bool) -> str:
     headers = [os.path.join(CSRC, "psc_internal.h"), os.path.join(INCLUDE, "psc.h")]
+    ops_headers = [os.path.join(CSRC, "ops_common.cuh"), os.path.join(INCLUDE, "psc_ops.h")]
     nvcc = _nvcc()
     jobs = []
     objs = []
@@ -58,7 +59,7 @@ def _build_locked(force: bool, verbose: bool) -> str:
         s = os.path.join(CSRC, src)
         o = os.path.join(BUILD, src + ".o")
         objs.append(o)
-        if force or _stale(o, [s] + headers):
+        if force or _stale(o, [s] + headers + ops_headers):
             jobs.append([nvcc, "-gencode", GENCODE, "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
                          "-I", INCLUDE, "-c", s, "-o", o])
 

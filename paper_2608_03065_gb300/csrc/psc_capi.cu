@@ -2629,6 +2629,17 @@ psc_status upload_tables(std::unique_ptr<psc_handle>& h, int tables) {
 }  // namespace
 
 // ====================================================================== ABI
+// The error path of the C entries in other files (process.cu, sample.cu, head.cu).
+namespace psc {
+psc_status ops_fail(psc_status code, const char* what, const char* why) noexcept {
+    try {
+        return fail_with(code, std::string(what) + ": " + why);
+    } catch (...) {
+        return PSC_ERR_OOM;
+    }
+}
+}  // namespace psc
+
 extern "C" {
 
 const char* psc_last_error(void) { return g_last_error.c_str(); }

@@ -28,6 +28,8 @@ EXPORTED = ["psc_compile", "psc_destroy", "psc_last_error", "psc_info", "psc_sta
             "psc_host_advance", "psc_fill_apply_noalloc", "psc_fill_apply_argmax", "psc_save", "psc_load",
             "psc_decode_step", "psc_decode_step_mask", "psc_decode_step_advance", "psc_state_copy",
             "psc_host_classify_bottom_up", "psc_state_faults", "psc_check_wait"]
+# include/psc_ops.h: the operators around the mask
+EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "psc_process_logits", "psc_sample"]
 NOALLOC_MAX_ROWS = 16384
 
 
@@ -95,6 +97,12 @@ def load(path: str = LIB_PATH):
         "psc_load": (i32, [ctypes.c_char_p, vp, vp]),
         "psc_state_faults": (i32, [vp, vp, i32, vp]),
         "psc_check_wait": (i32, [vp, i32, vp]),
+        "psc_quantize_rows": (i32, [vp, i32, i64, i32, i32, vp, i64, vp, vp]),
+        "psc_head_work_bytes": (i64, [i32, i32, i32]),
+        "psc_head_logits": (i32, [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
+        "psc_process_logits": (i32, [vp, i32, i64, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i32,
+                                     vp, vp]),
+        "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -436,3 +444,129 @@ def psc_fill_apply_noalloc(h: Handle, q, depth, status, stack, logits, bitmask_o
                                          stack.shape[1], B, _ptr(logits, None, "logits"), _dtype_code(logits),
                                          _row_stride(logits), V, _ptr(bitmask_out, torch.int32, "bitmask_out"),
                                          _stream(stream)))
+
+
+# ------------------------------------------------- the operators around the mask
+def _rows(t, dtype, name, rows=None, cols=None):
+    """(device address, row stride) of a 2-D tensor with unit column stride, at
+    least `rows` x `cols` elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] < cols):
+        raise ValueError(f"{name} must be [{rows}, >={cols}], got {list(t.shape)}")
+    # a row of its own or a column of its own may carry any stride
+    stride = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return _ptr(t, dtype, name), stride
+
+
+def _mask_ptr(bitmask, B, V):
+    import torch
+    if bitmask is None:
+        return None
+    W = (V + 31) // 32
+    if bitmask.shape != (B, W) or not bitmask.is_contiguous():
+        raise ValueError(f"bitmask must be a contiguous [{B}, {W}] tensor")
+    return _ptr(bitmask, torch.int32, "bitmask")
+
+
+def psc_quantize_rows(x, q, scale, stream=None):
+    """q, scale := the rows of x (bf16 or f32 [T, K]) in 8-bit integers (int8 [T, K])
+    with a scale each (f32 [T]): activations by token, or weights by output channel."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    T, K = x.shape
+    code = _dtype_code(x)
+    px, sx = _rows(x, None, "x", T, K)
+    pq, sq = _rows(q, torch.int8, "q", T, K)
+    _check(load().psc_quantize_rows(px, code, sx, T, K, pq, sq, _ptr(scale, torch.float32, "scale", T),
+                                    _stream(stream)))
+
+
+def psc_head_work_bytes(T: int, V: int, K: int) -> int:
+    return load().psc_head_work_bytes(T, V, K)
+
+
+def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, stream=None):
+    """logits[:, :V] := (q @ w.T) * scale[:, None] * w_scale, -inf where bitmask forbids.
+    q int8 [T, K], w int8 [V, K] (rows at 16-byte-aligned addresses take the tensor
+    cores), scale f32 [T], w_scale f32 [V], logits bf16 or f32 [T, >=V].  work: a
+    uint8 tensor of at least psc_head_work_bytes(T, V, K) bytes to reuse (one is
+    taken from torch's allocator for the call otherwise)."""
+    import torch
+    if q.dim() != 2 or w.dim() != 2 or q.shape[1] != w.shape[1]:
+        raise ValueError("q and w must be [T, K] and [V, K]")
+    (T, K), V = q.shape, w.shape[0]
+    code = _dtype_code(logits)
+    pq, sq = _rows(q, torch.int8, "q")
+    pw, sw = _rows(w, torch.int8, "w")
+    pl, sl = _rows(logits, None, "logits", T, V)
+    n = load().psc_head_work_bytes(T, V, K)
+    if work is None:
+        pm = _mask_ptr(bitmask, T, V)
+        if stream is None or isinstance(stream, int):
+            s = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(stream)
+        else:
+            s = stream
+        with torch.cuda.stream(s):
+            work = torch.empty(n, dtype=torch.uint8, device=logits.device)
+    else:
+        pm = _mask_ptr(bitmask, T, V)
+    _check(load().psc_head_logits(pq, sq, _ptr(scale, torch.float32, "scale", T), T, pw, sw,
+                                  _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
+                                  _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+
+
+def psc_process_logits(logits, out=None, history=None, history_len=None, prompt_len=None, repetition=None,
+                       frequency=None, presence=None, bias_ids=None, bias=None, bitmask=None, V: int | None = None,
+                       stream=None):
+    """out[:, :V] := logits[:, :V] with penalties for the tokens of the history, biases
+    and the mask applied (in place when out is None).  history int32 [B, H] of
+    token ids, its first history_len[b] used, the first prompt_len[b] of those the
+    prompt; repetition, frequency, presence f32 [B]; bias_ids int32 and bias f32
+    [B, n].  Each may be None."""
+    import torch
+    if logits.dim() != 2:
+        raise ValueError("logits must be a 2-D tensor")
+    B = logits.shape[0]
+    V = logits.shape[1] if V is None else V
+    code = _dtype_code(logits)
+    pl, sl = _rows(logits, None, "logits", B, V)
+    po, so = (pl, sl) if out is None else _rows(out, logits.dtype, "out", B, V)
+    ph, sh, H = None, 0, 0
+    if history is not None and history.numel():
+        ph, sh = _rows(history, torch.int32, "history", B, 0)
+        H = history.shape[1]
+    n_bias = 0
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias come together")
+    if bias_ids is not None:
+        if bias_ids.dim() != 2 or bias_ids.shape[0] != B or bias.shape != bias_ids.shape:
+            raise ValueError("bias_ids and bias must be [B, n] tensors")
+        n_bias = bias_ids.shape[1]
+    _check(load().psc_process_logits(
+        pl, code, sl, po, so, B, V, ph, sh, H, _ptr(history_len, torch.int32, "history_len", B),
+        _ptr(prompt_len, torch.int32, "prompt_len", B), _ptr(repetition, torch.float32, "repetition", B),
+        _ptr(frequency, torch.float32, "frequency", B), _ptr(presence, torch.float32, "presence", B),
+        _ptr(bias_ids, torch.int32, "bias_ids", B * n_bias) if n_bias else None,
+        _ptr(bias, torch.float32, "bias", B * n_bias) if n_bias else None, n_bias, _mask_ptr(bitmask, B, V),
+        _stream(stream)))
+
+
+def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature=None, top_k=None, top_p=None,
+               min_p=None, V: int | None = None, stream=None):
+    """tokens[b] := a token drawn among the allowed ones with uniform[b] (f32 in [0, 1)),
+    logprobs[b] := ln of the probability it was drawn with.  temperature, top_p,
+    min_p f32 [B], top_k int32 [B]; None leaves a filter off (temperature 1)."""
+    import torch
+    if logits.dim() != 2:
+        raise ValueError("logits must be a 2-D tensor")
+    B = logits.shape[0]
+    V = logits.shape[1] if V is None else V
+    code = _dtype_code(logits)
+    pl, sl = _rows(logits, None, "logits", B, V)
+    _check(load().psc_sample(
+        pl, code, sl, B, V, _mask_ptr(bitmask, B, V), _ptr(uniform, torch.float32, "uniform", B),
+        _ptr(temperature, torch.float32, "temperature", B), _ptr(top_k, torch.int32, "top_k", B),
+        _ptr(top_p, torch.float32, "top_p", B), _ptr(min_p, torch.float32, "min_p", B),
+        _ptr(tokens, torch.int32, "tokens", B), _ptr(logprobs, torch.float32, "logprobs", B), _stream(stream)))
