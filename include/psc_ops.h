@@ -49,7 +49,9 @@ int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K);
  *   d_bitmask     : uint32 [T][ceil(V/32)], or NULL (every token allowed)
  *   d_logits      : [T] rows of row_stride elements of dtype; columns >= V are left as they are
  *   d_work        : at least psc_head_work_bytes(T, V, K) bytes, 256-byte aligned; calls that
- *                   overlap on the GPU need workspaces of their own
+ *                   overlap on the GPU need workspaces of their own.  Its first int32 is
+ *                   afterwards the number of blocks in which a bounded wait gave up (a
+ *                   pipeline fault; some logits are then not written), 0 otherwise
  * Rows at 16-byte-aligned addresses (base and stride, of d_q and d_w) take the
  * tensor cores at any K; others a path of integer dot products.
  * PSC_ERR_LIMIT: K over 131,072 (a sum could pass 32 bits). */

@@ -1,5 +1,16 @@
 // psc_quantize_rows and psc_head_logits: the vocabulary projection in 8-bit
 // integers with a scale per token and per vocabulary row, under the grammar's mask.
+//
+// The product is sum_k q[t][k] w[v][k] over whole numbers of 8 bits.  This GPU's
+// integer tensor rate is far below its 16-bit one, and whole numbers up to 2^11 are
+// exact in f16, so the tensor cores take both operands as f16 and add in f32: the
+// sums are those of the integers while they stay below 2^24.  What it has to move
+// is the weights, one byte each, so they stay bytes up to the SM and are widened
+// there, on the way from the TMA's buffers to the tensor core's.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "ops_common.cuh"
@@ -56,11 +67,12 @@ struct Head {
 // Integer dot products at any alignment: a block per 64 tokens x 64 vocabulary
 // rows, 4 x 4 sums a thread, 64 bytes of K at a time through shared memory.
 template <typename T>
-__global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned4) {
+__global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned4, int* faults) {
     constexpr int TILE = 64, KB = 16, LD = KB + 1;      // words of K per step; odd row length: no bank conflicts
     __shared__ int sw[TILE * LD], sq[TILE * LD];
     dep_wait();
     dep_launch();
+    if (!blockIdx.x && !blockIdx.y && !threadIdx.x) *faults = 0;
     const int v0 = blockIdx.x * TILE, t0 = blockIdx.y * TILE;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     int any = !h.bitmask;
@@ -115,11 +127,423 @@ __global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned
     }
 }
 
+// ------------------------------------------------------------ the tensor-core path
+//
+// k_head_mma: a persistent block per SM over tiles of 128 vocabulary rows (the
+// tensor core's M) by up to 256 tokens (its N).  The weights are the large operand
+// and every one is used for all tokens of the batch at once, so each is loaded and
+// widened once per 256 tokens.  Per 64 columns of K:
+//   warp 0        TMA: 128 x 128 bytes of weights into the byte ring (128 columns at a time)
+//   warps 8-15    bytes -> f16 into the operand ring, in the tensor core's 128-byte swizzle
+//   warp 2        TMA: the tokens' f16 rows (k_head_prep widened them) beside them
+//   warp 1        four tcgen05.mma of 128 x N x 16 into one of two accumulators in TMEM
+//   warps 4-7     the other accumulator: scales, mask, logits (a lane per vocabulary row)
+// Byte b becomes f16 without a conversion: b + 128 under the exponent of 1024 is
+// 1152 + b, minus 1152; five instructions for four bytes.
+constexpr int VT = 128;                       // vocabulary rows of a tile
+constexpr int NT_MAX = 256;                   // tokens of a tile at most
+constexpr int KB = 64;                        // columns of K per operand stage (128 bytes of f16)
+constexpr int RAW_BYTES = VT * 128;           // a stage of the byte ring: 128 columns
+constexpr int A_BYTES = VT * KB * 2;
+constexpr int MAX_RAW = 8, MAX_OPS = 4;
+constexpr int MMA_THREADS = 512;
+constexpr int SMEM_MAX = 227 * 1024;
+
+struct Plan {
+    int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
+    int n_raw, n_ops;                         // stages of the two rings
+    int Kp;                                   // K rounded up to whole stages
+    int tmem;                                 // TMEM columns
+    size_t smem;
+    int64_t x_at, flags_at, bytes;            // in the workspace: the fault word, the f16 tokens, the tile flags
+};
+
+Plan plan_of(int T, int V, int K) {
+    Plan p;
+    p.n_nt = (T + NT_MAX - 1) / NT_MAX;
+    p.N = ((T + p.n_nt - 1) / p.n_nt + 15) / 16 * 16;
+    p.n_vt = (V + VT - 1) / VT;
+    p.Kp = (K + KB - 1) / KB * KB;
+    const int stage = A_BYTES + p.N * KB * 2;
+    p.n_ops = 3;
+    p.n_raw = std::min(MAX_RAW, (SMEM_MAX - 2048 - p.n_ops * stage) / RAW_BYTES);
+    p.smem = 1024 + (size_t)p.n_ops * stage + (size_t)p.n_raw * RAW_BYTES;
+    p.tmem = 32;
+    while (p.tmem < 2 * p.N) p.tmem <<= 1;
+    p.x_at = 256;
+    p.flags_at = p.x_at + ((int64_t)T * p.Kp * 2 + 255) / 256 * 256;
+    p.bytes = p.flags_at + ((int64_t)p.n_vt * p.n_nt + 255) / 256 * 256;
+    return p;
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded wait: gives up after some seconds, or soon after any other wait of the block did.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+    for (int it = 0; it < (1 << 22); it++) {
+        if (mbar_try(bar, parity)) return true;
+        if ((it & 1023) == 1023 && *failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+// Shared-memory operand descriptor: rows of 128 bytes in the 128-byte swizzle, 8 rows per 1024 bytes.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float v[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
+}
+
+// Four signed bytes as four f16.
+__device__ __forceinline__ uint2 widen4(uint32_t b) {
+    const uint32_t u = b ^ 0x80808080u, base = 0x64646464u;
+    uint32_t lo = __byte_perm(u, base, 0x4140), hi = __byte_perm(u, base, 0x4342);
+    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+    __half2 l = __hsub2(*reinterpret_cast<__half2*>(&lo), off), h = __hsub2(*reinterpret_cast<__half2*>(&hi), off);
+    return make_uint2(*reinterpret_cast<uint32_t*>(&l), *reinterpret_cast<uint32_t*>(&h));
+}
+
+// The tokens' rows in f16, zero past K; which tiles hold an allowed token; the fault word.
+__global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_vt, int n_nt, int x_blocks,
+                                                   int* faults, __half* x, uint8_t* flags) {
+    dep_wait();
+    dep_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    if ((int)blockIdx.x < x_blocks) {                 // 16 columns a thread
+        const int per = Kp / 16;
+        const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (i >= (int64_t)h.T * per) return;
+        const int t = (int)(i / per), k = (int)(i - (int64_t)t * per) * 16;
+        const int8_t* src = h.q + (size_t)t * h.q_stride + k;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (k + 16 <= h.K) {
+            const uint4 v = *reinterpret_cast<const uint4*>(src);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else {
+            for (int j = 0; j < 16 && k + j < h.K; j++) w[j >> 2] |= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
+        }
+        uint4* dst = reinterpret_cast<uint4*>(x + (size_t)t * Kp + k);
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            const uint2 a = widen4(w[2 * j]), c = widen4(w[2 * j + 1]);
+            dst[j] = make_uint4(a.x, a.y, c.x, c.y);
+        }
+        return;
+    }
+    const int item = (blockIdx.x - x_blocks) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (item >= n_vt * n_nt) return;
+    const int vt = item / n_nt, t0 = (item - vt * n_nt) * N, t1 = min(h.T, t0 + N);
+    uint32_t any = 0;
+    // a lane per word of a token's four, eight tokens at a time
+    for (int t = t0 + (lane >> 2); t < t1; t += 8) {
+        const int wi = vt * 4 + (lane & 3);
+        if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
+    }
+    any = __any_sync(FULL, any != 0);
+    if (lane == 0) flags[item] = (uint8_t)any;
+}
+
 template <typename T>
-psc_status head(const Head& h, T* logits, cudaStream_t cs) {
+__global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_constant__ CUtensorMap w_map,
+                                                             const __grid_constant__ CUtensorMap x_map, Head h,
+                                                             T* logits, int N, int n_nt, int n_items, int Kp, int n_raw,
+                                                             int n_ops, int tmem_cols, int* faults,
+                                                             const uint8_t* flags) {
+    extern __shared__ uint8_t dyn[];
+    __shared__ __align__(8) uint64_t s_bars[2 * MAX_RAW + 2 * MAX_OPS + 5];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
+    const int op_bytes = A_BYTES + N * KB * 2;
+    auto ops_at = [&](int s) { return base + s * op_bytes; };
+    auto raw_at = [&](int s) { return base + n_ops * op_bytes + s * RAW_BYTES; };
+    const uint32_t bars = smem_addr(s_bars);
+    auto raw_full = [&](int s) { return bars + 8 * s; };
+    auto raw_empty = [&](int s) { return bars + 8 * (MAX_RAW + s); };
+    auto op_full = [&](int s) { return bars + 8 * (2 * MAX_RAW + s); };
+    auto op_empty = [&](int s) { return bars + 8 * (2 * MAX_RAW + MAX_OPS + s); };
+    auto acc_full = [&](int s) { return bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + 2 + s); };
+    const uint32_t drained = bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + 4);
+
+    if (threadIdx.x == 0) {
+        s_failed = 0;
+        for (int s = 0; s < n_raw; s++) mbar_init(raw_full(s), 1), mbar_init(raw_empty(s), 8);
+        for (int s = 0; s < n_ops; s++) mbar_init(op_full(s), 9), mbar_init(op_empty(s), 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), 4);
+        mbar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)),
+                     "r"(tmem_cols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    volatile int* failed = &s_failed;
+    const int n_k = Kp / KB, n_k2 = (n_k + 1) / 2;
+    // k_head_prep began once every earlier kernel had completed, and this one after it had
+    // begun: only what k_head_prep writes (flags, f16 tokens) has to be waited for.
+    const bool masked = h.bitmask != nullptr;
+    if (warp != 0 || masked) dep_wait();
+    auto is_active = [&](int item) { return !masked || flags[item]; };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int c = 0;
+            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+                if (!is_active(item)) continue;
+                const int v0 = item / n_nt * VT;
+                for (int k = 0; k < n_k2; k++, c++) {
+                    const int s = c % n_raw;
+                    if (!mbar_wait(raw_empty(s), (c / n_raw + 1) & 1, failed)) break;
+                    mbar_arrive_tx(raw_full(s), RAW_BYTES);
+                    tma_2d(raw_at(s), &w_map, k * 128, v0, raw_full(s));
+                }
+            }
+            if (*failed)                              // let the copies in flight land
+                for (int i = max(0, c - n_raw); i < c; i++)
+                    for (int it = 0; it < (1 << 20) && !mbar_try(raw_full(i % n_raw), (i / n_raw) & 1); it++) {}
+        }
+    } else if (warp == 2) {
+        if (lane == 0) {
+            int c = 0;
+            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+                if (!is_active(item)) continue;
+                const int t0 = item % n_nt * N;
+                for (int k = 0; k < n_k; k++, c++) {
+                    const int s = c % n_ops;
+                    if (!mbar_wait(op_empty(s), (c / n_ops + 1) & 1, failed)) break;
+                    mbar_arrive_tx(op_full(s), N * KB * 2);
+                    tma_2d(ops_at(s) + A_BYTES, &x_map, k * KB, t0, op_full(s));
+                }
+            }
+            // a stage in flight may never become full (its weights are missing): time for its copy to land
+            if (*failed)
+                for (int it = 0; it < (1 << 16); it++) mbar_try(drained, 1);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // D f32, A and B f16, both along K; N and M
+            const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(VT >> 4) << 24);
+            int c = 0, a = 0;
+            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+                if (!is_active(item)) continue;
+                const int buf = a & 1;
+                if (!mbar_wait(acc_empty(buf), (a / 2 + 1) & 1, failed)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                bool ok = true;
+                for (int k = 0; k < n_k; k++, c++) {
+                    const int s = c % n_ops;
+                    if (!(ok = mbar_wait(op_full(s), (c / n_ops) & 1, failed))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = operand_desc(ops_at(s)), db = operand_desc(ops_at(s) + A_BYTES);
+#pragma unroll
+                    for (int j = 0; j < KB / 16; j++)
+                        mma_f16(tmem + buf * N, da + 2 * j, db + 2 * j, idesc, k | j);
+                    mma_commit(op_empty(s));
+                }
+                if (!ok) break;
+                mma_commit(acc_full(buf));
+                a++;
+            }
+            if (*failed) {                            // let the products in flight finish
+                mma_commit(drained);
+                for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
+            }
+        }
+    } else if (warp >= 8) {
+        const int wc = warp - 8;
+        int c = 0, cr = 0;
+        bool ok = true;                               // the same in all lanes
+        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
+            if (!is_active(item)) continue;
+            for (int k = 0; k < n_k; k++, c++) {
+                const int sr = cr % n_raw, s = c % n_ops;
+                if (!(k & 1) && !(ok = __all_sync(FULL, mbar_wait(raw_full(sr), (cr / n_raw) & 1, failed)))) break;
+                // 16 rows a warp; lanes 0-3 and 4-7 take rows 4 apart, so that eight lanes
+                // touch all 32 banks in both swizzles
+                uint4 v[2];
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const int r = wc * 16 + j * 8 + (lane >> 3) + ((lane >> 2) & 1) * 4;
+                    const int col = (k & 1) * 4 + (lane & 3);
+                    const uint32_t from = raw_at(sr) + r * 128 + ((col ^ (r & 7)) << 4);
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w)
+                                 : "r"(from));
+                }
+                if ((k & 1) || k + 1 == n_k) {        // this stage's bytes are in registers
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(raw_empty(sr));
+                    cr++;
+                }
+                if (!(ok = __all_sync(FULL, mbar_wait(op_empty(s), (c / n_ops + 1) & 1, failed)))) break;
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const int r = wc * 16 + j * 8 + (lane >> 3) + ((lane >> 2) & 1) * 4;
+                    const uint2 a = widen4(v[j].x), b = widen4(v[j].y), d = widen4(v[j].z), e = widen4(v[j].w);
+                    const int odd = (lane >> 2) & 1, col = (lane & 3) * 2;
+                    const uint32_t to = ops_at(s) + r * 128;
+                    const uint4 first = odd ? make_uint4(d.x, d.y, e.x, e.y) : make_uint4(a.x, a.y, b.x, b.y);
+                    const uint4 second = odd ? make_uint4(a.x, a.y, b.x, b.y) : make_uint4(d.x, d.y, e.x, e.y);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + (((col + odd) ^ (r & 7)) << 4)),
+                                 "r"(first.x), "r"(first.y), "r"(first.z), "r"(first.w)
+                                 : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + (((col + 1 - odd) ^ (r & 7)) << 4)),
+                                 "r"(second.x), "r"(second.y), "r"(second.z), "r"(second.w)
+                                 : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(op_full(s));
+            }
+        }
+    } else if (warp >= 4) {
+        const int quad = warp & 3;
+        int a = 0;
+        for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+            const bool active = is_active(item);
+            const int vt = item / n_nt, t0 = (item - vt * n_nt) * N;
+            const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
+            const float sw = v < h.V ? h.w_scale[v] : 0.f;
+            const int buf = a & 1;
+            if (active) {
+                if (!__all_sync(FULL, mbar_wait(acc_full(buf), (a / 2) & 1, failed))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            }
+            const int n = min(N, h.T - t0);
+            for (int c0 = 0; c0 < n; c0 += 16) {
+                float y[16];
+                if (active) tmem_load16(tmem + ((uint32_t)(quad * 32) << 16) + buf * N + c0, y);
+                float st = 0.f;
+                uint32_t word = FULL;
+                if (lane < 16 && c0 + lane < n) {
+                    const int t = t0 + c0 + lane;
+                    st = h.scale[t];
+                    if (masked) word = active && wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u;
+                }
+#pragma unroll
+                for (int j = 0; j < 16; j++) {
+                    const uint32_t wj = __shfl_sync(FULL, word, j);
+                    const float sj = __shfl_sync(FULL, st, j);
+                    if (c0 + j < n && v < h.V)
+                        store_f32(logits + (size_t)(t0 + c0 + j) * h.row_stride + v,
+                                  (wj >> lane) & 1 ? y[j] * sj * sw : __uint_as_float(0xFF800000u));
+                }
+            }
+            if (active) {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty(buf));
+                a++;
+            }
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 3) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+    }
+    if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
+}
+
+// A tensor map over rows of `stride` bytes, boxes of `cols` x `rows` in the 128-byte swizzle.
+bool tensor_map(CUtensorMap* m, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t stride,
+                uint32_t box_cols, uint32_t box_rows) {
+    static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return (PFN_cuTensorMapEncodeTiled_v12000)f;
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
+    const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
+    return encode(m, type, 2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T>
+psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    const Plan p = plan_of(h.T, h.V, h.K);
+    int* faults = (int*)work;
+    __half* x = (__half*)(work + p.x_at);
+    uint8_t* flags = work + p.flags_at;
+    CUtensorMap w_map, x_map;
+    if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, h.K, h.V, h.w_stride, 128, VT) ||
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x, p.Kp, h.T, (uint64_t)p.Kp * 2, KB, p.N))
+        return ops_fail(PSC_ERR_CUDA, "psc_head_logits", "cuTensorMapEncodeTiled failed");
+    const int items = p.n_vt * p.n_nt;
+    const int x_blocks = (int)(((int64_t)h.T * (p.Kp / 16) + 255) / 256);
+    psc_status s = ops_launch(k_head_prep, dim3(x_blocks + (h.bitmask ? (items + 7) / 8 : 0)), 256, 0, 1, cs,
+                              "k_head_prep", h, p.Kp, p.N, p.n_vt, p.n_nt, x_blocks, faults, x, flags);
+    if (s != PSC_OK) return s;
+    return ops_launch(k_head_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
+                      w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_ops, p.tmem, faults,
+                      (const uint8_t*)flags);
+}
+
+template <typename T>
+psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    if (is_aligned(h.w, h.w_stride, 16) && is_aligned(h.q, h.q_stride, 16)) return head_mma(h, logits, work, cs);
     const int aligned4 = is_aligned(h.w, h.w_stride, 4) && is_aligned(h.q, h.q_stride, 4);
     return ops_launch(k_head_dot<T>, dim3((h.V + 63) / 64, (h.T + 63) / 64), 256, 0, 1, cs, "k_head_dot", h, logits,
-                      aligned4);
+                      aligned4, (int*)work);
 }
 
 }  // namespace
@@ -141,8 +565,8 @@ psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_strid
 }
 
 int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K) {
-    (void)T, (void)V, (void)K;
-    return 256;
+    if (T <= 0 || V <= 0 || K <= 0) return 256;
+    return plan_of(T, V, K).bytes;
 }
 
 psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_scale, int32_t T, const int8_t* d_w,
@@ -159,8 +583,8 @@ psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_s
     if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_work_bytes(T, V, K))
         return ops_fail(PSC_ERR_ARG, me, "workspace missing, unaligned or too small");
     const Head h{d_q, q_stride, d_scale, T, d_w, w_stride, d_w_scale, V, K, d_bitmask, (V + 31) / 32, row_stride};
-    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (cudaStream_t)stream);
-    return head(h, (float*)d_logits, (cudaStream_t)stream);
+    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
+    return head(h, (float*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
 }
 
 }  // extern "C"
