@@ -165,7 +165,7 @@ Plan plan_of(int T, int V, int K) {
     p.n_vt = (V + VT - 1) / VT;
     p.Kp = (K + KB - 1) / KB * KB;
     const int stage = A_BYTES + p.N * KB * 2;
-    p.n_ops = 3;
+    p.n_ops = p.N <= 128 ? 4 : 3;
     p.n_raw = std::min(MAX_RAW, (SMEM_MAX - 2048 - p.n_ops * stage) / RAW_BYTES);
     p.smem = 1024 + (size_t)p.n_ops * stage + (size_t)p.n_raw * RAW_BYTES;
     p.tmem = 32;
@@ -287,12 +287,13 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
     if (lane == 0) flags[item] = (uint8_t)any;
 }
 
-template <typename T>
+template <typename T, int GROUPS>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_constant__ CUtensorMap w_map,
                                                              const __grid_constant__ CUtensorMap x_map, Head h,
                                                              T* logits, int N, int n_nt, int n_items, int Kp, int n_raw,
                                                              int n_ops, int tmem_cols, int* faults,
                                                              const uint8_t* flags) {
+    constexpr int PER = 8 / GROUPS, ROWS = VT / PER;      // converting warps of a group, rows of each
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) uint64_t s_bars[2 * MAX_RAW + 2 * MAX_OPS + 5];
     __shared__ uint32_t s_tmem;
@@ -313,8 +314,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
 
     if (threadIdx.x == 0) {
         s_failed = 0;
-        for (int s = 0; s < n_raw; s++) mbar_init(raw_full(s), 1), mbar_init(raw_empty(s), 8);
-        for (int s = 0; s < n_ops; s++) mbar_init(op_full(s), 9), mbar_init(op_empty(s), 1);
+        for (int s = 0; s < n_raw; s++) mbar_init(raw_full(s), 1), mbar_init(raw_empty(s), 2 * PER);
+        for (int s = 0; s < n_ops; s++) mbar_init(op_full(s), PER + 1), mbar_init(op_empty(s), 1);
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), 4);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -402,37 +403,36 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             }
         }
     } else if (warp >= 8) {
-        const int wc = warp - 8;
+        // GROUPS groups of warps, a group per operand stage in turn: what one stage waits for
+        // (its bytes, its slot, its stores to become visible) passes while others are converted.
+        // A group that waits for the slot of stage number c has itself filled number c - GROUPS,
+        // so c - GROUPS - n_ops has been consumed; a wait tells a phase from the one after next
+        // only once c - 2 n_ops has been, hence GROUPS <= n_ops.
+        const int group = (warp - 8) / PER, r0 = (warp % PER) * ROWS + (lane >> 3) + ((lane >> 2) & 1) * 4;
         int c = 0, cr = 0;
         bool ok = true;                               // the same in all lanes
         for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
             if (!is_active(item)) continue;
-            for (int k = 0; k < n_k; k++, c++) {
-                const int sr = cr % n_raw, s = c % n_ops;
-                if (!(k & 1) && !(ok = __all_sync(FULL, mbar_wait(raw_full(sr), (cr / n_raw) & 1, failed)))) break;
-                // 16 rows a warp; lanes 0-3 and 4-7 take rows 4 apart, so that eight lanes
-                // touch all 32 banks in both swizzles
-                uint4 v[2];
+            for (int k = (group - c) & (GROUPS - 1); k < n_k; k += GROUPS) {
+                const int ck = c + k, s = ck % n_ops, sr = (cr + (k >> 1)) % n_raw;
+                if (!(ok = __all_sync(FULL, mbar_wait(raw_full(sr), ((cr + (k >> 1)) / n_raw) & 1, failed)))) break;
+                // lanes 0-3 and 4-7 take rows 4 apart, so that eight lanes touch all 32
+                // banks in both swizzles
+                uint4 v[ROWS / 8];
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const int r = wc * 16 + j * 8 + (lane >> 3) + ((lane >> 2) & 1) * 4;
-                    const int col = (k & 1) * 4 + (lane & 3);
-                    const uint32_t from = raw_at(sr) + r * 128 + ((col ^ (r & 7)) << 4);
+                for (int j = 0; j < ROWS / 8; j++) {
+                    const int r = r0 + j * 8;
+                    const uint32_t from = raw_at(sr) + r * 128 + ((((k & 1) * 4 + (lane & 3)) ^ (r & 7)) << 4);
                     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                                  : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w)
                                  : "r"(from));
                 }
-                if ((k & 1) || k + 1 == n_k) {        // this stage's bytes are in registers
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(raw_empty(sr));
-                    cr++;
-                }
-                if (!(ok = __all_sync(FULL, mbar_wait(op_empty(s), (c / n_ops + 1) & 1, failed)))) break;
+                if (!(ok = __all_sync(FULL, mbar_wait(op_empty(s), (ck / n_ops + 1) & 1, failed)))) break;
+                const int odd = (lane >> 2) & 1, col = (lane & 3) * 2;
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const int r = wc * 16 + j * 8 + (lane >> 3) + ((lane >> 2) & 1) * 4;
+                for (int j = 0; j < ROWS / 8; j++) {
+                    const int r = r0 + j * 8;
                     const uint2 a = widen4(v[j].x), b = widen4(v[j].y), d = widen4(v[j].z), e = widen4(v[j].w);
-                    const int odd = (lane >> 2) & 1, col = (lane & 3) * 2;
                     const uint32_t to = ops_at(s) + r * 128;
                     const uint4 first = odd ? make_uint4(d.x, d.y, e.x, e.y) : make_uint4(a.x, a.y, b.x, b.y);
                     const uint4 second = odd ? make_uint4(a.x, a.y, b.x, b.y) : make_uint4(d.x, d.y, e.x, e.y);
@@ -445,8 +445,14 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(op_full(s));
+                if (lane == 0) {
+                    mbar_arrive(op_full(s));
+                    mbar_arrive(raw_empty(sr));       // each warp of both halves' groups
+                    if (!(k & 1) && k + 1 == n_k) mbar_arrive(raw_empty(sr));
+                }
             }
+            c += n_k;
+            cr += n_k2;
         }
     } else if (warp >= 4) {
         const int quad = warp & 3;
@@ -533,7 +539,8 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     psc_status s = ops_launch(k_head_prep, dim3(x_blocks + (h.bitmask ? (items + 7) / 8 : 0)), 256, 0, 1, cs,
                               "k_head_prep", h, p.Kp, p.N, p.n_vt, p.n_nt, x_blocks, faults, x, flags);
     if (s != PSC_OK) return s;
-    return ops_launch(k_head_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
+    // GROUPS <= n_ops (see the converting warps)
+    return ops_launch(p.n_ops >= 4 ? k_head_mma<T, 4> : k_head_mma<T, 2>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
                       w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_ops, p.tmem, faults,
                       (const uint8_t*)flags);
 }

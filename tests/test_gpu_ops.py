@@ -149,6 +149,13 @@ def test_head_logits(psc, T, V, K, dtype, mask):
     _head_case(psc, T, V, K, dtype, mask, pad=-K % 16)
 
 
+@pytest.mark.parametrize("T,V,K", [(16, 40000, 1024), (128, 20500, 2048), (256, 21000, 4096), (500, 9000, 1500)])
+def test_head_logits_of_many_tiles_a_block(psc, T, V, K):
+    """Several tiles per SM and long sums: every ring of the pipeline goes round many times."""
+    _head_case(psc, T, V, K, "bf16", "none", pad=-K % 16)
+    _head_case(psc, T, V, K, "f32", "mixed", pad=-K % 16)
+
+
 @pytest.mark.parametrize("T", [1, 5, 40, 200])
 @pytest.mark.parametrize("K,pad,shift", [(65, 0, 0), (64, 4, 0), (64, 0, 4), (64, 0, 1), (31, 17, 0), (100, 28, 16)])
 def test_head_logits_at_any_alignment(psc, T, K, pad, shift):
