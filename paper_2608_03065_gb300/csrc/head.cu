@@ -145,13 +145,13 @@ constexpr int NT_MAX = 256;                   // tokens of a tile at most
 constexpr int KB = 64;                        // columns of K per operand stage (128 bytes of f16)
 constexpr int RAW_BYTES = VT * 128;           // a stage of the byte ring: 128 columns
 constexpr int A_BYTES = VT * KB * 2;
-constexpr int MAX_RAW = 8, MAX_OPS = 4;
+constexpr int MAX_RAW = 8, N_A = 4, MAX_X = 4;     // stages of the rings: bytes, widened weights, tokens
 constexpr int MMA_THREADS = 512;
 constexpr int SMEM_MAX = 227 * 1024;
 
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
-    int n_raw, n_ops;                         // stages of the two rings
+    int n_raw, n_x, x_group;                           // stages of the byte ring and of the tokens' ring
     int Kp;                                   // K rounded up to whole stages
     int tmem;                                 // TMEM columns
     size_t smem;
@@ -164,10 +164,14 @@ Plan plan_of(int T, int V, int K) {
     p.N = ((T + p.n_nt - 1) / p.n_nt + 15) / 16 * 16;
     p.n_vt = (V + VT - 1) / VT;
     p.Kp = (K + KB - 1) / KB * KB;
-    const int stage = A_BYTES + p.N * KB * 2;
-    p.n_ops = p.N <= 128 ? 4 : 3;
-    p.n_raw = std::min(MAX_RAW, (SMEM_MAX - 2048 - p.n_ops * stage) / RAW_BYTES);
-    p.smem = 1024 + (size_t)p.n_ops * stage + (size_t)p.n_raw * RAW_BYTES;
+    // A stage of the tokens' ring holds several columns' stages where those are small, so
+    // that the issuing warp waits and releases seldom; the byte ring, which covers the
+    // memory's latency, gets the shared memory that is left.
+    p.x_group = p.N <= 32 ? 4 : p.N <= 64 ? 2 : 1;
+    const int x_bytes = p.N * KB * 2 * p.x_group;
+    p.n_x = p.N <= 128 ? MAX_X : 3;
+    p.n_raw = std::min(MAX_RAW, (SMEM_MAX - 2048 - N_A * A_BYTES - p.n_x * x_bytes) / RAW_BYTES);
+    p.smem = 1024 + (size_t)N_A * A_BYTES + (size_t)p.n_x * x_bytes + (size_t)p.n_raw * RAW_BYTES;
     p.tmem = 32;
     while (p.tmem < 2 * p.N) p.tmem <<= 1;
     p.x_at = 256;
@@ -206,6 +210,35 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     *failed = 1;
     return false;
 }
+// The same by a whole warp, with one answer for all lanes; and for two barriers at once
+// (a poll takes about a hundred cycles to answer, so both are asked before either is looked at).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+    for (int it = 0; it < (1 << 22); it++) {
+        if (__all_sync(FULL, mbar_try(bar, parity))) return true;
+        if ((it & 1023) == 1023 && __any_sync(FULL, *failed)) return false;
+    }
+    *failed = 1;
+    return false;
+}
+__device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1,
+                                           volatile int* failed) {
+    const bool a = mbar_try(bar0, parity0), b = mbar_try(bar1, parity1);
+    if (__all_sync(FULL, a && b)) return true;
+    return warp_wait(bar0, parity0, failed) && warp_wait(bar1, parity1, failed);
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
+// A place in a ring of n slots: the slot and the parity of its current use.
+struct Place {
+    int s = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++s == n) s = 0, parity ^= 1;
+    }
+};
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -287,35 +320,40 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
     if (lane == 0) flags[item] = (uint8_t)any;
 }
 
-template <typename T, int GROUPS>
+template <typename T>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_constant__ CUtensorMap w_map,
                                                              const __grid_constant__ CUtensorMap x_map, Head h,
                                                              T* logits, int N, int n_nt, int n_items, int Kp, int n_raw,
-                                                             int n_ops, int tmem_cols, int* faults,
+                                                             int n_x, int x_group, int tmem_cols, int* faults,
                                                              const uint8_t* flags) {
-    constexpr int PER = 8 / GROUPS, ROWS = VT / PER;      // converting warps of a group, rows of each
+    constexpr int PER = 8 / N_A, ROWS = VT / PER;      // converting warps of a group, rows of each
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * MAX_RAW + 2 * MAX_OPS + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * (MAX_RAW + N_A + MAX_X) + 5];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
-    const int op_bytes = A_BYTES + N * KB * 2;
-    auto ops_at = [&](int s) { return base + s * op_bytes; };
-    auto raw_at = [&](int s) { return base + n_ops * op_bytes + s * RAW_BYTES; };
+    const int x_block = N * KB * 2, x_bytes = x_block * x_group;
+    auto a_at = [&](int s) { return base + s * A_BYTES; };
+    auto x_at = [&](int s) { return base + N_A * A_BYTES + s * x_bytes; };
+    auto raw_at = [&](int s) { return base + N_A * A_BYTES + n_x * x_bytes + s * RAW_BYTES; };
     const uint32_t bars = smem_addr(s_bars);
     auto raw_full = [&](int s) { return bars + 8 * s; };
     auto raw_empty = [&](int s) { return bars + 8 * (MAX_RAW + s); };
-    auto op_full = [&](int s) { return bars + 8 * (2 * MAX_RAW + s); };
-    auto op_empty = [&](int s) { return bars + 8 * (2 * MAX_RAW + MAX_OPS + s); };
-    auto acc_full = [&](int s) { return bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + s); };
-    auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + 2 + s); };
-    const uint32_t drained = bars + 8 * (2 * MAX_RAW + 2 * MAX_OPS + 4);
+    auto a_full = [&](int s) { return bars + 8 * (2 * MAX_RAW + s); };
+    auto a_empty = [&](int s) { return bars + 8 * (2 * MAX_RAW + N_A + s); };
+    auto x_full = [&](int s) { return bars + 8 * (2 * (MAX_RAW + N_A) + s); };
+    auto x_empty = [&](int s) { return bars + 8 * (2 * (MAX_RAW + N_A) + MAX_X + s); };
+    constexpr int LAST = 2 * (MAX_RAW + N_A + MAX_X);
+    auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
+    const uint32_t drained = bars + 8 * (LAST + 4);
 
     if (threadIdx.x == 0) {
         s_failed = 0;
         for (int s = 0; s < n_raw; s++) mbar_init(raw_full(s), 1), mbar_init(raw_empty(s), 2 * PER);
-        for (int s = 0; s < n_ops; s++) mbar_init(op_full(s), PER + 1), mbar_init(op_empty(s), 1);
+        for (int s = 0; s < N_A; s++) mbar_init(a_full(s), PER), mbar_init(a_empty(s), 1);
+        for (int s = 0; s < n_x; s++) mbar_init(x_full(s), 1), mbar_init(x_empty(s), 1);
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), 4);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -340,15 +378,15 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
 
     if (warp == 0) {
         if (lane == 0) {
+            Place p;
             int c = 0;
             for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
                 if (!is_active(item)) continue;
                 const int v0 = item / n_nt * VT;
-                for (int k = 0; k < n_k2; k++, c++) {
-                    const int s = c % n_raw;
-                    if (!mbar_wait(raw_empty(s), (c / n_raw + 1) & 1, failed)) break;
-                    mbar_arrive_tx(raw_full(s), RAW_BYTES);
-                    tma_2d(raw_at(s), &w_map, k * 128, v0, raw_full(s));
+                for (int k = 0; k < n_k2; k++, c++, p.next(n_raw)) {
+                    if (!mbar_wait(raw_empty(p.s), p.parity ^ 1, failed)) break;
+                    mbar_arrive_tx(raw_full(p.s), RAW_BYTES);
+                    tma_2d(raw_at(p.s), &w_map, k * 128, v0, raw_full(p.s));
                 }
             }
             if (*failed)                              // let the copies in flight land
@@ -357,65 +395,73 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
         }
     } else if (warp == 2) {
         if (lane == 0) {
+            Place p;
             int c = 0;
             for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
                 if (!is_active(item)) continue;
                 const int t0 = item % n_nt * N;
-                for (int k = 0; k < n_k; k++, c++) {
-                    const int s = c % n_ops;
-                    if (!mbar_wait(op_empty(s), (c / n_ops + 1) & 1, failed)) break;
-                    mbar_arrive_tx(op_full(s), N * KB * 2);
-                    tma_2d(ops_at(s) + A_BYTES, &x_map, k * KB, t0, op_full(s));
+                for (int k = 0; k < n_k; k += x_group, c++, p.next(n_x)) {
+                    if (!mbar_wait(x_empty(p.s), p.parity ^ 1, failed)) break;
+                    const int n = min(x_group, n_k - k);
+                    mbar_arrive_tx(x_full(p.s), n * x_block);
+                    for (int j = 0; j < n; j++)
+                        tma_2d(x_at(p.s) + j * x_block, &x_map, (k + j) * KB, t0, x_full(p.s));
                 }
             }
-            // a stage in flight may never become full (its weights are missing): time for its copy to land
             if (*failed)
-                for (int it = 0; it < (1 << 16); it++) mbar_try(drained, 1);
+                for (int i = max(0, c - n_x); i < c; i++)
+                    for (int it = 0; it < (1 << 20) && !mbar_try(x_full(i % n_x), (i / n_x) & 1); it++) {}
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            // D f32, A and B f16, both along K; N and M
-            const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(VT >> 4) << 24);
-            int c = 0, a = 0;
-            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
-                if (!is_active(item)) continue;
-                const int buf = a & 1;
-                if (!mbar_wait(acc_empty(buf), (a / 2 + 1) & 1, failed)) break;
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers;
+        // one lane issues.  D f32, A and B f16, both along K; N and M.
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(VT >> 4) << 24);
+        const bool issuer = elect_one();
+        Place pa, px, acc;
+        bool ok = true;
+        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
+            if (!is_active(item)) continue;
+            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+            const uint32_t d = tmem + acc.s * N;
+            int in_group = 0;
+            for (int k = 0; k < n_k; k++, pa.next(N_A)) {
+                if (!(ok = in_group ? warp_wait(a_full(pa.s), pa.parity, failed)
+                                    : warp_wait2(x_full(px.s), px.parity, a_full(pa.s), pa.parity, failed)))
+                    break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                bool ok = true;
-                for (int k = 0; k < n_k; k++, c++) {
-                    const int s = c % n_ops;
-                    if (!(ok = mbar_wait(op_full(s), (c / n_ops) & 1, failed))) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = operand_desc(ops_at(s)), db = operand_desc(ops_at(s) + A_BYTES);
+                const uint64_t da = operand_desc(a_at(pa.s)), db = operand_desc(x_at(px.s) + in_group * x_block);
+                const bool last = ++in_group == x_group || k + 1 == n_k;
+                if (issuer) {
 #pragma unroll
-                    for (int j = 0; j < KB / 16; j++)
-                        mma_f16(tmem + buf * N, da + 2 * j, db + 2 * j, idesc, k | j);
-                    mma_commit(op_empty(s));
+                    for (int j = 0; j < KB / 16; j++) mma_f16(d, da + 2 * j, db + 2 * j, idesc, k | j);
+                    mma_commit(a_empty(pa.s));
+                    if (last) mma_commit(x_empty(px.s));
+                    if (k + 1 == n_k) mma_commit(acc_full(acc.s));
                 }
-                if (!ok) break;
-                mma_commit(acc_full(buf));
-                a++;
+                if (last) in_group = 0, px.next(n_x);
             }
-            if (*failed) {                            // let the products in flight finish
-                mma_commit(drained);
-                for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
-            }
+            acc.next(2);
+        }
+        if (!ok && issuer) {                          // let the products in flight finish
+            mma_commit(drained);
+            for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= 8) {
-        // GROUPS groups of warps, a group per operand stage in turn: what one stage waits for
-        // (its bytes, its slot, its stores to become visible) passes while others are converted.
-        // A group that waits for the slot of stage number c has itself filled number c - GROUPS,
-        // so c - GROUPS - n_ops has been consumed; a wait tells a phase from the one after next
-        // only once c - 2 n_ops has been, hence GROUPS <= n_ops.
+        // N_A groups of warps, a group per slot of the ring: what one stage waits for (its
+        // bytes, its slot, its stores to become visible) passes while others are converted.
+        // Each group sees every phase of its slot's barriers, so a parity names one phase.
         const int group = (warp - 8) / PER, r0 = (warp % PER) * ROWS + (lane >> 3) + ((lane >> 2) & 1) * 4;
-        int c = 0, cr = 0;
+        int c = 0, cr = 0, at = 0;                    // stages of both rings before this item; pr is number `at`
+        Place pr;
+        uint32_t parity = 1;                          // of the group's slot's next release
         bool ok = true;                               // the same in all lanes
         for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
             if (!is_active(item)) continue;
-            for (int k = (group - c) & (GROUPS - 1); k < n_k; k += GROUPS) {
-                const int ck = c + k, s = ck % n_ops, sr = (cr + (k >> 1)) % n_raw;
-                if (!(ok = __all_sync(FULL, mbar_wait(raw_full(sr), ((cr + (k >> 1)) / n_raw) & 1, failed)))) break;
+            for (int k = (group - c) & (N_A - 1); k < n_k; k += N_A) {
+                const int s = group;
+                for (; at < cr + (k >> 1); at++) pr.next(n_raw);
+                const int sr = pr.s;
+                if (!(ok = warp_wait(raw_full(sr), pr.parity, failed))) break;
                 // lanes 0-3 and 4-7 take rows 4 apart, so that eight lanes touch all 32
                 // banks in both swizzles
                 uint4 v[ROWS / 8];
@@ -427,13 +473,14 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                                  : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w)
                                  : "r"(from));
                 }
-                if (!(ok = __all_sync(FULL, mbar_wait(op_empty(s), (ck / n_ops + 1) & 1, failed)))) break;
+                if (!(ok = warp_wait(a_empty(s), parity, failed))) break;
+                parity ^= 1;
                 const int odd = (lane >> 2) & 1, col = (lane & 3) * 2;
 #pragma unroll
                 for (int j = 0; j < ROWS / 8; j++) {
                     const int r = r0 + j * 8;
                     const uint2 a = widen4(v[j].x), b = widen4(v[j].y), d = widen4(v[j].z), e = widen4(v[j].w);
-                    const uint32_t to = ops_at(s) + r * 128;
+                    const uint32_t to = a_at(s) + r * 128;
                     const uint4 first = odd ? make_uint4(d.x, d.y, e.x, e.y) : make_uint4(a.x, a.y, b.x, b.y);
                     const uint4 second = odd ? make_uint4(a.x, a.y, b.x, b.y) : make_uint4(d.x, d.y, e.x, e.y);
                     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + (((col + odd) ^ (r & 7)) << 4)),
@@ -446,7 +493,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(op_full(s));
+                    mbar_arrive(a_full(s));
                     mbar_arrive(raw_empty(sr));       // each warp of both halves' groups
                     if (!(k & 1) && k + 1 == n_k) mbar_arrive(raw_empty(sr));
                 }
@@ -456,21 +503,20 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
         }
     } else if (warp >= 4) {
         const int quad = warp & 3;
-        int a = 0;
+        Place acc;
         for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
             const bool active = is_active(item);
             const int vt = item / n_nt, t0 = (item - vt * n_nt) * N;
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
             const float sw = v < h.V ? h.w_scale[v] : 0.f;
-            const int buf = a & 1;
             if (active) {
-                if (!__all_sync(FULL, mbar_wait(acc_full(buf), (a / 2) & 1, failed))) break;
+                if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
             const int n = min(N, h.T - t0);
             for (int c0 = 0; c0 < n; c0 += 16) {
                 float y[16];
-                if (active) tmem_load16(tmem + ((uint32_t)(quad * 32) << 16) + buf * N + c0, y);
+                if (active) tmem_load16(tmem + ((uint32_t)(quad * 32) << 16) + acc.s * N + c0, y);
                 float st = 0.f;
                 uint32_t word = FULL;
                 if (lane < 16 && c0 + lane < n) {
@@ -490,8 +536,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             if (active) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty(buf));
-                a++;
+                if (lane == 0) mbar_arrive(acc_empty(acc.s));
+                acc.next(2);
             }
         }
     }
@@ -539,9 +585,8 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     psc_status s = ops_launch(k_head_prep, dim3(x_blocks + (h.bitmask ? (items + 7) / 8 : 0)), 256, 0, 1, cs,
                               "k_head_prep", h, p.Kp, p.N, p.n_vt, p.n_nt, x_blocks, faults, x, flags);
     if (s != PSC_OK) return s;
-    // GROUPS <= n_ops (see the converting warps)
-    return ops_launch(p.n_ops >= 4 ? k_head_mma<T, 4> : k_head_mma<T, 2>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
-                      w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_ops, p.tmem, faults,
+    return ops_launch(k_head_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
+                      w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_x, p.x_group, p.tmem, faults,
                       (const uint8_t*)flags);
 }
 
