@@ -259,16 +259,18 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float v[16]) {
-    uint32_t r[16];
+// 16 columns of the warp's 32 lanes; complete after tmem_wait.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t r[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t r[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 16; i++) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 32; i++) asm volatile("" : "+r"(r[i]));      // no use of r before the wait
 }
 
 // Four signed bytes as four f16.
@@ -506,31 +508,41 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
         Place acc;
         for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
             const bool active = is_active(item);
-            const int vt = item / n_nt, t0 = (item - vt * n_nt) * N;
+            const int vt = item / n_nt, t0 = (item - vt * n_nt) * N, n = min(N, h.T - t0);
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
+            // the tile's scales and mask words (a lane per token), read while its products run
             const float sw = v < h.V ? h.w_scale[v] : 0.f;
+            float st[NT_MAX / 32];
+            uint32_t word[NT_MAX / 32];
+#pragma unroll
+            for (int i = 0; i < NT_MAX / 32; i++) {
+                const int t = i * 32 + lane;
+                st[i] = t < n ? h.scale[t0 + t] : 0.f;
+                word[i] = !masked ? FULL : active && t < n && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u;
+            }
             if (active) {
                 if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            const int n = min(N, h.T - t0);
-            for (int c0 = 0; c0 < n; c0 += 16) {
-                float y[16];
-                if (active) tmem_load16(tmem + ((uint32_t)(quad * 32) << 16) + acc.s * N + c0, y);
-                float st = 0.f;
-                uint32_t word = FULL;
-                if (lane < 16 && c0 + lane < n) {
-                    const int t = t0 + c0 + lane;
-                    st = h.scale[t];
-                    if (masked) word = active && wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u;
+            T* out = logits + (size_t)t0 * h.row_stride + v;
+#pragma unroll
+            for (int i = 0; i < NT_MAX / 32; i++) {
+                if (i * 32 >= n) break;
+                uint32_t y[32] = {};
+                if (active) {
+                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * N + i * 32;
+                    tmem_load16(from, y);
+                    if (i * 32 + 16 < N) tmem_load16(from + 16, y + 16);
+                    tmem_wait(y);
                 }
 #pragma unroll
-                for (int j = 0; j < 16; j++) {
-                    const uint32_t wj = __shfl_sync(FULL, word, j);
-                    const float sj = __shfl_sync(FULL, st, j);
-                    if (c0 + j < n && v < h.V)
-                        store_f32(logits + (size_t)(t0 + c0 + j) * h.row_stride + v,
-                                  (wj >> lane) & 1 ? y[j] * sj * sw : __uint_as_float(0xFF800000u));
+                for (int j = 0; j < 32; j++) {
+                    const uint32_t wj = __shfl_sync(FULL, word[i], j);
+                    const float sj = __shfl_sync(FULL, st[i], j);
+                    if (i * 32 + j < n && v < h.V)
+                        store_f32(out, (wj >> lane) & 1 ? __uint_as_float(y[j]) * sj * sw
+                                                        : __uint_as_float(0xFF800000u));
+                    out += h.row_stride;
                 }
             }
             if (active) {
