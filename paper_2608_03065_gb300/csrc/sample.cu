@@ -6,7 +6,7 @@
 // weight; the one where e^z reaches min_p.  So a row is filtered by one
 // threshold, found digit by digit of the logits' order (a histogram per 8-bit
 // digit, of counts for top-k, of weights for top-p), and the draw is the same
-// search by index.  Weights are whole numbers of 2^-40 of the largest: integer
+// search by token.  Weights are whole numbers of 2^-40 of the largest: integer
 // sums are the same in any order, so neither the atomics nor the split of a row
 // over blocks can change a draw.  41 bits hold every f32 e^z over 2^-17 exactly;
 // what is rounded away of a row is below V * 2^-41 of its largest weight.
@@ -22,7 +22,11 @@ namespace {
 
 constexpr int NT = 512;                 // threads of a block
 constexpr int NW = NT / 32;
-constexpr int CHUNK = 256;              // tokens a warp takes at a time: 8 neighbours a lane
+constexpr int CHUNK = 256;              // tokens a warp takes at a time: a piece of 8 neighbours a lane
+constexpr int UNROLL = 4;               // chunks in flight per warp
+constexpr int LIST = 2048;              // candidates that a block holds
+constexpr int BINS = NT;                // of the histogram of the groups' maxima
+constexpr int NUCLEUS_GROUPS = 640;     // maxima above the bound from which a nucleus is looked for
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_V = 1 << 22;
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -30,14 +34,16 @@ constexpr float FLT_BIG = 3.402823466e+38f;
 
 typedef unsigned long long u64;
 
-// Order of f32 values as unsigned numbers.
+// Order of f32 values as unsigned numbers (0 and -0 are one value).
 __device__ __forceinline__ uint32_t ordered(float x) {
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(__fadd_rn(x, 0.f));
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
+// NaN as -inf, +inf as the largest finite value.
+__device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, NEG_INF), FLT_BIG); }
 
 struct Row {
     const void* logits;
@@ -45,60 +51,136 @@ struct Row {
     int V, lo, hi;          // this block's tokens, lo a multiple of CHUNK
 };
 
-// The 8 tokens of piece v0..v0+7: their logits, -inf where masked, NaN, or past the end.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const Row& r, int v0, float x[8]) {
-    const T* p = static_cast<const T*>(r.logits) + v0;
-    const int n = r.hi - v0;
-    uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
-    if (n < 8 && n > 0) bits &= (1u << n) - 1;
-    if (VEC && n >= 8 && bits) {
-        if (sizeof(T) == 2) {
-            const uint4 q = *reinterpret_cast<const uint4*>(p);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        } else {
-            const float4 a = reinterpret_cast<const float4*>(p)[0], c = reinterpret_cast<const float4*>(p)[1];
-            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = c.x, x[5] = c.y, x[6] = c.z, x[7] = c.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = (bits >> i) & 1 ? load_f32(p + i) : NEG_INF;
+// Eight neighbouring tokens, -inf where they are masked or past the end.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void read(const __nv_bfloat16* p) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p);
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
     }
+    __device__ __forceinline__ void set(int i, const __nv_bfloat16* p) {
+        const uint32_t h = *reinterpret_cast<const uint16_t*>(p);
+        w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | h << 16 : (w[i >> 1] & 0xffff0000u) | h;
+    }
+    __device__ __forceinline__ void keep(const uint4& m) {      // m: ones where allowed
+        const uint32_t k[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-    for (int i = 0; i < 8; i++) x[i] = ((bits >> i) & 1) && x[i] > NEG_INF ? fminf(x[i], FLT_BIG) : NEG_INF;
+        for (int i = 0; i < 4; i++) w[i] = (w[i] & k[i]) | (0xFF80FF80u & ~k[i]);
+    }
+    __device__ __forceinline__ float max8() const {             // NaN only if all are
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+        const __nv_bfloat162 a = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(a), __high2float(a));
+    }
+    __device__ __forceinline__ float get(int i) const {
+        return clean(__uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16));
+    }
+};
+template <>
+struct Piece<float> {
+    float x[8];
+    __device__ __forceinline__ void read(const float* p) {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], c = reinterpret_cast<const float4*>(p)[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = c.x, x[5] = c.y, x[6] = c.z, x[7] = c.w;
+    }
+    __device__ __forceinline__ void set(int i, const float* p) { x[i] = *p; }
+    __device__ __forceinline__ void keep(uint32_t bits) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = (bits >> i) & 1 ? x[i] : NEG_INF;
+    }
+    __device__ __forceinline__ float max8() const {
+        float m = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int i = 2; i < 8; i++) m = fmaxf(m, x[i]);
+        return m;
+    }
+    __device__ __forceinline__ float get(int i) const { return clean(x[i]); }
+};
+
+// Calls f(piece, first token, chunk, u, any) for every piece of the block's part of the
+// row, UNROLL chunks in flight per warp (u: which of them).
+// Whole warps call it; `any` is false where a lane's piece holds nothing.
+template <typename T, bool VEC, typename F>
+__device__ __forceinline__ void for_pieces(const Row& r, const uint4* lut, F&& f) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
+    for (int c0 = warp; c0 < n_chunks; c0 += UNROLL * NW) {
+        Piece<T> p[UNROLL];
+        uint32_t bits[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; u++) {
+            const int v0 = r.lo + (c0 + u * NW) * CHUNK + lane * 8, n = r.hi - v0;
+            bits[u] = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
+            if (n > 0 && n < 8) bits[u] &= (1u << n) - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; u++) {
+            const int v0 = r.lo + (c0 + u * NW) * CHUNK + lane * 8;
+            const T* at = static_cast<const T*>(r.logits) + v0;
+            if (!bits[u]) continue;
+            if (VEC && r.hi - v0 >= 8) {
+                p[u].read(at);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((bits[u] >> i) & 1) p[u].set(i, at + i);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; u++) {
+            const int c = c0 + u * NW;
+            if (c >= n_chunks) break;
+            if constexpr (sizeof(T) == 2) p[u].keep(lut[bits[u]]);
+            else p[u].keep(bits[u]);
+            f(p[u], r.lo + c * CHUNK + lane * 8, c, u, bits[u] != 0);
+        }
+    }
 }
 
 // What a row's weights are computed from; the arithmetic is the header's, step by step.
 struct Weigh {
     float m, inv, tau, min_e;
     __device__ __forceinline__ float z(float x) const { return __fmul_rn(__fsub_rn(x, m), inv); }
+    __device__ __forceinline__ float e(float x) const { return expf(z(x)); }
     // weight of x before the filters
-    __device__ __forceinline__ u64 raw(float x) const { return __float2ull_rn(expf(z(x)) * 0x1p40f); }
+    __device__ __forceinline__ u64 raw(float x) const { return __float2ull_rn(e(x) * 0x1p40f); }
     // weight after them
     __device__ __forceinline__ u64 kept(float x) const {
-        const float e = expf(z(x));
-        return x >= tau && e >= min_e ? __float2ull_rn(e * 0x1p40f) : 0ull;
+        const float y = e(x);
+        return x >= tau && y >= min_e ? __float2ull_rn(y * 0x1p40f) : 0ull;
+    }
+};
+// A sum of weights as two 32-bit sums: with t = 2^20 e, its whole part and its fraction in
+// units of 2^-20, each taken from the low bits of a sum with 2^23 (rounded down, then to
+// nearest even; together rint(2^40 e), since the whole part is an even number of units).
+// Good for 2048 weights.
+struct WeightSum {
+    uint32_t hi = 0, lo = 0;
+    __device__ __forceinline__ void add(float e) {
+        const float t = e * 0x1p20f, a = __fadd_rz(t, 0x1p23f);
+        const float c = __fmaf_rn(t - (a - 0x1p23f), 0x1p20f, 0x1p23f);
+        hi += __float_as_uint(a) - 0x4B000000u;
+        lo += __float_as_uint(c) - 0x4B000000u;
     }
 };
 
 struct Shared {
     uint32_t cnt[2][256], hi[2][256];   // a histogram's counts, or its weights as two words
+    uint32_t bins[BINS];
     u64 part[8];                        // this block's share of what the cluster combines, a slot per use
     u64 warp[NW];
     u64 found[2];
-    int at;
+    int at, n;
+    uint4 lut[256];                     // mask byte -> ones where it allows (bf16 pairs)
+    uint32_t key[LIST];                 // candidates: order of the value, token, weight
+    uint32_t token[LIST];
+    u64 weight[LIST];
 };
-
-__device__ __forceinline__ u64 warp_sum(u64 v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    return v;
-}
 
 // Sum over the block's threads of v before this thread; *total: over all of them.
 __device__ __forceinline__ u64 block_before(Shared& s, u64 v, u64* total) {
@@ -113,6 +195,7 @@ __device__ __forceinline__ u64 block_before(Shared& s, u64 v, u64* total) {
     if (lane == 31) s.warp[warp] = in;
     __syncthreads();
     u64 before = 0, all = 0;
+#pragma unroll
     for (int w = 0; w < NW; w++) {
         if (w < warp) before += s.warp[w];
         all += s.warp[w];
@@ -121,18 +204,19 @@ __device__ __forceinline__ u64 block_before(Shared& s, u64 v, u64* total) {
     return before + in - v;
 }
 
-// One digit of a search from the largest value down: the cluster's histogram of
-// the tokens whose order starts with `prefix`, then the first digit, from the top,
-// at which the running sum reaches `need`.  Returns the digit; need becomes what is
-// left to reach inside it.
+// One digit of a search from the largest key down: the histogram of the keys that start
+// with the digits found so far (over the cluster, or this block's alone), then the first
+// digit, from the top, at which the running sum reaches `need`.  Returns the digit; need
+// becomes what is left to reach inside it.
 template <bool MASS>
-__device__ int pick_digit(cg::cluster_group& cl, Shared& s, int buf, u64* need) {
-    cl.sync();                              // every block's histogram is whole
+__device__ int pick_digit(cg::cluster_group& cl, int n_blocks, Shared& s, int buf, u64* need) {
+    if (n_blocks > 1) cl.sync();            // every block's histogram is whole
+    else __syncthreads();
     u64 v = 0;
     const int bin = 255 - (int)threadIdx.x;
     if (threadIdx.x < 256) {
-        for (unsigned r = 0; r < cl.num_blocks(); r++) {
-            const Shared* p = cl.map_shared_rank(&s, r);
+        for (int r = 0; r < n_blocks; r++) {
+            const Shared* p = n_blocks > 1 ? cl.map_shared_rank(&s, r) : &s;
             v += MASS ? ((u64)p->hi[buf][bin] << 32) + p->cnt[buf][bin] : (u64)p->cnt[buf][bin];
         }
     }
@@ -146,6 +230,40 @@ __device__ int pick_digit(cg::cluster_group& cl, Shared& s, int buf, u64* need) 
     *need = s.found[0];
     return s.at;
 }
+template <bool MASS>
+__device__ __forceinline__ void count_in(Shared& s, int buf, int bin, u64 w) {
+    if (!MASS) {
+        atomicAdd(&s.cnt[buf][bin], 1u);
+    } else {
+        const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.cnt[buf][bin], lo);
+        const uint32_t up = (uint32_t)(w >> 32) + (old + lo < old);
+        if (up) atomicAdd(&s.hi[buf][bin], up);
+    }
+}
+
+// floor(total * u24 / 2^24)
+__device__ __forceinline__ u64 part_of(u64 total, u64 u24) {
+    return u24 * (total >> 24) + ((u24 * (total & 0xffffff)) >> 24);
+}
+
+// The search among the block's n listed candidates, by value (TOKEN false: the largest
+// first) or by token (the lowest first), of those for which `in` holds.
+template <bool MASS, bool TOKEN, typename In>
+__device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 need, In&& in) {
+    uint32_t prefix = 0;
+    for (int shift = TOKEN ? 16 : 24; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += NT) s.cnt[0][i] = s.hi[0][i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += NT) {
+            const uint32_t k = TOKEN ? ~s.token[i] & 0xffffff : s.key[i];
+            if (!in(i) || (shift < (TOKEN ? 16 : 24) && (k >> (shift + 8)) != prefix)) continue;
+            count_in<MASS>(s, 0, (k >> shift) & 255, MASS ? s.weight[i] : 1);
+        }
+        prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, 1, s, 0, &need);
+        __syncthreads();
+    }
+    return TOKEN ? ~prefix & 0xffffff : prefix;
+}
 
 struct Settings {
     const float* uniform;
@@ -156,25 +274,47 @@ struct Settings {
 };
 
 // A cluster of blocks per row, each with a contiguous part of the vocabulary.
+//
+// Pass 1 (from memory) finds the largest candidate and the maxima of a few thousand groups
+// of tokens.  At least k tokens lie at or above the k-th largest of those maxima, and not
+// many more: pass 2 (from L2) lists them, and top-k, top-p and the draw are searches in
+// that list by the cluster's first block.  Without top-k, pass 2 also sums all weights,
+// and a nucleus is sought among the tokens at or above the NUCLEUS_GROUPS-th maximum.
+// Rows without top-k or top-p need no list, and rows whose list is too long, or too
+// short to hold the nucleus, are searched in whole, digit by digit.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(NT) k_sample(const T* logits, int64_t stride, int V, int per_block,
-                                               const uint32_t* bitmask, int W, Settings S, int32_t* tokens,
-                                               float* logprobs) {
-    extern __shared__ u64 chunk_sum[];
-    __shared__ Shared s;
+__global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t stride, int V, int per_block,
+                                                  const uint32_t* bitmask, int W, Settings S, int32_t* tokens,
+                                                  float* logprobs) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    Shared& s = *reinterpret_cast<Shared*>(dyn);
+    u64* chunk_sum = reinterpret_cast<u64*>(dyn + sizeof(Shared));
     cg::cluster_group cl = cg::this_cluster();
     const int rank = (int)cl.block_rank(), n_blocks = (int)cl.num_blocks();
     const int b = blockIdx.x / n_blocks;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x < 256) {
+        auto pair = [&](int i) {
+            return ((threadIdx.x >> i) & 1) * 0x0000ffffu + ((threadIdx.x >> (i + 1)) & 1) * 0xffff0000u;
+        };
+        s.lut[threadIdx.x] = make_uint4(pair(0), pair(2), pair(4), pair(6));
+    }
+    s.bins[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.n = 0;
     dep_wait();
     dep_launch();
+    __syncthreads();
 
     Row r{logits + (size_t)b * stride, bitmask ? reinterpret_cast<const uint8_t*>(bitmask + (size_t)b * W) : nullptr, V,
           min(V, rank * per_block), min(V, (rank + 1) * per_block)};
     const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
-    float x[8];
-
-    auto combine_max = [&](u64 v, int slot) {   // over the cluster
+    auto sync = [&]() {
+        if (n_blocks > 1) cl.sync();
+        else __syncthreads();
+    };
+    auto peer = [&](int q) -> const Shared* { return n_blocks > 1 ? cl.map_shared_rank(&s, q) : &s; };
+    // the largest v over the cluster
+    auto combine_max = [&](u64 v, int slot) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) v = max(v, __shfl_xor_sync(FULL, v, o));
         if (lane == 0) s.warp[warp] = v;
@@ -183,135 +323,225 @@ __global__ void __launch_bounds__(NT) k_sample(const T* logits, int64_t stride, 
             for (int w = 1; w < NW; w++) v = max(v, s.warp[w]);
             s.part[slot] = v;
         }
-        cl.sync();
+        sync();
         v = 0;
-        for (int q = 0; q < n_blocks; q++) v = max(v, cl.map_shared_rank(&s, q)->part[slot]);
+        for (int q = 0; q < n_blocks; q++) v = max(v, peer(q)->part[slot]);
         return v;
     };
-
-    // the largest candidate
-    float mx = NEG_INF;
-    for (int c = warp; c < n_chunks; c += NW) {
-        load8<T, VEC>(r, r.lo + c * CHUNK + lane * 8, x);
-#pragma unroll
-        for (int i = 0; i < 8; i++) mx = fmaxf(mx, x[i]);
-    }
-    const float m = unordered((uint32_t)combine_max(ordered(mx), 0));
-    if (m == NEG_INF) {                         // nothing to choose from
-        if (rank == 0 && threadIdx.x == 0) {
-            tokens[b] = -1;
-            if (logprobs) logprobs[b] = NEG_INF;
+    // sum of v over the cluster, and over the blocks before this one
+    auto combine_sum = [&](u64 v, int slot, u64* lower) {
+        u64 total;
+        block_before(s, v, &total);
+        if (threadIdx.x == 0) s.part[slot] = total;
+        sync();
+        u64 sum = 0;
+        *lower = 0;
+        for (int q = 0; q < n_blocks; q++) {
+            const u64 w = peer(q)->part[slot];
+            if (q < rank) *lower += w;
+            sum += w;
         }
-        cl.sync();
+        return sum;
+    };
+    auto finish = [&](int token, float lp) {
+        tokens[b] = token;
+        if (logprobs) logprobs[b] = lp;
+    };
+
+    // pass 1
+    float group[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; u++) group[u] = NEG_INF;
+    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& p, int, int, int u, bool) { group[u] = fmaxf(group[u], p.max8()); });
+    uint32_t top = 0, low = 0;              // low: ~order, so that the largest is the lowest maximum
+#pragma unroll
+    for (int u = 0; u < UNROLL; u++) {
+        group[u] = clean(group[u]);
+        top = max(top, ordered(group[u]));
+        if (group[u] > NEG_INF) low = max(low, ~ordered(group[u]));
+    }
+    const uint32_t top_all = (uint32_t)combine_max(top, 0);
+    const float m = unordered(top_all);
+    if (m == NEG_INF) {                     // nothing to choose from
+        if (rank == 0 && threadIdx.x == 0) finish(-1, NEG_INF);
+        sync();
         return;
     }
     const float temp = S.temperature ? S.temperature[b] : 1.f;
-    if (!(temp >= 1e-6f)) {                     // greedy
-        uint32_t first = 0;                     // V - index, so that the largest is the lowest index
-        for (int c = warp; c < n_chunks; c += NW) {
-            const int v0 = r.lo + c * CHUNK + lane * 8;
-            load8<T, VEC>(r, v0, x);
+    if (!(temp >= 1e-6f)) {                 // greedy
+        uint32_t first = 0;                 // V - token, so that the largest is the lowest token
+        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& p, int v0, int, int, bool) {
+            if (!(p.max8() >= m)) return;
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                if (x[i] == m) first = max(first, (uint32_t)(V - v0 - i));
-        }
+                if (p.get(i) == m) first = max(first, (uint32_t)(V - v0 - i));
+        });
         const uint32_t all = (uint32_t)combine_max(first, 1);
-        if (rank == 0 && threadIdx.x == 0) {
-            tokens[b] = V - (int)all;
-            if (logprobs) logprobs[b] = 0.f;
-        }
-        cl.sync();
+        if (rank == 0 && threadIdx.x == 0) finish(V - (int)all, 0.f);
+        sync();                             // peers may still read this block's shared memory
         return;
     }
 
     Weigh g{m, __fdiv_rn(1.f, temp), NEG_INF, 0.f};
-    // the threshold of top_k, then of top_p, a digit at a time
-    int buf = 0;
-    auto search = [&](auto mass, u64 need, auto limit) -> float {
-        constexpr bool MASS = decltype(mass)::value;
-        uint32_t prefix = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
-            __syncthreads();
-            for (int c = warp; c < n_chunks; c += NW) {
-                load8<T, VEC>(r, r.lo + c * CHUNK + lane * 8, x);
+    const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < V ? S.top_k[b] : 0;
+    const float p = S.top_p ? S.top_p[b] : 1.f;
+    const u64 p24 = p < 1.f ? (u64)__float2ll_rn(fmaxf(p, 0.f) * 0x1p24f) : 0ull;
+    if (S.min_p && S.min_p[b] > 0.f) g.min_e = fminf(S.min_p[b], 1.f);
+    const float uf = S.uniform[b];
+    const u64 u24 = uf > 0.f ? min((u64)0xffffff, (u64)__float2ull_rz(fminf(uf, 1.f) * 0x1p24f)) : 0ull;
+    auto limit_of = [&](u64 total) { return max((u64)1, part_of(total, p24)); };
+
+    if (k || p < 1.f) {
+        // a bound that at least `want` groups reach, or no bound when there are fewer groups
+        const uint32_t low_all = (uint32_t)combine_max(low, 2);
+        const float range = m - unordered(~low_all), scale = BINS / range;
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const uint32_t k = ordered(x[i]);
-                    if (x[i] == NEG_INF || x[i] < g.tau || (shift < 24 && (k >> (shift + 8)) != prefix)) continue;
-                    const int bin = (k >> shift) & 255;
-                    if (!MASS) {
-                        atomicAdd(&s.cnt[buf][bin], 1u);
-                    } else {
-                        const u64 w = g.raw(x[i]);
-                        const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.cnt[buf][bin], lo);
-                        const uint32_t up = (uint32_t)(w >> 32) + (old + lo < old);
-                        if (up) atomicAdd(&s.hi[buf][bin], up);
-                    }
+        for (int u = 0; u < UNROLL; u++)
+            if (group[u] > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - group[u]) * scale))], 1u);
+        sync();
+        u64 v = 0, groups;
+        for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
+        const u64 before = block_before(s, v, &groups), want = k ? k : NUCLEUS_GROUPS;
+        if (groups < want) {
+            if (threadIdx.x == 0) s.at = BINS;
+        } else if (before < want && before + v >= want) {
+            s.at = threadIdx.x;
+        }
+        __syncthreads();
+        // a little below the bin's lower edge: the bins' own arithmetic is rounded
+        const float bound = s.at == BINS ? -FLT_BIG : m - (s.at + 1) * (range / BINS) * 1.001f - fabsf(m) * 0x1p-20f;
+        const float at_least = fmaxf(bound, -FLT_BIG);      // not NaN, not -inf
+        u64 total = 0;
+        // pass 2
+        WeightSum sum;
+        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int v0, int, int, bool any) {
+            if (!k && any) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum.add(g.e(q.get(i)));
+            }
+            if (!(q.max8() >= at_least)) return;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = q.get(i);
+                if (x >= at_least) {
+                    const int at = atomicAdd(&s.n, 1);
+                    if (at < LIST) s.key[at] = ordered(x), s.token[at] = v0 + i;
                 }
             }
-            if (shift == 24) need = limit(buf);
-            prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, s, buf, &need);
-            buf ^= 1;
-        }
-        return unordered(prefix);
-    };
-    // sum of the cluster's histogram
-    auto hist_total = [&](int at) {
-        cl.sync();
-        u64 v = 0;
-        if (threadIdx.x < 256)
-            for (int q = 0; q < n_blocks; q++) {
-                const Shared* p = cl.map_shared_rank(&s, q);
-                v += ((u64)p->hi[at][threadIdx.x] << 32) + p->cnt[at][threadIdx.x];
-            }
-        u64 total;
-        block_before(s, v, &total);
-        return total;
-    };
-    const int k = S.top_k ? S.top_k[b] : 0;
-    if (k > 0 && k < V) {
-        // fewer candidates than k: all stay
-        const float t = search(std::false_type{}, 0, [&](int at) { return min((u64)k, hist_total(at)); });
-        g.tau = t;
-    }
-    const float p = S.top_p ? S.top_p[b] : 1.f;
-    if (p < 1.f) {
-        const u64 p24 = (u64)__float2ll_rn(fmaxf(p, 0.f) * 0x1p24f);
-        const float t = search(std::true_type{}, 0, [&](int at) {
-            const u64 total = hist_total(at);
-            return max((u64)1, p24 * (total >> 24) + ((p24 * (total & 0xffffff)) >> 24));
         });
-        g.tau = t;
+        u64 lower;
+        if (!k) total = combine_sum(((u64)sum.hi << 20) + sum.lo, 3, &lower);
+        else sync();
+        // the first block gathers the lists; 0 where it cannot answer
+        if (rank == 0) {
+            __syncthreads();
+            int n = s.n;
+            for (int q = 1; q < n_blocks; q++) {
+                const Shared* o = peer(q);
+                const int more = o->n;
+                if (more <= LIST && n + more <= LIST)
+                    for (int i = threadIdx.x; i < more; i += NT) s.key[n + i] = o->key[i], s.token[n + i] = o->token[i];
+                n += more;
+            }
+            __syncthreads();
+            bool good = n <= LIST;
+            if (good) {
+                u64 w = 0;
+                for (int i = threadIdx.x; i < n; i += NT) w += s.weight[i] = g.raw(unordered(s.key[i]));
+                u64 listed;
+                block_before(s, w, &listed);
+                __syncthreads();
+                uint32_t tau = 0;
+                if (k && k < n) {
+                    tau = list_search<false, false>(cl, s, n, k, [&](int) { return true; });
+                    w = 0;
+                    for (int i = threadIdx.x; i < n; i += NT) w += s.key[i] >= tau ? s.weight[i] : 0ull;
+                    block_before(s, w, &listed);
+                }
+                if (p < 1.f) {
+                    const u64 limit = limit_of(k ? listed : total);
+                    good = limit <= listed;
+                    if (good)
+                        tau = list_search<true, false>(cl, s, n, limit, [&](int i) { return s.key[i] >= tau; });
+                }
+                if (good) {
+                    auto in = [&](int i) { return s.key[i] >= tau && g.e(unordered(s.key[i])) >= g.min_e; };
+                    w = 0;
+                    for (int i = threadIdx.x; i < n; i += NT) w += in(i) ? s.weight[i] : 0ull;
+                    u64 kept;
+                    block_before(s, w, &kept);
+                    const uint32_t token = list_search<true, true>(cl, s, n, part_of(kept, u24) + 1, in);
+                    for (int i = threadIdx.x; i < n; i += NT)
+                        if (s.token[i] == token)
+                            finish((int)token, g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
+                }
+            }
+            if (threadIdx.x == 0) s.part[4] = good;
+        }
+        sync();
+        if (peer(0)->part[4]) {
+            sync();
+            return;
+        }
+        // the row is searched in whole
+        int buf = 0;
+        auto search = [&](auto mass, auto limit) -> float {
+            constexpr bool MASS = decltype(mass)::value;
+            uint32_t prefix = 0;
+            u64 need = 0;
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
+                __syncthreads();
+                for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
+                    if (!any) return;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float x = q.get(i);
+                        const uint32_t key = ordered(x);
+                        if (x == NEG_INF || x < g.tau || (shift < 24 && (key >> (shift + 8)) != prefix)) continue;
+                        count_in<MASS>(s, buf, (key >> shift) & 255, MASS ? g.raw(x) : 1);
+                    }
+                });
+                if (shift == 24) need = limit(buf);
+                prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, n_blocks, s, buf, &need);
+                buf ^= 1;
+            }
+            return unordered(prefix);
+        };
+        // sum of the cluster's histogram
+        auto hist_total = [&](int at) {
+            sync();
+            u64 h = 0, all;
+            if (threadIdx.x < 256)
+                for (int q = 0; q < n_blocks; q++) h += ((u64)peer(q)->hi[at][threadIdx.x] << 32) + peer(q)->cnt[at][threadIdx.x];
+            block_before(s, h, &all);
+            return all;
+        };
+        // fewer candidates than k: all stay
+        if (k) g.tau = search(std::false_type{}, [&](int at) { return min((u64)k, hist_total(at)); });
+        if (p < 1.f) g.tau = search(std::true_type{}, [&](int at) { return limit_of(hist_total(at)); });
     }
-    if (S.min_p && S.min_p[b] > 0.f) g.min_e = fminf(S.min_p[b], 1.f);
 
     // the draw: weights by chunk, then the block, the chunk and the token that hold the target
-    u64 mine = 0;
-    for (int c = warp; c < n_chunks; c += NW) {
-        load8<T, VEC>(r, r.lo + c * CHUNK + lane * 8, x);
-        u64 w = 0;
+    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int c, int, bool any) {
+        WeightSum sum;
+        if (any) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) w += g.kept(x[i]);
-        w = warp_sum(w);
-        if (lane == 0) chunk_sum[c] = w;
-    }
+            for (int i = 0; i < 8; i++) {
+                const float x = q.get(i), e = g.e(x);
+                sum.add(x >= g.tau && e >= g.min_e ? e : 0.f);
+            }
+        }
+        const uint32_t hi = __reduce_add_sync(FULL, sum.hi), lo = __reduce_add_sync(FULL, sum.lo);
+        if (lane == 0) chunk_sum[c] = ((u64)hi << 20) + lo;
+    });
     __syncthreads();
     const int per = (n_chunks + NT - 1) / NT, c0 = min(n_chunks, (int)threadIdx.x * per), c1 = min(n_chunks, c0 + per);
+    u64 mine = 0, total, lower;
     for (int c = c0; c < c1; c++) mine += chunk_sum[c];
-    u64 total;
     u64 before = block_before(s, mine, &total);
-    if (threadIdx.x == 0) s.part[2] = total;
-    cl.sync();
-    u64 lower = 0, sum = 0;
-    for (int q = 0; q < n_blocks; q++) {
-        const u64 w = cl.map_shared_rank(&s, q)->part[2];
-        if (q < rank) lower += w;
-        sum += w;
-    }
-    const float uf = S.uniform[b];
-    const u64 u = uf > 0.f ? min((u64)0xffffff, (u64)__float2ull_rz(fminf(uf, 1.f) * 0x1p24f)) : 0ull;
-    const u64 target = u * (sum >> 24) + ((u * (sum & 0xffffff)) >> 24);
+    const u64 sum = combine_sum(mine, 5, &lower);
+    const u64 target = part_of(sum, u24);
     if (target >= lower && target < lower + total) {
         const u64 t = target - lower;
         if (t >= before && t < before + mine) {
@@ -322,40 +552,48 @@ __global__ void __launch_bounds__(NT) k_sample(const T* logits, int64_t stride, 
         }
         __syncthreads();
         if (warp == 0) {
-            const int v0 = r.lo + s.at * CHUNK + lane * 8;
-            u64 t2 = s.found[1], w = 0;
-            load8<T, VEC>(r, v0, x);
+            Row one = r;                    // the chunk alone
+            one.lo = r.lo + s.at * CHUNK;
+            one.hi = min(r.hi, one.lo + CHUNK);
+            u64 t2 = s.found[1];
+            for_pieces<T, VEC>(one, s.lut, [&](const Piece<T>& q, int v0, int, int, bool) {
+                u64 w = 0;
 #pragma unroll
-            for (int i = 0; i < 8; i++) w += g.kept(x[i]);
-            u64 in = w;
+                for (int i = 0; i < 8; i++) w += g.kept(q.get(i));
+                u64 in = w;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 y = __shfl_up_sync(FULL, in, o);
-                if (lane >= o) in += y;
-            }
-            if (t2 >= in - w && t2 < in) {
-                t2 -= in - w;
-                for (int i = 0; i < 8; i++) {
-                    const u64 wi = g.kept(x[i]);
-                    if (t2 < wi) {
-                        tokens[b] = v0 + i;
-                        if (logprobs) logprobs[b] = g.z(x[i]) - logf((float)sum * 0x1p-40f);
-                        break;
-                    }
-                    t2 -= wi;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 y = __shfl_up_sync(FULL, in, o);
+                    if (lane >= o) in += y;
                 }
-            }
+                if (t2 >= in - w && t2 < in) {
+                    t2 -= in - w;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const u64 wi = g.kept(q.get(i));
+                        if (t2 < wi) {
+                            finish(v0 + i, g.z(q.get(i)) - logf((float)sum * 0x1p-40f));
+                            break;
+                        }
+                        t2 -= wi;
+                    }
+                }
+            });
         }
     }
-    cl.sync();                                  // peers may still read this block's shared memory
+    sync();                                 // peers may still read this block's shared memory
 }
 
 template <typename T>
 psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
                   int32_t* tokens, float* logprobs, cudaStream_t cs) {
-    const int cluster = V > 524288 ? MAX_CLUSTER : 1;
+    // Enough blocks for four to an SM, each with 4096 tokens at least and 2^20 at most.
+    const int want = 4 * current_sms();
+    int cluster = 1;
+    while (cluster < MAX_CLUSTER && ((int64_t)B * cluster < want || V / cluster > 1 << 20) && V / (2 * cluster) >= 4096)
+        cluster *= 2;
     const int per = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
-    const size_t smem = (size_t)(per / CHUNK) * 8;
+    const size_t smem = sizeof(Shared) + (size_t)(per / CHUNK) * 8;
     const bool vec = is_aligned(logits, stride * sizeof(T), 16);
     return ops_launch(vec ? k_sample<T, true> : k_sample<T, false>, dim3((unsigned)B * cluster), NT, smem, cluster, cs,
                       "k_sample", logits, stride, V, per, bitmask, (V + 31) / 32, S, tokens, logprobs);
