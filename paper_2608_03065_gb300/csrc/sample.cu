@@ -27,6 +27,8 @@ constexpr int UNROLL = 4;               // chunks in flight per warp
 constexpr int LIST = 2048;              // candidates that a block holds
 constexpr int BINS = NT;                // of the histogram of the groups' maxima
 constexpr int NUCLEUS_GROUPS = 640;     // maxima above the bound from which a nucleus is looked for
+constexpr int PAIRS = 256;              // candidates that are compared pair by pair
+constexpr float Z_END = -29.f;          // below it a weight is 0: 2^40 e^-29 < 1/2
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_V = 1 << 22;
 constexpr float NEG_INF = -__builtin_huge_valf();
@@ -142,6 +144,44 @@ __device__ __forceinline__ void for_pieces(const Row& r, const uint4* lut, F&& f
     }
 }
 
+// Calls f(value, token) for the tokens of the thread's own groups whose maximum reaches `bound`.
+template <typename T, bool VEC, typename F>
+__device__ __forceinline__ void for_groups(const Row& r, const uint4* lut, const float (&group)[UNROLL], float bound,
+                                           F&& f) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
+    for (int u = 0; u < UNROLL; u++) {
+        float top = group[0];
+#pragma unroll
+        for (int j = 1; j < UNROLL; j++) top = u == j ? group[j] : top;
+        if (!(top >= bound)) continue;
+#pragma unroll 4
+        for (int c = warp + u * NW; c < n_chunks; c += UNROLL * NW) {
+            const int v0 = r.lo + c * CHUNK + lane * 8, n = r.hi - v0;
+            uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
+            if (n > 0 && n < 8) bits &= (1u << n) - 1;
+            if (!bits) continue;
+            const T* at = static_cast<const T*>(r.logits) + v0;
+            Piece<T> p;
+            if (VEC && n >= 8) {
+                p.read(at);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    if ((bits >> i) & 1) p.set(i, at + i);
+            }
+            if constexpr (sizeof(T) == 2) p.keep(lut[bits]);
+            else p.keep(bits);
+            if (!(p.max8() >= bound)) continue;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = p.get(i);
+                if (x >= bound) f(x, v0 + i);
+            }
+        }
+    }
+}
+
 // What a row's weights are computed from; the arithmetic is the header's, step by step.
 struct Weigh {
     float m, inv, tau, min_e;
@@ -155,27 +195,29 @@ struct Weigh {
         return x >= tau && y >= min_e ? __float2ull_rn(y * 0x1p40f) : 0ull;
     }
 };
-// A sum of weights as two 32-bit sums: with t = 2^20 e, its whole part and its fraction in
-// units of 2^-20, each taken from the low bits of a sum with 2^23 (rounded down, then to
-// nearest even; together rint(2^40 e), since the whole part is an even number of units).
-// Good for 2048 weights.
+// A sum of weights as two 32-bit sums: of 2^20 e, its whole part and its fraction in units
+// of 2^-20, each taken from the low bits of a sum with 2^23 (rounded down, then to nearest
+// even; together rint(2^40 e), since the whole part is an even number of units).  Good for
+// 2048 weights.
 struct WeightSum {
     uint32_t hi = 0, lo = 0;
-    __device__ __forceinline__ void add(float e) {
-        const float t = e * 0x1p20f, a = __fadd_rz(t, 0x1p23f);
-        const float c = __fmaf_rn(t - (a - 0x1p23f), 0x1p20f, 0x1p23f);
-        hi += __float_as_uint(a) - 0x4B000000u;
-        lo += __float_as_uint(c) - 0x4B000000u;
+    __device__ __forceinline__ void add(float e, WeightSum* also = nullptr, bool too = false) {
+        const float a = __fmaf_rz(e, 0x1p20f, 0x1p23f);
+        const float c = __fmaf_rn(__fmaf_rn(e, 0x1p20f, 0x1p23f - a), 0x1p20f, 0x1p23f);
+        const uint32_t h = __float_as_uint(a) - 0x4B000000u, l = __float_as_uint(c) - 0x4B000000u;
+        hi += h, lo += l;
+        if (also && too) also->hi += h, also->lo += l;
     }
+    __device__ __forceinline__ u64 value() const { return ((u64)hi << 20) + lo; }
 };
 
 struct Shared {
     uint32_t cnt[2][256], hi[2][256];   // a histogram's counts, or its weights as two words
-    uint32_t bins[BINS];
-    u64 part[8];                        // this block's share of what the cluster combines, a slot per use
+    uint32_t bins[BINS], bins_hi[BINS];
+    u64 part[12];                       // this block's share of what the cluster combines, a slot per use
     u64 warp[NW];
     u64 found[2];
-    int at, n;
+    int at, n, from, to;
     uint4 lut[256];                     // mask byte -> ones where it allows (bf16 pairs)
     uint32_t key[LIST];                 // candidates: order of the value, token, weight
     uint32_t token[LIST];
@@ -265,6 +307,137 @@ __device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 nee
     return TOKEN ? ~prefix & 0xffffff : prefix;
 }
 
+// The cluster's lists behind the first block's own; their length (over LIST: not gathered).
+__device__ int gather(cg::cluster_group& cl, Shared& s, int n_blocks) {
+    int n = s.n;
+    for (int q = 1; q < n_blocks; q++) {
+        const Shared* o = cl.map_shared_rank(&s, q);
+        const int more = o->n;
+        if (n + more <= LIST)
+            for (int i = threadIdx.x; i < more; i += NT) s.key[n + i] = o->key[i], s.token[n + i] = o->token[i];
+        n += more;
+    }
+    __syncthreads();
+    return n;
+}
+
+// Filters and draws among the block's n listed candidates, of which the weights sum to
+// `listed`: k (0: off), then a nucleus of `limit` (0: limit_of what top-k leaves, ~0: off),
+// then min_e.  The calling thread that holds the drawn one gets its place, others -1;
+// *kept: the weight of what stays.
+template <typename Limit>
+__device__ int settle(cg::cluster_group& cl, Shared& s, const Weigh& g, int n, int k, u64 listed, u64 limit,
+                      Limit&& limit_of, u64 u24, u64* kept) {
+    const int tid = threadIdx.x;
+    if (n <= PAIRS) {
+        // Pair by pair, `per` threads to a candidate: how many are larger, and their weight;
+        // then the weight that stays at lower tokens.
+        int per = 2;
+        while (per < 32 && 2 * per * n <= NT) per *= 2;
+        const int i = tid / per, j0 = tid & (per - 1);
+        const bool mine = i < n;
+        const uint32_t key = mine ? s.key[i] : 0, token = mine ? s.token[i] : 0;
+        u64 w = mine ? s.weight[i] : 0, over = 0;
+        int larger = 0;
+        if (mine)
+            for (int j = j0; j < n; j += per)
+                if (s.key[j] > key) larger++, over += s.weight[j];
+        for (int o = per >> 1; o; o >>= 1) {
+            larger += __shfl_xor_sync(FULL, larger, o);
+            over += __shfl_xor_sync(FULL, over, o);
+        }
+        bool stays = mine && (!k || larger < k);
+        if (!limit) {
+            block_before(s, stays && !j0 ? w : 0, &listed);
+            limit = limit_of(listed);
+        }
+        stays = stays && over < limit && g.e(unordered(key)) >= g.min_e;
+        if (!stays) w = 0;
+        __syncthreads();
+        if (mine && !j0) s.weight[i] = w;
+        block_before(s, j0 ? 0 : w, kept);      // and every weight is written
+        const u64 target = part_of(*kept, u24);
+        u64 before = 0;
+        if (mine)
+            for (int j = j0; j < n; j += per)
+                if (s.token[j] < token) before += s.weight[j];
+        for (int o = per >> 1; o; o >>= 1) before += __shfl_xor_sync(FULL, before, o);
+        return mine && !j0 && before <= target && target < before + w ? i : -1;
+    }
+    uint32_t tau = 0;
+    if (k && k < n) {
+        tau = list_search<false, false>(cl, s, n, k, [](int) { return true; });
+        u64 w = 0;
+        for (int i = tid; i < n; i += NT) w += s.key[i] >= tau ? s.weight[i] : 0ull;
+        block_before(s, w, &listed);
+    }
+    if (!limit) limit = limit_of(listed);
+    if (limit != ~0ull) {
+        const uint32_t low = tau;
+        tau = list_search<true, false>(cl, s, n, limit, [&](int i) { return s.key[i] >= low; });
+    }
+    auto in = [&](int i) { return s.key[i] >= tau && g.e(unordered(s.key[i])) >= g.min_e; };
+    u64 w = 0;
+    for (int i = tid; i < n; i += NT) w += in(i) ? s.weight[i] : 0ull;
+    block_before(s, w, kept);
+    const uint32_t token = list_search<true, true>(cl, s, n, part_of(*kept, u24) + 1, in);
+    for (int i = tid; i < n; i += NT)
+        if (s.token[i] == token) return i;
+    return -1;
+}
+
+// f(value) for the tokens of a row of one chunk, by one warp.
+template <typename T, bool VEC, typename F>
+__device__ __forceinline__ void one_chunk(const Row& r, const uint4* lut, F&& f) {
+    const int v0 = r.lo + (threadIdx.x & 31) * 8, n = r.hi - v0;
+    uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
+    if (n > 0 && n < 8) bits &= (1u << n) - 1;
+    if (!bits) return;
+    const T* at = static_cast<const T*>(r.logits) + v0;
+    for (int i = 0; i < 8; i++)
+        if ((bits >> i) & 1) f(clean(load_f32(at + i)));
+}
+
+// The search over the whole row, digit by digit of the values' order: of the candidates
+// that reach g.tau, the value at which the running count or weight from the largest
+// down reaches need_of(their sum).
+template <bool MASS, typename T, bool VEC, typename Need>
+__device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const Row& r, const Weigh& g, int n_blocks,
+                                         Need need_of) {
+    uint32_t prefix = 0;
+    u64 need = 0;
+    int buf = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
+        __syncthreads();
+        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
+            if (!any) return;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = q.get(i);
+                const uint32_t key = ordered(x);
+                if (x == NEG_INF || x < g.tau || (shift < 24 && (key >> (shift + 8)) != prefix)) continue;
+                count_in<MASS>(s, buf, (key >> shift) & 255, MASS ? g.raw(x) : 1);
+            }
+        });
+        if (shift == 24) {
+            if (n_blocks > 1) cl.sync();
+            else __syncthreads();
+            u64 h = 0, all;
+            if (threadIdx.x < 256)
+                for (int q = 0; q < n_blocks; q++) {
+                    const Shared* o = n_blocks > 1 ? cl.map_shared_rank(&s, q) : &s;
+                    h += (MASS ? (u64)o->hi[buf][threadIdx.x] << 32 : 0) + o->cnt[buf][threadIdx.x];
+                }
+            block_before(s, h, &all);
+            need = need_of(all);
+        }
+        prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, n_blocks, s, buf, &need);
+        buf ^= 1;
+    }
+    return unordered(prefix);
+}
+
 struct Settings {
     const float* uniform;
     const float* temperature;
@@ -275,13 +448,16 @@ struct Settings {
 
 // A cluster of blocks per row, each with a contiguous part of the vocabulary.
 //
-// Pass 1 (from memory) finds the largest candidate and the maxima of a few thousand groups
+// A pass from memory finds the largest candidate and the maxima of a few thousand groups
 // of tokens.  At least k tokens lie at or above the k-th largest of those maxima, and not
-// many more: pass 2 (from L2) lists them, and top-k, top-p and the draw are searches in
-// that list by the cluster's first block.  Without top-k, pass 2 also sums all weights,
-// and a nucleus is sought among the tokens at or above the NUCLEUS_GROUPS-th maximum.
-// Rows without top-k or top-p need no list, and rows whose list is too long, or too
-// short to hold the nucleus, are searched in whole, digit by digit.
+// many more; the groups that reach it are read again, their tokens listed, and top-k, top-p
+// and the draw are searches in that list by the cluster's first block.  Without top-k the
+// weights have to be summed in a second pass (from L2): the nucleus is sought in the list
+// of the tokens at or above the NUCLEUS_GROUPS-th maximum or, where a sample of the row
+// says that it ends below, in the stretch of z around the sample's estimate: its weights
+// go to bins, and the bin in which the nucleus ends is listed by a third pass.  The
+// estimate decides only what is looked at: whatever it misses is searched digit by digit
+// over the whole row.  What no list holds is drawn from sums by chunk.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t stride, int V, int per_block,
                                                   const uint32_t* bitmask, int W, Settings S, int32_t* tokens,
@@ -370,12 +546,7 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
     const float temp = S.temperature ? S.temperature[b] : 1.f;
     if (!(temp >= 1e-6f)) {                 // greedy
         uint32_t first = 0;                 // V - token, so that the largest is the lowest token
-        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& p, int v0, int, int, bool) {
-            if (!(p.max8() >= m)) return;
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (p.get(i) == m) first = max(first, (uint32_t)(V - v0 - i));
-        });
+        for_groups<T, VEC>(r, s.lut, group, m, [&](float, int v) { first = max(first, (uint32_t)(V - v)); });
         const uint32_t all = (uint32_t)combine_max(first, 1);
         if (rank == 0 && threadIdx.x == 0) finish(V - (int)all, 0.f);
         sync();                             // peers may still read this block's shared memory
@@ -385,141 +556,196 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
     Weigh g{m, __fdiv_rn(1.f, temp), NEG_INF, 0.f};
     const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < V ? S.top_k[b] : 0;
     const float p = S.top_p ? S.top_p[b] : 1.f;
-    const u64 p24 = p < 1.f ? (u64)__float2ll_rn(fmaxf(p, 0.f) * 0x1p24f) : 0ull;
+    const bool nucleus = p < 1.f;
+    const u64 p24 = nucleus ? (u64)__float2ll_rn(fmaxf(p, 0.f) * 0x1p24f) : 0ull;
     if (S.min_p && S.min_p[b] > 0.f) g.min_e = fminf(S.min_p[b], 1.f);
     const float uf = S.uniform[b];
     const u64 u24 = uf > 0.f ? min((u64)0xffffff, (u64)__float2ull_rz(fminf(uf, 1.f) * 0x1p24f)) : 0ull;
     auto limit_of = [&](u64 total) { return max((u64)1, part_of(total, p24)); };
 
-    if (k || p < 1.f) {
-        // a bound that at least `want` groups reach, or no bound when there are fewer groups
-        const uint32_t low_all = (uint32_t)combine_max(low, 2);
-        const float range = m - unordered(~low_all), scale = BINS / range;
+    if (k || nucleus || g.min_e > 0.f) {
+        float bound;
+        if (k || nucleus) {
+            // a bound that at least `want` groups reach, or no bound when there are fewer groups
+            const uint32_t low_all = (uint32_t)combine_max(low, 2);
+            const float range = m - unordered(~low_all), scale = BINS / range;
 #pragma unroll
-        for (int u = 0; u < UNROLL; u++)
-            if (group[u] > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - group[u]) * scale))], 1u);
-        sync();
-        u64 v = 0, groups;
-        for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
-        const u64 before = block_before(s, v, &groups), want = k ? k : NUCLEUS_GROUPS;
-        if (groups < want) {
-            if (threadIdx.x == 0) s.at = BINS;
-        } else if (before < want && before + v >= want) {
-            s.at = threadIdx.x;
+            for (int u = 0; u < UNROLL; u++)
+                if (group[u] > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - group[u]) * scale))], 1u);
+            sync();
+            u64 v = 0, groups;
+            for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
+            const u64 before = block_before(s, v, &groups), want = k ? k : NUCLEUS_GROUPS;
+            if (groups < want) {
+                if (threadIdx.x == 0) s.at = BINS;
+            } else if (before < want && before + v >= want) {
+                s.at = threadIdx.x;
+            }
+            __syncthreads();
+            // a little below the bin's lower edge: the bins' own arithmetic is rounded
+            bound = s.at == BINS ? -FLT_BIG : m - (s.at + 1) * (range / BINS) * 1.001f - fabsf(m) * 0x1p-20f;
+        } else {
+            // a little below the value at which e^z is min_e
+            bound = m + (logf(g.min_e) * 1.0001f - 1e-4f) * temp - fabsf(m) * 0x1p-20f;
         }
-        __syncthreads();
-        // a little below the bin's lower edge: the bins' own arithmetic is rounded
-        const float bound = s.at == BINS ? -FLT_BIG : m - (s.at + 1) * (range / BINS) * 1.001f - fabsf(m) * 0x1p-20f;
-        const float at_least = fmaxf(bound, -FLT_BIG);      // not NaN, not -inf
-        u64 total = 0;
-        // pass 2
-        WeightSum sum;
-        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int v0, int, int, bool any) {
-            if (!k && any) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) sum.add(g.e(q.get(i)));
-            }
-            if (!(q.max8() >= at_least)) return;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float x = q.get(i);
-                if (x >= at_least) {
-                    const int at = atomicAdd(&s.n, 1);
-                    if (at < LIST) s.key[at] = ordered(x), s.token[at] = v0 + i;
-                }
-            }
+        bound = fmaxf(bound, -FLT_BIG);     // not NaN, not -inf
+        for_groups<T, VEC>(r, s.lut, group, bound, [&](float x, int v) {
+            const int at = atomicAdd(&s.n, 1);
+            if (at < LIST) s.key[at] = ordered(x), s.token[at] = v;
         });
-        u64 lower;
-        if (!k) total = combine_sum(((u64)sum.hi << 20) + sum.lo, 3, &lower);
-        else sync();
-        // the first block gathers the lists; 0 where it cannot answer
-        if (rank == 0) {
-            __syncthreads();
-            int n = s.n;
-            for (int q = 1; q < n_blocks; q++) {
-                const Shared* o = peer(q);
-                const int more = o->n;
-                if (more <= LIST && n + more <= LIST)
-                    for (int i = threadIdx.x; i < more; i += NT) s.key[n + i] = o->key[i], s.token[n + i] = o->token[i];
-                n += more;
-            }
-            __syncthreads();
-            bool good = n <= LIST;
-            if (good) {
-                u64 w = 0;
-                for (int i = threadIdx.x; i < n; i += NT) w += s.weight[i] = g.raw(unordered(s.key[i]));
-                u64 listed;
-                block_before(s, w, &listed);
-                __syncthreads();
-                uint32_t tau = 0;
-                if (k && k < n) {
-                    tau = list_search<false, false>(cl, s, n, k, [&](int) { return true; });
-                    w = 0;
-                    for (int i = threadIdx.x; i < n; i += NT) w += s.key[i] >= tau ? s.weight[i] : 0ull;
-                    block_before(s, w, &listed);
-                }
-                if (p < 1.f) {
-                    const u64 limit = limit_of(k ? listed : total);
-                    good = limit <= listed;
-                    if (good)
-                        tau = list_search<true, false>(cl, s, n, limit, [&](int i) { return s.key[i] >= tau; });
-                }
-                if (good) {
-                    auto in = [&](int i) { return s.key[i] >= tau && g.e(unordered(s.key[i])) >= g.min_e; };
-                    w = 0;
-                    for (int i = threadIdx.x; i < n; i += NT) w += in(i) ? s.weight[i] : 0ull;
-                    u64 kept;
-                    block_before(s, w, &kept);
-                    const uint32_t token = list_search<true, true>(cl, s, n, part_of(kept, u24) + 1, in);
-                    for (int i = threadIdx.x; i < n; i += NT)
-                        if (s.token[i] == token)
-                            finish((int)token, g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
-                }
-            }
-            if (threadIdx.x == 0) s.part[4] = good;
-        }
         sync();
-        if (peer(0)->part[4]) {
-            sync();
-            return;
-        }
-        // the row is searched in whole
-        int buf = 0;
-        auto search = [&](auto mass, auto limit) -> float {
-            constexpr bool MASS = decltype(mass)::value;
-            uint32_t prefix = 0;
-            u64 need = 0;
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
-                __syncthreads();
-                for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
-                    if (!any) return;
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float x = q.get(i);
-                        const uint32_t key = ordered(x);
-                        if (x == NEG_INF || x < g.tau || (shift < 24 && (key >> (shift + 8)) != prefix)) continue;
-                        count_in<MASS>(s, buf, (key >> shift) & 255, MASS ? g.raw(x) : 1);
-                    }
-                });
-                if (shift == 24) need = limit(buf);
-                prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, n_blocks, s, buf, &need);
-                buf ^= 1;
+        // the first block gathers the lists and weighs what is listed
+        u64 listed = 0;
+        int n = 0;
+        if (rank == 0) {
+            n = gather(cl, s, n_blocks);
+            u64 w = 0;
+            if (n <= LIST) {
+                for (int i = threadIdx.x; i < n; i += NT) w += s.weight[i] = g.raw(unordered(s.key[i]));
+                block_before(s, w, &listed);
             }
-            return unordered(prefix);
-        };
-        // sum of the cluster's histogram
-        auto hist_total = [&](int at) {
+        }
+        if (k || !nucleus) {                // the list holds all that is needed
+            if (rank == 0) {
+                if (n <= LIST) {
+                    u64 kept;
+                    const int i = settle(cl, s, g, n, k, listed, nucleus ? 0 : ~0ull, limit_of, u24, &kept);
+                    if (i >= 0) finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
+                }
+                if (threadIdx.x == 0) s.part[4] = n <= LIST;
+            }
             sync();
-            u64 h = 0, all;
-            if (threadIdx.x < 256)
-                for (int q = 0; q < n_blocks; q++) h += ((u64)peer(q)->hi[at][threadIdx.x] << 32) + peer(q)->cnt[at][threadIdx.x];
-            block_before(s, h, &all);
-            return all;
-        };
-        // fewer candidates than k: all stay
-        if (k) g.tau = search(std::false_type{}, [&](int at) { return min((u64)k, hist_total(at)); });
-        if (p < 1.f) g.tau = search(std::true_type{}, [&](int at) { return limit_of(hist_total(at)); });
+            if (peer(0)->part[4]) {
+                sync();
+                return;
+            }
+            if (k) {                        // too many for the list: digit by digit (fewer than k candidates: all stay)
+                g.tau = row_search<false, T, VEC>(cl, s, r, g, n_blocks, [&](u64 all) { return min((u64)k, all); });
+                if (nucleus) g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
+            }
+        } else {
+            // Where the list ends and the nucleus may not, from a sample of the row: the
+            // weights below the bound in BINS bins of z, in units of the bound's weight / 2^16.
+            if (rank == 0 && threadIdx.x == 0) s.part[4] = n <= LIST ? listed : 0;
+            s.bins[threadIdx.x] = 0;
+            sync();
+            const u64 in_list = peer(0)->part[4];
+            const float unit = 65536.f / fmaxf(g.e(bound), 1e-37f), top_z = fmaxf(g.z(bound), Z_END + 1.f);
+            const float to_bin = BINS / (top_z - Z_END);
+            const int n_sample = min(n_chunks, UNROLL * NW);
+            for (int j = warp; j < n_sample; j += NW) {
+                Row one = r;
+                one.lo = r.lo + (int)((int64_t)j * n_chunks / n_sample) * CHUNK;
+                one.hi = min(r.hi, one.lo + CHUNK);
+                one_chunk<T, VEC>(one, s.lut, [&](float x) {
+                    if (x >= bound) return;
+                    const float z = g.z(x);
+                    if (z > Z_END)
+                        atomicAdd(&s.bins[min(BINS - 1, (int)((top_z - z) * to_bin))],
+                                  (uint32_t)fminf(g.e(x) * unit, 65536.f));
+                });
+            }
+            sync();
+            u64 v = 0, rest;
+            for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
+            const u64 upto = block_before(s, v, &rest) + v;
+            // sample units -> weights; the same in all blocks, also where the last one's part is short
+            const int full = per_block / CHUNK;
+            const float ratio = (float)full / min(full, UNROLL * NW) * 0x1p40f / unit;
+            const float est = (float)rest * ratio, need = p * ((float)in_list + est) - (float)in_list;
+            const float slack = 0.04f * est + 0.002f * (float)in_list;
+            const bool in_doubt = need + slack > 0.f;
+            // the stretch of z in which the nucleus ends, to be looked at closely
+            if (threadIdx.x == 0) s.from = 0, s.to = BINS;
+            __syncthreads();
+            const float mine = (float)upto * ratio, prior = (float)(upto - v) * ratio;
+            if (mine >= need - slack && prior < need - slack) s.from = threadIdx.x;
+            if (mine >= need + slack && prior < need + slack) s.to = threadIdx.x + 1;
+            __syncthreads();
+            const float z_from = !in_doubt || s.from == 0 ? 1.f : top_z - s.from / to_bin;
+            const float z_to = !in_doubt ? 1.f : s.to >= BINS ? Z_END : top_z - s.to / to_bin;
+            const float fine_top = fminf(z_from, 0.f), fine = BINS / fmaxf(fine_top - z_to, 1e-3f);
+            auto fine_bin = [&](float z) { return min(BINS - 1, (int)((fine_top - z) * fine)); };
+            sync();                         // every block has read the bins
+            s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+            __syncthreads();
+            // all weights; those above the stretch; those inside it by bins
+            WeightSum all, above;
+            for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
+                if (!any) return;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float z = g.z(q.get(i)), e = expf(z);
+                    all.add(e, &above, z >= z_from);
+                    if (z >= z_to && z < z_from) {
+                        const uint64_t w = __float2ull_rn(e * 0x1p40f);
+                        const int at = fine_bin(z);
+                        const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.bins[at], lo);
+                        const uint32_t up = (uint32_t)(w >> 32) + (old + lo < old);
+                        if (up) atomicAdd(&s.bins_hi[at], up);
+                    }
+                }
+            });
+            u64 lower;
+            const u64 total = combine_sum(all.value(), 5, &lower), limit = limit_of(total);
+            if (!in_doubt) {                // expected inside the list
+                if (rank == 0) {
+                    const bool good = n <= LIST && limit <= listed;
+                    if (good) {
+                        u64 kept;
+                        const int i = settle(cl, s, g, n, 0, listed, limit, limit_of, u24, &kept);
+                        if (i >= 0) finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
+                    }
+                    if (threadIdx.x == 0) s.part[6] = good;
+                }
+                sync();
+                if (peer(0)->part[6]) {
+                    sync();
+                    return;
+                }
+                g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
+            } else {
+                const u64 over = combine_sum(above.value(), 7, &lower);
+                u64 w = 0, inside;
+                for (int q = 0; q < n_blocks; q++)
+                    w += ((u64)peer(q)->bins_hi[threadIdx.x] << 32) + peer(q)->bins[threadIdx.x];
+                const u64 till = over + block_before(s, w, &inside);
+                const bool hit = limit > over && limit <= over + inside;
+                if (till < limit && limit <= till + w) s.at = threadIdx.x, s.found[0] = limit - till;
+                if (threadIdx.x == 0) s.n = 0;
+                __syncthreads();
+                const int bin = s.at;
+                const u64 left = s.found[0];
+                __syncthreads();
+                if (hit) {                  // the same in all blocks: the bin's tokens, and the value among them
+                    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int v0, int, int, bool any) {
+                        if (!any) return;
+#pragma unroll
+                        for (int i = 0; i < 8; i++) {
+                            const float x = q.get(i), z = g.z(x);
+                            if (z >= z_to && z < z_from && fine_bin(z) == bin) {
+                                const int at = atomicAdd(&s.n, 1);
+                                if (at < LIST) s.key[at] = ordered(x), s.token[at] = v0 + i;
+                            }
+                        }
+                    });
+                }
+                sync();
+                if (rank == 0) {
+                    uint32_t tau = 0;
+                    if (hit && (n = gather(cl, s, n_blocks)) <= LIST) {
+                        for (int i = threadIdx.x; i < n; i += NT) s.weight[i] = g.raw(unordered(s.key[i]));
+                        __syncthreads();
+                        tau = list_search<true, false>(cl, s, n, left, [](int) { return true; });
+                    }
+                    if (threadIdx.x == 0) s.part[8] = tau;
+                }
+                sync();
+                const uint32_t tau = (uint32_t)peer(0)->part[8];
+                if (tau) g.tau = unordered(tau);
+                else g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
+            }
+        }
     }
 
     // the draw: weights by chunk, then the block, the chunk and the token that hold the target
@@ -540,7 +766,7 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
     u64 mine = 0, total, lower;
     for (int c = c0; c < c1; c++) mine += chunk_sum[c];
     u64 before = block_before(s, mine, &total);
-    const u64 sum = combine_sum(mine, 5, &lower);
+    const u64 sum = combine_sum(mine, 9, &lower);
     const u64 target = part_of(sum, u24);
     if (target >= lower && target < lower + total) {
         const u64 t = target - lower;
