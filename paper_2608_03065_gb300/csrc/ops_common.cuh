@@ -49,6 +49,10 @@ psc_status ops_launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t sme
             cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), what);
         if (s != PSC_OK) return s;
     }
+    if (cluster > 8) {
+        psc_status s = ops_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), what);
+        if (s != PSC_OK) return s;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(block);

@@ -22,12 +22,13 @@ namespace {
 
 constexpr int NT = 512;                 // threads of a block
 constexpr int NW = NT / 32;
-constexpr int CHUNK = 256;              // tokens a warp takes at a time: a piece of 8 neighbours a lane
-constexpr int UNROLL = 4;               // chunks in flight per warp
+constexpr int PIECES = 4;               // pieces of 8 neighbouring tokens that a lane has in flight
+constexpr int CHUNK = PIECES * 256;     // tokens a warp takes at a time
 constexpr int LIST = 2048;              // candidates that a block holds
 constexpr int BINS = NT;                // of the histogram of the groups' maxima
 constexpr int NUCLEUS_GROUPS = 640;     // maxima above the bound from which a nucleus is looked for
-constexpr int PAIRS = 256;              // candidates that are compared pair by pair
+constexpr int PAIRS = 256;              // candidates that are compared pair by pair; more go to bins
+constexpr int FEW = 256;                // candidates of one bin that are
 constexpr float Z_END = -29.f;          // below it a weight is 0: 2^40 e^-29 < 1/2
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_V = 1 << 22;
@@ -79,9 +80,18 @@ struct Piece<__nv_bfloat16> {
         const __nv_bfloat162 a = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
         return fmaxf(__low2float(a), __high2float(a));
     }
-    __device__ __forceinline__ float get(int i) const {
-        return clean(__uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16));
+    __device__ __forceinline__ float max8_nan() const {         // NaN if any is
+        __nv_bfloat162 h[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+        const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        const float lo = __low2float(a), hi = __high2float(a);
+        return lo > hi ? lo : lo <= hi ? hi : lo + hi;
     }
+    __device__ __forceinline__ float raw(int i) const {
+        return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+    __device__ __forceinline__ float get(int i) const { return clean(raw(i)); }
 };
 template <>
 struct Piece<float> {
@@ -101,85 +111,141 @@ struct Piece<float> {
         for (int i = 2; i < 8; i++) m = fmaxf(m, x[i]);
         return m;
     }
+    __device__ __forceinline__ float max8_nan() const {
+        float m = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; i++) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(x[i]));
+        return m;
+    }
+    __device__ __forceinline__ float raw(int i) const { return x[i]; }
     __device__ __forceinline__ float get(int i) const { return clean(x[i]); }
 };
 
-// Calls f(piece, first token, chunk, u, any) for every piece of the block's part of the
-// row, UNROLL chunks in flight per warp (u: which of them).
-// Whole warps call it; `any` is false where a lane's piece holds nothing.
-template <typename T, bool VEC, typename F>
-__device__ __forceinline__ void for_pieces(const Row& r, const uint4* lut, F&& f) {
+// The lane's piece that starts at v0 (nothing read where no token of it is allowed).
+template <typename T, bool VEC>
+__device__ __forceinline__ uint32_t piece_bits(const Row& r, int v0) {
+    const int n = r.hi - v0;
+    uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
+    if (n > 0 && n < 8) bits &= (1u << n) - 1;
+    return bits;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void read_piece(const Row& r, int v0, uint32_t bits, Piece<T>& p) {
+    if (!bits) return;
+    const T* at = static_cast<const T*>(r.logits) + v0;
+    if (VEC && r.hi - v0 >= 8) {
+        p.read(at);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if ((bits >> i) & 1) p.set(i, at + i);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void mask_piece(const uint4* lut, uint32_t bits, Piece<T>& p) {
+    if constexpr (sizeof(T) == 2) p.keep(lut[bits]);
+    else p.keep(bits);
+}
+
+// Calls f(piece, first token, q, any) for every piece of the block's part of the row, q
+// its place in the chunk, and end(chunk) after a chunk's last, both by whole warps; `any`
+// is false where a lane's piece holds nothing.  A chunk's pieces are loaded together.  The
+// body is compiled PIECES times over if small (q a constant then), else twice: passes that
+// compute weights are long, and a row of its own runs each but once or twice.
+template <typename T, bool VEC, bool SMALL, typename F, typename End>
+__device__ __forceinline__ void for_pieces(const Row& r, const uint4* lut, F&& f, End&& end) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
-    for (int c0 = warp; c0 < n_chunks; c0 += UNROLL * NW) {
-        Piece<T> p[UNROLL];
-        uint32_t bits[UNROLL];
+    constexpr int BODIES = SMALL ? PIECES : 2;
+#pragma unroll 1
+    for (int c = warp; c < n_chunks; c += NW) {
+        const int v0 = r.lo + c * CHUNK + lane * 8;
+        Piece<T> p[PIECES];
+        uint32_t bits[PIECES];
 #pragma unroll
-        for (int u = 0; u < UNROLL; u++) {
-            const int v0 = r.lo + (c0 + u * NW) * CHUNK + lane * 8, n = r.hi - v0;
-            bits[u] = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
-            if (n > 0 && n < 8) bits[u] &= (1u << n) - 1;
-        }
+        for (int q = 0; q < PIECES; q++) bits[q] = piece_bits<T, VEC>(r, v0 + q * 256);
 #pragma unroll
-        for (int u = 0; u < UNROLL; u++) {
-            const int v0 = r.lo + (c0 + u * NW) * CHUNK + lane * 8;
-            const T* at = static_cast<const T*>(r.logits) + v0;
-            if (!bits[u]) continue;
-            if (VEC && r.hi - v0 >= 8) {
-                p[u].read(at);
-            } else {
+        for (int q = 0; q < PIECES; q++) read_piece<T, VEC>(r, v0 + q * 256, bits[q], p[q]);
+#pragma unroll 1
+        for (int q0 = 0; q0 < PIECES; q0 += BODIES) {
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if ((bits[u] >> i) & 1) p[u].set(i, at + i);
+            for (int q = 0; q < BODIES; q++) {
+                mask_piece<T>(lut, bits[q], p[q]);
+                f(p[q], v0 + (q0 + q) * 256, q0 + q, bits[q] != 0);
             }
-        }
 #pragma unroll
-        for (int u = 0; u < UNROLL; u++) {
-            const int c = c0 + u * NW;
-            if (c >= n_chunks) break;
-            if constexpr (sizeof(T) == 2) p[u].keep(lut[bits[u]]);
-            else p[u].keep(bits[u]);
-            f(p[u], r.lo + c * CHUNK + lane * 8, c, u, bits[u] != 0);
+            for (int q = 0; q + BODIES < PIECES; q++) p[q] = p[q + BODIES], bits[q] = bits[q + BODIES];
+        }
+        end(c);
+    }
+}
+
+// Calls f(value, token) for the tokens that reach `bound`, reading the groups whose maximum
+// does.  A group is a lane's q-th piece of every chunk of its warp; the warp's lanes share
+// out the pieces of its groups.
+template <typename T, bool VEC, typename F>
+__device__ __forceinline__ void for_groups(const Row& r, const uint4* lut, const float (&group)[PIECES], float bound,
+                                           F&& f) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
+    const int pieces = (n_chunks - warp + NW - 1) / NW;     // of a group of the warp
+    uint32_t hits[PIECES];
+    int n_hits = 0;
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) {
+        hits[q] = __ballot_sync(FULL, group[q] >= bound);
+        n_hits += __popc(hits[q]);
+    }
+    const int jobs = n_hits * pieces;       // job i: piece i % pieces of the i / pieces-th group
+#pragma unroll 2
+    for (int i = lane; i < jobs; i += 32) {
+        int h = i / pieces, q = 0;
+        const int j = i - h * pieces;
+        uint32_t left = hits[0];
+#pragma unroll
+        for (int o = 0; o < PIECES - 1; o++)
+            if (q == o && h >= __popc(left)) h -= __popc(left), q = o + 1, left = hits[o + 1];
+        for (; h; h--) left &= left - 1;
+        const int v0 = r.lo + (warp + j * NW) * CHUNK + q * 256 + (__ffs(left) - 1) * 8;
+        const uint32_t bits = piece_bits<T, VEC>(r, v0);
+        if (!bits) continue;
+        Piece<T> p;
+        read_piece<T, VEC>(r, v0, bits, p);
+        mask_piece<T>(lut, bits, p);
+        if (!(p.max8() >= bound)) continue;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const float x = p.get(e);
+            if (x >= bound) f(x, v0 + e);
         }
     }
 }
 
-// Calls f(value, token) for the tokens of the thread's own groups whose maximum reaches `bound`.
-template <typename T, bool VEC, typename F>
-__device__ __forceinline__ void for_groups(const Row& r, const uint4* lut, const float (&group)[UNROLL], float bound,
-                                           F&& f) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
-    for (int u = 0; u < UNROLL; u++) {
-        float top = group[0];
-#pragma unroll
-        for (int j = 1; j < UNROLL; j++) top = u == j ? group[j] : top;
-        if (!(top >= bound)) continue;
-#pragma unroll 4
-        for (int c = warp + u * NW; c < n_chunks; c += UNROLL * NW) {
-            const int v0 = r.lo + c * CHUNK + lane * 8, n = r.hi - v0;
-            uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
-            if (n > 0 && n < 8) bits &= (1u << n) - 1;
-            if (!bits) continue;
-            const T* at = static_cast<const T*>(r.logits) + v0;
-            Piece<T> p;
-            if (VEC && n >= 8) {
-                p.read(at);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++)
-                    if ((bits >> i) & 1) p.set(i, at + i);
-            }
-            if constexpr (sizeof(T) == 2) p.keep(lut[bits]);
-            else p.keep(bits);
-            if (!(p.max8() >= bound)) continue;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float x = p.get(i);
-                if (x >= bound) f(x, v0 + i);
-            }
-        }
+// A sum of weights as two 32-bit sums: of 2^20 e, its whole part and its fraction in units
+// of 2^-20, each taken from the low bits of a sum with 2^23 (rounded down, then to nearest
+// even; together rint(2^40 e), since the whole part is an even number of units).  Good for
+// 2048 weights.
+struct WeightSum {
+    uint32_t hi = 0, lo = 0;                // with 0x4B000000 for every weight added
+    int n = 0;
+    // e's two parts, as such bits
+    static __device__ __forceinline__ void split(float e, uint32_t* h, uint32_t* l) {
+        const float a = __fmaf_rz(e, 0x1p20f, 0x1p23f);
+        *h = __float_as_uint(a);
+        *l = __float_as_uint(__fmaf_rn(__fmaf_rn(e, 0x1p20f, 0x1p23f - a), 0x1p20f, 0x1p23f));
     }
+    static __device__ __forceinline__ u64 weight(uint32_t h, uint32_t l) {
+        return ((u64)(h - 0x4B000000u) << 20) + (l - 0x4B000000u);
+    }
+    __device__ __forceinline__ uint32_t high() const { return hi - n * 0x4B000000u; }
+    __device__ __forceinline__ uint32_t low() const { return lo - n * 0x4B000000u; }
+    __device__ __forceinline__ u64 value() const { return ((u64)high() << 20) + low(); }
+};
+// One weight, rint(2^40 e).  (The conversion instruction to 64 bits is slow here.)
+__device__ __forceinline__ u64 weight_of(float e) {
+    uint32_t h, l;
+    WeightSum::split(e, &h, &l);
+    return WeightSum::weight(h, l);
 }
 
 // What a row's weights are computed from; the arithmetic is the header's, step by step.
@@ -188,34 +254,22 @@ struct Weigh {
     __device__ __forceinline__ float z(float x) const { return __fmul_rn(__fsub_rn(x, m), inv); }
     __device__ __forceinline__ float e(float x) const { return expf(z(x)); }
     // weight of x before the filters
-    __device__ __forceinline__ u64 raw(float x) const { return __float2ull_rn(e(x) * 0x1p40f); }
+    __device__ __forceinline__ u64 raw(float x) const { return weight_of(e(x)); }
     // weight after them
     __device__ __forceinline__ u64 kept(float x) const {
         const float y = e(x);
-        return x >= tau && y >= min_e ? __float2ull_rn(y * 0x1p40f) : 0ull;
+        return x >= tau && y >= min_e ? weight_of(y) : 0ull;
     }
 };
-// A sum of weights as two 32-bit sums: of 2^20 e, its whole part and its fraction in units
-// of 2^-20, each taken from the low bits of a sum with 2^23 (rounded down, then to nearest
-// even; together rint(2^40 e), since the whole part is an even number of units).  Good for
-// 2048 weights.
-struct WeightSum {
-    uint32_t hi = 0, lo = 0;
-    __device__ __forceinline__ void add(float e, WeightSum* also = nullptr, bool too = false) {
-        const float a = __fmaf_rz(e, 0x1p20f, 0x1p23f);
-        const float c = __fmaf_rn(__fmaf_rn(e, 0x1p20f, 0x1p23f - a), 0x1p20f, 0x1p23f);
-        const uint32_t h = __float_as_uint(a) - 0x4B000000u, l = __float_as_uint(c) - 0x4B000000u;
-        hi += h, lo += l;
-        if (also && too) also->hi += h, also->lo += l;
-    }
-    __device__ __forceinline__ u64 value() const { return ((u64)hi << 20) + lo; }
-};
-
 struct Shared {
     uint32_t cnt[2][256], hi[2][256];   // a histogram's counts, or its weights as two words
-    uint32_t bins[BINS], bins_hi[BINS];
+    uint32_t bins[BINS], bins_hi[BINS], count[BINS], tau;
+    int few[FEW], n_few;
+    Row row;
+    Weigh g;
     u64 part[12];                       // this block's share of what the cluster combines, a slot per use
-    u64 warp[NW];
+    u64 warp[2][NW];                    // the warps' shares of what a block combines
+    uint8_t turn[NT];                   // which of the two a thread uses next
     u64 found[2];
     int at, n, from, to;
     uint4 lut[256];                     // mask byte -> ones where it allows (bf16 pairs)
@@ -224,7 +278,8 @@ struct Shared {
     u64 weight[LIST];
 };
 
-// Sum over the block's threads of v before this thread; *total: over all of them.
+// Sum over the block's threads of v before this thread; *total: over all of them.  One
+// barrier: successive calls use the two sets of s.warp in turn.
 __device__ __forceinline__ u64 block_before(Shared& s, u64 v, u64* total) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     u64 in = v;
@@ -233,17 +288,28 @@ __device__ __forceinline__ u64 block_before(Shared& s, u64 v, u64* total) {
         const u64 y = __shfl_up_sync(FULL, in, o);
         if (lane >= o) in += y;
     }
+    u64* w = s.warp[s.turn[threadIdx.x] ^= 1];
+    if (lane == 31) w[warp] = in;
     __syncthreads();
-    if (lane == 31) s.warp[warp] = in;
-    __syncthreads();
-    u64 before = 0, all = 0;
+    u64 t = w[lane & (NW - 1)];
 #pragma unroll
-    for (int w = 0; w < NW; w++) {
-        if (w < warp) before += s.warp[w];
-        all += s.warp[w];
+    for (int o = 1; o < NW; o <<= 1) {
+        const u64 y = __shfl_up_sync(FULL, t, o);
+        if ((lane & (NW - 1)) >= o) t += y;
     }
-    *total = all;
-    return before + in - v;
+    *total = __shfl_sync(FULL, t, NW - 1);
+    const u64 before = __shfl_sync(FULL, t, max(0, warp - 1));
+    return (warp ? before : 0) + in - v;
+}
+// The largest of two values over the block.
+__device__ __forceinline__ uint2 block_max(Shared& s, uint32_t x, uint32_t y) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    x = __reduce_max_sync(FULL, x), y = __reduce_max_sync(FULL, y);
+    u64* w = s.warp[s.turn[threadIdx.x] ^= 1];
+    if (lane == 0) w[warp] = (u64)x << 32 | y;
+    __syncthreads();
+    const u64 t = w[lane & (NW - 1)];
+    return make_uint2(__reduce_max_sync(FULL, (uint32_t)(t >> 32)), __reduce_max_sync(FULL, (uint32_t)t));
 }
 
 // One digit of a search from the largest key down: the histogram of the keys that start
@@ -283,28 +349,30 @@ __device__ __forceinline__ void count_in(Shared& s, int buf, int bin, u64 w) {
     }
 }
 
+// A sum as f32, good to a few parts in 2^24 (the conversion instruction is slow here).
+__device__ __forceinline__ float to_float(u64 v) {
+    return __uint2float_rn((uint32_t)(v >> 32)) * 0x1p32f + __uint2float_rn((uint32_t)v);
+}
 // floor(total * u24 / 2^24)
 __device__ __forceinline__ u64 part_of(u64 total, u64 u24) {
     return u24 * (total >> 24) + ((u24 * (total & 0xffffff)) >> 24);
 }
 
-// The search among the block's n listed candidates, by value (TOKEN false: the largest
-// first) or by token (the lowest first), of those for which `in` holds.
-template <bool MASS, bool TOKEN, typename In>
-__device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 need, In&& in) {
+// The value among the block's n listed candidates at which the running weight from the
+// largest down reaches `need`.
+__device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 need) {
     uint32_t prefix = 0;
-    for (int shift = TOKEN ? 16 : 24; shift >= 0; shift -= 8) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = threadIdx.x; i < 256; i += NT) s.cnt[0][i] = s.hi[0][i] = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < n; i += NT) {
-            const uint32_t k = TOKEN ? ~s.token[i] & 0xffffff : s.key[i];
-            if (!in(i) || (shift < (TOKEN ? 16 : 24) && (k >> (shift + 8)) != prefix)) continue;
-            count_in<MASS>(s, 0, (k >> shift) & 255, MASS ? s.weight[i] : 1);
+            const uint32_t k = s.key[i];
+            if (shift == 24 || (k >> (shift + 8)) == prefix) count_in<true>(s, 0, (k >> shift) & 255, s.weight[i]);
         }
-        prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, 1, s, 0, &need);
+        prefix = (prefix << 8) | (uint32_t)pick_digit<true>(cl, 1, s, 0, &need);
         __syncthreads();
     }
-    return TOKEN ? ~prefix & 0xffffff : prefix;
+    return prefix;
 }
 
 // The cluster's lists behind the first block's own; their length (over LIST: not gathered).
@@ -321,14 +389,41 @@ __device__ int gather(cg::cluster_group& cl, Shared& s, int n_blocks) {
     return n;
 }
 
+enum { FAILED = 0, DRAWN = 1, BOUNDED = 2 };    // what settle could do
+
+// Adds a weight to its bin (two words, with carry).
+__device__ __forceinline__ void add_to_bin(Shared& s, int bin, u64 w) {
+    const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.bins[bin], lo);
+    const uint32_t up = (uint32_t)(w >> 32) + (old + lo < old);
+    if (up) atomicAdd(&s.bins_hi[bin], up);
+}
+__device__ __forceinline__ u64 bin_weight(const Shared& s, int bin) {
+    return ((u64)s.bins_hi[bin] << 32) + s.bins[bin];
+}
+// The listed candidates for which `in` holds, as places in s.few; their number (over FEW: not all).
+template <typename In>
+__device__ int pick_few(Shared& s, int n, In&& in) {
+    if (threadIdx.x == 0) s.n_few = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT)
+        if (in(i)) {
+            const int at = atomicAdd(&s.n_few, 1);
+            if (at < FEW) s.few[at] = i;
+        }
+    __syncthreads();
+    return s.n_few;
+}
+
 // Filters and draws among the block's n listed candidates, of which the weights sum to
-// `listed`: k (0: off), then a nucleus of `limit` (0: limit_of what top-k leaves, ~0: off),
-// then min_e.  The calling thread that holds the drawn one gets its place, others -1;
-// *kept: the weight of what stays.
+// `listed` and none is below `bound`: k (0: off), then a nucleus of `limit` (0: limit_of what
+// top-k leaves, ~0: off), then min_e.  DRAWN: *place is the drawn one's place in the list
+// for the thread that found it, -1 for others, *kept the weight of what stays.  BOUNDED:
+// s.tau is the order of the last value that stays.
 template <typename Limit>
-__device__ int settle(cg::cluster_group& cl, Shared& s, const Weigh& g, int n, int k, u64 listed, u64 limit,
-                      Limit&& limit_of, u64 u24, u64* kept) {
+__device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V, int n, int k, u64 listed, u64 limit,
+                                   Limit limit_of, u64 u24, u64* kept, int* place) {
     const int tid = threadIdx.x;
+    *place = -1;
     if (n <= PAIRS) {
         // Pair by pair, `per` threads to a candidate: how many are larger, and their weight;
         // then the weight that stays at lower tokens.
@@ -362,40 +457,103 @@ __device__ int settle(cg::cluster_group& cl, Shared& s, const Weigh& g, int n, i
             for (int j = j0; j < n; j += per)
                 if (s.token[j] < token) before += s.weight[j];
         for (int o = per >> 1; o; o >>= 1) before += __shfl_xor_sync(FULL, before, o);
-        return mine && !j0 && before <= target && target < before + w ? i : -1;
+        if (mine && !j0 && before <= target && target < before + w) *place = i;
+        return DRAWN;
     }
+    // Counts and weights in bins of the value, then the few candidates of the bin in which
+    // a filter ends pair by pair; the same by token for the draw.
+    const float scale = BINS / (g.m - bound);
+    auto bin_of = [&](int i) { return min(BINS - 1, (int)fmaxf(0.f, (g.m - unordered(s.key[i])) * scale)); };
     uint32_t tau = 0;
-    if (k && k < n) {
-        tau = list_search<false, false>(cl, s, n, k, [](int) { return true; });
-        u64 w = 0;
-        for (int i = tid; i < n; i += NT) w += s.key[i] >= tau ? s.weight[i] : 0ull;
-        block_before(s, w, &listed);
-    }
-    if (!limit) limit = limit_of(listed);
-    if (limit != ~0ull) {
-        const uint32_t low = tau;
-        tau = list_search<true, false>(cl, s, n, limit, [&](int i) { return s.key[i] >= low; });
+    if ((k && k < n) || limit != ~0ull) {
+        __syncthreads();
+        s.bins[tid] = s.bins_hi[tid] = s.count[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += NT) {
+            const int bin = bin_of(i);
+            atomicAdd(&s.count[bin], 1u);
+            add_to_bin(s, bin, s.weight[i]);
+        }
+        __syncthreads();
+        // both sums at once: a weight below 2^51 over a count below 2^12
+        u64 all;
+        const u64 v = bin_weight(s, tid) << 12 | s.count[tid], before = block_before(s, v, &all);
+        int last = BINS;                        // the bin in which top-k ends
+        if (k && k < n) {
+            const int c = (int)(before & 4095);
+            if (c < k && k <= c + (int)(v & 4095)) s.at = tid, s.found[0] = k - c, s.found[1] = before >> 12;
+            __syncthreads();
+            last = s.at;
+            const int want = (int)s.found[0];
+            const u64 above = s.found[1];
+            const int few = pick_few(s, n, [&](int i) { return bin_of(i) == last; });
+            if (few > FEW) return FAILED;
+            if (tid == 0) s.tau = ~0u;
+            __syncthreads();
+            u64 w = 0;
+            if (tid < few) {
+                const uint32_t key = s.key[s.few[tid]];
+                int larger = 0;
+                for (int j = 0; j < few; j++) larger += s.key[s.few[j]] > key;
+                if (larger < want) {
+                    atomicMin(&s.tau, key);
+                    w = s.weight[s.few[tid]];
+                }
+            }
+            block_before(s, w, &listed);
+            listed += above;
+            tau = s.tau;
+        }
+        if (!limit) limit = limit_of(listed);
+        if (limit != ~0ull) {
+            const u64 over = before >> 12;
+            // beyond top-k's last bin nothing stays; that bin holds the limit where no earlier one does
+            const bool ends = over < limit && (tid == last || limit <= over + (v >> 12)) && tid <= last;
+            __syncthreads();
+            if (ends) s.at = tid, s.found[0] = over;
+            __syncthreads();
+            const int bin = s.at;
+            const u64 above = s.found[0];
+            const int few = pick_few(s, n, [&](int i) { return bin_of(i) == bin && s.key[i] >= tau; });
+            if (few > FEW) return FAILED;
+            if (tid == 0) s.tau = ~0u;
+            __syncthreads();
+            if (tid < few) {
+                const uint32_t key = s.key[s.few[tid]];
+                u64 w = above;
+                for (int j = 0; j < few; j++)
+                    if (s.key[s.few[j]] > key) w += s.weight[s.few[j]];
+                if (w < limit) atomicMin(&s.tau, key);
+            }
+            __syncthreads();
+            tau = s.tau;
+        }
     }
     auto in = [&](int i) { return s.key[i] >= tau && g.e(unordered(s.key[i])) >= g.min_e; };
-    u64 w = 0;
-    for (int i = tid; i < n; i += NT) w += in(i) ? s.weight[i] : 0ull;
-    block_before(s, w, kept);
-    const uint32_t token = list_search<true, true>(cl, s, n, part_of(*kept, u24) + 1, in);
+    auto part = [&](int i) { return (int)((int64_t)s.token[i] * BINS / V); };
+    __syncthreads();
+    s.bins[tid] = s.bins_hi[tid] = 0;
+    __syncthreads();
     for (int i = tid; i < n; i += NT)
-        if (s.token[i] == token) return i;
-    return -1;
-}
-
-// f(value) for the tokens of a row of one chunk, by one warp.
-template <typename T, bool VEC, typename F>
-__device__ __forceinline__ void one_chunk(const Row& r, const uint4* lut, F&& f) {
-    const int v0 = r.lo + (threadIdx.x & 31) * 8, n = r.hi - v0;
-    uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
-    if (n > 0 && n < 8) bits &= (1u << n) - 1;
-    if (!bits) return;
-    const T* at = static_cast<const T*>(r.logits) + v0;
-    for (int i = 0; i < 8; i++)
-        if ((bits >> i) & 1) f(clean(load_f32(at + i)));
+        if (in(i)) add_to_bin(s, part(i), s.weight[i]);
+    __syncthreads();
+    const u64 w = bin_weight(s, tid), before = block_before(s, w, kept), target = part_of(*kept, u24);
+    if (before <= target && target < before + w) s.at = tid, s.found[0] = target - before;
+    __syncthreads();
+    const int bin = s.at;
+    const u64 left = s.found[0];
+    const int few = pick_few(s, n, [&](int i) { return in(i) && part(i) == bin; });
+    if (tid == 0) s.tau = tau;
+    __syncthreads();
+    if (few > FEW) return BOUNDED;
+    if (tid < few) {
+        const int i = s.few[tid];
+        u64 lower = 0;
+        for (int j = 0; j < few; j++)
+            if (s.token[s.few[j]] < s.token[i]) lower += s.weight[s.few[j]];
+        if (lower <= left && left < lower + s.weight[i]) *place = i;
+    }
+    return DRAWN;
 }
 
 // The search over the whole row, digit by digit of the values' order: of the candidates
@@ -410,7 +568,7 @@ __device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
         __syncthreads();
-        for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
+        for_pieces<T, VEC, false>(r, s.lut, [&](const Piece<T>& q, int, int, bool any) {
             if (!any) return;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -419,7 +577,7 @@ __device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const
                 if (x == NEG_INF || x < g.tau || (shift < 24 && (key >> (shift + 8)) != prefix)) continue;
                 count_in<MASS>(s, buf, (key >> shift) & 255, MASS ? g.raw(x) : 1);
             }
-        });
+        }, [](int) {});
         if (shift == 24) {
             if (n_blocks > 1) cl.sync();
             else __syncthreads();
@@ -436,6 +594,162 @@ __device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const
         buf ^= 1;
     }
     return unordered(prefix);
+}
+
+// The passes over the block's part of the row, each a function of its own so that none
+// holds another's registers.  f(values, first token, any): the values cleaned if `odd`
+// (a NaN or +inf is among the block's candidates).
+template <typename T, bool VEC, typename F, typename End>
+__device__ __forceinline__ void for_values(const Shared& s, bool odd, F&& f, End&& end) {
+    for_pieces<T, VEC, false>(s.row, s.lut, [&](const Piece<T>& q, int v0, int, bool any) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = q.raw(i);
+        if (odd) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = clean(x[i]);
+        }
+        f(x, v0, any);
+    }, end);
+}
+// A chunk's sum, over the warp.
+__device__ __forceinline__ void put_chunk(u64* chunk_sum, int c, WeightSum& sum) {
+    const uint32_t hi = __reduce_add_sync(FULL, sum.high()), lo = __reduce_add_sync(FULL, sum.low());
+    if ((threadIdx.x & 31) == 0) chunk_sum[c] = ((u64)hi << 20) + lo;
+    sum = WeightSum();
+}
+
+// The sum of all weights (the thread's share).
+template <typename T, bool VEC>
+__device__ __noinline__ u64 sum_pass(const Shared& s, bool odd) {
+    const Weigh g = s.g;
+    WeightSum all;
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
+        if (!any) return;
+        all.n += 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            uint32_t h, l;
+            WeightSum::split(g.e(x[i]), &h, &l);
+            all.hi += h, all.lo += l;
+        }
+    }, [](int) {});
+    return all.value();
+}
+
+// The sums by chunk of what stays.
+template <typename T, bool VEC, bool FILTERED>
+__device__ __noinline__ void chunk_pass(const Shared& s, u64* chunk_sum, bool odd) {
+    const Weigh g = s.g;
+    WeightSum sum;
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
+        if (!any) return;
+        sum.n += 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float e = g.e(x[i]);
+            if (FILTERED) e = x[i] >= g.tau && e >= g.min_e ? e : 0.f;
+            uint32_t h, l;
+            WeightSum::split(e, &h, &l);
+            sum.hi += h, sum.lo += l;
+        }
+    }, [&](int c) { put_chunk(chunk_sum, c, sum); });
+}
+
+// A stretch of z, from z_from (excluded, above) down to z_to, in BINS bins.
+struct Stretch {
+    float z_from, z_to, top, fine;
+    __device__ __forceinline__ int bin(float z) const { return min(BINS - 1, (int)((top - z) * fine)); }
+};
+
+// All weights (the thread's share), those above the stretch (returned in *above, and by
+// chunk), and those inside it, in the block's bins.
+template <typename T, bool VEC>
+__device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, u64* above_all) {
+    const Weigh g = s.g;
+    WeightSum all, above, part;
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
+        if (!any) return;
+        all.n += 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float z = g.z(x[i]), e = expf(z);
+            uint32_t h, l;
+            WeightSum::split(e, &h, &l);
+            all.hi += h, all.lo += l;
+            if (z >= t.z_from) part.hi += h, part.lo += l, part.n++;
+            else if (z >= t.z_to) add_to_bin(s, t.bin(z), WeightSum::weight(h, l));
+        }
+    }, [&](int c) {
+        above.hi += part.hi, above.lo += part.lo, above.n += part.n;
+        put_chunk(chunk_sum, c, part);
+    });
+    *above_all = above.value();
+    return all.value();
+}
+
+// Lists the tokens of one bin of the stretch and adds those of the bins before it to the chunks' sums.
+template <typename T, bool VEC>
+__device__ __noinline__ void bin_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, int bin) {
+    const Weigh g = s.g;
+    WeightSum part;
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int v0, bool any) {
+        if (!any) return;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float z = g.z(x[i]);
+            if (!(z >= t.z_to && z < t.z_from)) continue;
+            const int in = t.bin(z);
+            if (in == bin) {
+                const int at = atomicAdd(&s.n, 1);
+                if (at < LIST) s.key[at] = ordered(x[i]), s.token[at] = v0 + i;
+            } else if (in < bin) {
+                uint32_t h, l;
+                WeightSum::split(expf(z), &h, &l);
+                part.hi += h, part.lo += l, part.n++;
+            }
+        }
+    }, [&](int c) {
+        const u64 till_now = chunk_sum[c];
+        __syncwarp();
+        put_chunk(chunk_sum, c, part);
+        if ((threadIdx.x & 31) == 0) chunk_sum[c] += till_now;
+    });
+}
+
+// Weights below the bound in bins of z, in units of `unit`: `taken` pieces of one chunk a
+// warp, the chunks spread evenly.
+template <typename T, bool VEC>
+__device__ __noinline__ void sample_pass(Shared& s, float bound, float unit, float top_z, float to_bin, int taken) {
+    const Weigh g = s.g;
+    const Row r = s.row;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK, n_sample = min(n_chunks, NW);
+    if (warp >= n_sample) return;
+    const int v0 = r.lo + (int)((int64_t)warp * n_chunks / n_sample) * CHUNK + lane * 8;
+#pragma unroll 1
+    for (int q = 0; q < taken; q++) {
+        const uint32_t bits = piece_bits<T, VEC>(r, v0 + q * 256);
+        if (!bits) continue;
+        Piece<T> one;
+        read_piece<T, VEC>(r, v0 + q * 256, bits, one);
+        mask_piece<T>(s.lut, bits, one);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float x = one.get(i), z = g.z(x);
+            if (x < bound && z > Z_END)
+                atomicAdd(&s.bins[min(BINS - 1, (int)((top_z - z) * to_bin))], (uint32_t)fminf(expf(z) * unit, 65536.f));
+        }
+    }
+}
+
+// Lists the tokens that reach the bound.
+template <typename T, bool VEC>
+__device__ __noinline__ void list_pass(Shared& s, const float (&group)[PIECES], float bound) {
+    for_groups<T, VEC>(s.row, s.lut, group, bound, [&](float x, int v) {
+        const int at = atomicAdd(&s.n, 1);
+        if (at < LIST) s.key[at] = ordered(x), s.token[at] = v;
+    });
 }
 
 struct Settings {
@@ -476,44 +790,49 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
         s.lut[threadIdx.x] = make_uint4(pair(0), pair(2), pair(4), pair(6));
     }
     s.bins[threadIdx.x] = 0;
+    s.turn[threadIdx.x] = 0;
     if (threadIdx.x == 0) s.n = 0;
     dep_wait();
     dep_launch();
     __syncthreads();
 
-    Row r{logits + (size_t)b * stride, bitmask ? reinterpret_cast<const uint8_t*>(bitmask + (size_t)b * W) : nullptr, V,
-          min(V, rank * per_block), min(V, (rank + 1) * per_block)};
+    const Row r{logits + (size_t)b * stride, bitmask ? reinterpret_cast<const uint8_t*>(bitmask + (size_t)b * W) : nullptr,
+                V, min(V, rank * per_block), min(V, (rank + 1) * per_block)};
+    if (threadIdx.x == 0) s.row = r;
     const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
     auto sync = [&]() {
         if (n_blocks > 1) cl.sync();
         else __syncthreads();
     };
     auto peer = [&](int q) -> const Shared* { return n_blocks > 1 ? cl.map_shared_rank(&s, q) : &s; };
-    // the largest v over the cluster
-    auto combine_max = [&](u64 v, int slot) {
+    // the largest of two values over the cluster
+    auto combine_max = [&](uint32_t x, uint32_t y, int slot) {
+        uint2 v = block_max(s, x, y);
+        if (n_blocks > 1) {
+            if (threadIdx.x == 0) s.part[slot] = (u64)v.x << 32 | v.y;
+            cl.sync();
 #pragma unroll
-        for (int o = 16; o; o >>= 1) v = max(v, __shfl_xor_sync(FULL, v, o));
-        if (lane == 0) s.warp[warp] = v;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < NW; w++) v = max(v, s.warp[w]);
-            s.part[slot] = v;
+            for (int q = 0; q < MAX_CLUSTER; q++)
+                if (q < n_blocks) {
+                    const u64 o = peer(q)->part[slot];
+                    v = make_uint2(max(v.x, (uint32_t)(o >> 32)), max(v.y, (uint32_t)o));
+                }
         }
-        sync();
-        v = 0;
-        for (int q = 0; q < n_blocks; q++) v = max(v, peer(q)->part[slot]);
         return v;
     };
     // sum of v over the cluster, and over the blocks before this one
     auto combine_sum = [&](u64 v, int slot, u64* lower) {
         u64 total;
         block_before(s, v, &total);
+        *lower = 0;
+        if (n_blocks == 1) return total;
         if (threadIdx.x == 0) s.part[slot] = total;
         sync();
         u64 sum = 0;
         *lower = 0;
-        for (int q = 0; q < n_blocks; q++) {
-            const u64 w = peer(q)->part[slot];
+#pragma unroll
+        for (int q = 0; q < MAX_CLUSTER; q++) {
+            const u64 w = q < n_blocks ? peer(q)->part[slot] : 0ull;
             if (q < rank) *lower += w;
             sum += w;
         }
@@ -525,19 +844,25 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
     };
 
     // pass 1
-    float group[UNROLL];
+    float group[PIECES];
 #pragma unroll
-    for (int u = 0; u < UNROLL; u++) group[u] = NEG_INF;
-    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& p, int, int, int u, bool) { group[u] = fmaxf(group[u], p.max8()); });
+    for (int u = 0; u < PIECES; u++) group[u] = NEG_INF;
+    int odd = 0;                            // a NaN or +inf among the block's candidates
+    for_pieces<T, VEC, true>(r, s.lut, [&](const Piece<T>& p, int, int q, bool) {
+        float x = p.max8_nan();
+        if (!(x <= FLT_BIG)) odd = 1, x = p.max8();
+        group[q] = fmaxf(group[q], x);
+    }, [](int) {});
+    odd = __syncthreads_or(odd);
     uint32_t top = 0, low = 0;              // low: ~order, so that the largest is the lowest maximum
 #pragma unroll
-    for (int u = 0; u < UNROLL; u++) {
+    for (int u = 0; u < PIECES; u++) {
         group[u] = clean(group[u]);
         top = max(top, ordered(group[u]));
         if (group[u] > NEG_INF) low = max(low, ~ordered(group[u]));
     }
-    const uint32_t top_all = (uint32_t)combine_max(top, 0);
-    const float m = unordered(top_all);
+    const uint2 ends = combine_max(top, low, 0);
+    const float m = unordered(ends.x);
     if (m == NEG_INF) {                     // nothing to choose from
         if (rank == 0 && threadIdx.x == 0) finish(-1, NEG_INF);
         sync();
@@ -547,34 +872,36 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
     if (!(temp >= 1e-6f)) {                 // greedy
         uint32_t first = 0;                 // V - token, so that the largest is the lowest token
         for_groups<T, VEC>(r, s.lut, group, m, [&](float, int v) { first = max(first, (uint32_t)(V - v)); });
-        const uint32_t all = (uint32_t)combine_max(first, 1);
+        const uint32_t all = combine_max(first, 0, 1).x;
         if (rank == 0 && threadIdx.x == 0) finish(V - (int)all, 0.f);
         sync();                             // peers may still read this block's shared memory
         return;
     }
 
-    Weigh g{m, __fdiv_rn(1.f, temp), NEG_INF, 0.f};
+    Weigh g{m, __fdiv_rn(1.f, temp), NEG_INF, S.min_p && S.min_p[b] > 0.f ? fminf(S.min_p[b], 1.f) : 0.f};
+    if (threadIdx.x == 0) s.g = g;          // a barrier follows before any pass reads it
     const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < V ? S.top_k[b] : 0;
     const float p = S.top_p ? S.top_p[b] : 1.f;
     const bool nucleus = p < 1.f;
-    const u64 p24 = nucleus ? (u64)__float2ll_rn(fmaxf(p, 0.f) * 0x1p24f) : 0ull;
-    if (S.min_p && S.min_p[b] > 0.f) g.min_e = fminf(S.min_p[b], 1.f);
+    const u64 p24 = nucleus ? __float2uint_rn(fmaxf(p, 0.f) * 0x1p24f) : 0u;
     const float uf = S.uniform[b];
-    const u64 u24 = uf > 0.f ? min((u64)0xffffff, (u64)__float2ull_rz(fminf(uf, 1.f) * 0x1p24f)) : 0ull;
+    const u64 u24 = uf > 0.f ? min(0xffffffu, __float2uint_rz(fminf(uf, 1.f) * 0x1p24f)) : 0u;
     auto limit_of = [&](u64 total) { return max((u64)1, part_of(total, p24)); };
 
+    bool summed = false;                    // chunk_sum holds what stays
     if (k || nucleus || g.min_e > 0.f) {
         float bound;
         if (k || nucleus) {
             // a bound that at least `want` groups reach, or no bound when there are fewer groups
-            const uint32_t low_all = (uint32_t)combine_max(low, 2);
-            const float range = m - unordered(~low_all), scale = BINS / range;
+            const float range = m - unordered(~ends.y), scale = BINS / range;
 #pragma unroll
-            for (int u = 0; u < UNROLL; u++)
+            for (int u = 0; u < PIECES; u++)
                 if (group[u] > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - group[u]) * scale))], 1u);
             sync();
             u64 v = 0, groups;
-            for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
+#pragma unroll
+            for (int q = 0; q < MAX_CLUSTER; q++)
+                if (q < n_blocks) v += peer(q)->bins[threadIdx.x];
             const u64 before = block_before(s, v, &groups), want = k ? k : NUCLEUS_GROUPS;
             if (groups < want) {
                 if (threadIdx.x == 0) s.at = BINS;
@@ -589,10 +916,7 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
             bound = m + (logf(g.min_e) * 1.0001f - 1e-4f) * temp - fabsf(m) * 0x1p-20f;
         }
         bound = fmaxf(bound, -FLT_BIG);     // not NaN, not -inf
-        for_groups<T, VEC>(r, s.lut, group, bound, [&](float x, int v) {
-            const int at = atomicAdd(&s.n, 1);
-            if (at < LIST) s.key[at] = ordered(x), s.token[at] = v;
-        });
+        list_pass<T, VEC>(s, group, bound);
         sync();
         // the first block gathers the lists and weighs what is listed
         u64 listed = 0;
@@ -607,19 +931,23 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
         }
         if (k || !nucleus) {                // the list holds all that is needed
             if (rank == 0) {
-                if (n <= LIST) {
-                    u64 kept;
-                    const int i = settle(cl, s, g, n, k, listed, nucleus ? 0 : ~0ull, limit_of, u24, &kept);
-                    if (i >= 0) finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
-                }
-                if (threadIdx.x == 0) s.part[4] = n <= LIST;
+                int done = FAILED, i = -1;
+                u64 kept;
+                if (n <= LIST)
+                    done = settle(s, g, bound, V, n, k, listed, nucleus ? 0 : ~0ull, limit_of, u24, &kept, &i);
+                if (done == DRAWN && i >= 0)
+                    finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
+                if (threadIdx.x == 0) s.part[4] = done, s.part[10] = s.tau;
             }
             sync();
-            if (peer(0)->part[4]) {
+            const int done = (int)peer(0)->part[4];
+            if (done == DRAWN) {
                 sync();
                 return;
             }
-            if (k) {                        // too many for the list: digit by digit (fewer than k candidates: all stay)
+            if (done == BOUNDED) {
+                g.tau = unordered((uint32_t)peer(0)->part[10]);
+            } else if (k) {                        // too many for the list: digit by digit (fewer than k candidates: all stay)
                 g.tau = row_search<false, T, VEC>(cl, s, r, g, n_blocks, [&](u64 all) { return min((u64)k, all); });
                 if (nucleus) g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
             }
@@ -629,138 +957,111 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
             if (rank == 0 && threadIdx.x == 0) s.part[4] = n <= LIST ? listed : 0;
             s.bins[threadIdx.x] = 0;
             sync();
-            const u64 in_list = peer(0)->part[4];
+            const float in_list = to_float(peer(0)->part[4]);
             const float unit = 65536.f / fmaxf(g.e(bound), 1e-37f), top_z = fmaxf(g.z(bound), Z_END + 1.f);
             const float to_bin = BINS / (top_z - Z_END);
-            const int n_sample = min(n_chunks, UNROLL * NW);
-            for (int j = warp; j < n_sample; j += NW) {
-                Row one = r;
-                one.lo = r.lo + (int)((int64_t)j * n_chunks / n_sample) * CHUNK;
-                one.hi = min(r.hi, one.lo + CHUNK);
-                one_chunk<T, VEC>(one, s.lut, [&](float x) {
-                    if (x >= bound) return;
-                    const float z = g.z(x);
-                    if (z > Z_END)
-                        atomicAdd(&s.bins[min(BINS - 1, (int)((top_z - z) * to_bin))],
-                                  (uint32_t)fminf(g.e(x) * unit, 65536.f));
-                });
-            }
+            const int full = per_block / CHUNK;
+            const int taken = min(PIECES, max(1, full / (2 * NW)));     // an eighth, or a piece per warp
+            sample_pass<T, VEC>(s, bound, unit, top_z, to_bin, taken);
             sync();
             u64 v = 0, rest;
-            for (int q = 0; q < n_blocks; q++) v += peer(q)->bins[threadIdx.x];
+#pragma unroll
+            for (int q = 0; q < MAX_CLUSTER; q++)
+                if (q < n_blocks) v += peer(q)->bins[threadIdx.x];
             const u64 upto = block_before(s, v, &rest) + v;
             // sample units -> weights; the same in all blocks, also where the last one's part is short
-            const int full = per_block / CHUNK;
-            const float ratio = (float)full / min(full, UNROLL * NW) * 0x1p40f / unit;
-            const float est = (float)rest * ratio, need = p * ((float)in_list + est) - (float)in_list;
-            const float slack = 0.04f * est + 0.002f * (float)in_list;
-            const bool in_doubt = need + slack > 0.f;
-            // the stretch of z in which the nucleus ends, to be looked at closely
+            const float ratio = (float)(full * PIECES) / (min(full, NW) * taken) * 0x1p40f / unit;
+            const float est = to_float(rest) * ratio, need = p * (in_list + est) - in_list;
+            const float slack = 0.03f * est + 0.002f * in_list;
             if (threadIdx.x == 0) s.from = 0, s.to = BINS;
             __syncthreads();
-            const float mine = (float)upto * ratio, prior = (float)(upto - v) * ratio;
+            const float mine = to_float(upto) * ratio, prior = to_float(upto - v) * ratio;
             if (mine >= need - slack && prior < need - slack) s.from = threadIdx.x;
             if (mine >= need + slack && prior < need + slack) s.to = threadIdx.x + 1;
-            __syncthreads();
-            const float z_from = !in_doubt || s.from == 0 ? 1.f : top_z - s.from / to_bin;
-            const float z_to = !in_doubt ? 1.f : s.to >= BINS ? Z_END : top_z - s.to / to_bin;
-            const float fine_top = fminf(z_from, 0.f), fine = BINS / fmaxf(fine_top - z_to, 1e-3f);
-            auto fine_bin = [&](float z) { return min(BINS - 1, (int)((fine_top - z) * fine)); };
-            sync();                         // every block has read the bins
-            s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
-            __syncthreads();
-            // all weights; those above the stretch; those inside it by bins
-            WeightSum all, above;
-            for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int, int, bool any) {
-                if (!any) return;
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float z = g.z(q.get(i)), e = expf(z);
-                    all.add(e, &above, z >= z_from);
-                    if (z >= z_to && z < z_from) {
-                        const uint64_t w = __float2ull_rn(e * 0x1p40f);
-                        const int at = fine_bin(z);
-                        const uint32_t lo = (uint32_t)w, old = atomicAdd(&s.bins[at], lo);
-                        const uint32_t up = (uint32_t)(w >> 32) + (old + lo < old);
-                        if (up) atomicAdd(&s.bins_hi[at], up);
-                    }
-                }
-            });
-            u64 lower;
-            const u64 total = combine_sum(all.value(), 5, &lower), limit = limit_of(total);
-            if (!in_doubt) {                // expected inside the list
+            u64 lower, total = 0, limit = 0;
+            bool found = false;
+            if (need + slack <= 0.f) {      // expected inside the list: the sum of all weights is what it wants
+                total = combine_sum(sum_pass<T, VEC>(s, odd), 5, &lower), limit = limit_of(total);
                 if (rank == 0) {
-                    const bool good = n <= LIST && limit <= listed;
-                    if (good) {
-                        u64 kept;
-                        const int i = settle(cl, s, g, n, 0, listed, limit, limit_of, u24, &kept);
-                        if (i >= 0) finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
-                    }
-                    if (threadIdx.x == 0) s.part[6] = good;
+                    int done = FAILED, i = -1;
+                    u64 kept;
+                    if (n <= LIST && limit <= listed)
+                        done = settle(s, g, bound, V, n, 0, listed, limit, limit_of, u24, &kept, &i);
+                    if (done == DRAWN && i >= 0)
+                        finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
+                    if (threadIdx.x == 0) s.part[6] = done, s.part[10] = s.tau;
                 }
                 sync();
-                if (peer(0)->part[6]) {
+                const int done = (int)peer(0)->part[6];
+                if (done == DRAWN) {
                     sync();
                     return;
                 }
-                g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
-            } else {
-                const u64 over = combine_sum(above.value(), 7, &lower);
+                if (done == BOUNDED) g.tau = unordered((uint32_t)peer(0)->part[10]), found = true;
+            }
+            // The stretch of z in which the nucleus ends, looked at closely: first the one that
+            // the sample points to, then (it has misled) all of the row.
+            for (int wide = need + slack <= 0.f; wide < 2 && !found; wide++) {
+                __syncthreads();            // s.from, s.to
+                Stretch t;
+                t.z_from = wide || s.from == 0 ? 1.f : top_z - s.from / to_bin;
+                t.z_to = wide || s.to >= BINS ? Z_END : top_z - s.to / to_bin;
+                t.top = fminf(t.z_from, 0.f), t.fine = BINS / fmaxf(t.top - t.z_to, 1e-3f);
+                sync();                     // every block has read the bins
+                s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+                __syncthreads();
+                u64 above;
+                total = combine_sum(bins_pass<T, VEC>(s, chunk_sum, odd, t, &above), 5, &lower);
+                limit = limit_of(total);
+                const u64 over = combine_sum(above, 7, &lower);
                 u64 w = 0, inside;
-                for (int q = 0; q < n_blocks; q++)
-                    w += ((u64)peer(q)->bins_hi[threadIdx.x] << 32) + peer(q)->bins[threadIdx.x];
+#pragma unroll
+                for (int q = 0; q < MAX_CLUSTER; q++)
+                    if (q < n_blocks) w += bin_weight(*peer(q), threadIdx.x);
                 const u64 till = over + block_before(s, w, &inside);
-                const bool hit = limit > over && limit <= over + inside;
                 if (till < limit && limit <= till + w) s.at = threadIdx.x, s.found[0] = limit - till;
                 if (threadIdx.x == 0) s.n = 0;
                 __syncthreads();
+                if (!(limit > over && limit <= over + inside)) continue;    // the same in all blocks
                 const int bin = s.at;
                 const u64 left = s.found[0];
-                __syncthreads();
-                if (hit) {                  // the same in all blocks: the bin's tokens, and the value among them
-                    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int v0, int, int, bool any) {
-                        if (!any) return;
-#pragma unroll
-                        for (int i = 0; i < 8; i++) {
-                            const float x = q.get(i), z = g.z(x);
-                            if (z >= z_to && z < z_from && fine_bin(z) == bin) {
-                                const int at = atomicAdd(&s.n, 1);
-                                if (at < LIST) s.key[at] = ordered(x), s.token[at] = v0 + i;
-                            }
-                        }
-                    });
-                }
+                // the bin's tokens, and the value among them at which the nucleus ends
+                bin_pass<T, VEC>(s, chunk_sum, odd, t, bin);
                 sync();
+                const int own = min(s.n, LIST);
                 if (rank == 0) {
                     uint32_t tau = 0;
-                    if (hit && (n = gather(cl, s, n_blocks)) <= LIST) {
+                    if ((n = gather(cl, s, n_blocks)) <= LIST) {
                         for (int i = threadIdx.x; i < n; i += NT) s.weight[i] = g.raw(unordered(s.key[i]));
                         __syncthreads();
-                        tau = list_search<true, false>(cl, s, n, left, [](int) { return true; });
+                        tau = list_search(cl, s, n, left);
                     }
                     if (threadIdx.x == 0) s.part[8] = tau;
                 }
                 sync();
                 const uint32_t tau = (uint32_t)peer(0)->part[8];
-                if (tau) g.tau = unordered(tau);
-                else g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
+                if (!tau) continue;         // the bin holds more than a list
+                g.tau = unordered(tau), found = true;
+                if (!(g.min_e > 0.f)) {     // the chunks' sums want only the bin's own tokens
+                    for (int i = threadIdx.x; i < own; i += NT)
+                        if (s.key[i] >= tau)
+                            atomicAdd(&chunk_sum[((int)s.token[i] - r.lo) / CHUNK], g.raw(unordered(s.key[i])));
+                    summed = true;
+                    __syncthreads();
+                }
             }
+            if (!found) g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
         }
     }
 
     // the draw: weights by chunk, then the block, the chunk and the token that hold the target
-    for_pieces<T, VEC>(r, s.lut, [&](const Piece<T>& q, int, int c, int, bool any) {
-        WeightSum sum;
-        if (any) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float x = q.get(i), e = g.e(x);
-                sum.add(x >= g.tau && e >= g.min_e ? e : 0.f);
-            }
-        }
-        const uint32_t hi = __reduce_add_sync(FULL, sum.hi), lo = __reduce_add_sync(FULL, sum.lo);
-        if (lane == 0) chunk_sum[c] = ((u64)hi << 20) + lo;
-    });
+    __syncthreads();
+    if (threadIdx.x == 0) s.g = g;          // with its threshold
+    __syncthreads();
+    if (!summed) {
+        if (g.tau > NEG_INF || g.min_e > 0.f) chunk_pass<T, VEC, true>(s, chunk_sum, odd);
+        else chunk_pass<T, VEC, false>(s, chunk_sum, odd);
+    }
     __syncthreads();
     const int per = (n_chunks + NT - 1) / NT, c0 = min(n_chunks, (int)threadIdx.x * per), c1 = min(n_chunks, c0 + per);
     u64 mine = 0, total, lower;
@@ -779,10 +1080,10 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
         __syncthreads();
         if (warp == 0) {
             Row one = r;                    // the chunk alone
-            one.lo = r.lo + s.at * CHUNK;
+            one.lo = r.lo + s.at * CHUNK;    // warp 0's first
             one.hi = min(r.hi, one.lo + CHUNK);
-            u64 t2 = s.found[1];
-            for_pieces<T, VEC>(one, s.lut, [&](const Piece<T>& q, int v0, int, int, bool) {
+            u64 left = s.found[1];
+            for_pieces<T, VEC, false>(one, s.lut, [&](const Piece<T>& q, int v0, int, bool) {
                 u64 w = 0;
 #pragma unroll
                 for (int i = 0; i < 8; i++) w += g.kept(q.get(i));
@@ -792,8 +1093,8 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
                     const u64 y = __shfl_up_sync(FULL, in, o);
                     if (lane >= o) in += y;
                 }
-                if (t2 >= in - w && t2 < in) {
-                    t2 -= in - w;
+                if (left >= in - w && left < in) {
+                    u64 t2 = left - (in - w);
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
                         const u64 wi = g.kept(q.get(i));
@@ -804,7 +1105,9 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
                         t2 -= wi;
                     }
                 }
-            });
+                const u64 all = __shfl_sync(FULL, in, 31);
+                left = left >= all ? left - all : ~0ull;    // found: no later piece
+            }, [](int) {});
         }
     }
     sync();                                 // peers may still read this block's shared memory
@@ -813,10 +1116,14 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
 template <typename T>
 psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
                   int32_t* tokens, float* logprobs, cudaStream_t cs) {
-    // Enough blocks for four to an SM, each with 4096 tokens at least and 2^20 at most.
-    const int want = 4 * current_sms();
+    // Two blocks run on an SM.  Rows are split until there are enough blocks for twice that,
+    // as long as most warps have a chunk; until the rows in flight leave half of the L2 to the
+    // later passes; and to 2^20 tokens a block (what WeightSum holds).
+    const int sms = current_sms();
     int cluster = 1;
-    while (cluster < MAX_CLUSTER && ((int64_t)B * cluster < want || V / cluster > 1 << 20) && V / (2 * cluster) >= 4096)
+    while (cluster < MAX_CLUSTER &&
+           (((int64_t)B * cluster < 4 * sms && V / (2 * cluster) >= NW * CHUNK * 3 / 4) || V / cluster > 1 << 20 ||
+            std::min<int64_t>(B, 2 * sms / cluster) * V * (int64_t)sizeof(T) > 128 << 20))
         cluster *= 2;
     const int per = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
     const size_t smem = sizeof(Shared) + (size_t)(per / CHUNK) * 8;
