@@ -197,26 +197,39 @@ __device__ __forceinline__ void for_groups(const Row& r, const uint4* lut, const
         n_hits += __popc(hits[q]);
     }
     const int jobs = n_hits * pieces;       // job i: piece i % pieces of the i / pieces-th group
-#pragma unroll 2
-    for (int i = lane; i < jobs; i += 32) {
-        int h = i / pieces, q = 0;
-        const int j = i - h * pieces;
-        uint32_t left = hits[0];
+    constexpr int BATCH = 4;                // a lane's jobs whose loads are in flight together
+    for (int i0 = lane; i0 < jobs; i0 += 32 * BATCH) {
+        int v0[BATCH];
+        uint32_t bits[BATCH];
+        Piece<T> p[BATCH];
 #pragma unroll
-        for (int o = 0; o < PIECES - 1; o++)
-            if (q == o && h >= __popc(left)) h -= __popc(left), q = o + 1, left = hits[o + 1];
-        for (; h; h--) left &= left - 1;
-        const int v0 = r.lo + (warp + j * NW) * CHUNK + q * 256 + (__ffs(left) - 1) * 8;
-        const uint32_t bits = piece_bits<T, VEC>(r, v0);
-        if (!bits) continue;
-        Piece<T> p;
-        read_piece<T, VEC>(r, v0, bits, p);
-        mask_piece<T>(lut, bits, p);
-        if (!(p.max8() >= bound)) continue;
+        for (int t = 0; t < BATCH; t++) {
+            const int i = i0 + 32 * t;
+            int h = i / pieces, q = 0;
+            const int j = i - h * pieces;
+            uint32_t left = hits[0];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            const float x = p.get(e);
-            if (x >= bound) f(x, v0 + e);
+            for (int o = 0; o < PIECES - 1; o++)
+                if (q == o && h >= __popc(left)) h -= __popc(left), q = o + 1, left = hits[o + 1];
+            bits[t] = 0;
+            if (i < jobs) {
+                for (; h; h--) left &= left - 1;
+                v0[t] = r.lo + (warp + j * NW) * CHUNK + q * 256 + (__ffs(left) - 1) * 8;
+                bits[t] = piece_bits<T, VEC>(r, v0[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < BATCH; t++)
+            if (bits[t]) read_piece<T, VEC>(r, v0[t], bits[t], p[t]);
+#pragma unroll
+        for (int t = 0; t < BATCH; t++) {
+            mask_piece<T>(lut, bits[t], p[t]);
+            if (!bits[t] || !(p[t].max8() >= bound)) continue;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float x = p[t].get(e);
+                if (x >= bound) f(x, v0[t] + e);
+            }
         }
     }
 }
@@ -358,16 +371,42 @@ __device__ __forceinline__ u64 part_of(u64 total, u64 u24) {
     return u24 * (total >> 24) + ((u24 * (total & 0xffffff)) >> 24);
 }
 
-// The value among the block's n listed candidates at which the running weight from the
-// largest down reaches `need`.
+// The value (its order) among the block's n listed candidates at which the running weight
+// from the largest down reaches `need`: few pair by pair, many digit by digit (a warp whose
+// digits are all the same adds once).
 __device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 need) {
+    if (n <= PAIRS) {
+        if (threadIdx.x == 0) s.tau = ~0u;
+        __syncthreads();
+        const int i = threadIdx.x >> 1;         // two threads to a candidate
+        u64 over = 0;
+        if (i < n)
+            for (int j = threadIdx.x & 1; j < n; j += 2)
+                if (s.key[j] > s.key[i]) over += s.weight[j];
+        over += __shfl_xor_sync(FULL, over, 1);
+        if (i < n && over < need) atomicMin(&s.tau, s.key[i]);
+        __syncthreads();
+        return s.tau;
+    }
     uint32_t prefix = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = threadIdx.x; i < 256; i += NT) s.cnt[0][i] = s.hi[0][i] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += NT) {
-            const uint32_t k = s.key[i];
-            if (shift == 24 || (k >> (shift + 8)) == prefix) count_in<true>(s, 0, (k >> shift) & 255, s.weight[i]);
+        for (int i0 = 0; i0 < n; i0 += NT) {
+            const int i = i0 + threadIdx.x;
+            const uint32_t k = i < n ? s.key[i] : 0u;
+            const bool in = i < n && (shift == 24 || (k >> (shift + 8)) == prefix);
+            const u64 w = in ? s.weight[i] : 0ull;
+            const uint32_t lanes = __ballot_sync(FULL, in);
+            if (!lanes) continue;
+            const uint32_t digit = (k >> shift) & 255, one = __shfl_sync(FULL, digit, __ffs(lanes) - 1);
+            if (__all_sync(FULL, !in || digit == one)) {
+                const uint32_t lo = __reduce_add_sync(FULL, (uint32_t)w & 0xfffff);
+                const uint32_t hi = __reduce_add_sync(FULL, (uint32_t)(w >> 20));
+                if ((threadIdx.x & 31) == 0) count_in<true>(s, 0, one, ((u64)hi << 20) + lo);
+            } else if (in) {
+                count_in<true>(s, 0, digit, w);
+            }
         }
         prefix = (prefix << 8) | (uint32_t)pick_digit<true>(cl, 1, s, 0, &need);
         __syncthreads();
@@ -375,15 +414,23 @@ __device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 nee
     return prefix;
 }
 
-// The cluster's lists behind the first block's own; their length (over LIST: not gathered).
+// The cluster's lists behind the first block's own, a warp per block; their length (over
+// LIST: not gathered).
 __device__ int gather(cg::cluster_group& cl, Shared& s, int n_blocks) {
-    int n = s.n;
-    for (int q = 1; q < n_blocks; q++) {
-        const Shared* o = cl.map_shared_rank(&s, q);
-        const int more = o->n;
-        if (n + more <= LIST)
-            for (int i = threadIdx.x; i < more; i += NT) s.key[n + i] = o->key[i], s.token[n + i] = o->token[i];
-        n += more;
+    if (n_blocks == 1) return s.n;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int own = lane < n_blocks ? (lane ? cl.map_shared_rank(&s, lane)->n : s.n) : 0;
+    int till = own;
+#pragma unroll
+    for (int o = 1; o < MAX_CLUSTER; o <<= 1) {
+        const int y = __shfl_up_sync(FULL, till, o);
+        if (lane >= o) till += y;
+    }
+    const int n = __shfl_sync(FULL, till, MAX_CLUSTER - 1);
+    if (n <= LIST && warp && warp < n_blocks) {
+        const Shared* o = cl.map_shared_rank(&s, warp);
+        const int more = __shfl_sync(FULL, own, warp), at = __shfl_sync(FULL, till, warp) - more;
+        for (int i = lane; i < more; i += 32) s.key[at + i] = o->key[i], s.token[at + i] = o->token[i];
     }
     __syncthreads();
     return n;
@@ -529,8 +576,9 @@ __device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V
             tau = s.tau;
         }
     }
-    auto in = [&](int i) { return s.key[i] >= tau && g.e(unordered(s.key[i])) >= g.min_e; };
-    auto part = [&](int i) { return (int)((int64_t)s.token[i] * BINS / V); };
+    auto in = [&](int i) { return s.key[i] >= tau && (!(g.min_e > 0.f) || g.e(unordered(s.key[i])) >= g.min_e); };
+    const float to_part = (float)BINS / V;
+    auto part = [&](int i) { return min(BINS - 1, (int)(s.token[i] * to_part)); };
     __syncthreads();
     s.bins[tid] = s.bins_hi[tid] = 0;
     __syncthreads();
@@ -688,11 +736,13 @@ __device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const
     return all.value();
 }
 
-// Lists the tokens of one bin of the stretch and adds those of the bins before it to the chunks' sums.
+// Lists the tokens of one bin of the stretch and adds those of the bins before it to the
+// chunks' sums.  The orders of the bin's smallest and largest value that the thread met: y, x.
 template <typename T, bool VEC>
-__device__ __noinline__ void bin_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, int bin) {
+__device__ __noinline__ uint2 bin_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, int bin) {
     const Weigh g = s.g;
     WeightSum part;
+    uint2 ends = make_uint2(0u, ~0u);
     for_values<T, VEC>(s, odd, [&](const float (&x)[8], int v0, bool any) {
         if (!any) return;
 #pragma unroll
@@ -701,8 +751,10 @@ __device__ __noinline__ void bin_pass(Shared& s, u64* chunk_sum, bool odd, const
             if (!(z >= t.z_to && z < t.z_from)) continue;
             const int in = t.bin(z);
             if (in == bin) {
+                const uint32_t key = ordered(x[i]);
+                ends = make_uint2(max(ends.x, key), min(ends.y, key));
                 const int at = atomicAdd(&s.n, 1);
-                if (at < LIST) s.key[at] = ordered(x[i]), s.token[at] = v0 + i;
+                if (at < LIST) s.key[at] = key, s.token[at] = v0 + i;
             } else if (in < bin) {
                 uint32_t h, l;
                 WeightSum::split(expf(z), &h, &l);
@@ -715,6 +767,7 @@ __device__ __noinline__ void bin_pass(Shared& s, u64* chunk_sum, bool odd, const
         put_chunk(chunk_sum, c, part);
         if ((threadIdx.x & 31) == 0) chunk_sum[c] += till_now;
     });
+    return ends;
 }
 
 // Weights below the bound in bins of z, in units of `unit`: `taken` pieces of one chunk a
@@ -971,16 +1024,25 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
             const u64 upto = block_before(s, v, &rest) + v;
             // sample units -> weights; the same in all blocks, also where the last one's part is short
             const float ratio = (float)(full * PIECES) / (min(full, NW) * taken) * 0x1p40f / unit;
-            const float est = to_float(rest) * ratio, need = p * (in_list + est) - in_list;
-            const float slack = 0.03f * est + 0.002f * in_list;
+            // The share of the weight below the bound that the nucleus holds: estimated well, since
+            // an error of the sample's total moves it by (1 - p) of that only.  The slack is
+            // three to four times what samples of these sizes were seen to be off.
+            const float sampled = fmaxf(to_float(rest), 1e-30f), list_to_rest = in_list / fmaxf(sampled * ratio, 1e-30f);
+            const float share = p - (1.f - p) * list_to_rest;
+            const float slack = 0.08f * fmaxf(share, 0.f) * (1.f - share) + 0.06f * (1.f - p) * list_to_rest + 5e-4f;
             if (threadIdx.x == 0) s.from = 0, s.to = BINS;
             __syncthreads();
-            const float mine = to_float(upto) * ratio, prior = to_float(upto - v) * ratio;
-            if (mine >= need - slack && prior < need - slack) s.from = threadIdx.x;
-            if (mine >= need + slack && prior < need + slack) s.to = threadIdx.x + 1;
+            const float mine = to_float(upto) / sampled, prior = to_float(upto - v) / sampled;
+            if (mine >= share - slack && prior < share - slack) s.from = threadIdx.x;
+            if (mine >= share + slack && prior < share + slack) s.to = threadIdx.x + 1;
+            __syncthreads();
+            const bool in_doubt = share + slack > 0.f;
+            // the stretch of z in which the nucleus is expected to end
+            float z_from = s.from == 0 ? 1.f : top_z - s.from / to_bin;
+            float z_to = s.to >= BINS ? Z_END : top_z - s.to / to_bin;
             u64 lower, total = 0, limit = 0;
             bool found = false;
-            if (need + slack <= 0.f) {      // expected inside the list: the sum of all weights is what it wants
+            if (!in_doubt) {                // expected inside the list: the sum of all weights is what it wants
                 total = combine_sum(sum_pass<T, VEC>(s, odd), 5, &lower), limit = limit_of(total);
                 if (rank == 0) {
                     int done = FAILED, i = -1;
@@ -998,14 +1060,13 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
                     return;
                 }
                 if (done == BOUNDED) g.tau = unordered((uint32_t)peer(0)->part[10]), found = true;
+                z_from = 1.f, z_to = Z_END;
             }
-            // The stretch of z in which the nucleus ends, looked at closely: first the one that
-            // the sample points to, then (it has misled) all of the row.
-            for (int wide = need + slack <= 0.f; wide < 2 && !found; wide++) {
-                __syncthreads();            // s.from, s.to
+            // The stretch looked at closely; where the nucleus does not end in it the whole row
+            // is, and where its bin holds more than a list that bin is the next stretch.
+            for (int turn = 0; turn < 6 && !found; turn++) {
                 Stretch t;
-                t.z_from = wide || s.from == 0 ? 1.f : top_z - s.from / to_bin;
-                t.z_to = wide || s.to >= BINS ? Z_END : top_z - s.to / to_bin;
+                t.z_from = z_from, t.z_to = z_to;
                 t.top = fminf(t.z_from, 0.f), t.fine = BINS / fmaxf(t.top - t.z_to, 1e-3f);
                 sync();                     // every block has read the bins
                 s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
@@ -1022,11 +1083,15 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
                 if (till < limit && limit <= till + w) s.at = threadIdx.x, s.found[0] = limit - till;
                 if (threadIdx.x == 0) s.n = 0;
                 __syncthreads();
-                if (!(limit > over && limit <= over + inside)) continue;    // the same in all blocks
+                if (!(limit > over && limit <= over + inside)) {            // the same in all blocks
+                    if (z_from == 1.f && z_to == Z_END) break;
+                    z_from = 1.f, z_to = Z_END;
+                    continue;
+                }
                 const int bin = s.at;
                 const u64 left = s.found[0];
                 // the bin's tokens, and the value among them at which the nucleus ends
-                bin_pass<T, VEC>(s, chunk_sum, odd, t, bin);
+                const uint2 mine = bin_pass<T, VEC>(s, chunk_sum, odd, t, bin), ends = combine_max(mine.x, ~mine.y, 11);
                 sync();
                 const int own = min(s.n, LIST);
                 if (rank == 0) {
@@ -1039,10 +1104,17 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
                     if (threadIdx.x == 0) s.part[8] = tau;
                 }
                 sync();
-                const uint32_t tau = (uint32_t)peer(0)->part[8];
-                if (!tau) continue;         // the bin holds more than a list
+                const uint32_t listed_tau = (uint32_t)peer(0)->part[8];
+                // equal values need no list
+                const uint32_t tau = listed_tau ? listed_tau : ends.x == ~ends.y ? ends.x : 0u;
+                if (!tau) {                 // the bin holds more than a list: its edges, a little apart
+                    const float off = 1e-4f / t.fine + 4e-6f * (1.f - t.top + bin / t.fine);
+                    z_from = bin ? t.top - bin / t.fine + off : t.z_from;
+                    z_to = fmaxf(t.top - (bin + 1) / t.fine - off, Z_END);
+                    continue;
+                }
                 g.tau = unordered(tau), found = true;
-                if (!(g.min_e > 0.f)) {     // the chunks' sums want only the bin's own tokens
+                if (listed_tau && !(g.min_e > 0.f)) {   // the chunks' sums want only the bin's own tokens
                     for (int i = threadIdx.x; i < own; i += NT)
                         if (s.key[i] >= tau)
                             atomicAdd(&chunk_sum[((int)s.token[i] - r.lo) / CHUNK], g.raw(unordered(s.key[i])));
@@ -1078,36 +1150,27 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t strid
             s.found[1] = t - before;
         }
         __syncthreads();
-        if (warp == 0) {
-            Row one = r;                    // the chunk alone
-            one.lo = r.lo + s.at * CHUNK;    // warp 0's first
-            one.hi = min(r.hi, one.lo + CHUNK);
-            u64 left = s.found[1];
-            for_pieces<T, VEC, false>(one, s.lut, [&](const Piece<T>& q, int v0, int, bool) {
-                u64 w = 0;
+        // a warp per piece of the chunk
+        const int v0 = r.lo + s.at * CHUNK + warp * 256 + lane * 8;
+        u64 w[8], in = 0;
+        Piece<T> q;
+        if (warp < PIECES) {
+            const uint32_t bits = piece_bits<T, VEC>(r, v0);
+            read_piece<T, VEC>(r, v0, bits, q);
+            mask_piece<T>(s.lut, bits, q);
 #pragma unroll
-                for (int i = 0; i < 8; i++) w += g.kept(q.get(i));
-                u64 in = w;
+            for (int i = 0; i < 8; i++) in += w[i] = g.kept(q.get(i));
+        }
+        u64 all;
+        u64 till = block_before(s, in, &all);
+        const u64 left = s.found[1];
+        if (left >= till && left < till + in) {
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 y = __shfl_up_sync(FULL, in, o);
-                    if (lane >= o) in += y;
-                }
-                if (left >= in - w && left < in) {
-                    u64 t2 = left - (in - w);
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const u64 wi = g.kept(q.get(i));
-                        if (t2 < wi) {
-                            finish(v0 + i, g.z(q.get(i)) - logf((float)sum * 0x1p-40f));
-                            break;
-                        }
-                        t2 -= wi;
-                    }
-                }
-                const u64 all = __shfl_sync(FULL, in, 31);
-                left = left >= all ? left - all : ~0ull;    // found: no later piece
-            }, [](int) {});
+            for (int i = 0; i < 8; i++) {
+                if (left >= till && left < till + w[i])
+                    finish(v0 + i, g.z(q.get(i)) - logf((float)sum * 0x1p-40f));
+                till += w[i];
+            }
         }
     }
     sync();                                 // peers may still read this block's shared memory
