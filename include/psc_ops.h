@@ -78,7 +78,7 @@ psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_s
  *   d_bias_ids, d_bias : int32 and float [B][n_bias] (NULL with n_bias = 0); ids outside [0, V)
  *                     are skipped, of equal ids in a row the last counts
  *   d_bitmask       : uint32 [B][ceil(V/32)], or NULL
- * PSC_ERR_LIMIT: H over 16,777,215 or n_bias over 4,096. */
+ * PSC_ERR_LIMIT: V over 2^30, H over 16,777,215 or n_bias over 4,096. */
 psc_status psc_process_logits(const void* d_logits, psc_dtype dtype, int64_t row_stride, void* d_out,
                               int64_t out_stride, int32_t B, int32_t V, const int32_t* d_history,
                               int64_t history_stride, int32_t H, const int32_t* d_history_len,

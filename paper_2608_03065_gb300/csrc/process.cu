@@ -12,6 +12,7 @@
 
 namespace {
 
+constexpr int MAX_V = 1 << 30;
 constexpr int MAX_BIAS = 4096;
 constexpr int MAX_HISTORY = (1 << 24) - 1;      // a count fits 24 bits
 constexpr uint32_t SEEN = 1u << 30;             // the token is in the prompt
@@ -19,7 +20,7 @@ constexpr uint32_t COUNT = (1u << 24) - 1;      // times in the output
 constexpr uint32_t EMPTY = 0xffffffffu;
 
 constexpr int HASH_SLOTS = 16384;               // most slots of a hashed table
-constexpr int PART = 16384;                     // tokens of the vocabulary per direct table
+constexpr int TABLE_BYTES = 192 * 1024;         // of a direct table at most
 
 template <typename T>
 struct Ninf;
@@ -105,60 +106,110 @@ struct Penalties {
 
 // The tokens that a row's history and biases name, counted in shared memory, then
 // rewritten one by one.  HASH: one block per row, an open-addressed table keyed by
-// token with at least twice as many slots as entries.  Otherwise a block per row
-// and PART tokens of the vocabulary, a table indexed by token: any history length.
-// Each table word holds the output count and the prompt bit; a second table the
-// last position among the biases, so that the order of threads does not matter.
-template <typename T, bool HASH>
-__global__ void __launch_bounds__(512) k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V,
-                                                  Penalties P, const uint32_t* bitmask, int W, int parts, int early) {
+// token with at least twice as many slots as history entries.  Otherwise, for any history
+// length, 2^shares blocks per row, each with a table indexed by token for every 2^shares-th
+// token (neighbours apart, because the frequent ones often have neighbouring ids).  A table
+// word holds the output count and the prompt bit.  The biases have a hashed table of their
+// own, of the last position of each id, so that the order of threads does not matter.
+// What takes the time is latency, not bytes: a thread loads LOADS ids, and rewrites BATCH
+// tokens, at a time.  (Measured on 20,000 ids of 151,936 tokens in 201 rows, with the copy:
+// tables of 16,384 neighbouring tokens 353 us, LOADS at a time 100 us; a table spread over a
+// cluster of 8 blocks, each id read once and counted in its owner's memory, 106 us.)
+constexpr int LOADS = 8;
+
+// The slot of token v in an open-addressed table of `cap` keys (never more than half full).
+__device__ __forceinline__ int hash_slot(uint32_t* key, int cap, int shift, uint32_t v) {
+    uint32_t i = (v * 2654435761u) >> shift;
+    for (int it = 0; it < cap; it++) {
+        const uint32_t k = atomicCAS(&key[i], EMPTY, v);
+        if (k == EMPTY || k == v) break;
+        i = (i + 1) & (cap - 1);
+    }
+    return (int)i;
+}
+// The slot that holds v, or -1.
+__device__ __forceinline__ int hash_find(const uint32_t* key, int cap, int shift, uint32_t v) {
+    uint32_t i = (v * 2654435761u) >> shift;
+    for (int it = 0; it < cap; it++) {
+        if (key[i] == v) return (int)i;
+        if (key[i] == EMPTY) break;
+        i = (i + 1) & (cap - 1);
+    }
+    return -1;
+}
+__host__ __device__ inline int hash_cap(int entries) {
+    int cap = 32;
+    while (cap < 2 * entries) cap <<= 1;
+    return cap;
+}
+
+// A direct table's words are 16 bits while no count can pass 15 (SHORT), 32 otherwise.
+enum TableKind { HASHED, SHORT, LONG };
+constexpr int SHORT_HISTORY = 32767;
+__host__ __device__ constexpr int table_threads(TableKind k) { return k == HASHED ? 512 : 1024; }
+
+template <typename T, TableKind KIND>
+__global__ void __launch_bounds__(table_threads(KIND), KIND == HASHED ? 2 : 1) k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V,
+                                                  Penalties P, const uint32_t* bitmask, int W, int shares, int early) {
+    constexpr bool HASH = KIND == HASHED;
+    constexpr int NT = table_threads(KIND);
     extern __shared__ uint32_t tab[];
     // After k_mask_copy, which began once every earlier kernel had completed, the table is
     // built while that copy still runs; otherwise the history may be an earlier kernel's.
     if (!early) dep_wait();
-    const int b = blockIdx.x / parts, v0 = (blockIdx.x - b * parts) * PART;
-    const int n_tok = HASH ? V : min(PART, V - v0);
+    const int b = HASH ? blockIdx.x : blockIdx.x >> shares, share = blockIdx.x & ((1 << shares) - 1);
+    const int places = HASH ? 0 : (V - share + (1 << shares) - 1) >> shares;
     const int len = !P.H ? 0 : P.history_len ? min(max(P.history_len[b], 0), P.H) : P.H;
     const int plen = P.prompt_len ? P.prompt_len[b] : 0;
-    int cap = n_tok, shift = 0;
-    if (HASH) {
-        const int need = 2 * (len + P.n_bias);
-        cap = 32;
-        while (cap < need) cap <<= 1;
-        shift = __clz(cap) + 1;                 // 32 - log2(cap)
-    }
-    uint32_t* cnt = tab;
-    uint32_t* pos = tab + cap;                  // used with biases only
-    uint32_t* key = HASH ? pos + (P.n_bias ? cap : 0) : nullptr;
-    for (int i = threadIdx.x; i < cap; i += blockDim.x) {
+    const int cap = HASH ? hash_cap(len) : places, shift = HASH ? __clz(cap) + 1 : 0;    // 32 - log2(cap)
+    const int bias_cap = P.n_bias ? hash_cap(P.n_bias) : 0, bias_shift = P.n_bias ? __clz(bias_cap) + 1 : 0;
+    uint32_t* bias_key = tab;
+    uint32_t* bias_pos = bias_key + bias_cap;
+    uint32_t* cnt = bias_pos + bias_cap;
+    uint32_t* key = cnt + cap;                  // HASH only
+    for (int i = threadIdx.x; i < bias_cap; i += NT) bias_key[i] = EMPTY, bias_pos[i] = 0;
+    for (int i = threadIdx.x; i < (KIND == SHORT ? (cap + 1) / 2 : cap); i += NT) {
         cnt[i] = 0;
-        if (P.n_bias) pos[i] = 0;
         if (HASH) key[i] = EMPTY;
     }
+    // a place's count and prompt bit; and nothing left of it
+    auto count_at = [&](int i) -> uint32_t {
+        if (KIND != SHORT) return cnt[i];
+        const uint32_t c = reinterpret_cast<const uint16_t*>(cnt)[i];
+        return (c & 0x7fff) | (c >> 15 ? SEEN : 0u);
+    };
+    auto clear = [&](int i) {
+        if (KIND == SHORT) reinterpret_cast<uint16_t*>(cnt)[i] = 0;
+        else cnt[i] = 0;
+    };
     __syncthreads();
 
-    auto slot_of = [&](uint32_t v) -> int {
-        if (!HASH) return (int)v - v0;
-        uint32_t i = (v * 2654435761u) >> shift;
-        for (int it = 0; it < cap; it++) {
-            const uint32_t k = atomicCAS(&key[i], EMPTY, v);
-            if (k == EMPTY || k == v) break;
-            i = (i + 1) & (cap - 1);
-        }
-        return (int)i;
-    };
     const int32_t* hist = P.history + (size_t)b * P.history_stride;
-    for (int i = threadIdx.x; i < len; i += blockDim.x) {
-        const int v = hist[i];
-        if (v < v0 || v >= v0 + n_tok) continue;
-        const int s = slot_of(v);
-        if (i < plen) atomicOr(&cnt[s], SEEN);
-        else atomicAdd(&cnt[s], 1u);
+    for (int i0 = threadIdx.x; i0 < len; i0 += LOADS * NT) {
+        int v[LOADS];
+#pragma unroll
+        for (int k = 0; k < LOADS; k++) v[k] = i0 + k * NT < len ? hist[i0 + k * NT] : -1;
+#pragma unroll
+        for (int k = 0; k < LOADS; k++) {
+            uint32_t *word, one = 1, seen = SEEN;
+            if (v[k] < 0 || v[k] >= V) continue;
+            if (HASH) {
+                word = &cnt[hash_slot(key, cap, shift, v[k])];
+            } else {
+                if ((v[k] & ((1 << shares) - 1)) != share) continue;
+                const int place = v[k] >> shares;
+                word = cnt + (KIND == SHORT ? place / 2 : place);
+                if (KIND == SHORT) one = place & 1 ? 0x10000u : 1u, seen = one << 15;
+            }
+            if (i0 + k * NT < plen) atomicOr(word, seen);
+            else atomicAdd(word, one);
+        }
     }
-    for (int j = threadIdx.x; j < P.n_bias; j += blockDim.x) {
+    for (int j = threadIdx.x; j < P.n_bias; j += NT) {
         const int v = P.bias_ids[(size_t)b * P.n_bias + j];
-        if (v < v0 || v >= v0 + n_tok) continue;
-        atomicMax(&pos[slot_of(v)], (uint32_t)j + 1);
+        if (v < 0 || v >= V) continue;
+        if (!HASH && (v & ((1 << shares) - 1)) != share) continue;
+        atomicMax(&bias_pos[hash_slot(bias_key, bias_cap, bias_shift, v)], (uint32_t)j + 1);
     }
     __syncthreads();
     if (early) dep_wait();                      // the masked copy is complete
@@ -170,16 +221,74 @@ __global__ void __launch_bounds__(512) k_penalize(const T* logits, int64_t strid
     const float rep = P.repetition ? P.repetition[b] : 1.f;
     const float freq = P.frequency ? P.frequency[b] : 0.f;
     const float pres = P.presence ? P.presence[b] : 0.f;
-    for (int i = threadIdx.x; i < cap; i += blockDim.x) {
-        const uint32_t c = cnt[i], j = P.n_bias ? pos[i] : 0u;
-        if (!c && !j) continue;
-        const int v = HASH ? (int)key[i] : v0 + i;
-        if (!allows(mask, v)) continue;
-        float y = load_f32(src + v);
-        if (c) y = y > 0.f ? y / rep : y * rep;
-        if (c & COUNT) y = y - freq * (float)(c & COUNT) - pres;
-        if (j) y += P.bias[(size_t)b * P.n_bias + j - 1];
-        store_f32(dst + v, y);
+    // a thread's tokens are fetched together (logit and mask word at once), then rewritten
+    constexpr int BATCH = 4;
+    auto rewrite = [&](int from, int n, auto&& pick, int by = table_threads(KIND)) {
+        for (int i0 = from; i0 < n; i0 += BATCH * by) {
+            int v[BATCH];
+            uint32_t c[BATCH], word[BATCH];
+            float bias[BATCH], y[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; k++) {
+                const int i = i0 + k * by;
+                v[k] = -1;
+                if (i < n) pick(i, &v[k], &c[k], &bias[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; k++) {
+                if (v[k] < 0) continue;
+                y[k] = load_f32(src + v[k]);
+                word[k] = mask ? mask[v[k] >> 5] : FULL;
+            }
+#pragma unroll
+            for (int k = 0; k < BATCH; k++) {
+                if (v[k] < 0 || !((word[k] >> (v[k] & 31)) & 1)) continue;
+                float z = y[k];
+                if (c[k]) z = z > 0.f ? z / rep : z * rep;
+                if (c[k] & COUNT) z = z - freq * (float)(c[k] & COUNT) - pres;
+                store_f32(dst + v[k], z + bias[k]);
+            }
+        }
+    };
+    // biased tokens, with what the history says of them; then the history's others
+    if (P.n_bias) {
+        rewrite(threadIdx.x, bias_cap, [&](int i, int* v, uint32_t* c, float* bias) {
+            if (bias_key[i] == EMPTY) return;
+            *v = (int)bias_key[i];
+            const int s = HASH ? hash_find(key, cap, shift, *v) : *v >> shares;
+            *c = s >= 0 ? count_at(s) : 0u;
+            if (s >= 0) clear(s);
+            *bias = P.bias[(size_t)b * P.n_bias + bias_pos[i] - 1];
+        });
+        __syncthreads();
+    }
+    auto named = [&](int i, int* v, uint32_t* c, float* bias) {
+        *c = count_at(i);
+        if (*c) *v = HASH ? (int)key[i] : i << shares | share;
+        *bias = 0.f;
+    };
+    // of a direct table few words are named: a thread's next 32 as bits, then those
+    if constexpr (HASH) rewrite(threadIdx.x, cap, named);
+    else for (int i0 = 0; i0 < cap; i0 += 32 * NT) {
+        uint32_t bits = 0;
+#pragma unroll 8
+        for (int k = 0; k < 32; k++) {
+            const int i = i0 + k * NT + threadIdx.x;
+            if (i < cap && count_at(i)) bits |= 1u << k;
+        }
+        while (bits) {
+            int place[BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; k++) {
+                place[k] = bits ? i0 + (__ffs(bits) - 1) * NT + (int)threadIdx.x : -1;
+                bits &= bits - 1;
+            }
+            rewrite(0, BATCH, [&](int k, int* v, uint32_t* c, float* bias) {
+#pragma unroll
+                for (int j = 0; j < BATCH; j++)
+                    if (j == k && place[j] >= 0) named(place[j], v, c, bias);
+            }, 1);
+        }
     }
 }
 
@@ -199,18 +308,17 @@ psc_status process(const T* logits, int64_t stride, T* out, int64_t out_stride, 
         s = psc_apply_mask(out, dtype, out_stride, bitmask, B, V, cs);
     }
     if (s != PSC_OK || (!P.H && !P.n_bias)) return s;
-    const int words = P.n_bias ? 2 : 1;
-    const int64_t entries = (int64_t)P.H + P.n_bias;
-    if (2 * entries <= HASH_SLOTS) {
-        int cap = 32;
-        while (cap < 2 * entries) cap <<= 1;
-        return ops_launch(k_penalize<T, true>, dim3(B), 512, (size_t)cap * (words + 1) * 4, 1, cs, "k_penalize", logits,
-                          stride, out, out_stride, V, P, bitmask, W, 1, early);
-    }
-    const int parts = (V + PART - 1) / PART;
-    return ops_launch(k_penalize<T, false>, dim3(B * parts), 512, (size_t)std::min(V, PART) * words * 4, 1, cs,
-                      "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, parts,
-                      early);
+    const size_t bias_bytes = P.n_bias ? (size_t)hash_cap(P.n_bias) * 8 : 0;
+    if (2 * P.H <= HASH_SLOTS)
+        return ops_launch(k_penalize<T, HASHED>, dim3(B), table_threads(HASHED), bias_bytes + (size_t)hash_cap(P.H) * 8,
+                          1, cs, "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, 0, early);
+    const bool narrow = P.H <= SHORT_HISTORY;
+    const int word = narrow ? 2 : 4;
+    int shares = 0;
+    while (((((int64_t)V - 1) >> shares) + 1) * word > TABLE_BYTES - (int64_t)bias_bytes / 2) shares++;
+    return ops_launch(narrow ? k_penalize<T, SHORT> : k_penalize<T, LONG>, dim3((unsigned)B << shares),
+                      table_threads(LONG), bias_bytes + (((V - 1) >> shares) + 2) / 2 * 2 * (size_t)word, 1, cs,
+                      "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, shares, early);
 }
 
 }  // namespace
@@ -228,10 +336,11 @@ extern "C" psc_status psc_process_logits(const void* d_logits, psc_dtype dtype, 
     if (H < 0 || n_bias < 0 || (H && history_stride < H) ||
         (B && ((H && !d_history) || (n_bias && (!d_bias_ids || !d_bias)))))
         return ops_fail(PSC_ERR_ARG, me, "bad history or biases");
+    if (V > MAX_V) return ops_fail(PSC_ERR_LIMIT, me, "vocabulary over 2^30 tokens");
     if (H > MAX_HISTORY) return ops_fail(PSC_ERR_LIMIT, me, "history over 16,777,215 tokens");
     if (n_bias > MAX_BIAS) return ops_fail(PSC_ERR_LIMIT, me, "more than 4,096 biases a row");
     if (B == 0) return PSC_OK;
-    if ((int64_t)B * ((V + PART - 1) / PART) > 0x7fffffff) return ops_fail(PSC_ERR_LIMIT, me, "batch too large");
+    if ((int64_t)B * (V / 16384 + 1) > 0x7fffffff) return ops_fail(PSC_ERR_LIMIT, me, "batch too large");
     const size_t e = dtype == PSC_BF16 ? 2 : 4;
     if (d_logits == d_out) {
         if (row_stride != out_stride) return ops_fail(PSC_ERR_ARG, me, "in place with two row strides");

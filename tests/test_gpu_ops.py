@@ -211,8 +211,8 @@ def _process_ref(x, lens, plens, hist, rep, freq, pres, ids, bias, allowed):
 
 
 @pytest.mark.parametrize("B,V,H,n", [(1, 1, 1, 0), (1, 33, 0, 3), (3, 1000, 1, 1), (2, 1025, 257, 40), (5, 4099, 700, 0),
-                                     (4, 32000, 8000, 300), (3, 50001, 9000, 17), (2, 70000, 40000, 0),
-                                     (2, 300, 20000, 5), (7, 2048, 100, 2048)])
+                                     (4, 32000, 8000, 300), (3, 50001, 9000, 17), (2, 70000, 40000, 0), (1, 1, 32767, 2), (2, 270001, 9001, 9),
+                                     (2, 300, 20000, 5), (7, 2048, 100, 2048), (2, 5000, 2047, 300)])
 @pytest.mark.parametrize("dtype,mask,where", [("bf16", "mixed", "out"), ("f32", "none", "in"), ("f32", "mixed", "in"),
                                               ("bf16", "none", "out"), ("bf16", "mixed", "ragged")])
 def test_process_logits(psc, B, V, H, n, dtype, mask, where):
