@@ -49,7 +49,7 @@ __device__ __forceinline__ uint4 mask_piece(uint4 v, uint32_t bits) {
 
 // out = mask ? logits : -inf, a warp per 1024 columns.
 template <typename T>
-__global__ void __launch_bounds__(256) k_mask_copy(const T* logits, int64_t stride, T* out, int64_t out_stride, int B,
+__global__ void __launch_bounds__(256, 4) k_mask_copy(const T* logits, int64_t stride, T* out, int64_t out_stride, int B,
                                                    int V, const uint32_t* bitmask, int W, int vec) {
     constexpr int E = 16 / sizeof(T), PASSES = 1024 / (32 * E);
     const int lane = threadIdx.x & 31;
@@ -144,14 +144,17 @@ __host__ __device__ inline int hash_cap(int entries) {
 }
 
 // A direct table's words are 16 bits while no count can pass 15 (SHORT), 32 otherwise.
-enum TableKind { HASHED, SHORT, LONG };
+// Hashed tables are worked by 256 threads where there are rows for every SM (four blocks of an
+// SM hide each other's latency; 1024 rows of 262,144 tokens: 34 us, 41 with 512 threads), else
+// by 1024 (64 rows of up to 2,047 ids and 300 biases: see the launch).
+enum TableKind { HASHED, WIDE, SHORT, LONG };
 constexpr int SHORT_HISTORY = 32767;
-__host__ __device__ constexpr int table_threads(TableKind k) { return k == HASHED ? 512 : 1024; }
+__host__ __device__ constexpr int table_threads(TableKind k) { return k == HASHED ? 256 : 1024; }
 
 template <typename T, TableKind KIND>
-__global__ void __launch_bounds__(table_threads(KIND), KIND == HASHED ? 2 : 1) k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V,
+__global__ void __launch_bounds__(table_threads(KIND), KIND == HASHED ? 4 : 1) k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V,
                                                   Penalties P, const uint32_t* bitmask, int W, int shares, int early) {
-    constexpr bool HASH = KIND == HASHED;
+    constexpr bool HASH = KIND == HASHED || KIND == WIDE;
     constexpr int NT = table_threads(KIND);
     extern __shared__ uint32_t tab[];
     // After k_mask_copy, which began once every earlier kernel had completed, the table is
@@ -301,7 +304,7 @@ psc_status process(const T* logits, int64_t stride, T* out, int64_t out_stride, 
     if (out != logits) {
         const int vec = is_aligned(logits, stride * sizeof(T), 16) && is_aligned(out, out_stride * sizeof(T), 16);
         const long chunks = (long)B * ((V + 1023) / 1024);
-        const int blocks = (int)std::min<long>((chunks + 7) / 8, (long)current_sms() * 8);
+        const int blocks = (int)std::min<long>((chunks + 7) / 8, (long)current_sms() * 4);
         s = ops_launch(k_mask_copy<T>, dim3(blocks), 256, 0, 1, cs, "k_mask_copy", logits, stride, out, out_stride, B,
                        V, bitmask, W, vec);
     } else if (bitmask) {
@@ -310,8 +313,8 @@ psc_status process(const T* logits, int64_t stride, T* out, int64_t out_stride, 
     if (s != PSC_OK || (!P.H && !P.n_bias)) return s;
     const size_t bias_bytes = P.n_bias ? (size_t)hash_cap(P.n_bias) * 8 : 0;
     if (2 * P.H <= HASH_SLOTS)
-        return ops_launch(k_penalize<T, HASHED>, dim3(B), table_threads(HASHED), bias_bytes + (size_t)hash_cap(P.H) * 8,
-                          1, cs, "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, 0, early);
+        return ops_launch(B > current_sms() ? k_penalize<T, HASHED> : k_penalize<T, WIDE>, dim3(B),
+                          table_threads(B > current_sms() ? HASHED : WIDE), bias_bytes + (size_t)hash_cap(P.H) * 8, 1, cs, "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, 0, early);
     const bool narrow = P.H <= SHORT_HISTORY;
     const int word = narrow ? 2 : 4;
     int shares = 0;
