@@ -26,11 +26,38 @@ inline psc_status ops_check(cudaError_t e, const char* what) {
     return ops_fail(e == cudaErrorMemoryAllocation ? PSC_ERR_OOM : PSC_ERR_CUDA, what, cudaGetErrorString(e));
 }
 
+// SMs of the current device (asked once per device and thread).
 inline int current_sms() {
-    int dev = 0, n = 0;
+    static thread_local int of = -1, n = 0;
+    int dev = 0;
     cudaGetDevice(&dev);
-    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (dev != of) {
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+        of = dev;
+    }
     return n > 0 ? n : 1;
+}
+
+// Allows `smem` bytes of dynamic shared memory for a kernel on the
+// current device; what this thread has already allowed is not asked for again.
+inline psc_status allow_smem(const void* kernel, int smem, const char* what) {
+    struct Allowed {
+        const void* kernel;
+        int dev, smem;
+    };
+    static thread_local Allowed known[64];
+    static thread_local int n = 0;
+    int dev = 0;
+    cudaGetDevice(&dev);
+    Allowed* a = nullptr;
+    for (int i = 0; i < n && !a; i++)
+        if (known[i].kernel == kernel && known[i].dev == dev) a = &known[i];
+    if (a && a->smem >= smem) return PSC_OK;
+    psc_status s = ops_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem), what);
+    if (s != PSC_OK) return s;
+    if (!a && n < 64) a = &known[n++];
+    if (a) *a = {kernel, dev, smem};
+    return PSC_OK;
 }
 
 inline bool is_dtype(psc_dtype d) { return d == PSC_F32 || d == PSC_BF16; }
@@ -45,12 +72,7 @@ template <typename... KArgs, typename... Args>
 psc_status ops_launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t cs,
                       const char* what, Args... args) {
     if (smem > 32 * 1024) {                     // with what a kernel declares itself, 48 KB need no asking
-        psc_status s = ops_check(
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem), what);
-        if (s != PSC_OK) return s;
-    }
-    if (cluster > 8) {
-        psc_status s = ops_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1), what);
+        psc_status s = allow_smem((const void*)kernel, (int)smem, what);
         if (s != PSC_OK) return s;
     }
     cudaLaunchConfig_t cfg = {};

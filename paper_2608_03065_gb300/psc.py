@@ -120,7 +120,10 @@ def _check(code: int):
 def _stream(stream) -> int | None:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        try:                                # the current stream's handle without a Stream object around it
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+        except AttributeError:
+            return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -502,16 +505,15 @@ def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, strea
     pw, sw = _rows(w, torch.int8, "w")
     pl, sl = _rows(logits, None, "logits", T, V)
     n = load().psc_head_work_bytes(T, V, K)
+    pm = _mask_ptr(bitmask, T, V)
     if work is None:
-        pm = _mask_ptr(bitmask, T, V)
-        if stream is None or isinstance(stream, int):
-            s = torch.cuda.current_stream() if stream is None else torch.cuda.ExternalStream(stream)
-        else:
-            s = stream
-        with torch.cuda.stream(s):
+        # of the allocator's pool for the stream that the kernels run on
+        if stream is None:
             work = torch.empty(n, dtype=torch.uint8, device=logits.device)
-    else:
-        pm = _mask_ptr(bitmask, T, V)
+        else:
+            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+            with torch.cuda.stream(s):
+                work = torch.empty(n, dtype=torch.uint8, device=logits.device)
     _check(load().psc_head_logits(pq, sq, _ptr(scale, torch.float32, "scale", T), T, pw, sw,
                                   _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
                                   _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
