@@ -127,6 +127,141 @@ __global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned
     }
 }
 
+// ------------------------------------------------------------------ few tokens
+//
+// k_head_rows: a warp per 4 vocabulary rows, integer dot products of their bytes (a lane's
+// 16 at once) with up to N tokens in shared memory.  With few tokens the weights' bytes are
+// all that counts; a tensor core would spend its time on 128-row operands that hardly any
+// column uses (about 56 cycles per product of 16 columns of K, whatever N).  Under a mask,
+// rows that no token allows are not read.  Measured without a mask on 128,256 x 2048 (with
+// k_head_mma in brackets): 1 token 45 us (64), 4 tokens 49 (62), 8 tokens 71 (62).
+constexpr int ROWS = 4;
+constexpr int ROWS_THREADS = 256;
+constexpr int ROWS_X_MAX = 64 * 1024;         // bytes of tokens held in shared memory
+
+// The first n (< 16) of 16 bytes, zeros behind them.
+__device__ __forceinline__ uint4 load_bytes(const int8_t* p, int n) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; j++)
+        if (j < n) w[j >> 2] |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T, int N, bool MASKED>
+__global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, int* faults) {
+    constexpr int WIDTH = MASKED ? 32 : ROWS;           // vocabulary rows of a warp's item
+    extern __shared__ __align__(16) uint8_t dyn[];
+    __shared__ float s_out[ROWS_THREADS / 32][N * WIDTH];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int chunks = (h.K + 15) / 16;                 // 16-byte pieces of a row
+    uint4* xs = reinterpret_cast<uint4*>(dyn);          // [N][chunks], zero past K and T
+    dep_wait();
+    dep_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    for (int i = threadIdx.x; i < N * chunks; i += ROWS_THREADS) {
+        const int t = i / chunks, k = (i - t * chunks) * 16;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (t < h.T) {
+            const int8_t* p = h.q + (size_t)t * h.q_stride + k;
+            x = k + 16 <= h.K ? *reinterpret_cast<const uint4*>(p) : load_bytes(p, h.K - k);
+        }
+        xs[i] = x;
+    }
+    __syncthreads();
+    // a row's last piece past K: within its stride, except perhaps in the last row
+    const bool ragged = h.K % 16 != 0;
+    // sums over K of the rows v0 + r[i] (none where r[i] < 0), to out[t * WIDTH + r[i]]
+    float* out = s_out[warp];
+    auto dots = [&](int v0, const int (&r)[ROWS]) {
+        int acc[ROWS][N] = {};
+#pragma unroll 2
+        for (int c = lane; c < chunks; c += 32) {
+            uint4 w[ROWS];
+#pragma unroll
+            for (int i = 0; i < ROWS; i++) {
+                w[i] = make_uint4(0, 0, 0, 0);
+                if (r[i] < 0) continue;
+                const int8_t* p = h.w + (size_t)(v0 + r[i]) * h.w_stride + c * 16;
+                if (ragged && c == chunks - 1 && v0 + r[i] == h.V - 1) w[i] = load_bytes(p, h.K - c * 16);
+                else w[i] = __ldcs(reinterpret_cast<const uint4*>(p));
+            }
+#pragma unroll
+            for (int t = 0; t < N; t++) {
+                const uint4 x = xs[t * chunks + c];
+#pragma unroll
+                for (int i = 0; i < ROWS; i++) {
+                    acc[i][t] = __dp4a((int)w[i].x, (int)x.x, acc[i][t]);
+                    acc[i][t] = __dp4a((int)w[i].y, (int)x.y, acc[i][t]);
+                    acc[i][t] = __dp4a((int)w[i].z, (int)x.z, acc[i][t]);
+                    acc[i][t] = __dp4a((int)w[i].w, (int)x.w, acc[i][t]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; i++)
+#pragma unroll
+            for (int t = 0; t < N; t++) {
+                const int sum = __reduce_add_sync(FULL, acc[i][t]);
+                if (lane == 0 && r[i] >= 0) out[t * WIDTH + r[i]] = (float)sum;
+            }
+    };
+    const int n_items = (h.V + WIDTH - 1) / WIDTH, n_warps = gridDim.x * (ROWS_THREADS / 32);
+    const int me = blockIdx.x * (ROWS_THREADS / 32) + warp;
+    if (!MASKED) {                                      // neighbouring rows, the same number for all warps
+        const int to = (int)((int64_t)(me + 1) * n_items / n_warps);
+        for (int item = (int)((int64_t)me * n_items / n_warps); item < to; item++) {
+            const int v0 = item * ROWS;
+            int r[ROWS];
+#pragma unroll
+            for (int i = 0; i < ROWS; i++) r[i] = v0 + i < h.V ? i : -1;
+            dots(v0, r);
+            __syncwarp();
+            for (int t0 = 0; t0 < h.T; t0 += 32 / ROWS) {
+                const int t = t0 + lane / ROWS, v = v0 + lane % ROWS;
+                if (t < h.T && v < h.V)
+                    store_f32(logits + (size_t)t * h.row_stride + v,
+                              out[t * ROWS + lane % ROWS] * h.scale[t] * h.w_scale[v]);
+            }
+            __syncwarp();
+        }
+    } else {                                            // a mask word each; what masks allow may lie together
+        for (int item = me; item < n_items; item += n_warps) {
+            const int v0 = item * 32, v = v0 + lane;
+            const uint32_t mine = lane < h.T ? h.bitmask[(size_t)lane * h.W + item] : 0u;
+            uint32_t rows = __reduce_or_sync(FULL, mine);
+            if (h.V - v0 < 32) rows &= (1u << (h.V - v0)) - 1;
+            while (rows) {
+                int r[ROWS];
+#pragma unroll
+                for (int i = 0; i < ROWS; i++) {
+                    r[i] = __ffs(rows) - 1;             // -1: none left
+                    rows &= rows - 1;
+                }
+                dots(v0, r);
+            }
+            __syncwarp();
+            const float sw = v < h.V ? h.w_scale[v] : 0.f;
+            for (int t = 0; t < h.T; t++) {
+                const uint32_t bits = __shfl_sync(FULL, mine, t);
+                if (v < h.V)
+                    store_f32(logits + (size_t)t * h.row_stride + v, (bits >> lane) & 1
+                                                                         ? out[t * WIDTH + lane] * h.scale[t] * sw
+                                                                         : __uint_as_float(0xFF800000u));
+            }
+            __syncwarp();
+        }
+    }
+}
+
+template <typename T, int N>
+psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    const size_t smem = (size_t)N * ((h.K + 15) / 16) * 16;
+    const int per_sm = N > 4 ? 2 : 3, items = h.bitmask ? h.W : (h.V + ROWS - 1) / ROWS;     // as their registers allow
+    return ops_launch(h.bitmask ? k_head_rows<T, N, true> : k_head_rows<T, N, false>, dim3(std::min((items + 7) / 8, current_sms() * per_sm)), ROWS_THREADS, smem, 1,
+                      cs, "k_head_rows", h, logits, (int*)work);
+}
+
 // ------------------------------------------------------------ the tensor-core path
 //
 // k_head_mma: a persistent block per SM over tiles of 128 vocabulary rows (the
@@ -604,7 +739,16 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
 
 template <typename T>
 psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
-    if (is_aligned(h.w, h.w_stride, 16) && is_aligned(h.q, h.q_stride, 16)) return head_mma(h, logits, work, cs);
+    if (is_aligned(h.w, h.w_stride, 16) && is_aligned(h.q, h.q_stride, 16)) {
+        // up to 4 tokens, or 16 under a mask (rows of the weights can be left out one by one)
+        const int64_t row = (h.K + 15) / 16 * 16;
+        if (h.T == 1 && row <= ROWS_X_MAX) return head_rows<T, 1>(h, logits, work, cs);
+        if (h.T == 2 && 2 * row <= ROWS_X_MAX) return head_rows<T, 2>(h, logits, work, cs);
+        if (h.T <= 4 && 4 * row <= ROWS_X_MAX) return head_rows<T, 4>(h, logits, work, cs);
+        if (h.T <= 8 && h.bitmask && 8 * row <= ROWS_X_MAX) return head_rows<T, 8>(h, logits, work, cs);
+        if (h.T <= 16 && h.bitmask && 16 * row <= ROWS_X_MAX) return head_rows<T, 16>(h, logits, work, cs);
+        return head_mma(h, logits, work, cs);
+    }
     const int aligned4 = is_aligned(h.w, h.w_stride, 4) && is_aligned(h.q, h.q_stride, 4);
     return ops_launch(k_head_dot<T>, dim3((h.V + 63) / 64, (h.T + 63) / 64), 256, 0, 1, cs, "k_head_dot", h, logits,
                       aligned4, (int*)work);
