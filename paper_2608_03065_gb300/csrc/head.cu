@@ -148,8 +148,23 @@ __device__ __forceinline__ uint4 load_bytes(const int8_t* p, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Whether a mask leaves so few rows (up to a quarter) that reading them one by one wins:
+// 16 tokens over 128,256 x 2048 take 174 us by rows and 64 us by k_head_mma when all are
+// needed, 17 and 47 us when some 300 are.  flags: of every tile, the rows that some token allows.
+__device__ __forceinline__ bool few_rows(const uint8_t* flags, int n_tiles, int V) {
+    int sum = 0;
+    for (int i = threadIdx.x; i < n_tiles; i += blockDim.x) sum += flags[i];
+    __shared__ int s_sum[32];
+    sum = __reduce_add_sync(FULL, sum);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = __reduce_add_sync(FULL, (threadIdx.x & 31) < blockDim.x / 32 ? s_sum[threadIdx.x & 31] : 0);
+    return 4 * (int64_t)sum <= V;
+}
+
 template <typename T, int N, bool MASKED>
-__global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, int* faults) {
+__global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, int* faults, const uint8_t* flags,
+                                                            int n_tiles) {
     constexpr int WIDTH = MASKED ? 32 : ROWS;           // vocabulary rows of a warp's item
     extern __shared__ __align__(16) uint8_t dyn[];
     __shared__ float s_out[ROWS_THREADS / 32][N * WIDTH];
@@ -158,7 +173,8 @@ __global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, i
     uint4* xs = reinterpret_cast<uint4*>(dyn);          // [N][chunks], zero past K and T
     dep_wait();
     dep_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    if (flags && !few_rows(flags, n_tiles, h.V)) return;        // k_head_mma's
+    if (!flags && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
     for (int i = threadIdx.x; i < N * chunks; i += ROWS_THREADS) {
         const int t = i / chunks, k = (i - t * chunks) * 16;
         uint4 x = make_uint4(0, 0, 0, 0);
@@ -255,11 +271,12 @@ __global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, i
 }
 
 template <typename T, int N>
-psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs, const uint8_t* flags = nullptr,
+                     int n_tiles = 0) {
     const size_t smem = (size_t)N * ((h.K + 15) / 16) * 16;
     const int per_sm = N > 4 ? 2 : 3, items = h.bitmask ? h.W : (h.V + ROWS - 1) / ROWS;     // as their registers allow
     return ops_launch(h.bitmask ? k_head_rows<T, N, true> : k_head_rows<T, N, false>, dim3(std::min((items + 7) / 8, current_sms() * per_sm)), ROWS_THREADS, smem, 1,
-                      cs, "k_head_rows", h, logits, (int*)work);
+                      cs, "k_head_rows", h, logits, (int*)work, flags, n_tiles);
 }
 
 // ------------------------------------------------------------ the tensor-core path
@@ -417,7 +434,7 @@ __device__ __forceinline__ uint2 widen4(uint32_t b) {
     return make_uint2(*reinterpret_cast<uint32_t*>(&l), *reinterpret_cast<uint32_t*>(&h));
 }
 
-// The tokens' rows in f16, zero past K; which tiles hold an allowed token; the fault word.
+// The tokens' rows in f16, zero past K; how many rows of each tile some token allows; the fault word.
 __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_vt, int n_nt, int x_blocks,
                                                    int* faults, __half* x, uint8_t* flags) {
     dep_wait();
@@ -453,8 +470,10 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
         const int wi = vt * 4 + (lane & 3);
         if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
     }
-    any = __any_sync(FULL, any != 0);
-    if (lane == 0) flags[item] = (uint8_t)any;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) any |= __shfl_xor_sync(FULL, any, o);
+    const int rows = __reduce_add_sync(FULL, lane < 4 ? __popc(any) : 0);
+    if (lane == 0) flags[item] = (uint8_t)rows;
 }
 
 template <typename T>
@@ -462,7 +481,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                                                              const __grid_constant__ CUtensorMap x_map, Head h,
                                                              T* logits, int N, int n_nt, int n_items, int Kp, int n_raw,
                                                              int n_x, int x_group, int tmem_cols, int* faults,
-                                                             const uint8_t* flags) {
+                                                             const uint8_t* flags, int leave_few) {
+    if (leave_few) {                                  // few rows are k_head_rows'
+        dep_wait();
+        if (few_rows(flags, n_items, h.V)) return;
+    }
     constexpr int PER = 8 / N_A, ROWS = VT / PER;      // converting warps of a group, rows of each
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) uint64_t s_bars[2 * (MAX_RAW + N_A + MAX_X) + 5];
@@ -732,21 +755,23 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     psc_status s = ops_launch(k_head_prep, dim3(x_blocks + (h.bitmask ? (items + 7) / 8 : 0)), 256, 0, 1, cs,
                               "k_head_prep", h, p.Kp, p.N, p.n_vt, p.n_nt, x_blocks, faults, x, flags);
     if (s != PSC_OK) return s;
+    const int leave_few = h.T <= 16 && h.bitmask && 16 * (int64_t)((h.K + 15) / 16 * 16) <= ROWS_X_MAX;
+    if (leave_few && (s = head_rows<T, 16>(h, logits, work, cs, flags, items)) != PSC_OK) return s;
     return ops_launch(k_head_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
                       w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_x, p.x_group, p.tmem, faults,
-                      (const uint8_t*)flags);
+                      (const uint8_t*)flags, leave_few);
 }
 
 template <typename T>
 psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     if (is_aligned(h.w, h.w_stride, 16) && is_aligned(h.q, h.q_stride, 16)) {
-        // up to 4 tokens, or 16 under a mask (rows of the weights can be left out one by one)
+        // up to 4 tokens, or 8 under a mask (rows of the weights can be left out one by one; up
+        // to 16 if it leaves few)
         const int64_t row = (h.K + 15) / 16 * 16;
         if (h.T == 1 && row <= ROWS_X_MAX) return head_rows<T, 1>(h, logits, work, cs);
         if (h.T == 2 && 2 * row <= ROWS_X_MAX) return head_rows<T, 2>(h, logits, work, cs);
         if (h.T <= 4 && 4 * row <= ROWS_X_MAX) return head_rows<T, 4>(h, logits, work, cs);
         if (h.T <= 8 && h.bitmask && 8 * row <= ROWS_X_MAX) return head_rows<T, 8>(h, logits, work, cs);
-        if (h.T <= 16 && h.bitmask && 16 * row <= ROWS_X_MAX) return head_rows<T, 16>(h, logits, work, cs);
         return head_mma(h, logits, work, cs);
     }
     const int aligned4 = is_aligned(h.w, h.w_stride, 4) && is_aligned(h.q, h.q_stride, 4);

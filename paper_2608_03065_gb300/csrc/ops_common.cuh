@@ -71,7 +71,7 @@ inline bool is_aligned(const void* p, int64_t stride_bytes, int64_t to) {
 template <typename... KArgs, typename... Args>
 psc_status ops_launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t cs,
                       const char* what, Args... args) {
-    if (smem > 32 * 1024) {                     // with what a kernel declares itself, 48 KB need no asking
+    if (smem > 16 * 1024) {                     // with what a kernel declares itself, 48 KB need no asking
         psc_status s = allow_smem((const void*)kernel, (int)smem, what);
         if (s != PSC_OK) return s;
     }

@@ -143,7 +143,8 @@ def _head_case(psc, T, V, K, dtype, mask, pad=0, shift=0, fill=None, out_pad=0, 
 @pytest.mark.parametrize("T,V,K", [(1, 1, 1), (1, 130, 16), (1, 1000, 48), (2, 257, 64), (3, 129, 100), (7, 512, 257),
                                    (8, 1000, 1024), (9, 640, 320), (16, 333, 512), (17, 300, 80), (33, 1024, 1040),
                                    (64, 129, 128), (100, 1500, 192), (130, 260, 2048), (256, 384, 64), (257, 500, 336),
-                                   (300, 127, 96), (513, 1300, 160)])
+                                   (300, 127, 96), (513, 1300, 160), (4, 300, 4096), (8, 700, 2048), (12, 3000, 2048),
+                                   (16, 2500, 4080), (16, 200, 4200)])
 @pytest.mark.parametrize("dtype,mask", [("bf16", "none"), ("f32", "mixed"), ("bf16", "tight")])
 def test_head_logits(psc, T, V, K, dtype, mask):
     _head_case(psc, T, V, K, dtype, mask, pad=-K % 16)
