@@ -274,12 +274,45 @@ struct Weigh {
         return x >= tau && y >= min_e ? weight_of(y) : 0ull;
     }
 };
+struct Settings {
+    const float* uniform;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+};
+
+// What a call is about.
+struct Job {
+    const void* logits;
+    int64_t stride;
+    int B, V, per_block, W;
+    const uint32_t* bitmask;
+    Settings settings;
+    int32_t* tokens;
+    float* logprobs;
+    uint8_t* pending;       // rows that k_sample_light leaves to k_sample, or NULL
+};
+
+// What is found out about a row, kept in shared memory: a register that lives across the
+// passes is one that they do not have.
+struct State {
+    int b, k, odd, n, bin, own;
+    float p, m, lowest, bound, z_from, z_to;
+    uint32_t p24, u24, tau;
+    bool in_doubt, hit;
+    u64 listed, left;
+};
+
 struct Shared {
+    Job job;
+    State st;
     uint32_t cnt[2][256], hi[2][256];   // a histogram's counts, or its weights as two words
     uint32_t bins[BINS], bins_hi[BINS], count[BINS], tau;
     int few[FEW], n_few;
     Row row;
     Weigh g;
+    float group[PIECES][NT];            // the maxima of the threads' groups
     u64 part[12];                       // this block's share of what the cluster combines, a slot per use
     u64 warp[2][NW];                    // the warps' shares of what a block combines
     uint8_t turn[NT];                   // which of the two a thread uses next
@@ -436,6 +469,9 @@ __device__ int gather(cg::cluster_group& cl, Shared& s, int n_blocks) {
     return n;
 }
 
+// The weight that a nucleus of `total` has to hold.
+__device__ __forceinline__ u64 limit_of(const Shared& s, u64 total) { return max((u64)1, part_of(total, s.st.p24)); }
+
 enum { FAILED = 0, DRAWN = 1, BOUNDED = 2 };    // what settle could do
 
 // Adds a weight to its bin (two words, with carry).
@@ -462,13 +498,14 @@ __device__ int pick_few(Shared& s, int n, In&& in) {
 }
 
 // Filters and draws among the block's n listed candidates, of which the weights sum to
-// `listed` and none is below `bound`: k (0: off), then a nucleus of `limit` (0: limit_of what
+// s.st.listed and none is below `bound`: k (0: off), then a nucleus of `limit` (0: limit_of what
 // top-k leaves, ~0: off), then min_e.  DRAWN: *place is the drawn one's place in the list
 // for the thread that found it, -1 for others, *kept the weight of what stays.  BOUNDED:
 // s.tau is the order of the last value that stays.
-template <typename Limit>
-__device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V, int n, int k, u64 listed, u64 limit,
-                                   Limit limit_of, u64 u24, u64* kept, int* place) {
+__device__ __noinline__ int settle(Shared& s, float bound, int k, u64 limit, u64* kept, int* place) {
+    const Weigh g = s.g;
+    const int n = s.st.n, V = s.row.V;
+    u64 listed = s.st.listed;
     const int tid = threadIdx.x;
     *place = -1;
     if (n <= PAIRS) {
@@ -491,14 +528,14 @@ __device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V
         bool stays = mine && (!k || larger < k);
         if (!limit) {
             block_before(s, stays && !j0 ? w : 0, &listed);
-            limit = limit_of(listed);
+            limit = limit_of(s, listed);
         }
         stays = stays && over < limit && g.e(unordered(key)) >= g.min_e;
         if (!stays) w = 0;
         __syncthreads();
         if (mine && !j0) s.weight[i] = w;
         block_before(s, j0 ? 0 : w, kept);      // and every weight is written
-        const u64 target = part_of(*kept, u24);
+        const u64 target = part_of(*kept, s.st.u24);
         u64 before = 0;
         if (mine)
             for (int j = j0; j < n; j += per)
@@ -551,7 +588,7 @@ __device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V
             listed += above;
             tau = s.tau;
         }
-        if (!limit) limit = limit_of(listed);
+        if (!limit) limit = limit_of(s, listed);
         if (limit != ~0ull) {
             const u64 over = before >> 12;
             // beyond top-k's last bin nothing stays; that bin holds the limit where no earlier one does
@@ -585,7 +622,7 @@ __device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V
     for (int i = tid; i < n; i += NT)
         if (in(i)) add_to_bin(s, part(i), s.weight[i]);
     __syncthreads();
-    const u64 w = bin_weight(s, tid), before = block_before(s, w, kept), target = part_of(*kept, u24);
+    const u64 w = bin_weight(s, tid), before = block_before(s, w, kept), target = part_of(*kept, s.st.u24);
     if (before <= target && target < before + w) s.at = tid, s.found[0] = target - before;
     __syncthreads();
     const int bin = s.at;
@@ -604,19 +641,22 @@ __device__ __noinline__ int settle(Shared& s, const Weigh& g, float bound, int V
     return DRAWN;
 }
 
-// The search over the whole row, digit by digit of the values' order: of the candidates
-// that reach g.tau, the value at which the running count or weight from the largest
-// down reaches need_of(their sum).
-template <bool MASS, typename T, bool VEC, typename Need>
-__device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const Row& r, const Weigh& g, int n_blocks,
-                                         Need need_of) {
+// The search over the whole row, digit by digit of the values' order: of the candidates that
+// reach s.g.tau, the value at which the running count (up to k) or weight (up to the nucleus')
+// from the largest down is reached; it becomes s.g.tau.
+template <bool MASS, typename T, bool VEC>
+__device__ __noinline__ void row_search(Shared& s) {
+    cg::cluster_group cl = cg::this_cluster();
+    const int n_blocks = (int)cl.num_blocks();
     uint32_t prefix = 0;
     u64 need = 0;
     int buf = 0;
+    __syncthreads();
+    const Weigh g = s.g;
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = threadIdx.x; i < 256; i += NT) s.cnt[buf][i] = s.hi[buf][i] = 0;
         __syncthreads();
-        for_pieces<T, VEC, false>(r, s.lut, [&](const Piece<T>& q, int, int, bool any) {
+        for_pieces<T, VEC, false>(s.row, s.lut, [&](const Piece<T>& q, int, int, bool any) {
             if (!any) return;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
@@ -636,12 +676,13 @@ __device__ __noinline__ float row_search(cg::cluster_group& cl, Shared& s, const
                     h += (MASS ? (u64)o->hi[buf][threadIdx.x] << 32 : 0) + o->cnt[buf][threadIdx.x];
                 }
             block_before(s, h, &all);
-            need = need_of(all);
+            need = MASS ? limit_of(s, all) : min((u64)s.st.k, all);     // fewer candidates than k: all stay
         }
         prefix = (prefix << 8) | (uint32_t)pick_digit<MASS>(cl, n_blocks, s, buf, &need);
         buf ^= 1;
     }
-    return unordered(prefix);
+    if (threadIdx.x == 0) s.g.tau = unordered(prefix);
+    __syncthreads();
 }
 
 // The passes over the block's part of the row, each a function of its own so that none
@@ -707,6 +748,8 @@ __device__ __noinline__ void chunk_pass(const Shared& s, u64* chunk_sum, bool od
 // A stretch of z, from z_from (excluded, above) down to z_to, in BINS bins.
 struct Stretch {
     float z_from, z_to, top, fine;
+    __device__ __forceinline__ Stretch(float from, float to)
+        : z_from(from), z_to(to), top(fminf(from, 0.f)), fine(BINS / fmaxf(fminf(from, 0.f) - to, 1e-3f)) {}
     __device__ __forceinline__ int bin(float z) const { return min(BINS - 1, (int)((top - z) * fine)); }
 };
 
@@ -796,22 +839,337 @@ __device__ __noinline__ void sample_pass(Shared& s, float bound, float unit, flo
     }
 }
 
+// The maxima of the thread's groups; whether it met a NaN or +inf.
+template <typename T, bool VEC>
+__device__ __noinline__ int max_pass(Shared& s) {
+    const Row r = s.row;
+    float group[PIECES];
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) group[q] = NEG_INF;
+    int odd = 0;
+    for_pieces<T, VEC, true>(r, s.lut, [&](const Piece<T>& p, int, int q, bool) {
+        float x = p.max8_nan();
+        if (!(x <= FLT_BIG)) odd = 1, x = p.max8();
+        group[q] = fmaxf(group[q], x);
+    }, [](int) {});
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) s.group[q][threadIdx.x] = clean(group[q]);
+    return odd;
+}
+
+template <typename T, bool VEC, typename F>
+__device__ __forceinline__ void own_groups(const Shared& s, float bound, F&& f) {
+    const Row r = s.row;
+    float group[PIECES];
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) group[q] = s.group[q][threadIdx.x];
+    for_groups<T, VEC>(r, s.lut, group, bound, f);
+}
+
+// V minus the lowest token with the value m that the thread met, 0 for none.
+template <typename T, bool VEC>
+__device__ __noinline__ uint32_t first_pass(const Shared& s, float m) {
+    uint32_t first = 0;
+    own_groups<T, VEC>(s, m, [&](float, int v) { first = max(first, (uint32_t)(s.row.V - v)); });
+    return first;
+}
+
 // Lists the tokens that reach the bound.
 template <typename T, bool VEC>
-__device__ __noinline__ void list_pass(Shared& s, const float (&group)[PIECES], float bound) {
-    for_groups<T, VEC>(s.row, s.lut, group, bound, [&](float x, int v) {
+__device__ __noinline__ void list_pass(Shared& s, float bound) {
+    own_groups<T, VEC>(s, bound, [&](float x, int v) {
         const int at = atomicAdd(&s.n, 1);
         if (at < LIST) s.key[at] = ordered(x), s.token[at] = v;
     });
 }
 
-struct Settings {
-    const float* uniform;
-    const float* temperature;
-    const int32_t* top_k;
-    const float* top_p;
-    const float* min_p;
+// The blocks of a row: one (LIGHT), or a cluster.
+template <bool LIGHT>
+struct Blocks {
+    __device__ __forceinline__ int rank() const { return LIGHT ? 0 : (int)cg::this_cluster().block_rank(); }
+    __device__ __forceinline__ int count() const { return LIGHT ? 1 : (int)cg::this_cluster().num_blocks(); }
+    __device__ __forceinline__ void sync() const {
+        if (count() > 1) cg::this_cluster().sync();
+        else __syncthreads();
+    }
+    __device__ __forceinline__ const Shared* peer(Shared& s, int q) const {
+        return count() > 1 ? cg::this_cluster().map_shared_rank(&s, q) : &s;
+    }
+    // the largest of two values over the blocks
+    __device__ __forceinline__ uint2 max2(Shared& s, uint32_t x, uint32_t y, int slot) const {
+        uint2 v = block_max(s, x, y);
+        const int n = count();
+        if (n > 1) {
+            if (threadIdx.x == 0) s.part[slot] = (u64)v.x << 32 | v.y;
+            sync();
+#pragma unroll
+            for (int q = 0; q < MAX_CLUSTER; q++)
+                if (q < n) {
+                    const u64 o = peer(s, q)->part[slot];
+                    v = make_uint2(max(v.x, (uint32_t)(o >> 32)), max(v.y, (uint32_t)o));
+                }
+        }
+        return v;
+    }
+    // sum of v over the blocks' threads; over those of earlier blocks; over this block's
+    __device__ __forceinline__ u64 sum(Shared& s, u64 v, int slot, u64* lower, u64* own) const {
+        block_before(s, v, own);
+        *lower = 0;
+        const int n = count(), me = rank();
+        if (n == 1) return *own;
+        if (threadIdx.x == 0) s.part[slot] = *own;
+        sync();
+        u64 all = 0;
+#pragma unroll
+        for (int q = 0; q < MAX_CLUSTER; q++) {
+            const u64 w = q < n ? peer(s, q)->part[slot] : 0ull;
+            if (q < me) *lower += w;
+            all += w;
+        }
+        return all;
+    }
+    // the blocks' bin of this thread's number, summed
+    __device__ __forceinline__ u64 bin(Shared& s, bool weights) const {
+        const int n = count();
+        u64 v = 0;
+#pragma unroll
+        for (int q = 0; q < MAX_CLUSTER; q++)
+            if (q < n) v += weights ? bin_weight(*peer(s, q), threadIdx.x) : (u64)peer(s, q)->bins[threadIdx.x];
+        return v;
+    }
 };
+
+template <bool LIGHT>
+__device__ __forceinline__ void finish(const Shared& s, int token, float lp) {
+    const Job& j = s.job;
+    j.tokens[s.st.b] = token;
+    if (j.logprobs) j.logprobs[s.st.b] = lp;
+    if (LIGHT) j.pending[s.st.b] = 0;
+}
+__device__ __forceinline__ float log_prob(const Weigh& g, float x, u64 sum) {
+    return g.z(x) - logf((float)sum * 0x1p-40f);
+}
+
+// From the groups' maxima: the largest candidate (-inf: none) and the smallest of them.
+template <bool LIGHT>
+__device__ __noinline__ float find_ends(Shared& s) {
+    uint32_t top = 0, low = 0;              // low: ~order, so that the largest is the lowest maximum
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) {
+        const float x = s.group[q][threadIdx.x];
+        top = max(top, ordered(x));
+        if (x > NEG_INF) low = max(low, ~ordered(x));
+    }
+    const uint2 ends = Blocks<LIGHT>().max2(s, top, low, 0);
+    if (threadIdx.x == 0) s.st.m = unordered(ends.x), s.st.lowest = unordered(~ends.y);
+    __syncthreads();
+    return unordered(ends.x);
+}
+
+// After first_pass: the greedy choice.
+template <bool LIGHT>
+__device__ __noinline__ void finish_greedy(Shared& s, uint32_t first) {
+    const Blocks<LIGHT> blocks;
+    const uint32_t all = blocks.max2(s, first, 0, 1).x;
+    if (blocks.rank() == 0 && threadIdx.x == 0) finish<LIGHT>(s, s.row.V - (int)all, 0.f);
+    blocks.sync();                          // peers may still read this block's shared memory
+}
+
+// After sum_pass: the weight that the nucleus has to hold.
+__device__ __noinline__ u64 find_limit(Shared& s, u64 all) {
+    u64 lower, own;
+    return limit_of(s, Blocks<false>().sum(s, all, 3, &lower, &own));
+}
+
+// A bound that at least `want` groups reach, or no bound when there are fewer groups.
+template <bool LIGHT>
+__device__ __noinline__ void find_bound(Shared& s, int want) {
+    const Blocks<LIGHT> blocks;
+    const float m = s.st.m, range = m - s.st.lowest, scale = BINS / range;
+#pragma unroll
+    for (int q = 0; q < PIECES; q++) {
+        const float x = s.group[q][threadIdx.x];
+        if (x > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - x) * scale))], 1u);
+    }
+    blocks.sync();
+    u64 groups;
+    const u64 v = blocks.bin(s, false), before = block_before(s, v, &groups);
+    // a little below the bin's lower edge: the bins' own arithmetic is rounded
+    float bound = -FLT_BIG;
+    if (groups >= want) bound = m - (threadIdx.x + 1) * (range / BINS) * 1.001f - fabsf(m) * 0x1p-20f;
+    if (groups < want ? threadIdx.x == 0 : before < want && before + v >= want)
+        s.st.bound = fmaxf(bound, -FLT_BIG);        // not NaN, not -inf
+    __syncthreads();
+}
+
+// The first block gathers the blocks' lists and weighs what is listed.
+template <bool LIGHT>
+__device__ __noinline__ void weigh_list(Shared& s) {
+    const Blocks<LIGHT> blocks;
+    blocks.sync();
+    if (blocks.rank() == 0) {
+        cg::cluster_group cl = cg::this_cluster();
+        const int n = gather(cl, s, blocks.count());
+        const Weigh g = s.g;
+        u64 w = 0, listed = 0;
+        if (n <= LIST) {
+            for (int i = threadIdx.x; i < n; i += NT) w += s.weight[i] = g.raw(unordered(s.key[i]));
+            block_before(s, w, &listed);
+        }
+        if (threadIdx.x == 0) s.st.n = n, s.st.listed = listed;
+        __syncthreads();
+    }
+}
+
+// The first block settles the row by its list: top-k of k, then a nucleus of `limit` (as for
+// settle).  What came of it, the same in all blocks; BOUNDED: s.g.tau is set.
+template <bool LIGHT>
+__device__ __noinline__ int settle_list(Shared& s, int k, u64 limit, int slot) {
+    const Blocks<LIGHT> blocks;
+    if (blocks.rank() == 0) {
+        int done = FAILED, place = -1;
+        u64 kept;
+        // without top-k the nucleus has to end in the list
+        if (s.st.n <= LIST && (k || limit == ~0ull || limit <= s.st.listed))
+            done = settle(s, s.st.bound, k, limit, &kept, &place);
+        if (done == DRAWN && place >= 0)
+            finish<LIGHT>(s, (int)s.token[place], log_prob(s.g, unordered(s.key[place]), kept));
+        if (threadIdx.x == 0) s.part[slot] = (u64)s.tau << 32 | (uint32_t)done;
+    }
+    blocks.sync();
+    const u64 said = blocks.peer(s, 0)->part[slot];
+    if (threadIdx.x == 0 && (int)said == BOUNDED) s.g.tau = unordered((uint32_t)(said >> 32));
+    blocks.sync();                          // also: the first block's shared memory has been read
+    return (int)said;
+}
+
+// From a sample of the weights below the bound: where the nucleus is expected to end.  Estimated
+// is the share of the weight below the bound that it holds: an error of the sample's total
+// moves that by (1 - p) of itself only.  The slack is three to four times what samples of these
+// sizes were seen to be off.
+template <typename T, bool VEC>
+__device__ __noinline__ void find_stretch(Shared& s) {
+    const Blocks<false> blocks;
+    if (blocks.rank() == 0 && threadIdx.x == 0) s.part[4] = s.st.n <= LIST ? s.st.listed : 0;
+    s.bins[threadIdx.x] = 0;
+    blocks.sync();
+    const float in_list = to_float(blocks.peer(s, 0)->part[4]), bound = s.st.bound;
+    // bins of z; weights in units of the bound's / 2^16
+    const float unit = 65536.f / fmaxf(s.g.e(bound), 1e-37f), top_z = fmaxf(s.g.z(bound), Z_END + 1.f);
+    const float to_bin = BINS / (top_z - Z_END);
+    const int full = s.job.per_block / CHUNK;
+    const int taken = min(PIECES, max(1, full / (2 * NW)));     // an eighth, or a piece per warp
+    sample_pass<T, VEC>(s, bound, unit, top_z, to_bin, taken);
+    blocks.sync();
+    u64 rest;
+    const u64 v = blocks.bin(s, false), upto = block_before(s, v, &rest) + v;
+    // sample units -> weights; the same in all blocks, also where the last one's part is short
+    const float ratio = (float)(full * PIECES) / (min(full, NW) * taken) * 0x1p40f / unit;
+    const float sampled = fmaxf(to_float(rest), 1e-30f), list_to_rest = in_list / fmaxf(sampled * ratio, 1e-30f);
+    const float p = s.st.p, share = p - (1.f - p) * list_to_rest;
+    const float slack = 0.08f * fmaxf(share, 0.f) * (1.f - share) + 0.06f * (1.f - p) * list_to_rest + 5e-4f;
+    if (threadIdx.x == 0) s.st.z_from = 1.f, s.st.z_to = Z_END, s.st.in_doubt = share + slack > 0.f;
+    __syncthreads();
+    const float till = to_float(upto) / sampled, prior = to_float(upto - v) / sampled;
+    if (threadIdx.x && till >= share - slack && prior < share - slack) s.st.z_from = top_z - threadIdx.x / to_bin;
+    if (threadIdx.x < BINS - 1 && till >= share + slack && prior < share + slack)
+        s.st.z_to = top_z - (threadIdx.x + 1) / to_bin;
+    blocks.sync();                          // and every block has read the bins
+    s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+    __syncthreads();
+}
+
+// After bins_pass: whether the nucleus ends in the stretch, in which bin, and after how much of it.
+__device__ __noinline__ void find_bin(Shared& s, u64 all, u64 above) {
+    const Blocks<false> blocks;
+    u64 lower, own, inside;
+    const u64 limit = limit_of(s, blocks.sum(s, all, 5, &lower, &own));
+    const u64 over = blocks.sum(s, above, 7, &lower, &own);
+    const u64 w = blocks.bin(s, true), till = over + block_before(s, w, &inside);
+    if (till < limit && limit <= till + w) s.st.bin = threadIdx.x, s.st.left = limit - till;
+    if (threadIdx.x == 0) s.n = 0, s.st.hit = limit > over && limit <= over + inside;
+    blocks.sync();                          // and every block has read the bins
+    s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+    __syncthreads();
+}
+
+// After bin_pass (ends: of the values in the bin): the value at which the nucleus ends, 0 where
+// the list does not tell.
+__device__ __noinline__ uint32_t find_tau(Shared& s, uint2 ends, bool* by_list) {
+    const Blocks<false> blocks;
+    const uint2 all = blocks.max2(s, ends.x, ~ends.y, 6);
+    blocks.sync();
+    if (threadIdx.x == 0) s.st.own = min(s.n, LIST);
+    if (blocks.rank() == 0) {
+        cg::cluster_group cl = cg::this_cluster();
+        const int n = gather(cl, s, blocks.count());
+        uint32_t tau = 0;
+        if (n <= LIST) {
+            const Weigh g = s.g;
+            for (int i = threadIdx.x; i < n; i += NT) s.weight[i] = g.raw(unordered(s.key[i]));
+            __syncthreads();
+            tau = list_search(cl, s, n, s.st.left);
+        }
+        if (threadIdx.x == 0) s.part[8] = tau;
+    }
+    blocks.sync();
+    const uint32_t tau = (uint32_t)blocks.peer(s, 0)->part[8];
+    *by_list = tau != 0;
+    return tau ? tau : all.x == ~all.y ? all.x : 0u;    // equal values need no list
+}
+
+// The chunks' sums hold what lies above the bin: adds the bin's own tokens that stay.
+__device__ __noinline__ void add_own(Shared& s, u64* chunk_sum, uint32_t tau) {
+    const Weigh g = s.g;
+    for (int i = threadIdx.x; i < s.st.own; i += NT)
+        if (s.key[i] >= tau) atomicAdd(&chunk_sum[((int)s.token[i] - s.row.lo) / CHUNK], g.raw(unordered(s.key[i])));
+    __syncthreads();
+}
+
+// The draw from the chunks' sums: the block, the chunk and the token that hold the target.
+template <typename T, bool VEC>
+__device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
+    const Blocks<false> blocks;
+    const Row r = s.row;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
+    const int per = (n_chunks + NT - 1) / NT, c0 = min(n_chunks, (int)threadIdx.x * per), c1 = min(n_chunks, c0 + per);
+    u64 mine = 0, total, lower;
+    for (int c = c0; c < c1; c++) mine += chunk_sum[c];
+    u64 before = block_before(s, mine, &total);
+    const u64 sum = blocks.sum(s, mine, 9, &lower, &total), target = part_of(sum, s.st.u24);
+    if (target >= lower && target < lower + total) {
+        const u64 t = target - lower;
+        if (t >= before && t < before + mine) {
+            int c = c0;
+            while (before + chunk_sum[c] <= t) before += chunk_sum[c++];
+            s.at = c;
+            s.found[1] = t - before;
+        }
+        __syncthreads();
+        // a warp per piece of the chunk
+        const Weigh g = s.g;
+        const int v0 = r.lo + s.at * CHUNK + warp * 256 + lane * 8;
+        u64 w[8], in = 0, all;
+        Piece<T> q;
+        if (warp < PIECES) {
+            const uint32_t bits = piece_bits<T, VEC>(r, v0);
+            read_piece<T, VEC>(r, v0, bits, q);
+            mask_piece<T>(s.lut, bits, q);
+#pragma unroll
+            for (int i = 0; i < 8; i++) in += w[i] = g.kept(q.get(i));
+        }
+        u64 till = block_before(s, in, &all);
+        const u64 left = s.found[1];
+        if (left >= till && left < till + in) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                if (left >= till && left < till + w[i]) finish<false>(s, v0 + i, log_prob(g, q.get(i), sum));
+                till += w[i];
+            }
+        }
+    }
+}
 
 // A cluster of blocks per row, each with a contiguous part of the vocabulary.
 //
@@ -825,391 +1183,249 @@ struct Settings {
 // go to bins, and the bin in which the nucleus ends is listed by a third pass.  The
 // estimate decides only what is looked at: whatever it misses is searched digit by digit
 // over the whole row.  What no list holds is drawn from sums by chunk.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(NT, 2) k_sample(const T* logits, int64_t stride, int V, int per_block,
-                                                  const uint32_t* bitmask, int W, Settings S, int32_t* tokens,
-                                                  float* logprobs) {
-    extern __shared__ __align__(16) uint8_t dyn[];
-    Shared& s = *reinterpret_cast<Shared*>(dyn);
-    u64* chunk_sum = reinterpret_cast<u64*>(dyn + sizeof(Shared));
-    cg::cluster_group cl = cg::this_cluster();
-    const int rank = (int)cl.block_rank(), n_blocks = (int)cl.num_blocks();
-    const int b = blockIdx.x / n_blocks;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+//
+// Rows that need no weights of all tokens (greedy, top-k, min-p alone) and those that do
+// differ tenfold in time and want different splits, so a batch whose settings may hold both is
+// done by two kernels: k_sample_light, a block per row, does the first kind and marks the
+// others, which k_sample, a cluster per row, then does.  LIGHT: without what those need.
+template <typename T, bool VEC, bool LIGHT>
+__device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
+    const Blocks<LIGHT> blocks;
+    State& st = s.st;
+    {
+        const Job& j = s.job;
+        const Settings& S = j.settings;
+        const float temp = S.temperature ? S.temperature[b] : 1.f, p = S.top_p ? S.top_p[b] : 1.f;
+        const float min_e = S.min_p && S.min_p[b] > 0.f ? fminf(S.min_p[b], 1.f) : 0.f;
+        const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < j.V ? S.top_k[b] : 0;
+        if (LIGHT && temp >= 1e-6f && !k && (p < 1.f || !(min_e > 0.f))) {
+            if (threadIdx.x == 0) j.pending[b] = 1;
+            return;
+        }
+        s.bins[threadIdx.x] = 0;
+        if (threadIdx.x == 0) {
+            const float u = S.uniform[b];
+            s.n = 0;
+            st.b = b, st.k = k, st.p = p;
+            st.p24 = p < 1.f ? __float2uint_rn(fmaxf(p, 0.f) * 0x1p24f) : 0u;
+            st.u24 = u > 0.f ? min(0xffffffu, __float2uint_rz(fminf(u, 1.f) * 0x1p24f)) : 0u;
+            s.g = Weigh{0.f, temp >= 1e-6f ? __fdiv_rn(1.f, temp) : 0.f, NEG_INF, min_e};
+            s.row = Row{static_cast<const T*>(j.logits) + (size_t)b * j.stride,
+                        j.bitmask ? reinterpret_cast<const uint8_t*>(j.bitmask + (size_t)b * j.W) : nullptr, j.V,
+                        min(j.V, blocks.rank() * j.per_block), min(j.V, (blocks.rank() + 1) * j.per_block)};
+        }
+    }
+    __syncthreads();
+    const int odd = __syncthreads_or(max_pass<T, VEC>(s));      // a NaN or +inf among the block's candidates
+    const float m = find_ends<LIGHT>(s);
+    if (m == NEG_INF) {                     // nothing to choose from
+        if (blocks.rank() == 0 && threadIdx.x == 0) finish<LIGHT>(s, -1, NEG_INF);
+        blocks.sync();                      // peers may still read this block's shared memory
+        return;
+    }
+    if (s.g.inv == 0.f) {                   // greedy
+        finish_greedy<LIGHT>(s, first_pass<T, VEC>(s, m));
+        return;
+    }
+    if (threadIdx.x == 0) {
+        s.g.m = m;
+        // min-p alone: a little below the value at which e^z is min_e
+        st.bound = fmaxf(m + (logf(s.g.min_e) * 1.0001f - 1e-4f) / s.g.inv - fabsf(m) * 0x1p-20f, -FLT_BIG);
+    }
+    __syncthreads();
+    const bool nucleus = st.p < 1.f;
+    bool summed = false;                    // chunk_sum holds what stays
+    if (st.k || nucleus || s.g.min_e > 0.f) {
+        if (st.k || nucleus) find_bound<LIGHT>(s, st.k ? st.k : NUCLEUS_GROUPS);
+        list_pass<T, VEC>(s, st.bound);
+        weigh_list<LIGHT>(s);
+        if (LIGHT || st.k || !nucleus) {    // the list holds all that is needed
+            const int done = settle_list<LIGHT>(s, st.k, st.p < 1.f ? 0 : ~0ull, 2);
+            if (done == DRAWN) return;
+            if (LIGHT) {
+                if (threadIdx.x == 0) s.job.pending[st.b] = 1;
+                return;
+            }
+            if constexpr (!LIGHT) {
+                if (done == FAILED && st.k) {           // too many for the list
+                    row_search<false, T, VEC>(s);
+                    if (st.p < 1.f) row_search<true, T, VEC>(s);
+                }
+            }
+        } else if constexpr (!LIGHT) {
+            bool found = false;
+            find_stretch<T, VEC>(s);
+            if (!st.in_doubt) {             // expected inside the list: the sum of all weights is what it wants
+                const int done = settle_list<false>(s, 0, find_limit(s, sum_pass<T, VEC>(s, odd)), 2);
+                if (done == DRAWN) return;
+                found = done == BOUNDED;
+                if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END;
+                s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+                __syncthreads();
+            }
+            // The stretch looked at closely; where the nucleus does not end in it the whole row
+            // is, and where its bin holds more than a list that bin is the next stretch.
+            for (int turn = 0; turn < 6 && !found; turn++) {
+                u64 above;
+                const u64 all = bins_pass<T, VEC>(s, chunk_sum, odd, Stretch(st.z_from, st.z_to), &above);
+                find_bin(s, all, above);
+                if (!st.hit) {              // the same in all blocks
+                    if (st.z_from == 1.f && st.z_to == Z_END) break;
+                    __syncthreads();
+                    if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END;
+                    __syncthreads();
+                    continue;
+                }
+                bool by_list;
+                const uint32_t tau = find_tau(s, bin_pass<T, VEC>(s, chunk_sum, odd, Stretch(st.z_from, st.z_to), st.bin),
+                                              &by_list);
+                if (threadIdx.x == 0) {
+                    if (tau) {
+                        s.g.tau = unordered(tau);
+                    } else {                // the bin's edges, a little apart
+                        const Stretch t(st.z_from, st.z_to);
+                        const float off = 1e-4f / t.fine + 4e-6f * (1.f - t.top + st.bin / t.fine);
+                        if (st.bin) st.z_from = t.top - st.bin / t.fine + off;
+                        st.z_to = fmaxf(t.top - (st.bin + 1) / t.fine - off, Z_END);
+                    }
+                }
+                __syncthreads();
+                found = tau != 0;
+                if (by_list && !(s.g.min_e > 0.f)) {
+                    add_own(s, chunk_sum, tau);
+                    summed = true;
+                }
+            }
+            if (!found) row_search<true, T, VEC>(s);
+        }
+    }
+    if constexpr (!LIGHT) {                 // every light row has a list
+        if (!summed) {
+            if (s.g.tau > NEG_INF || s.g.min_e > 0.f) chunk_pass<T, VEC, true>(s, chunk_sum, odd);
+            else chunk_pass<T, VEC, false>(s, chunk_sum, odd);
+            __syncthreads();
+        }
+        draw<T, VEC>(s, chunk_sum);
+        blocks.sync();                      // peers may still read this block's shared memory
+    }
+}
+
+__device__ __forceinline__ void set_up(Shared& s) {
     if (threadIdx.x < 256) {
         auto pair = [&](int i) {
             return ((threadIdx.x >> i) & 1) * 0x0000ffffu + ((threadIdx.x >> (i + 1)) & 1) * 0xffff0000u;
         };
         s.lut[threadIdx.x] = make_uint4(pair(0), pair(2), pair(4), pair(6));
     }
-    s.bins[threadIdx.x] = 0;
+    __syncthreads();
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(NT, 2) k_sample_light(const __grid_constant__ Job j) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    Shared& s = *reinterpret_cast<Shared*>(dyn);
     s.turn[threadIdx.x] = 0;
-    if (threadIdx.x == 0) s.n = 0;
+    if (threadIdx.x == 0) s.job = j;
+    dep_wait();
+    dep_launch();
+    set_up(s);
+    sample_row<T, VEC, true>(s, nullptr, blockIdx.x);
+}
+
+// The i-th row that `pending` marks (that is there, where it is NULL), -1 past the last.
+__device__ __forceinline__ int find_row(Shared& s, int i) {
+    const Job& j = s.job;
+    if (!j.pending) return i;
+    // a thread's share of the rows, and how many are marked before it
+    const int per = (j.B + NT - 1) / NT, from = min(j.B, (int)threadIdx.x * per), to = min(j.B, from + per);
+    u64 total;
+    int own = 0;
+    for (int b = from; b < to; b++) own += j.pending[b];
+    const int before = (int)block_before(s, own, &total);
+    if (i >= (int)total) return -1;
+    if (i >= before && i < before + own) {
+        int left = i - before, b = from;
+        for (; !j.pending[b] || left--; b++) {}
+        s.at = b;
+    }
+    __syncthreads();
+    return s.at;
+}
+
+// A cluster for each row that `pending` marks (all of them where it is NULL).  No loop over rows:
+// with one the compiler leaves the passes too few registers.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(NT, 2) k_sample(const __grid_constant__ Job j) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    Shared& s = *reinterpret_cast<Shared*>(dyn);
+    s.turn[threadIdx.x] = 0;
+    if (threadIdx.x == 0) s.job = j;
     dep_wait();
     dep_launch();
     __syncthreads();
-
-    const Row r{logits + (size_t)b * stride, bitmask ? reinterpret_cast<const uint8_t*>(bitmask + (size_t)b * W) : nullptr,
-                V, min(V, rank * per_block), min(V, (rank + 1) * per_block)};
-    if (threadIdx.x == 0) s.row = r;
-    const int n_chunks = (r.hi - r.lo + CHUNK - 1) / CHUNK;
-    auto sync = [&]() {
-        if (n_blocks > 1) cl.sync();
-        else __syncthreads();
-    };
-    auto peer = [&](int q) -> const Shared* { return n_blocks > 1 ? cl.map_shared_rank(&s, q) : &s; };
-    // the largest of two values over the cluster
-    auto combine_max = [&](uint32_t x, uint32_t y, int slot) {
-        uint2 v = block_max(s, x, y);
-        if (n_blocks > 1) {
-            if (threadIdx.x == 0) s.part[slot] = (u64)v.x << 32 | v.y;
-            cl.sync();
-#pragma unroll
-            for (int q = 0; q < MAX_CLUSTER; q++)
-                if (q < n_blocks) {
-                    const u64 o = peer(q)->part[slot];
-                    v = make_uint2(max(v.x, (uint32_t)(o >> 32)), max(v.y, (uint32_t)o));
-                }
-        }
-        return v;
-    };
-    // sum of v over the cluster, and over the blocks before this one
-    auto combine_sum = [&](u64 v, int slot, u64* lower) {
-        u64 total;
-        block_before(s, v, &total);
-        *lower = 0;
-        if (n_blocks == 1) return total;
-        if (threadIdx.x == 0) s.part[slot] = total;
-        sync();
-        u64 sum = 0;
-        *lower = 0;
-#pragma unroll
-        for (int q = 0; q < MAX_CLUSTER; q++) {
-            const u64 w = q < n_blocks ? peer(q)->part[slot] : 0ull;
-            if (q < rank) *lower += w;
-            sum += w;
-        }
-        return sum;
-    };
-    auto finish = [&](int token, float lp) {
-        tokens[b] = token;
-        if (logprobs) logprobs[b] = lp;
-    };
-
-    // pass 1
-    float group[PIECES];
-#pragma unroll
-    for (int u = 0; u < PIECES; u++) group[u] = NEG_INF;
-    int odd = 0;                            // a NaN or +inf among the block's candidates
-    for_pieces<T, VEC, true>(r, s.lut, [&](const Piece<T>& p, int, int q, bool) {
-        float x = p.max8_nan();
-        if (!(x <= FLT_BIG)) odd = 1, x = p.max8();
-        group[q] = fmaxf(group[q], x);
-    }, [](int) {});
-    odd = __syncthreads_or(odd);
-    uint32_t top = 0, low = 0;              // low: ~order, so that the largest is the lowest maximum
-#pragma unroll
-    for (int u = 0; u < PIECES; u++) {
-        group[u] = clean(group[u]);
-        top = max(top, ordered(group[u]));
-        if (group[u] > NEG_INF) low = max(low, ~ordered(group[u]));
-    }
-    const uint2 ends = combine_max(top, low, 0);
-    const float m = unordered(ends.x);
-    if (m == NEG_INF) {                     // nothing to choose from
-        if (rank == 0 && threadIdx.x == 0) finish(-1, NEG_INF);
-        sync();
-        return;
-    }
-    const float temp = S.temperature ? S.temperature[b] : 1.f;
-    if (!(temp >= 1e-6f)) {                 // greedy
-        uint32_t first = 0;                 // V - token, so that the largest is the lowest token
-        for_groups<T, VEC>(r, s.lut, group, m, [&](float, int v) { first = max(first, (uint32_t)(V - v)); });
-        const uint32_t all = combine_max(first, 0, 1).x;
-        if (rank == 0 && threadIdx.x == 0) finish(V - (int)all, 0.f);
-        sync();                             // peers may still read this block's shared memory
-        return;
-    }
-
-    Weigh g{m, __fdiv_rn(1.f, temp), NEG_INF, S.min_p && S.min_p[b] > 0.f ? fminf(S.min_p[b], 1.f) : 0.f};
-    if (threadIdx.x == 0) s.g = g;          // a barrier follows before any pass reads it
-    const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < V ? S.top_k[b] : 0;
-    const float p = S.top_p ? S.top_p[b] : 1.f;
-    const bool nucleus = p < 1.f;
-    const u64 p24 = nucleus ? __float2uint_rn(fmaxf(p, 0.f) * 0x1p24f) : 0u;
-    const float uf = S.uniform[b];
-    const u64 u24 = uf > 0.f ? min(0xffffffu, __float2uint_rz(fminf(uf, 1.f) * 0x1p24f)) : 0u;
-    auto limit_of = [&](u64 total) { return max((u64)1, part_of(total, p24)); };
-
-    bool summed = false;                    // chunk_sum holds what stays
-    if (k || nucleus || g.min_e > 0.f) {
-        float bound;
-        if (k || nucleus) {
-            // a bound that at least `want` groups reach, or no bound when there are fewer groups
-            const float range = m - unordered(~ends.y), scale = BINS / range;
-#pragma unroll
-            for (int u = 0; u < PIECES; u++)
-                if (group[u] > NEG_INF) atomicAdd(&s.bins[min(BINS - 1, (int)fmaxf(0.f, (m - group[u]) * scale))], 1u);
-            sync();
-            u64 v = 0, groups;
-#pragma unroll
-            for (int q = 0; q < MAX_CLUSTER; q++)
-                if (q < n_blocks) v += peer(q)->bins[threadIdx.x];
-            const u64 before = block_before(s, v, &groups), want = k ? k : NUCLEUS_GROUPS;
-            if (groups < want) {
-                if (threadIdx.x == 0) s.at = BINS;
-            } else if (before < want && before + v >= want) {
-                s.at = threadIdx.x;
-            }
-            __syncthreads();
-            // a little below the bin's lower edge: the bins' own arithmetic is rounded
-            bound = s.at == BINS ? -FLT_BIG : m - (s.at + 1) * (range / BINS) * 1.001f - fabsf(m) * 0x1p-20f;
-        } else {
-            // a little below the value at which e^z is min_e
-            bound = m + (logf(g.min_e) * 1.0001f - 1e-4f) * temp - fabsf(m) * 0x1p-20f;
-        }
-        bound = fmaxf(bound, -FLT_BIG);     // not NaN, not -inf
-        list_pass<T, VEC>(s, group, bound);
-        sync();
-        // the first block gathers the lists and weighs what is listed
-        u64 listed = 0;
-        int n = 0;
-        if (rank == 0) {
-            n = gather(cl, s, n_blocks);
-            u64 w = 0;
-            if (n <= LIST) {
-                for (int i = threadIdx.x; i < n; i += NT) w += s.weight[i] = g.raw(unordered(s.key[i]));
-                block_before(s, w, &listed);
-            }
-        }
-        if (k || !nucleus) {                // the list holds all that is needed
-            if (rank == 0) {
-                int done = FAILED, i = -1;
-                u64 kept;
-                if (n <= LIST)
-                    done = settle(s, g, bound, V, n, k, listed, nucleus ? 0 : ~0ull, limit_of, u24, &kept, &i);
-                if (done == DRAWN && i >= 0)
-                    finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
-                if (threadIdx.x == 0) s.part[4] = done, s.part[10] = s.tau;
-            }
-            sync();
-            const int done = (int)peer(0)->part[4];
-            if (done == DRAWN) {
-                sync();
-                return;
-            }
-            if (done == BOUNDED) {
-                g.tau = unordered((uint32_t)peer(0)->part[10]);
-            } else if (k) {                        // too many for the list: digit by digit (fewer than k candidates: all stay)
-                g.tau = row_search<false, T, VEC>(cl, s, r, g, n_blocks, [&](u64 all) { return min((u64)k, all); });
-                if (nucleus) g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
-            }
-        } else {
-            // Where the list ends and the nucleus may not, from a sample of the row: the
-            // weights below the bound in BINS bins of z, in units of the bound's weight / 2^16.
-            if (rank == 0 && threadIdx.x == 0) s.part[4] = n <= LIST ? listed : 0;
-            s.bins[threadIdx.x] = 0;
-            sync();
-            const float in_list = to_float(peer(0)->part[4]);
-            const float unit = 65536.f / fmaxf(g.e(bound), 1e-37f), top_z = fmaxf(g.z(bound), Z_END + 1.f);
-            const float to_bin = BINS / (top_z - Z_END);
-            const int full = per_block / CHUNK;
-            const int taken = min(PIECES, max(1, full / (2 * NW)));     // an eighth, or a piece per warp
-            sample_pass<T, VEC>(s, bound, unit, top_z, to_bin, taken);
-            sync();
-            u64 v = 0, rest;
-#pragma unroll
-            for (int q = 0; q < MAX_CLUSTER; q++)
-                if (q < n_blocks) v += peer(q)->bins[threadIdx.x];
-            const u64 upto = block_before(s, v, &rest) + v;
-            // sample units -> weights; the same in all blocks, also where the last one's part is short
-            const float ratio = (float)(full * PIECES) / (min(full, NW) * taken) * 0x1p40f / unit;
-            // The share of the weight below the bound that the nucleus holds: estimated well, since
-            // an error of the sample's total moves it by (1 - p) of that only.  The slack is
-            // three to four times what samples of these sizes were seen to be off.
-            const float sampled = fmaxf(to_float(rest), 1e-30f), list_to_rest = in_list / fmaxf(sampled * ratio, 1e-30f);
-            const float share = p - (1.f - p) * list_to_rest;
-            const float slack = 0.08f * fmaxf(share, 0.f) * (1.f - share) + 0.06f * (1.f - p) * list_to_rest + 5e-4f;
-            if (threadIdx.x == 0) s.from = 0, s.to = BINS;
-            __syncthreads();
-            const float mine = to_float(upto) / sampled, prior = to_float(upto - v) / sampled;
-            if (mine >= share - slack && prior < share - slack) s.from = threadIdx.x;
-            if (mine >= share + slack && prior < share + slack) s.to = threadIdx.x + 1;
-            __syncthreads();
-            const bool in_doubt = share + slack > 0.f;
-            // the stretch of z in which the nucleus is expected to end
-            float z_from = s.from == 0 ? 1.f : top_z - s.from / to_bin;
-            float z_to = s.to >= BINS ? Z_END : top_z - s.to / to_bin;
-            u64 lower, total = 0, limit = 0;
-            bool found = false;
-            if (!in_doubt) {                // expected inside the list: the sum of all weights is what it wants
-                total = combine_sum(sum_pass<T, VEC>(s, odd), 5, &lower), limit = limit_of(total);
-                if (rank == 0) {
-                    int done = FAILED, i = -1;
-                    u64 kept;
-                    if (n <= LIST && limit <= listed)
-                        done = settle(s, g, bound, V, n, 0, listed, limit, limit_of, u24, &kept, &i);
-                    if (done == DRAWN && i >= 0)
-                        finish((int)s.token[i], g.z(unordered(s.key[i])) - logf((float)kept * 0x1p-40f));
-                    if (threadIdx.x == 0) s.part[6] = done, s.part[10] = s.tau;
-                }
-                sync();
-                const int done = (int)peer(0)->part[6];
-                if (done == DRAWN) {
-                    sync();
-                    return;
-                }
-                if (done == BOUNDED) g.tau = unordered((uint32_t)peer(0)->part[10]), found = true;
-                z_from = 1.f, z_to = Z_END;
-            }
-            // The stretch looked at closely; where the nucleus does not end in it the whole row
-            // is, and where its bin holds more than a list that bin is the next stretch.
-            for (int turn = 0; turn < 6 && !found; turn++) {
-                Stretch t;
-                t.z_from = z_from, t.z_to = z_to;
-                t.top = fminf(t.z_from, 0.f), t.fine = BINS / fmaxf(t.top - t.z_to, 1e-3f);
-                sync();                     // every block has read the bins
-                s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
-                __syncthreads();
-                u64 above;
-                total = combine_sum(bins_pass<T, VEC>(s, chunk_sum, odd, t, &above), 5, &lower);
-                limit = limit_of(total);
-                const u64 over = combine_sum(above, 7, &lower);
-                u64 w = 0, inside;
-#pragma unroll
-                for (int q = 0; q < MAX_CLUSTER; q++)
-                    if (q < n_blocks) w += bin_weight(*peer(q), threadIdx.x);
-                const u64 till = over + block_before(s, w, &inside);
-                if (till < limit && limit <= till + w) s.at = threadIdx.x, s.found[0] = limit - till;
-                if (threadIdx.x == 0) s.n = 0;
-                __syncthreads();
-                if (!(limit > over && limit <= over + inside)) {            // the same in all blocks
-                    if (z_from == 1.f && z_to == Z_END) break;
-                    z_from = 1.f, z_to = Z_END;
-                    continue;
-                }
-                const int bin = s.at;
-                const u64 left = s.found[0];
-                // the bin's tokens, and the value among them at which the nucleus ends
-                const uint2 mine = bin_pass<T, VEC>(s, chunk_sum, odd, t, bin), ends = combine_max(mine.x, ~mine.y, 11);
-                sync();
-                const int own = min(s.n, LIST);
-                if (rank == 0) {
-                    uint32_t tau = 0;
-                    if ((n = gather(cl, s, n_blocks)) <= LIST) {
-                        for (int i = threadIdx.x; i < n; i += NT) s.weight[i] = g.raw(unordered(s.key[i]));
-                        __syncthreads();
-                        tau = list_search(cl, s, n, left);
-                    }
-                    if (threadIdx.x == 0) s.part[8] = tau;
-                }
-                sync();
-                const uint32_t listed_tau = (uint32_t)peer(0)->part[8];
-                // equal values need no list
-                const uint32_t tau = listed_tau ? listed_tau : ends.x == ~ends.y ? ends.x : 0u;
-                if (!tau) {                 // the bin holds more than a list: its edges, a little apart
-                    const float off = 1e-4f / t.fine + 4e-6f * (1.f - t.top + bin / t.fine);
-                    z_from = bin ? t.top - bin / t.fine + off : t.z_from;
-                    z_to = fmaxf(t.top - (bin + 1) / t.fine - off, Z_END);
-                    continue;
-                }
-                g.tau = unordered(tau), found = true;
-                if (listed_tau && !(g.min_e > 0.f)) {   // the chunks' sums want only the bin's own tokens
-                    for (int i = threadIdx.x; i < own; i += NT)
-                        if (s.key[i] >= tau)
-                            atomicAdd(&chunk_sum[((int)s.token[i] - r.lo) / CHUNK], g.raw(unordered(s.key[i])));
-                    summed = true;
-                    __syncthreads();
-                }
-            }
-            if (!found) g.tau = row_search<true, T, VEC>(cl, s, r, g, n_blocks, limit_of);
-        }
-    }
-
-    // the draw: weights by chunk, then the block, the chunk and the token that hold the target
-    __syncthreads();
-    if (threadIdx.x == 0) s.g = g;          // with its threshold
-    __syncthreads();
-    if (!summed) {
-        if (g.tau > NEG_INF || g.min_e > 0.f) chunk_pass<T, VEC, true>(s, chunk_sum, odd);
-        else chunk_pass<T, VEC, false>(s, chunk_sum, odd);
-    }
-    __syncthreads();
-    const int per = (n_chunks + NT - 1) / NT, c0 = min(n_chunks, (int)threadIdx.x * per), c1 = min(n_chunks, c0 + per);
-    u64 mine = 0, total, lower;
-    for (int c = c0; c < c1; c++) mine += chunk_sum[c];
-    u64 before = block_before(s, mine, &total);
-    const u64 sum = combine_sum(mine, 9, &lower);
-    const u64 target = part_of(sum, u24);
-    if (target >= lower && target < lower + total) {
-        const u64 t = target - lower;
-        if (t >= before && t < before + mine) {
-            int c = c0;
-            while (before + chunk_sum[c] <= t) before += chunk_sum[c++];
-            s.at = c;
-            s.found[1] = t - before;
-        }
-        __syncthreads();
-        // a warp per piece of the chunk
-        const int v0 = r.lo + s.at * CHUNK + warp * 256 + lane * 8;
-        u64 w[8], in = 0;
-        Piece<T> q;
-        if (warp < PIECES) {
-            const uint32_t bits = piece_bits<T, VEC>(r, v0);
-            read_piece<T, VEC>(r, v0, bits, q);
-            mask_piece<T>(s.lut, bits, q);
-#pragma unroll
-            for (int i = 0; i < 8; i++) in += w[i] = g.kept(q.get(i));
-        }
-        u64 all;
-        u64 till = block_before(s, in, &all);
-        const u64 left = s.found[1];
-        if (left >= till && left < till + in) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (left >= till && left < till + w[i])
-                    finish(v0 + i, g.z(q.get(i)) - logf((float)sum * 0x1p-40f));
-                till += w[i];
-            }
-        }
-    }
-    sync();                                 // peers may still read this block's shared memory
+    const int b = find_row(s, blockIdx.x / (int)cg::this_cluster().num_blocks());
+    if (b < 0) return;
+    set_up(s);
+    sample_row<T, VEC, false>(s, reinterpret_cast<u64*>(dyn + sizeof(Shared)), b);
 }
 
-template <typename T>
-psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
-                  int32_t* tokens, float* logprobs, cudaStream_t cs) {
-    // Two blocks run on an SM.  Rows are split until there are enough blocks for twice that,
-    // as long as most warps have a chunk; until the rows in flight leave half of the L2 to the
-    // later passes; and to 2^20 tokens a block (what WeightSum holds).
+// Blocks per row: two run on an SM.  Rows are split until there are blocks for all of them, as
+// long as most warps have a chunk; until the rows in flight leave room in the L2 for the later
+// passes; and to 2^20 tokens a block (what WeightSum holds).
+int split(int rows, int V, size_t bytes) {
     const int sms = current_sms();
     int cluster = 1;
     while (cluster < MAX_CLUSTER &&
-           (((int64_t)B * cluster < 4 * sms && V / (2 * cluster) >= NW * CHUNK * 3 / 4) || V / cluster > 1 << 20 ||
-            std::min<int64_t>(B, 2 * sms / cluster) * V * (int64_t)sizeof(T) > 128 << 20))
+           (((int64_t)rows * cluster < 2 * sms && V / (2 * cluster) >= NW * CHUNK * 3 / 4) || V / cluster > 1 << 20 ||
+            std::min<int64_t>(rows, 2 * sms / cluster) * V * (int64_t)bytes > 128 << 20))
         cluster *= 2;
-    const int per = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
-    const size_t smem = sizeof(Shared) + (size_t)(per / CHUNK) * 8;
+    return cluster;
+}
+
+// Batches of at least this many rows, with top-k or min-p, are done by two kernels.
+constexpr int TWO_KERNELS = 48;
+
+template <typename T>
+psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
+                  int32_t* tokens, float* logprobs, uint8_t* pending, cudaStream_t cs) {
     const bool vec = is_aligned(logits, stride * sizeof(T), 16);
-    return ops_launch(vec ? k_sample<T, true> : k_sample<T, false>, dim3((unsigned)B * cluster), NT, smem, cluster, cs,
-                      "k_sample", logits, stride, V, per, bitmask, (V + 31) / 32, S, tokens, logprobs);
+    const bool both = B >= TWO_KERNELS && V <= 1 << 20 && (S.top_k || S.min_p);
+    Job j{logits, stride, B, V, (V + CHUNK - 1) / CHUNK * CHUNK, (V + 31) / 32, bitmask, S, tokens, logprobs,
+          both ? pending : nullptr};
+    if (both) {
+        psc_status s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT, sizeof(Shared), 1,
+                                  cs, "k_sample_light", j);
+        if (s != PSC_OK) return s;
+    }
+    // of a mixed batch about a quarter is left
+    const int cluster = split(both ? (B + 3) / 4 : B, V, sizeof(T));
+    j.per_block = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
+    const size_t smem = sizeof(Shared) + (size_t)(j.per_block / CHUNK) * 8;
+    return ops_launch(vec ? k_sample<T, true> : k_sample<T, false>, dim3((unsigned)B * cluster), NT, smem, cluster,
+                      cs, "k_sample", j);
 }
 
 }  // namespace
 
+extern "C" int64_t psc_sample_work_bytes(int32_t B) { return B > 0 ? ((int64_t)B + 15) / 16 * 16 : 16; }
+
 extern "C" psc_status psc_sample(const void* d_logits, psc_dtype dtype, int64_t row_stride, int32_t B, int32_t V,
                                  const uint32_t* d_bitmask, const float* d_uniform, const float* d_temperature,
                                  const int32_t* d_top_k, const float* d_top_p, const float* d_min_p,
-                                 int32_t* d_tokens, float* d_logprobs, void* stream) {
+                                 int32_t* d_tokens, float* d_logprobs, void* d_work, int64_t work_bytes,
+                                 void* stream) {
     const char* me = "psc_sample";
     if (B < 0 || V <= 0 || row_stride < V || !is_dtype(dtype) || (B && (!d_logits || !d_uniform || !d_tokens)))
         return ops_fail(PSC_ERR_ARG, me, "bad arguments");
     if (V > MAX_V) return ops_fail(PSC_ERR_LIMIT, me, "vocabulary over 4,194,304 tokens");
     if (B > 0x7fffffff / MAX_CLUSTER) return ops_fail(PSC_ERR_LIMIT, me, "batch too large");
     if (B == 0) return PSC_OK;
+    if (!d_work || work_bytes < psc_sample_work_bytes(B))
+        return ops_fail(PSC_ERR_ARG, me, "workspace missing or too small");
     const Settings S{d_uniform, d_temperature, d_top_k, d_top_p, d_min_p};
     if (dtype == PSC_BF16)
         return sample((const __nv_bfloat16*)d_logits, row_stride, B, V, d_bitmask, S, d_tokens, d_logprobs,
-                      (cudaStream_t)stream);
-    return sample((const float*)d_logits, row_stride, B, V, d_bitmask, S, d_tokens, d_logprobs, (cudaStream_t)stream);
+                      (uint8_t*)d_work, (cudaStream_t)stream);
+    return sample((const float*)d_logits, row_stride, B, V, d_bitmask, S, d_tokens, d_logprobs, (uint8_t*)d_work,
+                  (cudaStream_t)stream);
 }

@@ -29,7 +29,8 @@ EXPORTED = ["psc_compile", "psc_destroy", "psc_last_error", "psc_info", "psc_sta
             "psc_decode_step", "psc_decode_step_mask", "psc_decode_step_advance", "psc_state_copy",
             "psc_host_classify_bottom_up", "psc_state_faults", "psc_check_wait"]
 # include/psc_ops.h: the operators around the mask
-EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "psc_process_logits", "psc_sample"]
+EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "psc_process_logits",
+                "psc_sample_work_bytes", "psc_sample"]
 NOALLOC_MAX_ROWS = 16384
 
 
@@ -102,7 +103,8 @@ def load(path: str = LIB_PATH):
         "psc_head_logits": (i32, [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
         "psc_process_logits": (i32, [vp, i32, i64, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i32,
                                      vp, vp]),
-        "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "psc_sample_work_bytes": (i64, [i32]),
+        "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -472,6 +474,15 @@ def _mask_ptr(bitmask, B, V):
     return _ptr(bitmask, torch.int32, "bitmask")
 
 
+def _workspace(n: int, device, stream):
+    """n bytes of torch's allocator, from the pool of the stream that the kernels run on."""
+    import torch
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 def psc_quantize_rows(x, q, scale, stream=None):
     """q, scale := the rows of x (bf16 or f32 [T, K]) in 8-bit integers (int8 [T, K])
     with a scale each (f32 [T]): activations by token, or weights by output channel."""
@@ -507,13 +518,7 @@ def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, strea
     n = load().psc_head_work_bytes(T, V, K)
     pm = _mask_ptr(bitmask, T, V)
     if work is None:
-        # of the allocator's pool for the stream that the kernels run on
-        if stream is None:
-            work = torch.empty(n, dtype=torch.uint8, device=logits.device)
-        else:
-            s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-            with torch.cuda.stream(s):
-                work = torch.empty(n, dtype=torch.uint8, device=logits.device)
+        work = _workspace(n, logits.device, stream)
     _check(load().psc_head_logits(pq, sq, _ptr(scale, torch.float32, "scale", T), T, pw, sw,
                                   _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
                                   _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
@@ -556,10 +561,11 @@ def psc_process_logits(logits, out=None, history=None, history_len=None, prompt_
 
 
 def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature=None, top_k=None, top_p=None,
-               min_p=None, V: int | None = None, stream=None):
+               min_p=None, V: int | None = None, work=None, stream=None):
     """tokens[b] := a token drawn among the allowed ones with uniform[b] (f32 in [0, 1)),
     logprobs[b] := ln of the probability it was drawn with.  temperature, top_p,
-    min_p f32 [B], top_k int32 [B]; None leaves a filter off (temperature 1)."""
+    min_p f32 [B], top_k int32 [B]; None leaves a filter off (temperature 1).  work: a
+    uint8 tensor of at least psc_sample_work_bytes(B) bytes to reuse."""
     import torch
     if logits.dim() != 2:
         raise ValueError("logits must be a 2-D tensor")
@@ -567,8 +573,16 @@ def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature
     V = logits.shape[1] if V is None else V
     code = _dtype_code(logits)
     pl, sl = _rows(logits, None, "logits", B, V)
+    n = (B + 15) // 16 * 16 or 16           # psc_sample_work_bytes(B)
+    if work is None:
+        work = _workspace(n, logits.device, stream)
     _check(load().psc_sample(
         pl, code, sl, B, V, _mask_ptr(bitmask, B, V), _ptr(uniform, torch.float32, "uniform", B),
         _ptr(temperature, torch.float32, "temperature", B), _ptr(top_k, torch.int32, "top_k", B),
         _ptr(top_p, torch.float32, "top_p", B), _ptr(min_p, torch.float32, "min_p", B),
-        _ptr(tokens, torch.int32, "tokens", B), _ptr(logprobs, torch.float32, "logprobs", B), _stream(stream)))
+        _ptr(tokens, torch.int32, "tokens", B), _ptr(logprobs, torch.float32, "logprobs", B),
+        _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+
+
+def psc_sample_work_bytes(B: int) -> int:
+    return load().psc_sample_work_bytes(B)
