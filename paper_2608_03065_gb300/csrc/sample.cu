@@ -291,8 +291,10 @@ struct Job {
     Settings settings;
     int32_t* tokens;
     float* logprobs;
-    uint8_t* pending;       // rows that k_sample_light leaves to k_sample, or NULL
+    int rows;               // which rows a kernel does
+    uint8_t* pending;       // [B]: rows that k_sample_light could not settle
 };
+enum { ALL_ROWS, HEAVY_ROWS, PENDING_ROWS };
 
 // What is found out about a row, kept in shared memory: a register that lives across the
 // passes is one that they do not have.
@@ -895,19 +897,24 @@ struct Blocks {
     __device__ __forceinline__ const Shared* peer(Shared& s, int q) const {
         return count() > 1 ? cg::this_cluster().map_shared_rank(&s, q) : &s;
     }
+    // f(block's number, its shared memory) for all; those past the last are the last again, so
+    // that the reads need no branches and go out together
+    template <typename F>
+    __device__ __forceinline__ void each(Shared& s, F&& f) const {
+        const int n = count();
+#pragma unroll
+        for (int q = 0; q < MAX_CLUSTER; q++) f(q, q < n, peer(s, min(q, n - 1)));
+    }
     // the largest of two values over the blocks
     __device__ __forceinline__ uint2 max2(Shared& s, uint32_t x, uint32_t y, int slot) const {
         uint2 v = block_max(s, x, y);
-        const int n = count();
-        if (n > 1) {
+        if (count() > 1) {
             if (threadIdx.x == 0) s.part[slot] = (u64)v.x << 32 | v.y;
             sync();
-#pragma unroll
-            for (int q = 0; q < MAX_CLUSTER; q++)
-                if (q < n) {
-                    const u64 o = peer(s, q)->part[slot];
-                    v = make_uint2(max(v.x, (uint32_t)(o >> 32)), max(v.y, (uint32_t)o));
-                }
+            each(s, [&](int, bool, const Shared* o) {
+                const u64 w = o->part[slot];
+                v = make_uint2(max(v.x, (uint32_t)(w >> 32)), max(v.y, (uint32_t)w));
+            });
         }
         return v;
     }
@@ -915,26 +922,42 @@ struct Blocks {
     __device__ __forceinline__ u64 sum(Shared& s, u64 v, int slot, u64* lower, u64* own) const {
         block_before(s, v, own);
         *lower = 0;
-        const int n = count(), me = rank();
-        if (n == 1) return *own;
+        if (count() == 1) return *own;
         if (threadIdx.x == 0) s.part[slot] = *own;
         sync();
         u64 all = 0;
-#pragma unroll
-        for (int q = 0; q < MAX_CLUSTER; q++) {
-            const u64 w = q < n ? peer(s, q)->part[slot] : 0ull;
+        const int me = rank();
+        each(s, [&](int q, bool there, const Shared* o) {
+            const u64 w = o->part[slot];
             if (q < me) *lower += w;
-            all += w;
-        }
+            if (there) all += w;
+        });
         return all;
+    }
+    // sums of two values over the blocks' threads (slots slot and slot + 1)
+    __device__ __forceinline__ u64 sum2(Shared& s, u64 v, u64* w, int slot) const {
+        u64 x, y;
+        block_before(s, v, &x);
+        block_before(s, *w, &y);
+        if (count() > 1) {
+            if (threadIdx.x == 0) s.part[slot] = x, s.part[slot + 1] = y;
+            sync();
+            x = y = 0;
+            each(s, [&](int, bool there, const Shared* o) {
+                const u64 p = o->part[slot], q = o->part[slot + 1];
+                if (there) x += p, y += q;
+            });
+        }
+        *w = y;
+        return x;
     }
     // the blocks' bin of this thread's number, summed
     __device__ __forceinline__ u64 bin(Shared& s, bool weights) const {
-        const int n = count();
         u64 v = 0;
-#pragma unroll
-        for (int q = 0; q < MAX_CLUSTER; q++)
-            if (q < n) v += weights ? bin_weight(*peer(s, q), threadIdx.x) : (u64)peer(s, q)->bins[threadIdx.x];
+        each(s, [&](int, bool there, const Shared* o) {
+            const u64 w = weights ? bin_weight(*o, threadIdx.x) : (u64)o->bins[threadIdx.x];
+            if (there) v += w;
+        });
         return v;
     }
 };
@@ -1082,9 +1105,8 @@ __device__ __noinline__ void find_stretch(Shared& s) {
 // After bins_pass: whether the nucleus ends in the stretch, in which bin, and after how much of it.
 __device__ __noinline__ void find_bin(Shared& s, u64 all, u64 above) {
     const Blocks<false> blocks;
-    u64 lower, own, inside;
-    const u64 limit = limit_of(s, blocks.sum(s, all, 5, &lower, &own));
-    const u64 over = blocks.sum(s, above, 7, &lower, &own);
+    u64 over = above, inside;
+    const u64 limit = limit_of(s, blocks.sum2(s, all, &over, 10));
     const u64 w = blocks.bin(s, true), till = over + block_before(s, w, &inside);
     if (till < limit && limit <= till + w) s.st.bin = threadIdx.x, s.st.left = limit - till;
     if (threadIdx.x == 0) s.n = 0, s.st.hit = limit > over && limit <= over + inside;
@@ -1185,9 +1207,16 @@ __device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
 // over the whole row.  What no list holds is drawn from sums by chunk.
 //
 // Rows that need no weights of all tokens (greedy, top-k, min-p alone) and those that do
-// differ tenfold in time and want different splits, so a batch whose settings may hold both is
-// done by two kernels: k_sample_light, a block per row, does the first kind and marks the
-// others, which k_sample, a cluster per row, then does.  LIGHT: without what those need.
+// differ tenfold in time and want different splits, so a large batch whose settings may hold
+// both is done by three kernels: k_sample begins with the heavy rows, a cluster for each;
+// k_sample_light does the others meanwhile, a block for each; and k_sample comes back for
+// rows whose candidates turned out to be more than a list.  LIGHT: without what heavy rows need.
+__device__ __forceinline__ bool is_light(const Settings& S, int V, int b) {
+    if (S.temperature && !(S.temperature[b] >= 1e-6f)) return true;
+    if (S.top_k && S.top_k[b] > 0 && S.top_k[b] < V) return true;
+    return S.min_p && S.min_p[b] > 0.f && !(S.top_p && S.top_p[b] < 1.f);
+}
+
 template <typename T, bool VEC, bool LIGHT>
 __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
     const Blocks<LIGHT> blocks;
@@ -1198,10 +1227,6 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
         const float temp = S.temperature ? S.temperature[b] : 1.f, p = S.top_p ? S.top_p[b] : 1.f;
         const float min_e = S.min_p && S.min_p[b] > 0.f ? fminf(S.min_p[b], 1.f) : 0.f;
         const int k = S.top_k && S.top_k[b] > 0 && S.top_k[b] < j.V ? S.top_k[b] : 0;
-        if (LIGHT && temp >= 1e-6f && !k && (p < 1.f || !(min_e > 0.f))) {
-            if (threadIdx.x == 0) j.pending[b] = 1;
-            return;
-        }
         s.bins[threadIdx.x] = 0;
         if (threadIdx.x == 0) {
             const float u = S.uniform[b];
@@ -1320,40 +1345,33 @@ __device__ __forceinline__ void set_up(Shared& s) {
     __syncthreads();
 }
 
+// It follows k_sample, which began when all earlier kernels had completed, and waits for
+// nothing of it; one block sees to it that this kernel does not complete before that one.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(NT, 2) k_sample_light(const __grid_constant__ Job j) {
     extern __shared__ __align__(16) uint8_t dyn[];
     Shared& s = *reinterpret_cast<Shared*>(dyn);
-    s.turn[threadIdx.x] = 0;
-    if (threadIdx.x == 0) s.job = j;
-    dep_wait();
-    dep_launch();
-    set_up(s);
-    sample_row<T, VEC, true>(s, nullptr, blockIdx.x);
+    if (is_light(j.settings, j.V, blockIdx.x)) {
+        s.turn[threadIdx.x] = 0;
+        if (threadIdx.x == 0) s.job = j;
+        set_up(s);
+        sample_row<T, VEC, true>(s, nullptr, blockIdx.x);
+    } else if (threadIdx.x == 0) {
+        j.pending[blockIdx.x] = 0;
+    }
+    if (blockIdx.x == 0) dep_wait();
 }
 
-// The i-th row that `pending` marks (that is there, where it is NULL), -1 past the last.
+// The cluster's row; -1: there is none for it.
 __device__ __forceinline__ int find_row(Shared& s, int i) {
     const Job& j = s.job;
-    if (!j.pending) return i;
-    // a thread's share of the rows, and how many are marked before it
-    const int per = (j.B + NT - 1) / NT, from = min(j.B, (int)threadIdx.x * per), to = min(j.B, from + per);
-    u64 total;
-    int own = 0;
-    for (int b = from; b < to; b++) own += j.pending[b];
-    const int before = (int)block_before(s, own, &total);
-    if (i >= (int)total) return -1;
-    if (i >= before && i < before + own) {
-        int left = i - before, b = from;
-        for (; !j.pending[b] || left--; b++) {}
-        s.at = b;
-    }
-    __syncthreads();
-    return s.at;
+    if (j.rows == ALL_ROWS) return i;
+    if (j.rows == HEAVY_ROWS) return is_light(j.settings, j.V, i) ? -1 : i;
+    return j.pending[i] ? i : -1;
 }
 
-// A cluster for each row that `pending` marks (all of them where it is NULL).  No loop over rows:
-// with one the compiler leaves the passes too few registers.
+// A cluster for each row.  (No loop over rows: with one the compiler leaves the passes too few
+// registers.)
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(NT, 2) k_sample(const __grid_constant__ Job j) {
     extern __shared__ __align__(16) uint8_t dyn[];
@@ -1369,40 +1387,43 @@ __global__ void __launch_bounds__(NT, 2) k_sample(const __grid_constant__ Job j)
     sample_row<T, VEC, false>(s, reinterpret_cast<u64*>(dyn + sizeof(Shared)), b);
 }
 
-// Blocks per row: two run on an SM.  Rows are split until there are blocks for all of them, as
+// Blocks per row: two run on an SM.  Rows are split while there are blocks for all of them at once, as
 // long as most warps have a chunk; until the rows in flight leave room in the L2 for the later
 // passes; and to 2^20 tokens a block (what WeightSum holds).
 int split(int rows, int V, size_t bytes) {
     const int sms = current_sms();
     int cluster = 1;
     while (cluster < MAX_CLUSTER &&
-           (((int64_t)rows * cluster < 2 * sms && V / (2 * cluster) >= NW * CHUNK * 3 / 4) || V / cluster > 1 << 20 ||
+           (((int64_t)rows * cluster * 2 <= 2 * sms && V / (2 * cluster) >= NW * CHUNK * 3 / 4) || V / cluster > 1 << 20 ||
             std::min<int64_t>(rows, 2 * sms / cluster) * V * (int64_t)bytes > 128 << 20))
         cluster *= 2;
     return cluster;
 }
 
-// Batches of at least this many rows, with top-k or min-p, are done by two kernels.
-constexpr int TWO_KERNELS = 48;
+// Batches of at least this many rows, with top-k or min-p, are done by three kernels.
+constexpr int THREE_KERNELS = 48;
+constexpr int HEAVY_SPLIT = 4;          // blocks per heavy row then
 
 template <typename T>
 psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
                   int32_t* tokens, float* logprobs, uint8_t* pending, cudaStream_t cs) {
     const bool vec = is_aligned(logits, stride * sizeof(T), 16);
-    const bool both = B >= TWO_KERNELS && V <= 1 << 20 && (S.top_k || S.min_p);
-    Job j{logits, stride, B, V, (V + CHUNK - 1) / CHUNK * CHUNK, (V + 31) / 32, bitmask, S, tokens, logprobs,
-          both ? pending : nullptr};
-    if (both) {
-        psc_status s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT, sizeof(Shared), 1,
-                                  cs, "k_sample_light", j);
-        if (s != PSC_OK) return s;
-    }
-    // of a mixed batch about a quarter is left
-    const int cluster = split(both ? (B + 3) / 4 : B, V, sizeof(T));
-    j.per_block = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
-    const size_t smem = sizeof(Shared) + (size_t)(j.per_block / CHUNK) * 8;
-    return ops_launch(vec ? k_sample<T, true> : k_sample<T, false>, dim3((unsigned)B * cluster), NT, smem, cluster,
-                      cs, "k_sample", j);
+    Job j{logits, stride, B, V, 0, (V + 31) / 32, bitmask, S, tokens, logprobs, ALL_ROWS, pending};
+    auto launch = [&](int rows, int cluster) {
+        j.rows = rows;
+        j.per_block = ((V + cluster - 1) / cluster + CHUNK - 1) / CHUNK * CHUNK;
+        const size_t smem = sizeof(Shared) + (size_t)(j.per_block / CHUNK) * 8;
+        return ops_launch(vec ? k_sample<T, true> : k_sample<T, false>, dim3((unsigned)B * cluster), NT, smem, cluster,
+                          cs, "k_sample", j);
+    };
+    if (B < THREE_KERNELS || V > 1 << 20 || !(S.top_k || S.min_p)) return launch(ALL_ROWS, split(B, V, sizeof(T)));
+    // heavy rows are few of a mixed batch (a fifth, say) and slow
+    psc_status s = launch(HEAVY_ROWS, split(std::min(B, 2 * current_sms() / HEAVY_SPLIT), V, sizeof(T)));
+    if (s != PSC_OK) return s;
+    j.per_block = (V + CHUNK - 1) / CHUNK * CHUNK;
+    s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT, sizeof(Shared), 1, cs,
+                   "k_sample_light", j);
+    return s != PSC_OK ? s : launch(PENDING_ROWS, 1);
 }
 
 }  // namespace
