@@ -464,3 +464,44 @@ def test_results_do_not_depend_on_the_batch_around_a_row(psc):
         t1, l1 = torch.empty(1, dtype=torch.int32, device="cuda"), torch.empty(1, device="cuda")
         psc.psc_sample(one, u[b:b + 1], t1, logprobs=l1, top_p=p[b:b + 1])
         assert t1[0] == tok[b] and l1[0] == lp[b]
+
+
+def test_buffers_that_change_between_calls_without_a_wait(psc):
+    """Kernels overlap the ends of those before them: twenty steps on the same buffers, each
+    input written on the stream right before the call, give what each gives alone."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    B, V, K, H = 60, 40000, 128, 9000
+    x = torch.empty(B, K, device="cuda", dtype=torch.bfloat16)
+    wf = torch.empty(V, K, device="cuda")
+    q, sx = torch.empty(B, K, dtype=torch.int8, device="cuda"), torch.empty(B, device="cuda")
+    w, sw = torch.empty(V, K, dtype=torch.int8, device="cuda"), torch.empty(V, device="cuda")
+    logits, out = torch.empty(B, V, device="cuda"), torch.empty(B, V, device="cuda")
+    hist = torch.empty(B, H, dtype=torch.int32, device="cuda")
+    mask = torch.empty(B, (V + 31) // 32, dtype=torch.int32, device="cuda")
+    k, p = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, device="cuda")
+    u, tok = torch.empty(B, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    pres = torch.full((B,), 0.5, device="cuda")
+    steps = [{"x": torch.randn(B, K, device="cuda", generator=g).bfloat16(),
+              "wf": torch.randn(V, K, device="cuda", generator=g),
+              "hist": torch.randint(0, V, (B, H), device="cuda", generator=g).int(),
+              "mask": torch.randint(-2 ** 31, 2 ** 31, mask.shape, device="cuda", generator=g).int(),
+              "k": torch.randint(0, 2, (B,), device="cuda", generator=g).int() * 30,
+              "p": torch.rand(B, device="cuda", generator=g) + 0.3, "u": torch.rand(B, device="cuda", generator=g)}
+             for _ in range(20)]
+
+    def step(s):
+        for name, buf in (("x", x), ("wf", wf), ("hist", hist), ("mask", mask), ("k", k), ("p", p), ("u", u)):
+            buf.copy_(s[name])
+        psc.psc_quantize_rows(x, q, sx)
+        psc.psc_quantize_rows(wf, w, sw)              # the weights straight before their use
+        psc.psc_head_logits(q, sx, w, sw, logits, bitmask=mask)
+        psc.psc_process_logits(logits, out=out, history=hist, presence=pres, bitmask=mask)
+        psc.psc_sample(out, u, tok, bitmask=mask, top_k=k, top_p=p)
+        return tok.clone(), out.clone()
+
+    chained = [step(s) for s in steps]
+    torch.cuda.synchronize()
+    for s, (t, y) in zip(steps, chained):
+        t2, y2 = step(s)
+        torch.cuda.synchronize()
+        assert torch.equal(t, t2) and torch.equal(y, y2)
