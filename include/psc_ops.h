@@ -36,8 +36,9 @@ extern "C" {
 psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_stride, int32_t T, int32_t K,
                              int8_t* d_q, int64_t q_stride, float* d_scale, void* stream);
 
-/* Bytes of workspace that psc_head_logits needs for these sizes. */
-int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K);
+/* Bytes of workspace that psc_head_logits needs for these sizes; aligned: whether d_w
+ * and w_stride are multiples of 16. */
+int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned);
 
 /* The vocabulary projection in 8-bit integers, under the mask:
  *     logits[t][v] = (sum_k q[t][k] * w[v][k]) * scale[t] * w_scale[v]
@@ -48,13 +49,13 @@ int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K);
  *   d_scale       : float [T], d_w_scale : float [V]
  *   d_bitmask     : uint32 [T][ceil(V/32)], or NULL (every token allowed)
  *   d_logits      : [T] rows of row_stride elements of dtype; columns >= V are left as they are
- *   d_work        : at least psc_head_work_bytes(T, V, K) bytes, 256-byte aligned; calls that
- *                   overlap on the GPU need workspaces of their own.  Its first int32 is
- *                   afterwards the number of blocks in which a bounded wait gave up (a
- *                   pipeline fault; some logits are then not written), 0 otherwise
- * Rows at 16-byte-aligned addresses (base and stride, of d_q and d_w) take the
- * tensor cores at any K; others a path of integer dot products.
- * PSC_ERR_LIMIT: K over 131,072 (a sum could pass 32 bits). */
+ *   d_work        : at least psc_head_work_bytes bytes, 256-byte aligned; calls that overlap
+ *                   on the GPU need workspaces of their own.  Its first int32 is afterwards
+ *                   the number of blocks in which a bounded wait gave up (a pipeline fault;
+ *                   some logits are then not written), 0 otherwise
+ * Weights whose rows are at 16-byte-aligned addresses (d_w and w_stride; any K) are
+ * read where they are; others are packed into the workspace first, a slab at a time.
+ * PSC_ERR_LIMIT: K over 131,072 (a sum could pass 32 bits), T over 2^24. */
 psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_scale, int32_t T, const int8_t* d_w,
                            int64_t w_stride, const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask,
                            void* d_logits, psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes,

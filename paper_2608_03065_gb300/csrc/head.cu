@@ -60,69 +60,51 @@ struct Head {
     const float* w_scale;
     int V, K;
     const uint32_t* bitmask;
-    int W;
+    int W;                              // mask words of a row here, and from row to row
+    int mask_stride;
     int64_t row_stride;
+    int first;                          // the call's first slab: the fault word starts at 0
 };
 
-// Integer dot products at any alignment: a block per 64 tokens x 64 vocabulary
-// rows, 4 x 4 sums a thread, 64 bytes of K at a time through shared memory.
-template <typename T>
-__global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned4, int* faults) {
-    constexpr int TILE = 64, KB = 16, LD = KB + 1;      // words of K per step; odd row length: no bank conflicts
-    __shared__ int sw[TILE * LD], sq[TILE * LD];
+// Sixteen bytes at any address, of which the first n (if fewer) are there; zeros behind them.
+__device__ __forceinline__ uint4 load_bytes(const int8_t* p, int n) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 16; j++)
+        if (j < n) w[j >> 2] |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Rows at any address -> rows of `pitch` bytes (a multiple of 16) at aligned ones, zeros past
+// K: a warp per row, 16 bytes a lane, put together from the two aligned pieces that hold
+// them.  [begin, end) are the source's bytes; pieces that are not all inside go byte by byte.
+__global__ void __launch_bounds__(256) k_pack_rows(const int8_t* w, int64_t stride, int rows, int K, int pitch,
+                                                   const int8_t* begin, const int8_t* end, int8_t* out) {
+    const int lane = threadIdx.x & 31, n_warps = gridDim.x * 8;
     dep_wait();
     dep_launch();
-    if (!blockIdx.x && !blockIdx.y && !threadIdx.x) *faults = 0;
-    const int v0 = blockIdx.x * TILE, t0 = blockIdx.y * TILE;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    int any = !h.bitmask;
-    if (h.bitmask && threadIdx.x < TILE * 2) {
-        const int t = t0 + (threadIdx.x >> 1), wi = (v0 >> 5) + (threadIdx.x & 1);
-        any = t < h.T && wi < h.W && h.bitmask[(size_t)t * h.W + wi] != 0;
-    }
-    any = __syncthreads_or(any);
-    int acc[4][4] = {};
-    auto load = [&](int* dst, const int8_t* src, int64_t stride, int r0, int rows, int k0) {
-        for (int i = threadIdx.x; i < TILE * KB; i += 256) {
-            const int r = i / KB, k = k0 + (i % KB) * 4;
-            int word = 0;
-            if (r0 + r < rows && k < h.K) {
-                const int8_t* p = src + (size_t)(r0 + r) * stride + k;
-                if (aligned4 && k + 4 <= h.K) word = *reinterpret_cast<const int*>(p);
-                else
-                    for (int j = 0; j < 4 && k + j < h.K; j++) word |= (int)(uint8_t)p[j] << (8 * j);
+    for (int r = blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += n_warps) {
+        const int8_t* row = w + (size_t)r * stride;
+        const int off = (int)((uintptr_t)row & 15);
+        const int8_t* base = row - off;
+        for (int c0 = 0; c0 < pitch / 16; c0 += 32) {
+            const int c = c0 + lane, left = K - c * 16;
+            const int8_t* at = base + c * 16;
+            uint4 v;
+            if (off && left >= 16 && at >= begin && at + 32 <= end) {
+                const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at + 16);
+                const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                const int words = off >> 2, bits = 8 * (off & 3);
+                uint32_t y[5];
+#pragma unroll
+                for (int i = 0; i < 5; i++)
+                    y[i] = words == 0 ? x[i] : words == 1 ? x[i + 1] : words == 2 ? x[i + 2] : i < 4 ? x[i + 3] : x[7];
+                v = make_uint4(__funnelshift_r(y[0], y[1], bits), __funnelshift_r(y[1], y[2], bits),
+                               __funnelshift_r(y[2], y[3], bits), __funnelshift_r(y[3], y[4], bits));
+            } else {
+                v = off == 0 && left >= 16 ? *reinterpret_cast<const uint4*>(at) : load_bytes(row + c * 16, left);
             }
-            dst[r * LD + i % KB] = word;
-        }
-    };
-    if (any) {
-        for (int k0 = 0; k0 < h.K; k0 += KB * 4) {
-            load(sw, h.w, h.w_stride, v0, h.V, k0);
-            load(sq, h.q, h.q_stride, t0, h.T, k0);
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < KB; k++) {
-                int a[4], c[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++) a[i] = sw[(tx + 16 * i) * LD + k], c[i] = sq[(ty + 16 * i) * LD + k];
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) acc[i][j] = __dp4a(a[i], c[j], acc[i][j]);
-            }
-            __syncthreads();
-        }
-    }
-    for (int j = 0; j < 4; j++) {
-        const int t = t0 + ty + 16 * j;
-        if (t >= h.T) break;
-        const float st = h.scale[t];
-        const uint32_t* mask = h.bitmask ? h.bitmask + (size_t)t * h.W : nullptr;
-        for (int i = 0; i < 4; i++) {
-            const int v = v0 + tx + 16 * i;
-            if (v >= h.V) continue;
-            const float y = allows(mask, v) ? (float)acc[i][j] * st * h.w_scale[v] : __uint_as_float(0xFF800000u);
-            store_f32(logits + (size_t)t * h.row_stride + v, y);
+            if (c < pitch / 16) *reinterpret_cast<uint4*>(out + (size_t)r * pitch + c * 16) = v;
         }
     }
 }
@@ -138,15 +120,6 @@ __global__ void __launch_bounds__(256) k_head_dot(Head h, T* logits, int aligned
 constexpr int ROWS = 4;
 constexpr int ROWS_THREADS = 256;
 constexpr int ROWS_X_MAX = 64 * 1024;         // bytes of tokens held in shared memory
-
-// The first n (< 16) of 16 bytes, zeros behind them.
-__device__ __forceinline__ uint4 load_bytes(const int8_t* p, int n) {
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < 16; j++)
-        if (j < n) w[j >> 2] |= (uint32_t)(uint8_t)p[j] << (8 * (j & 3));
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // Whether a mask leaves so few rows (up to a quarter) that reading them one by one wins:
 // 16 tokens over 128,256 x 2048 take 174 us by rows and 64 us by k_head_mma when all are
@@ -174,13 +147,13 @@ __global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, i
     dep_wait();
     dep_launch();
     if (flags && !few_rows(flags, n_tiles, h.V)) return;        // k_head_mma's
-    if (!flags && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    if (!flags && h.first && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
     for (int i = threadIdx.x; i < N * chunks; i += ROWS_THREADS) {
         const int t = i / chunks, k = (i - t * chunks) * 16;
         uint4 x = make_uint4(0, 0, 0, 0);
         if (t < h.T) {
             const int8_t* p = h.q + (size_t)t * h.q_stride + k;
-            x = k + 16 <= h.K ? *reinterpret_cast<const uint4*>(p) : load_bytes(p, h.K - k);
+            x = k + 16 <= h.K && !((uintptr_t)p & 15) ? *reinterpret_cast<const uint4*>(p) : load_bytes(p, h.K - k);
         }
         xs[i] = x;
     }
@@ -244,7 +217,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) k_head_rows(Head h, T* logits, i
     } else {                                            // a mask word each; what masks allow may lie together
         for (int item = me; item < n_items; item += n_warps) {
             const int v0 = item * 32, v = v0 + lane;
-            const uint32_t mine = lane < h.T ? h.bitmask[(size_t)lane * h.W + item] : 0u;
+            const uint32_t mine = lane < h.T ? h.bitmask[(size_t)lane * h.mask_stride + item] : 0u;
             uint32_t rows = __reduce_or_sync(FULL, mine);
             if (h.V - v0 < 32) rows &= (1u << (h.V - v0)) - 1;
             while (rows) {
@@ -439,20 +412,16 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
                                                    int* faults, __half* x, uint8_t* flags) {
     dep_wait();
     dep_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    if (h.first && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
     if ((int)blockIdx.x < x_blocks) {                 // 16 columns a thread
         const int per = Kp / 16;
         const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
         if (i >= (int64_t)h.T * per) return;
         const int t = (int)(i / per), k = (int)(i - (int64_t)t * per) * 16;
         const int8_t* src = h.q + (size_t)t * h.q_stride + k;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (k + 16 <= h.K) {
-            const uint4 v = *reinterpret_cast<const uint4*>(src);
-            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-        } else {
-            for (int j = 0; j < 16 && k + j < h.K; j++) w[j >> 2] |= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
-        }
+        const uint4 v = k + 16 <= h.K && !((uintptr_t)src & 15) ? *reinterpret_cast<const uint4*>(src)
+                                                                : load_bytes(src, h.K - k);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         uint4* dst = reinterpret_cast<uint4*>(x + (size_t)t * Kp + k);
 #pragma unroll
         for (int j = 0; j < 2; j++) {
@@ -468,7 +437,7 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
     // a lane per word of a token's four, eight tokens at a time
     for (int t = t0 + (lane >> 2); t < t1; t += 8) {
         const int wi = vt * 4 + (lane & 3);
-        if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
+        if (wi < h.W) any |= h.bitmask[(size_t)t * h.mask_stride + wi];
     }
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) any |= __shfl_xor_sync(FULL, any, o);
@@ -676,7 +645,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             for (int i = 0; i < NT_MAX / 32; i++) {
                 const int t = i * 32 + lane;
                 st[i] = t < n ? h.scale[t0 + t] : 0.f;
-                word[i] = !masked ? FULL : active && t < n && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u;
+                word[i] = !masked ? FULL : active && t < n && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.mask_stride + wi] : 0u;
             }
             if (active) {
                 if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
@@ -762,21 +731,49 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
                       (const uint8_t*)flags, leave_few);
 }
 
+// Weights whose rows are not at 16-byte-aligned addresses are packed into the workspace a slab at
+// a time: about 40 MB, which the L2 still holds when the products read it.
+constexpr int64_t SLAB_BYTES = 40 << 20;
+int slab_rows(int V, int K) {
+    const int64_t pitch = (K + 15) / 16 * 16;
+    return (int)std::min<int64_t>((V + VT - 1) / VT * VT, std::max<int64_t>(VT, SLAB_BYTES / pitch / VT * VT));
+}
+bool is_packed(const int8_t* w, int64_t stride) { return is_aligned(w, stride, 16); }
+
+template <typename T>
+psc_status head_aligned(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    // up to 4 tokens, or 8 under a mask (rows of the weights can be left out one by one; up
+    // to 16 if it leaves few)
+    const int64_t row = (h.K + 15) / 16 * 16;
+    if (h.T == 1 && row <= ROWS_X_MAX) return head_rows<T, 1>(h, logits, work, cs);
+    if (h.T == 2 && 2 * row <= ROWS_X_MAX) return head_rows<T, 2>(h, logits, work, cs);
+    if (h.T <= 4 && 4 * row <= ROWS_X_MAX) return head_rows<T, 4>(h, logits, work, cs);
+    if (h.T <= 8 && h.bitmask && 8 * row <= ROWS_X_MAX) return head_rows<T, 8>(h, logits, work, cs);
+    return head_mma(h, logits, work, cs);
+}
+
 template <typename T>
 psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
-    if (is_aligned(h.w, h.w_stride, 16) && is_aligned(h.q, h.q_stride, 16)) {
-        // up to 4 tokens, or 8 under a mask (rows of the weights can be left out one by one; up
-        // to 16 if it leaves few)
-        const int64_t row = (h.K + 15) / 16 * 16;
-        if (h.T == 1 && row <= ROWS_X_MAX) return head_rows<T, 1>(h, logits, work, cs);
-        if (h.T == 2 && 2 * row <= ROWS_X_MAX) return head_rows<T, 2>(h, logits, work, cs);
-        if (h.T <= 4 && 4 * row <= ROWS_X_MAX) return head_rows<T, 4>(h, logits, work, cs);
-        if (h.T <= 8 && h.bitmask && 8 * row <= ROWS_X_MAX) return head_rows<T, 8>(h, logits, work, cs);
-        return head_mma(h, logits, work, cs);
+    if (is_packed(h.w, h.w_stride)) return head_aligned(h, logits, work, cs);
+    const int rows = slab_rows(h.V, h.K), pitch = (h.K + 15) / 16 * 16;
+    int8_t* slab = (int8_t*)work + plan_of(h.T, h.V, h.K).bytes;
+    const int8_t* end = h.w + (size_t)(h.V - 1) * h.w_stride + h.K;
+    for (int v0 = 0; v0 < h.V; v0 += rows) {
+        Head part = h;
+        part.V = std::min(rows, h.V - v0);
+        part.first = v0 == 0;
+        psc_status s = ops_launch(k_pack_rows, dim3(std::min((part.V + 7) / 8, current_sms() * 8)), 256, 0, 1, cs,
+                                  "k_pack_rows", h.w + (size_t)v0 * h.w_stride, h.w_stride, part.V, h.K, pitch, h.w, end,
+                                  slab);
+        if (s != PSC_OK) return s;
+        part.w = slab;
+        part.w_stride = pitch;
+        part.w_scale += v0;
+        part.W = (part.V + 31) / 32;
+        if (part.bitmask) part.bitmask += v0 / 32;
+        if ((s = head_aligned(part, logits + v0, work, cs)) != PSC_OK) return s;
     }
-    const int aligned4 = is_aligned(h.w, h.w_stride, 4) && is_aligned(h.q, h.q_stride, 4);
-    return ops_launch(k_head_dot<T>, dim3((h.V + 63) / 64, (h.T + 63) / 64), 256, 0, 1, cs, "k_head_dot", h, logits,
-                      aligned4, (int*)work);
+    return PSC_OK;
 }
 
 }  // namespace
@@ -797,9 +794,9 @@ psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_strid
                       K, d_q, q_stride, d_scale);
 }
 
-int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K) {
+int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned) {
     if (T <= 0 || V <= 0 || K <= 0) return 256;
-    return plan_of(T, V, K).bytes;
+    return plan_of(T, V, K).bytes + (aligned ? 0 : (int64_t)slab_rows(V, K) * ((K + 15) / 16 * 16));
 }
 
 psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_scale, int32_t T, const int8_t* d_w,
@@ -811,11 +808,12 @@ psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_s
         !d_w_scale || (T && (!d_q || !d_scale || !d_logits)))
         return ops_fail(PSC_ERR_ARG, me, "bad arguments");
     if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 131,072");
-    if (T > 65535 * 64) return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
+    if ((int64_t)((T + NT_MAX - 1) / NT_MAX) * ((V + VT - 1) / VT) > 0x7fffffff || T > 1 << 24)
+        return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
     if (T == 0) return PSC_OK;
-    if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_work_bytes(T, V, K))
+    if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_work_bytes(T, V, K, is_packed(d_w, w_stride)))
         return ops_fail(PSC_ERR_ARG, me, "workspace missing, unaligned or too small");
-    const Head h{d_q, q_stride, d_scale, T, d_w, w_stride, d_w_scale, V, K, d_bitmask, (V + 31) / 32, row_stride};
+    const Head h{d_q, q_stride, d_scale, T, d_w, w_stride, d_w_scale, V, K, d_bitmask, (V + 31) / 32, (V + 31) / 32, row_stride, 1};
     if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
     return head(h, (float*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
 }

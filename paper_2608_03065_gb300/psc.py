@@ -99,7 +99,7 @@ def load(path: str = LIB_PATH):
         "psc_state_faults": (i32, [vp, vp, i32, vp]),
         "psc_check_wait": (i32, [vp, i32, vp]),
         "psc_quantize_rows": (i32, [vp, i32, i64, i32, i32, vp, i64, vp, vp]),
-        "psc_head_work_bytes": (i64, [i32, i32, i32]),
+        "psc_head_work_bytes": (i64, [i32, i32, i32, i32]),
         "psc_head_logits": (i32, [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
         "psc_process_logits": (i32, [vp, i32, i64, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i32,
                                      vp, vp]),
@@ -497,14 +497,16 @@ def psc_quantize_rows(x, q, scale, stream=None):
                                     _stream(stream)))
 
 
-def psc_head_work_bytes(T: int, V: int, K: int) -> int:
-    return load().psc_head_work_bytes(T, V, K)
+def psc_head_work_bytes(T: int, V: int, K: int, aligned: bool = True) -> int:
+    """Bytes of workspace for psc_head_logits; aligned: the weights' rows are at addresses
+    that are multiples of 16."""
+    return load().psc_head_work_bytes(T, V, K, 1 if aligned else 0)
 
 
 def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, stream=None):
     """logits[:, :V] := (q @ w.T) * scale[:, None] * w_scale, -inf where bitmask forbids.
-    q int8 [T, K], w int8 [V, K] (rows at 16-byte-aligned addresses take the tensor
-    cores), scale f32 [T], w_scale f32 [V], logits bf16 or f32 [T, >=V].  work: a
+    q int8 [T, K], w int8 [V, K] (rows at 16-byte-aligned addresses are read where they
+    are, others packed first), scale f32 [T], w_scale f32 [V], logits bf16 or f32 [T, >=V].  work: a
     uint8 tensor of at least psc_head_work_bytes(T, V, K) bytes to reuse (one is
     taken from torch's allocator for the call otherwise)."""
     import torch
@@ -515,7 +517,7 @@ def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, strea
     pq, sq = _rows(q, torch.int8, "q")
     pw, sw = _rows(w, torch.int8, "w")
     pl, sl = _rows(logits, None, "logits", T, V)
-    n = load().psc_head_work_bytes(T, V, K)
+    n = load().psc_head_work_bytes(T, V, K, 0 if (pw or 0) % 16 or sw % 16 else 1)
     pm = _mask_ptr(bitmask, T, V)
     if work is None:
         work = _workspace(n, logits.device, stream)

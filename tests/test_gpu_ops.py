@@ -164,6 +164,14 @@ def test_head_logits_at_any_alignment(psc, T, K, pad, shift):
     _head_case(psc, T, 321, K, "bf16", "none", pad=pad, shift=shift, out_pad=1)
 
 
+@pytest.mark.parametrize("T,V,K,pad,shift", [(1, 50000, 1001, 0, 0), (3, 20000, 4095, 0, 0), (12, 30001, 2047, 0, 3),
+                                             (40, 25000, 2050, 0, 2), (257, 21000, 2047, 0, 0)])
+def test_head_logits_of_several_slabs(psc, T, V, K, pad, shift):
+    """Unaligned rows over more than one slab of the workspace."""
+    _head_case(psc, T, V, K, "bf16", "mixed", pad=pad, shift=shift)
+    _head_case(psc, T, V, K, "f32", "none", pad=pad, shift=shift, out_pad=2)
+
+
 @pytest.mark.parametrize("T", [1, 4, 20, 150])
 @pytest.mark.parametrize("fill", [127, -128])
 def test_head_logits_largest_sums(psc, T, fill):
