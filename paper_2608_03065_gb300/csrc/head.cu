@@ -261,8 +261,15 @@ psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs, c
 //   warp 0        TMA: 128 x 128 bytes of weights into the byte ring (128 columns at a time)
 //   warps 8-15    bytes -> f16 into the operand ring, in the tensor core's 128-byte swizzle
 //   warp 2        TMA: the tokens' f16 rows (k_head_prep widened them) beside them
-//   warp 1        four tcgen05.mma of 128 x N x 16 into one of two accumulators in TMEM
+//   warp 1        four tcgen05.mma of 128 x N x 16 into one of two accumulators in TMEM (of a
+//                 pair: the first block's, 256 x N x 16; the second's says when its operands are there)
 //   warps 4-7     the other accumulator: scales, mask, logits (a lane per vocabulary row)
+// With many tokens what bounds it is shared memory: per 64 columns of K and 256 tokens a block
+// on its own moves 112 KB through it (bytes in and out 16, widened weights in and out 32,
+// tokens in and out 64), 875 cycles where the products take 512.  So blocks pair up (PAIR):
+// 256 rows of weights, 128 in each, by the same tokens, half in each (tcgen05's
+// cta_group::2), which leaves 80 KB.  256 tokens over 262,144 x 4096: 424 -> 364 us, 1511
+// TFLOP/s; 64 tokens over 128,256 x 2048: 66 us alone, 77 in pairs.
 // Byte b becomes f16 without a conversion: b + 128 under the exponent of 1024 is
 // 1152 + b, minus 1152; five instructions for four bytes.
 constexpr int VT = 128;                       // vocabulary rows of a tile
@@ -276,25 +283,31 @@ constexpr int SMEM_MAX = 227 * 1024;
 
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
-    int n_raw, n_x, x_group;                           // stages of the byte ring and of the tokens' ring
+    bool pair;                                // two blocks work on 256 vocabulary rows together
+    int n_raw, n_x, x_group;                  // stages of the byte ring, of the tokens' ring; columns' stages in one of those
     int Kp;                                   // K rounded up to whole stages
     int tmem;                                 // TMEM columns
     size_t smem;
     int64_t x_at, flags_at, bytes;            // in the workspace: the fault word, the f16 tokens, the tile flags
 };
 
+constexpr int PAIR_N = 128;                   // tokens of a tile from which blocks pair up
+
 Plan plan_of(int T, int V, int K) {
     Plan p;
     p.n_nt = (T + NT_MAX - 1) / NT_MAX;
     p.N = ((T + p.n_nt - 1) / p.n_nt + 15) / 16 * 16;
     p.n_vt = (V + VT - 1) / VT;
+    p.pair = p.N >= PAIR_N && p.n_vt > 1;
+    if (p.pair) p.N = (p.N + 31) / 32 * 32;
     p.Kp = (K + KB - 1) / KB * KB;
     // A stage of the tokens' ring holds several columns' stages where those are small, so
     // that the issuing warp waits and releases seldom; the byte ring, which covers the
     // memory's latency, gets the shared memory that is left.
-    p.x_group = p.N <= 32 ? 4 : p.N <= 64 ? 2 : 1;
-    const int x_bytes = p.N * KB * 2 * p.x_group;
-    p.n_x = p.N <= 128 ? MAX_X : 3;
+    const int own = p.pair ? p.N / 2 : p.N;   // tokens in a block's shared memory
+    p.x_group = own <= 32 ? 4 : own <= 64 ? 2 : 1;
+    const int x_bytes = own * KB * 2 * p.x_group;
+    p.n_x = own <= 128 ? MAX_X : 3;
     p.n_raw = std::min(MAX_RAW, (SMEM_MAX - 2048 - N_A * A_BYTES - p.n_x * x_bytes) / RAW_BYTES);
     p.smem = 1024 + (size_t)N_A * A_BYTES + (size_t)p.n_x * x_bytes + (size_t)p.n_raw * RAW_BYTES;
     p.tmem = 32;
@@ -374,15 +387,47 @@ __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
     return (uint64_t)((addr & 0x3FFFF) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
+// D (+)= A B; of a pair: 256 rows, A's 128 and half of B's columns from each block.
+template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(add)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(add)
+            : "memory");
 }
+// Arrives at the barrier (of both blocks of a pair) when the products so far are done.
+template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if (PAIR)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+}
+// Arrives at the first block's barrier of that place.
+__device__ __forceinline__ void arrive_at_first(uint32_t bar) {
+    asm volatile(
+        "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n"
+        " mbarrier.arrive.shared::cluster.b64 _, [r];\n}" ::"r"(bar)
+        : "memory");
 }
 // 16 columns of the warp's 32 lanes; complete after tmem_wait.
 __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t r[16]) {
@@ -445,24 +490,29 @@ __global__ void __launch_bounds__(256) k_head_prep(Head h, int Kp, int N, int n_
     if (lane == 0) flags[item] = (uint8_t)rows;
 }
 
-template <typename T>
+template <typename T, bool PAIR>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_constant__ CUtensorMap w_map,
                                                              const __grid_constant__ CUtensorMap x_map, Head h,
-                                                             T* logits, int N, int n_nt, int n_items, int Kp, int n_raw,
+                                                             T* logits, int N, int n_nt, int n_vt, int Kp, int n_raw,
                                                              int n_x, int x_group, int tmem_cols, int* faults,
                                                              const uint8_t* flags, int leave_few) {
     if (leave_few) {                                  // few rows are k_head_rows'
         dep_wait();
-        if (few_rows(flags, n_items, h.V)) return;
+        if (few_rows(flags, n_vt * n_nt, h.V)) return;
     }
     constexpr int PER = 8 / N_A, ROWS = VT / PER;      // converting warps of a group, rows of each
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * (MAX_RAW + N_A + MAX_X) + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * (MAX_RAW + N_A + MAX_X) + 5 + N_A];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
-    const int x_block = N * KB * 2, x_bytes = x_block * x_group;
+    // of a pair, the blocks have 128 vocabulary rows and half of the tokens each
+    constexpr int SIDES = PAIR ? 2 : 1;
+    const int side = PAIR ? (int)cluster_rank() : 0, own_n = N / SIDES;
+    const int n_items = (n_vt + SIDES - 1) / SIDES * n_nt;
+    const int first = blockIdx.x / SIDES, step = gridDim.x / SIDES;
+    const int x_block = own_n * KB * 2, x_bytes = x_block * x_group;
     auto a_at = [&](int s) { return base + s * A_BYTES; };
     auto x_at = [&](int s) { return base + N_A * A_BYTES + s * x_bytes; };
     auto raw_at = [&](int s) { return base + N_A * A_BYTES + n_x * x_bytes + s * RAW_BYTES; };
@@ -477,24 +527,35 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
     auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
     auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
     const uint32_t drained = bars + 8 * (LAST + 4);
+    auto other_full = [&](int s) { return bars + 8 * (LAST + 5 + s); };    // the second block's operands are there
 
     if (threadIdx.x == 0) {
         s_failed = 0;
         for (int s = 0; s < n_raw; s++) mbar_init(raw_full(s), 1), mbar_init(raw_empty(s), 2 * PER);
         for (int s = 0; s < N_A; s++) mbar_init(a_full(s), PER), mbar_init(a_empty(s), 1);
         for (int s = 0; s < n_x; s++) mbar_init(x_full(s), 1), mbar_init(x_empty(s), 1);
-        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), 4);
-        mbar_init(drained, 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), 4 * SIDES);
+        for (int s = 0; s < N_A; s++) mbar_init(other_full(s), 1);
+        mbar_init(drained, SIDES > 1 ? 2 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (PAIR) cluster_sync();
     if (warp == 3) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)),
-                     "r"(tmem_cols)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)),
+                         "r"(tmem_cols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)),
+                         "r"(tmem_cols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
@@ -503,15 +564,21 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
     // begun: only what k_head_prep writes (flags, f16 tokens) has to be waited for.
     const bool masked = h.bitmask != nullptr;
     if (warp != 0 || masked) dep_wait();
-    auto is_active = [&](int item) { return !masked || flags[item]; };
+    // whether an item's tiles (of all its blocks) hold an allowed token
+    auto is_active = [&](int item) {
+        if (!masked) return true;
+        if (!PAIR) return flags[item] != 0;
+        const int vt = item / n_nt * 2, nt = item % n_nt;
+        return (flags[vt * n_nt + nt] | (vt + 1 < n_vt ? flags[(vt + 1) * n_nt + nt] : 0)) != 0;
+    };
 
     if (warp == 0) {
         if (lane == 0) {
             Place p;
             int c = 0;
-            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+            for (int item = first; item < n_items && !*failed; item += step) {
                 if (!is_active(item)) continue;
-                const int v0 = item / n_nt * VT;
+                const int v0 = (item / n_nt * SIDES + side) * VT;
                 for (int k = 0; k < n_k2; k++, c++, p.next(n_raw)) {
                     if (!mbar_wait(raw_empty(p.s), p.parity ^ 1, failed)) break;
                     mbar_arrive_tx(raw_full(p.s), RAW_BYTES);
@@ -526,9 +593,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
         if (lane == 0) {
             Place p;
             int c = 0;
-            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+            for (int item = first; item < n_items && !*failed; item += step) {
                 if (!is_active(item)) continue;
-                const int t0 = item % n_nt * N;
+                const int t0 = item % n_nt * N + side * own_n;
                 for (int k = 0; k < n_k; k += x_group, c++, p.next(n_x)) {
                     if (!mbar_wait(x_empty(p.s), p.parity ^ 1, failed)) break;
                     const int n = min(x_group, n_k - k);
@@ -542,37 +609,45 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                     for (int it = 0; it < (1 << 20) && !mbar_try(x_full(i % n_x), (i / n_x) & 1); it++) {}
         }
     } else if (warp == 1) {
-        // The whole warp waits, so that addresses and descriptors stay in uniform registers;
-        // one lane issues.  D f32, A and B f16, both along K; N and M.
-        const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(VT >> 4) << 24);
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one
+        // lane issues.  Of a pair the first block issues, and the second tells it of its operands.
+        // D f32, A and B f16, both along K; N and M.
+        const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(VT * SIDES >> 4) << 24);
         const bool issuer = elect_one();
         Place pa, px, acc;
         bool ok = true;
-        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
+        for (int item = first; item < n_items && ok; item += step) {
             if (!is_active(item)) continue;
-            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+            if (side == 0 && !(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
             const uint32_t d = tmem + acc.s * N;
             int in_group = 0;
             for (int k = 0; k < n_k; k++, pa.next(N_A)) {
                 if (!(ok = in_group ? warp_wait(a_full(pa.s), pa.parity, failed)
                                     : warp_wait2(x_full(px.s), px.parity, a_full(pa.s), pa.parity, failed)))
                     break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t da = operand_desc(a_at(pa.s)), db = operand_desc(x_at(px.s) + in_group * x_block);
-                const bool last = ++in_group == x_group || k + 1 == n_k;
-                if (issuer) {
+                const bool last = in_group + 1 == x_group || k + 1 == n_k;
+                if (side == 0) {
+                    if (PAIR && !(ok = warp_wait(other_full(pa.s), pa.parity, failed))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = operand_desc(a_at(pa.s)), db = operand_desc(x_at(px.s) + in_group * x_block);
+                    if (issuer) {
 #pragma unroll
-                    for (int j = 0; j < KB / 16; j++) mma_f16(d, da + 2 * j, db + 2 * j, idesc, k | j);
-                    mma_commit(a_empty(pa.s));
-                    if (last) mma_commit(x_empty(px.s));
-                    if (k + 1 == n_k) mma_commit(acc_full(acc.s));
+                        for (int j = 0; j < KB / 16; j++) mma_f16<PAIR>(d, da + 2 * j, db + 2 * j, idesc, k | j);
+                        mma_commit<PAIR>(a_empty(pa.s));
+                        if (last) mma_commit<PAIR>(x_empty(px.s));
+                        if (k + 1 == n_k) mma_commit<PAIR>(acc_full(acc.s));
+                    }
+                } else if (issuer) {
+                    arrive_at_first(other_full(pa.s));
                 }
+                in_group++;
                 if (last) in_group = 0, px.next(n_x);
             }
             acc.next(2);
         }
-        if (!ok && issuer) {                          // let the products in flight finish
-            mma_commit(drained);
+        if (!ok && issuer && side == 0) {             // let the products in flight finish
+            mma_commit<PAIR>(drained);
+            if (PAIR) mma_commit<PAIR>(drained);
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= 8) {
@@ -584,7 +659,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
         Place pr;
         uint32_t parity = 1;                          // of the group's slot's next release
         bool ok = true;                               // the same in all lanes
-        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
+        for (int item = first; item < n_items && ok; item += step) {
             if (!is_active(item)) continue;
             for (int k = (group - c) & (N_A - 1); k < n_k; k += N_A) {
                 const int s = group;
@@ -633,9 +708,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
     } else if (warp >= 4) {
         const int quad = warp & 3;
         Place acc;
-        for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+        for (int item = first; item < n_items; item += step) {
             const bool active = is_active(item);
-            const int vt = item / n_nt, t0 = (item - vt * n_nt) * N, n = min(N, h.T - t0);
+            const int vt = item / n_nt * SIDES + side, t0 = item % n_nt * N, n = min(N, h.T - t0);
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
             // the tile's scales and mask words (a lane per token), read while its products run
             const float sw = v < h.V ? h.w_scale[v] : 0.f;
@@ -675,7 +750,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             if (active) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty(acc.s));
+                if (lane == 0) {
+                    if (PAIR) arrive_at_first(acc_empty(acc.s));
+                    else mbar_arrive(acc_empty(acc.s));
+                }
                 acc.next(2);
             }
         }
@@ -683,9 +761,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();                         // nothing of this block is used by the other any more
     if (warp == 3) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
     }
     if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
 }
@@ -717,7 +797,7 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     uint8_t* flags = work + p.flags_at;
     CUtensorMap w_map, x_map;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, h.K, h.V, h.w_stride, 128, VT) ||
-        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x, p.Kp, h.T, (uint64_t)p.Kp * 2, KB, p.N))
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x, p.Kp, h.T, (uint64_t)p.Kp * 2, KB, p.pair ? p.N / 2 : p.N))
         return ops_fail(PSC_ERR_CUDA, "psc_head_logits", "cuTensorMapEncodeTiled failed");
     const int items = p.n_vt * p.n_nt;
     const int x_blocks = (int)(((int64_t)h.T * (p.Kp / 16) + 255) / 256);
@@ -726,8 +806,10 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     if (s != PSC_OK) return s;
     const int leave_few = h.T <= 16 && h.bitmask && 16 * (int64_t)((h.K + 15) / 16 * 16) <= ROWS_X_MAX;
     if (leave_few && (s = head_rows<T, 16>(h, logits, work, cs, flags, items)) != PSC_OK) return s;
-    return ops_launch(k_head_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_head_mma",
-                      w_map, x_map, h, logits, p.N, p.n_nt, items, p.Kp, p.n_raw, p.n_x, p.x_group, p.tmem, faults,
+    const int sides = p.pair ? 2 : 1, wide = (p.n_vt + sides - 1) / sides * p.n_nt;
+    return ops_launch(p.pair ? k_head_mma<T, true> : k_head_mma<T, false>,
+                      dim3(std::min(wide, current_sms() / sides) * sides), MMA_THREADS, p.smem, sides, cs, "k_head_mma",
+                      w_map, x_map, h, logits, p.N, p.n_nt, p.n_vt, p.Kp, p.n_raw, p.n_x, p.x_group, p.tmem, faults,
                       (const uint8_t*)flags, leave_few);
 }
 
