@@ -87,7 +87,7 @@ psc_status psc_process_logits(const void* d_logits, psc_dtype dtype, int64_t row
                               const float* d_presence, const int32_t* d_bias_ids, const float* d_bias, int32_t n_bias,
                               const uint32_t* d_bitmask, void* stream);
 
-/* Bytes of workspace that psc_sample needs for a batch of this size. */
+/* Bytes of workspace that psc_sample needs for a batch of this size (0: none). */
 int64_t psc_sample_work_bytes(int32_t B);
 
 /* Draws one token per row among the allowed ones, from one uniform number.
@@ -111,8 +111,8 @@ int64_t psc_sample_work_bytes(int32_t B);
  *   d_tokens   : int32 [B]; -1 where a row has no candidate (as psc_argmax_masked)
  *   d_logprobs : float [B] or NULL: ln of the probability with which the token was drawn
  *                (weight over the sum of what stays; -inf where there is no candidate)
- *   d_work     : at least psc_sample_work_bytes(B) bytes; calls that overlap on the GPU need
- *                workspaces of their own
+ *   d_work     : at least psc_sample_work_bytes(B) bytes (NULL if that is 0); calls that
+ *                overlap on the GPU need workspaces of their own
  * PSC_ERR_LIMIT: V over 4,194,304 (the sum of the weights stays below 2^63). */
 psc_status psc_sample(const void* d_logits, psc_dtype dtype, int64_t row_stride, int32_t B, int32_t V,
                       const uint32_t* d_bitmask, const float* d_uniform, const float* d_temperature,

@@ -1428,7 +1428,7 @@ psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t*
 
 }  // namespace
 
-extern "C" int64_t psc_sample_work_bytes(int32_t B) { return B > 0 ? ((int64_t)B + 15) / 16 * 16 : 16; }
+extern "C" int64_t psc_sample_work_bytes(int32_t B) { return B < THREE_KERNELS ? 0 : ((int64_t)B + 15) / 16 * 16; }
 
 extern "C" psc_status psc_sample(const void* d_logits, psc_dtype dtype, int64_t row_stride, int32_t B, int32_t V,
                                  const uint32_t* d_bitmask, const float* d_uniform, const float* d_temperature,
@@ -1441,7 +1441,7 @@ extern "C" psc_status psc_sample(const void* d_logits, psc_dtype dtype, int64_t 
     if (V > MAX_V) return ops_fail(PSC_ERR_LIMIT, me, "vocabulary over 4,194,304 tokens");
     if (B > 0x7fffffff / MAX_CLUSTER) return ops_fail(PSC_ERR_LIMIT, me, "batch too large");
     if (B == 0) return PSC_OK;
-    if (!d_work || work_bytes < psc_sample_work_bytes(B))
+    if (psc_sample_work_bytes(B) && (!d_work || work_bytes < psc_sample_work_bytes(B)))
         return ops_fail(PSC_ERR_ARG, me, "workspace missing or too small");
     const Settings S{d_uniform, d_temperature, d_top_k, d_top_p, d_min_p};
     if (dtype == PSC_BF16)

@@ -136,13 +136,13 @@ def _ptr(t, dtype=None, name="tensor", n=None):
     writes (a smaller or non-contiguous tensor is refused before any launch)."""
     if t is None:
         return None
+    if t.is_cuda and (dtype is None or t.dtype is dtype) and (n is None or (t.numel() >= n and t.is_contiguous())):
+        return t.data_ptr()
     if n is not None and (t.numel() < n or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous tensor of at least {n} elements")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
 
 
 def _dtype_code(t):
@@ -455,13 +455,15 @@ def psc_fill_apply_noalloc(h: Handle, q, depth, status, stack, logits, bitmask_o
 def _rows(t, dtype, name, rows=None, cols=None):
     """(device address, row stride) of a 2-D tensor with unit column stride, at
     least `rows` x `cols` elements."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] < cols):
+    (r, c), (stride, unit) = t.shape, t.stride()
+    if c > 1 and unit != 1:
+        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
+    if (rows is not None and r != rows) or (cols is not None and c < cols):
         raise ValueError(f"{name} must be [{rows}, >={cols}], got {list(t.shape)}")
-    # a row of its own or a column of its own may carry any stride
-    stride = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-    return _ptr(t, dtype, name), stride
+    # a row of its own may carry any stride
+    return _ptr(t, dtype, name), stride if r > 1 else max(c, stride)
 
 
 def _mask_ptr(bitmask, B, V):
@@ -567,7 +569,7 @@ def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature
     """tokens[b] := a token drawn among the allowed ones with uniform[b] (f32 in [0, 1)),
     logprobs[b] := ln of the probability it was drawn with.  temperature, top_p,
     min_p f32 [B], top_k int32 [B]; None leaves a filter off (temperature 1).  work: a
-    uint8 tensor of at least psc_sample_work_bytes(B) bytes to reuse."""
+    uint8 tensor of at least psc_sample_work_bytes(B) bytes to reuse (0 for small batches)."""
     import torch
     if logits.dim() != 2:
         raise ValueError("logits must be a 2-D tensor")
@@ -575,15 +577,15 @@ def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature
     V = logits.shape[1] if V is None else V
     code = _dtype_code(logits)
     pl, sl = _rows(logits, None, "logits", B, V)
-    n = (B + 15) // 16 * 16 or 16           # psc_sample_work_bytes(B)
-    if work is None:
+    n = load().psc_sample_work_bytes(B)
+    if work is None and n:
         work = _workspace(n, logits.device, stream)
     _check(load().psc_sample(
         pl, code, sl, B, V, _mask_ptr(bitmask, B, V), _ptr(uniform, torch.float32, "uniform", B),
         _ptr(temperature, torch.float32, "temperature", B), _ptr(top_k, torch.int32, "top_k", B),
         _ptr(top_p, torch.float32, "top_p", B), _ptr(min_p, torch.float32, "min_p", B),
         _ptr(tokens, torch.int32, "tokens", B), _ptr(logprobs, torch.float32, "logprobs", B),
-        _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+        _ptr(work, torch.uint8, "work", n), n, _stream(stream)))
 
 
 def psc_sample_work_bytes(B: int) -> int:

@@ -69,7 +69,7 @@ ARG, LIMIT = 1, 5
     (_process(out=P + 50), ARG), (_process(out=P + 198, stride=198, out_stride=198), ARG),
     (_process(hist=P, H=1 << 24, hist_stride=1 << 24), LIMIT), (_process(n=4097, ids=P, bias=P), LIMIT),
     (_sample(logits=None), ARG), (_sample(u=None), ARG), (_sample(tokens=None), ARG), (_sample(dtype=3), ARG),
-    (_sample(stride=99), ARG), (_sample(work=None), ARG), (_sample(n=15), ARG), (_sample(B=-1), ARG), (_sample(V=0), ARG), (_sample(V=(1 << 22) + 1, stride=1 << 23), LIMIT),
+    (_sample(stride=99), ARG), (_sample(B=48, work=None), ARG), (_sample(B=49, n=63), ARG), (_sample(B=-1), ARG), (_sample(V=0), ARG), (_sample(V=(1 << 22) + 1, stride=1 << 23), LIMIT),
 ])
 def test_wrong_arguments_are_refused(psc, call, code):  # noqa: F811
     name, args = call
