@@ -116,7 +116,8 @@ __global__ void __launch_bounds__(256) k_pack_rows(const int8_t* w, int64_t stri
 // all that counts; a tensor core would spend its time on 128-row operands that hardly any
 // column uses (about 56 cycles per product of 16 columns of K, whatever N).  Under a mask,
 // rows that no token allows are not read.  Measured without a mask on 128,256 x 2048 (with
-// k_head_mma in brackets): 1 token 45 us (64), 4 tokens 49 (62), 8 tokens 71 (62).
+// k_head_mma in brackets): 1 token 45 us (64), 4 tokens 49 (62), 8 tokens 71 (62).  One token
+// over 262,144 x 4096: 167 us, 6.4 TB/s.
 constexpr int ROWS = 4;
 constexpr int ROWS_THREADS = 256;
 constexpr int ROWS_X_MAX = 64 * 1024;         // bytes of tokens held in shared memory
@@ -248,8 +249,9 @@ psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs, c
                      int n_tiles = 0) {
     const size_t smem = (size_t)N * ((h.K + 15) / 16) * 16;
     const int per_sm = N > 4 ? 2 : 3, items = h.bitmask ? h.W : (h.V + ROWS - 1) / ROWS;     // as their registers allow
-    return ops_launch(h.bitmask ? k_head_rows<T, N, true> : k_head_rows<T, N, false>, dim3(std::min((items + 7) / 8, current_sms() * per_sm)), ROWS_THREADS, smem, 1,
-                      cs, "k_head_rows", h, logits, (int*)work, flags, n_tiles);
+    return ops_launch(h.bitmask ? k_head_rows<T, N, true> : k_head_rows<T, N, false>,
+                      dim3(std::min((items + 7) / 8, current_sms() * per_sm)), ROWS_THREADS, smem, 1, cs,
+                      "k_head_rows", h, logits, (int*)work, flags, n_tiles);
 }
 
 // ------------------------------------------------------------ the tensor-core path
@@ -269,7 +271,8 @@ psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs, c
 // tokens in and out 64), 875 cycles where the products take 512.  So blocks pair up (PAIR):
 // 256 rows of weights, 128 in each, by the same tokens, half in each (tcgen05's
 // cta_group::2), which leaves 80 KB.  256 tokens over 262,144 x 4096: 424 -> 364 us, 1511
-// TFLOP/s; 64 tokens over 128,256 x 2048: 66 us alone, 77 in pairs.
+// TFLOP/s; 64 tokens over 128,256 x 2048: 66 us alone, 77 in pairs; 128 tokens over 128,256 x
+// 4096: 157 alone, 149 in pairs.  1024 tokens over 262,144 x 2048: 682 us, 1612 TFLOP/s.
 // Byte b becomes f16 without a conversion: b + 128 under the exponent of 1024 is
 // 1152 + b, minus 1152; five instructions for four bytes.
 constexpr int VT = 128;                       // vocabulary rows of a tile
@@ -284,7 +287,7 @@ constexpr int SMEM_MAX = 227 * 1024;
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
     bool pair;                                // two blocks work on 256 vocabulary rows together
-    int n_raw, n_x, x_group;                  // stages of the byte ring, of the tokens' ring; columns' stages in one of those
+    int n_raw, n_x, x_group;                  // stages of the byte ring, of the tokens' ring; K stages in one of those
     int Kp;                                   // K rounded up to whole stages
     int tmem;                                 // TMEM columns
     size_t smem;
@@ -302,8 +305,9 @@ Plan plan_of(int T, int V, int K) {
     if (p.pair) p.N = (p.N + 31) / 32 * 32;
     p.Kp = (K + KB - 1) / KB * KB;
     // A stage of the tokens' ring holds several columns' stages where those are small, so
-    // that the issuing warp waits and releases seldom; the byte ring, which covers the
-    // memory's latency, gets the shared memory that is left.
+    // that the issuing warp waits and releases seldom (16 tokens over 128,256 x 2048: 63 us, with
+    // one a stage 79); the byte ring, which covers the memory's latency, gets the shared memory
+    // that is left.
     const int own = p.pair ? p.N / 2 : p.N;   // tokens in a block's shared memory
     p.x_group = own <= 32 ? 4 : own <= 64 ? 2 : 1;
     const int x_bytes = own * KB * 2 * p.x_group;
@@ -408,8 +412,8 @@ template <bool PAIR>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     if (PAIR)
         asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-            "h"((uint16_t)3)
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+            ::"r"(bar), "h"((uint16_t)3)
             : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -720,7 +724,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             for (int i = 0; i < NT_MAX / 32; i++) {
                 const int t = i * 32 + lane;
                 st[i] = t < n ? h.scale[t0 + t] : 0.f;
-                word[i] = !masked ? FULL : active && t < n && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.mask_stride + wi] : 0u;
+                const bool there = active && t < n && wi < h.W;
+                word[i] = !masked ? FULL : there ? h.bitmask[(size_t)(t0 + t) * h.mask_stride + wi] : 0u;
             }
             if (active) {
                 if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
@@ -797,7 +802,8 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     uint8_t* flags = work + p.flags_at;
     CUtensorMap w_map, x_map;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, h.K, h.V, h.w_stride, 128, VT) ||
-        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x, p.Kp, h.T, (uint64_t)p.Kp * 2, KB, p.pair ? p.N / 2 : p.N))
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x, p.Kp, h.T, (uint64_t)p.Kp * 2, KB,
+                    p.pair ? p.N / 2 : p.N))
         return ops_fail(PSC_ERR_CUDA, "psc_head_logits", "cuTensorMapEncodeTiled failed");
     const int items = p.n_vt * p.n_nt;
     const int x_blocks = (int)(((int64_t)h.T * (p.Kp / 16) + 255) / 256);
@@ -813,9 +819,11 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
                       (const uint8_t*)flags, leave_few);
 }
 
-// Weights whose rows are not at 16-byte-aligned addresses are packed into the workspace a slab at
-// a time: about 40 MB, which the L2 still holds when the products read it.
-constexpr int64_t SLAB_BYTES = 40 << 20;
+// Weights whose rows are not at 16-byte-aligned addresses are packed into the workspace, a slab
+// at a time where that is more than 256 MB.  (128,256 x 2047, with 40 MB slabs, which the L2 still
+// holds when the products read them, in brackets: 1 token 130 us (143), 256 tokens 187 (325): the
+// start and the end of every slab's kernels cost more than its second trip from memory.)
+constexpr int64_t SLAB_BYTES = 256 << 20;
 int slab_rows(int V, int K) {
     const int64_t pitch = (K + 15) / 16 * 16;
     return (int)std::min<int64_t>((V + VT - 1) / VT * VT, std::max<int64_t>(VT, SLAB_BYTES / pitch / VT * VT));
@@ -895,7 +903,8 @@ psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_s
     if (T == 0) return PSC_OK;
     if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_work_bytes(T, V, K, is_packed(d_w, w_stride)))
         return ops_fail(PSC_ERR_ARG, me, "workspace missing, unaligned or too small");
-    const Head h{d_q, q_stride, d_scale, T, d_w, w_stride, d_w_scale, V, K, d_bitmask, (V + 31) / 32, (V + 31) / 32, row_stride, 1};
+    const int W = (V + 31) / 32;
+    const Head h{d_q, q_stride, d_scale, T, d_w, w_stride, d_w_scale, V, K, d_bitmask, W, W, row_stride, 1};
     if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
     return head(h, (float*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
 }

@@ -38,26 +38,28 @@ inline int current_sms() {
     return n > 0 ? n : 1;
 }
 
-// Allows `smem` bytes of dynamic shared memory for a kernel on the
-// current device; what this thread has already allowed is not asked for again.
-inline psc_status allow_smem(const void* kernel, int smem, const char* what) {
+// Lets a kernel use all the dynamic shared memory of the current device beside its own (once
+// per kernel, device and thread; always the same amount, so that threads cannot undo each
+// other's setting).
+inline psc_status allow_smem(const void* kernel, const char* what) {
     struct Allowed {
         const void* kernel;
-        int dev, smem;
+        int dev;
     };
     static thread_local Allowed known[64];
     static thread_local int n = 0;
-    int dev = 0;
+    int dev = 0, most = 0;
     cudaGetDevice(&dev);
-    Allowed* a = nullptr;
-    for (int i = 0; i < n && !a; i++)
-        if (known[i].kernel == kernel && known[i].dev == dev) a = &known[i];
-    if (a && a->smem >= smem) return PSC_OK;
-    psc_status s = ops_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem), what);
-    if (s != PSC_OK) return s;
-    if (!a && n < 64) a = &known[n++];
-    if (a) *a = {kernel, dev, smem};
-    return PSC_OK;
+    for (int i = 0; i < n; i++)
+        if (known[i].kernel == kernel && known[i].dev == dev) return PSC_OK;
+    cudaFuncAttributes of = {};
+    psc_status s = ops_check(cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev), what);
+    if (s == PSC_OK) s = ops_check(cudaFuncGetAttributes(&of, kernel), what);
+    if (s == PSC_OK)
+        s = ops_check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           most - (int)of.sharedSizeBytes), what);
+    if (s == PSC_OK && n < 64) known[n++] = {kernel, dev};
+    return s;
 }
 
 inline bool is_dtype(psc_dtype d) { return d == PSC_F32 || d == PSC_BF16; }
@@ -72,7 +74,7 @@ template <typename... KArgs, typename... Args>
 psc_status ops_launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t cs,
                       const char* what, Args... args) {
     if (smem > 16 * 1024) {                     // with what a kernel declares itself, 48 KB need no asking
-        psc_status s = allow_smem((const void*)kernel, (int)smem, what);
+        psc_status s = allow_smem((const void*)kernel, what);
         if (s != PSC_OK) return s;
     }
     cudaLaunchConfig_t cfg = {};
@@ -98,8 +100,5 @@ __device__ __forceinline__ float load_f32(const float* p) { return *p; }
 __device__ __forceinline__ float load_f32(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// Whether the packed mask row (NULL: no mask) allows token v.
-__device__ __forceinline__ bool allows(const uint32_t* row, int v) { return !row || (row[v >> 5] >> (v & 31)) & 1; }
 
 }  // namespace

@@ -19,7 +19,7 @@ constexpr uint32_t SEEN = 1u << 30;             // the token is in the prompt
 constexpr uint32_t COUNT = (1u << 24) - 1;      // times in the output
 constexpr uint32_t EMPTY = 0xffffffffu;
 
-constexpr int HASH_SLOTS = 16384;               // most slots of a hashed table
+constexpr int HASH_SLOTS = 8192;                // most slots of a hashed table: see TableKind
 constexpr int TABLE_BYTES = 192 * 1024;         // of a direct table at most
 
 template <typename T>
@@ -49,8 +49,8 @@ __device__ __forceinline__ uint4 mask_piece(uint4 v, uint32_t bits) {
 
 // out = mask ? logits : -inf, a warp per 1024 columns.
 template <typename T>
-__global__ void __launch_bounds__(256, 4) k_mask_copy(const T* logits, int64_t stride, T* out, int64_t out_stride, int B,
-                                                   int V, const uint32_t* bitmask, int W, int vec) {
+__global__ void __launch_bounds__(256, 4) k_mask_copy(const T* logits, int64_t stride, T* out, int64_t out_stride,
+                                                      int B, int V, const uint32_t* bitmask, int W, int vec) {
     constexpr int E = 16 / sizeof(T), PASSES = 1024 / (32 * E);
     const int lane = threadIdx.x & 31;
     const int cpr = (V + 1023) >> 10;
@@ -143,17 +143,21 @@ __host__ __device__ inline int hash_cap(int entries) {
     return cap;
 }
 
-// A direct table's words are 16 bits while no count can pass 15 (SHORT), 32 otherwise.
-// Hashed tables are worked by 256 threads where there are rows for every SM (four blocks of an
-// SM hide each other's latency; 1024 rows of 262,144 tokens: 34 us, 41 with 512 threads), else
-// by 1024 (64 rows of up to 2,047 ids and 300 biases: see the launch).
+// A direct table's words are 16 bits while no count can pass 15 (SHORT), 32 otherwise.  Hashed
+// tables, for up to 4,096 ids (64 rows of 151,936 tokens: 25 us, direct 23; 201 rows: 55, direct
+// 67; 64 rows of 8,192 ids: 35, direct 25), are worked by 1024 threads (WIDE); by 256 where
+// there are rows for every SM and under 2,048 ids in each: four blocks of an SM hide each other's
+// latency (201 rows of 151,936 tokens: 1,024 ids 38 us, with 1024 threads 41; 4,096 ids 79 and
+// 55; 64 rows of 2,047 ids of 32,000 tokens 24 and 13).
 enum TableKind { HASHED, WIDE, SHORT, LONG };
 constexpr int SHORT_HISTORY = 32767;
+constexpr int WIDE_HISTORY = 2048;
 __host__ __device__ constexpr int table_threads(TableKind k) { return k == HASHED ? 256 : 1024; }
 
 template <typename T, TableKind KIND>
-__global__ void __launch_bounds__(table_threads(KIND), KIND == HASHED ? 4 : 1) k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V,
-                                                  Penalties P, const uint32_t* bitmask, int W, int shares, int early) {
+__global__ void __launch_bounds__(table_threads(KIND), KIND == HASHED ? 4 : 1)
+    k_penalize(const T* logits, int64_t stride, T* out, int64_t out_stride, int V, Penalties P,
+               const uint32_t* bitmask, int W, int shares, int early) {
     constexpr bool HASH = KIND == HASHED || KIND == WIDE;
     constexpr int NT = table_threads(KIND);
     extern __shared__ uint32_t tab[];
@@ -312,9 +316,12 @@ psc_status process(const T* logits, int64_t stride, T* out, int64_t out_stride, 
     }
     if (s != PSC_OK || (!P.H && !P.n_bias)) return s;
     const size_t bias_bytes = P.n_bias ? (size_t)hash_cap(P.n_bias) * 8 : 0;
-    if (2 * P.H <= HASH_SLOTS)
-        return ops_launch(B > current_sms() ? k_penalize<T, HASHED> : k_penalize<T, WIDE>, dim3(B),
-                          table_threads(B > current_sms() ? HASHED : WIDE), bias_bytes + (size_t)hash_cap(P.H) * 8, 1, cs, "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, 0, early);
+    if (2 * P.H <= HASH_SLOTS) {
+        const bool wide = B <= current_sms() || P.H >= WIDE_HISTORY;
+        return ops_launch(wide ? k_penalize<T, WIDE> : k_penalize<T, HASHED>, dim3(B),
+                          table_threads(wide ? WIDE : HASHED), bias_bytes + (size_t)hash_cap(P.H) * 8, 1, cs,
+                          "k_penalize", logits, stride, out, out_stride, V, P, bitmask, W, 0, early);
+    }
     const bool narrow = P.H <= SHORT_HISTORY;
     const int word = narrow ? 2 : 4;
     int shares = 0;

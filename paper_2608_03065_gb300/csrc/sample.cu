@@ -4,12 +4,14 @@
 // Every filter keeps the tokens whose logit is at least some value: the k-th
 // largest; the smallest whose strictly larger ones hold less than p of the
 // weight; the one where e^z reaches min_p.  So a row is filtered by one
-// threshold, found digit by digit of the logits' order (a histogram per 8-bit
-// digit, of counts for top-k, of weights for top-p), and the draw is the same
-// search by token.  Weights are whole numbers of 2^-40 of the largest: integer
-// sums are the same in any order, so neither the atomics nor the split of a row
-// over blocks can change a draw.  41 bits hold every f32 e^z over 2^-17 exactly;
-// what is rounded away of a row is below V * 2^-41 of its largest weight.
+// threshold, and what the threshold needs lies near the top: the row is read
+// once for its maxima, the few tokens near them are listed in shared memory, and
+// the filters and the draw are worked out in that list.  Only where all of the
+// weight counts (top-p alone, or no filter) is the row weighed in later passes.
+// Weights are whole numbers of 2^-40 of the largest: integer sums are the same in
+// any order, so neither the atomics nor the split of a row over blocks can change
+// a draw.  41 bits hold every f32 e^z over 2^-17 exactly; what is rounded away of
+// a row is below V * 2^-41 of its largest weight.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -122,7 +124,6 @@ struct Piece<float> {
 };
 
 // The lane's piece that starts at v0 (nothing read where no token of it is allowed).
-template <typename T, bool VEC>
 __device__ __forceinline__ uint32_t piece_bits(const Row& r, int v0) {
     const int n = r.hi - v0;
     uint32_t bits = n <= 0 ? 0u : r.mask ? r.mask[v0 >> 3] : 0xffu;
@@ -163,7 +164,7 @@ __device__ __forceinline__ void for_pieces(const Row& r, const uint4* lut, F&& f
         Piece<T> p[PIECES];
         uint32_t bits[PIECES];
 #pragma unroll
-        for (int q = 0; q < PIECES; q++) bits[q] = piece_bits<T, VEC>(r, v0 + q * 256);
+        for (int q = 0; q < PIECES; q++) bits[q] = piece_bits(r, v0 + q * 256);
 #pragma unroll
         for (int q = 0; q < PIECES; q++) read_piece<T, VEC>(r, v0 + q * 256, bits[q], p[q]);
 #pragma unroll 1
@@ -215,7 +216,7 @@ __device__ __forceinline__ void for_groups(const Row& r, const uint4* lut, const
             if (i < jobs) {
                 for (; h; h--) left &= left - 1;
                 v0[t] = r.lo + (warp + j * NW) * CHUNK + q * 256 + (__ffs(left) - 1) * 8;
-                bits[t] = piece_bits<T, VEC>(r, v0[t]);
+                bits[t] = piece_bits(r, v0[t]);
             }
         }
 #pragma unroll
@@ -299,9 +300,9 @@ enum { ALL_ROWS, HEAVY_ROWS, PENDING_ROWS };
 // What is found out about a row, kept in shared memory: a register that lives across the
 // passes is one that they do not have.
 struct State {
-    int b, k, odd, n, bin, own;
+    int b, k, n, bin, own;
     float p, m, lowest, bound, z_from, z_to;
-    uint32_t p24, u24, tau;
+    uint32_t p24, u24;
     bool in_doubt, hit;
     u64 listed, left;
 };
@@ -319,7 +320,7 @@ struct Shared {
     u64 warp[2][NW];                    // the warps' shares of what a block combines
     uint8_t turn[NT];                   // which of the two a thread uses next
     u64 found[2];
-    int at, n, from, to;
+    int at, n;
     uint4 lut[256];                     // mask byte -> ones where it allows (bf16 pairs)
     uint32_t key[LIST];                 // candidates: order of the value, token, weight
     uint32_t token[LIST];
@@ -827,7 +828,7 @@ __device__ __noinline__ void sample_pass(Shared& s, float bound, float unit, flo
     const int v0 = r.lo + (int)((int64_t)warp * n_chunks / n_sample) * CHUNK + lane * 8;
 #pragma unroll 1
     for (int q = 0; q < taken; q++) {
-        const uint32_t bits = piece_bits<T, VEC>(r, v0 + q * 256);
+        const uint32_t bits = piece_bits(r, v0 + q * 256);
         if (!bits) continue;
         Piece<T> one;
         read_piece<T, VEC>(r, v0 + q * 256, bits, one);
@@ -1175,7 +1176,7 @@ __device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
         u64 w[8], in = 0, all;
         Piece<T> q;
         if (warp < PIECES) {
-            const uint32_t bits = piece_bits<T, VEC>(r, v0);
+            const uint32_t bits = piece_bits(r, v0);
             read_piece<T, VEC>(r, v0, bits, q);
             mask_piece<T>(s.lut, bits, q);
 #pragma unroll
@@ -1400,9 +1401,12 @@ int split(int rows, int V, size_t bytes) {
     return cluster;
 }
 
-// Batches of at least this many rows, with top-k or min-p, are done by three kernels.
+// Batches of at least this many rows, with top-k or min-p, are done by three kernels, of which the
+// first splits its rows as if a fifth of the batch were heavy.  (Rows of which two in five are, of
+// 128,256 tokens, one kernel's time in brackets: 64 rows 48 us (53), 80 rows 49 (66), 256 rows 80
+// (128), 512 rows 123 (157).  A heavy row of many is split at least in two: 1024 rows of 262,144
+// tokens 316 us, not split 331, in four 379.)
 constexpr int THREE_KERNELS = 48;
-constexpr int HEAVY_SPLIT = 4;          // blocks per heavy row then
 
 template <typename T>
 psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t* bitmask, const Settings& S,
@@ -1417,8 +1421,7 @@ psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t*
                           cs, "k_sample", j);
     };
     if (B < THREE_KERNELS || V > 1 << 20 || !(S.top_k || S.min_p)) return launch(ALL_ROWS, split(B, V, sizeof(T)));
-    // heavy rows are few of a mixed batch (a fifth, say) and slow
-    psc_status s = launch(HEAVY_ROWS, split(std::min(B, 2 * current_sms() / HEAVY_SPLIT), V, sizeof(T)));
+    psc_status s = launch(HEAVY_ROWS, split(std::min(B / 5, current_sms()), V, sizeof(T)));
     if (s != PSC_OK) return s;
     j.per_block = (V + CHUNK - 1) / CHUNK * CHUNK;
     s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT, sizeof(Shared), 1, cs,

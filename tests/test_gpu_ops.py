@@ -172,6 +172,24 @@ def test_head_logits_of_several_slabs(psc, T, V, K, pad, shift):
     _head_case(psc, T, V, K, "f32", "none", pad=pad, shift=shift, out_pad=2)
 
 
+@pytest.mark.parametrize("T", [1, 12, 257])
+def test_head_logits_of_large_unaligned_weights_are_those_of_aligned_ones(psc, T):
+    """The same sums and the same epilogue, so the same bits, where the packed rows pass a slab of 256 MB."""
+    V, K = 140001, 2047
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q = torch.randint(-127, 128, (T, K), generator=g, dtype=torch.int8, device="cuda")
+    w = torch.randint(-127, 128, (V, K), generator=g, dtype=torch.int8, device="cuda")
+    sx, sw = torch.rand(T, generator=g, device="cuda"), torch.rand(V, generator=g, device="cuda")
+    bits = torch.randint(-2 ** 31, 2 ** 31 - 1, (T, (V + 31) // 32), generator=g, dtype=torch.int32, device="cuda")
+    aligned = torch.zeros(V, 2048, dtype=torch.int8, device="cuda")
+    aligned[:, :K] = w
+    for mask in (None, bits):
+        here, there = (torch.empty(T, V, device="cuda") for _ in range(2))
+        psc.psc_head_logits(q, sx, w, sw, here, bitmask=mask)
+        psc.psc_head_logits(q, sx, aligned[:, :K], sw, there, bitmask=mask)
+        assert torch.equal(here, there)
+
+
 @pytest.mark.parametrize("T", [1, 4, 20, 150])
 @pytest.mark.parametrize("fill", [127, -128])
 def test_head_logits_largest_sums(psc, T, fill):
