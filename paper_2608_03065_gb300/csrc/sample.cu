@@ -27,6 +27,7 @@ constexpr int NW = NT / 32;
 constexpr int PIECES = 4;               // pieces of 8 neighbouring tokens that a lane has in flight
 constexpr int CHUNK = PIECES * 256;     // tokens a warp takes at a time
 constexpr int LIST = 2048;              // candidates that a block holds
+constexpr int SPAN = 8192;              // tokens of a stretch of values that it does
 constexpr int BINS = NT;                // of the histogram of the groups' maxima
 constexpr int NUCLEUS_GROUPS = 640;     // maxima above the bound from which a nucleus is looked for
 constexpr int PAIRS = 256;              // candidates that are compared pair by pair; more go to bins
@@ -322,9 +323,9 @@ struct Shared {
     u64 found[2];
     int at, n;
     uint4 lut[256];                     // mask byte -> ones where it allows (bf16 pairs)
-    uint32_t key[LIST];                 // candidates: order of the value, token, weight
-    uint32_t token[LIST];
+    uint32_t key[LIST];                 // candidates: order of the value, weight, token
     u64 weight[LIST];
+    uint32_t token[SPAN];               // (of them LIST in k_sample_light)
 };
 
 // Sum over the block's threads of v before this thread; *total: over all of them.  One
@@ -407,7 +408,7 @@ __device__ __forceinline__ u64 part_of(u64 total, u64 u24) {
     return u24 * (total >> 24) + ((u24 * (total & 0xffffff)) >> 24);
 }
 
-// The value (its order) among the block's n listed candidates at which the running weight
+// The value (its order) among the block's n candidates at which the running weight
 // from the largest down reaches `need`: few pair by pair, many digit by digit (a warp whose
 // digits are all the same adds once).
 __device__ uint32_t list_search(cg::cluster_group& cl, Shared& s, int n, u64 need) {
@@ -757,12 +758,12 @@ struct Stretch {
 };
 
 // All weights (the thread's share), those above the stretch (returned in *above, and by
-// chunk), and those inside it, in the block's bins.
+// chunk), and those inside it, in the block's bins; the stretch's tokens, listed.
 template <typename T, bool VEC>
 __device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, u64* above_all) {
     const Weigh g = s.g;
     WeightSum all, above, part;
-    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int v0, bool any) {
         if (!any) return;
         all.n += 8;
 #pragma unroll
@@ -772,7 +773,11 @@ __device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const
             WeightSum::split(e, &h, &l);
             all.hi += h, all.lo += l;
             if (z >= t.z_from) part.hi += h, part.lo += l, part.n++;
-            else if (z >= t.z_to) add_to_bin(s, t.bin(z), WeightSum::weight(h, l));
+            else if (z >= t.z_to) {
+                add_to_bin(s, t.bin(z), WeightSum::weight(h, l));
+                const int at = atomicAdd(&s.n, 1);
+                if (at < SPAN) s.token[at] = v0 + i;
+            }
         }
     }, [&](int c) {
         above.hi += part.hi, above.lo += part.lo, above.n += part.n;
@@ -782,13 +787,69 @@ __device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const
     return all.value();
 }
 
-// Lists the tokens of one bin of the stretch and adds those of the bins before it to the
-// chunks' sums.  The orders of the bin's smallest and largest value that the thread met: y, x.
+// Adds a token's weight to its chunk's: in the bins, as two words, where these are as many (an
+// atomic sum of 64 bits is a loop); add_own adds those up.
+__device__ __forceinline__ void add_to_chunk(Shared& s, u64* chunk_sum, int token, u64 w) {
+    const int c = (token - s.row.lo) / CHUNK;
+    if (s.row.hi - s.row.lo <= BINS * CHUNK) add_to_bin(s, c, w);
+    else atomicAdd(&chunk_sum[c], w);
+}
+
+// Lists the tokens of one bin of the stretch and adds those of the bins before it to the chunks
+// (in the bins, which it clears): from the tokens of the stretch, where the block holds them all.
+// The orders of the bin's smallest and largest value that the thread met: y, x.
+template <typename T>
+__device__ __noinline__ uint2 take_bin(Shared& s, u64* chunk_sum, const Stretch t, int bin) {
+    const Weigh g = s.g;
+    const Row r = s.row;
+    const int n = s.n;
+    constexpr int BATCH = 8;
+    static_assert(BATCH * NT >= LIST, "the candidates overwrite the first batch only");
+    uint2 ends = make_uint2(0u, ~0u);
+    for (int i0 = 0; i0 < n; i0 += BATCH * NT) {
+        int token[BATCH];
+#pragma unroll
+        for (int q = 0; q < BATCH; q++) {
+            const int i = i0 + q * NT + threadIdx.x;
+            token[q] = i < n ? (int)s.token[i] : -1;
+        }
+        if (i0 == 0) {
+            __syncthreads();
+            if (threadIdx.x == 0) s.n = 0;
+            __syncthreads();
+        }
+        float x[BATCH];
+#pragma unroll
+        for (int q = 0; q < BATCH; q++) x[q] = token[q] < 0 ? 0.f : load_f32(static_cast<const T*>(r.logits) + token[q]);
+#pragma unroll
+        for (int q = 0; q < BATCH; q++) {
+            if (token[q] < 0) continue;
+            const float y = clean(x[q]);
+            const int in = t.bin(g.z(y));
+            if (in == bin) {
+                const uint32_t key = ordered(y);
+                ends = make_uint2(max(ends.x, key), min(ends.y, key));
+                const int at = atomicAdd(&s.n, 1);
+                if (at < LIST) s.key[at] = key, s.token[at] = token[q];
+            } else if (in < bin) {
+                add_to_chunk(s, chunk_sum, token[q], g.raw(y));
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) s.st.own = min(s.n, LIST);
+    return ends;
+}
+
+// The same from the row, where it does not.
 template <typename T, bool VEC>
 __device__ __noinline__ uint2 bin_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, int bin) {
     const Weigh g = s.g;
     WeightSum part;
     uint2 ends = make_uint2(0u, ~0u);
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
     for_values<T, VEC>(s, odd, [&](const float (&x)[8], int v0, bool any) {
         if (!any) return;
 #pragma unroll
@@ -813,6 +874,8 @@ __device__ __noinline__ uint2 bin_pass(Shared& s, u64* chunk_sum, bool odd, cons
         put_chunk(chunk_sum, c, part);
         if ((threadIdx.x & 31) == 0) chunk_sum[c] += till_now;
     });
+    __syncthreads();
+    if (threadIdx.x == 0) s.st.own = min(s.n, LIST);
     return ends;
 }
 
@@ -1099,8 +1162,6 @@ __device__ __noinline__ void find_stretch(Shared& s) {
     if (threadIdx.x < BINS - 1 && till >= share + slack && prior < share + slack)
         s.st.z_to = top_z - (threadIdx.x + 1) / to_bin;
     blocks.sync();                          // and every block has read the bins
-    s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
-    __syncthreads();
 }
 
 // After bins_pass: whether the nucleus ends in the stretch, in which bin, and after how much of it.
@@ -1110,19 +1171,18 @@ __device__ __noinline__ void find_bin(Shared& s, u64 all, u64 above) {
     const u64 limit = limit_of(s, blocks.sum2(s, all, &over, 10));
     const u64 w = blocks.bin(s, true), till = over + block_before(s, w, &inside);
     if (till < limit && limit <= till + w) s.st.bin = threadIdx.x, s.st.left = limit - till;
-    if (threadIdx.x == 0) s.n = 0, s.st.hit = limit > over && limit <= over + inside;
+    if (threadIdx.x == 0) s.st.hit = limit > over && limit <= over + inside;
     blocks.sync();                          // and every block has read the bins
     s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
     __syncthreads();
 }
 
-// After bin_pass (ends: of the values in the bin): the value at which the nucleus ends, 0 where
+// After take_bin or bin_pass (ends: of the values in the bin): the value at which the nucleus ends, 0 where
 // the list does not tell.
 __device__ __noinline__ uint32_t find_tau(Shared& s, uint2 ends, bool* by_list) {
     const Blocks<false> blocks;
     const uint2 all = blocks.max2(s, ends.x, ~ends.y, 6);
     blocks.sync();
-    if (threadIdx.x == 0) s.st.own = min(s.n, LIST);
     if (blocks.rank() == 0) {
         cg::cluster_group cl = cg::this_cluster();
         const int n = gather(cl, s, blocks.count());
@@ -1141,11 +1201,14 @@ __device__ __noinline__ uint32_t find_tau(Shared& s, uint2 ends, bool* by_list) 
     return tau ? tau : all.x == ~all.y ? all.x : 0u;    // equal values need no list
 }
 
-// The chunks' sums hold what lies above the bin: adds the bin's own tokens that stay.
+// Adds the listed tokens of the bin that stay to the chunks, and what the bins hold of those.
 __device__ __noinline__ void add_own(Shared& s, u64* chunk_sum, uint32_t tau) {
     const Weigh g = s.g;
+    const int n_chunks = (s.row.hi - s.row.lo + CHUNK - 1) / CHUNK;
     for (int i = threadIdx.x; i < s.st.own; i += NT)
-        if (s.key[i] >= tau) atomicAdd(&chunk_sum[((int)s.token[i] - s.row.lo) / CHUNK], g.raw(unordered(s.key[i])));
+        if (s.key[i] >= tau) add_to_chunk(s, chunk_sum, (int)s.token[i], g.raw(unordered(s.key[i])));
+    __syncthreads();
+    if (n_chunks <= BINS && threadIdx.x < n_chunks) chunk_sum[threadIdx.x] += bin_weight(s, threadIdx.x);
     __syncthreads();
 }
 
@@ -1286,13 +1349,15 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                 if (done == DRAWN) return;
                 found = done == BOUNDED;
                 if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END;
-                s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
                 __syncthreads();
             }
             // The stretch looked at closely; where the nucleus does not end in it the whole row
             // is, and where its bin holds more than a list that bin is the next stretch.
             for (int turn = 0; turn < 6 && !found; turn++) {
                 u64 above;
+                s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
+                if (threadIdx.x == 0) s.n = 0;
+                __syncthreads();
                 const u64 all = bins_pass<T, VEC>(s, chunk_sum, odd, Stretch(st.z_from, st.z_to), &above);
                 find_bin(s, all, above);
                 if (!st.hit) {              // the same in all blocks
@@ -1302,14 +1367,15 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                     __syncthreads();
                     continue;
                 }
+                const Stretch t(st.z_from, st.z_to);
+                const uint2 ends = s.n <= SPAN ? take_bin<T>(s, chunk_sum, t, st.bin)
+                                               : bin_pass<T, VEC>(s, chunk_sum, odd, t, st.bin);
                 bool by_list;
-                const uint32_t tau = find_tau(s, bin_pass<T, VEC>(s, chunk_sum, odd, Stretch(st.z_from, st.z_to), st.bin),
-                                              &by_list);
+                const uint32_t tau = find_tau(s, ends, &by_list);
                 if (threadIdx.x == 0) {
                     if (tau) {
                         s.g.tau = unordered(tau);
                     } else {                // the bin's edges, a little apart
-                        const Stretch t(st.z_from, st.z_to);
                         const float off = 1e-4f / t.fine + 4e-6f * (1.f - t.top + st.bin / t.fine);
                         if (st.bin) st.z_from = t.top - st.bin / t.fine + off;
                         st.z_to = fmaxf(t.top - (st.bin + 1) / t.fine - off, Z_END);
@@ -1424,8 +1490,8 @@ psc_status sample(const T* logits, int64_t stride, int B, int V, const uint32_t*
     psc_status s = launch(HEAVY_ROWS, split(std::min(B / 5, current_sms()), V, sizeof(T)));
     if (s != PSC_OK) return s;
     j.per_block = (V + CHUNK - 1) / CHUNK * CHUNK;
-    s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT, sizeof(Shared), 1, cs,
-                   "k_sample_light", j);
+    s = ops_launch(vec ? k_sample_light<T, true> : k_sample_light<T, false>, dim3(B), NT,
+                   offsetof(Shared, token) + LIST * sizeof(uint32_t), 1, cs, "k_sample_light", j);
     return s != PSC_OK ? s : launch(PENDING_ROWS, 1);
 }
 
