@@ -27,7 +27,8 @@ constexpr int NW = NT / 32;
 constexpr int PIECES = 4;               // pieces of 8 neighbouring tokens that a lane has in flight
 constexpr int CHUNK = PIECES * 256;     // tokens a warp takes at a time
 constexpr int LIST = 2048;              // candidates that a block holds
-constexpr int SPAN = 8192;              // tokens of a stretch of values that it does
+constexpr int SPAN = 8192;              // tokens of a stretch of values that it does; with 4,096 a
+                                        // mixed batch of 1024 rows of 262,144 took 277 us, with these 270
 constexpr int BINS = NT;                // of the histogram of the groups' maxima
 constexpr int NUCLEUS_GROUPS = 640;     // maxima above the bound from which a nucleus is looked for
 constexpr int PAIRS = 256;              // candidates that are compared pair by pair; more go to bins
@@ -757,15 +758,16 @@ struct Stretch {
     __device__ __forceinline__ int bin(float z) const { return min(BINS - 1, (int)((top - z) * fine)); }
 };
 
-// All weights (the thread's share), those above the stretch (returned in *above, and by
-// chunk), and those inside it, in the block's bins; the stretch's tokens, listed.
+// All weights (the thread's share) and those above the stretch (returned in *above, and by
+// chunk); the stretch's tokens are listed, and counted where the block cannot hold them all.
 template <typename T, bool VEC>
-__device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, u64* above_all) {
+__device__ __noinline__ u64 stretch_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, u64* above_all) {
     const Weigh g = s.g;
     WeightSum all, above, part;
     for_values<T, VEC>(s, odd, [&](const float (&x)[8], int v0, bool any) {
         if (!any) return;
         all.n += 8;
+        uint32_t inside = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float z = g.z(x[i]), e = expf(z);
@@ -773,18 +775,52 @@ __device__ __noinline__ u64 bins_pass(Shared& s, u64* chunk_sum, bool odd, const
             WeightSum::split(e, &h, &l);
             all.hi += h, all.lo += l;
             if (z >= t.z_from) part.hi += h, part.lo += l, part.n++;
-            else if (z >= t.z_to) {
-                add_to_bin(s, t.bin(z), WeightSum::weight(h, l));
-                const int at = atomicAdd(&s.n, 1);
-                if (at < SPAN) s.token[at] = v0 + i;
-            }
+            else if (z >= t.z_to) inside |= 1u << i;
         }
+        if (!inside) return;
+        int at = atomicAdd(&s.n, __popc(inside));
+        for (; inside; inside &= inside - 1, at++)
+            if (at < SPAN) s.token[at] = v0 + __ffs(inside) - 1;
     }, [&](int c) {
         above.hi += part.hi, above.lo += part.lo, above.n += part.n;
         put_chunk(chunk_sum, c, part);
     });
     *above_all = above.value();
     return all.value();
+}
+
+// The weights inside the stretch, in the block's bins: from the list, every thread with some, or
+// from the row.  (In stretch_pass, where few threads of a warp have one at a time, the same work
+// made 1024 top-p rows of 262,144 tokens 20 us slower, 64 rows of 32,000 2 us.)
+template <typename T, bool VEC>
+__device__ __noinline__ void bins_pass(Shared& s, bool odd, const Stretch t) {
+    const Weigh g = s.g;
+    __syncthreads();
+    const int n = s.n;
+    if (n <= SPAN) {
+        constexpr int BATCH = 8;
+        for (int i0 = threadIdx.x; i0 < n; i0 += BATCH * NT) {
+            float x[BATCH];
+#pragma unroll
+            for (int q = 0; q < BATCH; q++)
+                x[q] = i0 + q * NT < n ? load_f32(static_cast<const T*>(s.row.logits) + s.token[i0 + q * NT]) : 0.f;
+#pragma unroll
+            for (int q = 0; q < BATCH; q++) {
+                if (i0 + q * NT >= n) break;
+                const float z = g.z(clean(x[q]));
+                add_to_bin(s, t.bin(z), weight_of(expf(z)));
+            }
+        }
+        return;
+    }
+    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
+        if (!any) return;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float z = g.z(x[i]);
+            if (z >= t.z_to && z < t.z_from) add_to_bin(s, t.bin(z), weight_of(expf(z)));
+        }
+    }, [](int) {});
 }
 
 // Adds a token's weight to its chunk's: in the bins, as two words, where these are as many (an
@@ -1164,7 +1200,7 @@ __device__ __noinline__ void find_stretch(Shared& s) {
     blocks.sync();                          // and every block has read the bins
 }
 
-// After bins_pass: whether the nucleus ends in the stretch, in which bin, and after how much of it.
+// After stretch_pass and bins_pass: whether the nucleus ends in the stretch, in which bin, and after how much of it.
 __device__ __noinline__ void find_bin(Shared& s, u64 all, u64 above) {
     const Blocks<false> blocks;
     u64 over = above, inside;
@@ -1265,10 +1301,16 @@ __device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
 // and the draw are searches in that list by the cluster's first block.  Without top-k the
 // weights have to be summed in a second pass (from L2): the nucleus is sought in the list
 // of the tokens at or above the NUCLEUS_GROUPS-th maximum or, where a sample of the row
-// says that it ends below, in the stretch of z around the sample's estimate: its weights
-// go to bins, and the bin in which the nucleus ends is listed by a third pass.  The
-// estimate decides only what is looked at: whatever it misses is searched digit by digit
-// over the whole row.  What no list holds is drawn from sums by chunk.
+// says that it ends below, in the stretch of z around the sample's estimate: its tokens are
+// listed by the same pass, their weights go to bins, and the bin in which the nucleus ends is
+// searched.  A stretch of more than SPAN tokens costs two passes more.  The estimate decides
+// only what is looked at: whatever it misses is searched digit by digit over the whole row.
+// What no list holds is drawn from sums by chunk.
+//
+// Measured (bf16, device time): 1 row of 262,144 tokens 15 us with top-k, 42 with top-p alone;
+// 1024 rows 115 us greedy, 147 top-k, 310 temperature alone, 676 top-p alone: the first two
+// at 4 TB/s and more, the others by their instructions (some 20 a token for e^z and its two
+// whole numbers).  A single row is a chain of some ten short steps with a barrier each.
 //
 // Rows that need no weights of all tokens (greedy, top-k, min-p alone) and those that do
 // differ tenfold in time and want different splits, so a large batch whose settings may hold
@@ -1358,7 +1400,9 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                 s.bins[threadIdx.x] = s.bins_hi[threadIdx.x] = 0;
                 if (threadIdx.x == 0) s.n = 0;
                 __syncthreads();
-                const u64 all = bins_pass<T, VEC>(s, chunk_sum, odd, Stretch(st.z_from, st.z_to), &above);
+                const Stretch t(st.z_from, st.z_to);
+                const u64 all = stretch_pass<T, VEC>(s, chunk_sum, odd, t, &above);
+                bins_pass<T, VEC>(s, odd, t);
                 find_bin(s, all, above);
                 if (!st.hit) {              // the same in all blocks
                     if (st.z_from == 1.f && st.z_to == Z_END) break;
@@ -1367,7 +1411,6 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                     __syncthreads();
                     continue;
                 }
-                const Stretch t(st.z_from, st.z_to);
                 const uint2 ends = s.n <= SPAN ? take_bin<T>(s, chunk_sum, t, st.bin)
                                                : bin_pass<T, VEC>(s, chunk_sum, odd, t, st.bin);
                 bool by_list;
