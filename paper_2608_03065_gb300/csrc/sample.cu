@@ -305,7 +305,7 @@ struct State {
     int b, k, n, bin, own;
     float p, m, lowest, bound, z_from, z_to;
     uint32_t p24, u24;
-    bool in_doubt, hit;
+    bool in_doubt, hit, wide;
     u64 listed, left;
 };
 
@@ -759,8 +759,9 @@ struct Stretch {
 };
 
 // All weights (the thread's share) and those above the stretch (returned in *above, and by
-// chunk); the stretch's tokens are listed, and counted where the block cannot hold them all.
-template <typename T, bool VEC>
+// chunk).  LISTED: the stretch's tokens are listed, and counted where the block cannot hold
+// them all; else their weights go to the block's bins.
+template <typename T, bool VEC, bool LISTED>
 __device__ __noinline__ u64 stretch_pass(Shared& s, u64* chunk_sum, bool odd, const Stretch t, u64* above_all) {
     const Weigh g = s.g;
     WeightSum all, above, part;
@@ -774,8 +775,12 @@ __device__ __noinline__ u64 stretch_pass(Shared& s, u64* chunk_sum, bool odd, co
             uint32_t h, l;
             WeightSum::split(e, &h, &l);
             all.hi += h, all.lo += l;
-            if (z >= t.z_from) part.hi += h, part.lo += l, part.n++;
-            else if (z >= t.z_to) inside |= 1u << i;
+            if (z >= t.z_from) {
+                part.hi += h, part.lo += l, part.n++;
+            } else if (z >= t.z_to) {
+                if (LISTED) inside |= 1u << i;
+                else add_to_bin(s, t.bin(z), WeightSum::weight(h, l));
+            }
         }
         if (!inside) return;
         int at = atomicAdd(&s.n, __popc(inside));
@@ -789,38 +794,26 @@ __device__ __noinline__ u64 stretch_pass(Shared& s, u64* chunk_sum, bool odd, co
     return all.value();
 }
 
-// The weights inside the stretch, in the block's bins: from the list, every thread with some, or
-// from the row.  (In stretch_pass, where few threads of a warp have one at a time, the same work
-// made 1024 top-p rows of 262,144 tokens 20 us slower, 64 rows of 32,000 2 us.)
-template <typename T, bool VEC>
-__device__ __noinline__ void bins_pass(Shared& s, bool odd, const Stretch t) {
+// The weights of the listed tokens of the stretch, in the block's bins.  (In stretch_pass, where
+// few threads of a warp have one at a time, the same work made 1024 top-p rows of 262,144 tokens
+// 20 us slower, 64 rows of 32,000 2 us.)
+template <typename T>
+__device__ __noinline__ void bins_pass(Shared& s, const Stretch t) {
     const Weigh g = s.g;
-    __syncthreads();
     const int n = s.n;
-    if (n <= SPAN) {
-        constexpr int BATCH = 8;
-        for (int i0 = threadIdx.x; i0 < n; i0 += BATCH * NT) {
-            float x[BATCH];
+    constexpr int BATCH = 8;
+    for (int i0 = threadIdx.x; i0 < n; i0 += BATCH * NT) {
+        float x[BATCH];
 #pragma unroll
-            for (int q = 0; q < BATCH; q++)
-                x[q] = i0 + q * NT < n ? load_f32(static_cast<const T*>(s.row.logits) + s.token[i0 + q * NT]) : 0.f;
+        for (int q = 0; q < BATCH; q++)
+            x[q] = i0 + q * NT < n ? load_f32(static_cast<const T*>(s.row.logits) + s.token[i0 + q * NT]) : 0.f;
 #pragma unroll
-            for (int q = 0; q < BATCH; q++) {
-                if (i0 + q * NT >= n) break;
-                const float z = g.z(clean(x[q]));
-                add_to_bin(s, t.bin(z), weight_of(expf(z)));
-            }
+        for (int q = 0; q < BATCH; q++) {
+            if (i0 + q * NT >= n) break;
+            const float z = g.z(clean(x[q]));
+            add_to_bin(s, t.bin(z), weight_of(expf(z)));
         }
-        return;
     }
-    for_values<T, VEC>(s, odd, [&](const float (&x)[8], int, bool any) {
-        if (!any) return;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float z = g.z(x[i]);
-            if (z >= t.z_to && z < t.z_from) add_to_bin(s, t.bin(z), weight_of(expf(z)));
-        }
-    }, [](int) {});
 }
 
 // Adds a token's weight to its chunk's: in the bins, as two words, where these are as many (an
@@ -1197,6 +1190,12 @@ __device__ __noinline__ void find_stretch(Shared& s) {
     if (threadIdx.x && till >= share - slack && prior < share - slack) s.st.z_from = top_z - threadIdx.x / to_bin;
     if (threadIdx.x < BINS - 1 && till >= share + slack && prior < share + slack)
         s.st.z_to = top_z - (threadIdx.x + 1) / to_bin;
+    // how many tokens that is of the row, from the weight of one in each bin
+    u64 tokens;
+    const float one = s.g.e(bound) * unit * expf(-(threadIdx.x + 0.5f) / to_bin);
+    const bool in = till >= share - slack && prior < share + slack;
+    block_before(s, in ? (u64)__float2uint_rn(fminf(to_float(v) / fmaxf(one, 1.f), 1e6f)) : 0, &tokens);
+    if (threadIdx.x == 0) s.st.wide = tokens * (full * PIECES) / (min(full, NW) * taken) > SPAN * blocks.count() * 7 / 8;
     blocks.sync();                          // and every block has read the bins
 }
 
@@ -1390,7 +1389,7 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                 const int done = settle_list<false>(s, 0, find_limit(s, sum_pass<T, VEC>(s, odd)), 2);
                 if (done == DRAWN) return;
                 found = done == BOUNDED;
-                if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END;
+                if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END, st.wide = true;
                 __syncthreads();
             }
             // The stretch looked at closely; where the nucleus does not end in it the whole row
@@ -1401,18 +1400,24 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                 if (threadIdx.x == 0) s.n = 0;
                 __syncthreads();
                 const Stretch t(st.z_from, st.z_to);
-                const u64 all = stretch_pass<T, VEC>(s, chunk_sum, odd, t, &above);
-                bins_pass<T, VEC>(s, odd, t);
+                u64 all;
+                if (!st.wide) {
+                    all = stretch_pass<T, VEC, true>(s, chunk_sum, odd, t, &above);
+                    __syncthreads();
+                }
+                const bool listed = !st.wide && s.n <= SPAN;
+                if (listed) bins_pass<T>(s, t);
+                else all = stretch_pass<T, VEC, false>(s, chunk_sum, odd, t, &above);
                 find_bin(s, all, above);
                 if (!st.hit) {              // the same in all blocks
                     if (st.z_from == 1.f && st.z_to == Z_END) break;
                     __syncthreads();
-                    if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END;
+                    if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END, st.wide = true;
                     __syncthreads();
                     continue;
                 }
-                const uint2 ends = s.n <= SPAN ? take_bin<T>(s, chunk_sum, t, st.bin)
-                                               : bin_pass<T, VEC>(s, chunk_sum, odd, t, st.bin);
+                const uint2 ends = listed ? take_bin<T>(s, chunk_sum, t, st.bin)
+                                          : bin_pass<T, VEC>(s, chunk_sum, odd, t, st.bin);
                 bool by_list;
                 const uint32_t tau = find_tau(s, ends, &by_list);
                 if (threadIdx.x == 0) {
@@ -1422,6 +1427,7 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                         const float off = 1e-4f / t.fine + 4e-6f * (1.f - t.top + st.bin / t.fine);
                         if (st.bin) st.z_from = t.top - st.bin / t.fine + off;
                         st.z_to = fmaxf(t.top - (st.bin + 1) / t.fine - off, Z_END);
+                        st.wide = false;
                     }
                 }
                 __syncthreads();
