@@ -1302,12 +1302,12 @@ __device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
 // of the tokens at or above the NUCLEUS_GROUPS-th maximum or, where a sample of the row
 // says that it ends below, in the stretch of z around the sample's estimate: its tokens are
 // listed by the same pass, their weights go to bins, and the bin in which the nucleus ends is
-// searched.  A stretch of more than SPAN tokens costs two passes more.  The estimate decides
+// searched.  A stretch of more than SPAN tokens costs a pass more.  The estimate decides
 // only what is looked at: whatever it misses is searched digit by digit over the whole row.
 // What no list holds is drawn from sums by chunk.
 //
-// Measured (bf16, device time): 1 row of 262,144 tokens 15 us with top-k, 42 with top-p alone;
-// 1024 rows 115 us greedy, 147 top-k, 310 temperature alone, 676 top-p alone: the first two
+// Measured (bf16, device time): 1 row of 262,144 tokens 15 us with top-k, 30 with top-p alone;
+// 1024 rows 116 us greedy, 147 top-k, 314 temperature alone, 555 to 732 top-p alone: the first two
 // at 4 TB/s and more, the others by their instructions (some 20 a token for e^z and its two
 // whole numbers).  A single row is a chain of some ten short steps with a barrier each.
 //
@@ -1389,7 +1389,9 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
                 const int done = settle_list<false>(s, 0, find_limit(s, sum_pass<T, VEC>(s, odd)), 2);
                 if (done == DRAWN) return;
                 found = done == BOUNDED;
-                if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END, st.wide = true;
+                // all of the row then, listed if that may fit under a mask and costs little if not
+                // (64 masked f32 rows of 32,000 tokens: 46 us, 52 not listed)
+                if (threadIdx.x == 0) st.z_from = 1.f, st.z_to = Z_END, st.wide = s.job.per_block > 4 * SPAN;
                 __syncthreads();
             }
             // The stretch looked at closely; where the nucleus does not end in it the whole row
