@@ -384,6 +384,48 @@ def test_sample(psc, B, V, dtype, mask, kind, shape):
     assert torch.equal(tok, again) and torch.equal(lp, lp2)
 
 
+@pytest.mark.parametrize("V", [9000, 100001, 262144])
+@pytest.mark.parametrize("dtype,mask", [("f32", "none"), ("bf16", "mixed")])
+@pytest.mark.parametrize("shape", ["narrow", "lumpy", "long"])
+def test_sample_a_nucleus_that_is_hard_to_find(psc, V, dtype, mask, shape):
+    """Rows that no list holds and that a sample misjudges: values hardly apart, values that
+    depend on a block of 1024 tokens, and a heavy start with a long even tail."""
+    B = 5
+    rng = np.random.default_rng([V, len(shape)])
+    x = rng.standard_normal((B, V))
+    lump = (np.arange(V) // 1024) % 8 == 0
+    x = {"narrow": x * 1e-3, "lumpy": x + np.where(lump, -3.0, 2.0) * (1 - 2 * (np.arange(B)[:, None] % 2)),
+         "long": np.where(np.arange(V) < 3000, x + 5, x * 0.05)}[shape]
+    _, xd = _strided(x, DT[dtype], 8, 0)
+    u = rng.random(B).astype(np.float32)
+    p = np.array([0.2, 0.55, 0.8, 0.95, 0.999], dtype=np.float32)
+    allowed = _mask(rng, mask, B, V)
+    tok, lp = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, device="cuda")
+    psc.psc_sample(xd, _dev(u), tok, logprobs=lp, bitmask=None if allowed is None else _pack(allowed), top_p=_dev(p))
+    _check_draws(tok.cpu().numpy(), _f64(lp), _f64(xd), allowed, u, np.ones(B), np.zeros(B, dtype=int),
+                 p.astype(np.float64), np.zeros(B))
+
+
+@pytest.mark.parametrize("B,V", [(160, 150001), (400, 50000)])
+@pytest.mark.parametrize("shape", ["flat", "lumpy"])
+def test_sample_a_batch_in_which_every_row_is_heavy(psc, B, V, shape):
+    """With top_k given but off: many rows, few blocks each, and the first rows checked."""
+    rng = np.random.default_rng([B, V])
+    g = torch.Generator(device="cuda").manual_seed(B)
+    xd = torch.randn(B, V, generator=g, device="cuda")
+    if shape == "lumpy":
+        xd += torch.where(torch.arange(V, device="cuda") // 1024 % 8 == 0, -3.0, 2.0)
+    xd = xd.bfloat16()
+    u = rng.random(B).astype(np.float32)
+    p = np.tile(np.array([0.5, 0.9, 0.97, 0.999], dtype=np.float32), B // 4)
+    tok, lp = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, device="cuda")
+    psc.psc_sample(xd, _dev(u), tok, logprobs=lp, top_k=torch.zeros(B, dtype=torch.int32, device="cuda"), top_p=_dev(p))
+    rows = [0, 1, 2, 3, B // 2, B // 2 + 1, B - 2, B - 1]
+    n = len(rows)
+    _check_draws(tok.cpu().numpy()[rows], _f64(lp)[rows], _f64(xd[rows]), None, u[rows], np.ones(n),
+                 np.zeros(n, dtype=int), p[rows].astype(np.float64), np.zeros(n))
+
+
 @pytest.mark.parametrize("V", [100, 5000, 70000])
 def test_sample_infinities_nan_and_masked_values(psc, V):
     rng = np.random.default_rng(V)
