@@ -506,7 +506,8 @@ __device__ int pick_few(Shared& s, int n, In&& in) {
 // s.st.listed and none is below `bound`: k (0: off), then a nucleus of `limit` (0: limit_of what
 // top-k leaves, ~0: off), then min_e.  DRAWN: *place is the drawn one's place in the list
 // for the thread that found it, -1 for others, *kept the weight of what stays.  BOUNDED:
-// s.tau is the order of the last value that stays.
+// s.tau is the order of a value that, min_e apart, all that stays reaches and nothing else of the
+// row does.
 __device__ __noinline__ int settle(Shared& s, float bound, int k, u64 limit, u64* kept, int* place) {
     const Weigh g = s.g;
     const int n = s.st.n, V = s.row.V;
@@ -553,7 +554,7 @@ __device__ __noinline__ int settle(Shared& s, float bound, int k, u64 limit, u64
     // a filter ends pair by pair; the same by token for the draw.
     const float scale = BINS / (g.m - bound);
     auto bin_of = [&](int i) { return min(BINS - 1, (int)fmaxf(0.f, (g.m - unordered(s.key[i])) * scale)); };
-    uint32_t tau = 0;
+    uint32_t tau = ordered(bound);              // every listed one, and no other of the row, reaches it
     if ((k && k < n) || limit != ~0ull) {
         __syncthreads();
         s.bins[tid] = s.bins_hi[tid] = s.count[tid] = 0;

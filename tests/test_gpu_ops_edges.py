@@ -1,0 +1,64 @@
+"""The operators around the mask on the GPU where their variants meet: values and masks
+that send a row from one way of drawing to another, sizes at which rings and slabs go
+round.  Reference forms and tolerances are those of test_gpu_ops."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_ops import DT, NEG, _check_draws, _dev, _f64, _pack, psc  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+# ----------------------------------------------------------------------- sample
+def _draw(psc, x, dtype, u, allowed=None, T=None, k=None, p=None, m=None, rows=None):  # noqa: F811
+    """One call, checked against the 64-bit draw on `rows` (all if None); None leaves a filter out."""
+    B, V = x.shape
+    xd = _dev(x.astype(np.float32)).to(DT[dtype])
+    tok, lp = torch.full((B,), -7, dtype=torch.int32, device="cuda"), torch.full((B,), 7.0, device="cuda")
+    f32 = [None if a is None else np.asarray(a, dtype=np.float32) for a in (T, p, m)]
+    psc.psc_sample(xd, _dev(u), tok, logprobs=lp, bitmask=None if allowed is None else _pack(allowed),
+                   temperature=None if T is None else _dev(f32[0]), top_p=None if p is None else _dev(f32[1]),
+                   min_p=None if m is None else _dev(f32[2]),
+                   top_k=None if k is None else _dev(np.asarray(k, dtype=np.int32)))
+    rows = np.arange(B) if rows is None else np.asarray(rows)
+    T, p, m = (np.full(B, d) if a is None else a.astype(np.float64) for a, d in zip(f32, (1.0, 1.0, 0.0)))
+    k = np.zeros(B, dtype=int) if k is None else np.asarray(k)
+    _check_draws(tok.cpu().numpy()[rows], _f64(lp)[rows], _f64(xd[rows]), None if allowed is None else allowed[rows],
+                 u[rows], T[rows], k[rows], p[rows], m[rows])
+    return tok.cpu().numpy(), _f64(lp)
+
+
+@pytest.mark.parametrize("V,first,n", [(262144, 1024, 400), (262144, 1000, 1000), (200001, 1564, 380),
+                                       (151936, 600, 280), (140001, 100, 2000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [1, 60])
+def test_sample_among_neighbouring_tokens(psc, V, first, n, dtype, B):  # noqa: F811
+    """What stays lies close together (the digits of a number, the names of one prefix), and the
+    filters leave all that is listed: min-p alone, top-k of no fewer than the candidates."""
+    rng = np.random.default_rng([V, n, B])
+    x = np.full((B, V), -20.0)
+    x[:, first:first + n] = rng.standard_normal((B, n)) * 0.25
+    allowed = np.zeros((B, V), dtype=bool)
+    allowed[:, first:first + n] = True
+    u = rng.random(B).astype(np.float32)
+    rows = np.unique([0, B // 2, B - 1])
+    for mask in (None, allowed):
+        _draw(psc, x, dtype, u, mask, m=np.full(B, 0.01), rows=rows)
+        _draw(psc, x, dtype, u, mask, m=np.full(B, 1e-4), T=np.full(B, 0.8), rows=rows)
+    _draw(psc, x, dtype, u, allowed, k=np.full(B, n), rows=rows)
+    _draw(psc, x, dtype, u, allowed, k=np.full(B, 5000), rows=rows)
+    _draw(psc, x, dtype, u, allowed, k=np.full(B, 5000), m=np.full(B, 0.3), rows=rows)
+    _draw(psc, x, dtype, u, allowed, k=np.full(B, 5000), p=np.full(B, 0.9), rows=rows)
+
+
+def test_sample_top_k_of_as_many_tokens_as_reach_the_bound(psc):  # noqa: F811
+    """Every one of the k largest lies in a group of its own, so that the list holds them and no
+    other; the tokens below it would take nearly all of the weight."""
+    V, n = 1 << 22, 400
+    x = np.full((1, V), -3.0)
+    x[0, np.arange(n) * 8] = np.arange(n) * 1e-3
+    for u in (0.25, 0.75):
+        _draw(psc, x, "f32", np.array([u], dtype=np.float32), k=[n])
