@@ -655,9 +655,13 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= 8) {
-        // N_A groups of warps, a group per slot of the ring: what one stage waits for (its
-        // bytes, its slot, its stores to become visible) passes while others are converted.
-        // Each group sees every phase of its slot's barriers, so a parity names one phase.
+        // N_A groups of warps, a group per slot of the operand ring: what one stage waits for (its
+        // slot, its bytes, its stores to become visible) passes while others are converted.
+        // A parity names one phase only to whom the phase before is known to be complete.  Of its
+        // own slot a group sees every phase.  A byte slot goes round among the groups, so the
+        // wait for the operand slot comes first: it ends when the products of the stage N_A before
+        // are done, so every byte stage up to that one has landed, and with at least N_A byte
+        // slots the last use of this stage's slot is one of those.
         const int group = (warp - 8) / PER, r0 = (warp % PER) * ROWS + (lane >> 3) + ((lane >> 2) & 1) * 4;
         int c = 0, cr = 0, at = 0;                    // stages of both rings before this item; pr is number `at`
         Place pr;
@@ -669,6 +673,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                 const int s = group;
                 for (; at < cr + (k >> 1); at++) pr.next(n_raw);
                 const int sr = pr.s;
+                if (!(ok = warp_wait(a_empty(s), parity, failed))) break;
+                parity ^= 1;
                 if (!(ok = warp_wait(raw_full(sr), pr.parity, failed))) break;
                 // lanes 0-3 and 4-7 take rows 4 apart, so that eight lanes touch all 32
                 // banks in both swizzles
@@ -681,8 +687,6 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_head_mma(const __grid_consta
                                  : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w)
                                  : "r"(from));
                 }
-                if (!(ok = warp_wait(a_empty(s), parity, failed))) break;
-                parity ^= 1;
                 const int odd = (lane >> 2) & 1, col = (lane & 3) * 2;
 #pragma unroll
                 for (int j = 0; j < ROWS / 8; j++) {

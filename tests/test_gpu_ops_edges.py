@@ -6,7 +6,7 @@ from __future__ import annotations
 import numpy as np
 import pytest
 
-from tests.test_gpu_ops import DT, NEG, _check_draws, _dev, _f64, _pack, psc  # noqa: F401
+from tests.test_gpu_ops import DT, NEG, _check_draws, _dev, _f64, _head_case, _pack, psc  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -62,3 +62,15 @@ def test_sample_top_k_of_as_many_tokens_as_reach_the_bound(psc):  # noqa: F811
     x[0, np.arange(n) * 8] = np.arange(n) * 1e-3
     for u in (0.25, 0.75):
         _draw(psc, x, "f32", np.array([u], dtype=np.float32), k=[n])
+
+
+# ------------------------------------------------------------------------- head
+@pytest.mark.parametrize("T,V,K", [(20, 300001, 64), (24, 280000, 16), (48, 290000, 48), (100, 280001, 64),
+                                   (128, 280000, 64), (200, 270001, 64), (300, 150000, 33), (1000, 70000, 64),
+                                   (20, 120001, 129), (160000, 100, 192), (160000, 128, 320), (128000, 77, 448),
+                                   (110000, 60, 64)])
+def test_head_logits_of_short_rows_and_many_tiles(psc, T, V, K):  # noqa: F811
+    """A tile is one or few stages of the pipeline, and a block has a dozen tiles and more: the
+    rings go round across tiles, and a byte slot is used by one group after another."""
+    _head_case(psc, T, V, K, "bf16", "none", pad=-K % 16)
+    _head_case(psc, T, V, K, "f32", "mixed" if T < 2000 else "none", pad=-K % 16)
