@@ -103,7 +103,8 @@ int64_t psc_sample_work_bytes(int32_t B);
  * first token by index at which the running weight of what stays passes
  * uniform[b] times its sum.  Weights are whole numbers, so every sum is exact
  * and the draw depends on the inputs alone.  T below 1e-6 (or NaN) is greedy: the
- * lowest index of the largest candidate, with log-probability 0.
+ * lowest index of the largest candidate, with log-probability 0; +inf counts as the
+ * largest finite value (an even draw among what stays).
  *   d_logits   : [B] rows of row_stride elements of dtype, unchanged
  *   d_bitmask  : uint32 [B][ceil(V/32)], or NULL
  *   d_uniform  : float [B] in [0, 1), of which the first 24 bits are used

@@ -1340,7 +1340,9 @@ __device__ __forceinline__ void sample_row(Shared& s, u64* chunk_sum, int b) {
             st.b = b, st.k = k, st.p = p;
             st.p24 = p < 1.f ? __float2uint_rn(fmaxf(p, 0.f) * 0x1p24f) : 0u;
             st.u24 = u > 0.f ? min(0xffffffu, __float2uint_rz(fminf(u, 1.f) * 0x1p24f)) : 0u;
-            s.g = Weigh{0.f, temp >= 1e-6f ? __fdiv_rn(1.f, temp) : 0.f, NEG_INF, min_e};
+            // 0 stands for greedy; the largest temperatures have an inverse (no flush of small
+            // numbers), under which every z of ordinary logits is a weight of 1
+            s.g = Weigh{0.f, temp >= 1e-6f ? __fdiv_rn(1.f, fminf(temp, FLT_BIG)) : 0.f, NEG_INF, min_e};
             s.row = Row{static_cast<const T*>(j.logits) + (size_t)b * j.stride,
                         j.bitmask ? reinterpret_cast<const uint8_t*>(j.bitmask + (size_t)b * j.W) : nullptr, j.V,
                         min(j.V, blocks.rank() * j.per_block), min(j.V, (blocks.rank() + 1) * j.per_block)};

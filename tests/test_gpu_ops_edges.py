@@ -64,6 +64,27 @@ def test_sample_top_k_of_as_many_tokens_as_reach_the_bound(psc):  # noqa: F811
         _draw(psc, x, "f32", np.array([u], dtype=np.float32), k=[n])
 
 
+@pytest.mark.parametrize("B,V", [(7, 1000), (60, 9000), (5, 150001)])
+@pytest.mark.parametrize("dtype,filters", [("bf16", ""), ("f32", "k"), ("bf16", "p"), ("f32", "m"), ("bf16", "kpm")])
+@pytest.mark.filterwarnings("ignore:invalid value")          # -inf / inf of the reference's masked tokens
+def test_sample_at_an_infinite_temperature_is_uniform(psc, B, V, dtype, filters):  # noqa: F811
+    """z = (x - m) * (1 / T) is 0 for every candidate: what the filters keep is drawn evenly.  Rows
+    at the largest finite temperature, at 0 and NaN (greedy) and at 1 beside them."""
+    rng = np.random.default_rng([V, B])
+    x = rng.integers(-12, 12, (B, V)) * 0.25
+    allowed = rng.random((B, V)) < 0.5
+    T = np.resize([np.inf, np.finfo(np.float32).max, 0.0, np.inf, 1.0, np.nan, np.inf], B)
+    u = ((np.arange(B) + 0.5) / B).astype(np.float32)
+    rows = np.arange(min(B, 7))
+    tok, lp = _draw(psc, x, dtype, u, allowed, T=T, rows=rows, k=np.full(B, 50) if "k" in filters else None,
+                    p=np.full(B, 0.3) if "p" in filters else None, m=np.full(B, 0.5) if "m" in filters else None)
+    if not filters:                                          # the u-th of the allowed, in order
+        for b in np.flatnonzero(np.isinf(T)):
+            at = np.flatnonzero(allowed[b])
+            assert tok[b] == at[int(np.floor(u[b] * 2.0 ** 24)) * len(at) >> 24]
+            assert abs(lp[b] + np.log(len(at))) <= 1e-6 * np.log(len(at))
+
+
 # ------------------------------------------------------------------------- head
 @pytest.mark.parametrize("T,V,K", [(20, 300001, 64), (24, 280000, 16), (48, 290000, 48), (100, 280001, 64),
                                    (128, 280000, 64), (200, 270001, 64), (300, 150000, 33), (1000, 70000, 64),
