@@ -55,6 +55,7 @@ class Decoder:
         self.top_p = torch.full((rows,), top_p, device=dev)
         self.repetition = torch.full((rows,), repetition, device=dev)
         self.head_work = torch.empty(psc.psc_head_work_bytes(rows, V, hidden), dtype=torch.uint8, device=dev)
+        self.faults = self.head_work[:4].view(torch.int32)     # of the last projection, on the device
         self.sample_work = torch.empty(psc.psc_sample_work_bytes(rows), dtype=torch.uint8, device=dev)
 
     def step(self):
@@ -84,6 +85,7 @@ def run(rows: int = 8, steps: int = 40, use_graph: bool = True, seed: int = 0):
     workload = configs.load(2, batch=1)
     d = Decoder(workload, rows, steps, seed=seed)
     logprobs = torch.empty(steps, rows, device="cuda")
+    faults = torch.zeros(1, dtype=torch.int32, device="cuda")
     graph = None
     for i in range(steps):
         d.new_inputs()
@@ -96,7 +98,10 @@ def run(rows: int = 8, steps: int = 40, use_graph: bool = True, seed: int = 0):
                     d.step()
             graph.replay()
         logprobs[i] = d.logprobs
+        faults += d.faults
     torch.cuda.synchronize()
+    if faults.item():                   # a bounded wait gave up: some logits were not written
+        raise RuntimeError(f"psc_head_logits: {faults.item()} blocks gave up")
     return workload, d.history.cpu(), logprobs.t().cpu(), d.status.cpu()
 
 

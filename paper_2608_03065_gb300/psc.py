@@ -510,7 +510,8 @@ def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, strea
     q int8 [T, K], w int8 [V, K] (rows at 16-byte-aligned addresses are read where they
     are, others packed first), scale f32 [T], w_scale f32 [V], logits bf16 or f32 [T, >=V].  work: a
     uint8 tensor of at least psc_head_work_bytes(T, V, K) bytes to reuse (one is
-    taken from torch's allocator for the call otherwise)."""
+    taken from torch's allocator for the call otherwise).  Returns the workspace, for
+    psc_head_faults."""
     import torch
     if q.dim() != 2 or w.dim() != 2 or q.shape[1] != w.shape[1]:
         raise ValueError("q and w must be [T, K] and [V, K]")
@@ -526,6 +527,18 @@ def psc_head_logits(q, scale, w, w_scale, logits, bitmask=None, work=None, strea
     _check(load().psc_head_logits(pq, sq, _ptr(scale, torch.float32, "scale", T), T, pw, sw,
                                   _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
                                   _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+    return work
+
+
+def psc_head_faults(work, stream=None) -> int:
+    """Blocks of the last psc_head_logits call with this workspace in which a bounded wait
+    gave up (synchronises the stream); not 0: some of its logits were not written."""
+    import torch
+    _ptr(work, torch.uint8, "work", 4)
+    if stream is None:
+        return work.view(-1)[:4].view(torch.int32).item()
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return work.view(-1)[:4].view(torch.int32).item()
 
 
 def psc_process_logits(logits, out=None, history=None, history_len=None, prompt_len=None, repetition=None,

@@ -95,3 +95,33 @@ def test_head_logits_of_short_rows_and_many_tiles(psc, T, V, K):  # noqa: F811
     rings go round across tiles, and a byte slot is used by one group after another."""
     _head_case(psc, T, V, K, "bf16", "none", pad=-K % 16)
     _head_case(psc, T, V, K, "f32", "mixed" if T < 2000 else "none", pad=-K % 16)
+
+
+@pytest.mark.parametrize("T,V,K,shift,mask", [(1, 5000, 256, 0, 0), (4, 5000, 256, 0, 1), (8, 5000, 256, 0, 1),
+                                              (12, 30000, 512, 0, 1), (12, 30000, 512, 0, 2), (12, 30000, 512, 0, 0),
+                                              (60, 30000, 512, 0, 1), (200, 60000, 512, 0, 1), (200, 60000, 512, 0, 0),
+                                              (3, 9000, 2047, 1, 0), (40, 140000, 2047, 1, 1), (300, 140000, 2047, 1, 0)])
+def test_head_faults_is_what_the_last_call_says(psc, T, V, K, shift, mask):  # noqa: F811
+    """Rows, single blocks, pairs, one slab and several: a call leaves the number of blocks that gave
+    up, whatever the workspace held before.  (No wait is made to give up on the GPU: a number is written in.)"""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    q = torch.randint(-127, 128, (T, K), generator=g, dtype=torch.int8, device="cuda")
+    w = torch.randint(-127, 128, (V, K + shift), generator=g, dtype=torch.int8, device="cuda")[:, shift:]
+    sx, sw, out = torch.rand(T, device="cuda"), torch.rand(V, device="cuda"), torch.empty(T, V, device="cuda")
+    bits = torch.randint(-2 ** 31, 2 ** 31 - 1, (T, (V + 31) // 32), generator=g, dtype=torch.int32, device="cuda")
+    bits = None if mask == 0 else bits if mask == 1 else bits * (torch.arange((V + 31) // 32, device="cuda") % 50 == 0)
+    bits = bits if bits is None else bits.int()
+    work = psc.psc_head_logits(q, sx, w, sw, out, bitmask=bits)          # one of its own
+    assert psc.psc_head_faults(work) == 0
+    work.fill_(1)
+    assert psc.psc_head_faults(work) == 0x01010101
+    assert psc.psc_head_logits(q, sx, w, sw, out, bitmask=bits, work=work) is work
+    assert psc.psc_head_faults(work) == 0
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    work[:4].view(torch.int32).fill_(3)
+    side.wait_stream(torch.cuda.current_stream())
+    for s in (side, side.cuda_stream):
+        psc.psc_head_logits(q, sx, w, sw, out, bitmask=bits, work=work, stream=s)
+        assert psc.psc_head_faults(work, stream=s) == 0
+    torch.cuda.current_stream().wait_stream(side)
