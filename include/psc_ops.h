@@ -32,12 +32,13 @@ extern "C" {
  * and q 0, so that whatever is computed from it shows it.
  *   d_x      : [T] rows of row_stride elements of dtype, K of them used
  *   d_q      : int8 [T] rows of q_stride bytes; bytes past K are left as they are
- *   d_scale  : float [T] */
+ *   d_scale  : float [T]
+ * PSC_ERR_LIMIT: K over 2^30. */
 psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_stride, int32_t T, int32_t K,
                              int8_t* d_q, int64_t q_stride, float* d_scale, void* stream);
 
 /* Bytes of workspace that psc_head_logits needs for these sizes; aligned: whether d_w
- * and w_stride are multiples of 16. */
+ * and w_stride are multiples of 16.  (256 for sizes that it refuses.) */
 int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned);
 
 /* The vocabulary projection in 8-bit integers, under the mask:
@@ -55,7 +56,8 @@ int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned);
  *                   some logits are then not written), 0 otherwise
  * Weights whose rows are at 16-byte-aligned addresses (d_w and w_stride; any K) are
  * read where they are; others are packed into the workspace first, a slab at a time.
- * PSC_ERR_LIMIT: K over 131,072 (a sum could pass 32 bits), T over 2^24. */
+ * PSC_ERR_LIMIT: K over 131,072 (a sum could pass 32 bits), T over 2^24, V over 2^30, or
+ * ceil(T/256) * ceil(V/128) over 2^31 - 1. */
 psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_scale, int32_t T, const int8_t* d_w,
                            int64_t w_stride, const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask,
                            void* d_logits, psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes,

@@ -18,6 +18,8 @@
 namespace {
 
 constexpr int MAX_K = 131072;           // K * 127 * 128 stays below 2^31
+constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, rounded up to tiles, too
+constexpr int MAX_QUANTIZE_K = 1 << 30;
 
 // One block per row: the largest magnitude, then the quotients.
 template <typename T>
@@ -879,6 +881,7 @@ psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_strid
     const char* me = "psc_quantize_rows";
     if (T < 0 || K <= 0 || row_stride < K || q_stride < K || !is_dtype(dtype) || (T && (!d_x || !d_q || !d_scale)))
         return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    if (K > MAX_QUANTIZE_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 2^30");
     if (T == 0) return PSC_OK;
     cudaStream_t cs = (cudaStream_t)stream;
     if (dtype == PSC_BF16)
@@ -889,7 +892,7 @@ psc_status psc_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_strid
 }
 
 int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned) {
-    if (T <= 0 || V <= 0 || K <= 0) return 256;
+    if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K) return 256;
     return plan_of(T, V, K).bytes + (aligned ? 0 : (int64_t)slab_rows(V, K) * ((K + 15) / 16 * 16));
 }
 
@@ -902,7 +905,7 @@ psc_status psc_head_logits(const int8_t* d_q, int64_t q_stride, const float* d_s
         !d_w_scale || (T && (!d_q || !d_scale || !d_logits)))
         return ops_fail(PSC_ERR_ARG, me, "bad arguments");
     if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 131,072");
-    if ((int64_t)((T + NT_MAX - 1) / NT_MAX) * ((V + VT - 1) / VT) > 0x7fffffff || T > 1 << 24)
+    if (T > MAX_T || V > MAX_V || (int64_t)((T + NT_MAX - 1) / NT_MAX) * ((V + VT - 1) / VT) > 0x7fffffff)
         return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
     if (T == 0) return PSC_OK;
     if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_work_bytes(T, V, K, is_packed(d_w, w_stride)))
