@@ -44,8 +44,11 @@ int64_t psc_head_work_bytes(int32_t T, int32_t V, int32_t K, int32_t aligned);
 /* The vocabulary projection in 8-bit integers, under the mask:
  *     logits[t][v] = (sum_k q[t][k] * w[v][k]) * scale[t] * w_scale[v]
  * where the mask allows v for row t, -inf elsewhere; rows of w that no token
- * allows need not be read.  Sums are exact while every partial sum stays below
- * 2^24 in magnitude (always for K <= 1040) and carry f32 roundings beyond.
+ * allows need not be read.  Sums are exact while every partial sum stays within
+ * 2^24 in magnitude (always for K <= 1024; for K <= 1040 where neither side holds -128).
+ * Beyond, they carry roundings that depend on T: up to 16 tokens may be summed in whole
+ * numbers of 32 bits and rounded once, larger batches are summed in f32, so that a token's
+ * logits may differ in their last bits between a small batch and a large one.
  *   d_q, d_w      : int8 [T] and [V] rows of q_stride and w_stride bytes, K of them used
  *   d_scale       : float [T], d_w_scale : float [V]
  *   d_bitmask     : uint32 [T][ceil(V/32)], or NULL (every token allowed)

@@ -125,3 +125,22 @@ def test_head_faults_is_what_the_last_call_says(psc, T, V, K, shift, mask):  # n
         psc.psc_head_logits(q, sx, w, sw, out, bitmask=bits, work=work, stream=s)
         assert psc.psc_head_faults(work, stream=s) == 0
     torch.cuda.current_stream().wait_stream(side)
+
+
+@pytest.mark.parametrize("K", [1024, 1000])
+@pytest.mark.parametrize("T", [1, 4, 16, 24, 150])
+def test_head_sums_of_any_bytes_are_exact_up_to_1024_columns(psc, T, K):  # noqa: F811
+    """-128 on both sides: every sum is a whole number within 2^24, and with scales of 1 the
+    logits are those numbers, whichever variant forms them."""
+    rng = np.random.default_rng([T, K])
+    V = 700
+    q, w = rng.integers(-128, 128, (T, K)), rng.integers(-128, 128, (V, K))
+    q[0] = w[0] = w[V - 1] = -128
+    w[1] = 127
+    w[2] = np.where(np.arange(K) % 2, 127, -128)
+    out = torch.empty(T, V, device="cuda")
+    pitch = (K + 15) // 16 * 16
+    wd = torch.empty(V, pitch, dtype=torch.int8, device="cuda")[:, :K]
+    wd.copy_(_dev(w, torch.int8))
+    psc.psc_head_logits(_dev(q, torch.int8), torch.ones(T, device="cuda"), wd, torch.ones(V, device="cuda"), out)
+    np.testing.assert_array_equal(_f64(out), (q @ w.T).astype(np.float64))
