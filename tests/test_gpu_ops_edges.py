@@ -6,7 +6,7 @@ from __future__ import annotations
 import numpy as np
 import pytest
 
-from tests.test_gpu_ops import DT, NEG, _check_draws, _dev, _f64, _head_case, _pack, psc  # noqa: F401
+from tests.test_gpu_ops import DT, NEG, U, UB, _check_draws, _dev, _f64, _head_case, _pack, psc  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -144,3 +144,40 @@ def test_head_sums_of_any_bytes_are_exact_up_to_1024_columns(psc, T, K):  # noqa
     wd.copy_(_dev(w, torch.int8))
     psc.psc_head_logits(_dev(q, torch.int8), torch.ones(T, device="cuda"), wd, torch.ones(V, device="cuda"), out)
     np.testing.assert_array_equal(_f64(out), (q @ w.T).astype(np.float64))
+
+
+@pytest.mark.parametrize("T,V,K,pad,shift", [(3, 70001, 4095, 0, 0), (12, 70001, 4095, 0, 1), (40, 70001, 4095, 0, 0),
+                                             (140, 280003, 1001, 0, 2), (2, 1100000, 250, 1, 0)])
+@pytest.mark.parametrize("dtype,mask", [("f32", "none"), ("bf16", "mixed"), ("f32", "tight")])
+def test_head_logits_of_packed_rows_over_two_slabs(psc, T, V, K, pad, shift, dtype, mask):  # noqa: F811
+    """Packed rows of more than 256 MB: the second slab's rows, scales and mask words against 64
+    bits, on the rows around the slabs' edge, the first and the last."""
+    pitch = (K + 15) // 16 * 16
+    edge = (256 << 20) // pitch // 128 * 128
+    assert edge < V < 2 * edge
+    rng = np.random.default_rng([T, V, K])
+    q = rng.integers(-127, 128, (T, K), dtype=np.int8)
+    flat = torch.randint(-127, 128, (V * (K + pad) + shift,), dtype=torch.int8, device="cuda",
+                         generator=torch.Generator(device="cuda").manual_seed(K))
+    w = flat[shift:].view(V, K + pad)[:, :K]
+    sx, sw = rng.uniform(0.01, 0.1, T).astype(np.float32), rng.uniform(1e-4, 1e-3, V).astype(np.float32)
+    allowed = None if mask == "none" else rng.random((T, V)) < (0.5 if mask == "mixed" else 0.001)
+    if allowed is not None:
+        allowed[0] = False
+        allowed[-1, edge - 3:edge + 3] = allowed[-1, V - 1] = True
+    big = torch.full((T, V + 3), 7.0, dtype=DT[dtype], device="cuda")
+    psc.psc_head_logits(_dev(q), _dev(sx), w, _dev(sw), big[:, :V], bitmask=None if allowed is None else _pack(allowed))
+    assert (big[:, V:] == 7).all()
+    rows = np.unique(np.r_[0:300, edge - 300:edge + 300, V - 300:V, rng.integers(0, V, 300)])
+    at = torch.from_numpy(rows).cuda()
+    got, wr = _f64(big[:, at]), w[at].cpu().numpy().astype(np.float64)
+    exact = q.astype(np.float64) @ wr.T * sx.astype(np.float64)[:, None] * sw[rows].astype(np.float64)
+    tol = (3 * U + (UB if dtype == "bf16" else 0)) * np.abs(exact)
+    if K > 1040:                          # as in _head_case
+        size = np.abs(q).astype(np.float64) @ np.abs(wr).T
+        tol = tol + np.where(size >= 2.0 ** 24, 2 * U * (K / 16) * size * sx[:, None] * sw[rows], 0)
+    if allowed is not None:
+        assert (got[~allowed[:, rows]] == NEG).all()
+        assert int(big[:, :V].isneginf().sum()) == int((~allowed).sum())
+        exact, tol, got = (a[allowed[:, rows]] for a in (exact, tol, got))
+    assert (np.abs(got - exact) <= tol * 1.0000001).all()
