@@ -272,9 +272,9 @@ psc_status head_rows(const Head& h, T* logits, uint8_t* work, cudaStream_t cs, c
 // on its own moves 112 KB through it (bytes in and out 16, widened weights in and out 32,
 // tokens in and out 64), 875 cycles where the products take 512.  So blocks pair up (PAIR):
 // 256 rows of weights, 128 in each, by the same tokens, half in each (tcgen05's
-// cta_group::2), which leaves 80 KB.  256 tokens over 262,144 x 4096: 424 -> 364 us, 1511
+// cta_group::2), which leaves 80 KB.  256 tokens over 262,144 x 4096: 424 -> 366 us, 1502
 // TFLOP/s; 64 tokens over 128,256 x 2048: 66 us alone, 77 in pairs; 128 tokens over 128,256 x
-// 4096: 157 alone, 149 in pairs.  1024 tokens over 262,144 x 2048: 682 us, 1612 TFLOP/s.
+// 4096: 157 alone, 149 in pairs.  1024 tokens over 262,144 x 2048: 681 us, 1615 TFLOP/s.
 // Byte b becomes f16 without a conversion: b + 128 under the exponent of 1024 is
 // 1152 + b, minus 1152; five instructions for four bytes.
 constexpr int VT = 128;                       // vocabulary rows of a tile

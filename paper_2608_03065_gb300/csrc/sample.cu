@@ -1308,9 +1308,10 @@ __device__ __noinline__ void draw(Shared& s, const u64* chunk_sum) {
 // What no list holds is drawn from sums by chunk.
 //
 // Measured (bf16, device time): 1 row of 262,144 tokens 15 us with top-k, 30 with top-p alone;
-// 1024 rows 116 us greedy, 147 top-k, 314 temperature alone, 555 to 732 top-p alone: the first two
-// at 4 TB/s and more, the others by their instructions (some 20 a token for e^z and its two
-// whole numbers).  A single row is a chain of some ten short steps with a barrier each.
+// 1024 rows 116 us greedy, 127 min-p, 142 top-k, 316 temperature alone, 658 top-p 0.9 alone, 898 top-p
+// 0.99: the first three at 3.8 TB/s and more, the others by their instructions (some 20 a token for e^z and
+// its two whole numbers, in two passes for top-p).  A single row is a chain of some ten short
+// steps with a barrier each.
 //
 // Rows that need no weights of all tokens (greedy, top-k, min-p alone) and those that do
 // differ tenfold in time and want different splits, so a large batch whose settings may hold
