@@ -1,4 +1,4 @@
-"""Thin Python binding of the PSC C ABI (include/psc.h): argument marshalling only.
+"""Thin Python binding of the PSC C ABI (include/psc.h, psc_ops.h, psc_mx4.h, psc_norm.h): argument marshalling only.
 
 Every function here converts its arguments (torch tensors -> device pointers,
 torch streams -> cudaStream_t) and calls the library function of the same
@@ -31,6 +31,11 @@ EXPORTED = ["psc_compile", "psc_destroy", "psc_last_error", "psc_info", "psc_sta
 # include/psc_ops.h: the operators around the mask
 EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "psc_process_logits",
                 "psc_sample_work_bytes", "psc_sample"]
+# include/psc_mx4.h: the vocabulary projection in microscaled 4-bit floating point
+EXPORTED_MX4 = ["psc_mx4_block_bytes", "psc_quantize_mx4", "psc_dequantize_mx4", "psc_head_mx4_work_bytes",
+                "psc_head_logits_mx4"]
+# include/psc_norm.h: the norm in front of either projection
+EXPORTED_NORM = ["psc_norm_quantize_rows", "psc_norm_quantize_mx4"]
 NOALLOC_MAX_ROWS = 16384
 
 
@@ -70,6 +75,7 @@ def load(path: str = LIB_PATH):
         raise RuntimeError(f"{path} is missing: build it with paper_2608_03065_gb300.build.build()")
     lib = ctypes.CDLL(path)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    f32 = ctypes.c_float
     sig = {
         "psc_compile": (i32, [ctypes.c_char_p, sz, vp, vp, i32, i32, vp, vp]),
         "psc_destroy": (None, [vp]),
@@ -103,6 +109,13 @@ def load(path: str = LIB_PATH):
         "psc_head_logits": (i32, [vp, i64, vp, i32, vp, i64, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
         "psc_process_logits": (i32, [vp, i32, i64, vp, i64, i32, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, i32,
                                      vp, vp]),
+        "psc_norm_quantize_rows": (i32, [vp, i32, i64, vp, i64, vp, i64, vp, f32, i32, i32, vp, i64, vp, vp]),
+        "psc_mx4_block_bytes": (i64, [i32, i32]),
+        "psc_quantize_mx4": (i32, [vp, i32, i64, i32, i32, vp, i64, vp, vp]),
+        "psc_dequantize_mx4": (i32, [vp, i64, vp, vp, i32, i32, vp, i32, i64, vp]),
+        "psc_norm_quantize_mx4": (i32, [vp, i32, i64, vp, i64, vp, i64, vp, f32, i32, i32, vp, i64, vp, vp, vp]),
+        "psc_head_mx4_work_bytes": (i64, [i32, i32, i32]),
+        "psc_head_logits_mx4": (i32, [vp, i64, vp, vp, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
         "psc_sample_work_bytes": (i64, [i32]),
         "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
@@ -499,6 +512,31 @@ def psc_quantize_rows(x, q, scale, stream=None):
                                     _stream(stream)))
 
 
+def _norm_inputs(x, residual, sum_out, gain):
+    """What the two norms share: x's sizes and type, and the inputs' addresses and strides."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    T, K = x.shape
+    code = _dtype_code(x)
+    px, sx = _rows(x, None, "x", T, K)
+    pr, sr = (None, 0) if residual is None else _rows(residual, x.dtype, "residual", T, K)
+    ps, ss = (None, 0) if sum_out is None else _rows(sum_out, x.dtype, "sum_out", T, K)
+    return T, K, code, (px, code, sx, pr, sr, ps, ss, _ptr(gain, torch.float32, "gain", K))
+
+
+def psc_norm_quantize_rows(x, q, scale, gain=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None):
+    """q, scale := the rows of the root-mean-square norm of h = x + residual, times gain, in
+    8-bit integers (int8 [T, K]) with a scale each (f32 [T]), as psc_quantize_rows makes
+    them of activations; sum_out := h.  x, residual, sum_out bf16 or f32 [T, K], gain f32 [K];
+    gain, residual and sum_out may be None, and sum_out may be x or residual."""
+    import torch
+    T, K, _, inputs = _norm_inputs(x, residual, sum_out, gain)
+    pq, sq = _rows(q, torch.int8, "q", T, K)
+    _check(load().psc_norm_quantize_rows(*inputs, eps, T, K, pq, sq, _ptr(scale, torch.float32, "scale", T),
+                                         _stream(stream)))
+
+
 def psc_head_work_bytes(T: int, V: int, K: int, aligned: bool = True) -> int:
     """Bytes of workspace for psc_head_logits; aligned: the weights' rows are at addresses
     that are multiples of 16."""
@@ -599,6 +637,87 @@ def psc_sample(logits, uniform, tokens, logprobs=None, bitmask=None, temperature
         _ptr(top_p, torch.float32, "top_p", B), _ptr(min_p, torch.float32, "min_p", B),
         _ptr(tokens, torch.int32, "tokens", B), _ptr(logprobs, torch.float32, "logprobs", B),
         _ptr(work, torch.uint8, "work", n), n, _stream(stream)))
+
+
+# ------------------------------------ the projection in microscaled 4-bit floating point
+def psc_mx4_row_bytes(K: int) -> int:
+    """Bytes of a row's codes: whole blocks of 32 columns."""
+    return (K + 31) // 32 * 16
+
+
+def psc_mx4_block_bytes(rows: int, K: int) -> int:
+    """Bytes of the blocks' exponents of a matrix, in tiles as include/psc_mx4.h lays them out."""
+    return load().psc_mx4_block_bytes(rows, K)
+
+
+def _mx4(q, blocks, rows, K, name):
+    """(address of the codes, their stride, address of the exponents)."""
+    import torch
+    pq, sq = _rows(q, torch.uint8, name, rows, psc_mx4_row_bytes(K))
+    return pq, sq, _ptr(blocks, torch.uint8, f"{name}'s blocks", load().psc_mx4_block_bytes(rows, K))
+
+
+def psc_quantize_mx4(x, q, blocks, stream=None):
+    """q, blocks := the rows of x (bf16 or f32 [T, K]) in microscaled 4-bit floating point:
+    uint8 [T, >= psc_mx4_row_bytes(K)] codes, two a byte, and uint8 [psc_mx4_block_bytes(T, K)]
+    exponents of blocks of 32 columns.  Activations by token, or weights by output channel."""
+    if x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    T, K = x.shape
+    code = _dtype_code(x)
+    px, sx = _rows(x, None, "x", T, K)
+    _check(load().psc_quantize_mx4(px, code, sx, T, K, *_mx4(q, blocks, T, K, "q"), _stream(stream)))
+
+
+def psc_dequantize_mx4(q, blocks, y, scale=None, stream=None):
+    """y := the values that q and blocks hold (bf16 or f32 [T, K]), times scale (f32 [T])."""
+    import torch
+    if y.dim() != 2:
+        raise ValueError("y must be a 2-D tensor")
+    T, K = y.shape
+    code = _dtype_code(y)
+    py, sy = _rows(y, None, "y", T, K)
+    _check(load().psc_dequantize_mx4(*_mx4(q, blocks, T, K, "q"), _ptr(scale, torch.float32, "scale", T), T, K, py,
+                                     code, sy, _stream(stream)))
+
+
+def psc_norm_quantize_mx4(x, q, blocks, scale, gain=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None):
+    """psc_norm_quantize_rows with an output in 4 bits: q and blocks as psc_quantize_mx4 makes
+    them of h * gain, scale (f32 [T]) := 1 / sqrt(mean h^2 + eps)."""
+    import torch
+    T, K, _, inputs = _norm_inputs(x, residual, sum_out, gain)
+    _check(load().psc_norm_quantize_mx4(*inputs, eps, T, K, *_mx4(q, blocks, T, K, "q"),
+                                        _ptr(scale, torch.float32, "scale", T), _stream(stream)))
+
+
+def psc_head_mx4_work_bytes(T: int, V: int, K: int) -> int:
+    """Bytes of workspace for psc_head_logits_mx4."""
+    return load().psc_head_mx4_work_bytes(T, V, K)
+
+
+def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_scale=None, bitmask=None, work=None,
+                        stream=None):
+    """logits[:, :V] := (x @ w.T) * scale[:, None] * w_scale over the values of matrices in 4 bits,
+    x [T, K] (q, q_blocks) and w [V, K] (w, w_blocks), -inf where bitmask forbids.  scale f32 [T]
+    and w_scale f32 [V] may be None; logits bf16 or f32 [T, >=V].  work: a uint8 tensor of at
+    least psc_head_mx4_work_bytes(T, V, K) bytes to reuse (one is taken from torch's allocator
+    for the call otherwise).  Returns the workspace, for psc_head_faults."""
+    import torch
+    if q.dim() != 2 or w.dim() != 2:
+        raise ValueError("q and w must be 2-D tensors")
+    T, V = q.shape[0], w.shape[0]
+    code = _dtype_code(logits)
+    pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
+    pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
+    pl, sl = _rows(logits, None, "logits", T, V)
+    n = load().psc_head_mx4_work_bytes(T, V, K)
+    pm = _mask_ptr(bitmask, T, V)
+    if work is None:
+        work = _workspace(n, logits.device, stream)
+    _check(load().psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
+                                      _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
+                                      _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+    return work
 
 
 def psc_sample_work_bytes(B: int) -> int:

@@ -1,0 +1,144 @@
+"""The 4-bit operators and the norm on the CPU: the binding matches include/psc_mx4.h and
+psc_norm.h, and wrong arguments are refused before anything is launched (the library's own
+checks are reached with addresses that it must not use)."""
+from __future__ import annotations
+
+import os
+import re
+
+import pytest
+
+from tests.test_library_cpu import ROOT, _c_type, psc  # noqa: F401
+from tests.test_ops_binding import ARG, LIMIT, P
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("header,names", [("psc_mx4.h", "EXPORTED_MX4"), ("psc_norm.h", "EXPORTED_NORM")])
+def test_binding_matches_the_header(psc, header, names):  # noqa: F811
+    lib = psc.load()
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", header)).read(), flags=re.S)
+    protos = re.findall(r"([A-Za-z_][\w ]*?\**)\s*\b(psc_\w+)\s*\(([^)]*)\)\s*;", text)
+    assert sorted(p[1] for p in protos) == sorted(getattr(psc, names))
+    import ctypes
+    for ret, name, params in protos:
+        f = getattr(lib, name)
+        args = [p.strip() for p in params.split(",")]
+        assert len(f.argtypes) == len(args), name
+        for decl, t in zip(args, f.argtypes):
+            if decl.startswith("float ") and "*" not in decl:
+                assert t is ctypes.c_float, (name, decl)
+                continue
+            want = _c_type(decl.rsplit(" ", 1)[0] if "*" not in decl.split()[-1] else decl)
+            assert t in want, (name, decl, t)
+        assert f.restype in _c_type(ret), (name, ret, f.restype)
+
+
+def _norm(op="rows", x=P, dtype=1, stride=64, res=None, res_stride=0, sum_=None, sum_stride=0, gain=None, eps=1e-6,
+          T=4, K=64, q=P, q_stride=64, blocks=P, scale=P):
+    head = (x, dtype, stride, res, res_stride, sum_, sum_stride, gain, eps, T, K, q, q_stride)
+    if op == "rows":
+        return "psc_norm_quantize_rows", head + (scale, None)
+    return "psc_norm_quantize_mx4", head + (blocks, scale, None)
+
+
+def _quantize(x=P, dtype=1, stride=64, T=4, K=64, q=P, q_stride=32, blocks=P):
+    return "psc_quantize_mx4", (x, dtype, stride, T, K, q, q_stride, blocks, None)
+
+
+def _dequantize(q=P, q_stride=32, blocks=P, scale=None, T=4, K=64, y=P, dtype=1, stride=64):
+    return "psc_dequantize_mx4", (q, q_stride, blocks, scale, T, K, y, dtype, stride, None)
+
+
+def _head(q=P, q_stride=32, qb=P, T=4, w=P, w_stride=32, wb=P, V=100, K=64, out=P, dtype=1, stride=100, work=P,
+          n=1 << 40):
+    return "psc_head_logits_mx4", (q, q_stride, qb, None, T, w, w_stride, wb, None, V, K, None, out, dtype, stride,
+                                   work, n, None)
+
+
+M = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("call,code", [
+    (_norm(op, **kw), code) for op in ("rows", "mx4") for kw, code in [
+        (dict(x=None), ARG), (dict(q=None), ARG), (dict(scale=None), ARG), (dict(dtype=2), ARG), (dict(stride=63), ARG),
+        (dict(q_stride=16), ARG), (dict(T=-1), ARG), (dict(K=0), ARG), (dict(res=P, res_stride=63), ARG),
+        (dict(sum_=2 * P, sum_stride=63), ARG), (dict(sum_=P, sum_stride=80), ARG),
+        (dict(res=2 * P, res_stride=64, sum_=2 * P, sum_stride=72), ARG), (dict(eps=-1e-9), ARG),
+        (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
+        (dict(K=2 ** 30 + 1, stride=M, q_stride=M // 16 * 16), LIMIT)]
+] + [
+    (_norm("mx4", blocks=None), ARG), (_norm("mx4", q=P + 8), ARG), (_norm("mx4", q_stride=40), ARG),
+    (_norm("mx4", blocks=P + 4), ARG),
+    (_quantize(x=None), ARG), (_quantize(q=None), ARG), (_quantize(blocks=None), ARG), (_quantize(dtype=-1), ARG),
+    (_quantize(stride=63), ARG), (_quantize(q_stride=16), ARG), (_quantize(q_stride=40), ARG), (_quantize(q=P + 4), ARG),
+    (_quantize(blocks=P + 8), ARG), (_quantize(T=-1), ARG), (_quantize(K=0), ARG), (_quantize(K=65, stride=65), ARG),
+    (_quantize(K=M, stride=M, q_stride=2 ** 31), LIMIT),
+    (_dequantize(q=None), ARG), (_dequantize(y=None), ARG), (_dequantize(blocks=None), ARG), (_dequantize(dtype=5), ARG),
+    (_dequantize(stride=63), ARG), (_dequantize(q_stride=16), ARG), (_dequantize(q=P + 1), ARG),
+    (_dequantize(T=-1), ARG), (_dequantize(K=-3), ARG), (_dequantize(K=M, stride=M, q_stride=2 ** 31), LIMIT),
+    (_head(q=None), ARG), (_head(qb=None), ARG), (_head(w=None), ARG), (_head(wb=None), ARG), (_head(out=None), ARG),
+    (_head(dtype=2), ARG), (_head(stride=99), ARG), (_head(T=-1), ARG), (_head(V=0), ARG), (_head(K=0), ARG),
+    (_head(q=P + 8), ARG), (_head(q_stride=24), ARG), (_head(w=P + 8), ARG), (_head(w_stride=40), ARG),
+    (_head(qb=P + 8), ARG), (_head(wb=P + 2), ARG), (_head(work=None), ARG), (_head(work=P + 16), ARG),
+    (_head(n=255), ARG), (_head(K=131073, q_stride=65552, w_stride=65552), LIMIT), (_head(T=2 ** 24 + 1), LIMIT),
+    (_head(V=2 ** 30 + 1, stride=M), LIMIT),
+])
+def test_wrong_arguments_are_refused(psc, call, code):  # noqa: F811
+    name, args = call
+    assert getattr(psc.load(), name)(*args) == code
+    assert name in psc.load().psc_last_error().decode()
+
+
+@pytest.mark.parametrize("call", [_norm("rows", x=None, q=None, scale=None, T=0), _norm("mx4", x=None, scale=None, T=0),
+                                  _quantize(x=None, T=0), _dequantize(y=None, T=0),
+                                  _head(q=None, qb=None, out=None, work=None, T=0)])
+def test_empty_batches_are_nothing_to_do(psc, call):  # noqa: F811
+    name, args = call
+    assert getattr(psc.load(), name)(*args) == 0
+
+
+def test_sizes(psc):  # noqa: F811
+    for rows, K, n in [(1, 1, 512), (128, 128, 512), (129, 128, 1024), (128, 129, 1024), (300, 1000, 3 * 8 * 512),
+                       (M, 2 ** 30, 2 ** 24 * 2 ** 23 * 512), (0, 5, 0), (5, 0, 0), (-1, 5, 0), (5, 2 ** 30 + 1, 0)]:
+        assert psc.psc_mx4_block_bytes(rows, K) == n
+    assert [psc.psc_mx4_row_bytes(k) for k in (1, 32, 33, 2048)] == [16, 16, 32, 1024]
+    for T, V, K in [(M, 100, 64), (4, M, 64), (4, 100, M), (0, 1, 1), (2 ** 24 + 1, 1, 1), (1, 2 ** 30 + 1, 1)]:
+        assert psc.psc_head_mx4_work_bytes(T, V, K) == 256
+    for T, V, K in [(1, 1, 1), (2 ** 24, 1, 131072), (1, 2 ** 30, 131072), (1024, 262144, 2048)]:
+        assert psc.psc_head_mx4_work_bytes(T, V, K) >= 256
+
+
+def test_binding_refuses_tensors_of_the_wrong_kind(psc):  # noqa: F811
+    x, s = torch.zeros(4, 100), torch.zeros(4)
+    q, b = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="CUDA"):
+        psc.psc_quantize_mx4(x, q, b)
+    with pytest.raises(ValueError, match="2-D"):
+        psc.psc_quantize_mx4(s, q, b)
+    with pytest.raises(ValueError, match="bf16 or f32"):
+        psc.psc_quantize_mx4(x.half(), q, b)
+    with pytest.raises(ValueError, match="unit column stride"):
+        psc.psc_dequantize_mx4(q, b, x.t())
+    with pytest.raises(ValueError, match="bf16 or f32"):
+        psc.psc_dequantize_mx4(q, b, x.double())
+    with pytest.raises(ValueError, match="2-D"):
+        psc.psc_norm_quantize_rows(s, q, s)
+    with pytest.raises(ValueError, match="CUDA"):
+        psc.psc_norm_quantize_mx4(x, q, b, s)
+    with pytest.raises(ValueError, match="2-D"):
+        psc.psc_head_logits_mx4(s, b, q, b, x, 100)
+
+
+def test_the_formats_values_by_hand():
+    """The reference of the GPU tests against the format's own table."""
+    from tests._mx4_ref import decode, quantize
+    import numpy as np
+    x = np.zeros((1, 33), dtype=np.float32)
+    x[0, :12] = [6, -0.5, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -0.2, 4.99, -7.9]      # the largest in [4, 8): e = 0
+    x[0, 32] = -1e-3
+    codes, e = quantize(x)
+    assert e.tolist() == [[127, 127 - 12]]      # 1e-3 lies in 2^-10 (1, 2)
+    assert codes[0, :12].tolist() == [7, 9, 0, 2, 2, 4, 4, 6, 6, 8, 6, 15]
+    assert codes[0, 32] == 8 + 6                # 1e-3 * 2^12 = 4.096
+    assert decode(codes, e)[0, :12].tolist() == [6, -0.5, 0, 1, 1, 2, 2, 4, 4, 0, 4, -6]
