@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libpsc_gb300.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 CXX_SOURCES = ["grammar.cpp", "lexer.cpp", "lalr.cpp", "classifier.cpp", "bottomup.cpp", "persist.cpp"]
-CU_SOURCES = ["psc_capi.cu", "process.cu", "sample.cu", "head.cu", "norm.cu", "mx4.cu"]
+CU_SOURCES = ["psc_capi.cu", "process.cu", "sample.cu", "head.cu", "norm.cu", "mx4.cu",
+              "mx4_head.cu"]
 GENCODE = "arch=compute_103a,code=sm_103a"
 
 
@@ -44,9 +45,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
 def _build_locked(force: bool, verbose: bool) -> str:
     headers = [os.path.join(CSRC, "psc_internal.h"), os.path.join(INCLUDE, "psc.h")]
-    ops_headers = [os.path.join(CSRC, "ops_common.cuh"), os.path.join(CSRC, "mx4.cuh"),
-                   os.path.join(INCLUDE, "psc_ops.h"), os.path.join(INCLUDE, "psc_mx4.h"),
-                   os.path.join(INCLUDE, "psc_norm.h")]
+    ops_headers = [os.path.join(CSRC, f) for f in ("ops_common.cuh", "mx4.cuh", "tcgen05.cuh")]
+    ops_headers += [os.path.join(INCLUDE, f) for f in ("psc_ops.h", "psc_mx4.h", "psc_norm.h")]
     nvcc = _nvcc()
     jobs = []
     objs = []

@@ -1,0 +1,476 @@
+// psc_head_logits_mx4: the vocabulary projection in microscaled 4-bit floating point, under the
+// grammar's mask.
+#include <algorithm>
+
+#include "mx4.cuh"
+#include "tcgen05.cuh"
+
+namespace {
+
+constexpr int MAX_K = 131072;
+constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, rounded up to tiles, in 32 bits
+
+struct Head {
+    const uint8_t* q;
+    int64_t q_stride;
+    const uint8_t* q_blocks;
+    const float* scale;
+    int T;
+    const uint8_t* w;
+    int64_t w_stride;
+    const uint8_t* w_blocks;
+    const float* w_scale;
+    int V, K;
+    const uint32_t* bitmask;
+    int W;                              // mask words of a row
+    int64_t row_stride;
+};
+
+// Eight codes as bytes of twice their values, in order.
+__device__ __forceinline__ uint2 doubled8(uint32_t codes) {
+    const uint32_t m = codes & 0x77777777u, side = ((codes >> 1) & 0x44444444u) | 0x32103210u;
+    uint2 out;
+    // the magnitudes' bytes, their negatives, and of each byte the one that its sign picks
+    out.x = __byte_perm(__byte_perm(0x03020100u, 0x0C080604u, m), __byte_perm(0xFDFEFF00u, 0xF4F8FAFCu, m), side);
+    out.y = __byte_perm(__byte_perm(0x03020100u, 0x0C080604u, m >> 16), __byte_perm(0xFDFEFF00u, 0xF4F8FAFCu, m >> 16),
+                        side >> 16);
+    return out;
+}
+// The smaller and the larger; NaN if one is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// k_mx4_rows: a warp per 32 vocabulary rows (a word of the masks), of which those that some of up
+// to N tokens allow are read, 4 at once, a lane per block of 32 columns.  A block's products are
+// summed in whole numbers (quarters; exact), then scaled: the smaller power of two first, so that
+// nothing leaves f32 on the way to a sum that does not.
+constexpr int ROWS = 4;
+constexpr int ROWS_THREADS = 256;
+
+template <typename T, int N>
+__global__ void __launch_bounds__(ROWS_THREADS) k_mx4_rows(Head h, int t0, T* logits) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    __shared__ float s_out[ROWS_THREADS / 32][N * 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nb = (h.K + 31) / 32, n_tiles = (h.K + 127) / 128, n = min(N, h.T - t0);
+    uint2* xs = reinterpret_cast<uint2*>(dyn);                          // [N][4][nb]: doubled codes, eight a piece
+    float* xe = reinterpret_cast<float*>(dyn + (size_t)N * nb * 32);    // [N][nb]
+    dep_wait();
+    dep_launch();
+    for (int i = threadIdx.x; i < N * nb * 4; i += ROWS_THREADS) {
+        const int t = i / (nb * 4), c = i - t * nb * 4, b = c >> 2;
+        const bool there = t < n;
+        xs[(t * 4 + (c & 3)) * nb + b] =
+            there ? doubled8(*reinterpret_cast<const uint32_t*>(h.q + (size_t)(t0 + t) * h.q_stride + c * 4))
+                  : make_uint2(0, 0);
+        if (!(c & 3)) xe[t * nb + b] = there ? block_value(h.q_blocks[block_at(t0 + t, b, n_tiles)]) : 0.f;
+    }
+    __syncthreads();
+    float* out = s_out[warp];
+    for (int item = blockIdx.x * (ROWS_THREADS / 32) + warp; item < h.W; item += gridDim.x * (ROWS_THREADS / 32)) {
+        const int v0 = item * 32, v = v0 + lane;
+        const uint32_t mine = lane >= n ? 0u : h.bitmask ? h.bitmask[(size_t)(t0 + lane) * h.W + item] : FULL;
+        uint32_t rows = __reduce_or_sync(FULL, mine);
+        if (h.V - v0 < 32) rows &= (1u << (h.V - v0)) - 1;
+        while (rows) {
+            int r[ROWS];
+#pragma unroll
+            for (int i = 0; i < ROWS; i++) {
+                r[i] = __ffs(rows) - 1;             // -1: none left
+                rows &= rows - 1;
+            }
+            float acc[ROWS][N] = {};
+            for (int b = lane; b < nb; b += 32) {
+                uint4 w[ROWS];
+                float e[ROWS];
+#pragma unroll
+                for (int i = 0; i < ROWS; i++) {
+                    w[i] = make_uint4(0, 0, 0, 0);
+                    e[i] = 0.f;
+                    if (r[i] < 0) continue;
+                    w[i] = __ldcs(reinterpret_cast<const uint4*>(h.w + (size_t)(v0 + r[i]) * h.w_stride + b * 16));
+                    e[i] = block_value(h.w_blocks[block_at(v0 + r[i], b, n_tiles)]);
+                }
+#pragma unroll
+                for (int i = 0; i < ROWS; i++) {
+                    const uint32_t c[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    uint2 d[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) d[j] = doubled8(c[j]);
+#pragma unroll
+                    for (int t = 0; t < N; t++) {
+                        int s = 0;
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const uint2 x = xs[(t * 4 + j) * nb + b];
+                            s = __dp4a((int)d[j].x, (int)x.x, s);
+                            s = __dp4a((int)d[j].y, (int)x.y, s);
+                        }
+                        const float f = xe[t * nb + b];
+                        acc[i][t] = fmaf((float)s * 0.25f * min_nan(e[i], f), max_nan(e[i], f), acc[i][t]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS; i++)
+#pragma unroll
+                for (int t = 0; t < N; t++) {
+                    float s = acc[i][t];
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
+                    if (lane == 0 && r[i] >= 0) out[t * 32 + r[i]] = s;
+                }
+        }
+        __syncwarp();
+        const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
+        for (int t = 0; t < n; t++) {
+            const uint32_t bits = __shfl_sync(FULL, mine, t);
+            const float st = h.scale ? h.scale[t0 + t] : 1.f;
+            if (v < h.V)
+                store_f32(logits + (size_t)(t0 + t) * h.row_stride + v,
+                          (bits >> lane) & 1 ? out[t * 32 + lane] * st * sw : __uint_as_float(0xFF800000u));
+        }
+        __syncwarp();
+    }
+}
+
+template <typename T, int N>
+psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
+    const int nb = (h.K + 31) / 32;
+    for (int t0 = 0; t0 < h.T; t0 += N) {
+        psc_status s = ops_launch(k_mx4_rows<T, N>, dim3(std::min((h.W + 7) / 8, current_sms() * 2)), ROWS_THREADS,
+                                  (size_t)N * nb * 36, 1, cs, "k_mx4_rows", h, t0, logits);
+        if (s != PSC_OK) return s;
+    }
+    return PSC_OK;
+}
+
+// ------------------------------------------------------------ the tensor-core path
+//
+// k_mx4_mma: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by
+// up to 192 tokens (its N).  Both operands stay in 4 bits all the way; the tensor core takes their
+// blocks' powers of two from TMEM.  A stage is 256 columns of K:
+//   warp 0        TMA: 128 x 128 bytes of weights, N x 128 bytes of tokens, and both sides' tiles
+//                 of exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
+//   warp 1        tcgen05.cp of the exponents into TMEM, then four tcgen05.mma of 128 x N x 64 into
+//                 one of two accumulators
+//   warps 4-11    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
+//                 for 32 of them)
+constexpr int VT = 128;                       // vocabulary rows of a tile
+constexpr int NT = 192;                       // tokens of a tile at most; tiles start at multiples of 64
+constexpr int KS = 256;                       // columns of K of a stage (128 bytes of codes)
+constexpr int A_BYTES = VT * KS / 2;
+constexpr int SF = 512;                       // a tile of exponents: 128 rows by 128 columns
+constexpr int MAX_STAGES = 11;
+constexpr int MMA_THREADS = 384, EPILOGUE = 8;  // threads; warps of the epilogue
+
+struct Plan {
+    int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
+    int b_tiles;                              // 128-row tiles of exponents that a tile of tokens touches at most
+    int stages, stage_bytes;
+    int acc, sf_cols;                         // TMEM columns of an accumulator, of a stage's exponents
+    size_t smem;
+    int64_t flags_at, bytes;                  // in the workspace: the fault word, the tiles' flags
+};
+
+Plan plan_of(int T, int V) {
+    Plan p;
+    p.n_nt = (T + NT - 1) / NT;
+    p.N = p.n_nt > 1 ? NT : (T + 15) / 16 * 16;
+    p.n_vt = (V + VT - 1) / VT;
+    p.b_tiles = p.N > 128 ? 2 : 1;
+    p.stage_bytes = A_BYTES + p.N * KS / 2 + 2 * SF * (1 + p.b_tiles);
+    p.acc = (p.N + 31) / 32 * 32;
+    p.sf_cols = 8 + 8 * p.b_tiles;
+    // a stage's exponents have TMEM columns of their own, free when the stage is
+    p.stages = std::min({MAX_STAGES, (SMEM_MAX - 2048) / p.stage_bytes, (512 - 2 * p.acc) / p.sf_cols});
+    p.smem = 1024 + (size_t)p.stages * p.stage_bytes;
+    p.flags_at = 256;
+    p.bytes = p.flags_at + ((int64_t)p.n_vt * p.n_nt + 255) / 256 * 256;
+    return p;
+}
+
+// Exponents' tiles: 32 rows of 16 bytes, 8 rows every 128 bytes, no swizzle.
+__device__ __forceinline__ uint64_t exponent_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
+}
+// 512 bytes to four TMEM columns, the same in all four quarters of the lanes.
+__device__ __forceinline__ void copy_exponents(uint32_t to, uint32_t from) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(from)) : "memory");
+}
+__device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                        uint32_t add) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
+        : "memory");
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// How many rows of each tile some token allows, and the fault word.
+__global__ void __launch_bounds__(256) k_mx4_flags(Head h, int N, int n_vt, int n_nt, int* faults, uint8_t* flags) {
+    dep_wait();
+    dep_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    const int item = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (item >= n_vt * n_nt) return;
+    const int vt = item / n_nt, t0 = (item - vt * n_nt) * N, t1 = min(h.T, t0 + N);
+    uint32_t any = 0;
+    // a lane per word of a token's four, eight tokens at a time
+    for (int t = t0 + (lane >> 2); t < t1; t += 8) {
+        const int wi = vt * 4 + (lane & 3);
+        if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
+    }
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) any |= __shfl_xor_sync(FULL, any, o);
+    const int rows = __reduce_add_sync(FULL, lane < 4 ? __popc(any) : 0);
+    if (lane == 0) flags[item] = (uint8_t)rows;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constant__ CUtensorMap w_map,
+                                                            const __grid_constant__ CUtensorMap x_map, Head h,
+                                                            T* logits, Plan p, int* faults, const uint8_t* flags,
+                                                            int leave_few) {
+    extern __shared__ uint8_t dyn[];
+    __shared__ __align__(8) uint64_t s_bars[2 * MAX_STAGES + 5];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
+    const int b_bytes = p.N * KS / 2, n_items = p.n_vt * p.n_nt;
+    // operands first (multiples of 1024 bytes), then the exponents
+    auto a_at = [&](int s) { return base + s * (A_BYTES + b_bytes); };
+    auto sf_at = [&](int s) { return base + p.stages * (A_BYTES + b_bytes) + s * 2 * SF * (1 + p.b_tiles); };
+    const uint32_t bars = smem_addr(s_bars);
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto empty = [&](int s) { return bars + 8 * (MAX_STAGES + s); };
+    auto acc_full = [&](int s) { return bars + 8 * (2 * MAX_STAGES + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_STAGES + 2 + s); };
+    const uint32_t drained = bars + 8 * (2 * MAX_STAGES + 4);
+
+    if (threadIdx.x == 0) {
+        s_failed = 0;
+        for (int s = 0; s < p.stages; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE);
+        mbar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    volatile int* failed = &s_failed;
+    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
+    dep_wait();
+    dep_launch();
+    const bool masked = h.bitmask != nullptr;
+    // A block that fails has polled for a good part of a second before it counts itself.
+    if (!masked && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    auto is_active = [&](int item) { return !masked || flags[item] != 0; };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            Place at;
+            int c = 0;
+            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
+                if (!is_active(item)) continue;
+                const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N;
+                const uint8_t* wb = h.w_blocks + (int64_t)vt * n_tiles * SF;
+                const uint8_t* xb = h.q_blocks + (int64_t)(t0 / 128) * n_tiles * SF;
+                const int xb_n = min(p.b_tiles, (h.T + 127) / 128 - t0 / 128);
+                for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
+                    const uint32_t sf = min(2, n_tiles - 2 * k) * SF, a = a_at(at.s), e = sf_at(at.s);
+                    if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
+                    mbar_arrive_tx(full(at.s), A_BYTES + b_bytes + sf * (1 + xb_n));
+                    tma_2d(a, &w_map, k * 128, vt * VT, full(at.s));
+                    tma_2d(a + A_BYTES, &x_map, k * 128, t0, full(at.s));
+                    bulk_copy(e, wb + k * 2 * SF, sf, full(at.s));
+                    for (int j = 0; j < xb_n; j++)
+                        bulk_copy(e + (1 + j) * 2 * SF, xb + ((int64_t)j * n_tiles + 2 * k) * SF, sf, full(at.s));
+                }
+            }
+            if (*failed)                              // let the copies in flight land
+                for (int i = max(0, c - p.stages); i < c; i++)
+                    for (int it = 0; it < (1 << 20) && !mbar_try(full(i % p.stages), (i / p.stages) & 1); it++) {}
+        }
+    } else if (warp == 1) {
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
+        const bool issuer = elect_one();
+        Place at, acc;
+        bool ok = true;
+        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
+            if (!is_active(item)) continue;
+            const int t0 = item % p.n_nt * p.N, n = min(p.N, (h.T - t0 + 15) / 16 * 16);
+            const int xb_n = min(p.b_tiles, (h.T + 127) / 128 - t0 / 128);
+            // D f32; A and B of E2M1, both along K; exponents alone as scales; N and M
+            const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
+                                   ((uint32_t)(VT >> 4) << 24);
+            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+            const uint32_t d = tmem + acc.s * p.acc;
+            for (int k = 0; k < n_k; k++, at.next(p.stages)) {
+                if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t da = operand_desc(a_at(at.s)), db = operand_desc(a_at(at.s) + A_BYTES);
+                const uint32_t e = sf_at(at.s), sf = tmem + 2 * p.acc + at.s * p.sf_cols;
+                const int chunks = min(2, n_tiles - 2 * k);
+                if (issuer) {
+                    for (int c = 0; c < chunks; c++) {
+                        const uint32_t sfa = sf + 4 * c, sfb = sf + 8 + 4 * p.b_tiles * c;
+                        copy_exponents(sfa, e + c * SF);
+                        for (int j = 0; j < xb_n; j++) copy_exponents(sfb + 4 * j, e + ((1 + j) * 2 + c) * SF);
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {           // which two of a word's four exponents
+                            const uint32_t id = 2 * i;
+                            mma_mx4(d, da + 4 * c + 2 * i, db + 4 * c + 2 * i, idesc | (id << 29) | (id << 4), sfa,
+                                    sfb + t0 % 128 / 32, k | c | i);
+                        }
+                    }
+                    mma_commit<false>(empty(at.s));
+                    if (k + 1 == n_k) mma_commit<false>(acc_full(acc.s));
+                }
+            }
+            acc.next(2);
+        }
+        if (!ok && issuer) {                          // let the products in flight finish
+            mma_commit<false>(drained);
+            for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
+        }
+    } else if (warp >= 4) {
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        Place acc;
+        for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+            const bool active = is_active(item);
+            const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N, n = min(p.N, h.T - t0);
+            const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
+            // the tile's scales and mask words (a lane per token), read while its products run
+            const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
+            float st[NT / 64];
+            uint32_t word[NT / 64];
+#pragma unroll
+            for (int i = 0; i < NT / 64; i++) {
+                const int t = (2 * i + half) * 32 + lane;
+                st[i] = t < n && h.scale ? h.scale[t0 + t] : 1.f;
+                const bool there = active && t < n && wi < h.W;
+                word[i] = !masked ? FULL : there ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u;
+            }
+            if (active) {
+                if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            }
+#pragma unroll
+            for (int i = 0; i < NT / 64; i++) {
+                const int g = 2 * i + half;
+                if (g * 32 >= n) break;
+                T* out = logits + (size_t)(t0 + g * 32) * h.row_stride + v;
+                uint32_t y[32] = {};
+                if (active) {
+                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + g * 32;
+                    tmem_load16(from, y);
+                    tmem_load16(from + 16, y + 16);
+                    tmem_wait(y);
+                }
+#pragma unroll
+                for (int j = 0; j < 32; j++) {
+                    const uint32_t wj = __shfl_sync(FULL, word[i], j);
+                    const float sj = __shfl_sync(FULL, st[i], j);
+                    if (g * 32 + j < n && v < h.V)
+                        store_f32(out, (wj >> lane) & 1 ? __uint_as_float(y[j]) * sj * sw
+                                                        : __uint_as_float(0xFF800000u));
+                    out += h.row_stride;
+                }
+            }
+            if (active) {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(acc_empty(acc.s));
+                acc.next(2);
+            }
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 3) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+    if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
+}
+
+template <typename T>
+psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    const char* me = "psc_head_logits_mx4";
+    const Plan p = plan_of(h.T, h.V);
+    int* faults = (int*)work;
+    uint8_t* flags = work + p.flags_at;
+    CUtensorMap w_map, x_map;
+    const uint64_t row = (h.K + 31) / 32 * 16;
+    if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, VT) ||
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, p.N))
+        return ops_fail(PSC_ERR_CUDA, me, "cuTensorMapEncodeTiled failed");
+    const int items = p.n_vt * p.n_nt;
+    if (h.bitmask) {
+        psc_status s = ops_launch(k_mx4_flags, dim3((items + 7) / 8), 256, 0, 1, cs, "k_mx4_flags", h, p.N, p.n_vt,
+                                  p.n_nt, faults, flags);
+        if (s != PSC_OK) return s;
+    }
+    return ops_launch(k_mx4_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
+                      w_map, x_map, h, logits, p, faults, (const uint8_t*)flags, 0);
+}
+
+template <typename T>
+psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    return head_mma(h, logits, work, cs);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K) {
+    if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K) return 256;
+    return plan_of(T, V).bytes;
+}
+
+psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
+                               int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
+                               const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
+                               psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes, void* stream) {
+    const char* me = "psc_head_logits_mx4";
+    if (T < 0 || V <= 0 || K <= 0 || row_stride < V || !is_dtype(dtype) || !d_w || !d_w_blocks ||
+        (T && (!d_q || !d_q_blocks || !d_logits)))
+        return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 131,072");
+    if (T > MAX_T || V > MAX_V || (int64_t)((T + NT - 1) / NT) * ((V + VT - 1) / VT) > 0x7fffffff)
+        return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
+    if (!is_mx4(d_w, w_stride, d_w_blocks, K) || (T && !is_mx4(d_q, q_stride, d_q_blocks, K)))
+        return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+    if (T == 0) return PSC_OK;
+    if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_mx4_work_bytes(T, V, K))
+        return ops_fail(PSC_ERR_ARG, me, "workspace missing, unaligned or too small");
+    const Head h{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
+                 (V + 31) / 32, row_stride};
+    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
+    return head(h, (float*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
+}
+
+}  // extern "C"

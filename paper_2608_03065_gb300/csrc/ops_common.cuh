@@ -1,4 +1,4 @@
-// What the operators around the mask (process.cu, sample.cu, head.cu, norm.cu, mx4.cu) share:
+// What the operators around the mask (process.cu, sample.cu, head.cu, norm.cu, mx4.cu, mx4_head.cu) share:
 // the C entries' error path, launches, and small device helpers.
 #pragma once
 

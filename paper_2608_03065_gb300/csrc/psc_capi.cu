@@ -2629,7 +2629,7 @@ psc_status upload_tables(std::unique_ptr<psc_handle>& h, int tables) {
 }  // namespace
 
 // ====================================================================== ABI
-// The error path of the C entries in other files (process.cu, sample.cu, head.cu, norm.cu, mx4.cu).
+// The error path of the C entries in other files (process.cu, sample.cu, head.cu, norm.cu, mx4.cu, mx4_head.cu).
 namespace psc {
 psc_status ops_fail(psc_status code, const char* what, const char* why) noexcept {
     try {
