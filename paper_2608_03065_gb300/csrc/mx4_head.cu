@@ -158,8 +158,8 @@ psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
 // k_mx4_mma: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by
 // up to 192 tokens (its N).  Both operands stay in 4 bits all the way; the tensor core takes their
 // blocks' powers of two from TMEM.  A stage is 256 columns of K:
-//   warp 0        TMA: 128 x 128 bytes of weights, N x 128 bytes of tokens, and both sides' tiles
-//                 of exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
+//   warps 0, 2, 3 TMA: 128 x 128 bytes of weights; N x 128 bytes of tokens; both sides' tiles of
+//                 exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
 //   warp 1        tcgen05.cp of the exponents into TMEM, then four tcgen05.mma of 128 x N x 64 into
 //                 one of two accumulators
 //   warps 4-11    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
@@ -198,13 +198,17 @@ Plan plan_of(int T, int V) {
     return p;
 }
 
-// Exponents' tiles: 32 rows of 16 bytes, 8 rows every 128 bytes, no swizzle.
-__device__ __forceinline__ uint64_t exponent_desc(uint32_t addr) {
-    return (uint64_t)((addr & 0x3FFFF) >> 4) | (8ull << 16) | (8ull << 32) | (1ull << 46);
+// Descriptors by their low words (addresses in units of 16 bytes).  Exponents' tiles: 32 rows of 16
+// bytes, 8 rows every 128 bytes, no swizzle; operands: operand_desc's.
+__device__ __forceinline__ uint64_t exponent_desc(uint32_t lo) {
+    return (uint64_t)(8u | (1u << 14)) << 32 | (lo | (8u << 16));
+}
+__device__ __forceinline__ uint64_t codes_desc(uint32_t lo) {
+    return (uint64_t)(64u | (1u << 14) | (2u << 29)) << 32 | (lo | (1u << 16));
 }
 // 512 bytes to four TMEM columns, the same in all four quarters of the lanes.
-__device__ __forceinline__ void copy_exponents(uint32_t to, uint32_t from) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(from)) : "memory");
+__device__ __forceinline__ void copy_exponents(uint32_t to, uint32_t lo) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(lo)) : "memory");
 }
 __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t add) {
@@ -214,10 +218,24 @@ __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint
         "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
         : "memory");
 }
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+// A stage's copies and products: exponents of CHUNKS times 128 columns (those of the weights, then those
+// of the tokens' B tiles), each of which two products of 64 columns use.  lo: the stage's start and
+// its exponents' in units of 16 bytes; sf: its TMEM columns; shift: where the tokens' begin in theirs.
+template <int B, int CHUNKS>
+__device__ __forceinline__ void issue_stage(uint32_t lo, uint32_t e, uint32_t sf, uint32_t shift, uint32_t d,
+                                            uint32_t idesc, uint32_t add) {
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+        copy_exponents(sf + 4 * c, e + 32 * c);
+#pragma unroll
+        for (int j = 0; j < B; j++) copy_exponents(sf + 8 + 4 * B * c + 4 * j, e + 64 * (1 + j) + 32 * c);
+    }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++)
+#pragma unroll
+        for (int i = 0; i < 2; i++)               // the first or the second two of a word's four exponents
+            mma_mx4(d, codes_desc(lo + 4 * c + 2 * i), codes_desc(lo + A_BYTES / 16 + 4 * c + 2 * i),
+                    idesc | (2u * i << 29) | (2u * i << 4), sf + 4 * c, sf + 8 + 4 * B * c + shift, add | c | i);
 }
 
 // How many rows of each tile some token allows, and the fault word.
@@ -240,9 +258,11 @@ __global__ void __launch_bounds__(256) k_mx4_flags(Head h, int N, int n_vt, int 
     if (lane == 0) flags[item] = (uint8_t)rows;
 }
 
-template <typename T>
+template <typename T, int B>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constant__ CUtensorMap w_map,
-                                                            const __grid_constant__ CUtensorMap x_map, Head h,
+                                                            const __grid_constant__ CUtensorMap x_map,
+                                                            const __grid_constant__ CUtensorMap w_blocks_map,
+                                                            const __grid_constant__ CUtensorMap x_blocks_map, Head h,
                                                             T* logits, Plan p, int* faults, const uint8_t* flags,
                                                             int leave_few) {
     extern __shared__ uint8_t dyn[];
@@ -252,9 +272,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
     const int b_bytes = p.N * KS / 2, n_items = p.n_vt * p.n_nt;
-    // operands first (multiples of 1024 bytes), then the exponents
-    auto a_at = [&](int s) { return base + s * (A_BYTES + b_bytes); };
-    auto sf_at = [&](int s) { return base + p.stages * (A_BYTES + b_bytes) + s * 2 * SF * (1 + p.b_tiles); };
+    // a stage's weights, tokens (multiples of 1024 bytes) and exponents
+    auto a_at = [&](int s) { return base + s * p.stage_bytes; };
     const uint32_t bars = smem_addr(s_bars);
     auto full = [&](int s) { return bars + 8 * s; };
     auto empty = [&](int s) { return bars + 8 * (MAX_STAGES + s); };
@@ -264,12 +283,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
 
     if (threadIdx.x == 0) {
         s_failed = 0;
-        for (int s = 0; s < p.stages; s++) mbar_init(full(s), 1), mbar_init(empty(s), 1);
+        for (int s = 0; s < p.stages; s++) mbar_init(full(s), 3), mbar_init(empty(s), 1);
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 3) {
+    if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -287,25 +306,27 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     if (!masked && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
     auto is_active = [&](int item) { return !masked || flags[item] != 0; };
 
-    if (warp == 0) {
+    if (warp != 1 && warp < 4) {
+        // Three threads load, each its part of every stage (weights, tokens, exponents of both): one alone
+        // takes 950 cycles for a stage's copies, of which the products of 192 tokens take 384.
         if (lane == 0) {
+            const int bytes = warp == 0 ? A_BYTES : warp == 2 ? b_bytes : 2 * SF * (1 + B);
+            const int part = warp == 0 ? 0 : warp == 2 ? A_BYTES : A_BYTES + b_bytes;
             Place at;
             int c = 0;
             for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
                 if (!is_active(item)) continue;
                 const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N;
-                const uint8_t* wb = h.w_blocks + (int64_t)vt * n_tiles * SF;
-                const uint8_t* xb = h.q_blocks + (int64_t)(t0 / 128) * n_tiles * SF;
-                const int xb_n = min(p.b_tiles, (h.T + 127) / 128 - t0 / 128);
                 for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
-                    const uint32_t sf = min(2, n_tiles - 2 * k) * SF, a = a_at(at.s), e = sf_at(at.s);
+                    const uint32_t to = a_at(at.s) + part, bar = full(at.s);
                     if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
-                    mbar_arrive_tx(full(at.s), A_BYTES + b_bytes + sf * (1 + xb_n));
-                    tma_2d(a, &w_map, k * 128, vt * VT, full(at.s));
-                    tma_2d(a + A_BYTES, &x_map, k * 128, t0, full(at.s));
-                    bulk_copy(e, wb + k * 2 * SF, sf, full(at.s));
-                    for (int j = 0; j < xb_n; j++)
-                        bulk_copy(e + (1 + j) * 2 * SF, xb + ((int64_t)j * n_tiles + 2 * k) * SF, sf, full(at.s));
+                    mbar_arrive_tx(bar, bytes);
+                    if (warp == 0) tma_2d(to, &w_map, k * 128, vt * VT, bar);
+                    else if (warp == 2) tma_2d(to, &x_map, k * 128, t0, bar);
+                    else {
+                        tma_2d(to, &w_blocks_map, k * 256, vt, bar);
+                        tma_2d(to + 2 * SF, &x_blocks_map, k * 256, t0 / 128, bar);
+                    }
                 }
             }
             if (*failed)                              // let the copies in flight land
@@ -315,35 +336,25 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     } else if (warp == 1) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
         const bool issuer = elect_one();
+        const uint32_t e_at = (A_BYTES + b_bytes) / 16;
         Place at, acc;
         bool ok = true;
         for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
             if (!is_active(item)) continue;
             const int t0 = item % p.n_nt * p.N, n = min(p.N, (h.T - t0 + 15) / 16 * 16);
-            const int xb_n = min(p.b_tiles, (h.T + 127) / 128 - t0 / 128);
             // D f32; A and B of E2M1, both along K; exponents alone as scales; N and M
             const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
                                    ((uint32_t)(VT >> 4) << 24);
             if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
-            const uint32_t d = tmem + acc.s * p.acc;
+            const uint32_t d = tmem + acc.s * p.acc, shift = t0 % 128 / 32;
             for (int k = 0; k < n_k; k++, at.next(p.stages)) {
+                const uint32_t lo = (a_at(at.s) & 0x3FFFF) >> 4, sf = tmem + 2 * p.acc + at.s * p.sf_cols;
+                const bool half = 2 * k + 1 == n_tiles;
                 if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t da = operand_desc(a_at(at.s)), db = operand_desc(a_at(at.s) + A_BYTES);
-                const uint32_t e = sf_at(at.s), sf = tmem + 2 * p.acc + at.s * p.sf_cols;
-                const int chunks = min(2, n_tiles - 2 * k);
                 if (issuer) {
-                    for (int c = 0; c < chunks; c++) {
-                        const uint32_t sfa = sf + 4 * c, sfb = sf + 8 + 4 * p.b_tiles * c;
-                        copy_exponents(sfa, e + c * SF);
-                        for (int j = 0; j < xb_n; j++) copy_exponents(sfb + 4 * j, e + ((1 + j) * 2 + c) * SF);
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {           // which two of a word's four exponents
-                            const uint32_t id = 2 * i;
-                            mma_mx4(d, da + 4 * c + 2 * i, db + 4 * c + 2 * i, idesc | (id << 29) | (id << 4), sfa,
-                                    sfb + t0 % 128 / 32, k | c | i);
-                        }
-                    }
+                    if (!half) issue_stage<B, 2>(lo, lo + e_at, sf, shift, d, idesc, k);
+                    else issue_stage<B, 1>(lo, lo + e_at, sf, shift, d, idesc, k);
                     mma_commit<false>(empty(at.s));
                     if (k + 1 == n_k) mma_commit<false>(acc_full(acc.s));
                 }
@@ -409,7 +420,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 3) {
+    if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
@@ -423,9 +434,14 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     int* faults = (int*)work;
     uint8_t* flags = work + p.flags_at;
     CUtensorMap w_map, x_map;
-    const uint64_t row = (h.K + 31) / 32 * 16;
+    CUtensorMap w_blocks_map, x_blocks_map;
+    const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, VT) ||
-        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, p.N))
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, p.N) ||
+        !tensor_map(&w_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.w_blocks, n_tiles * SF / 4, p.n_vt, n_tiles * SF,
+                    256, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, (h.T + 127) / 128,
+                    n_tiles * SF, 256, p.b_tiles, CU_TENSOR_MAP_SWIZZLE_NONE))
         return ops_fail(PSC_ERR_CUDA, me, "cuTensorMapEncodeTiled failed");
     const int items = p.n_vt * p.n_nt;
     if (h.bitmask) {
@@ -433,8 +449,8 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
                                   p.n_nt, faults, flags);
         if (s != PSC_OK) return s;
     }
-    return ops_launch(k_mx4_mma<T>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
-                      w_map, x_map, h, logits, p, faults, (const uint8_t*)flags, 0);
+    return ops_launch(p.b_tiles == 2 ? k_mx4_mma<T, 2> : k_mx4_mma<T, 1>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
+                      w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults, (const uint8_t*)flags, 0);
 }
 
 template <typename T>

@@ -120,9 +120,9 @@ __device__ __forceinline__ void tmem_wait(uint32_t r[32]) {
     for (int i = 0; i < 32; i++) asm volatile("" : "+r"(r[i]));      // no use of r before the wait
 }
 
-// A tensor map over rows of `stride` bytes, boxes of `cols` x `rows` in the 128-byte swizzle.
+// A tensor map over rows of `stride` bytes, boxes of `cols` x `rows`.
 bool tensor_map(CUtensorMap* m, CUtensorMapDataType type, const void* p, uint64_t cols, uint64_t rows, uint64_t stride,
-                uint32_t box_cols, uint32_t box_rows) {
+                uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult r;
@@ -135,7 +135,7 @@ bool tensor_map(CUtensorMap* m, CUtensorMapDataType type, const void* p, uint64_
     const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
     const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
     return encode(m, type, 2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
