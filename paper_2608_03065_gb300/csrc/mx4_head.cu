@@ -170,7 +170,10 @@ constexpr int KS = 256;                       // columns of K of a stage (128 by
 constexpr int A_BYTES = VT * KS / 2;
 constexpr int SF = 512;                       // a tile of exponents: 128 rows by 128 columns
 constexpr int MAX_STAGES = 11;
-constexpr int MMA_THREADS = 384, EPILOGUE = 8;  // threads; warps of the epilogue
+constexpr int PARTS = 2, EPILOGUE = 4 * PARTS;  // warps for the same 32 vocabulary rows, of the epilogue in all
+constexpr int GROUPS = NT / 32 / PARTS;       // a warp's groups of 32 tokens
+constexpr int SMEM_OWN = 2048 + NT * 32;      // beside the stages: alignment, barriers, the epilogue's tokens
+constexpr int MMA_THREADS = 32 * (4 + EPILOGUE);
 
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
@@ -191,7 +194,7 @@ Plan plan_of(int T, int V) {
     p.acc = (p.N + 31) / 32 * 32;
     p.sf_cols = 8 + 8 * p.b_tiles;
     // a stage's exponents have TMEM columns of their own, free when the stage is
-    p.stages = std::min({MAX_STAGES, (SMEM_MAX - 2048) / p.stage_bytes, (512 - 2 * p.acc) / p.sf_cols});
+    p.stages = std::min({MAX_STAGES, (SMEM_MAX - SMEM_OWN) / p.stage_bytes, (512 - 2 * p.acc) / p.sf_cols});
     p.smem = 1024 + (size_t)p.stages * p.stage_bytes;
     p.flags_at = 256;
     p.bytes = p.flags_at + ((int64_t)p.n_vt * p.n_nt + 255) / 256 * 256;
@@ -258,15 +261,67 @@ __global__ void __launch_bounds__(256) k_mx4_flags(Head h, int N, int n_vt, int 
     if (lane == 0) flags[item] = (uint8_t)rows;
 }
 
-template <typename T, int B>
+// What the epilogue knows of a token: its scale, and the mask's word for the warp's 32 vocabulary rows.
+struct __align__(8) Token {
+    float scale;
+    uint32_t word;
+};
+
+// Products of a lane's vocabulary row (the lanes' are neighbours) with 32 tokens, as logits: out is
+// the first token's, `left` how many rows there are from the lane's on.  Two bf16 logits of a token
+// go out in one store: lanes pair up, the even one takes the first of two tokens, the odd one the
+// second (4-byte aligned where `even` says so).
+template <bool MASKED>
+__device__ __forceinline__ float logit(uint32_t y, float scale, uint32_t word, float sw, uint32_t bit) {
+    const float x = __uint_as_float(y) * scale * sw;
+    return !MASKED || (word & bit) ? x : __uint_as_float(0xFF800000u);
+}
+template <bool MASKED, typename T>
+__device__ __forceinline__ void store_group(T* out, int64_t stride, const uint32_t y[32], const Token* tokens, float sw,
+                                            int n, int left, bool even) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t bit = 1u << lane;
+    const float4* pairs = reinterpret_cast<const float4*>(tokens);          // of two tokens each
+    const bool whole = n == 32 && __all_sync(FULL, left > 0);
+    if (sizeof(T) == 2 && whole && even) {
+        const bool odd = lane & 1;
+        const uint32_t pick = odd ? 0x3276u : 0x5410u;
+        T* at = out + (odd ? stride - 1 : 0);
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float4 p = pairs[j / 2];
+            const uint32_t u = pack_bf16(logit<MASKED>(y[j], p.x, __float_as_uint(p.y), sw, bit),
+                                         logit<MASKED>(y[j + 1], p.z, __float_as_uint(p.w), sw, bit));
+            *reinterpret_cast<uint32_t*>(at) = __byte_perm(u, __shfl_xor_sync(FULL, u, 1), pick);
+            at += 2 * stride;
+        }
+    } else if (whole) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float4 p = pairs[j / 2];
+            store_f32(out, logit<MASKED>(y[j], p.x, __float_as_uint(p.y), sw, bit));
+            store_f32(out + stride, logit<MASKED>(y[j + 1], p.z, __float_as_uint(p.w), sw, bit));
+            out += 2 * stride;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; j++) {
+            if (j < n && left > 0) store_f32(out, logit<MASKED>(y[j], tokens[j].scale, tokens[j].word, sw, bit));
+            out += stride;
+        }
+    }
+}
+
+template <typename T, int B, bool MASKED>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
                                                             const __grid_constant__ CUtensorMap w_blocks_map,
                                                             const __grid_constant__ CUtensorMap x_blocks_map, Head h,
                                                             T* logits, Plan p, int* faults, const uint8_t* flags,
-                                                            int leave_few) {
+                                                            bool even) {
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) uint64_t s_bars[2 * MAX_STAGES + 5];
+    __shared__ __align__(16) Token s_tokens[EPILOGUE][GROUPS * 32];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -301,10 +356,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
     dep_wait();
     dep_launch();
-    const bool masked = h.bitmask != nullptr;
     // A block that fails has polled for a good part of a second before it counts itself.
-    if (!masked && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    auto is_active = [&](int item) { return !masked || flags[item] != 0; };
+    if (!MASKED && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    auto is_active = [&](int item) { return !MASKED || flags[item] != 0; };
 
     if (warp != 1 && warp < 4) {
         // Three threads load, each its part of every stage (weights, tokens, exponents of both): one alone
@@ -366,32 +420,33 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= 4) {
-        const int quad = warp & 3, half = (warp - 4) >> 2;
+        const int quad = warp & 3, part = (warp - 4) >> 2;      // of every PARTS groups of 32 tokens, this warp's
+        Token* tokens = s_tokens[warp - 4];
         Place acc;
         for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
             const bool active = is_active(item);
             const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N, n = min(p.N, h.T - t0);
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
-            // the tile's scales and mask words (a lane per token), read while its products run
+            // the tile's scales and mask words, read while its products run
             const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
-            float st[NT / 64];
-            uint32_t word[NT / 64];
+            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < NT / 64; i++) {
-                const int t = (2 * i + half) * 32 + lane;
-                st[i] = t < n && h.scale ? h.scale[t0 + t] : 1.f;
-                const bool there = active && t < n && wi < h.W;
-                word[i] = !masked ? FULL : there ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u;
+            for (int i = 0; i < GROUPS; i++) {
+                const int t = (PARTS * i + part) * 32 + lane;
+                if (t >= n) continue;
+                tokens[i * 32 + lane] = {
+                    h.scale ? h.scale[t0 + t] : 1.f,
+                    !MASKED ? FULL : active && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u};
             }
+            __syncwarp();
             if (active) {
                 if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-#pragma unroll
-            for (int i = 0; i < NT / 64; i++) {
-                const int g = 2 * i + half;
+#pragma unroll 1
+            for (int i = 0; i < GROUPS; i++) {
+                const int g = PARTS * i + part;
                 if (g * 32 >= n) break;
-                T* out = logits + (size_t)(t0 + g * 32) * h.row_stride + v;
                 uint32_t y[32] = {};
                 if (active) {
                     const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + g * 32;
@@ -399,15 +454,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
                     tmem_load16(from + 16, y + 16);
                     tmem_wait(y);
                 }
-#pragma unroll
-                for (int j = 0; j < 32; j++) {
-                    const uint32_t wj = __shfl_sync(FULL, word[i], j);
-                    const float sj = __shfl_sync(FULL, st[i], j);
-                    if (g * 32 + j < n && v < h.V)
-                        store_f32(out, (wj >> lane) & 1 ? __uint_as_float(y[j]) * sj * sw
-                                                        : __uint_as_float(0xFF800000u));
-                    out += h.row_stride;
-                }
+                store_group<MASKED>(logits + (size_t)(t0 + g * 32) * h.row_stride + v, h.row_stride, y, tokens + i * 32,
+                                    sw, min(32, n - g * 32), h.V - v, even);
             }
             if (active) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -449,8 +497,11 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
                                   p.n_nt, faults, flags);
         if (s != PSC_OK) return s;
     }
-    return ops_launch(p.b_tiles == 2 ? k_mx4_mma<T, 2> : k_mx4_mma<T, 1>, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
-                      w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults, (const uint8_t*)flags, 0);
+    auto kernel = h.bitmask ? (p.b_tiles == 2 ? k_mx4_mma<T, 2, true> : k_mx4_mma<T, 1, true>)
+                            : (p.b_tiles == 2 ? k_mx4_mma<T, 2, false> : k_mx4_mma<T, 1, false>);
+    const bool even = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 4);
+    return ops_launch(kernel, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
+                      w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults, (const uint8_t*)flags, even);
 }
 
 template <typename T>
