@@ -158,44 +158,64 @@ psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
 // k_mx4_mma: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by
 // up to 192 tokens (its N).  Both operands stay in 4 bits all the way; the tensor core takes their
 // blocks' powers of two from TMEM.  A stage is 256 columns of K:
-//   warps 0, 2, 3 TMA: 128 x 128 bytes of weights; N x 128 bytes of tokens; both sides' tiles of
-//                 exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
+//   warps 0, 2, 3 TMA: 128 x 128 bytes of weights and their exponents (512 bytes for 128 rows by 128
+//                 columns, as they lie in memory); N x 128 bytes of tokens; the tokens' exponents
 //   warp 1        tcgen05.cp of the exponents into TMEM, then four tcgen05.mma of 128 x N x 64 into
 //                 one of two accumulators
 //   warps 4-11    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
 //                 for 32 of them)
+// Beyond 128 tokens blocks pair up (PAIR): 256 vocabulary rows, 128 in each, by the same tokens, half of
+// their codes in each (tcgen05's cta_group::2; all of their exponents in both).  An SM takes in 64
+// bytes a cycle, and 192 tokens by 128 rows need 43 KB for a stage's 384 cycles of products; in a
+// pair it is 31 KB, and where a tile's weights fit shared memory (K up to 2048), they stay there
+// for all tiles of tokens (`stay`), which leaves 14 KB.
 constexpr int VT = 128;                       // vocabulary rows of a tile
 constexpr int NT = 192;                       // tokens of a tile at most; tiles start at multiples of 64
 constexpr int KS = 256;                       // columns of K of a stage (128 bytes of codes)
-constexpr int A_BYTES = VT * KS / 2;
+constexpr int A_CODES = VT * KS / 2;
 constexpr int SF = 512;                       // a tile of exponents: 128 rows by 128 columns
-constexpr int MAX_STAGES = 11;
+constexpr int A_BYTES = A_CODES + 2 * SF;
+constexpr int MAX_A = 12, MAX_B = 11;         // slots of the rings: weights, tokens
 constexpr int PARTS = 2, EPILOGUE = 4 * PARTS;  // warps for the same 32 vocabulary rows, of the epilogue in all
 constexpr int GROUPS = NT / 32 / PARTS;       // a warp's groups of 32 tokens
-constexpr int SMEM_OWN = 2048 + NT * 32;      // beside the stages: alignment, barriers, the epilogue's tokens
+constexpr int SMEM_OWN = 2048 + NT * 32;      // beside the rings: alignment, barriers, the epilogue's tokens
 constexpr int MMA_THREADS = 32 * (4 + EPILOGUE);
 
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
-    int b_tiles;                              // 128-row tiles of exponents that a tile of tokens touches at most
-    int stages, stage_bytes;
+    bool pair, stay;
+    int n_k;                                  // stages of K
+    int n_a, n_b, b_codes, b_bytes;           // slots of the rings, a slot's bytes of tokens (in a block)
     int acc, sf_cols;                         // TMEM columns of an accumulator, of a stage's exponents
+    int items;                                // tiles (of pairs: two by two)
     size_t smem;
     int64_t flags_at, bytes;                  // in the workspace: the fault word, the tiles' flags
 };
 
-Plan plan_of(int T, int V) {
+Plan plan_of(int T, int V, int K) {
     Plan p;
     p.n_nt = (T + NT - 1) / NT;
     p.N = p.n_nt > 1 ? NT : (T + 15) / 16 * 16;
     p.n_vt = (V + VT - 1) / VT;
-    p.b_tiles = p.N > 128 ? 2 : 1;
-    p.stage_bytes = A_BYTES + p.N * KS / 2 + 2 * SF * (1 + p.b_tiles);
+    p.pair = p.N > 128;
+    if (p.pair) p.N = (p.N + 31) / 32 * 32;
+    p.n_k = (K + KS - 1) / KS;
+    p.b_codes = (p.pair ? p.N / 2 : p.N) * KS / 2;
+    p.b_bytes = p.b_codes + 2 * SF * (p.pair ? 2 : 1);
     p.acc = (p.N + 31) / 32 * 32;
-    p.sf_cols = 8 + 8 * p.b_tiles;
-    // a stage's exponents have TMEM columns of their own, free when the stage is
-    p.stages = std::min({MAX_STAGES, (SMEM_MAX - SMEM_OWN) / p.stage_bytes, (512 - 2 * p.acc) / p.sf_cols});
-    p.smem = 1024 + (size_t)p.stages * p.stage_bytes;
+    p.sf_cols = p.pair ? 24 : 16;
+    // a stage's exponents have TMEM columns of their own, free when the tokens' slot is
+    const int room = SMEM_MAX - SMEM_OWN, most = std::min(MAX_B, (512 - 2 * p.acc) / p.sf_cols);
+    p.n_b = std::min(most, room / (A_BYTES + p.b_bytes));
+    p.n_a = p.n_b;
+    p.stay = p.n_nt > 1 && p.n_k <= MAX_A && p.n_k * A_BYTES + 4 * p.b_bytes <= room;
+    if (p.stay) {
+        p.n_b = std::min(most, (room - p.n_k * A_BYTES) / p.b_bytes);
+        p.n_a = std::min(MAX_A, (room - p.n_b * p.b_bytes) / A_BYTES);
+    }
+    const int64_t items = (int64_t)(p.pair ? (p.n_vt + 1) / 2 : p.n_vt) * p.n_nt;
+    p.items = (int)std::min<int64_t>(items, 0x7fffffff);
+    p.smem = 1024 + (size_t)p.n_a * A_BYTES + (size_t)p.n_b * p.b_bytes;
     p.flags_at = 256;
     p.bytes = p.flags_at + ((int64_t)p.n_vt * p.n_nt + 255) / 256 * 256;
     return p;
@@ -209,36 +229,69 @@ __device__ __forceinline__ uint64_t exponent_desc(uint32_t lo) {
 __device__ __forceinline__ uint64_t codes_desc(uint32_t lo) {
     return (uint64_t)(64u | (1u << 14) | (2u << 29)) << 32 | (lo | (1u << 16));
 }
-// 512 bytes to four TMEM columns, the same in all four quarters of the lanes.
+// 512 bytes to four TMEM columns, the same in all four quarters of the lanes (of both blocks of a pair,
+// from their own shared memory).
+template <bool PAIR>
 __device__ __forceinline__ void copy_exponents(uint32_t to, uint32_t lo) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(lo)) : "memory");
+    if (PAIR)
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(lo)) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(exponent_desc(lo)) : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t add) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
+            : "memory");
+}
+// A tile into this block's shared memory; of a pair, the barrier is the first block's.
+template <bool PAIR>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        tma_2d(dst, map, x, y, bar);
+}
+// The address of the first block's barrier in the pair's shared memory.
+__device__ __forceinline__ uint32_t at_first(uint32_t bar) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
 }
 // A stage's copies and products: exponents of CHUNKS times 128 columns (those of the weights, then those
-// of the tokens' B tiles), each of which two products of 64 columns use.  lo: the stage's start and
-// its exponents' in units of 16 bytes; sf: its TMEM columns; shift: where the tokens' begin in theirs.
-template <int B, int CHUNKS>
-__device__ __forceinline__ void issue_stage(uint32_t lo, uint32_t e, uint32_t sf, uint32_t shift, uint32_t d,
-                                            uint32_t idesc, uint32_t add) {
+// of the tokens, 128 or, of a pair, 256 rows), each of which two products of 64 columns use.  a, b: the
+// slots of both sides, ea, eb: their exponents, in units of 16 bytes; sf: the stage's TMEM columns;
+// shift: where the tile's tokens begin in theirs.
+template <bool PAIR, int CHUNKS>
+__device__ __forceinline__ void issue_stage(uint32_t a, uint32_t ea, uint32_t b, uint32_t eb, uint32_t sf,
+                                            uint32_t shift, uint32_t d, uint32_t idesc, uint32_t add) {
+    constexpr int B = PAIR ? 2 : 1;
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        copy_exponents(sf + 4 * c, e + 32 * c);
+        copy_exponents<PAIR>(sf + 4 * c, ea + 32 * c);
 #pragma unroll
-        for (int j = 0; j < B; j++) copy_exponents(sf + 8 + 4 * B * c + 4 * j, e + 64 * (1 + j) + 32 * c);
+        for (int j = 0; j < B; j++) copy_exponents<PAIR>(sf + 8 + 4 * B * c + 4 * j, eb + 64 * j + 32 * c);
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++)
 #pragma unroll
         for (int i = 0; i < 2; i++)               // the first or the second two of a word's four exponents
-            mma_mx4(d, codes_desc(lo + 4 * c + 2 * i), codes_desc(lo + A_BYTES / 16 + 4 * c + 2 * i),
-                    idesc | (2u * i << 29) | (2u * i << 4), sf + 4 * c, sf + 8 + 4 * B * c + shift, add | c | i);
+            mma_mx4<PAIR>(d, codes_desc(a + 4 * c + 2 * i), codes_desc(b + 4 * c + 2 * i),
+                          idesc | (2u * i << 29) | (2u * i << 4), sf + 4 * c, sf + 8 + 4 * B * c + shift, add | c | i);
 }
 
 // How many rows of each tile some token allows, and the fault word.
@@ -312,7 +365,7 @@ __device__ __forceinline__ void store_group(T* out, int64_t stride, const uint32
     }
 }
 
-template <typename T, int B, bool MASKED>
+template <typename T, bool PAIR, bool MASKED>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
                                                             const __grid_constant__ CUtensorMap w_blocks_map,
@@ -320,113 +373,165 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
                                                             T* logits, Plan p, int* faults, const uint8_t* flags,
                                                             bool even) {
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * MAX_STAGES + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * (MAX_A + MAX_B) + 5];
     __shared__ __align__(16) Token s_tokens[EPILOGUE][GROUPS * 32];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int SIDES = PAIR ? 2 : 1;
+    const int side = PAIR ? (int)cluster_rank() : 0;
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
-    const int b_bytes = p.N * KS / 2, n_items = p.n_vt * p.n_nt;
-    // a stage's weights, tokens (multiples of 1024 bytes) and exponents
-    auto a_at = [&](int s) { return base + s * p.stage_bytes; };
+    // slots start at multiples of 1024 bytes: codes, then exponents
+    auto a_at = [&](int s) { return base + s * A_BYTES; };
+    auto b_at = [&](int s) { return base + p.n_a * A_BYTES + s * p.b_bytes; };
     const uint32_t bars = smem_addr(s_bars);
-    auto full = [&](int s) { return bars + 8 * s; };
-    auto empty = [&](int s) { return bars + 8 * (MAX_STAGES + s); };
-    auto acc_full = [&](int s) { return bars + 8 * (2 * MAX_STAGES + s); };
-    auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_STAGES + 2 + s); };
-    const uint32_t drained = bars + 8 * (2 * MAX_STAGES + 4);
+    auto a_full = [&](int s) { return bars + 8 * s; };
+    auto a_empty = [&](int s) { return bars + 8 * (MAX_A + s); };
+    auto b_full = [&](int s) { return bars + 8 * (2 * MAX_A + s); };
+    auto b_empty = [&](int s) { return bars + 8 * (2 * MAX_A + MAX_B + s); };
+    constexpr int LAST = 2 * (MAX_A + MAX_B);
+    auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
+    const uint32_t drained = bars + 8 * (LAST + 4);
 
     if (threadIdx.x == 0) {
         s_failed = 0;
-        for (int s = 0; s < p.stages; s++) mbar_init(full(s), 3), mbar_init(empty(s), 1);
-        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE);
+        for (int s = 0; s < p.n_a; s++) mbar_init(a_full(s), 1), mbar_init(a_empty(s), 1);
+        for (int s = 0; s < p.n_b; s++) mbar_init(b_full(s), 2), mbar_init(b_empty(s), 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * SIDES);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (PAIR) cluster_sync();
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
-    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
+    const int n_tiles = (h.K + 127) / 128, n_k = p.n_k;
     dep_wait();
     dep_launch();
     // A block that fails has polled for a good part of a second before it counts itself.
     if (!MASKED && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    auto is_active = [&](int item) { return !MASKED || flags[item] != 0; };
+    // This block's (pair's) items, all tiles of tokens of a tile of vocabulary rows after each other.
+    const int me = blockIdx.x / SIDES, all = gridDim.x / SIDES;
+    const int begin = (int)((int64_t)p.items * me / all), end = (int)((int64_t)p.items * (me + 1) / all);
+    // whether an item (its vocabulary tile and tile of tokens) has an allowed token, in either block
+    auto is_active = [&](int vt, int nt) {
+        if (!MASKED) return true;
+        const int at = vt * SIDES * p.n_nt + nt;
+        return flags[at] != 0 || (PAIR && vt * 2 + 1 < p.n_vt && flags[at + p.n_nt] != 0);
+    };
+    // of a tile of tokens: how many the products take (both halves of a pair's in whole eights)
+    auto tokens_of = [&](int t0) {
+        const int n = min(p.N, h.T - t0);
+        return PAIR ? (n + 31) / 32 * 32 : (n + 15) / 16 * 16;
+    };
 
-    if (warp != 1 && warp < 4) {
-        // Three threads load, each its part of every stage (weights, tokens, exponents of both): one alone
-        // takes 950 cycles for a stage's copies, of which the products of 192 tokens take 384.
+    if (warp == 0 || warp == 2 || warp == 3) {
+        // Three threads load, each its part of every stage: one alone takes 950 cycles for a stage's copies.
         if (lane == 0) {
-            const int bytes = warp == 0 ? A_BYTES : warp == 2 ? b_bytes : 2 * SF * (1 + B);
-            const int part = warp == 0 ? 0 : warp == 2 ? A_BYTES : A_BYTES + b_bytes;
+            const bool weights = warp == 0;
+            const int slots = weights ? p.n_a : p.n_b;
+            const int bytes = SIDES * (weights ? A_BYTES : warp == 2 ? p.b_codes : p.b_bytes - p.b_codes);
+            const int part = warp == 3 ? p.b_codes : 0;
+            auto full = [&](int s) { return weights ? a_full(s) : b_full(s); };
             Place at;
             int c = 0;
-            for (int item = blockIdx.x; item < n_items && !*failed; item += gridDim.x) {
-                if (!is_active(item)) continue;
-                const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N;
-                for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
-                    const uint32_t to = a_at(at.s) + part, bar = full(at.s);
-                    if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
-                    mbar_arrive_tx(bar, bytes);
-                    if (warp == 0) tma_2d(to, &w_map, k * 128, vt * VT, bar);
-                    else if (warp == 2) tma_2d(to, &x_map, k * 128, t0, bar);
-                    else {
-                        tma_2d(to, &w_blocks_map, k * 256, vt, bar);
-                        tma_2d(to + 2 * SF, &x_blocks_map, k * 256, t0 / 128, bar);
+            bool fresh = true;                        // the tile's weights are not there yet
+            for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && !*failed; item++) {
+                if (is_active(vt, nt) && (!weights || fresh || !p.stay)) {
+                    fresh = false;
+                    const int t0 = nt * p.N, x0 = t0 + side * (tokens_of(t0) / 2);
+                    for (int k = 0; k < n_k; k++, c++, at.next(slots)) {
+                        if (!mbar_wait(weights ? a_empty(at.s) : b_empty(at.s), at.parity ^ 1, failed)) break;
+                        const uint32_t to = (weights ? a_at(at.s) : b_at(at.s)) + part;
+                        const uint32_t own = full(at.s), bar = PAIR ? at_first(own) : own;
+                        if (!PAIR || side == 0) mbar_arrive_tx(own, bytes);
+                        if (weights) {
+                            load_tile<PAIR>(to, &w_map, k * 128, (vt * SIDES + side) * VT, bar);
+                            load_tile<PAIR>(to + A_CODES, &w_blocks_map, k * 256, vt * SIDES + side, bar);
+                        } else if (warp == 2) {
+                            load_tile<PAIR>(to, &x_map, k * 128, x0, bar);
+                        } else {
+                            load_tile<PAIR>(to, &x_blocks_map, k * 256, t0 / 128, bar);
+                        }
                     }
                 }
+                if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
             }
-            if (*failed)                              // let the copies in flight land
-                for (int i = max(0, c - p.stages); i < c; i++)
-                    for (int it = 0; it < (1 << 20) && !mbar_try(full(i % p.stages), (i / p.stages) & 1); it++) {}
+            // let the copies in flight land (of a pair, the first block sees both blocks', and the second
+            // does not end before it)
+            if (*failed && side == 0)
+                for (int i = max(0, c - slots); i < c; i++)
+                    for (int it = 0; it < (1 << 20) && !mbar_try(full(i % slots), (i / slots) & 1); it++) {}
         }
-    } else if (warp == 1) {
-        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
+    } else if (warp == 1 && side == 0) {
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
+        // issues (of a pair, for both blocks).
         const bool issuer = elect_one();
-        const uint32_t e_at = (A_BYTES + b_bytes) / 16;
-        Place at, acc;
-        bool ok = true;
-        for (int item = blockIdx.x; item < n_items && ok; item += gridDim.x) {
-            if (!is_active(item)) continue;
-            const int t0 = item % p.n_nt * p.N, n = min(p.N, (h.T - t0 + 15) / 16 * 16);
-            // D f32; A and B of E2M1, both along K; exponents alone as scales; N and M
-            const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
-                                   ((uint32_t)(VT >> 4) << 24);
-            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
-            const uint32_t d = tmem + acc.s * p.acc, shift = t0 % 128 / 32;
-            for (int k = 0; k < n_k; k++, at.next(p.stages)) {
-                const uint32_t lo = (a_at(at.s) & 0x3FFFF) >> 4, sf = tmem + 2 * p.acc + at.s * p.sf_cols;
-                const bool half = 2 * k + 1 == n_tiles;
-                if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (issuer) {
-                    if (!half) issue_stage<B, 2>(lo, lo + e_at, sf, shift, d, idesc, k);
-                    else issue_stage<B, 1>(lo, lo + e_at, sf, shift, d, idesc, k);
-                    mma_commit<false>(empty(at.s));
-                    if (k + 1 == n_k) mma_commit<false>(acc_full(acc.s));
+        Place unit, at_b, acc;                        // unit: the first slot of the tile's weights
+        bool ok = true, fresh = true;
+        for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && ok; item++) {
+            if (is_active(vt, nt)) {
+                // whether the weights have to be waited for, and whether nothing of them is used after this item
+                const bool first = fresh || !p.stay;
+                bool last = true;
+                if (p.stay)
+                    for (int i = item + 1, j = nt + 1; last && i < end && j < p.n_nt; i++, j++) last = !is_active(vt, j);
+                fresh = false;
+                const int t0 = nt * p.N;
+                // D f32; A and B of E2M1, both along K; exponents alone as scales; N and M
+                const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(tokens_of(t0) >> 3) << 17) | (1u << 23) |
+                                       ((uint32_t)(VT * SIDES >> 4) << 24);
+                const uint32_t d = tmem + acc.s * p.acc, shift = t0 % 128 / 32;
+                if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+                Place at_a = unit;
+                for (int k = 0; k < n_k; k++, at_a.next(p.n_a), at_b.next(p.n_b)) {
+                    const uint32_t a = (a_at(at_a.s) & 0x3FFFF) >> 4, b = (b_at(at_b.s) & 0x3FFFF) >> 4;
+                    const uint32_t ea = a + A_CODES / 16, eb = b + p.b_codes / 16, sf = tmem + 2 * p.acc + at_b.s * p.sf_cols;
+                    if (!(ok = first ? warp_wait2(a_full(at_a.s), at_a.parity, b_full(at_b.s), at_b.parity, failed)
+                                     : warp_wait(b_full(at_b.s), at_b.parity, failed)))
+                        break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (issuer) {
+                        if (2 * k + 2 <= n_tiles) issue_stage<PAIR, 2>(a, ea, b, eb, sf, shift, d, idesc, k);
+                        else issue_stage<PAIR, 1>(a, ea, b, eb, sf, shift, d, idesc, k);
+                        mma_commit<PAIR>(b_empty(at_b.s));
+                        if (last) mma_commit<PAIR>(a_empty(at_a.s));
+                        if (k + 1 == n_k) mma_commit<PAIR>(acc_full(acc.s));
+                    }
                 }
+                if (last) unit = at_a;
+                acc.next(2);
             }
-            acc.next(2);
+            if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
         }
         if (!ok && issuer) {                          // let the products in flight finish
-            mma_commit<false>(drained);
+            mma_commit<PAIR>(drained);
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= 4) {
         const int quad = warp & 3, part = (warp - 4) >> 2;      // of every PARTS groups of 32 tokens, this warp's
         Token* tokens = s_tokens[warp - 4];
         Place acc;
-        for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-            const bool active = is_active(item);
-            const int vt = item / p.n_nt, t0 = item % p.n_nt * p.N, n = min(p.N, h.T - t0);
+        for (int item = begin, pt = begin / p.n_nt, nt = begin % p.n_nt; item < end; item++) {
+            const bool active = is_active(pt, nt);
+            const int vt = pt * SIDES + side, t0 = nt * p.N, n = min(p.N, h.T - t0);
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
+            if (++nt == p.n_nt) nt = 0, pt++;
             // the tile's scales and mask words, read while its products run
             const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
             __syncwarp();
@@ -460,7 +565,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
             if (active) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty(acc.s));
+                if (lane == 0) {
+                    if (PAIR) arrive_at_first(acc_empty(acc.s));
+                    else mbar_arrive(acc_empty(acc.s));
+                }
                 acc.next(2);
             }
         }
@@ -468,9 +576,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (PAIR) cluster_sync();                         // nothing of this block is used by the other any more
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
     if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
 }
@@ -478,18 +588,19 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
 template <typename T>
 psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     const char* me = "psc_head_logits_mx4";
-    const Plan p = plan_of(h.T, h.V);
+    const Plan p = plan_of(h.T, h.V, h.K);
     int* faults = (int*)work;
     uint8_t* flags = work + p.flags_at;
     CUtensorMap w_map, x_map;
     CUtensorMap w_blocks_map, x_blocks_map;
     const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, VT) ||
-        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, p.N) ||
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128,
+                    p.pair ? p.N / 2 : p.N) ||
         !tensor_map(&w_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.w_blocks, n_tiles * SF / 4, p.n_vt, n_tiles * SF,
                     256, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, (h.T + 127) / 128,
-                    n_tiles * SF, 256, p.b_tiles, CU_TENSOR_MAP_SWIZZLE_NONE))
+                    n_tiles * SF, 256, p.pair ? 2 : 1, CU_TENSOR_MAP_SWIZZLE_NONE))
         return ops_fail(PSC_ERR_CUDA, me, "cuTensorMapEncodeTiled failed");
     const int items = p.n_vt * p.n_nt;
     if (h.bitmask) {
@@ -497,11 +608,13 @@ psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
                                   p.n_nt, faults, flags);
         if (s != PSC_OK) return s;
     }
-    auto kernel = h.bitmask ? (p.b_tiles == 2 ? k_mx4_mma<T, 2, true> : k_mx4_mma<T, 1, true>)
-                            : (p.b_tiles == 2 ? k_mx4_mma<T, 2, false> : k_mx4_mma<T, 1, false>);
+    auto kernel = h.bitmask ? (p.pair ? k_mx4_mma<T, true, true> : k_mx4_mma<T, false, true>)
+                            : (p.pair ? k_mx4_mma<T, true, false> : k_mx4_mma<T, false, false>);
     const bool even = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 4);
-    return ops_launch(kernel, dim3(std::min(items, current_sms())), MMA_THREADS, p.smem, 1, cs, "k_mx4_mma",
-                      w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults, (const uint8_t*)flags, even);
+    const int sides = p.pair ? 2 : 1;
+    return ops_launch(kernel, dim3(std::min(p.items, current_sms() / sides) * sides), MMA_THREADS, p.smem, sides, cs,
+                      "k_mx4_mma", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults,
+                      (const uint8_t*)flags, even);
 }
 
 template <typename T>
@@ -515,7 +628,7 @@ extern "C" {
 
 int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K) {
     if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K) return 256;
-    return plan_of(T, V).bytes;
+    return plan_of(T, V, K).bytes;
 }
 
 psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
