@@ -158,11 +158,11 @@ psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
 // k_mx4_mma: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by
 // up to 192 tokens (its N).  Both operands stay in 4 bits all the way; the tensor core takes their
 // blocks' powers of two from TMEM.  A stage is 256 columns of K:
-//   warps 0, 2, 3 TMA: 128 x 128 bytes of weights and their exponents (512 bytes for 128 rows by 128
-//                 columns, as they lie in memory); N x 128 bytes of tokens; the tokens' exponents
+//   warps 0, 2-4  TMA, a part of each stage by each: 128 x 128 bytes of weights; N x 128 bytes of
+//                 tokens; both sides' exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
 //   warp 1        tcgen05.cp of the exponents into TMEM, then four tcgen05.mma of 128 x N x 64 into
 //                 one of two accumulators
-//   warps 4-11    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
+//   warps 8-15    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
 //                 for 32 of them)
 // Beyond 128 tokens blocks pair up (PAIR): 256 vocabulary rows, 128 in each, by the same tokens, half of
 // their codes in each (tcgen05's cta_group::2; all of their exponents in both).  An SM takes in 64
@@ -179,7 +179,8 @@ constexpr int MAX_A = 12, MAX_B = 11;         // slots of the rings: weights, to
 constexpr int PARTS = 2, EPILOGUE = 4 * PARTS;  // warps for the same 32 vocabulary rows, of the epilogue in all
 constexpr int GROUPS = NT / 32 / PARTS;       // a warp's groups of 32 tokens
 constexpr int SMEM_OWN = 2048 + NT * 32;      // beside the rings: alignment, barriers, the epilogue's tokens
-constexpr int MMA_THREADS = 32 * (4 + EPILOGUE);
+constexpr int FIRST = 8;                      // of the epilogue's warps
+constexpr int MMA_THREADS = 32 * (FIRST + EPILOGUE);
 
 struct Plan {
     int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
 
     if (threadIdx.x == 0) {
         s_failed = 0;
-        for (int s = 0; s < p.n_a; s++) mbar_init(a_full(s), 1), mbar_init(a_empty(s), 1);
+        for (int s = 0; s < p.n_a; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
         for (int s = 0; s < p.n_b; s++) mbar_init(b_full(s), 2), mbar_init(b_empty(s), 1);
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * SIDES);
         mbar_init(drained, 1);
@@ -440,44 +441,48 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
         return PAIR ? (n + 31) / 32 * 32 : (n + 15) / 16 * 16;
     };
 
-    if (warp == 0 || warp == 2 || warp == 3) {
-        // Three threads load, each its part of every stage: one alone takes 950 cycles for a stage's copies.
-        if (lane == 0) {
-            const bool weights = warp == 0;
-            const int slots = weights ? p.n_a : p.n_b;
-            const int bytes = SIDES * (weights ? A_BYTES : warp == 2 ? p.b_codes : p.b_bytes - p.b_codes);
-            const int part = warp == 3 ? p.b_codes : 0;
-            auto full = [&](int s) { return weights ? a_full(s) : b_full(s); };
-            Place at;
-            int c = 0;
-            bool fresh = true;                        // the tile's weights are not there yet
-            for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && !*failed; item++) {
-                if (is_active(vt, nt) && (!weights || fresh || !p.stay)) {
-                    fresh = false;
-                    const int t0 = nt * p.N, x0 = t0 + side * (tokens_of(t0) / 2);
-                    for (int k = 0; k < n_k; k++, c++, at.next(slots)) {
-                        if (!mbar_wait(weights ? a_empty(at.s) : b_empty(at.s), at.parity ^ 1, failed)) break;
-                        const uint32_t to = (weights ? a_at(at.s) : b_at(at.s)) + part;
-                        const uint32_t own = full(at.s), bar = PAIR ? at_first(own) : own;
-                        if (!PAIR || side == 0) mbar_arrive_tx(own, bytes);
-                        if (weights) {
-                            load_tile<PAIR>(to, &w_map, k * 128, (vt * SIDES + side) * VT, bar);
-                            load_tile<PAIR>(to + A_CODES, &w_blocks_map, k * 256, vt * SIDES + side, bar);
-                        } else if (warp == 2) {
-                            load_tile<PAIR>(to, &x_map, k * 128, x0, bar);
-                        } else {
-                            load_tile<PAIR>(to, &x_blocks_map, k * 256, t0 / 128, bar);
-                        }
-                    }
+    // Loads one part of every stage: a box at (x, y), x + step, ... of a map into its place in the slots of
+    // a ring.  origin: (x, y) of a vocabulary tile and a tile of tokens; once: weights that stay.
+    auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
+                         uint32_t empty0, int bytes, bool once, auto row_of) {
+        const uint32_t there0 = PAIR ? at_first(full0) : full0;
+        const bool counts = !PAIR || side == 0;
+        Place at;
+        int c = 0;
+        bool fresh = true;                            // the tile's weights are not there yet
+        for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && !*failed; item++) {
+            if (is_active(vt, nt) && (fresh || !once)) {
+                fresh = false;
+                const int y = row_of(vt, nt);
+                int x = 0;
+                for (int k = 0; k < n_k; k++, x += step, at.next(slots)) {
+                    if (!mbar_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) break;
+                    if (counts) mbar_arrive_tx(full0 + 8 * at.s, bytes);
+                    load_tile<PAIR>(to0 + at.s * slot_bytes, map, x, y, there0 + 8 * at.s);
+                    c++;
                 }
-                if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
             }
-            // let the copies in flight land (of a pair, the first block sees both blocks', and the second
-            // does not end before it)
-            if (*failed && side == 0)
-                for (int i = max(0, c - slots); i < c; i++)
-                    for (int it = 0; it < (1 << 20) && !mbar_try(full(i % slots), (i / slots) & 1); it++) {}
+            if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
         }
+        // let the copies in flight land (of a pair, the first block sees both blocks', and the second does
+        // not end before it)
+        if (*failed && counts)
+            for (int i = max(0, c - slots); i < c; i++)
+                for (int it = 0; it < (1 << 20) && !mbar_try(full0 + 8 * (i % slots), (i / slots) & 1); it++) {}
+    };
+
+    if (warp == 0 && lane == 0) {
+        load_part(&w_map, 128, a_at(0), A_BYTES, p.n_a, a_full(0), a_empty(0), SIDES * A_CODES, p.stay,
+                  [&](int vt, int) { return (vt * SIDES + side) * VT; });
+    } else if (warp == 2 && lane == 0) {
+        load_part(&x_map, 128, b_at(0), p.b_bytes, p.n_b, b_full(0), b_empty(0), SIDES * p.b_codes, false,
+                  [&](int, int nt) { return nt * p.N + side * (tokens_of(nt * p.N) / 2); });
+    } else if (warp == 3 && lane == 0) {
+        load_part(&x_blocks_map, 256, b_at(0) + p.b_codes, p.b_bytes, p.n_b, b_full(0), b_empty(0),
+                  SIDES * (p.b_bytes - p.b_codes), false, [&](int, int nt) { return nt * p.N / 128; });
+    } else if (warp == 4 && lane == 0) {
+        load_part(&w_blocks_map, 256, a_at(0) + A_CODES, A_BYTES, p.n_a, a_full(0), a_empty(0), SIDES * 2 * SF, p.stay,
+                  [&](int vt, int) { return vt * SIDES + side; });
     } else if (warp == 1 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
         // issues (of a pair, for both blocks).
@@ -523,9 +528,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
             mma_commit<PAIR>(drained);
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
-    } else if (warp >= 4) {
-        const int quad = warp & 3, part = (warp - 4) >> 2;      // of every PARTS groups of 32 tokens, this warp's
-        Token* tokens = s_tokens[warp - 4];
+    } else if (warp >= FIRST) {
+        const int quad = warp & 3, part = (warp - FIRST) >> 2;      // of every PARTS groups of 32 tokens, this warp's
+        Token* tokens = s_tokens[warp - FIRST];
         Place acc;
         for (int item = begin, pt = begin / p.n_nt, nt = begin % p.n_nt; item < end; item++) {
             const bool active = is_active(pt, nt);
