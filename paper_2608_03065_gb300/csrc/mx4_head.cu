@@ -7,6 +7,8 @@
 
 namespace {
 
+const char* const ME = "psc_head_logits_mx4";
+
 constexpr int MAX_K = 131072;
 constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, rounded up to tiles, in 32 bits
 
@@ -155,72 +157,14 @@ psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
 
 // ------------------------------------------------------------ the tensor-core path
 //
-// k_mx4_mma: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by
-// up to 192 tokens (its N).  Both operands stay in 4 bits all the way; the tensor core takes their
-// blocks' powers of two from TMEM.  A stage is 256 columns of K:
-//   warps 0, 2-4  TMA, a part of each stage by each: 128 x 128 bytes of weights; N x 128 bytes of
-//                 tokens; both sides' exponents (512 bytes for 128 rows by 128 columns, as they lie in memory)
-//   warp 1        tcgen05.cp of the exponents into TMEM, then four tcgen05.mma of 128 x N x 64 into
-//                 one of two accumulators
-//   warps 8-15    the other accumulator: scales, mask, logits (a lane per vocabulary row, two warps
-//                 for 32 of them)
-// Beyond 128 tokens blocks pair up (PAIR): 256 vocabulary rows, 128 in each, by the same tokens, half of
-// their codes in each (tcgen05's cta_group::2; all of their exponents in both).  An SM takes in 64
-// bytes a cycle, and 192 tokens by 128 rows need 43 KB for a stage's 384 cycles of products; in a
-// pair it is 31 KB, and where a tile's weights fit shared memory (K up to 2048), they stay there
-// for all tiles of tokens (`stay`), which leaves 14 KB.
-constexpr int VT = 128;                       // vocabulary rows of a tile
-constexpr int NT = 192;                       // tokens of a tile at most; tiles start at multiples of 64
-constexpr int KS = 256;                       // columns of K of a stage (128 bytes of codes)
-constexpr int A_CODES = VT * KS / 2;
-constexpr int SF = 512;                       // a tile of exponents: 128 rows by 128 columns
-constexpr int A_BYTES = A_CODES + 2 * SF;
-constexpr int MAX_A = 12, MAX_B = 11;         // slots of the rings: weights, tokens
-constexpr int PARTS = 2, EPILOGUE = 4 * PARTS;  // warps for the same 32 vocabulary rows, of the epilogue in all
-constexpr int GROUPS = NT / 32 / PARTS;       // a warp's groups of 32 tokens
-constexpr int SMEM_OWN = 2048 + NT * 32;      // beside the rings: alignment, barriers, the epilogue's tokens
-constexpr int FIRST = 8;                      // of the epilogue's warps
+// Both operands stay in 4 bits all the way; the tensor core takes their blocks' powers of two from
+// TMEM.  A stage is 256 columns of K (128 bytes of codes a row): tcgen05.cp of its exponents, then four
+// tcgen05.mma of 64 columns each.  Threads load by TMA, each one part of every stage, into rings of
+// slots, and other warps take the other one of two accumulators to the logits meanwhile.
+constexpr int KS = 256;                       // columns of K of a stage
+constexpr int SF = 512;                       // a tile of exponents: 128 rows by 128 columns, as it lies in memory
+constexpr int EPILOGUE = 8, FIRST = 8;        // warps of the epilogue, the first of them
 constexpr int MMA_THREADS = 32 * (FIRST + EPILOGUE);
-
-struct Plan {
-    int N, n_nt, n_vt;                        // tokens per tile, tiles of tokens and of vocabulary rows
-    bool pair, stay;
-    int n_k;                                  // stages of K
-    int n_a, n_b, b_codes, b_bytes;           // slots of the rings, a slot's bytes of tokens (in a block)
-    int acc, sf_cols;                         // TMEM columns of an accumulator, of a stage's exponents
-    int items;                                // tiles (of pairs: two by two)
-    size_t smem;
-    int64_t flags_at, bytes;                  // in the workspace: the fault word, the tiles' flags
-};
-
-Plan plan_of(int T, int V, int K) {
-    Plan p;
-    p.n_nt = (T + NT - 1) / NT;
-    p.N = p.n_nt > 1 ? NT : (T + 15) / 16 * 16;
-    p.n_vt = (V + VT - 1) / VT;
-    p.pair = p.N > 128;
-    if (p.pair) p.N = (p.N + 31) / 32 * 32;
-    p.n_k = (K + KS - 1) / KS;
-    p.b_codes = (p.pair ? p.N / 2 : p.N) * KS / 2;
-    p.b_bytes = p.b_codes + 2 * SF * (p.pair ? 2 : 1);
-    p.acc = (p.N + 31) / 32 * 32;
-    p.sf_cols = p.pair ? 24 : 16;
-    // a stage's exponents have TMEM columns of their own, free when the tokens' slot is
-    const int room = SMEM_MAX - SMEM_OWN, most = std::min(MAX_B, (512 - 2 * p.acc) / p.sf_cols);
-    p.n_b = std::min(most, room / (A_BYTES + p.b_bytes));
-    p.n_a = p.n_b;
-    p.stay = p.n_nt > 1 && p.n_k <= MAX_A && p.n_k * A_BYTES + 4 * p.b_bytes <= room;
-    if (p.stay) {
-        p.n_b = std::min(most, (room - p.n_k * A_BYTES) / p.b_bytes);
-        p.n_a = std::min(MAX_A, (room - p.n_b * p.b_bytes) / A_BYTES);
-    }
-    const int64_t items = (int64_t)(p.pair ? (p.n_vt + 1) / 2 : p.n_vt) * p.n_nt;
-    p.items = (int)std::min<int64_t>(items, 0x7fffffff);
-    p.smem = 1024 + (size_t)p.n_a * A_BYTES + (size_t)p.n_b * p.b_bytes;
-    p.flags_at = 256;
-    p.bytes = p.flags_at + ((int64_t)p.n_vt * p.n_nt + 255) / 256 * 256;
-    return p;
-}
 
 // Descriptors by their low words (addresses in units of 16 bytes).  Exponents' tiles: 32 rows of 16
 // bytes, 8 rows every 128 bytes, no swizzle; operands: operand_desc's.
@@ -229,6 +173,10 @@ __device__ __forceinline__ uint64_t exponent_desc(uint32_t lo) {
 }
 __device__ __forceinline__ uint64_t codes_desc(uint32_t lo) {
     return (uint64_t)(64u | (1u << 14) | (2u << 29)) << 32 | (lo | (1u << 16));
+}
+// D f32; A and B of E2M1, both along K; exponents alone as scales; N and M.
+__device__ __forceinline__ uint32_t instruction(int m, int n) {
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24);
 }
 // 512 bytes to four TMEM columns, the same in all four quarters of the lanes (of both blocks of a pair,
 // from their own shared memory).
@@ -255,64 +203,103 @@ __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint
             "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
             : "memory");
 }
-// A tile into this block's shared memory; of a pair, the barrier is the first block's.
-template <bool PAIR>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if (PAIR)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    else
-        tma_2d(dst, map, x, y, bar);
-}
-// The address of the first block's barrier in the pair's shared memory.
-__device__ __forceinline__ uint32_t at_first(uint32_t bar) {
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
-    return r;
-}
-// A stage's copies and products: exponents of CHUNKS times 128 columns (those of the weights, then those
-// of the tokens, 128 or, of a pair, 256 rows), each of which two products of 64 columns use.  a, b: the
-// slots of both sides, ea, eb: their exponents, in units of 16 bytes; sf: the stage's TMEM columns;
-// shift: where the tile's tokens begin in theirs.
-template <bool PAIR, int CHUNKS>
-__device__ __forceinline__ void issue_stage(uint32_t a, uint32_t ea, uint32_t b, uint32_t eb, uint32_t sf,
-                                            uint32_t shift, uint32_t d, uint32_t idesc, uint32_t add) {
-    constexpr int B = PAIR ? 2 : 1;
+// A stage's exponents of CHUNKS times 128 columns to TMEM from column sf on: four columns each of side
+// A's 128 rows, then of side B's B_TILES times 128; a, b: where they are, in units of 16 bytes.
+template <bool PAIR, int B_TILES, int CHUNKS>
+__device__ __forceinline__ void copy_stage(uint32_t a, uint32_t b, uint32_t sf) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        copy_exponents<PAIR>(sf + 4 * c, ea + 32 * c);
+        copy_exponents<PAIR>(sf + 4 * c, a + 32 * c);
 #pragma unroll
-        for (int j = 0; j < B; j++) copy_exponents<PAIR>(sf + 8 + 4 * B * c + 4 * j, eb + 64 * j + 32 * c);
+        for (int j = 0; j < B_TILES; j++) copy_exponents<PAIR>(sf + 8 + 4 * B_TILES * c + 4 * j, b + 64 * j + 32 * c);
     }
+}
+// A stage's products; a, b: the operands' slots in units of 16 bytes; shift: where B's exponents begin.
+template <bool PAIR, int B_TILES, int CHUNKS>
+__device__ __forceinline__ void mma_stage(uint32_t a, uint32_t b, uint32_t sf, uint32_t shift, uint32_t d, uint32_t idesc,
+                                          uint32_t add) {
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++)
 #pragma unroll
         for (int i = 0; i < 2; i++)               // the first or the second two of a word's four exponents
             mma_mx4<PAIR>(d, codes_desc(a + 4 * c + 2 * i), codes_desc(b + 4 * c + 2 * i),
-                          idesc | (2u * i << 29) | (2u * i << 4), sf + 4 * c, sf + 8 + 4 * B * c + shift, add | c | i);
+                          idesc | (2u * i << 29) | (2u * i << 4), sf + 4 * c, sf + 8 + 4 * B_TILES * c + shift, add | c | i);
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_alloc(uint32_t* to) {
+    if (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(to)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(to)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_free(uint32_t tmem) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+// Lets the copies in flight land: those of the last `slots` of c uses of a ring.
+__device__ __forceinline__ void drain(uint32_t full0, int c, int slots) {
+    for (int i = max(0, c - slots); i < c; i++)
+        for (int it = 0; it < (1 << 20) && !mbar_try(full0 + 8 * (i % slots), (i / slots) & 1); it++) {}
+}
+
+// -------------------------------------------------------------------- up to 128 tokens
+//
+// k_mx4_few: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by all
+// tokens (its N): with few tokens the weights' bytes are all that counts, and tensor cores that give
+// most of their columns away keep up with them.
+//   warps 0, 2-4  TMA: the weights' codes (16 KB a stage), the tokens', both sides' exponents
+//   warp 1        the exponents' way to TMEM, the products
+//   warps 8-15    a lane per vocabulary row, two warps for 32 of them: scales, mask, logits
+constexpr int FEW = 128;                      // tokens at most
+constexpr int VT = 128;                       // vocabulary rows of a tile
+constexpr int W_CODES = VT * KS / 2;
+constexpr int MAX_STAGES = 11;
+constexpr int GROUPS = FEW / 32 / 2;          // a warp's groups of 32 tokens
+
+struct Few {
+    int N, n_vt;                              // tokens, rounded up; tiles of vocabulary rows
+    int stages, stage_bytes;
+    int acc;                                  // TMEM columns of an accumulator
+    size_t smem;
+    int64_t flags_at, bytes;                  // in the workspace: the fault word, the tiles' flags
+};
+
+Few few_of(int T, int V) {
+    Few p;
+    p.N = (T + 15) / 16 * 16;
+    p.n_vt = (V + VT - 1) / VT;
+    p.stage_bytes = W_CODES + p.N * KS / 2 + 4 * SF;
+    p.acc = (p.N + 31) / 32 * 32;
+    // a stage's exponents have TMEM columns of their own, free when the stage is
+    p.stages = std::min({MAX_STAGES, (SMEM_MAX - 6 * 1024) / p.stage_bytes, (512 - 2 * p.acc) / 16});
+    p.smem = 1024 + (size_t)p.stages * p.stage_bytes;
+    p.flags_at = 256;
+    p.bytes = p.flags_at + ((int64_t)p.n_vt + 255) / 256 * 256;
+    return p;
 }
 
 // How many rows of each tile some token allows, and the fault word.
-__global__ void __launch_bounds__(256) k_mx4_flags(Head h, int N, int n_vt, int n_nt, int* faults, uint8_t* flags) {
+__global__ void __launch_bounds__(256) k_mx4_flags(Head h, int n_vt, int* faults, uint8_t* flags) {
     dep_wait();
     dep_launch();
     if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    const int item = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (item >= n_vt * n_nt) return;
-    const int vt = item / n_nt, t0 = (item - vt * n_nt) * N, t1 = min(h.T, t0 + N);
+    const int vt = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (vt >= n_vt) return;
     uint32_t any = 0;
     // a lane per word of a token's four, eight tokens at a time
-    for (int t = t0 + (lane >> 2); t < t1; t += 8) {
+    for (int t = lane >> 2; t < h.T; t += 8) {
         const int wi = vt * 4 + (lane & 3);
         if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
     }
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) any |= __shfl_xor_sync(FULL, any, o);
     const int rows = __reduce_add_sync(FULL, lane < 4 ? __popc(any) : 0);
-    if (lane == 0) flags[item] = (uint8_t)rows;
+    if (lane == 0) flags[vt] = (uint8_t)rows;
 }
 
 // What the epilogue knows of a token: its scale, and the mask's word for the warp's 32 vocabulary rows.
@@ -366,187 +353,121 @@ __device__ __forceinline__ void store_group(T* out, int64_t stride, const uint32
     }
 }
 
-template <typename T, bool PAIR, bool MASKED>
-__global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constant__ CUtensorMap w_map,
+template <typename T, bool MASKED>
+__global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
                                                             const __grid_constant__ CUtensorMap w_blocks_map,
                                                             const __grid_constant__ CUtensorMap x_blocks_map, Head h,
-                                                            T* logits, Plan p, int* faults, const uint8_t* flags,
+                                                            T* logits, Few p, int* faults, const uint8_t* flags,
                                                             bool even) {
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * (MAX_A + MAX_B) + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * MAX_STAGES + 5];
     __shared__ __align__(16) Token s_tokens[EPILOGUE][GROUPS * 32];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int SIDES = PAIR ? 2 : 1;
-    const int side = PAIR ? (int)cluster_rank() : 0;
-    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u;
-    // slots start at multiples of 1024 bytes: codes, then exponents
-    auto a_at = [&](int s) { return base + s * A_BYTES; };
-    auto b_at = [&](int s) { return base + p.n_a * A_BYTES + s * p.b_bytes; };
+    // stages start at multiples of 1024 bytes: weights, tokens, the weights' exponents, the tokens'
+    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, x_codes = p.N * KS / 2;
     const uint32_t bars = smem_addr(s_bars);
-    auto a_full = [&](int s) { return bars + 8 * s; };
-    auto a_empty = [&](int s) { return bars + 8 * (MAX_A + s); };
-    auto b_full = [&](int s) { return bars + 8 * (2 * MAX_A + s); };
-    auto b_empty = [&](int s) { return bars + 8 * (2 * MAX_A + MAX_B + s); };
-    constexpr int LAST = 2 * (MAX_A + MAX_B);
-    auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
-    auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
-    const uint32_t drained = bars + 8 * (LAST + 4);
+    auto full = [&](int s) { return bars + 8 * s; };
+    auto empty = [&](int s) { return bars + 8 * (MAX_STAGES + s); };
+    auto acc_full = [&](int s) { return bars + 8 * (2 * MAX_STAGES + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_STAGES + 2 + s); };
+    const uint32_t drained = bars + 8 * (2 * MAX_STAGES + 4);
 
     if (threadIdx.x == 0) {
         s_failed = 0;
-        for (int s = 0; s < p.n_a; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
-        for (int s = 0; s < p.n_b; s++) mbar_init(b_full(s), 2), mbar_init(b_empty(s), 1);
-        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * SIDES);
+        for (int s = 0; s < p.stages; s++) mbar_init(full(s), 4), mbar_init(empty(s), 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE);
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (PAIR) cluster_sync();
-    if (warp == 1) {
-        if (PAIR) {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem))
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        }
-    }
+    if (warp == 1) tmem_alloc<false>(&s_tmem);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (PAIR) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
-    const int n_tiles = (h.K + 127) / 128, n_k = p.n_k;
+    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
     dep_wait();
     dep_launch();
     // A block that fails has polled for a good part of a second before it counts itself.
     if (!MASKED && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    // This block's (pair's) items, all tiles of tokens of a tile of vocabulary rows after each other.
-    const int me = blockIdx.x / SIDES, all = gridDim.x / SIDES;
-    const int begin = (int)((int64_t)p.items * me / all), end = (int)((int64_t)p.items * (me + 1) / all);
-    // whether an item (its vocabulary tile and tile of tokens) has an allowed token, in either block
-    auto is_active = [&](int vt, int nt) {
-        if (!MASKED) return true;
-        const int at = vt * SIDES * p.n_nt + nt;
-        return flags[at] != 0 || (PAIR && vt * 2 + 1 < p.n_vt && flags[at + p.n_nt] != 0);
-    };
-    // of a tile of tokens: how many the products take (both halves of a pair's in whole eights)
-    auto tokens_of = [&](int t0) {
-        const int n = min(p.N, h.T - t0);
-        return PAIR ? (n + 31) / 32 * 32 : (n + 15) / 16 * 16;
-    };
+    auto is_active = [&](int vt) { return !MASKED || flags[vt] != 0; };
 
-    // Loads one part of every stage: a box at (x, y), x + step, ... of a map into its place in the slots of
-    // a ring.  origin: (x, y) of a vocabulary tile and a tile of tokens; once: weights that stay.
-    auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
-                         uint32_t empty0, int bytes, bool once, auto row_of) {
-        const uint32_t there0 = PAIR ? at_first(full0) : full0;
-        const bool counts = !PAIR || side == 0;
+    // Loads one part of every stage: a box at (x, y), x + step, ... of a map; y_step: from tile to tile.
+    auto load_part = [&](const CUtensorMap* map, int step, int y_step, int part, int bytes) {
         Place at;
         int c = 0;
-        bool fresh = true;                            // the tile's weights are not there yet
-        for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && !*failed; item++) {
-            if (is_active(vt, nt) && (fresh || !once)) {
-                fresh = false;
-                const int y = row_of(vt, nt);
-                int x = 0;
-                for (int k = 0; k < n_k; k++, x += step, at.next(slots)) {
-                    if (!mbar_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) break;
-                    if (counts) mbar_arrive_tx(full0 + 8 * at.s, bytes);
-                    load_tile<PAIR>(to0 + at.s * slot_bytes, map, x, y, there0 + 8 * at.s);
-                    c++;
-                }
+        for (int vt = blockIdx.x; vt < p.n_vt && !*failed; vt += gridDim.x) {
+            if (!is_active(vt)) continue;
+            for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
+                if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
+                mbar_arrive_tx(full(at.s), bytes);
+                tma_2d(base + at.s * p.stage_bytes + part, map, k * step, vt * y_step, full(at.s));
             }
-            if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
         }
-        // let the copies in flight land (of a pair, the first block sees both blocks', and the second does
-        // not end before it)
-        if (*failed && counts)
-            for (int i = max(0, c - slots); i < c; i++)
-                for (int it = 0; it < (1 << 20) && !mbar_try(full0 + 8 * (i % slots), (i / slots) & 1); it++) {}
+        if (*failed) drain(full(0), c, p.stages);
     };
 
     if (warp == 0 && lane == 0) {
-        load_part(&w_map, 128, a_at(0), A_BYTES, p.n_a, a_full(0), a_empty(0), SIDES * A_CODES, p.stay,
-                  [&](int vt, int) { return (vt * SIDES + side) * VT; });
+        load_part(&w_map, 128, VT, 0, W_CODES);
     } else if (warp == 2 && lane == 0) {
-        load_part(&x_map, 128, b_at(0), p.b_bytes, p.n_b, b_full(0), b_empty(0), SIDES * p.b_codes, false,
-                  [&](int, int nt) { return nt * p.N + side * (tokens_of(nt * p.N) / 2); });
+        load_part(&x_map, 128, 0, W_CODES, x_codes);
     } else if (warp == 3 && lane == 0) {
-        load_part(&x_blocks_map, 256, b_at(0) + p.b_codes, p.b_bytes, p.n_b, b_full(0), b_empty(0),
-                  SIDES * (p.b_bytes - p.b_codes), false, [&](int, int nt) { return nt * p.N / 128; });
+        load_part(&w_blocks_map, 256, 1, W_CODES + x_codes, 2 * SF);
     } else if (warp == 4 && lane == 0) {
-        load_part(&w_blocks_map, 256, a_at(0) + A_CODES, A_BYTES, p.n_a, a_full(0), a_empty(0), SIDES * 2 * SF, p.stay,
-                  [&](int vt, int) { return vt * SIDES + side; });
-    } else if (warp == 1 && side == 0) {
-        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
-        // issues (of a pair, for both blocks).
+        load_part(&x_blocks_map, 256, 0, W_CODES + x_codes + 2 * SF, 2 * SF);
+    } else if (warp == 1) {
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
         const bool issuer = elect_one();
-        Place unit, at_b, acc;                        // unit: the first slot of the tile's weights
-        bool ok = true, fresh = true;
-        for (int item = begin, vt = begin / p.n_nt, nt = begin % p.n_nt; item < end && ok; item++) {
-            if (is_active(vt, nt)) {
-                // whether the weights have to be waited for, and whether nothing of them is used after this item
-                const bool first = fresh || !p.stay;
-                bool last = true;
-                if (p.stay)
-                    for (int i = item + 1, j = nt + 1; last && i < end && j < p.n_nt; i++, j++) last = !is_active(vt, j);
-                fresh = false;
-                const int t0 = nt * p.N;
-                // D f32; A and B of E2M1, both along K; exponents alone as scales; N and M
-                const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)(tokens_of(t0) >> 3) << 17) | (1u << 23) |
-                                       ((uint32_t)(VT * SIDES >> 4) << 24);
-                const uint32_t d = tmem + acc.s * p.acc, shift = t0 % 128 / 32;
-                if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
-                Place at_a = unit;
-                for (int k = 0; k < n_k; k++, at_a.next(p.n_a), at_b.next(p.n_b)) {
-                    const uint32_t a = (a_at(at_a.s) & 0x3FFFF) >> 4, b = (b_at(at_b.s) & 0x3FFFF) >> 4;
-                    const uint32_t ea = a + A_CODES / 16, eb = b + p.b_codes / 16, sf = tmem + 2 * p.acc + at_b.s * p.sf_cols;
-                    if (!(ok = first ? warp_wait2(a_full(at_a.s), at_a.parity, b_full(at_b.s), at_b.parity, failed)
-                                     : warp_wait(b_full(at_b.s), at_b.parity, failed)))
-                        break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (issuer) {
-                        if (2 * k + 2 <= n_tiles) issue_stage<PAIR, 2>(a, ea, b, eb, sf, shift, d, idesc, k);
-                        else issue_stage<PAIR, 1>(a, ea, b, eb, sf, shift, d, idesc, k);
-                        mma_commit<PAIR>(b_empty(at_b.s));
-                        if (last) mma_commit<PAIR>(a_empty(at_a.s));
-                        if (k + 1 == n_k) mma_commit<PAIR>(acc_full(acc.s));
+        const uint32_t lo = (base & 0x3FFFF) >> 4, step = p.stage_bytes / 16, idesc = instruction(VT, p.N);
+        Place at, acc;
+        bool ok = true;
+        for (int vt = blockIdx.x; vt < p.n_vt && ok; vt += gridDim.x) {
+            if (!is_active(vt)) continue;
+            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+            const uint32_t d = tmem + acc.s * p.acc;
+            for (int k = 0; k < n_k; k++, at.next(p.stages)) {
+                const uint32_t a = lo + at.s * step, b = a + W_CODES / 16, e = b + x_codes / 16;
+                const uint32_t sf = tmem + 2 * p.acc + at.s * 16;
+                if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issuer) {
+                    if (2 * k + 2 <= n_tiles) {
+                        copy_stage<false, 1, 2>(e, e + 64, sf);
+                        mma_stage<false, 1, 2>(a, b, sf, 0, d, idesc, k);
+                    } else {
+                        copy_stage<false, 1, 1>(e, e + 64, sf);
+                        mma_stage<false, 1, 1>(a, b, sf, 0, d, idesc, k);
                     }
+                    mma_commit<false>(empty(at.s));
+                    if (k + 1 == n_k) mma_commit<false>(acc_full(acc.s));
                 }
-                if (last) unit = at_a;
-                acc.next(2);
             }
-            if (++nt == p.n_nt) nt = 0, vt++, fresh = true;
+            acc.next(2);
         }
         if (!ok && issuer) {                          // let the products in flight finish
-            mma_commit<PAIR>(drained);
+            mma_commit<false>(drained);
             for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= FIRST) {
-        const int quad = warp & 3, part = (warp - FIRST) >> 2;      // of every PARTS groups of 32 tokens, this warp's
+        const int quad = warp & 3, part = (warp - FIRST) >> 2;      // of every two groups of 32 tokens, this warp's
         Token* tokens = s_tokens[warp - FIRST];
         Place acc;
-        for (int item = begin, pt = begin / p.n_nt, nt = begin % p.n_nt; item < end; item++) {
-            const bool active = is_active(pt, nt);
-            const int vt = pt * SIDES + side, t0 = nt * p.N, n = min(p.N, h.T - t0);
+        for (int vt = blockIdx.x; vt < p.n_vt; vt += gridDim.x) {
+            const bool active = is_active(vt);
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
-            if (++nt == p.n_nt) nt = 0, pt++;
             // the tile's scales and mask words, read while its products run
             const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < GROUPS; i++) {
-                const int t = (PARTS * i + part) * 32 + lane;
-                if (t >= n) continue;
+                const int t = (2 * i + part) * 32 + lane;
+                if (t >= h.T) continue;
                 tokens[i * 32 + lane] = {
-                    h.scale ? h.scale[t0 + t] : 1.f,
-                    !MASKED ? FULL : active && wi < h.W ? h.bitmask[(size_t)(t0 + t) * h.W + wi] : 0u};
+                    h.scale ? h.scale[t] : 1.f,
+                    !MASKED ? FULL : active && wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u};
             }
             __syncwarp();
             if (active) {
@@ -555,25 +476,22 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
             }
 #pragma unroll 1
             for (int i = 0; i < GROUPS; i++) {
-                const int g = PARTS * i + part;
-                if (g * 32 >= n) break;
+                const int t = (2 * i + part) * 32;
+                if (t >= h.T) break;
                 uint32_t y[32] = {};
                 if (active) {
-                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + g * 32;
+                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + t;
                     tmem_load16(from, y);
                     tmem_load16(from + 16, y + 16);
                     tmem_wait(y);
                 }
-                store_group<MASKED>(logits + (size_t)(t0 + g * 32) * h.row_stride + v, h.row_stride, y, tokens + i * 32,
-                                    sw, min(32, n - g * 32), h.V - v, even);
+                store_group<MASKED>(logits + (size_t)t * h.row_stride + v, h.row_stride, y, tokens + i * 32, sw,
+                                    min(32, h.T - t), h.V - v, even);
             }
             if (active) {
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) arrive_at_first(acc_empty(acc.s));
-                    else mbar_arrive(acc_empty(acc.s));
-                }
+                if (lane == 0) mbar_arrive(acc_empty(acc.s));
                 acc.next(2);
             }
         }
@@ -581,50 +499,376 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_mma(const __grid_constan
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (PAIR) cluster_sync();                         // nothing of this block is used by the other any more
-    if (warp == 1) {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-    }
+    if (warp == 1) tmem_free<false>(tmem);
     if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
 }
 
 template <typename T>
-psc_status head_mma(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
-    const char* me = "psc_head_logits_mx4";
-    const Plan p = plan_of(h.T, h.V, h.K);
+psc_status head_few(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    const Few p = few_of(h.T, h.V);
     int* faults = (int*)work;
     uint8_t* flags = work + p.flags_at;
-    CUtensorMap w_map, x_map;
-    CUtensorMap w_blocks_map, x_blocks_map;
+    CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
     const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, VT) ||
-        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128,
-                    p.pair ? p.N / 2 : p.N) ||
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, p.N) ||
         !tensor_map(&w_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.w_blocks, n_tiles * SF / 4, p.n_vt, n_tiles * SF,
                     256, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
-        !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, (h.T + 127) / 128,
-                    n_tiles * SF, 256, p.pair ? 2 : 1, CU_TENSOR_MAP_SWIZZLE_NONE))
-        return ops_fail(PSC_ERR_CUDA, me, "cuTensorMapEncodeTiled failed");
-    const int items = p.n_vt * p.n_nt;
+        !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, 1, n_tiles * SF, 256, 1,
+                    CU_TENSOR_MAP_SWIZZLE_NONE))
+        return ops_fail(PSC_ERR_CUDA, ME, "cuTensorMapEncodeTiled failed");
     if (h.bitmask) {
-        psc_status s = ops_launch(k_mx4_flags, dim3((items + 7) / 8), 256, 0, 1, cs, "k_mx4_flags", h, p.N, p.n_vt,
-                                  p.n_nt, faults, flags);
+        psc_status s = ops_launch(k_mx4_flags, dim3((p.n_vt + 7) / 8), 256, 0, 1, cs, "k_mx4_flags", h, p.n_vt, faults,
+                                  flags);
         if (s != PSC_OK) return s;
     }
-    auto kernel = h.bitmask ? (p.pair ? k_mx4_mma<T, true, true> : k_mx4_mma<T, false, true>)
-                            : (p.pair ? k_mx4_mma<T, true, false> : k_mx4_mma<T, false, false>);
     const bool even = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 4);
-    const int sides = p.pair ? 2 : 1;
-    return ops_launch(kernel, dim3(std::min(p.items, current_sms() / sides) * sides), MMA_THREADS, p.smem, sides, cs,
-                      "k_mx4_mma", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p, faults,
-                      (const uint8_t*)flags, even);
+    return ops_launch(h.bitmask ? k_mx4_few<T, true> : k_mx4_few<T, false>, dim3(std::min(p.n_vt, current_sms())),
+                      MMA_THREADS, p.smem, 1, cs, "k_mx4_few", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p,
+                      faults, (const uint8_t*)flags, even);
+}
+
+// ------------------------------------------------------------------------ many tokens
+//
+// k_mx4_many: pairs of blocks (tcgen05's cta_group::2) over tiles of 256 tokens (the tensor core's M, 128
+// in each block) by 192 vocabulary rows (its N; half of their codes in each block, all of their
+// exponents in both).  Where a tile's tokens fit shared memory (K up to 2048) they stay there, and
+// only the weights are loaded, from memory once and from the L2 for the other tiles of tokens: an SM
+// takes in 64 bytes a cycle, and a stage's 384 cycles of products need 14 KB this way, 31 KB where
+// the tokens come along.  A lane of the epilogue has a token, and 32 neighbouring logits of it with one
+// word of the mask; they go out by way of shared memory, 64 bytes of a token at a time.
+//   warps 0, 2-4  TMA: the weights' codes and exponents, the tokens' codes and exponents
+//   warp 5        the exponents' way to TMEM
+//   warp 1        the products
+//   warps 8-15    32 tokens by 96 vocabulary rows each
+constexpr int MT = 256;                       // tokens of a tile
+constexpr int NV = 192;                       // vocabulary rows of a tile
+constexpr int TOGETHER = 4;                   // tiles of tokens that are worked on at the same time
+constexpr int A_CODES = MT / 2 * KS / 2, A_BYTES = A_CODES + 2 * SF;
+constexpr int B_CODES = NV / 2 * KS / 2, B_BYTES = B_CODES + 4 * SF;
+constexpr int A_SLOTS = 8, B_SLOTS = 5;
+constexpr int SF_COLS = 24;                   // TMEM columns of a stage's exponents
+static_assert(2 * NV + B_SLOTS * SF_COLS <= 512, "TMEM");
+constexpr int STAGING = 32 * 64;              // a warp's, in the epilogue
+constexpr size_t MANY_SMEM = 1024 + A_SLOTS * A_BYTES + B_SLOTS * B_BYTES + EPILOGUE * STAGING;
+
+// A tile into this block's shared memory; the barrier is the pair's first block's.
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+// The address of the first block's barrier in the pair's shared memory.
+__device__ __forceinline__ uint32_t at_first(uint32_t bar) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+// Arrives at this block's barrier when the pair's copies and products so far are done.
+__device__ __forceinline__ void commit_here(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Two products at once.
+__device__ __forceinline__ void times2(uint32_t& a, uint32_t& b, float x, float y) {
+    asm("{\n .reg .b64 u, v;\n mov.b64 u, {%0, %1};\n mov.b64 v, {%2, %3};\n mul.rn.f32x2 u, u, v;\n"
+        " mov.b64 {%0, %1}, u;\n}"
+        : "+r"(a), "+r"(b)
+        : "f"(x), "f"(y));
+}
+
+template <typename T, bool MASKED>
+__global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_constant__ CUtensorMap w_map,
+                                                             const __grid_constant__ CUtensorMap x_map,
+                                                             const __grid_constant__ CUtensorMap w_blocks_map,
+                                                             const __grid_constant__ CUtensorMap x_blocks_map, Head h,
+                                                             T* logits, int n_mt, int n_vt, int* faults, bool wide) {
+    extern __shared__ uint8_t dyn[];
+    __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 3 * B_SLOTS + 5];
+    __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int side = (int)cluster_rank();
+    // slots start at multiples of 1024 bytes: codes, then exponents
+    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, b_base = base + A_SLOTS * A_BYTES;
+    const uint32_t bars = smem_addr(s_bars);
+    auto a_full = [&](int s) { return bars + 8 * s; };
+    auto a_empty = [&](int s) { return bars + 8 * (A_SLOTS + s); };
+    auto b_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + s); };
+    auto b_empty = [&](int s) { return bars + 8 * (2 * A_SLOTS + B_SLOTS + s); };
+    auto sf_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 2 * B_SLOTS + s); };
+    constexpr int LAST = 2 * A_SLOTS + 3 * B_SLOTS;
+    auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
+    auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
+    const uint32_t drained = bars + 8 * (LAST + 4);
+
+    if (threadIdx.x == 0) {
+        s_failed = 0;
+        for (int s = 0; s < A_SLOTS; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
+        for (int s = 0; s < B_SLOTS; s++) mbar_init(b_full(s), 2), mbar_init(b_empty(s), 1), mbar_init(sf_full(s), 1);
+        for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * 2);
+        mbar_init(drained, 2);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_sync();
+    if (warp == 1) tmem_alloc<true>(&s_tmem);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    volatile int* failed = &s_failed;
+    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
+    const bool stay = n_k <= A_SLOTS;
+    const int a_slots = stay ? n_k : B_SLOTS;
+    dep_wait();
+    dep_launch();
+    // A block that fails has polled for a good part of a second before it counts itself.
+    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
+    // This pair's items, in order: up to TOGETHER tiles of tokens at a time, a pair staying with one of
+    // them; pairs that share a tile of vocabulary rows come to it at the same time.  f(tile of tokens, of
+    // vocabulary rows, whether its tokens are new, whether they are not used after it) says whether to go on.
+    const int me = blockIdx.x / 2, all = gridDim.x / 2;
+    auto each = [&](auto f) {
+        for (int m0 = 0; m0 < n_mt; m0 += TOGETHER) {
+            const int c = min(min(TOGETHER, n_mt - m0), all), per = all / c, g = me / c;
+            if (g >= per) continue;
+            for (int m = m0 + me % c; m < min(m0 + TOGETHER, n_mt); m += c)
+                for (int vt = g; vt < n_vt; vt += per)
+                    if (!f(m, vt, vt == g || !stay, vt + per >= n_vt || !stay)) return;
+        }
+    };
+    // vocabulary rows of a tile that the products take: both halves in whole sixteens
+    auto rows_of = [&](int vt) { return (min(NV, h.V - vt * NV) + 31) / 32 * 32; };
+
+    // Loads one part of every stage of the items for which `when` holds.
+    auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
+                         uint32_t empty0, int bytes, bool tokens, auto row_of) {
+        const uint32_t there0 = at_first(full0);
+        Place at;
+        int c = 0;
+        each([&](int mt, int vt, bool fresh, bool) {
+            if (tokens && !fresh) return true;
+            const int y = row_of(mt, vt);
+            int x = 0;
+            for (int k = 0; k < n_k; k++, c++, x += step, at.next(slots)) {
+                if (!mbar_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) return false;
+                if (side == 0) mbar_arrive_tx(full0 + 8 * at.s, 2 * bytes);
+                load_tile(to0 + at.s * slot_bytes, map, x, y, there0 + 8 * at.s);
+            }
+            return !*failed;
+        });
+        // the first block sees both blocks' copies land, and the second does not end before it
+        if (*failed && side == 0) drain(full0, c, slots);
+    };
+
+    if (warp == 0 && lane == 0) {
+        load_part(&w_map, 128, b_base, B_BYTES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false,
+                  [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); });
+    } else if (warp == 2 && lane == 0) {
+        load_part(&w_blocks_map, 256, b_base + B_CODES, B_BYTES, B_SLOTS, b_full(0), b_empty(0), 4 * SF, false,
+                  [&](int, int vt) { return vt * NV / 128; });
+    } else if (warp == 3 && lane == 0) {
+        load_part(&x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
+                  [&](int mt, int) { return mt * MT + side * (MT / 2); });
+    } else if (warp == 4 && lane == 0) {
+        load_part(&x_blocks_map, 256, base + A_CODES, A_BYTES, a_slots, a_full(0), a_empty(0), 2 * SF, true,
+                  [&](int mt, int) { return mt * 2 + side; });
+    } else if (warp == 5 && side == 0) {
+        // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
+        // issues, for both blocks.
+        const bool issuer = elect_one();
+        const uint32_t a_lo = ((base + A_CODES) & 0x3FFFF) >> 4, b_lo = ((b_base + B_CODES) & 0x3FFFF) >> 4;
+        Place unit, at_b;                             // unit: the first slot of the tile's tokens
+        each([&](int, int, bool fresh, bool last) {
+            Place at_a = unit;
+            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(B_SLOTS)) {
+                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_BYTES / 16);
+                const uint32_t sf = tmem + 2 * NV + at_b.s * SF_COLS;
+                if (!(fresh ? warp_wait2(a_full(at_a.s), at_a.parity, b_full(at_b.s), at_b.parity, failed)
+                            : warp_wait(b_full(at_b.s), at_b.parity, failed)))
+                    return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issuer) {
+                    if (2 * k + 2 <= n_tiles) copy_stage<true, 2, 2>(a, b, sf);
+                    else copy_stage<true, 2, 1>(a, b, sf);
+                    commit_here(sf_full(at_b.s));
+                }
+            }
+            if (last) unit = at_a;
+            return true;
+        });
+    } else if (warp == 1 && side == 0) {
+        const bool issuer = elect_one();
+        const uint32_t a_lo = (base & 0x3FFFF) >> 4, b_lo = (b_base & 0x3FFFF) >> 4;
+        Place unit, at_b, acc;
+        bool ok = true;
+        each([&](int, int vt, bool, bool last) {
+            const uint32_t idesc = instruction(MT, rows_of(vt)), d = tmem + acc.s * NV, shift = vt * NV % 128 / 32;
+            Place at_a = unit;
+            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) return false;
+            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(B_SLOTS)) {
+                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_BYTES / 16);
+                const uint32_t sf = tmem + 2 * NV + at_b.s * SF_COLS;
+                // exponents that are in TMEM came with the codes, in both blocks
+                if (!(ok = warp_wait(sf_full(at_b.s), at_b.parity, failed))) return false;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (issuer) {
+                    if (2 * k + 2 <= n_tiles) mma_stage<true, 2, 2>(a, b, sf, shift, d, idesc, k);
+                    else mma_stage<true, 2, 1>(a, b, sf, shift, d, idesc, k);
+                    mma_commit<true>(b_empty(at_b.s));
+                    if (last) mma_commit<true>(a_empty(at_a.s));
+                    if (k + 1 == n_k) mma_commit<true>(acc_full(acc.s));
+                }
+            }
+            if (last) unit = at_a;
+            acc.next(2);
+            return true;
+        });
+        if (!ok && issuer) {                          // let the products in flight finish
+            mma_commit<true>(drained);
+            mma_commit<true>(drained);
+            for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
+        }
+    } else if (warp >= FIRST) {
+        constexpr int COLS = 64 / sizeof(T);          // logits of a token that go out together
+        const int quad = warp & 3, part = (warp - FIRST) >> 2;
+        const uint32_t staging = b_base + B_SLOTS * B_BYTES + (warp - FIRST) * STAGING;
+        const uint32_t own = staging + lane * 64, own_swap = (lane >> 1) & 3;       // 16-byte pieces change places by rows
+        float* scales = s_scale[warp - FIRST];
+        Place acc;
+        each([&](int mt, int vt, bool, bool) {
+            const int t0 = mt * MT + side * (MT / 2) + quad * 32, t = t0 + lane;
+            const int v0 = vt * NV + part * (NV / 2);
+            // scales and mask words, read while the products run
+            const float st = t < h.T && h.scale ? h.scale[t] : 1.f;
+            uint32_t words[3];
+#pragma unroll
+            for (int i = 0; i < 3; i++) {
+                const int wi = v0 / 32 + i;
+                words[i] = !MASKED ? FULL : t < h.T && wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u;
+            }
+            if (h.w_scale) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 3; i++)
+                    if (v0 + i * 32 + lane < h.V) scales[i * 32 + lane] = h.w_scale[v0 + i * 32 + lane];
+                __syncwarp();
+            }
+            if (!warp_wait(acc_full(acc.s), acc.parity, failed)) return false;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            T* rows = logits + (size_t)(t0 + (lane >> 2)) * h.row_stride + v0 + (lane & 3) * (COLS / 4);
+#pragma unroll
+            for (int i = 0; i < 3; i++) {
+                const int n = min(32, h.V - v0 - i * 32);             // vocabulary rows that there are
+                uint32_t y[32];
+                if (t0 < h.T && n > 0) {
+                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * NV + part * (NV / 2) + i * 32;
+                    tmem_load16(from, y);
+                    tmem_load16(from + 16, y + 16);
+                    tmem_wait(y);
+                }
+                if (i == 2) {                         // the accumulator is free
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_at_first(acc_empty(acc.s));
+                }
+                if (t0 >= h.T || n <= 0) continue;
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) times2(y[j], y[j + 1], st, st);
+                if (h.w_scale) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 s = *reinterpret_cast<const float4*>(scales + i * 32 + j);
+                        times2(y[j], y[j + 1], s.x, s.y);
+                        times2(y[j + 2], y[j + 3], s.z, s.w);
+                    }
+                }
+                if (MASKED) {
+#pragma unroll
+                    for (int j = 0; j < 32; j++)
+                        if (!((words[i] >> j) & 1)) y[j] = 0xFF800000u;
+                }
+#pragma unroll
+                for (int half = 0; half < (int)sizeof(T) / 2; half++) {       // 64 bytes a token
+                    uint32_t u[16];
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        u[j] = sizeof(T) == 2 ? pack_bf16(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1]))
+                                              : y[half * 16 + j];
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(own + ((j ^ own_swap) << 4)),
+                                     "r"(u[4 * j]), "r"(u[4 * j + 1]), "r"(u[4 * j + 2]), "r"(u[4 * j + 3])
+                                     : "memory");
+                    __syncwarp();
+                    const int c0 = i * 32 + half * 16;
+                    if (wide && n == 32) {            // four lanes a token, eight tokens at a time
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const int r = j * 8 + (lane >> 2);
+                            uint4 x;
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                         : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                                         : "r"(staging + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)));
+                            if (t0 + r < h.T) *reinterpret_cast<uint4*>(rows + (size_t)(j * 8) * h.row_stride + c0) = x;
+                        }
+                    } else {                          // a lane a logit
+                        for (int r = 0; r < 32 && t0 + r < h.T; r++) {
+                            const uint32_t at = staging + r * 64 + (((lane * 4 / COLS) ^ ((r >> 1) & 3)) << 4) +
+                                                (lane % (COLS / 4)) * (int)sizeof(T);
+                            if (lane < COLS && half * 16 + lane < n) {
+                                T* out = logits + (size_t)(t0 + r) * h.row_stride + v0 + c0 + lane;
+                                if (sizeof(T) == 2) {
+                                    uint16_t x;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at));
+                                    *reinterpret_cast<uint16_t*>(out) = x;
+                                } else {
+                                    uint32_t x;
+                                    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at));
+                                    *reinterpret_cast<uint32_t*>(out) = x;
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+            acc.next(2);
+            return true;
+        });
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();                                   // nothing of this block is used by the other any more
+    if (warp == 1) tmem_free<true>(tmem);
+    if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
+}
+
+template <typename T>
+psc_status head_many(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+    CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
+    const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
+    if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, NV / 2) ||
+        !tensor_map(&x_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.q, row, h.T, h.q_stride, 128, MT / 2) ||
+        !tensor_map(&w_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.w_blocks, n_tiles * SF / 4, (h.V + 127) / 128,
+                    n_tiles * SF, 256, 2, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, (h.T + 127) / 128,
+                    n_tiles * SF, 256, 1, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return ops_fail(PSC_ERR_CUDA, ME, "cuTensorMapEncodeTiled failed");
+    const int n_mt = (h.T + MT - 1) / MT, n_vt = (h.V + NV - 1) / NV;
+    const bool wide = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 16);
+    const int pairs = (int)std::min<int64_t>((int64_t)n_mt * n_vt, std::max(1, current_sms() / 2));
+    return ops_launch(h.bitmask ? k_mx4_many<T, true> : k_mx4_many<T, false>, dim3(2 * pairs), MMA_THREADS, MANY_SMEM, 2,
+                      cs, "k_mx4_many", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, n_mt, n_vt, (int*)work, wide);
 }
 
 template <typename T>
 psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
-    return head_mma(h, logits, work, cs);
+    return h.T <= FEW ? head_few(h, logits, work, cs) : head_many(h, logits, work, cs);
 }
 
 }  // namespace
@@ -632,26 +876,24 @@ psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
 extern "C" {
 
 int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K) {
-    if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K) return 256;
-    return plan_of(T, V, K).bytes;
+    if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K || T > FEW) return 256;
+    return few_of(T, V).bytes;
 }
 
 psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
                                int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                                const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
                                psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes, void* stream) {
-    const char* me = "psc_head_logits_mx4";
     if (T < 0 || V <= 0 || K <= 0 || row_stride < V || !is_dtype(dtype) || !d_w || !d_w_blocks ||
         (T && (!d_q || !d_q_blocks || !d_logits)))
-        return ops_fail(PSC_ERR_ARG, me, "bad arguments");
-    if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 131,072");
-    if (T > MAX_T || V > MAX_V || (int64_t)((T + NT - 1) / NT) * ((V + VT - 1) / VT) > 0x7fffffff)
-        return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
+        return ops_fail(PSC_ERR_ARG, ME, "bad arguments");
+    if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, ME, "K over 131,072");
+    if (T > MAX_T || V > MAX_V) return ops_fail(PSC_ERR_LIMIT, ME, "too many rows");
     if (!is_mx4(d_w, w_stride, d_w_blocks, K) || (T && !is_mx4(d_q, q_stride, d_q_blocks, K)))
-        return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+        return ops_fail(PSC_ERR_ARG, ME, "codes or blocks with a bad stride or alignment");
     if (T == 0) return PSC_OK;
     if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_mx4_work_bytes(T, V, K))
-        return ops_fail(PSC_ERR_ARG, me, "workspace missing, unaligned or too small");
+        return ops_fail(PSC_ERR_ARG, ME, "workspace missing, unaligned or too small");
     const Head h{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
                  (V + 31) / 32, row_stride};
     if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
