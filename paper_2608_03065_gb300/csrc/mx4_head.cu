@@ -203,23 +203,24 @@ __device__ __forceinline__ void mma_mx4(uint32_t d, uint64_t a, uint64_t b, uint
             "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(add)
             : "memory");
 }
-// A stage's exponents of CHUNKS times 128 columns to TMEM from column sf on: four columns each of side
-// A's 128 rows, then of side B's B_TILES times 128; a, b: where they are, in units of 16 bytes.
-template <bool PAIR, int B_TILES, int CHUNKS>
+// A stage's exponents (two tiles a row) to TMEM from column sf on: four columns each of side A's 128
+// rows, then of side B's B_TILES times 128; a, b: where they are, in units of 16 bytes.
+template <bool PAIR, int B_TILES>
 __device__ __forceinline__ void copy_stage(uint32_t a, uint32_t b, uint32_t sf) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; c++) {
+    for (int c = 0; c < 2; c++) {
         copy_exponents<PAIR>(sf + 4 * c, a + 32 * c);
 #pragma unroll
         for (int j = 0; j < B_TILES; j++) copy_exponents<PAIR>(sf + 8 + 4 * B_TILES * c + 4 * j, b + 64 * j + 32 * c);
     }
 }
 // A stage's products; a, b: the operands' slots in units of 16 bytes; shift: where B's exponents begin.
-template <bool PAIR, int B_TILES, int CHUNKS>
+// Past K codes and exponents are zeros, as the TMA fills them in.
+template <bool PAIR, int B_TILES>
 __device__ __forceinline__ void mma_stage(uint32_t a, uint32_t b, uint32_t sf, uint32_t shift, uint32_t d, uint32_t idesc,
                                           uint32_t add) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; c++)
+    for (int c = 0; c < 2; c++)
 #pragma unroll
         for (int i = 0; i < 2; i++)               // the first or the second two of a word's four exponents
             mma_mx4<PAIR>(d, codes_desc(a + 4 * c + 2 * i), codes_desc(b + 4 * c + 2 * i),
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
-    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
+    const int n_k = (h.K + KS - 1) / KS;
     dep_wait();
     dep_launch();
     // A block that fails has polled for a good part of a second before it counts itself.
@@ -434,13 +435,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
                 if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
-                    if (2 * k + 2 <= n_tiles) {
-                        copy_stage<false, 1, 2>(e, e + 64, sf);
-                        mma_stage<false, 1, 2>(a, b, sf, 0, d, idesc, k);
-                    } else {
-                        copy_stage<false, 1, 1>(e, e + 64, sf);
-                        mma_stage<false, 1, 1>(a, b, sf, 0, d, idesc, k);
-                    }
+                    copy_stage<false, 1>(e, e + 64, sf);
+                    mma_stage<false, 1>(a, b, sf, 0, d, idesc, k);
                     mma_commit<false>(empty(at.s));
                     if (k + 1 == n_k) mma_commit<false>(acc_full(acc.s));
                 }
@@ -620,7 +616,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
-    const int n_tiles = (h.K + 127) / 128, n_k = (n_tiles + 1) / 2;
+    const int n_k = (h.K + KS - 1) / KS;
     const bool stay = n_k <= A_SLOTS;
     const int a_slots = stay ? n_k : B_SLOTS;
     dep_wait();
@@ -692,8 +688,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
-                    if (2 * k + 2 <= n_tiles) copy_stage<true, 2, 2>(a, b, sf);
-                    else copy_stage<true, 2, 1>(a, b, sf);
+                    copy_stage<true, 2>(a, b, sf);
                     commit_here(sf_full(at_b.s));
                 }
             }
@@ -716,8 +711,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                 if (!(ok = warp_wait(sf_full(at_b.s), at_b.parity, failed))) return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
-                    if (2 * k + 2 <= n_tiles) mma_stage<true, 2, 2>(a, b, sf, shift, d, idesc, k);
-                    else mma_stage<true, 2, 1>(a, b, sf, shift, d, idesc, k);
+                    mma_stage<true, 2>(a, b, sf, shift, d, idesc, k);
                     mma_commit<true>(b_empty(at_b.s));
                     if (last) mma_commit<true>(a_empty(at_a.s));
                     if (k + 1 == n_k) mma_commit<true>(acc_full(acc.s));
