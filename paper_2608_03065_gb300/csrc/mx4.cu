@@ -7,48 +7,116 @@
 
 namespace {
 
-// Sixteen lanes per tile of a row (128 columns).
-template <typename T>
-__global__ void __launch_bounds__(256) k_quantize_mx4(const T* x, int64_t stride, int64_t items, int n_tiles, int K,
-                                                      uint8_t* q, int64_t q_stride, uint8_t* blocks, bool wide) {
+constexpr int AT_ONCE = 2;              // pieces that a thread has under way
+
+// Both ways a thread has eight neighbouring columns.  I: what counts a matrix's pieces.
+template <typename T, bool WIDE, typename I>
+__global__ void __launch_bounds__(256) k_quantize_mx4(const T* x, int64_t stride, I items, int n_tiles, int K, uint8_t* q,
+                                                      int64_t q_stride, uint8_t* blocks) {
     dep_wait();
     dep_launch();
-    // whole warps go round together: their lanes share blocks and tiles
-    for (int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i < (items + 1) / 2 * 2; i += (int64_t)gridDim.x * 16) {
-        const int row = (int)(i / n_tiles), tile = (int)(i - (int64_t)row * n_tiles);
-        const int c = tile * 16 + (threadIdx.x & 15);
-        float v[8] = {};
-        const bool there = i < items;
-        if (there && c * 8 < K) load8(x + (size_t)row * stride, c * 8, K, wide, v);
-        quantize8(v, c, there ? K : 0, row, q + (size_t)row * q_stride, blocks);
+    // sixteen lanes a tile of a row; whole warps go round together, as their lanes share blocks and tiles
+    const I step = (I)gridDim.x * 16, end = (items + 1) / 2 * 2;
+    for (I i0 = (I)blockIdx.x * 16 + (threadIdx.x >> 4); i0 < end; i0 += step * AT_ONCE) {
+        float v[AT_ONCE][8];
+        int row[AT_ONCE], c[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; j++) {
+            const I i = i0 + j * step;
+            row[j] = (int)(i / (I)n_tiles), c[j] = (int)(i - (I)row[j] * n_tiles) * 16 + (threadIdx.x & 15);
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[j][e] = 0.f;
+            if (i < items && c[j] * 8 < K) load8<WIDE>(x + (size_t)row[j] * stride, c[j] * 8, K, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; j++)
+            if (i0 + j * step < end)            // of both of the warp's tiles
+                quantize8(v[j], c[j], i0 + j * step < items ? K : 0, row[j], q + (size_t)row[j] * q_stride, blocks);
     }
 }
 
-template <typename T>
+// The values of a byte's two codes.
+__device__ __forceinline__ float2 values2(uint32_t codes) {
+    uint32_t pair;
+    asm("{\n .reg .b8 a, b;\n .reg .b16 h;\n cvt.u16.u32 h, %1;\n mov.b16 {a, b}, h;\n cvt.rn.f16x2.e2m1x2 %0, a;\n}"
+        : "=r"(pair)
+        : "r"(codes));
+    return __half22float2(*reinterpret_cast<const __half2*>(&pair));
+}
+
+template <typename T, bool WIDE, typename I>
 __global__ void __launch_bounds__(256) k_dequantize_mx4(const uint8_t* q, int64_t q_stride, const uint8_t* blocks,
-                                                        const float* scale, int64_t items, int chunks, int K, T* y,
-                                                        int64_t stride, bool wide) {
+                                                        const float* scale, I items, int chunks, int K, T* y,
+                                                        int64_t stride) {
     dep_wait();
     dep_launch();
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
-        const int row = (int)(i / chunks), c = (int)(i - (int64_t)row * chunks);
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(q + (size_t)row * q_stride + c * 4);
-        const float top = block_value(blocks[block_at(row, c / 4, (K + 127) / 128)]);
-        const float s = scale ? scale[row] : 1.f;
-        float v[8];
+    const I step = (I)gridDim.x * 256, end = (items + 31) / 32 * 32;
+    for (I i0 = (I)blockIdx.x * 256 + threadIdx.x; i0 < end; i0 += step * AT_ONCE) {
+        uint32_t codes[AT_ONCE], byte[AT_ONCE];
+        int row[AT_ONCE], c[AT_ONCE];
+        float s[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            uint32_t pair;
-            asm("{\n .reg .b8 a, b;\n .reg .b16 h;\n cvt.u16.u32 h, %1;\n mov.b16 {a, b}, h;\n"
-                " cvt.rn.f16x2.e2m1x2 %0, a;\n}"
-                : "=r"(pair)
-                : "r"(codes >> (8 * j)));
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
-            v[2 * j] = f.x * top * s;
-            v[2 * j + 1] = f.y * top * s;
+        for (int j = 0; j < AT_ONCE; j++) {
+            const I i = i0 + j * step;
+            row[j] = i < items ? (int)(i / (I)chunks) : 0, c[j] = i < items ? (int)(i - (I)row[j] * chunks) : 0;
+            codes[j] = *reinterpret_cast<const uint32_t*>(q + (size_t)row[j] * q_stride + c[j] * 4);
+            byte[j] = blocks[block_at(row[j], c[j] / 4, (K + 127) / 128)];
+            s[j] = scale ? scale[row[j]] : 1.f;
         }
-        store8(y + (size_t)row * stride, c * 8, K, wide, v);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; j++) {
+            const float top = block_value(byte[j]);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float2 f = values2(codes[j] >> (8 * e));
+                v[2 * e] = f.x * top * s[j];
+                v[2 * e + 1] = f.y * top * s[j];
+            }
+            store8<WIDE>(y + (size_t)row[j] * stride, c[j] * 8, K, v, i0 + j * step < items, c[j] > 0);
+        }
     }
+}
+
+template <typename T, bool WIDE>
+psc_status quantize(const T* x, int64_t stride, int T_, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
+                    cudaStream_t cs) {
+    const int n_tiles = (K + 127) / 128;
+    const int64_t items = (int64_t)T_ * n_tiles;
+    const dim3 grid((unsigned)std::min<int64_t>((items + 16 * AT_ONCE - 1) / (16 * AT_ONCE), 1 << 22));
+    if (items < (1ll << 30))
+        return ops_launch(k_quantize_mx4<T, WIDE, uint32_t>, grid, 256, 0, 1, cs, "k_quantize_mx4", x, stride,
+                          (uint32_t)items, n_tiles, K, q, q_stride, blocks);
+    return ops_launch(k_quantize_mx4<T, WIDE, int64_t>, grid, 256, 0, 1, cs, "k_quantize_mx4", x, stride, items, n_tiles,
+                      K, q, q_stride, blocks);
+}
+
+template <typename T, bool WIDE>
+psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int T_, int K, T* y,
+                      int64_t stride, cudaStream_t cs) {
+    const int chunks = (K + 7) / 8;
+    const int64_t items = (int64_t)T_ * chunks;
+    const dim3 grid((unsigned)std::min<int64_t>((items + 256 * AT_ONCE - 1) / (256 * AT_ONCE), 1 << 22));
+    if (items < (1ll << 30))
+        return ops_launch(k_dequantize_mx4<T, WIDE, uint32_t>, grid, 256, 0, 1, cs, "k_dequantize_mx4", q, q_stride,
+                          blocks, scale, (uint32_t)items, chunks, K, y, stride);
+    return ops_launch(k_dequantize_mx4<T, WIDE, int64_t>, grid, 256, 0, 1, cs, "k_dequantize_mx4", q, q_stride, blocks,
+                      scale, items, chunks, K, y, stride);
+}
+
+template <typename T>
+psc_status quantize(const void* x, int64_t stride, int T_, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
+                    cudaStream_t cs) {
+    if (wide_rows<T>(x, stride, K)) return quantize<T, true>((const T*)x, stride, T_, K, q, q_stride, blocks, cs);
+    return quantize<T, false>((const T*)x, stride, T_, K, q, q_stride, blocks, cs);
+}
+
+template <typename T>
+psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int T_, int K,
+                      void* y, int64_t stride, cudaStream_t cs) {
+    if (wide_rows<T>(y, stride, K))
+        return dequantize<T, true>(q, q_stride, blocks, scale, T_, K, (T*)y, stride, cs);
+    return dequantize<T, false>(q, q_stride, blocks, scale, T_, K, (T*)y, stride, cs);
 }
 
 }  // namespace
@@ -69,15 +137,9 @@ psc_status psc_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_stride
     if (!is_mx4(d_q, q_stride, d_blocks, K))
         return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
     if (T == 0) return PSC_OK;
-    const int n_tiles = (K + 127) / 128;
-    const int64_t items = (int64_t)T * n_tiles;
-    const dim3 grid((unsigned)std::min<int64_t>((items + 15) / 16, 1 << 30));
     if (dtype == PSC_BF16)
-        return ops_launch(k_quantize_mx4<__nv_bfloat16>, grid, 256, 0, 1, (cudaStream_t)stream, "k_quantize_mx4",
-                          (const __nv_bfloat16*)d_x, row_stride, items, n_tiles, K, d_q, q_stride, d_blocks,
-                          wide_rows<__nv_bfloat16>(d_x, row_stride, K));
-    return ops_launch(k_quantize_mx4<float>, grid, 256, 0, 1, (cudaStream_t)stream, "k_quantize_mx4", (const float*)d_x,
-                      row_stride, items, n_tiles, K, d_q, q_stride, d_blocks, wide_rows<float>(d_x, row_stride, K));
+        return quantize<__nv_bfloat16>(d_x, row_stride, T, K, d_q, q_stride, d_blocks, (cudaStream_t)stream);
+    return quantize<float>(d_x, row_stride, T, K, d_q, q_stride, d_blocks, (cudaStream_t)stream);
 }
 
 psc_status psc_dequantize_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_blocks, const float* d_scale,
@@ -89,15 +151,9 @@ psc_status psc_dequantize_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_
     if (!is_mx4(d_q, q_stride, d_blocks, K))
         return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
     if (T == 0) return PSC_OK;
-    const int chunks = (K + 7) / 8;
-    const int64_t items = (int64_t)T * chunks;
-    const dim3 grid((unsigned)std::min<int64_t>((items + 255) / 256, 1 << 30));
     if (dtype == PSC_BF16)
-        return ops_launch(k_dequantize_mx4<__nv_bfloat16>, grid, 256, 0, 1, (cudaStream_t)stream, "k_dequantize_mx4",
-                          d_q, q_stride, d_blocks, d_scale, items, chunks, K, (__nv_bfloat16*)d_y, row_stride,
-                          wide_rows<__nv_bfloat16>(d_y, row_stride, K));
-    return ops_launch(k_dequantize_mx4<float>, grid, 256, 0, 1, (cudaStream_t)stream, "k_dequantize_mx4", d_q, q_stride,
-                      d_blocks, d_scale, items, chunks, K, (float*)d_y, row_stride, wide_rows<float>(d_y, row_stride, K));
+        return dequantize<__nv_bfloat16>(d_q, q_stride, d_blocks, d_scale, T, K, d_y, row_stride, (cudaStream_t)stream);
+    return dequantize<float>(d_q, q_stride, d_blocks, d_scale, T, K, d_y, row_stride, (cudaStream_t)stream);
 }
 
 }  // extern "C"

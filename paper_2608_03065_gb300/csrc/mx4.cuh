@@ -9,56 +9,136 @@ namespace {
 
 constexpr int MAX_QUANTIZE_K = 1 << 30;
 
-// Eight values of a row from column k on, zeros past K.  vec: 16-byte loads are in place (then K
-// is a multiple of 8).
-__device__ __forceinline__ void load8(const float* row, int k, int K, bool vec, float v[8]) {
-    if (vec) {
-        const float4 a = *reinterpret_cast<const float4*>(row + k), b = *reinterpret_cast<const float4*>(row + k + 4);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = k + j < K ? row[k + j] : 0.f;
-    }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* row, int k, int K, bool vec, float v[8]) {
-    if (vec) {
-        const uint4 a = *reinterpret_cast<const uint4*>(row + k);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            v[2 * j] = __uint_as_float(w[j] << 16);
-            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = k + j < K ? __bfloat162float(row[k + j]) : 0.f;
-    }
-}
-__device__ __forceinline__ void store8(float* row, int k, int K, bool vec, const float v[8]) {
-    if (vec) {
-        *reinterpret_cast<float4*>(row + k) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(row + k + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (k + j < K) row[k + j] = v[j];
-    }
-}
+// Eight neighbouring columns (a chunk) of a row go in and out by 16-byte accesses.  Where a row starts
+// elsewhere than at a multiple of 16 bytes, or does not end with a chunk, they still do (WIDE false), but
+// for its ends: what is loaded at aligned addresses is shifted into place, and stores take over the end
+// of the previous lane's chunk.  (Element by element: 16,384 rows of 4,095 bf16 columns through the
+// norm into 8 bits 379 us; 16,384 x 4,096 at aligned addresses 111.)
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&p);
 }
-__device__ __forceinline__ void store8(__nv_bfloat16* row, int k, int K, bool vec, const float v[8]) {
-    if (vec) {
-        *reinterpret_cast<uint4*>(row + k) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
-                                                        pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    } else {
+// A chunk's words as values and back.
+__device__ __forceinline__ void unpack8(const uint32_t (&w)[8], float v[8], const float*) {
 #pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (k + j < K) row[k + j] = __float2bfloat16_rn(v[j]);
+    for (int j = 0; j < 8; j++) v[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ void unpack8(const uint32_t (&w)[4], float v[8], const __nv_bfloat16*) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
 }
-// Whether rows of these elements take load8's and store8's 16-byte accesses.
+__device__ __forceinline__ void pack8(const float v[8], uint32_t (&w)[8], const float*) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) w[j] = __float_as_uint(v[j]);
+}
+__device__ __forceinline__ void pack8(const float v[8], uint32_t (&w)[4], const __nv_bfloat16*) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+}
+// x[i] = x[i + by], by < 4.
+template <int N>
+__device__ __forceinline__ void shift_words(uint32_t (&x)[N], int by) {
+#pragma unroll
+    for (int i = 0; i + 1 < N; i++) x[i] = by & 1 ? x[i + 1] : x[i];
+#pragma unroll
+    for (int i = 0; i + 2 < N; i++) x[i] = by & 2 ? x[i + 2] : x[i];
+}
+
+// Columns k to k + 7 of a row, zeros past K.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load8(const T* row, int k, int K, float v[8]) {
+    constexpr int N = sizeof(T) * 2;                    // words of a chunk
+    const int off = WIDE ? 0 : (int)((uintptr_t)(row + k) & 15);
+    const uint4* at = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row + k) - off);
+    uint32_t w[N];
+    if (WIDE || (off == 0 && k + 8 <= K)) {
+#pragma unroll
+        for (int i = 0; i < N / 4; i++) {
+            const uint4 x = at[i];
+            w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+        }
+    } else if ((const void*)at >= (const void*)row && (const void*)(at + N / 4 + 1) <= (const void*)(row + K)) {
+        uint32_t x[N + 4];
+#pragma unroll
+        for (int i = 0; i <= N / 4; i++) {
+            const uint4 y = at[i];
+            x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
+        }
+        shift_words(x, off >> 2);
+#pragma unroll
+        for (int i = 0; i < N; i++) w[i] = sizeof(T) == 2 ? __funnelshift_r(x[i], x[i + 1], (off & 2) * 8) : x[i];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = k + j < K ? load_f32(row + k + j) : 0.f;
+        return;
+    }
+    unpack8(w, v, (const T*)nullptr);
+}
+
+// A chunk of N words to `to`, of which the first `valid` elements (of ES bytes) are there.  All lanes of a warp
+// call it; follows: the lane's chunk lies behind the lane's before it.  Pieces of P words start at multiples
+// of their size.
+template <int N, int P, int ES>
+__device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N], int valid, bool follows) {
+    constexpr int ELEMENTS = 4 * N / ES;
+    const int lane = threadIdx.x & 31, off = (int)((uintptr_t)to & (4 * P - 1));
+    const bool whole = valid >= ELEMENTS;
+    const bool joins = __shfl_up_sync(FULL, whole, 1) && whole && follows && lane > 0;      // the lane before, to this one
+    const bool joined = __shfl_down_sync(FULL, joins, 1) && lane < 31;
+    uint32_t x[P + 1 + N];                              // the last words before the chunk (and one for shifts), the chunk
+#pragma unroll
+    for (int i = 0; i < P; i++) x[1 + i] = __shfl_up_sync(FULL, w[N - P + i], 1);
+    x[0] = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) x[P + 1 + i] = w[i];
+    auto element = [&](int e) {
+        if (ES == 4) reinterpret_cast<uint32_t*>(to)[e] = w[e];
+        else if (ES == 2) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+        else to[e] = (uint8_t)(w[e / 4] >> (8 * (e & 3)));
+    };
+    // the elements one by one: all of a partial chunk, else those in pieces that are not all this lane's to store
+    const int head = off == 0 || joins ? 0 : (4 * P - off) / ES, tail = off == 0 || joined ? 0 : off / ES;
+#pragma unroll
+    for (int e = 0; e < ELEMENTS; e++)
+        if (whole ? e < head || e >= ELEMENTS - tail : e < valid) element(e);
+    if (!whole) return;
+    // words from P - off / 4 on, and the bits of the word before where off is no multiple of 4
+    shift_words(x, P - (off >> 2) == P ? 0 : P - (off >> 2));
+    if (off >> 2 == 0) {
+#pragma unroll
+        for (int i = 0; i <= N; i++) x[i] = x[P + i];
+    }
+#pragma unroll
+    for (int q = 0; q < N / P; q++) {
+        if (q == 0 && off != 0 && !joins) continue;
+        uint32_t y[P];
+#pragma unroll
+        for (int i = 0; i < P; i++) y[i] = ES == 4 ? x[q * P + i + 1] : __funnelshift_l(x[q * P + i], x[q * P + i + 1], (off & 3) * 8);
+        uint8_t* at = to - off + q * 4 * P;
+        if (P == 4) *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
+        else *reinterpret_cast<uint2*>(at) = make_uint2(y[0], y[1]);
+    }
+}
+
+// Columns k to k + 7 of a row, up to K.  WIDE false: all lanes of a warp call it, `there` or not.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store8(T* row, int k, int K, const float v[8], bool there, bool follows) {
+    constexpr int N = sizeof(T) * 2;
+    uint32_t w[N];
+    pack8(v, w, (const T*)nullptr);
+    if (WIDE) {
+        if (!there) return;
+#pragma unroll
+        for (int i = 0; i < N / 4; i++)
+            reinterpret_cast<uint4*>(row + k)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+        store_shifted<N, 4, sizeof(T)>(reinterpret_cast<uint8_t*>(row + k), w, there ? min(8, K - k) : 0, follows);
+    }
+}
+// Whether rows of these elements (none at all, too) are whole chunks at multiples of 16 bytes.
 template <typename T>
 inline bool wide_rows(const void* p, int64_t stride, int K) {
     return !p || (K % 8 == 0 && is_aligned(p, stride * (int64_t)sizeof(T), 16));

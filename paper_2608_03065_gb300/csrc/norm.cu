@@ -5,6 +5,7 @@
 // row.  Quantisation by the row's (or a block's) own largest magnitude does not see such a
 // factor, so the codes are made of v = h gain and r goes into the row's scale: the codes
 // need not wait for the sum of squares, and do not carry its rounding.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -27,172 +28,235 @@ struct Norm {
     int64_t q_stride;
     uint8_t* blocks;
     float* scale;
-    bool wide, wide_gain, wide_q;               // 16-byte accesses are in place
 };
-
-constexpr int NORM_WARPS = 32;
 
 struct RowStats {
     float squares;
     uint32_t h, v;                              // the largest magnitudes' bits
 };
 
-// Over the block, the same in every thread; the order of the sum depends on the block's size alone.
-__device__ __forceinline__ RowStats over_block(RowStats s) {
-    __shared__ float s_squares[NORM_WARPS];
-    __shared__ uint32_t s_h[NORM_WARPS], s_v[NORM_WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x >> 5;
+// Over the block, the same in every thread.
+__device__ __forceinline__ void over_warp(RowStats& s) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) s.squares += __shfl_xor_sync(FULL, s.squares, o);
     s.h = __reduce_max_sync(FULL, s.h);
     s.v = __reduce_max_sync(FULL, s.v);
-    if (n == 1) return s;
-    if (lane == 0) s_squares[warp] = s.squares, s_h[warp] = s.h, s_v[warp] = s.v;
+}
+__device__ __forceinline__ void over_warps(RowStats& s, int n) {           // of n warps, which have over_warp's
+    __shared__ RowStats s_all[32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (n == 1 && blockDim.x == 32) return;
+    if (lane == 0 && warp < n) s_all[warp] = s;
     __syncthreads();
-    s.squares = lane < n ? s_squares[lane] : 0.f;
-    s.h = lane < n ? s_h[lane] : 0u;
-    s.v = lane < n ? s_v[lane] : 0u;
+    s = lane < n ? s_all[lane] : RowStats{0.f, 0u, 0u};
+    over_warp(s);
+}
+// The same for SHARES threads in the place of each of a quarter of the block (that have a chunk each of what
+// it would have), the sums in its order.
+template <int SHARES>
+__device__ __forceinline__ void over_block(RowStats& s) {
+    const int warps = blockDim.x / 32 / SHARES;
+    if (SHARES > 1) {
+        __shared__ float s_squares[1024];
+        __shared__ uint32_t s_h[32], s_v[32];
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x / SHARES;
+        s_squares[threadIdx.x] = s.squares;
+        s.h = __reduce_max_sync(FULL, s.h);
+        s.v = __reduce_max_sync(FULL, s.v);
+        if (lane == 0) s_h[warp] = s.h, s_v[warp] = s.v;
+        __syncthreads();
+        const int at = threadIdx.x % n;
+        s.squares = s_squares[at];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s.squares += __shfl_xor_sync(FULL, s.squares, o);
-    s.h = __reduce_max_sync(FULL, s.h);
-    s.v = __reduce_max_sync(FULL, s.v);
-    return s;
+        for (int i = 1; i < SHARES; i++) s.squares += s_squares[at + i * n];
+        s.h = lane < (int)blockDim.x / 32 ? s_h[lane] : 0u;
+        s.v = lane < (int)blockDim.x / 32 ? s_v[lane] : 0u;
+    }
+    over_warp(s);
+    if (SHARES == 1 || warps > 1) over_warps(s, warps);
 }
 
-// A block per row, eight columns (a chunk) at a time in a thread.  NV chunks of a thread are kept in
-// registers (0: any number, read again for what comes after the sums).
-template <typename T, bool MX4, int NV>
-__global__ void __launch_bounds__(1024) k_norm(Norm a) {
-    const int row = blockIdx.x, chunks = (a.K + 7) / 8;
-    dep_wait();
-    dep_launch();
-    const T* x = (const T*)a.x + (size_t)row * a.x_stride;
-    const T* res = a.residual ? (const T*)a.residual + (size_t)row * a.residual_stride : nullptr;
-    T* sum = a.sum ? (T*)a.sum + (size_t)row * a.sum_stride : nullptr;
-    uint8_t* q = a.q + (size_t)row * a.q_stride;
-    auto load_h = [&](int c, float h[8]) {
-        load8(x, c * 8, a.K, a.wide, h);
-        if (res) {
+// A row of the inputs, a chunk (eight columns from k on) at a time; all lanes of a warp call these.
+template <typename T, bool WIDE>
+struct Row {
+    const T *x, *residual;
+    T* sum;
+    const float* gain;
+    int K;
+    __device__ __forceinline__ Row(const Norm& a, int row)
+        : x((const T*)a.x + (size_t)row * a.x_stride),
+          residual(a.residual ? (const T*)a.residual + (size_t)row * a.residual_stride : nullptr),
+          sum(a.sum ? (T*)a.sum + (size_t)row * a.sum_stride : nullptr), gain(a.gain), K(a.K) {}
+    // h; again: the second time, when the sum may have replaced an input
+    __device__ __forceinline__ void load_h(int k, bool there, float h[8], bool again = false) const {
+#pragma unroll
+        for (int j = 0; j < 8; j++) h[j] = 0.f;
+        if (!there) return;
+        if (again && sum) return load8<WIDE>(sum, k, K, h);
+        load8<WIDE>(x, k, K, h);
+        if (residual) {
             float r[8];
-            load8(res, c * 8, a.K, a.wide, r);
+            load8<WIDE>(residual, k, K, r);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 h[j] += r[j];
-                if (sizeof(T) == 2) h[j] = __bfloat162float(__float2bfloat16_rn(h[j]));    // as the stream holds it
+                if (sizeof(T) == 2) h[j] = __bfloat162float(__float2bfloat16_rn(h[j]));       // as the stream holds it
             }
         }
-        if (sum) store8(sum, c * 8, a.K, a.wide, h);
-    };
-    auto load_gain = [&](int c, float g[8]) {
-        if (a.gain) load8(a.gain, c * 8, a.K, a.wide_gain, g);
-        else
-#pragma unroll
-            for (int j = 0; j < 8; j++) g[j] = 1.f;
-    };
-    auto add = [&](const float h[8], const float v[8], RowStats& s) {
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            s.squares = fmaf(h[j], h[j], s.squares);
-            s.h = max(s.h, magnitude(h[j]));
-            s.v = max(s.v, magnitude(v[j]));
-        }
-    };
-    auto store_q = [&](int c, const float v[8], float s) {              // v / s in whole numbers
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float y = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(v[j], s)), -127.f), 127.f) : 0.f;
-            w[j >> 2] |= (uint32_t)(uint8_t)(int8_t)(int)y << (8 * (j & 3));
-        }
-        if (a.wide_q) *reinterpret_cast<uint2*>(q + c * 8) = make_uint2(w[0], w[1]);
-        else
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (c * 8 + j < a.K) q[c * 8 + j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
-    };
-
-    constexpr int KEPT = NV ? NV : 1;
-    float h[KEPT][8], v[KEPT][8];
-    RowStats s = {0.f, 0u, 0u};
-    // whole warps go round together: a warp's lanes share blocks and tiles
-    const int rounds = (chunks + blockDim.x - 1) / blockDim.x;
-#pragma unroll
-    for (int i = 0; i < (NV ? NV : rounds); i++) {
-        const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
-        float g[8] = {};
-#pragma unroll
-        for (int j = 0; j < 8; j++) h[at][j] = 0.f;
-        if (c < chunks) load_h(c, h[at]), load_gain(c, g);
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[at][j] = h[at][j] * g[j];
-        add(h[at], v[at], s);
-        if (MX4) quantize8(v[at], c, a.K, row, q, a.blocks);
     }
-    s = over_block(s);
+    __device__ __forceinline__ void load_gain(int k, bool there, float g[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; j++) g[j] = 1.f;
+        if (gain && there) load8<WIDE>(gain, k, K, g);
+    }
+};
 
+// What a row's sums give: r, and the unit of the 8-bit codes.
+struct Factor {
+    double r;
+    float unit;                                 // NaN: the row is not finite
+};
+// again(f): this thread's part of the sum of (h f)^2.
+template <int SHARES, typename Again>
+__device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, Again again) {
     const bool bad = s.h >= INF_BITS || s.v >= INF_BITS;
     double r;
     if (!bad && s.h && (s.h > 0x57800000u || s.h < 0x2b800000u)) {
         // beyond 2^48 or below 2^-40 the squares (or r) may leave f32: again, with the largest magnitude near 1
         const int e = max(1, min(253, (int)(s.h >> 23)));
         const float f = __uint_as_float((uint32_t)(254 - e) << 23);
-        float again = 0.f;
-        for (int i = 0; i < rounds; i++) {
-            const int c = i * blockDim.x + threadIdx.x;
-            float y[8] = {};
-            if (c < chunks) {
-                if (NV) {
-#pragma unroll
-                    for (int n = 0; n < KEPT; n++)
-                        if (n == i)
-#pragma unroll
-                            for (int j = 0; j < 8; j++) y[j] = h[n][j];
-                } else if (sum) load8(sum, c * 8, a.K, a.wide, y);
-                else load_h(c, y);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; j++) again = fmaf(y[j] * f, y[j] * f, again);
-        }
+        RowStats t = {again(f), 0u, 0u};
         __syncthreads();
-        const RowStats t = over_block({again, 0u, 0u});
+        over_block<SHARES>(t);
         r = 1.0 / sqrt((double)t.squares / a.K / ((double)f * f) + a.eps);
     } else {
         r = __fdiv_rn(1.f, __fsqrt_rn(__fdiv_rn(s.squares, (float)a.K) + a.eps));
     }
-    const float nan = __uint_as_float(0x7fc00000u);
-    if (MX4) {
-        // 1 / sqrt(0): a row of zeros with eps 0
-        if (threadIdx.x == 0) a.scale[row] = bad ? nan : s.h == 0 && a.eps == 0.f ? 0.f : (float)r;
-        return;
-    }
-    const float unit = bad ? nan : __fmul_rn(__uint_as_float(s.v), 1.f / 127.f);
-    if (threadIdx.x == 0) a.scale[row] = unit == 0.f ? 0.f : (float)(unit * r);
+    return {r, bad ? __uint_as_float(0x7fc00000u) : __fmul_rn(__uint_as_float(s.v), 1.f / 127.f)};
+}
+
+// Eight codes v / unit in two words.  A quotient within 127 is v * inverse to 2^-16 (inverse is the rounded
+// 1 / unit, 2^-24 of it off, and the quotient has its own rounding), so the nearest whole number to that product is
+// the code unless the product is that close to a half; it is rounded to a whole number by adding 1.5 * 2^23,
+// whose low byte then is the code.
+__device__ __forceinline__ uint2 codes_of(const float v[8], float unit, float inverse) {
+    constexpr float BIG = 12582912.f, NEAR = 0.5f - 0x1p-15f;
+    uint32_t w[8];
+    bool sure = true;
 #pragma unroll
-    for (int i = 0; i < (NV ? NV : rounds); i++) {
+    for (int j = 0; j < 8; j++) {
+        const float m = fmaf(v[j], inverse, BIG);
+        sure &= fabsf(fmaf(v[j], inverse, BIG - m)) <= NEAR;
+        w[j] = __float_as_uint(m);
+    }
+    if (!sure)                                  // near a half, or the unit is 0 or NaN or has no inverse
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            w[j] = unit > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(v[j], unit)), -127.f), 127.f) : 0u;
+    return make_uint2(__byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410));
+}
+
+// A block per row, NV chunks of it in a thread's registers (0: any number, read again for what comes after
+// the sums).  Small blocks whose threads have four chunks each keep most loads under way (16,384 rows of 4,096
+// bf16 columns: 128 threads 111 us, 512 threads 141); where there are too few rows for that, four times as many
+// threads, a chunk each, are done sooner (1 row of 2,048 columns: 4.1 us with 64 threads, 1.9 with 256).  Both add
+// up in the same order (SHARES).
+template <typename T, bool MX4, bool WIDE, int NV, int SHARES, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_norm(Norm a) {
+    const int chunks = (a.K + 7) / 8;
+    dep_wait();
+    dep_launch();
+    // whole warps go round together: a warp's lanes share blocks and tiles
+    const int rounds = NV ? NV : (chunks + blockDim.x - 1) / blockDim.x;
+    constexpr int KEPT = NV ? NV : 1;
+    const Row<T, WIDE> row(a, blockIdx.x);
+    uint8_t* q = a.q + (size_t)blockIdx.x * a.q_stride;
+    float v[KEPT][8];
+    RowStats s = {0.f, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < (NV ? NV : 0); i++) {           // all loads on their way before any is used
+        const int c = i * blockDim.x + threadIdx.x;
+        row.load_h(c * 8, c < chunks, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < rounds; i++) {
         const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
-        if (c >= chunks) break;
+        float g[8], squares = 0.f;
+        if (!NV) row.load_h(c * 8, c < chunks, v[0]);
+        row.load_gain(c * 8, c < chunks, g);
+        if (row.sum) store8<WIDE>(row.sum, c * 8, a.K, v[at], c < chunks, c > 0);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            float& x = v[at][j];
+            squares = fmaf(x, x, squares);
+            s.h = max(s.h, magnitude(x));
+            x *= g[j];
+            s.v = max(s.v, magnitude(x));
+        }
+        s.squares += squares;
+        if (MX4) quantize8(v[at], c, a.K, blockIdx.x, q, a.blocks);
+    }
+    over_block<SHARES>(s);
+    const Factor f = factor_of<SHARES>(a, s, [&](float by) {
+        float sum = 0.f;
+        for (int c = threadIdx.x; c < chunks; c += blockDim.x) {
+            float h[8];
+            row.load_h(c * 8, true, h, true);
+            float part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; j++) part = fmaf(h[j] * by, h[j] * by, part);
+            sum += part;
+        }
+        return sum;
+    });
+    if (threadIdx.x == 0) {
+        float* out = a.scale + blockIdx.x;
+        if (!MX4) *out = f.unit == 0.f ? 0.f : (float)(f.unit * f.r);
+        else if (isnan(f.unit)) *out = f.unit;
+        else *out = s.h == 0 && a.eps == 0.f ? 0.f : (float)f.r;        // 1 / sqrt(0): a row of zeros with eps 0
+    }
+    if (MX4) return;
+    const float inverse = __fdiv_rn(1.f, f.unit);
+#pragma unroll
+    for (int i = 0; i < rounds; i++) {
+        const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
         if (!NV) {
             float g[8];
-            if (sum) load8(sum, c * 8, a.K, a.wide, h[0]);
-            else load_h(c, h[0]);
-            load_gain(c, g);
+            row.load_h(c * 8, c < chunks, v[0], true);
+            row.load_gain(c * 8, c < chunks, g);
 #pragma unroll
-            for (int j = 0; j < 8; j++) v[0][j] = h[0][j] * g[j];
+            for (int j = 0; j < 8; j++) v[0][j] *= g[j];
         }
-        store_q(c, v[at], unit);
+        const uint2 codes = codes_of(v[at], f.unit, inverse);
+        if (WIDE) {
+            if (c < chunks) *reinterpret_cast<uint2*>(q + c * 8) = codes;
+        } else {
+            const uint32_t w[2] = {codes.x, codes.y};
+            store_shifted<2, 2, 1>(q + c * 8, w, c < chunks ? min(8, a.K - c * 8) : 0, c > 0);
+        }
     }
 }
 
+template <typename T, bool MX4, bool WIDE>
+psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
+    // a thread's share goes by the width alone, and so do the sums' orders
+    const int chunks = (a.K + 7) / 8, quarter = (chunks + 3) / 4;
+    const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
+    if (threads <= 256 && a.T <= 2 * current_sms())
+        return ops_launch(k_norm<T, MX4, WIDE, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
+    return ops_launch(threads <= 256         ? k_norm<T, MX4, WIDE, 4, 1, 256>
+                      : chunks <= 4 * threads ? k_norm<T, MX4, WIDE, 4, 1, 1024>
+                                              : k_norm<T, MX4, WIDE, 0, 1, 1024>,
+                      dim3(a.T), threads, 0, 1, cs, me, a);
+}
+
 template <typename T, bool MX4>
-psc_status norm(Norm a, const char* me, cudaStream_t cs) {
-    a.wide = wide_rows<T>(a.x, a.x_stride, a.K) && wide_rows<T>(a.residual, a.residual_stride, a.K) &&
-             wide_rows<T>(a.sum, a.sum_stride, a.K);
-    a.wide_gain = wide_rows<float>(a.gain, 0, a.K);
-    a.wide_q = a.K % 8 == 0 && is_aligned(a.q, a.q_stride, 8);
-    const int chunks = (a.K + 7) / 8;
-    const int threads = chunks < 1024 ? (chunks + 31) / 32 * 32 : 1024, rounds = (chunks + threads - 1) / threads;
-    auto kernel = rounds == 1 ? k_norm<T, MX4, 1> : rounds == 2 ? k_norm<T, MX4, 2> : k_norm<T, MX4, 0>;
-    return ops_launch(kernel, dim3(a.T), threads, 0, 1, cs, me, a);
+psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
+    const bool wide = wide_rows<T>(a.x, a.x_stride, a.K) && wide_rows<T>(a.residual, a.residual_stride, a.K) &&
+                      wide_rows<T>(a.sum, a.sum_stride, a.K) && wide_rows<float>(a.gain, 0, a.K) && a.K % 8 == 0 &&
+                      is_aligned(a.q, a.q_stride, 8);
+    return wide ? norm<T, MX4, true>(a, me, cs) : norm<T, MX4, false>(a, me, cs);
 }
 
 template <bool MX4>
@@ -222,7 +286,7 @@ psc_status psc_norm_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_
                                   void* stream) {
     return norm_entry<false>("psc_norm_quantize_rows",
                              Norm{d_x, row_stride, d_residual, residual_stride, d_sum, sum_stride, d_gain, eps, T, K,
-                                  (uint8_t*)d_q, q_stride, nullptr, d_scale, false, false, false},
+                                  (uint8_t*)d_q, q_stride, nullptr, d_scale},
                              dtype, stream);
 }
 
@@ -232,7 +296,7 @@ psc_status psc_norm_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_s
                                  float* d_scale, void* stream) {
     return norm_entry<true>("psc_norm_quantize_mx4",
                             Norm{d_x, row_stride, d_residual, residual_stride, d_sum, sum_stride, d_gain, eps, T, K,
-                                 d_q, q_stride, d_blocks, d_scale, false, false, false},
+                                 d_q, q_stride, d_blocks, d_scale},
                             dtype, stream);
 }
 

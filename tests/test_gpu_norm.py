@@ -2,10 +2,10 @@
 
 Codes and the sum h are compared exactly: they are made of correctly rounded f32 products,
 sums and quotients on both sides.  A scale holds r = 1 / sqrt(mean h^2 + eps): the squares are
-all positive, so a sum of K of them in f32, no addend passing through more than
-K / (8 threads) + 12 additions, is off by that many u = 2^-24 of itself at most; the quotient
-by K, the addition of eps, the root and the reciprocal are a rounding each, and the root halves
-what is in front of it.
+all positive, so a sum of K of them in f32, no addend passing through more additions than a
+thread has columns (32, or K / 1024 rounded up to a chunk of 8 in wider rows) and 12 across
+threads, is off by that many u = 2^-24 of itself at most; the quotient by K, the addition of
+eps, the root and the reciprocal are a rounding each, and the root halves what is in front of it.
 """
 from __future__ import annotations
 
@@ -20,8 +20,7 @@ pytestmark = pytest.mark.gpu
 
 
 def _adds(K):
-    threads = min(1024, -(-(-(-K // 8)) // 32) * 32)
-    return 8 * -(-K // (8 * threads)) + 12
+    return max(32, 8 * -(-K // 8192)) + 12
 
 
 def _tolerance(K):
