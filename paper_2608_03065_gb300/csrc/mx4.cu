@@ -7,31 +7,42 @@
 
 namespace {
 
-constexpr int AT_ONCE = 2;              // pieces that a thread has under way
+// Both ways sixteen lanes have a tile of a row (128 columns), eight neighbouring columns each, and go from row to
+// row in steps of rows_step (n_tiles * rows_step sixteens of lanes in all; whole warps go round
+// together, as their lanes share blocks and tiles).  AT_ONCE rows of a lane are under way together.
+constexpr int AT_ONCE = 2, TURNS = 2;
 
-// Both ways a thread has eight neighbouring columns.  I: what counts a matrix's pieces.
-template <typename T, bool WIDE, typename I>
-__global__ void __launch_bounds__(256) k_quantize_mx4(const T* x, int64_t stride, I items, int n_tiles, int K, uint8_t* q,
-                                                      int64_t q_stride, uint8_t* blocks) {
+struct Lane {
+    uint32_t row;                           // the first
+    int c;                                  // the chunk
+    bool there;
+};
+__device__ __forceinline__ Lane lane_of(int n_tiles, uint32_t rows_step) {
+    const uint32_t i = blockIdx.x * 16u + (threadIdx.x >> 4), row = i / (uint32_t)n_tiles;
+    return {row, (int)(i - row * n_tiles) * 16 + (int)(threadIdx.x & 15), row < rows_step};
+}
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) k_quantize_mx4(const T* x, int64_t stride, uint32_t rows, int n_tiles,
+                                                      uint32_t rows_step, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks) {
+    const Lane l = lane_of(n_tiles, rows_step);
+    const bool inside = l.c * 8 < K;
     dep_wait();
     dep_launch();
-    // sixteen lanes a tile of a row; whole warps go round together, as their lanes share blocks and tiles
-    const I step = (I)gridDim.x * 16, end = (items + 1) / 2 * 2;
-    for (I i0 = (I)blockIdx.x * 16 + (threadIdx.x >> 4); i0 < end; i0 += step * AT_ONCE) {
+    for (uint32_t r0 = l.row; __any_sync(FULL, r0 < rows); r0 += rows_step * AT_ONCE) {
         float v[AT_ONCE][8];
-        int row[AT_ONCE], c[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
-            const I i = i0 + j * step;
-            row[j] = (int)(i / (I)n_tiles), c[j] = (int)(i - (I)row[j] * n_tiles) * 16 + (threadIdx.x & 15);
+            const uint32_t row = r0 + j * rows_step;
 #pragma unroll
             for (int e = 0; e < 8; e++) v[j][e] = 0.f;
-            if (i < items && c[j] * 8 < K) load8<WIDE>(x + (size_t)row[j] * stride, c[j] * 8, K, v[j]);
+            if (l.there && inside && row < rows) load8<WIDE>(x + (size_t)row * stride, l.c * 8, K, v[j]);
         }
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; j++)
-            if (i0 + j * step < end)            // of both of the warp's tiles
-                quantize8(v[j], c[j], i0 + j * step < items ? K : 0, row[j], q + (size_t)row[j] * q_stride, blocks);
+        for (int j = 0; j < AT_ONCE; j++) {
+            const uint32_t row = r0 + j * rows_step;
+            quantize8(v[j], largest8(v[j]), l.c, l.there && row < rows ? K : 0, row, q + (size_t)row * q_stride, blocks);
+        }
     }
 }
 
@@ -44,27 +55,31 @@ __device__ __forceinline__ float2 values2(uint32_t codes) {
     return __half22float2(*reinterpret_cast<const __half2*>(&pair));
 }
 
-template <typename T, bool WIDE, typename I>
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) k_dequantize_mx4(const uint8_t* q, int64_t q_stride, const uint8_t* blocks,
-                                                        const float* scale, I items, int chunks, int K, T* y,
-                                                        int64_t stride) {
+                                                        const float* scale, uint32_t rows, int n_tiles,
+                                                        uint32_t rows_step, int K,
+                                                        T* y, int64_t stride) {
+    const Lane l = lane_of(n_tiles, rows_step);
+    const bool inside = l.there && l.c * 8 < K;
     dep_wait();
     dep_launch();
-    const I step = (I)gridDim.x * 256, end = (items + 31) / 32 * 32;
-    for (I i0 = (I)blockIdx.x * 256 + threadIdx.x; i0 < end; i0 += step * AT_ONCE) {
+    for (uint32_t r0 = l.row; __any_sync(FULL, r0 < rows); r0 += rows_step * AT_ONCE) {
         uint32_t codes[AT_ONCE], byte[AT_ONCE];
-        int row[AT_ONCE], c[AT_ONCE];
         float s[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
-            const I i = i0 + j * step;
-            row[j] = i < items ? (int)(i / (I)chunks) : 0, c[j] = i < items ? (int)(i - (I)row[j] * chunks) : 0;
-            codes[j] = *reinterpret_cast<const uint32_t*>(q + (size_t)row[j] * q_stride + c[j] * 4);
-            byte[j] = blocks[block_at(row[j], c[j] / 4, (K + 127) / 128)];
-            s[j] = scale ? scale[row[j]] : 1.f;
+            const uint32_t row = r0 + j * rows_step;
+            codes[j] = byte[j] = 0;
+            s[j] = 1.f;
+            if (!inside || row >= rows) continue;
+            codes[j] = *reinterpret_cast<const uint32_t*>(q + (size_t)row * q_stride + l.c * 4);
+            byte[j] = blocks[block_at(row, l.c / 4, n_tiles)];
+            if (scale) s[j] = scale[row];
         }
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
+            const uint32_t row = r0 + j * rows_step;
             const float top = block_value(byte[j]);
             float v[8];
 #pragma unroll
@@ -73,50 +88,37 @@ __global__ void __launch_bounds__(256) k_dequantize_mx4(const uint8_t* q, int64_
                 v[2 * e] = f.x * top * s[j];
                 v[2 * e + 1] = f.y * top * s[j];
             }
-            store8<WIDE>(y + (size_t)row[j] * stride, c[j] * 8, K, v, i0 + j * step < items, c[j] > 0);
+            store8<WIDE>(y + (size_t)row * stride, l.c * 8, K, v, inside && row < rows, l.c & 15);
         }
     }
 }
 
-template <typename T, bool WIDE>
-psc_status quantize(const T* x, int64_t stride, int T_, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
-                    cudaStream_t cs) {
-    const int n_tiles = (K + 127) / 128;
-    const int64_t items = (int64_t)T_ * n_tiles;
-    const dim3 grid((unsigned)std::min<int64_t>((items + 16 * AT_ONCE - 1) / (16 * AT_ONCE), 1 << 22));
-    if (items < (1ll << 30))
-        return ops_launch(k_quantize_mx4<T, WIDE, uint32_t>, grid, 256, 0, 1, cs, "k_quantize_mx4", x, stride,
-                          (uint32_t)items, n_tiles, K, q, q_stride, blocks);
-    return ops_launch(k_quantize_mx4<T, WIDE, int64_t>, grid, 256, 0, 1, cs, "k_quantize_mx4", x, stride, items, n_tiles,
-                      K, q, q_stride, blocks);
-}
-
-template <typename T, bool WIDE>
-psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int T_, int K, T* y,
-                      int64_t stride, cudaStream_t cs) {
-    const int chunks = (K + 7) / 8;
-    const int64_t items = (int64_t)T_ * chunks;
-    const dim3 grid((unsigned)std::min<int64_t>((items + 256 * AT_ONCE - 1) / (256 * AT_ONCE), 1 << 22));
-    if (items < (1ll << 30))
-        return ops_launch(k_dequantize_mx4<T, WIDE, uint32_t>, grid, 256, 0, 1, cs, "k_dequantize_mx4", q, q_stride,
-                          blocks, scale, (uint32_t)items, chunks, K, y, stride);
-    return ops_launch(k_dequantize_mx4<T, WIDE, int64_t>, grid, 256, 0, 1, cs, "k_dequantize_mx4", q, q_stride, blocks,
-                      scale, items, chunks, K, y, stride);
+// Rows under way at a time: enough for some waves of blocks over the GPU, of which none ends much later than
+// the others, each lane with a few turns.
+struct Grid {
+    int n_tiles, rows_step;
+    dim3 blocks;
+};
+Grid grid_of(int rows, int K) {
+    const int n_tiles = (K + 127) / 128, wave = (current_sms() * 8 * 16 + n_tiles - 1) / n_tiles;
+    const int step = std::max(1, std::min(std::max(wave, rows / (AT_ONCE * TURNS)), (rows + AT_ONCE - 1) / AT_ONCE));
+    return {n_tiles, step, dim3((unsigned)(((int64_t)n_tiles * step + 15) / 16))};
 }
 
 template <typename T>
-psc_status quantize(const void* x, int64_t stride, int T_, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
+psc_status quantize(const void* x, int64_t stride, int rows, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
                     cudaStream_t cs) {
-    if (wide_rows<T>(x, stride, K)) return quantize<T, true>((const T*)x, stride, T_, K, q, q_stride, blocks, cs);
-    return quantize<T, false>((const T*)x, stride, T_, K, q, q_stride, blocks, cs);
+    const Grid g = grid_of(rows, K);
+    return ops_launch(wide_rows<T>(x, stride, K) ? k_quantize_mx4<T, true> : k_quantize_mx4<T, false>, g.blocks, 256, 0, 1,
+                      cs, "k_quantize_mx4", (const T*)x, stride, rows, g.n_tiles, g.rows_step, K, q, q_stride, blocks);
 }
 
 template <typename T>
-psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int T_, int K,
+psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int rows, int K,
                       void* y, int64_t stride, cudaStream_t cs) {
-    if (wide_rows<T>(y, stride, K))
-        return dequantize<T, true>(q, q_stride, blocks, scale, T_, K, (T*)y, stride, cs);
-    return dequantize<T, false>(q, q_stride, blocks, scale, T_, K, (T*)y, stride, cs);
+    const Grid g = grid_of(rows, K);
+    return ops_launch(wide_rows<T>(y, stride, K) ? k_dequantize_mx4<T, true> : k_dequantize_mx4<T, false>, g.blocks, 256, 0,
+                      1, cs, "k_dequantize_mx4", q, q_stride, blocks, scale, rows, g.n_tiles, g.rows_step, K, (T*)y, stride);
 }
 
 }  // namespace

@@ -2,6 +2,8 @@
 // four neighbouring threads a block of 32 columns, sixteen a row's piece of a tile of exponents.
 #pragma once
 
+#include <type_traits>
+
 #include "../../include/psc_mx4.h"
 #include "ops_common.cuh"
 
@@ -38,13 +40,13 @@ __device__ __forceinline__ void pack8(const float v[8], uint32_t (&w)[4], const 
 #pragma unroll
     for (int j = 0; j < 4; j++) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
 }
-// x[i] = x[i + by], by < 4.
-template <int N>
-__device__ __forceinline__ void shift_words(uint32_t (&x)[N], int by) {
-#pragma unroll
-    for (int i = 0; i + 1 < N; i++) x[i] = by & 1 ? x[i + 1] : x[i];
-#pragma unroll
-    for (int i = 0; i + 2 < N; i++) x[i] = by & 2 ? x[i + 2] : x[i];
+// f(std::integral_constant) of a number from 0 to 3 (words' places have to be known to the compiler).
+template <typename F>
+__device__ __forceinline__ void with_place(int i, F f) {
+    if (i == 0) f(std::integral_constant<int, 0>());
+    else if (i == 1) f(std::integral_constant<int, 1>());
+    else if (i == 2) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 3>());
 }
 
 // Columns k to k + 7 of a row, zeros past K.
@@ -67,9 +69,12 @@ __device__ __forceinline__ void load8(const T* row, int k, int K, float v[8]) {
             const uint4 y = at[i];
             x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
         }
-        shift_words(x, off >> 2);
+        with_place(off >> 2, [&](auto known) {
+            constexpr int place = decltype(known)::value;
 #pragma unroll
-        for (int i = 0; i < N; i++) w[i] = sizeof(T) == 2 ? __funnelshift_r(x[i], x[i + 1], (off & 2) * 8) : x[i];
+            for (int i = 0; i < N; i++)
+                w[i] = sizeof(T) == 2 ? __funnelshift_r(x[i + place], x[i + place + 1], (off & 2) * 8) : x[i + place];
+        });
     } else {
 #pragma unroll
         for (int j = 0; j < 8; j++) v[j] = k + j < K ? load_f32(row + k + j) : 0.f;
@@ -101,26 +106,27 @@ __device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N
     };
     // the elements one by one: all of a partial chunk, else those in pieces that are not all this lane's to store
     const int head = off == 0 || joins ? 0 : (4 * P - off) / ES, tail = off == 0 || joined ? 0 : off / ES;
+    if (!whole || head || tail)
 #pragma unroll
-    for (int e = 0; e < ELEMENTS; e++)
-        if (whole ? e < head || e >= ELEMENTS - tail : e < valid) element(e);
+        for (int e = 0; e < ELEMENTS; e++)
+            if (whole ? e < head || e >= ELEMENTS - tail : e < valid) element(e);
     if (!whole) return;
-    // words from P - off / 4 on, and the bits of the word before where off is no multiple of 4
-    shift_words(x, P - (off >> 2) == P ? 0 : P - (off >> 2));
-    if (off >> 2 == 0) {
+    with_place(off >> 2, [&](auto known) {
+        constexpr int place = decltype(known)::value, from = place < P ? P + 1 - place : 1;
+        if (place >= P) return;
 #pragma unroll
-        for (int i = 0; i <= N; i++) x[i] = x[P + i];
-    }
+        for (int q = 0; q < N / P; q++) {
+            if (q == 0 && off != 0 && !joins) continue;
+            uint32_t y[P];
 #pragma unroll
-    for (int q = 0; q < N / P; q++) {
-        if (q == 0 && off != 0 && !joins) continue;
-        uint32_t y[P];
-#pragma unroll
-        for (int i = 0; i < P; i++) y[i] = ES == 4 ? x[q * P + i + 1] : __funnelshift_l(x[q * P + i], x[q * P + i + 1], (off & 3) * 8);
-        uint8_t* at = to - off + q * 4 * P;
-        if (P == 4) *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
-        else *reinterpret_cast<uint2*>(at) = make_uint2(y[0], y[1]);
-    }
+            for (int i = 0; i < P; i++) {               // words from off / 4 before the chunk on, the bits in front from the word before
+                y[i] = ES == 4 ? x[q * P + i + from] : __funnelshift_l(x[q * P + i + from - 1], x[q * P + i + from], (off & 3) * 8);
+            }
+            uint8_t* at = to - off + q * 4 * P;
+            if (P == 4) *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
+            else *reinterpret_cast<uint2*>(at) = make_uint2(y[0], y[1]);
+        }
+    });
 }
 
 // Columns k to k + 7 of a row, up to K.  WIDE false: all lanes of a warp call it, `there` or not.
@@ -144,8 +150,13 @@ inline bool wide_rows(const void* p, int64_t stride, int K) {
     return !p || (K % 8 == 0 && is_aligned(p, stride * (int64_t)sizeof(T), 16));
 }
 
-// The magnitudes' bit patterns order as the magnitudes do, with infinities and NaN above all.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The larger of a and |b|; NaN if one is.  As bit patterns magnitudes order as they do as numbers, with
+// infinities and then NaN above all.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
 constexpr uint32_t INF_BITS = 0x7f800000u;
 
 // Where the exponent of row r's block b is; n_tiles = ceil(K / 128).
@@ -177,17 +188,16 @@ __device__ __forceinline__ uint32_t codes8(const float v[8], float inverse) {
     return out;
 }
 
-// A thread's eight columns from 8 c on of a row, to codes and exponents.  All 32 lanes of a warp
-// call it for neighbouring chunks c, lane 0's a multiple of 16; what lies past the row's last
-// tile stores nothing.
-__device__ __forceinline__ void quantize8(const float v[8], int c, int K, int row, uint8_t* q_row, uint8_t* blocks) {
+// A thread's eight columns from 8 c on of a row, to codes and exponents; `top` the largest magnitude of
+// them.  All 32 lanes of a warp call it for neighbouring chunks c (or 16 of one row and 16 of another), lane
+// 0's a multiple of 16; what lies past the row's last tile stores nothing.  Returns whether the block is NaN.
+__device__ __forceinline__ bool quantize8(const float v[8], float top, int c, int K, int row, uint8_t* q_row,
+                                          uint8_t* blocks) {
     const int lane = threadIdx.x & 31;
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; j++) top = max(top, magnitude(v[j]));
-    top = max(top, __shfl_xor_sync(FULL, top, 1));
-    top = max(top, __shfl_xor_sync(FULL, top, 2));
-    const uint32_t byte = block_byte(top);
+    uint32_t bits = __float_as_uint(top) & 0x7fffffffu;
+    bits = max(bits, __shfl_xor_sync(FULL, bits, 1));
+    bits = max(bits, __shfl_xor_sync(FULL, bits, 2));
+    const uint32_t byte = block_byte(bits);
     if (c < (K + 31) / 32 * 4)
         *reinterpret_cast<uint32_t*>(q_row + c * 4) = byte == 255 ? 0u : codes8(v, block_inverse(byte));
     // the four blocks of a tile's row, by one of its sixteen lanes
@@ -197,6 +207,13 @@ __device__ __forceinline__ void quantize8(const float v[8], int c, int K, int ro
     const int n_tiles = (K + 127) / 128;
     if (!(lane & 15) && c < n_tiles * 16)
         *reinterpret_cast<uint32_t*>(blocks + block_at(row, c / 4, n_tiles)) = word;
+    return byte == 255;
+}
+__device__ __forceinline__ float largest8(const float v[8]) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; j++) top = larger(top, v[j]);
+    return top;
 }
 
 inline bool is_mx4(const void* q, int64_t stride, const void* blocks, int K) {

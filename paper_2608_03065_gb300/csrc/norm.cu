@@ -31,16 +31,15 @@ struct Norm {
 };
 
 struct RowStats {
-    float squares;
-    uint32_t h, v;                              // the largest magnitudes' bits
+    float squares;                              // of h
+    uint32_t top;                               // the largest magnitude's bits (of v, in the first pass)
 };
 
 // Over the block, the same in every thread.
 __device__ __forceinline__ void over_warp(RowStats& s) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) s.squares += __shfl_xor_sync(FULL, s.squares, o);
-    s.h = __reduce_max_sync(FULL, s.h);
-    s.v = __reduce_max_sync(FULL, s.v);
+    s.top = __reduce_max_sync(FULL, s.top);
 }
 __device__ __forceinline__ void over_warps(RowStats& s, int n) {           // of n warps, which have over_warp's
     __shared__ RowStats s_all[32];
@@ -48,29 +47,27 @@ __device__ __forceinline__ void over_warps(RowStats& s, int n) {           // of
     if (n == 1 && blockDim.x == 32) return;
     if (lane == 0 && warp < n) s_all[warp] = s;
     __syncthreads();
-    s = lane < n ? s_all[lane] : RowStats{0.f, 0u, 0u};
+    s = lane < n ? s_all[lane] : RowStats{0.f, 0u};
     over_warp(s);
 }
-// The same for SHARES threads in the place of each of a quarter of the block (that have a chunk each of what
-// it would have), the sums in its order.
+// The same where SHARES threads stand for each of a smaller block (and have a chunk each of what it would have),
+// the sums in its order.
 template <int SHARES>
 __device__ __forceinline__ void over_block(RowStats& s) {
     const int warps = blockDim.x / 32 / SHARES;
     if (SHARES > 1) {
         __shared__ float s_squares[1024];
-        __shared__ uint32_t s_h[32], s_v[32];
+        __shared__ uint32_t s_top[32];
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = blockDim.x / SHARES;
         s_squares[threadIdx.x] = s.squares;
-        s.h = __reduce_max_sync(FULL, s.h);
-        s.v = __reduce_max_sync(FULL, s.v);
-        if (lane == 0) s_h[warp] = s.h, s_v[warp] = s.v;
+        s.top = __reduce_max_sync(FULL, s.top);
+        if (lane == 0) s_top[warp] = s.top;
         __syncthreads();
         const int at = threadIdx.x % n;
         s.squares = s_squares[at];
 #pragma unroll
         for (int i = 1; i < SHARES; i++) s.squares += s_squares[at + i * n];
-        s.h = lane < (int)blockDim.x / 32 ? s_h[lane] : 0u;
-        s.v = lane < (int)blockDim.x / 32 ? s_v[lane] : 0u;
+        s.top = lane < (int)blockDim.x / 32 ? s_top[lane] : 0u;
     }
     over_warp(s);
     if (SHARES == 1 || warps > 1) over_warps(s, warps);
@@ -111,28 +108,35 @@ struct Row {
     }
 };
 
-// What a row's sums give: r, and the unit of the 8-bit codes.
+// What a row's sums give.
 struct Factor {
-    double r;
-    float unit;                                 // NaN: the row is not finite
+    float unit;                                 // of the 8-bit codes; NaN: the row is not finite
+    float scale;                                // the row's, for 8 or for 4 bits
 };
-// again(f): this thread's part of the sum of (h f)^2.
-template <int SHARES, typename Again>
+// again(f): this thread's part of the sum of (h f)^2, and the largest |h f|.
+template <bool MX4, int SHARES, typename Again>
 __device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, Again again) {
-    const bool bad = s.h >= INF_BITS || s.v >= INF_BITS;
-    double r;
-    if (!bad && s.h && (s.h > 0x57800000u || s.h < 0x2b800000u)) {
-        // beyond 2^48 or below 2^-40 the squares (or r) may leave f32: again, with the largest magnitude near 1
-        const int e = max(1, min(253, (int)(s.h >> 23)));
-        const float f = __uint_as_float((uint32_t)(254 - e) << 23);
-        RowStats t = {again(f), 0u, 0u};
-        __syncthreads();
-        over_block<SHARES>(t);
-        r = 1.0 / sqrt((double)t.squares / a.K / ((double)f * f) + a.eps);
-    } else {
-        r = __fdiv_rn(1.f, __fsqrt_rn(__fdiv_rn(s.squares, (float)a.K) + a.eps));
+    const float unit = s.top >= INF_BITS ? __uint_as_float(0x7fc00000u) : __fmul_rn(__uint_as_float(s.top), 1.f / 127.f);
+    if (isnan(unit)) return {unit, unit};
+    if (s.squares >= 0x1p-76f && s.squares <= 0x1p126f) {
+        const float r = __fdiv_rn(1.f, __fsqrt_rn(__fdiv_rn(s.squares, (float)a.K) + a.eps));
+        return {unit, MX4 ? r : unit * r};
     }
-    return {r, bad ? __uint_as_float(0x7fc00000u) : __fmul_rn(__uint_as_float(s.v), 1.f / 127.f)};
+    // the squares, or r, may leave f32 (squares of less than 2^-126 lose bits, but not of a sum from 2^-76
+    // on): once more, with the largest magnitude near 1
+    RowStats t = again(1.f);
+    __syncthreads();
+    over_block<SHARES>(t);
+    const int e = max(1, min(253, (int)(t.top >> 23)));
+    const bool zeros = t.top == 0;
+    const float f = __uint_as_float((uint32_t)(254 - e) << 23);
+    t = again(f);
+    __syncthreads();
+    over_block<SHARES>(t);
+    const double r = 1.0 / sqrt((double)t.squares / a.K / ((double)f * f) + a.eps);
+    // a row of zeros with eps 0, or of no unit: 0, not the product with an infinite r
+    if (MX4) return {unit, zeros && a.eps == 0.f ? 0.f : (float)r};
+    return {unit, unit == 0.f ? 0.f : (float)(unit * r)};
 }
 
 // Eight codes v / unit in two words.  A quotient within 127 is v * inverse to 2^-16 (inverse is the rounded
@@ -163,7 +167,7 @@ __device__ __forceinline__ uint2 codes_of(const float v[8], float unit, float in
 // threads, a chunk each, are done sooner (1 row of 2,048 columns: 4.1 us with 64 threads, 1.9 with 256).  Both add
 // up in the same order (SHARES).
 template <typename T, bool MX4, bool WIDE, int NV, int SHARES, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm(Norm a) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     const int chunks = (a.K + 7) / 8;
     dep_wait();
     dep_launch();
@@ -173,7 +177,9 @@ __global__ void __launch_bounds__(THREADS) k_norm(Norm a) {
     const Row<T, WIDE> row(a, blockIdx.x);
     uint8_t* q = a.q + (size_t)blockIdx.x * a.q_stride;
     float v[KEPT][8];
-    RowStats s = {0.f, 0u, 0u};
+    RowStats s = {0.f, 0u};
+    float top = 0.f;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < (NV ? NV : 0); i++) {           // all loads on their way before any is used
         const int c = i * blockDim.x + threadIdx.x;
@@ -182,7 +188,7 @@ __global__ void __launch_bounds__(THREADS) k_norm(Norm a) {
 #pragma unroll
     for (int i = 0; i < rounds; i++) {
         const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
-        float g[8], squares = 0.f;
+        float g[8], squares = 0.f, most = 0.f;
         if (!NV) row.load_h(c * 8, c < chunks, v[0]);
         row.load_gain(c * 8, c < chunks, g);
         if (row.sum) store8<WIDE>(row.sum, c * 8, a.K, v[at], c < chunks, c > 0);
@@ -190,32 +196,30 @@ __global__ void __launch_bounds__(THREADS) k_norm(Norm a) {
         for (int j = 0; j < 8; j++) {
             float& x = v[at][j];
             squares = fmaf(x, x, squares);
-            s.h = max(s.h, magnitude(x));
             x *= g[j];
-            s.v = max(s.v, magnitude(x));
+            most = larger(most, x);
         }
         s.squares += squares;
-        if (MX4) quantize8(v[at], c, a.K, blockIdx.x, q, a.blocks);
+        if (MX4) bad |= quantize8(v[at], most, c, a.K, blockIdx.x, q, a.blocks);
+        else top = larger(top, most);
     }
+    s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
     over_block<SHARES>(s);
-    const Factor f = factor_of<SHARES>(a, s, [&](float by) {
-        float sum = 0.f;
+    const Factor f = factor_of<MX4, SHARES>(a, s, [&](float by) {
+        RowStats t = {0.f, 0u};
         for (int c = threadIdx.x; c < chunks; c += blockDim.x) {
-            float h[8];
+            float h[8], part = 0.f;
             row.load_h(c * 8, true, h, true);
-            float part = 0.f;
 #pragma unroll
-            for (int j = 0; j < 8; j++) part = fmaf(h[j] * by, h[j] * by, part);
-            sum += part;
+            for (int j = 0; j < 8; j++) {
+                part = fmaf(h[j] * by, h[j] * by, part);
+                t.top = max(t.top, __float_as_uint(h[j] * by) & 0x7fffffffu);
+            }
+            t.squares += part;
         }
-        return sum;
+        return t;
     });
-    if (threadIdx.x == 0) {
-        float* out = a.scale + blockIdx.x;
-        if (!MX4) *out = f.unit == 0.f ? 0.f : (float)(f.unit * f.r);
-        else if (isnan(f.unit)) *out = f.unit;
-        else *out = s.h == 0 && a.eps == 0.f ? 0.f : (float)f.r;        // 1 / sqrt(0): a row of zeros with eps 0
-    }
+    if (threadIdx.x == 0) a.scale[blockIdx.x] = f.scale;
     if (MX4) return;
     const float inverse = __fdiv_rn(1.f, f.unit);
 #pragma unroll
