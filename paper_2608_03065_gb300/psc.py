@@ -132,13 +132,20 @@ def _check(code: int):
         raise PscError(code, (load().psc_last_error() or b"").decode(errors="replace"))
 
 
+_current = None         # of the current device, the current stream's handle
+
+
 def _stream(stream) -> int | None:
+    global _current
     if stream is None:
-        import torch
-        try:                                # the current stream's handle without a Stream object around it
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
-        except AttributeError:
-            return torch.cuda.current_stream().cuda_stream or None
+        if _current is None:
+            import torch
+            try:                            # without a Stream object around it
+                raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+                _current = lambda: raw(device())  # noqa: E731
+            except AttributeError:
+                _current = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+        return _current() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -479,6 +486,17 @@ def _rows(t, dtype, name, rows=None, cols=None):
     return _ptr(t, dtype, name), stride if r > 1 else max(c, stride)
 
 
+def _at(t, dtype, name, rows, cols):
+    """What _rows gives, without its questions one by one for a tensor that is as it should be
+    (of the time of a small call the questions are a large part)."""
+    shape = t.shape
+    if t.dtype is dtype and t.is_cuda and len(shape) == 2 and shape[0] == rows and shape[1] >= cols:
+        stride, unit = t.stride()
+        if unit == 1:
+            return t.data_ptr(), stride if rows > 1 else max(shape[1], stride)
+    return _rows(t, dtype, name, rows, cols)
+
+
 def _mask_ptr(bitmask, B, V):
     import torch
     if bitmask is None:
@@ -513,16 +531,17 @@ def psc_quantize_rows(x, q, scale, stream=None):
 
 
 def _norm_inputs(x, residual, sum_out, gain):
-    """What the two norms share: x's sizes and type, and the inputs' addresses and strides."""
+    """What the two norms share: x's sizes, and the inputs' addresses and strides."""
     import torch
-    if x.dim() != 2:
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2:
         raise ValueError("x must be a 2-D tensor")
-    T, K = x.shape
+    T, K = shape
     code = _dtype_code(x)
-    px, sx = _rows(x, None, "x", T, K)
-    pr, sr = (None, 0) if residual is None else _rows(residual, x.dtype, "residual", T, K)
-    ps, ss = (None, 0) if sum_out is None else _rows(sum_out, x.dtype, "sum_out", T, K)
-    return T, K, code, (px, code, sx, pr, sr, ps, ss, _ptr(gain, torch.float32, "gain", K))
+    px, sx = _at(x, dtype, "x", T, K)
+    pr, sr = (None, 0) if residual is None else _at(residual, dtype, "residual", T, K)
+    ps, ss = (None, 0) if sum_out is None else _at(sum_out, dtype, "sum_out", T, K)
+    return T, K, (px, code, sx, pr, sr, ps, ss, _ptr(gain, torch.float32, "gain", K))
 
 
 def psc_norm_quantize_rows(x, q, scale, gain=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None):
@@ -531,10 +550,10 @@ def psc_norm_quantize_rows(x, q, scale, gain=None, eps: float = 1e-6, residual=N
     them of activations; sum_out := h.  x, residual, sum_out bf16 or f32 [T, K], gain f32 [K];
     gain, residual and sum_out may be None, and sum_out may be x or residual."""
     import torch
-    T, K, _, inputs = _norm_inputs(x, residual, sum_out, gain)
-    pq, sq = _rows(q, torch.int8, "q", T, K)
-    _check(load().psc_norm_quantize_rows(*inputs, eps, T, K, pq, sq, _ptr(scale, torch.float32, "scale", T),
-                                         _stream(stream)))
+    T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
+    pq, sq = _at(q, torch.int8, "q", T, K)
+    _check((_lib or load()).psc_norm_quantize_rows(*inputs, eps, T, K, pq, sq, _ptr(scale, torch.float32, "scale", T),
+                                                   _stream(stream)))
 
 
 def psc_head_work_bytes(T: int, V: int, K: int, aligned: bool = True) -> int:
@@ -653,41 +672,46 @@ def psc_mx4_block_bytes(rows: int, K: int) -> int:
 def _mx4(q, blocks, rows, K, name):
     """(address of the codes, their stride, address of the exponents)."""
     import torch
-    pq, sq = _rows(q, torch.uint8, name, rows, psc_mx4_row_bytes(K))
-    return pq, sq, _ptr(blocks, torch.uint8, f"{name}'s blocks", load().psc_mx4_block_bytes(rows, K))
+    pq, sq = _at(q, torch.uint8, name, rows, (K + 31) // 32 * 16)
+    return pq, sq, _ptr(blocks, torch.uint8, f"{name}'s blocks", (rows + 127) // 128 * ((K + 127) // 128) * 512)
 
 
 def psc_quantize_mx4(x, q, blocks, stream=None):
     """q, blocks := the rows of x (bf16 or f32 [T, K]) in microscaled 4-bit floating point:
     uint8 [T, >= psc_mx4_row_bytes(K)] codes, two a byte, and uint8 [psc_mx4_block_bytes(T, K)]
     exponents of blocks of 32 columns.  Activations by token, or weights by output channel."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("x must be a 2-D tensor")
-    T, K = x.shape
+    T, K = shape
     code = _dtype_code(x)
-    px, sx = _rows(x, None, "x", T, K)
-    _check(load().psc_quantize_mx4(px, code, sx, T, K, *_mx4(q, blocks, T, K, "q"), _stream(stream)))
+    px, sx = _at(x, x.dtype, "x", T, K)
+    pq, sq, pb = _mx4(q, blocks, T, K, "q")
+    _check((_lib or load()).psc_quantize_mx4(px, code, sx, T, K, pq, sq, pb, _stream(stream)))
 
 
 def psc_dequantize_mx4(q, blocks, y, scale=None, stream=None):
     """y := the values that q and blocks hold (bf16 or f32 [T, K]), times scale (f32 [T])."""
     import torch
-    if y.dim() != 2:
+    shape = y.shape
+    if len(shape) != 2:
         raise ValueError("y must be a 2-D tensor")
-    T, K = y.shape
+    T, K = shape
     code = _dtype_code(y)
-    py, sy = _rows(y, None, "y", T, K)
-    _check(load().psc_dequantize_mx4(*_mx4(q, blocks, T, K, "q"), _ptr(scale, torch.float32, "scale", T), T, K, py,
-                                     code, sy, _stream(stream)))
+    py, sy = _at(y, y.dtype, "y", T, K)
+    pq, sq, pb = _mx4(q, blocks, T, K, "q")
+    _check((_lib or load()).psc_dequantize_mx4(pq, sq, pb, _ptr(scale, torch.float32, "scale", T), T, K, py, code, sy,
+                                               _stream(stream)))
 
 
 def psc_norm_quantize_mx4(x, q, blocks, scale, gain=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None):
     """psc_norm_quantize_rows with an output in 4 bits: q and blocks as psc_quantize_mx4 makes
     them of h * gain, scale (f32 [T]) := 1 / sqrt(mean h^2 + eps)."""
     import torch
-    T, K, _, inputs = _norm_inputs(x, residual, sum_out, gain)
-    _check(load().psc_norm_quantize_mx4(*inputs, eps, T, K, *_mx4(q, blocks, T, K, "q"),
-                                        _ptr(scale, torch.float32, "scale", T), _stream(stream)))
+    T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
+    pq, sq, pb = _mx4(q, blocks, T, K, "q")
+    _check((_lib or load()).psc_norm_quantize_mx4(*inputs, eps, T, K, pq, sq, pb, _ptr(scale, torch.float32, "scale", T),
+                                                  _stream(stream)))
 
 
 def psc_head_mx4_work_bytes(T: int, V: int, K: int) -> int:
@@ -703,20 +727,21 @@ def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_
     least psc_head_mx4_work_bytes(T, V, K) bytes to reuse (one is taken from torch's allocator
     for the call otherwise).  Returns the workspace, for psc_head_faults."""
     import torch
-    if q.dim() != 2 or w.dim() != 2:
+    qs, ws = q.shape, w.shape
+    if len(qs) != 2 or len(ws) != 2:
         raise ValueError("q and w must be 2-D tensors")
-    T, V = q.shape[0], w.shape[0]
+    T, V = qs[0], ws[0]
+    lib = _lib or load()
     code = _dtype_code(logits)
     pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
     pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
-    pl, sl = _rows(logits, None, "logits", T, V)
-    n = load().psc_head_mx4_work_bytes(T, V, K)
+    pl, sl = _at(logits, logits.dtype, "logits", T, V)
     pm = _mask_ptr(bitmask, T, V)
     if work is None:
-        work = _workspace(n, logits.device, stream)
-    _check(load().psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
-                                      _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
-                                      _ptr(work, torch.uint8, "work", n), work.numel(), _stream(stream)))
+        work = _workspace(lib.psc_head_mx4_work_bytes(T, V, K), logits.device, stream)
+    _check(lib.psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
+                                   _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
+                                   _ptr(work, torch.uint8, "work", 256), work.numel(), _stream(stream)))
     return work
 
 
