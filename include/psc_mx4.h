@@ -50,9 +50,6 @@ psc_status psc_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_stride
 psc_status psc_dequantize_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_blocks, const float* d_scale,
                               int32_t T, int32_t K, void* d_y, psc_dtype dtype, int64_t row_stride, void* stream);
 
-/* Bytes of workspace that psc_head_logits_mx4 needs (256 for sizes that it refuses). */
-int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K);
-
 /* The vocabulary projection in 4 bits, under the mask:
  *     logits[t][v] = (sum_k x_t[k] w_v[k]) * scale[t] * w_scale[v]
  * over the values of both matrices, where the mask allows v for row t, -inf elsewhere; rows of
@@ -62,15 +59,17 @@ int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K);
  *   d_scale         : float [T], d_w_scale : float [V], each NULL for ones
  *   d_bitmask       : uint32 [T][ceil(V/32)], or NULL (every token allowed)
  *   d_logits        : [T] rows of row_stride elements of dtype; columns >= V are left as they are
- *   d_work          : at least psc_head_mx4_work_bytes bytes, 256-byte aligned; calls that overlap
- *                     on the GPU need workspaces of their own.  Its first int32 is afterwards the
- *                     number of blocks in which a bounded wait gave up (some logits are then not
- *                     written), 0 otherwise
+ * A block in which a bounded wait gives up (a pipeline fault) leaves some logits unwritten and
+ * is counted (psc_mx4_faults).
  * PSC_ERR_LIMIT: K over 131,072, T over 2^24 or V over 2^30. */
 psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
                                int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                                const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
-                               psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes, void* stream);
+                               psc_dtype dtype, int64_t row_stride, void* stream);
+
+/* Blocks of psc_head_logits_mx4 on the current device in which a bounded wait gave up, since the
+ * library was loaded or the last reset; synchronises the stream (not while it is captured). */
+psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,6 +12,9 @@ const char* const ME = "psc_head_logits_mx4";
 constexpr int MAX_K = 131072;
 constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, rounded up to tiles, in 32 bits
 
+// Blocks in which a bounded wait gave up.
+__device__ int g_faults;
+
 struct Head {
     const uint8_t* q;
     int64_t q_stride;
@@ -27,133 +30,6 @@ struct Head {
     int W;                              // mask words of a row
     int64_t row_stride;
 };
-
-// Eight codes as bytes of twice their values, in order.
-__device__ __forceinline__ uint2 doubled8(uint32_t codes) {
-    const uint32_t m = codes & 0x77777777u, side = ((codes >> 1) & 0x44444444u) | 0x32103210u;
-    uint2 out;
-    // the magnitudes' bytes, their negatives, and of each byte the one that its sign picks
-    out.x = __byte_perm(__byte_perm(0x03020100u, 0x0C080604u, m), __byte_perm(0xFDFEFF00u, 0xF4F8FAFCu, m), side);
-    out.y = __byte_perm(__byte_perm(0x03020100u, 0x0C080604u, m >> 16), __byte_perm(0xFDFEFF00u, 0xF4F8FAFCu, m >> 16),
-                        side >> 16);
-    return out;
-}
-// The smaller and the larger; NaN if one is.
-__device__ __forceinline__ float min_nan(float a, float b) {
-    float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-
-// k_mx4_rows: a warp per 32 vocabulary rows (a word of the masks), of which those that some of up
-// to N tokens allow are read, 4 at once, a lane per block of 32 columns.  A block's products are
-// summed in whole numbers (quarters; exact), then scaled: the smaller power of two first, so that
-// nothing leaves f32 on the way to a sum that does not.
-constexpr int ROWS = 4;
-constexpr int ROWS_THREADS = 256;
-
-template <typename T, int N>
-__global__ void __launch_bounds__(ROWS_THREADS) k_mx4_rows(Head h, int t0, T* logits) {
-    extern __shared__ __align__(16) uint8_t dyn[];
-    __shared__ float s_out[ROWS_THREADS / 32][N * 32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int nb = (h.K + 31) / 32, n_tiles = (h.K + 127) / 128, n = min(N, h.T - t0);
-    uint2* xs = reinterpret_cast<uint2*>(dyn);                          // [N][4][nb]: doubled codes, eight a piece
-    float* xe = reinterpret_cast<float*>(dyn + (size_t)N * nb * 32);    // [N][nb]
-    dep_wait();
-    dep_launch();
-    for (int i = threadIdx.x; i < N * nb * 4; i += ROWS_THREADS) {
-        const int t = i / (nb * 4), c = i - t * nb * 4, b = c >> 2;
-        const bool there = t < n;
-        xs[(t * 4 + (c & 3)) * nb + b] =
-            there ? doubled8(*reinterpret_cast<const uint32_t*>(h.q + (size_t)(t0 + t) * h.q_stride + c * 4))
-                  : make_uint2(0, 0);
-        if (!(c & 3)) xe[t * nb + b] = there ? block_value(h.q_blocks[block_at(t0 + t, b, n_tiles)]) : 0.f;
-    }
-    __syncthreads();
-    float* out = s_out[warp];
-    for (int item = blockIdx.x * (ROWS_THREADS / 32) + warp; item < h.W; item += gridDim.x * (ROWS_THREADS / 32)) {
-        const int v0 = item * 32, v = v0 + lane;
-        const uint32_t mine = lane >= n ? 0u : h.bitmask ? h.bitmask[(size_t)(t0 + lane) * h.W + item] : FULL;
-        uint32_t rows = __reduce_or_sync(FULL, mine);
-        if (h.V - v0 < 32) rows &= (1u << (h.V - v0)) - 1;
-        while (rows) {
-            int r[ROWS];
-#pragma unroll
-            for (int i = 0; i < ROWS; i++) {
-                r[i] = __ffs(rows) - 1;             // -1: none left
-                rows &= rows - 1;
-            }
-            float acc[ROWS][N] = {};
-            for (int b = lane; b < nb; b += 32) {
-                uint4 w[ROWS];
-                float e[ROWS];
-#pragma unroll
-                for (int i = 0; i < ROWS; i++) {
-                    w[i] = make_uint4(0, 0, 0, 0);
-                    e[i] = 0.f;
-                    if (r[i] < 0) continue;
-                    w[i] = __ldcs(reinterpret_cast<const uint4*>(h.w + (size_t)(v0 + r[i]) * h.w_stride + b * 16));
-                    e[i] = block_value(h.w_blocks[block_at(v0 + r[i], b, n_tiles)]);
-                }
-#pragma unroll
-                for (int i = 0; i < ROWS; i++) {
-                    const uint32_t c[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                    uint2 d[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) d[j] = doubled8(c[j]);
-#pragma unroll
-                    for (int t = 0; t < N; t++) {
-                        int s = 0;
-#pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            const uint2 x = xs[(t * 4 + j) * nb + b];
-                            s = __dp4a((int)d[j].x, (int)x.x, s);
-                            s = __dp4a((int)d[j].y, (int)x.y, s);
-                        }
-                        const float f = xe[t * nb + b];
-                        acc[i][t] = fmaf((float)s * 0.25f * min_nan(e[i], f), max_nan(e[i], f), acc[i][t]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < ROWS; i++)
-#pragma unroll
-                for (int t = 0; t < N; t++) {
-                    float s = acc[i][t];
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
-                    if (lane == 0 && r[i] >= 0) out[t * 32 + r[i]] = s;
-                }
-        }
-        __syncwarp();
-        const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
-        for (int t = 0; t < n; t++) {
-            const uint32_t bits = __shfl_sync(FULL, mine, t);
-            const float st = h.scale ? h.scale[t0 + t] : 1.f;
-            if (v < h.V)
-                store_f32(logits + (size_t)(t0 + t) * h.row_stride + v,
-                          (bits >> lane) & 1 ? out[t * 32 + lane] * st * sw : __uint_as_float(0xFF800000u));
-        }
-        __syncwarp();
-    }
-}
-
-template <typename T, int N>
-psc_status head_rows(const Head& h, T* logits, cudaStream_t cs) {
-    const int nb = (h.K + 31) / 32;
-    for (int t0 = 0; t0 < h.T; t0 += N) {
-        psc_status s = ops_launch(k_mx4_rows<T, N>, dim3(std::min((h.W + 7) / 8, current_sms() * 2)), ROWS_THREADS,
-                                  (size_t)N * nb * 36, 1, cs, "k_mx4_rows", h, t0, logits);
-        if (s != PSC_OK) return s;
-    }
-    return PSC_OK;
-}
 
 // ------------------------------------------------------------ the tensor-core path
 //
@@ -261,13 +137,13 @@ constexpr int VT = 128;                       // vocabulary rows of a tile
 constexpr int W_CODES = VT * KS / 2;
 constexpr int MAX_STAGES = 11;
 constexpr int GROUPS = FEW / 32 / 2;          // a warp's groups of 32 tokens
+constexpr int MAX_TILES = 8192;               // of a block, for which masks are looked at beforehand
 
 struct Few {
     int N, n_vt;                              // tokens, rounded up; tiles of vocabulary rows
     int stages, stage_bytes;
     int acc;                                  // TMEM columns of an accumulator
     size_t smem;
-    int64_t flags_at, bytes;                  // in the workspace: the fault word, the tiles' flags
 };
 
 Few few_of(int T, int V) {
@@ -277,30 +153,9 @@ Few few_of(int T, int V) {
     p.stage_bytes = W_CODES + p.N * KS / 2 + 4 * SF;
     p.acc = (p.N + 31) / 32 * 32;
     // a stage's exponents have TMEM columns of their own, free when the stage is
-    p.stages = std::min({MAX_STAGES, (SMEM_MAX - 6 * 1024) / p.stage_bytes, (512 - 2 * p.acc) / 16});
+    p.stages = std::min({MAX_STAGES, (SMEM_MAX - 7 * 1024) / p.stage_bytes, (512 - 2 * p.acc) / 16});
     p.smem = 1024 + (size_t)p.stages * p.stage_bytes;
-    p.flags_at = 256;
-    p.bytes = p.flags_at + ((int64_t)p.n_vt + 255) / 256 * 256;
     return p;
-}
-
-// How many rows of each tile some token allows, and the fault word.
-__global__ void __launch_bounds__(256) k_mx4_flags(Head h, int n_vt, int* faults, uint8_t* flags) {
-    dep_wait();
-    dep_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    const int vt = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (vt >= n_vt) return;
-    uint32_t any = 0;
-    // a lane per word of a token's four, eight tokens at a time
-    for (int t = lane >> 2; t < h.T; t += 8) {
-        const int wi = vt * 4 + (lane & 3);
-        if (wi < h.W) any |= h.bitmask[(size_t)t * h.W + wi];
-    }
-#pragma unroll
-    for (int o = 4; o < 32; o <<= 1) any |= __shfl_xor_sync(FULL, any, o);
-    const int rows = __reduce_add_sync(FULL, lane < 4 ? __popc(any) : 0);
-    if (lane == 0) flags[vt] = (uint8_t)rows;
 }
 
 // What the epilogue knows of a token: its scale, and the mask's word for the warp's 32 vocabulary rows.
@@ -354,16 +209,32 @@ __device__ __forceinline__ void store_group(T* out, int64_t stride, const uint32
     }
 }
 
+// -inf for `n` neighbouring logits of each of T tokens, by the epilogue's warps.
+template <typename T>
+__device__ __forceinline__ void forbid_tile(T* out, int64_t stride, int tokens, int n, bool wide) {
+    constexpr uint32_t NONE = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    constexpr int EACH = 16 / sizeof(T);
+    const int warp = (threadIdx.x >> 5) - FIRST, lane = threadIdx.x & 31;
+    if (wide && n == VT) {
+        constexpr int LANES = VT / EACH;              // of a token
+        for (int t = warp * (32 / LANES) + lane / LANES; t < tokens; t += EPILOGUE * (32 / LANES))
+            *reinterpret_cast<uint4*>(out + (size_t)t * stride + lane % LANES * EACH) = make_uint4(NONE, NONE, NONE, NONE);
+    } else {
+        for (int t = warp; t < tokens; t += EPILOGUE)
+            for (int i = lane; i < n; i += 32) store_f32(out + (size_t)t * stride + i, __uint_as_float(0xFF800000u));
+    }
+}
+
 template <typename T, bool MASKED>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
                                                             const __grid_constant__ CUtensorMap w_blocks_map,
                                                             const __grid_constant__ CUtensorMap x_blocks_map, Head h,
-                                                            T* logits, Few p, int* faults, const uint8_t* flags,
-                                                            bool even) {
+                                                            T* logits, Few p, bool even, bool wide) {
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) uint64_t s_bars[2 * MAX_STAGES + 5];
     __shared__ __align__(16) Token s_tokens[EPILOGUE][GROUPS * 32];
+    __shared__ uint32_t s_active[MASKED ? MAX_TILES / 32 : 1];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -390,18 +261,38 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
     const int n_k = (h.K + KS - 1) / KS;
+    if (!MASKED && warp == 0 && lane == 0)            // the first stages' weights on their way to the L2
+        for (int i = 0; i < min(p.stages, n_k); i++)
+            asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(&w_map), "r"(i * 128),
+                         "r"((int)blockIdx.x * VT)
+                         : "memory");
     dep_wait();
     dep_launch();
-    // A block that fails has polled for a good part of a second before it counts itself.
-    if (!MASKED && blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
-    auto is_active = [&](int vt) { return !MASKED || flags[vt] != 0; };
+    // Of this block's tiles, those in which some token is allowed; the others' weights are not read.
+    const int mine = (p.n_vt - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    if (MASKED) {
+        for (int i = threadIdx.x; i < MAX_TILES / 32; i += MMA_THREADS) s_active[i] = mine > MAX_TILES ? FULL : 0u;
+        __syncthreads();
+        for (int i = warp; i < min(mine, MAX_TILES); i += MMA_THREADS / 32) {
+            uint32_t any = 0;
+            // a lane per word of a token's four, eight tokens at a time
+            const int wi = (blockIdx.x + i * gridDim.x) * 4 + (lane & 3);
+            if (wi < h.W)
+                for (int t = lane >> 2; t < h.T; t += 8) any |= h.bitmask[(size_t)t * h.W + wi];
+            if (__any_sync(FULL, any) && lane == 0) atomicOr(&s_active[i / 32], 1u << (i & 31));
+        }
+        __syncthreads();
+    }
+    auto is_active = [&](int i) { return !MASKED || mine > MAX_TILES || (s_active[i / 32] >> (i & 31) & 1); };
+    const int vt0 = blockIdx.x, vt_step = gridDim.x;  // tile i of this block
 
     // Loads one part of every stage: a box at (x, y), x + step, ... of a map; y_step: from tile to tile.
     auto load_part = [&](const CUtensorMap* map, int step, int y_step, int part, int bytes) {
         Place at;
         int c = 0;
-        for (int vt = blockIdx.x; vt < p.n_vt && !*failed; vt += gridDim.x) {
-            if (!is_active(vt)) continue;
+        for (int i = 0; i < mine && !*failed; i++) {
+            if (!is_active(i)) continue;
+            const int vt = vt0 + i * vt_step;
             for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
                 if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
                 mbar_arrive_tx(full(at.s), bytes);
@@ -425,8 +316,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
         const uint32_t lo = (base & 0x3FFFF) >> 4, step = p.stage_bytes / 16, idesc = instruction(VT, p.N);
         Place at, acc;
         bool ok = true;
-        for (int vt = blockIdx.x; vt < p.n_vt && ok; vt += gridDim.x) {
-            if (!is_active(vt)) continue;
+        for (int i = 0; i < mine && ok; i++) {
+            if (!is_active(i)) continue;
             if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
             const uint32_t d = tmem + acc.s * p.acc;
             for (int k = 0; k < n_k; k++, at.next(p.stages)) {
@@ -451,8 +342,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
         const int quad = warp & 3, part = (warp - FIRST) >> 2;      // of every two groups of 32 tokens, this warp's
         Token* tokens = s_tokens[warp - FIRST];
         Place acc;
-        for (int vt = blockIdx.x; vt < p.n_vt; vt += gridDim.x) {
-            const bool active = is_active(vt);
+        for (int it = 0; it < mine; it++) {
+            const int vt = vt0 + it * vt_step;
+            if (!is_active(it)) {
+                forbid_tile(logits + vt * VT, h.row_stride, h.T, min(VT, h.V - vt * VT), wide);
+                continue;
+            }
             const int v = vt * VT + quad * 32 + lane, wi = vt * 4 + quad;
             // the tile's scales and mask words, read while its products run
             const float sw = v < h.V && h.w_scale ? h.w_scale[v] : 1.f;
@@ -463,47 +358,39 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
                 if (t >= h.T) continue;
                 tokens[i * 32 + lane] = {
                     h.scale ? h.scale[t] : 1.f,
-                    !MASKED ? FULL : active && wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u};
+                    !MASKED ? FULL : wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u};
             }
             __syncwarp();
-            if (active) {
-                if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            }
+            if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int i = 0; i < GROUPS; i++) {
                 const int t = (2 * i + part) * 32;
                 if (t >= h.T) break;
-                uint32_t y[32] = {};
-                if (active) {
-                    const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + t;
-                    tmem_load16(from, y);
-                    tmem_load16(from + 16, y + 16);
-                    tmem_wait(y);
-                }
+                uint32_t y[32];
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc.s * p.acc + t;
+                tmem_load16(from, y);
+                tmem_load16(from + 16, y + 16);
+                tmem_wait(y);
                 store_group<MASKED>(logits + (size_t)t * h.row_stride + v, h.row_stride, y, tokens + i * 32, sw,
                                     min(32, h.T - t), h.V - v, even);
             }
-            if (active) {
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(acc_empty(acc.s));
-                acc.next(2);
-            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_empty(acc.s));
+            acc.next(2);
         }
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == 1) tmem_free<false>(tmem);
-    if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
+    if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
 
 template <typename T>
-psc_status head_few(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+psc_status head_few(const Head& h, T* logits, cudaStream_t cs) {
     const Few p = few_of(h.T, h.V);
-    int* faults = (int*)work;
-    uint8_t* flags = work + p.flags_at;
     CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
     const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, VT) ||
@@ -513,15 +400,11 @@ psc_status head_few(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
         !tensor_map(&x_blocks_map, CU_TENSOR_MAP_DATA_TYPE_UINT32, h.q_blocks, n_tiles * SF / 4, 1, n_tiles * SF, 256, 1,
                     CU_TENSOR_MAP_SWIZZLE_NONE))
         return ops_fail(PSC_ERR_CUDA, ME, "cuTensorMapEncodeTiled failed");
-    if (h.bitmask) {
-        psc_status s = ops_launch(k_mx4_flags, dim3((p.n_vt + 7) / 8), 256, 0, 1, cs, "k_mx4_flags", h, p.n_vt, faults,
-                                  flags);
-        if (s != PSC_OK) return s;
-    }
-    const bool even = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 4);
+    const int64_t stride = h.row_stride * (int64_t)sizeof(T);
+    const bool even = is_aligned(logits, stride, 4), wide = is_aligned(logits, stride, 16);
     return ops_launch(h.bitmask ? k_mx4_few<T, true> : k_mx4_few<T, false>, dim3(std::min(p.n_vt, current_sms())),
                       MMA_THREADS, p.smem, 1, cs, "k_mx4_few", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p,
-                      faults, (const uint8_t*)flags, even);
+                      even, wide);
 }
 
 // ------------------------------------------------------------------------ many tokens
@@ -579,7 +462,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                                                              const __grid_constant__ CUtensorMap x_map,
                                                              const __grid_constant__ CUtensorMap w_blocks_map,
                                                              const __grid_constant__ CUtensorMap x_blocks_map, Head h,
-                                                             T* logits, int n_mt, int n_vt, int* faults, bool wide) {
+                                                             T* logits, int n_mt, int n_vt, bool wide) {
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 3 * B_SLOTS + 5];
     __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
@@ -621,8 +504,6 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     const int a_slots = stay ? n_k : B_SLOTS;
     dep_wait();
     dep_launch();
-    // A block that fails has polled for a good part of a second before it counts itself.
-    if (blockIdx.x == 0 && threadIdx.x == 0) *faults = 0;
     // This pair's items, in order: up to TOGETHER tiles of tokens at a time, a pair staying with one of
     // them; pairs that share a tile of vocabulary rows come to it at the same time.  f(tile of tokens, of
     // vocabulary rows, whether its tokens are new, whether they are not used after it) says whether to go on.
@@ -839,11 +720,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     __syncthreads();
     cluster_sync();                                   // nothing of this block is used by the other any more
     if (warp == 1) tmem_free<true>(tmem);
-    if (threadIdx.x == 0 && s_failed) atomicAdd(faults, 1);
+    if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
 
 template <typename T>
-psc_status head_many(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
+psc_status head_many(const Head& h, T* logits, cudaStream_t cs) {
     CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
     const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
     if (!tensor_map(&w_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, h.w, row, h.V, h.w_stride, 128, NV / 2) ||
@@ -857,27 +738,22 @@ psc_status head_many(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
     const bool wide = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 16);
     const int pairs = (int)std::min<int64_t>((int64_t)n_mt * n_vt, std::max(1, current_sms() / 2));
     return ops_launch(h.bitmask ? k_mx4_many<T, true> : k_mx4_many<T, false>, dim3(2 * pairs), MMA_THREADS, MANY_SMEM, 2,
-                      cs, "k_mx4_many", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, n_mt, n_vt, (int*)work, wide);
+                      cs, "k_mx4_many", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, n_mt, n_vt, wide);
 }
 
 template <typename T>
-psc_status head(const Head& h, T* logits, uint8_t* work, cudaStream_t cs) {
-    return h.T <= FEW ? head_few(h, logits, work, cs) : head_many(h, logits, work, cs);
+psc_status head(const Head& h, T* logits, cudaStream_t cs) {
+    return h.T <= FEW ? head_few(h, logits, cs) : head_many(h, logits, cs);
 }
 
 }  // namespace
 
 extern "C" {
 
-int64_t psc_head_mx4_work_bytes(int32_t T, int32_t V, int32_t K) {
-    if (T <= 0 || V <= 0 || K <= 0 || T > MAX_T || V > MAX_V || K > MAX_K || T > FEW) return 256;
-    return few_of(T, V).bytes;
-}
-
 psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
                                int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                                const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
-                               psc_dtype dtype, int64_t row_stride, void* d_work, int64_t work_bytes, void* stream) {
+                               psc_dtype dtype, int64_t row_stride, void* stream) {
     if (T < 0 || V <= 0 || K <= 0 || row_stride < V || !is_dtype(dtype) || !d_w || !d_w_blocks ||
         (T && (!d_q || !d_q_blocks || !d_logits)))
         return ops_fail(PSC_ERR_ARG, ME, "bad arguments");
@@ -886,12 +762,23 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
     if (!is_mx4(d_w, w_stride, d_w_blocks, K) || (T && !is_mx4(d_q, q_stride, d_q_blocks, K)))
         return ops_fail(PSC_ERR_ARG, ME, "codes or blocks with a bad stride or alignment");
     if (T == 0) return PSC_OK;
-    if (!d_work || (uintptr_t)d_work % 256 || work_bytes < psc_head_mx4_work_bytes(T, V, K))
-        return ops_fail(PSC_ERR_ARG, ME, "workspace missing, unaligned or too small");
     const Head h{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
                  (V + 31) / 32, row_stride};
-    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
-    return head(h, (float*)d_logits, (uint8_t*)d_work, (cudaStream_t)stream);
+    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (cudaStream_t)stream);
+    return head(h, (float*)d_logits, (cudaStream_t)stream);
+}
+
+psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream) {
+    const char* me = "psc_mx4_faults";
+    if (!h_faults) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    cudaStream_t cs = (cudaStream_t)stream;
+    psc_status s = ops_check(cudaMemcpyFromSymbolAsync(h_faults, g_faults, 4, 0, cudaMemcpyDeviceToHost, cs), me);
+    if (s == PSC_OK) s = ops_check(cudaStreamSynchronize(cs), me);
+    if (s == PSC_OK && reset) {
+        static const int none = 0;
+        s = ops_check(cudaMemcpyToSymbolAsync(g_faults, &none, 4, 0, cudaMemcpyHostToDevice, cs), me);
+    }
+    return s;
 }
 
 }  // extern "C"

@@ -32,8 +32,8 @@ EXPORTED = ["psc_compile", "psc_destroy", "psc_last_error", "psc_info", "psc_sta
 EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "psc_process_logits",
                 "psc_sample_work_bytes", "psc_sample"]
 # include/psc_mx4.h: the vocabulary projection in microscaled 4-bit floating point
-EXPORTED_MX4 = ["psc_mx4_block_bytes", "psc_quantize_mx4", "psc_dequantize_mx4", "psc_head_mx4_work_bytes",
-                "psc_head_logits_mx4"]
+EXPORTED_MX4 = ["psc_mx4_block_bytes", "psc_quantize_mx4", "psc_dequantize_mx4", "psc_head_logits_mx4",
+                "psc_mx4_faults"]
 # include/psc_norm.h: the norm in front of either projection
 EXPORTED_NORM = ["psc_norm_quantize_rows", "psc_norm_quantize_mx4"]
 NOALLOC_MAX_ROWS = 16384
@@ -114,8 +114,8 @@ def load(path: str = LIB_PATH):
         "psc_quantize_mx4": (i32, [vp, i32, i64, i32, i32, vp, i64, vp, vp]),
         "psc_dequantize_mx4": (i32, [vp, i64, vp, vp, i32, i32, vp, i32, i64, vp]),
         "psc_norm_quantize_mx4": (i32, [vp, i32, i64, vp, i64, vp, i64, vp, f32, i32, i32, vp, i64, vp, vp, vp]),
-        "psc_head_mx4_work_bytes": (i64, [i32, i32, i32]),
-        "psc_head_logits_mx4": (i32, [vp, i64, vp, vp, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, i64, vp, i64, vp]),
+        "psc_head_logits_mx4": (i32, [vp, i64, vp, vp, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, i64, vp]),
+        "psc_mx4_faults": (i32, [vp, i32, vp]),
         "psc_sample_work_bytes": (i64, [i32]),
         "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
@@ -714,35 +714,30 @@ def psc_norm_quantize_mx4(x, q, blocks, scale, gain=None, eps: float = 1e-6, res
                                                   _stream(stream)))
 
 
-def psc_head_mx4_work_bytes(T: int, V: int, K: int) -> int:
-    """Bytes of workspace for psc_head_logits_mx4."""
-    return load().psc_head_mx4_work_bytes(T, V, K)
-
-
-def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_scale=None, bitmask=None, work=None,
-                        stream=None):
+def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_scale=None, bitmask=None, stream=None):
     """logits[:, :V] := (x @ w.T) * scale[:, None] * w_scale over the values of matrices in 4 bits,
     x [T, K] (q, q_blocks) and w [V, K] (w, w_blocks), -inf where bitmask forbids.  scale f32 [T]
-    and w_scale f32 [V] may be None; logits bf16 or f32 [T, >=V].  work: a uint8 tensor of at
-    least psc_head_mx4_work_bytes(T, V, K) bytes to reuse (one is taken from torch's allocator
-    for the call otherwise).  Returns the workspace, for psc_head_faults."""
+    and w_scale f32 [V] may be None; logits bf16 or f32 [T, >=V]."""
     import torch
     qs, ws = q.shape, w.shape
     if len(qs) != 2 or len(ws) != 2:
         raise ValueError("q and w must be 2-D tensors")
     T, V = qs[0], ws[0]
-    lib = _lib or load()
     code = _dtype_code(logits)
     pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
     pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
     pl, sl = _at(logits, logits.dtype, "logits", T, V)
-    pm = _mask_ptr(bitmask, T, V)
-    if work is None:
-        work = _workspace(lib.psc_head_mx4_work_bytes(T, V, K), logits.device, stream)
-    _check(lib.psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
-                                   _ptr(w_scale, torch.float32, "w_scale", V), V, K, pm, pl, code, sl,
-                                   _ptr(work, torch.uint8, "work", 256), work.numel(), _stream(stream)))
-    return work
+    _check((_lib or load()).psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
+                                                _ptr(w_scale, torch.float32, "w_scale", V), V, K,
+                                                _mask_ptr(bitmask, T, V), pl, code, sl, _stream(stream)))
+
+
+def psc_mx4_faults(reset: bool = False, stream=None) -> int:
+    """Blocks of psc_head_logits_mx4 on the current device in which a bounded wait gave up, since
+    the library was loaded or the last reset (synchronises the stream); not 0: logits are missing."""
+    out = ctypes.c_int32(0)
+    _check(load().psc_mx4_faults(ctypes.byref(out), 1 if reset else 0, _stream(stream)))
+    return out.value
 
 
 def psc_sample_work_bytes(B: int) -> int:

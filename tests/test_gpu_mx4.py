@@ -99,10 +99,10 @@ def _head_case(psc, T, V, K, dtype, mask, scales=True, pad=0, out_pad=0, spread=
     sx, sw = rng.uniform(0.01, 0.1, T).astype(np.float32), rng.uniform(0.1, 10, V).astype(np.float32)
     allowed = _mask(rng, mask, T, V)
     big = torch.full((T, V + out_pad), 7.0, dtype=DT[dtype], device="cuda")
-    work = psc.psc_head_logits_mx4(*_matrix(psc, qc, qe, K, pad), *_matrix(psc, wc, we, K, pad), big[:, :V], K,
-                                   scale=_dev(sx) if scales else None, w_scale=_dev(sw) if scales else None,
-                                   bitmask=None if allowed is None else _pack(allowed), stream=stream)
-    assert psc.psc_head_faults(work, stream=stream) == 0
+    psc.psc_head_logits_mx4(*_matrix(psc, qc, qe, K, pad), *_matrix(psc, wc, we, K, pad), big[:, :V], K,
+                            scale=_dev(sx) if scales else None, w_scale=_dev(sw) if scales else None,
+                            bitmask=None if allowed is None else _pack(allowed), stream=stream)
+    assert psc.psc_mx4_faults(stream=stream) == 0
     got = _f64(big)
     assert (got[:, V:] == 7).all()
     got = got[:, :V]
@@ -203,7 +203,7 @@ def test_what_is_not_a_number_stays_in_its_rows(psc, T, masked):  # noqa: F811
         assert (got[~a] == NEG).all()
 
 
-def test_workspace_streams_and_graphs(psc):  # noqa: F811
+def test_streams_and_graphs(psc):  # noqa: F811
     rng = np.random.default_rng(9)
     for T, V, K, mask in [(1, 3000, 512, None), (12, 3000, 512, "tight"), (90, 3000, 512, "mixed"), (400, 3000, 512, None)]:
         x, w = rng.standard_normal((T, K)).astype(np.float32), rng.standard_normal((V, K)).astype(np.float32)
@@ -214,21 +214,20 @@ def test_workspace_streams_and_graphs(psc):  # noqa: F811
         def buffers():
             return (torch.zeros(T, n, dtype=torch.uint8, device="cuda"), _blocks_of(psc, T, K),
                     torch.zeros(V, n, dtype=torch.uint8, device="cuda"), _blocks_of(psc, V, K),
-                    torch.zeros(T, V, device="cuda"),
-                    torch.full((psc.psc_head_mx4_work_bytes(T, V, K),), 255, dtype=torch.uint8, device="cuda"))
+                    torch.zeros(T, V, device="cuda"))
 
         def call(o, stream=None):
             # the weights are made by the kernel in front, so that nothing may be read before it is done
             psc.psc_quantize_mx4(xd, o[0], o[1], stream=stream)
             psc.psc_quantize_mx4(wd, o[2], o[3], stream=stream)
-            psc.psc_head_logits_mx4(o[0], o[1], o[2], o[3], o[4], K, bitmask=bm, work=o[5], stream=stream)
+            psc.psc_head_logits_mx4(o[0], o[1], o[2], o[3], o[4], K, bitmask=bm, stream=stream)
 
         a, b, c = buffers(), buffers(), buffers()
         call(a)
         torch.cuda.synchronize()
         side = torch.cuda.Stream()
         call(b, side)
-        assert psc.psc_head_faults(b[5], stream=side) == 0
+        assert psc.psc_mx4_faults(stream=side) == 0
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             call(c)

@@ -50,10 +50,9 @@ def _dequantize(q=P, q_stride=32, blocks=P, scale=None, T=4, K=64, y=P, dtype=1,
     return "psc_dequantize_mx4", (q, q_stride, blocks, scale, T, K, y, dtype, stride, None)
 
 
-def _head(q=P, q_stride=32, qb=P, T=4, w=P, w_stride=32, wb=P, V=100, K=64, out=P, dtype=1, stride=100, work=P,
-          n=1 << 40):
+def _head(q=P, q_stride=32, qb=P, T=4, w=P, w_stride=32, wb=P, V=100, K=64, out=P, dtype=1, stride=100):
     return "psc_head_logits_mx4", (q, q_stride, qb, None, T, w, w_stride, wb, None, V, K, None, out, dtype, stride,
-                                   work, n, None)
+                                   None)
 
 
 M = 2 ** 31 - 1
@@ -80,8 +79,8 @@ M = 2 ** 31 - 1
     (_head(q=None), ARG), (_head(qb=None), ARG), (_head(w=None), ARG), (_head(wb=None), ARG), (_head(out=None), ARG),
     (_head(dtype=2), ARG), (_head(stride=99), ARG), (_head(T=-1), ARG), (_head(V=0), ARG), (_head(K=0), ARG),
     (_head(q=P + 8), ARG), (_head(q_stride=24), ARG), (_head(w=P + 8), ARG), (_head(w_stride=40), ARG),
-    (_head(qb=P + 8), ARG), (_head(wb=P + 2), ARG), (_head(work=None), ARG), (_head(work=P + 16), ARG),
-    (_head(n=255), ARG), (_head(K=131073, q_stride=65552, w_stride=65552), LIMIT), (_head(T=2 ** 24 + 1), LIMIT),
+    (_head(qb=P + 8), ARG), (_head(wb=P + 2), ARG),
+    (("psc_mx4_faults", (None, 0, None)), ARG), (_head(K=131073, q_stride=65552, w_stride=65552), LIMIT), (_head(T=2 ** 24 + 1), LIMIT),
     (_head(V=2 ** 30 + 1, stride=M), LIMIT),
 ])
 def test_wrong_arguments_are_refused(psc, call, code):  # noqa: F811
@@ -92,7 +91,7 @@ def test_wrong_arguments_are_refused(psc, call, code):  # noqa: F811
 
 @pytest.mark.parametrize("call", [_norm("rows", x=None, q=None, scale=None, T=0), _norm("mx4", x=None, scale=None, T=0),
                                   _quantize(x=None, T=0), _dequantize(y=None, T=0),
-                                  _head(q=None, qb=None, out=None, work=None, T=0)])
+                                  _head(q=None, qb=None, out=None, T=0)])
 def test_empty_batches_are_nothing_to_do(psc, call):  # noqa: F811
     name, args = call
     assert getattr(psc.load(), name)(*args) == 0
@@ -103,10 +102,6 @@ def test_sizes(psc):  # noqa: F811
                        (M, 2 ** 30, 2 ** 24 * 2 ** 23 * 512), (0, 5, 0), (5, 0, 0), (-1, 5, 0), (5, 2 ** 30 + 1, 0)]:
         assert psc.psc_mx4_block_bytes(rows, K) == n
     assert [psc.psc_mx4_row_bytes(k) for k in (1, 32, 33, 2048)] == [16, 16, 32, 1024]
-    for T, V, K in [(M, 100, 64), (4, M, 64), (4, 100, M), (0, 1, 1), (2 ** 24 + 1, 1, 1), (1, 2 ** 30 + 1, 1)]:
-        assert psc.psc_head_mx4_work_bytes(T, V, K) == 256
-    for T, V, K in [(1, 1, 1), (2 ** 24, 1, 131072), (1, 2 ** 30, 131072), (1024, 262144, 2048)]:
-        assert psc.psc_head_mx4_work_bytes(T, V, K) >= 256
 
 
 def test_binding_refuses_tensors_of_the_wrong_kind(psc):  # noqa: F811
