@@ -424,12 +424,12 @@ constexpr int MT = 256;                       // tokens of a tile
 constexpr int NV = 192;                       // vocabulary rows of a tile
 constexpr int TOGETHER = 4;                   // tiles of tokens that are worked on at the same time
 constexpr int A_CODES = MT / 2 * KS / 2, A_BYTES = A_CODES + 2 * SF;
-constexpr int B_CODES = NV / 2 * KS / 2, B_BYTES = B_CODES + 4 * SF;
-constexpr int A_SLOTS = 8, B_SLOTS = 5;
+constexpr int B_CODES = NV / 2 * KS / 2, B_EXPS = 4 * SF;
+constexpr int A_SLOTS = 8, B_SLOTS = 5;       // (of the weights: their codes, their exponents, TMEM columns for them)
 constexpr int SF_COLS = 24;                   // TMEM columns of a stage's exponents
 static_assert(2 * NV + B_SLOTS * SF_COLS <= 512, "TMEM");
 constexpr int STAGING = 32 * 64;              // a warp's, in the epilogue
-constexpr size_t MANY_SMEM = 1024 + A_SLOTS * A_BYTES + B_SLOTS * B_BYTES + EPILOGUE * STAGING;
+constexpr size_t MANY_SMEM = 1024 + A_SLOTS * A_BYTES + B_SLOTS * (B_CODES + B_EXPS) + EPILOGUE * STAGING;
 
 // A tile into this block's shared memory; the barrier is the pair's first block's.
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -464,21 +464,24 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                                                              const __grid_constant__ CUtensorMap x_blocks_map, Head h,
                                                              T* logits, int n_mt, int n_vt, bool wide) {
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 3 * B_SLOTS + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 5 * B_SLOTS + 5];
     __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = (int)cluster_rank();
-    // slots start at multiples of 1024 bytes: codes, then exponents
+    // slots start at multiples of 1024 bytes: the tokens' codes and exponents, the weights' codes, their exponents
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, b_base = base + A_SLOTS * A_BYTES;
+    const uint32_t e_base = b_base + B_SLOTS * B_CODES;
     const uint32_t bars = smem_addr(s_bars);
     auto a_full = [&](int s) { return bars + 8 * s; };
     auto a_empty = [&](int s) { return bars + 8 * (A_SLOTS + s); };
     auto b_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + s); };
     auto b_empty = [&](int s) { return bars + 8 * (2 * A_SLOTS + B_SLOTS + s); };
-    auto sf_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 2 * B_SLOTS + s); };
-    constexpr int LAST = 2 * A_SLOTS + 3 * B_SLOTS;
+    auto e_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 2 * B_SLOTS + s); };
+    auto e_empty = [&](int s) { return bars + 8 * (2 * A_SLOTS + 3 * B_SLOTS + s); };
+    auto sf_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 4 * B_SLOTS + s); };
+    constexpr int LAST = 2 * A_SLOTS + 5 * B_SLOTS;
     auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
     auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
     const uint32_t drained = bars + 8 * (LAST + 4);
@@ -486,7 +489,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     if (threadIdx.x == 0) {
         s_failed = 0;
         for (int s = 0; s < A_SLOTS; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
-        for (int s = 0; s < B_SLOTS; s++) mbar_init(b_full(s), 2), mbar_init(b_empty(s), 1), mbar_init(sf_full(s), 1);
+        for (int s = 0; s < B_SLOTS; s++) {
+            mbar_init(b_full(s), 1), mbar_init(b_empty(s), 1);
+            mbar_init(e_full(s), 1), mbar_init(e_empty(s), 1), mbar_init(sf_full(s), 1);
+        }
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * 2);
         mbar_init(drained, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -501,7 +507,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     volatile int* failed = &s_failed;
     const int n_k = (h.K + KS - 1) / KS;
     const bool stay = n_k <= A_SLOTS;
-    const int a_slots = stay ? n_k : B_SLOTS;
+    const int a_slots = stay ? n_k : A_SLOTS;
     dep_wait();
     dep_launch();
     // This pair's items, in order: up to TOGETHER tiles of tokens at a time, a pair staying with one of
@@ -542,10 +548,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     };
 
     if (warp == 0 && lane == 0) {
-        load_part(&w_map, 128, b_base, B_BYTES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false,
+        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false,
                   [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); });
     } else if (warp == 2 && lane == 0) {
-        load_part(&w_blocks_map, 256, b_base + B_CODES, B_BYTES, B_SLOTS, b_full(0), b_empty(0), 4 * SF, false,
+        load_part(&w_blocks_map, 256, e_base, B_EXPS, B_SLOTS, e_full(0), e_empty(0), B_EXPS, false,
                   [&](int, int vt) { return vt * NV / 128; });
     } else if (warp == 3 && lane == 0) {
         load_part(&x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
@@ -555,22 +561,24 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                   [&](int mt, int) { return mt * 2 + side; });
     } else if (warp == 5 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
-        // issues, for both blocks.
+        // issues, for both blocks.  Exponents go to TMEM as soon as the products of B_SLOTS stages before are
+        // done with theirs, while the codes that take those products' place are still on their way.
         const bool issuer = elect_one();
-        const uint32_t a_lo = ((base + A_CODES) & 0x3FFFF) >> 4, b_lo = ((b_base + B_CODES) & 0x3FFFF) >> 4;
-        Place unit, at_b;                             // unit: the first slot of the tile's tokens
+        const uint32_t a_lo = ((base + A_CODES) & 0x3FFFF) >> 4, e_lo = (e_base & 0x3FFFF) >> 4;
+        Place unit, at;                               // unit: the first slot of the tile's tokens
         each([&](int, int, bool fresh, bool last) {
             Place at_a = unit;
-            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(B_SLOTS)) {
-                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_BYTES / 16);
-                const uint32_t sf = tmem + 2 * NV + at_b.s * SF_COLS;
-                if (!(fresh ? warp_wait2(a_full(at_a.s), at_a.parity, b_full(at_b.s), at_b.parity, failed)
-                            : warp_wait(b_full(at_b.s), at_b.parity, failed)))
+            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at.next(B_SLOTS)) {
+                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), e = e_lo + at.s * (B_EXPS / 16);
+                const uint32_t sf = tmem + 2 * NV + at.s * SF_COLS;
+                if (!warp_wait2(e_full(at.s), at.parity, b_empty(at.s), at.parity ^ 1, failed) ||
+                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed)))
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
-                    copy_stage<true, 2>(a, b, sf);
-                    commit_here(sf_full(at_b.s));
+                    copy_stage<true, 2>(a, e, sf);
+                    commit_here(sf_full(at.s));
+                    mma_commit<true>(e_empty(at.s));
                 }
             }
             if (last) unit = at_a;
@@ -581,15 +589,16 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
         const uint32_t a_lo = (base & 0x3FFFF) >> 4, b_lo = (b_base & 0x3FFFF) >> 4;
         Place unit, at_b, acc;
         bool ok = true;
-        each([&](int, int vt, bool, bool last) {
+        each([&](int, int vt, bool fresh, bool last) {
             const uint32_t idesc = instruction(MT, rows_of(vt)), d = tmem + acc.s * NV, shift = vt * NV % 128 / 32;
             Place at_a = unit;
             if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) return false;
             for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(B_SLOTS)) {
-                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_BYTES / 16);
+                const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_CODES / 16);
                 const uint32_t sf = tmem + 2 * NV + at_b.s * SF_COLS;
-                // exponents that are in TMEM came with the codes, in both blocks
-                if (!(ok = warp_wait(sf_full(at_b.s), at_b.parity, failed))) return false;
+                ok = warp_wait2(sf_full(at_b.s), at_b.parity, b_full(at_b.s), at_b.parity, failed) &&
+                     (!fresh || warp_wait(a_full(at_a.s), at_a.parity, failed));
+                if (!ok) return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
                     mma_stage<true, 2>(a, b, sf, shift, d, idesc, k);
@@ -610,7 +619,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     } else if (warp >= FIRST) {
         constexpr int COLS = 64 / sizeof(T);          // logits of a token that go out together
         const int quad = warp & 3, part = (warp - FIRST) >> 2;
-        const uint32_t staging = b_base + B_SLOTS * B_BYTES + (warp - FIRST) * STAGING;
+        const uint32_t staging = e_base + B_SLOTS * B_EXPS + (warp - FIRST) * STAGING;
         const uint32_t own = staging + lane * 64, own_swap = (lane >> 1) & 3;       // 16-byte pieces change places by rows
         float* scales = s_scale[warp - FIRST];
         Place acc;
