@@ -118,6 +118,10 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem) {
     if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
+// A tile on its way to the L2.
+__device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 // Lets the copies in flight land: those of the last `slots` of c uses of a ring.
 __device__ __forceinline__ void drain(uint32_t full0, int c, int slots) {
     for (int i = max(0, c - slots); i < c; i++)
@@ -263,9 +267,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     const int n_k = (h.K + KS - 1) / KS;
     if (!MASKED && warp == 0 && lane == 0)            // the first stages' weights on their way to the L2
         for (int i = 0; i < min(p.stages, n_k); i++)
-            asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(&w_map), "r"(i * 128),
-                         "r"((int)blockIdx.x * VT)
-                         : "memory");
+            prefetch_tile(&w_map, i * 128, (int)blockIdx.x * VT);
     dep_wait();
     dep_launch();
     // Of this block's tiles, those in which some token is allowed; the others' weights are not read.
@@ -526,9 +528,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     // vocabulary rows of a tile that the products take: both halves in whole sixteens
     auto rows_of = [&](int vt) { return (min(NV, h.V - vt * NV) + 31) / 32 * 32; };
 
-    // Loads one part of every stage of the items for which `when` holds.
+    // Loads one part of every stage (of tokens that stay, of the first item with them); also(k, x, tile of vocabulary
+    // rows) after each.
     auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
-                         uint32_t empty0, int bytes, bool tokens, auto row_of) {
+                         uint32_t empty0, int bytes, bool tokens, auto row_of, auto also) {
         const uint32_t there0 = at_first(full0);
         Place at;
         int c = 0;
@@ -540,6 +543,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                 if (!mbar_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) return false;
                 if (side == 0) mbar_arrive_tx(full0 + 8 * at.s, 2 * bytes);
                 load_tile(to0 + at.s * slot_bytes, map, x, y, there0 + 8 * at.s);
+                also(k, vt);
             }
             return !*failed;
         });
@@ -547,18 +551,29 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
         if (*failed && side == 0) drain(full0, c, slots);
     };
 
+    auto nothing = [](int, int) {};
+    auto codes_row = [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); };
     if (warp == 0 && lane == 0) {
-        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false,
-                  [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); });
+        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false, codes_row, nothing);
     } else if (warp == 2 && lane == 0) {
+        // One of the pairs that come to a tile together has it brought to the L2 an item before: the slots cover
+        // the L2's latency, not the memory's.
+        const int c = min(min(TOGETHER, n_mt), all), per = all / c;
+        const bool first = c > 1 && me % c == 0;
         load_part(&w_blocks_map, 256, e_base, B_EXPS, B_SLOTS, e_full(0), e_empty(0), B_EXPS, false,
-                  [&](int, int vt) { return vt * NV / 128; });
+                  [&](int, int vt) { return vt * NV / 128; },
+                  [&](int k, int vt) {
+                      const int next = vt + per;
+                      if (!first || next >= n_vt) return;
+                      prefetch_tile(&w_map, k * 128, codes_row(0, next));
+                      if (side == 0) prefetch_tile(&w_blocks_map, k * 256, next * NV / 128);
+                  });
     } else if (warp == 3 && lane == 0) {
         load_part(&x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
-                  [&](int mt, int) { return mt * MT + side * (MT / 2); });
+                  [&](int mt, int) { return mt * MT + side * (MT / 2); }, nothing);
     } else if (warp == 4 && lane == 0) {
         load_part(&x_blocks_map, 256, base + A_CODES, A_BYTES, a_slots, a_full(0), a_empty(0), 2 * SF, true,
-                  [&](int mt, int) { return mt * 2 + side; });
+                  [&](int mt, int) { return mt * 2 + side; }, nothing);
     } else if (warp == 5 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
         // issues, for both blocks.  Exponents go to TMEM as soon as the products of B_SLOTS stages before are
