@@ -290,27 +290,31 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
 
     // Loads one part of every stage: a box at (x, y), x + step, ... of a map; y_step: from tile to tile.
     auto load_part = [&](const CUtensorMap* map, int step, int y_step, int part, int bytes) {
+        const bool issuer = elect_one();
         Place at;
         int c = 0;
         for (int i = 0; i < mine && !*failed; i++) {
             if (!is_active(i)) continue;
             const int vt = vt0 + i * vt_step;
             for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
-                if (!mbar_wait(empty(at.s), at.parity ^ 1, failed)) break;
-                mbar_arrive_tx(full(at.s), bytes);
-                tma_2d(base + at.s * p.stage_bytes + part, map, k * step, vt * y_step, full(at.s));
+                const uint32_t to = base + at.s * p.stage_bytes + part, bar = full(at.s);
+                if (!warp_wait(empty(at.s), at.parity ^ 1, failed)) break;
+                if (issuer) {
+                    mbar_arrive_tx(bar, bytes);
+                    tma_2d(to, map, k * step, vt * y_step, bar);
+                }
             }
         }
-        if (*failed) drain(full(0), c, p.stages);
+        if (*failed && issuer) drain(full(0), c, p.stages);
     };
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         load_part(&w_map, 128, VT, 0, W_CODES);
-    } else if (warp == 2 && lane == 0) {
+    } else if (warp == 2) {
         load_part(&x_map, 128, 0, W_CODES, x_codes);
-    } else if (warp == 3 && lane == 0) {
+    } else if (warp == 3) {
         load_part(&w_blocks_map, 256, 1, W_CODES + x_codes, 2 * SF);
-    } else if (warp == 4 && lane == 0) {
+    } else if (warp == 4) {
         load_part(&x_blocks_map, 256, 0, W_CODES + x_codes + 2 * SF, 2 * SF);
     } else if (warp == 1) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
@@ -469,7 +473,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 5 * B_SLOTS + 5];
     __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_failed;
+    __shared__ int s_failed, s_item;                  // how many items' weights have begun to be loaded
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = (int)cluster_rank();
     // slots start at multiples of 1024 bytes: the tokens' codes and exponents, the weights' codes, their exponents
@@ -489,7 +493,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     const uint32_t drained = bars + 8 * (LAST + 4);
 
     if (threadIdx.x == 0) {
-        s_failed = 0;
+        s_failed = 0, s_item = 0;
         for (int s = 0; s < A_SLOTS; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
         for (int s = 0; s < B_SLOTS; s++) {
             mbar_init(b_full(s), 1), mbar_init(b_empty(s), 1);
@@ -528,11 +532,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     // vocabulary rows of a tile that the products take: both halves in whole sixteens
     auto rows_of = [&](int vt) { return (min(NV, h.V - vt * NV) + 31) / 32 * 32; };
 
-    // Loads one part of every stage (of tokens that stay, of the first item with them); also(k, x, tile of vocabulary
-    // rows) after each.
+    // Loads one part of every stage (of tokens that stay, of the first item with them).
     auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
-                         uint32_t empty0, int bytes, bool tokens, auto row_of, auto also) {
+                         uint32_t empty0, int bytes, bool tokens, auto row_of) {
         const uint32_t there0 = at_first(full0);
+        const bool issuer = elect_one();
         Place at;
         int c = 0;
         each([&](int mt, int vt, bool fresh, bool) {
@@ -540,40 +544,45 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             const int y = row_of(mt, vt);
             int x = 0;
             for (int k = 0; k < n_k; k++, c++, x += step, at.next(slots)) {
-                if (!mbar_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) return false;
-                if (side == 0) mbar_arrive_tx(full0 + 8 * at.s, 2 * bytes);
-                load_tile(to0 + at.s * slot_bytes, map, x, y, there0 + 8 * at.s);
-                also(k, vt);
+                const uint32_t to = to0 + at.s * slot_bytes, own = full0 + 8 * at.s, bar = there0 + 8 * at.s;
+                if (!warp_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) return false;
+                if (issuer) {
+                    if (side == 0) mbar_arrive_tx(own, 2 * bytes);
+                    load_tile(to, map, x, y, bar);
+                }
             }
             return !*failed;
         });
         // the first block sees both blocks' copies land, and the second does not end before it
-        if (*failed && side == 0) drain(full0, c, slots);
+        if (*failed && side == 0 && issuer) drain(full0, c, slots);
     };
 
-    auto nothing = [](int, int) {};
     auto codes_row = [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); };
-    if (warp == 0 && lane == 0) {
-        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false, codes_row, nothing);
-    } else if (warp == 2 && lane == 0) {
-        // One of the pairs that come to a tile together has it brought to the L2 an item before: the slots cover
-        // the L2's latency, not the memory's.
-        const int c = min(min(TOGETHER, n_mt), all), per = all / c;
-        const bool first = c > 1 && me % c == 0;
-        load_part(&w_blocks_map, 256, e_base, B_EXPS, B_SLOTS, e_full(0), e_empty(0), B_EXPS, false,
-                  [&](int, int vt) { return vt * NV / 128; },
-                  [&](int k, int vt) {
-                      const int next = vt + per;
-                      if (!first || next >= n_vt) return;
-                      prefetch_tile(&w_map, k * 128, codes_row(0, next));
-                      if (side == 0) prefetch_tile(&w_blocks_map, k * 256, next * NV / 128);
-                  });
-    } else if (warp == 3 && lane == 0) {
+    if (warp == 0) {
+        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false, codes_row);
+    } else if (warp == 2) {
+        load_part(&w_blocks_map, 256, e_base, B_EXPS, B_SLOTS, e_full(0), e_empty(0), B_EXPS, false, [&](int, int vt) {
+            *const_cast<volatile int*>(&s_item) = s_item + 1;
+            return vt * NV / 128;
+        });
+    } else if (warp == 6 && lane == 0) {
+        // Brings the next item's weights to the L2 when an item's are loaded: the slots cover the L2's latency, not
+        // the memory's.  Pairs that come to a tile together share its stages out.
+        int item = 0;
+        each([&](int mt, int vt, bool, bool) {
+            const int c = min(min(TOGETHER, n_mt - mt / TOGETHER * TOGETHER), all), next = vt + all / c;
+            item++;
+            if (c == 1 || next >= n_vt) return true;
+            for (int i = 0; i < (1 << 16) && *const_cast<volatile int*>(&s_item) < item && !*failed; i++) __nanosleep(100);
+            for (int k = me % c; k < n_k; k += c) prefetch_tile(&w_map, k * 128, codes_row(0, next));
+            return !*failed;
+        });
+    } else if (warp == 3) {
         load_part(&x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
-                  [&](int mt, int) { return mt * MT + side * (MT / 2); }, nothing);
-    } else if (warp == 4 && lane == 0) {
+                  [&](int mt, int) { return mt * MT + side * (MT / 2); });
+    } else if (warp == 4) {
         load_part(&x_blocks_map, 256, base + A_CODES, A_BYTES, a_slots, a_full(0), a_empty(0), 2 * SF, true,
-                  [&](int mt, int) { return mt * 2 + side; }, nothing);
+                  [&](int mt, int) { return mt * 2 + side; });
     } else if (warp == 5 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
         // issues, for both blocks.  Exponents go to TMEM as soon as the products of B_SLOTS stages before are
