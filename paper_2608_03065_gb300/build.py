@@ -7,6 +7,7 @@ import fcntl
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -18,6 +19,7 @@ CXX_SOURCES = ["grammar.cpp", "lexer.cpp", "lalr.cpp", "classifier.cpp", "bottom
 CU_SOURCES = ["psc_capi.cu", "process.cu", "sample.cu", "head.cu", "norm.cu", "mx4.cu",
               "mx4_head.cu"]
 GENCODE = "arch=compute_103a,code=sm_103a"
+MARSHAL = os.path.join(HERE, "_marshal.so")      # the binding's Python module (psc.py does without it where Python.h is missing)
 
 
 def _nvcc() -> str:
@@ -64,6 +66,11 @@ def _build_locked(force: bool, verbose: bool) -> str:
         if force or _stale(o, [s] + headers + ops_headers):
             jobs.append([nvcc, "-gencode", GENCODE, "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
                          "-I", INCLUDE, "-c", s, "-o", o])
+
+    python = sysconfig.get_paths()["include"]
+    marshal = os.path.join(CSRC, "marshal.cpp")
+    if os.path.exists(os.path.join(python, "Python.h")) and (force or _stale(MARSHAL, [marshal])):
+        jobs.append(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", python, marshal, "-o", MARSHAL])
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)

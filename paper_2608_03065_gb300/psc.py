@@ -64,6 +64,28 @@ class InfoT(ctypes.Structure):
 
 
 _lib = None
+_marshal = None          # csrc/marshal.cpp, where it is built: the small calls' tensors taken apart in C
+
+
+def _load_marshal(lib, device=None):
+    global _marshal
+    path = os.path.join(_HERE, "_marshal.so")
+    if not os.path.exists(path):
+        return
+    try:
+        import importlib.util
+        import torch
+        spec = importlib.util.spec_from_file_location("_marshal", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError:                     # no torch, or another Python's module
+        return
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+    module.setup((torch.bfloat16, torch.float32, torch.int8, torch.uint8, torch.int32),
+                 tuple(address(f) for f in (lib.psc_norm_quantize_rows, lib.psc_norm_quantize_mx4, lib.psc_quantize_mx4,
+                                            lib.psc_dequantize_mx4, lib.psc_head_logits_mx4)), _stream,
+                 device or getattr(torch._C, "_cuda_getDevice", _device))
+    _marshal = module
 
 
 def load(path: str = LIB_PATH):
@@ -124,12 +146,25 @@ def load(path: str = LIB_PATH):
         f.restype = res
         f.argtypes = args
     _lib = lib
+    _load_marshal(lib)
     return lib
 
 
 def _check(code: int):
     if code != 0:
         raise PscError(code, (load().psc_last_error() or b"").decode(errors="replace"))
+
+
+def _device() -> int:
+    """The current device."""
+    import torch
+    return torch.cuda.current_device()
+
+
+def _here(t, name):
+    """Kernels run on the current device: a tensor of another one is refused."""
+    if t.is_cuda and t.get_device() != _device():
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, and the current device is cuda:{_device()}")
 
 
 _current = None         # of the current device, the current stream's handle
@@ -538,6 +573,7 @@ def _norm_inputs(x, residual, sum_out, gain):
         raise ValueError("x must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(x)
+    _here(x, "x")
     px, sx = _at(x, dtype, "x", T, K)
     pr, sr = (None, 0) if residual is None else _at(residual, dtype, "residual", T, K)
     ps, ss = (None, 0) if sum_out is None else _at(sum_out, dtype, "sum_out", T, K)
@@ -549,6 +585,10 @@ def psc_norm_quantize_rows(x, q, scale, gain=None, eps: float = 1e-6, residual=N
     8-bit integers (int8 [T, K]) with a scale each (f32 [T]), as psc_quantize_rows makes
     them of activations; sum_out := h.  x, residual, sum_out bf16 or f32 [T, K], gain f32 [K];
     gain, residual and sum_out may be None, and sum_out may be x or residual."""
+    if _marshal is not None:
+        code = _marshal.norm_rows(x, q, scale, gain, eps, residual, sum_out, stream)
+        if code is not None:
+            return _check(code) if code else None
     import torch
     T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
     pq, sq = _at(q, torch.int8, "q", T, K)
@@ -680,11 +720,16 @@ def psc_quantize_mx4(x, q, blocks, stream=None):
     """q, blocks := the rows of x (bf16 or f32 [T, K]) in microscaled 4-bit floating point:
     uint8 [T, >= psc_mx4_row_bytes(K)] codes, two a byte, and uint8 [psc_mx4_block_bytes(T, K)]
     exponents of blocks of 32 columns.  Activations by token, or weights by output channel."""
+    if _marshal is not None:
+        code = _marshal.quantize_mx4(x, q, blocks, stream)
+        if code is not None:
+            return _check(code) if code else None
     shape = x.shape
     if len(shape) != 2:
         raise ValueError("x must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(x)
+    _here(x, "x")
     px, sx = _at(x, x.dtype, "x", T, K)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
     _check((_lib or load()).psc_quantize_mx4(px, code, sx, T, K, pq, sq, pb, _stream(stream)))
@@ -692,12 +737,17 @@ def psc_quantize_mx4(x, q, blocks, stream=None):
 
 def psc_dequantize_mx4(q, blocks, y, scale=None, stream=None):
     """y := the values that q and blocks hold (bf16 or f32 [T, K]), times scale (f32 [T])."""
+    if _marshal is not None:
+        code = _marshal.dequantize_mx4(q, blocks, y, scale, stream)
+        if code is not None:
+            return _check(code) if code else None
     import torch
     shape = y.shape
     if len(shape) != 2:
         raise ValueError("y must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(y)
+    _here(y, "y")
     py, sy = _at(y, y.dtype, "y", T, K)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
     _check((_lib or load()).psc_dequantize_mx4(pq, sq, pb, _ptr(scale, torch.float32, "scale", T), T, K, py, code, sy,
@@ -707,6 +757,10 @@ def psc_dequantize_mx4(q, blocks, y, scale=None, stream=None):
 def psc_norm_quantize_mx4(x, q, blocks, scale, gain=None, eps: float = 1e-6, residual=None, sum_out=None, stream=None):
     """psc_norm_quantize_rows with an output in 4 bits: q and blocks as psc_quantize_mx4 makes
     them of h * gain, scale (f32 [T]) := 1 / sqrt(mean h^2 + eps)."""
+    if _marshal is not None:
+        code = _marshal.norm_mx4(x, q, blocks, scale, gain, eps, residual, sum_out, stream)
+        if code is not None:
+            return _check(code) if code else None
     import torch
     T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
@@ -718,12 +772,17 @@ def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_
     """logits[:, :V] := (x @ w.T) * scale[:, None] * w_scale over the values of matrices in 4 bits,
     x [T, K] (q, q_blocks) and w [V, K] (w, w_blocks), -inf where bitmask forbids.  scale f32 [T]
     and w_scale f32 [V] may be None; logits bf16 or f32 [T, >=V]."""
+    if _marshal is not None:
+        code = _marshal.head_logits_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask, stream)
+        if code is not None:
+            return _check(code) if code else None
     import torch
     qs, ws = q.shape, w.shape
     if len(qs) != 2 or len(ws) != 2:
         raise ValueError("q and w must be 2-D tensors")
     T, V = qs[0], ws[0]
     code = _dtype_code(logits)
+    _here(q, "q")
     pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
     pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
     pl, sl = _at(logits, logits.dtype, "logits", T, V)

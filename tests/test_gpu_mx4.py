@@ -244,3 +244,52 @@ def test_streams_and_graphs(psc):  # noqa: F811
             call(b, side)
         side.synchronize()
         assert torch.equal(a[4], b[4])
+
+
+def test_binding_without_its_module(psc, monkeypatch):  # noqa: F811
+    """The same calls from Python alone, for tensors that are plainly in order and for others."""
+    rng = np.random.default_rng(2)
+    for T, V, K, pad in [(1, 300, 256, 0), (1, 300, 250, 8), (9, 300, 256, 8), (140, 200, 100, 0)]:
+        x = _strided(rng.standard_normal((T, K)), torch.bfloat16, pad, 0)[1]
+        w = _dev(rng.standard_normal((V, K)).astype(np.float32))
+        n = psc.psc_mx4_row_bytes(K)
+        bm = _pack(rng.random((T, V)) < 0.5)
+
+        def run():
+            q, b, s = torch.zeros(T, n + 16, dtype=torch.uint8, device="cuda"), _blocks_of(psc, T, K), torch.zeros(T, device="cuda")
+            wq, wb = torch.zeros(V, n, dtype=torch.uint8, device="cuda"), _blocks_of(psc, V, K)
+            h, y, out = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, K, device="cuda"), torch.zeros(T, V, device="cuda")
+            q8, s8 = torch.zeros(T, K, dtype=torch.int8, device="cuda"), torch.zeros(T, device="cuda")
+            psc.psc_quantize_mx4(w, wq, wb)
+            psc.psc_norm_quantize_mx4(x, q, b, s, residual=x, sum_out=h)
+            psc.psc_norm_quantize_rows(x, q8, s8, residual=x, sum_out=h)
+            psc.psc_dequantize_mx4(q, b, y, scale=s)
+            psc.psc_head_logits_mx4(q, b, wq, wb, out, K, scale=s, bitmask=bm)
+            torch.cuda.synchronize()
+            return wq, wb, q, b, s, h, y, out, q8, s8
+
+        with monkeypatch.context() as m:
+            m.setattr(psc, "_marshal", None)
+            a = run()
+        assert psc._marshal is not None
+        for u, v in zip(a, run()):
+            assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("module", [True, False])
+def test_tensors_of_another_device_are_refused(psc, monkeypatch, module):  # noqa: F811
+    if not module:
+        monkeypatch.setattr(psc, "_marshal", None)
+    else:
+        psc._load_marshal(psc.load(), lambda: 3)
+    monkeypatch.setattr(psc, "_device", lambda: 3)
+    x, q, s = torch.zeros(2, 64, device="cuda"), torch.zeros(2, 32, dtype=torch.uint8, device="cuda"), torch.zeros(2, device="cuda")
+    b, q8, y = _blocks_of(psc, 2, 64), torch.zeros(2, 64, dtype=torch.int8, device="cuda"), torch.zeros(2, 2, device="cuda")
+    try:
+        for call in (lambda: psc.psc_norm_quantize_rows(x, q8, s), lambda: psc.psc_norm_quantize_mx4(x, q, b, s),
+                     lambda: psc.psc_quantize_mx4(x, q, b), lambda: psc.psc_dequantize_mx4(q, b, x),
+                     lambda: psc.psc_head_logits_mx4(q, b, q, b, y, 64)):
+            with pytest.raises(ValueError, match="current device"):
+                call()
+    finally:
+        psc._load_marshal(psc.load())
