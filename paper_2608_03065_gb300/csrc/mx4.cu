@@ -55,40 +55,54 @@ __device__ __forceinline__ float2 values2(uint32_t codes) {
     return __half22float2(*reinterpret_cast<const __half2*>(&pair));
 }
 
+// WIDE false: chunks at columns 8 c - shift, as y's rows lie (load8_at); their codes come from two words, their
+// exponents from up to two blocks.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) k_dequantize_mx4(const uint8_t* q, int64_t q_stride, const uint8_t* blocks,
-                                                        const float* scale, uint32_t rows, int n_tiles,
-                                                        uint32_t rows_step, int K,
-                                                        T* y, int64_t stride) {
-    const Lane l = lane_of(n_tiles, rows_step);
-    const bool inside = l.there && l.c * 8 < K;
+                                                        const float* scale, uint32_t rows, int n_tiles, int lane_tiles,
+                                                        uint32_t rows_step, int K, T* y, int64_t stride) {
+    const Lane l = lane_of(lane_tiles, rows_step);
+    const int words = (K + 31) / 32 * 4;
     dep_wait();
     dep_launch();
-    for (uint32_t r0 = l.row; __any_sync(FULL, r0 < rows); r0 += rows_step * AT_ONCE) {
-        uint32_t codes[AT_ONCE], byte[AT_ONCE];
+    if (!l.there) return;
+    for (uint32_t r0 = l.row; r0 < rows; r0 += rows_step * AT_ONCE) {
+        uint32_t codes[AT_ONCE], byte[AT_ONCE], byte2[AT_ONCE];
         float s[AT_ONCE];
+        int k[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
             const uint32_t row = r0 + j * rows_step;
-            codes[j] = byte[j] = 0;
+            codes[j] = byte[j] = byte2[j] = 0;
             s[j] = 1.f;
-            if (!inside || row >= rows) continue;
-            codes[j] = *reinterpret_cast<const uint32_t*>(q + (size_t)row * q_stride + l.c * 4);
-            byte[j] = blocks[block_at(row, l.c / 4, n_tiles)];
+            const int shift = WIDE ? 0 : row_shift(y + (size_t)row * stride);
+            k[j] = l.c * 8 - shift;
+            if (k[j] >= K || row >= rows) continue;
+            const uint32_t* from = reinterpret_cast<const uint32_t*>(q + (size_t)row * q_stride);
+            if (shift) {
+                const uint32_t lo = l.c > 0 ? from[l.c - 1] : 0u, hi = l.c < words ? from[l.c] : 0u;
+                codes[j] = __funnelshift_r(lo, hi, 4 * (8 - shift));
+                byte2[j] = blocks[block_at(row, min(k[j] + 7, K - 1) / 32, n_tiles)];
+            } else {
+                codes[j] = from[l.c];
+            }
+            byte[j] = blocks[block_at(row, max(k[j], 0) / 32, n_tiles)];
             if (scale) s[j] = scale[row];
         }
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
             const uint32_t row = r0 + j * rows_step;
-            const float top = block_value(byte[j]);
+            if (k[j] >= K || row >= rows) continue;
+            const float top = block_value(byte[j]), top2 = block_value(byte2[j]);
+            const int second = WIDE || (k[j] & 31) < 25 ? 8 : 32 - (k[j] & 31);     // the first column of the next block
             float v[8];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 const float2 f = values2(codes[j] >> (8 * e));
-                v[2 * e] = f.x * top * s[j];
-                v[2 * e + 1] = f.y * top * s[j];
+                v[2 * e] = f.x * (2 * e < second ? top : top2) * s[j];
+                v[2 * e + 1] = f.y * (2 * e + 1 < second ? top : top2) * s[j];
             }
-            store8<WIDE>(y + (size_t)row * stride, l.c * 8, K, v, inside && row < rows, l.c & 15);
+            store8_at(y + (size_t)row * stride, k[j], K, true, v);
         }
     }
 }
@@ -99,8 +113,8 @@ struct Grid {
     int n_tiles, rows_step;
     dim3 blocks;
 };
-Grid grid_of(int rows, int K) {
-    const int n_tiles = (K + 127) / 128, wave = (current_sms() * 8 * 16 + n_tiles - 1) / n_tiles;
+Grid grid_of(int rows, int n_tiles) {
+    const int wave = (current_sms() * 8 * 16 + n_tiles - 1) / n_tiles;
     const int step = std::max(1, std::min(std::max(wave, rows / (AT_ONCE * TURNS)), (rows + AT_ONCE - 1) / AT_ONCE));
     return {n_tiles, step, dim3((unsigned)(((int64_t)n_tiles * step + 15) / 16))};
 }
@@ -108,7 +122,7 @@ Grid grid_of(int rows, int K) {
 template <typename T>
 psc_status quantize(const void* x, int64_t stride, int rows, int K, uint8_t* q, int64_t q_stride, uint8_t* blocks,
                     cudaStream_t cs) {
-    const Grid g = grid_of(rows, K);
+    const Grid g = grid_of(rows, (K + 127) / 128);
     return ops_launch(wide_rows<T>(x, stride, K) ? k_quantize_mx4<T, true> : k_quantize_mx4<T, false>, g.blocks, 256, 0, 1,
                       cs, "k_quantize_mx4", (const T*)x, stride, rows, g.n_tiles, g.rows_step, K, q, q_stride, blocks);
 }
@@ -116,9 +130,11 @@ psc_status quantize(const void* x, int64_t stride, int rows, int K, uint8_t* q, 
 template <typename T>
 psc_status dequantize(const uint8_t* q, int64_t q_stride, const uint8_t* blocks, const float* scale, int rows, int K,
                       void* y, int64_t stride, cudaStream_t cs) {
-    const Grid g = grid_of(rows, K);
-    return ops_launch(wide_rows<T>(y, stride, K) ? k_dequantize_mx4<T, true> : k_dequantize_mx4<T, false>, g.blocks, 256, 0,
-                      1, cs, "k_dequantize_mx4", q, q_stride, blocks, scale, rows, g.n_tiles, g.rows_step, K, (T*)y, stride);
+    const bool wide = wide_rows<T>(y, stride, K);
+    const Grid g = grid_of(rows, (K + (wide ? 0 : 7) + 127) / 128);
+    return ops_launch(wide ? k_dequantize_mx4<T, true> : k_dequantize_mx4<T, false>, g.blocks, 256, 0, 1, cs,
+                      "k_dequantize_mx4", q, q_stride, blocks, scale, rows, (K + 127) / 128, g.n_tiles, g.rows_step, K, (T*)y,
+                      stride);
 }
 
 }  // namespace

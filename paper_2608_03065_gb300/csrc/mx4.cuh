@@ -83,12 +83,11 @@ __device__ __forceinline__ void load8(const T* row, int k, int K, float v[8]) {
     unpack8(w, v, (const T*)nullptr);
 }
 
-// A chunk of N words to `to`, of which the first `valid` elements (of ES bytes) are there.  All lanes of a warp
-// call it; follows: the lane's chunk lies behind the lane's before it.  Pieces of P words start at multiples
-// of their size.
-template <int N, int P, int ES>
+// A chunk of N words to `to`, of which the first `valid` elements (of ES bytes) are there, in pieces of 16 bytes.
+// All lanes of a warp call it; follows: the lane's chunk lies behind the lane's before it.
+template <int N, int ES>
 __device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N], int valid, bool follows) {
-    constexpr int ELEMENTS = 4 * N / ES;
+    constexpr int ELEMENTS = 4 * N / ES, P = 4;
     const int lane = threadIdx.x & 31, off = (int)((uintptr_t)to & (4 * P - 1));
     const bool whole = valid >= ELEMENTS;
     const bool joins = __shfl_up_sync(FULL, whole, 1) && whole && follows && lane > 0;      // the lane before, to this one
@@ -101,8 +100,7 @@ __device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N
     for (int i = 0; i < N; i++) x[P + 1 + i] = w[i];
     auto element = [&](int e) {
         if (ES == 4) reinterpret_cast<uint32_t*>(to)[e] = w[e];
-        else if (ES == 2) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
-        else to[e] = (uint8_t)(w[e / 4] >> (8 * (e & 3)));
+        else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
     };
     // the elements one by one: all of a partial chunk, else those in pieces that are not all this lane's to store
     const int head = off == 0 || joins ? 0 : (4 * P - off) / ES, tail = off == 0 || joined ? 0 : off / ES;
@@ -112,8 +110,7 @@ __device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N
             if (whole ? e < head || e >= ELEMENTS - tail : e < valid) element(e);
     if (!whole) return;
     with_place(off >> 2, [&](auto known) {
-        constexpr int place = decltype(known)::value, from = place < P ? P + 1 - place : 1;
-        if (place >= P) return;
+        constexpr int from = P + 1 - decltype(known)::value;
 #pragma unroll
         for (int q = 0; q < N / P; q++) {
             if (q == 0 && off != 0 && !joins) continue;
@@ -122,9 +119,7 @@ __device__ __forceinline__ void store_shifted(uint8_t* to, const uint32_t (&w)[N
             for (int i = 0; i < P; i++) {               // words from off / 4 before the chunk on, the bits in front from the word before
                 y[i] = ES == 4 ? x[q * P + i + from] : __funnelshift_l(x[q * P + i + from - 1], x[q * P + i + from], (off & 3) * 8);
             }
-            uint8_t* at = to - off + q * 4 * P;
-            if (P == 4) *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
-            else *reinterpret_cast<uint2*>(at) = make_uint2(y[0], y[1]);
+            *reinterpret_cast<uint4*>(to - off + q * 4 * P) = make_uint4(y[0], y[1], y[2], y[3]);
         }
     });
 }
@@ -141,8 +136,29 @@ __device__ __forceinline__ void store8(T* row, int k, int K, const float v[8], b
         for (int i = 0; i < N / 4; i++)
             reinterpret_cast<uint4*>(row + k)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     } else {
-        store_shifted<N, 4, sizeof(T)>(reinterpret_cast<uint8_t*>(row + k), w, there ? min(8, K - k) : 0, follows);
+        store_shifted<N, sizeof(T)>(reinterpret_cast<uint8_t*>(row + k), w, there ? min(8, K - k) : 0, follows);
     }
+}
+// Where rows start at no multiple of 16 bytes, but all that a chunk takes part in starts alike (tensors of one
+// shape do), chunks may start there instead, at column 8 c - shift: all are then whole and aligned but a row's
+// first and last.  These take any columns k to k + 7, of which some may lie outside of the row, `in_place`
+// where the whole chunk is at an aligned address.
+template <typename T>
+__device__ __forceinline__ int row_shift(const T* row) {
+    return (int)((uintptr_t)row / sizeof(T) & 7);
+}
+template <typename T>
+__device__ __forceinline__ void load8_at(const T* row, int k, int K, bool in_place, float v[8]) {
+    if (in_place && k >= 0 && k + 8 <= K) return load8<true>(row, k, K, v);
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = k + j >= 0 && k + j < K ? load_f32(row + k + j) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store8_at(T* row, int k, int K, bool in_place, const float v[8]) {
+    if (in_place && k >= 0 && k + 8 <= K) return store8<true>(row, k, K, v, true, false);
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+        if (k + j >= 0 && k + j < K) store_f32(row + k + j, v[j]);
 }
 // Whether rows of these elements (none at all, too) are whole chunks at multiples of 16 bytes.
 template <typename T>

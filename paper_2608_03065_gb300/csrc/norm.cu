@@ -73,27 +73,44 @@ __device__ __forceinline__ void over_block(RowStats& s) {
     if (SHARES == 1 || warps > 1) over_warps(s, warps);
 }
 
+// How a kernel's chunks lie: WIDE, whole and aligned; SHIFTED, at columns 8 c - shift (load8_at); BLOCKS, at columns
+// 8 c as the blocks of 32 columns ask for, aligned or not.
+enum Chunks { WIDE, SHIFTED, BLOCKS };
+
 // A row of the inputs, a chunk (eight columns from k on) at a time; all lanes of a warp call these.
-template <typename T, bool WIDE>
+template <typename T, Chunks C>
 struct Row {
     const T *x, *residual;
     T* sum;
+    uint8_t* q;
     const float* gain;
-    int K;
+    int K, shift;
+    bool in_place;
     __device__ __forceinline__ Row(const Norm& a, int row)
         : x((const T*)a.x + (size_t)row * a.x_stride),
           residual(a.residual ? (const T*)a.residual + (size_t)row * a.residual_stride : nullptr),
-          sum(a.sum ? (T*)a.sum + (size_t)row * a.sum_stride : nullptr), gain(a.gain), K(a.K) {}
+          sum(a.sum ? (T*)a.sum + (size_t)row * a.sum_stride : nullptr), q(a.q + (size_t)row * a.q_stride), gain(a.gain),
+          K(a.K), shift(0), in_place(true) {
+        if (C != SHIFTED) return;
+        shift = row_shift(x);
+        in_place = (!residual || row_shift(residual) == shift) && (!sum || row_shift(sum) == shift) &&
+                   row_shift(q) == shift;
+    }
+    __device__ __forceinline__ int column(int c) const { return C == SHIFTED ? c * 8 - shift : c * 8; }
+    __device__ __forceinline__ void load(const T* from, int k, float h[8]) const {
+        if (C == SHIFTED) load8_at(from, k, K, in_place, h);
+        else load8<C == WIDE>(from, k, K, h);
+    }
     // h; again: the second time, when the sum may have replaced an input
-    __device__ __forceinline__ void load_h(int k, bool there, float h[8], bool again = false) const {
+    __device__ __forceinline__ void load_h(int k, float h[8], bool again = false) const {
 #pragma unroll
         for (int j = 0; j < 8; j++) h[j] = 0.f;
-        if (!there) return;
-        if (again && sum) return load8<WIDE>(sum, k, K, h);
-        load8<WIDE>(x, k, K, h);
+        if (k >= K) return;
+        if (again && sum) return load(sum, k, h);
+        load(x, k, h);
         if (residual) {
             float r[8];
-            load8<WIDE>(residual, k, K, r);
+            load(residual, k, r);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 h[j] += r[j];
@@ -101,10 +118,30 @@ struct Row {
             }
         }
     }
-    __device__ __forceinline__ void load_gain(int k, bool there, float g[8]) const {
+    __device__ __forceinline__ void store_h(int k, const float h[8]) const {
+        if (!sum) return;
+        if (C == SHIFTED) {
+            if (k < K) store8_at(sum, k, K, in_place, h);
+        } else {
+            store8<C == WIDE>(sum, k, K, h, k < K, k > 0);
+        }
+    }
+    __device__ __forceinline__ void load_gain(int k, float g[8]) const {
 #pragma unroll
         for (int j = 0; j < 8; j++) g[j] = 1.f;
-        if (gain && there) load8<WIDE>(gain, k, K, g);
+        if (!gain || k >= K) return;
+        if (C == SHIFTED && k < 0) load8_at(gain, k, K, false, g);
+        else load8<C == WIDE>(gain, k, K, g);
+    }
+    __device__ __forceinline__ void store_codes(int k, uint2 w) const {
+        if (k >= K) return;
+        if (C == WIDE || (in_place && k >= 0 && k + 8 <= K)) {
+            *reinterpret_cast<uint2*>(q + k) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (k + j >= 0 && k + j < K) q[k + j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+        }
     }
 };
 
@@ -166,32 +203,29 @@ __device__ __forceinline__ uint2 codes_of(const float v[8], float unit, float in
 // bf16 columns: 128 threads 111 us, 512 threads 141); where there are too few rows for that, four times as many
 // threads, a chunk each, are done sooner (1 row of 2,048 columns: 4.1 us with 64 threads, 1.9 with 256).  Both add
 // up in the same order (SHARES).
-template <typename T, bool MX4, bool WIDE, int NV, int SHARES, int THREADS>
+template <typename T, bool MX4, Chunks C, int NV, int SHARES, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
-    const int chunks = (a.K + 7) / 8;
     dep_wait();
     dep_launch();
+    const Row<T, C> row(a, blockIdx.x);
+    const int chunks = (a.K + row.shift + 7) / 8;
     // whole warps go round together: a warp's lanes share blocks and tiles
     const int rounds = NV ? NV : (chunks + blockDim.x - 1) / blockDim.x;
     constexpr int KEPT = NV ? NV : 1;
-    const Row<T, WIDE> row(a, blockIdx.x);
-    uint8_t* q = a.q + (size_t)blockIdx.x * a.q_stride;
     float v[KEPT][8];
     RowStats s = {0.f, 0u};
     float top = 0.f;
     bool bad = false;
+    auto column = [&](int i) { return row.column(i * blockDim.x + threadIdx.x); };
 #pragma unroll
-    for (int i = 0; i < (NV ? NV : 0); i++) {           // all loads on their way before any is used
-        const int c = i * blockDim.x + threadIdx.x;
-        row.load_h(c * 8, c < chunks, v[i]);
-    }
+    for (int i = 0; i < (NV ? NV : 0); i++) row.load_h(column(i), v[i]);       // all on their way before any is used
 #pragma unroll
     for (int i = 0; i < rounds; i++) {
-        const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
+        const int k = column(i), at = NV ? i : 0;
         float g[8], squares = 0.f, most = 0.f;
-        if (!NV) row.load_h(c * 8, c < chunks, v[0]);
-        row.load_gain(c * 8, c < chunks, g);
-        if (row.sum) store8<WIDE>(row.sum, c * 8, a.K, v[at], c < chunks, c > 0);
+        if (!NV) row.load_h(k, v[0]);
+        row.load_gain(k, g);
+        row.store_h(k, v[at]);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             float& x = v[at][j];
@@ -200,16 +234,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
             most = larger(most, x);
         }
         s.squares += squares;
-        if (MX4) bad |= quantize8(v[at], most, c, a.K, blockIdx.x, q, a.blocks);
+        if (MX4) bad |= quantize8(v[at], most, k / 8, a.K, blockIdx.x, row.q, a.blocks);
         else top = larger(top, most);
     }
     s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
     over_block<SHARES>(s);
     const Factor f = factor_of<MX4, SHARES>(a, s, [&](float by) {
         RowStats t = {0.f, 0u};
-        for (int c = threadIdx.x; c < chunks; c += blockDim.x) {
+        for (int i = 0; i * (int)blockDim.x < chunks; i++) {
             float h[8], part = 0.f;
-            row.load_h(c * 8, true, h, true);
+            row.load_h(column(i), h, true);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
                 part = fmaf(h[j] * by, h[j] * by, part);
@@ -224,34 +258,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     const float inverse = __fdiv_rn(1.f, f.unit);
 #pragma unroll
     for (int i = 0; i < rounds; i++) {
-        const int c = i * blockDim.x + threadIdx.x, at = NV ? i : 0;
+        const int k = column(i), at = NV ? i : 0;
         if (!NV) {
             float g[8];
-            row.load_h(c * 8, c < chunks, v[0], true);
-            row.load_gain(c * 8, c < chunks, g);
+            row.load_h(k, v[0], true);
+            row.load_gain(k, g);
 #pragma unroll
             for (int j = 0; j < 8; j++) v[0][j] *= g[j];
         }
-        const uint2 codes = codes_of(v[at], f.unit, inverse);
-        if (WIDE) {
-            if (c < chunks) *reinterpret_cast<uint2*>(q + c * 8) = codes;
-        } else {
-            const uint32_t w[2] = {codes.x, codes.y};
-            store_shifted<2, 2, 1>(q + c * 8, w, c < chunks ? min(8, a.K - c * 8) : 0, c > 0);
-        }
+        row.store_codes(k, codes_of(v[at], f.unit, inverse));
     }
 }
 
-template <typename T, bool MX4, bool WIDE>
+template <typename T, bool MX4, Chunks C>
 psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     // a thread's share goes by the width alone, and so do the sums' orders
-    const int chunks = (a.K + 7) / 8, quarter = (chunks + 3) / 4;
+    const int chunks = (a.K + (C == SHIFTED ? 14 : 7)) / 8, quarter = (chunks + 3) / 4;
     const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
     if (threads <= 256 && a.T <= 2 * current_sms())
-        return ops_launch(k_norm<T, MX4, WIDE, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
-    return ops_launch(threads <= 256         ? k_norm<T, MX4, WIDE, 4, 1, 256>
-                      : chunks <= 4 * threads ? k_norm<T, MX4, WIDE, 4, 1, 1024>
-                                              : k_norm<T, MX4, WIDE, 0, 1, 1024>,
+        return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
+    return ops_launch(threads <= 256         ? k_norm<T, MX4, C, 4, 1, 256>
+                      : chunks <= 4 * threads ? k_norm<T, MX4, C, 4, 1, 1024>
+                                              : k_norm<T, MX4, C, 0, 1, 1024>,
                       dim3(a.T), threads, 0, 1, cs, me, a);
 }
 
@@ -260,7 +288,7 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     const bool wide = wide_rows<T>(a.x, a.x_stride, a.K) && wide_rows<T>(a.residual, a.residual_stride, a.K) &&
                       wide_rows<T>(a.sum, a.sum_stride, a.K) && wide_rows<float>(a.gain, 0, a.K) && a.K % 8 == 0 &&
                       is_aligned(a.q, a.q_stride, 8);
-    return wide ? norm<T, MX4, true>(a, me, cs) : norm<T, MX4, false>(a, me, cs);
+    return wide ? norm<T, MX4, WIDE>(a, me, cs) : norm<T, MX4, MX4 ? BLOCKS : SHIFTED>(a, me, cs);
 }
 
 template <bool MX4>
