@@ -41,8 +41,10 @@ __device__ __forceinline__ void over_warp(RowStats& s) {
     for (int o = 16; o; o >>= 1) s.squares += __shfl_xor_sync(FULL, s.squares, o);
     s.top = __reduce_max_sync(FULL, s.top);
 }
-__device__ __forceinline__ void over_warps(RowStats& s, int n) {           // of n warps, which have over_warp's
-    __shared__ RowStats s_all[32];
+// Of n warps, which have over_warp's.  turn: counts a block's calls (what one reads, the next but one writes).
+__device__ __forceinline__ void over_warps(RowStats& s, int n, int turn) {
+    __shared__ RowStats s_both[2][32];
+    RowStats* s_all = s_both[turn & 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (n == 1 && blockDim.x == 32) return;
     if (lane == 0 && warp < n) s_all[warp] = s;
@@ -53,7 +55,7 @@ __device__ __forceinline__ void over_warps(RowStats& s, int n) {           // of
 // The same where SHARES threads stand for each of a smaller block (and have a chunk each of what it would have),
 // the sums in its order.
 template <int SHARES>
-__device__ __forceinline__ void over_block(RowStats& s) {
+__device__ __forceinline__ void over_block(RowStats& s, int turn) {
     const int warps = blockDim.x / 32 / SHARES;
     if (SHARES > 1) {
         __shared__ float s_squares[1024];
@@ -70,7 +72,7 @@ __device__ __forceinline__ void over_block(RowStats& s) {
         s.top = lane < (int)blockDim.x / 32 ? s_top[lane] : 0u;
     }
     over_warp(s);
-    if (SHARES == 1 || warps > 1) over_warps(s, warps);
+    if (SHARES == 1 || warps > 1) over_warps(s, warps, turn);
 }
 
 // How a kernel's chunks lie: WIDE, whole and aligned; SHIFTED, at columns 8 c - shift (load8_at); BLOCKS, at columns
@@ -152,7 +154,7 @@ struct Factor {
 };
 // again(f): this thread's part of the sum of (h f)^2, and the largest |h f|.
 template <bool MX4, int SHARES, typename Again>
-__device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, Again again) {
+__device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, int& turn, Again again) {
     const float unit = s.top >= INF_BITS ? __uint_as_float(0x7fc00000u) : __fmul_rn(__uint_as_float(s.top), 1.f / 127.f);
     if (isnan(unit)) return {unit, unit};
     if (s.squares >= 0x1p-76f && s.squares <= 0x1p126f) {
@@ -163,13 +165,13 @@ __device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, Ag
     // on): once more, with the largest magnitude near 1
     RowStats t = again(1.f);
     __syncthreads();
-    over_block<SHARES>(t);
+    over_block<SHARES>(t, turn++);
     const int e = max(1, min(253, (int)(t.top >> 23)));
     const bool zeros = t.top == 0;
     const float f = __uint_as_float((uint32_t)(254 - e) << 23);
     t = again(f);
     __syncthreads();
-    over_block<SHARES>(t);
+    over_block<SHARES>(t, turn++);
     const double r = 1.0 / sqrt((double)t.squares / a.K / ((double)f * f) + a.eps);
     // a row of zeros with eps 0, or of no unit: 0, not the product with an infinite r
     if (MX4) return {unit, zeros && a.eps == 0.f ? 0.f : (float)r};
@@ -196,6 +198,128 @@ __device__ __forceinline__ uint2 codes_of(const float v[8], float unit, float in
             w[j] = unit > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(v[j], unit)), -127.f), 127.f) : 0u;
     return make_uint2(__byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410),
                       __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410));
+}
+
+// h of a chunk from its words.
+__device__ __forceinline__ void unpack_h(const uint32_t (&x)[4], const uint32_t (&r)[4], bool residual, float h[8],
+                                         const __nv_bfloat16*) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        // a sum of two bf16 rounded to bf16 at once is the one rounded to f32 on the way: where that rounding is
+        // not exact, the smaller is below 2^-16 of the larger, and the sum far from where bf16's rounding turns
+        __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&x[j]);
+        if (residual) s = __hadd2_rn(s, *reinterpret_cast<const __nv_bfloat162*>(&r[j]));
+        w[j] = *reinterpret_cast<const uint32_t*>(&s);
+    }
+    unpack8(w, h, (const __nv_bfloat16*)nullptr);
+}
+__device__ __forceinline__ void unpack_h(const uint32_t (&x)[8], const uint32_t (&r)[8], bool residual, float h[8],
+                                         const float*) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) h[j] = residual ? __uint_as_float(x[j]) + __uint_as_float(r[j]) : __uint_as_float(x[j]);
+}
+
+// Many aligned rows: blocks stay and go from row to row, and each thread copies its chunks of the next `stages`
+// rows into shared memory ahead (cp.async; nobody else reads them, so that only their own thread waits).  In k_norm
+// a block's loads all come at its beginning, and half of its time nothing is under way: 16,384 rows of
+// 4,096 bf16 columns with residual 114 us, this way 91.
+template <typename T, bool MX4>
+__global__ void __launch_bounds__(256, 4) k_norm_many(Norm a, int stages) {
+    constexpr int NV = 4, N = sizeof(T) * 2, PIECES = N / 4;           // words, 16-byte pieces of a chunk
+    extern __shared__ uint4 s_ring[];
+    const int chunks = a.K / 8, parts = a.residual ? 2 : 1, step = blockDim.x;
+    dep_wait();
+    dep_launch();
+    // a thread's pieces of a stage, one of each thread after the other
+    auto place = [&](int stage, int part, int i, int piece) {
+        return s_ring + (((stage * parts + part) * NV + i) * PIECES + piece) * step + threadIdx.x;
+    };
+    auto copy = [&](int stage, uint32_t r) {
+        if (r < (uint32_t)a.T)
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                const int c = i * step + threadIdx.x;
+                if (c >= chunks) break;
+                for (int part = 0; part < parts; part++) {
+                    const T* from = (part ? (const T*)a.residual + (size_t)r * a.residual_stride
+                                          : (const T*)a.x + (size_t)r * a.x_stride) + c * 8;
+#pragma unroll
+                    for (int piece = 0; piece < PIECES; piece++)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                         (uint32_t)__cvta_generic_to_shared(place(stage, part, i, piece))),
+                                     "l"((const char*)from + 16 * piece)
+                                     : "memory");
+                }
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto read = [&](int stage, int part, int i, uint32_t (&w)[N]) {
+#pragma unroll
+        for (int piece = 0; piece < PIECES; piece++) {
+            const uint4 x = *place(stage, part, i, piece);
+            w[4 * piece] = x.x, w[4 * piece + 1] = x.y, w[4 * piece + 2] = x.z, w[4 * piece + 3] = x.w;
+        }
+    };
+    for (int i = 0; i < stages; i++) copy(i, blockIdx.x + i * gridDim.x);
+    int stage = 0, turn = 0;
+    for (uint32_t r = blockIdx.x; r < (uint32_t)a.T; r += gridDim.x, stage = stage + 1 == stages ? 0 : stage + 1) {
+        const Row<T, WIDE> row(a, r);
+        // this row's copies, the oldest of `stages` groups
+        if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else asm volatile("cp.async.wait_group 3;" ::: "memory");
+        float v[NV][8];
+        RowStats s = {0.f, 0u};
+        float top = 0.f;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const int c = i * step + threadIdx.x;
+            uint32_t x[N] = {}, res[N] = {};
+            if (c < chunks) {
+                read(stage, 0, i, x);
+                if (parts == 2) read(stage, 1, i, res);
+            }
+            unpack_h(x, res, parts == 2, v[i], (const T*)nullptr);
+            float g[8], squares = 0.f, most = 0.f;
+            row.load_gain(c * 8, g);
+            row.store_h(c * 8, v[i]);
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                float& h = v[i][j];
+                squares = fmaf(h, h, squares);
+                h *= g[j];
+                most = larger(most, h);
+            }
+            s.squares += squares;
+            if (MX4) bad |= quantize8(v[i], most, c, a.K, r, row.q, a.blocks);
+            else top = larger(top, most);
+        }
+        copy(stage, r + stages * gridDim.x);
+        s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
+        over_block<1>(s, turn++);
+        const Factor f = factor_of<MX4, 1>(a, s, turn, [&](float by) {
+            RowStats t = {0.f, 0u};
+            for (int c = threadIdx.x; c < chunks; c += step) {
+                float h[8], part = 0.f;
+                row.load_h(c * 8, h, true);
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    part = fmaf(h[j] * by, h[j] * by, part);
+                    t.top = max(t.top, __float_as_uint(h[j] * by) & 0x7fffffffu);
+                }
+                t.squares += part;
+            }
+            return t;
+        });
+        if (threadIdx.x == 0) a.scale[r] = f.scale;
+        if (MX4) continue;
+        const float inverse = __fdiv_rn(1.f, f.unit);
+#pragma unroll
+        for (int i = 0; i < NV; i++) row.store_codes((i * step + threadIdx.x) * 8, codes_of(v[i], f.unit, inverse));
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // A block per row, NV chunks of it in a thread's registers (0: any number, read again for what comes after
@@ -238,8 +362,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
         else top = larger(top, most);
     }
     s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
-    over_block<SHARES>(s);
-    const Factor f = factor_of<MX4, SHARES>(a, s, [&](float by) {
+    int turn = 0;
+    over_block<SHARES>(s, turn++);
+    const Factor f = factor_of<MX4, SHARES>(a, s, turn, [&](float by) {
         RowStats t = {0.f, 0u};
         for (int i = 0; i * (int)blockDim.x < chunks; i++) {
             float h[8], part = 0.f;
@@ -270,6 +395,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     }
 }
 
+constexpr int RING_BYTES = 200 * 1024;            // of an SM's shared memory, for rows under way
+
 template <typename T, bool MX4, Chunks C>
 psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     // a thread's share goes by the width alone, and so do the sums' orders
@@ -277,6 +404,14 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
     if (threads <= 256 && a.T <= 2 * current_sms())
         return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
+    if (C == WIDE && threads <= 256) {
+        // as many blocks as registers leave room for, as many rows ahead as shared memory does
+        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = 1024 / threads;
+        const int blocks = std::min(most, RING_BYTES / (2 * stage)), stages = std::min(4, RING_BYTES / (blocks * stage));
+        if (a.T >= 4 * blocks * current_sms())
+            return ops_launch(k_norm_many<T, MX4>, dim3(blocks * current_sms()), threads, (size_t)stages * stage, 1, cs, me,
+                              a, stages);
+    }
     return ops_launch(threads <= 256         ? k_norm<T, MX4, C, 4, 1, 256>
                       : chunks <= 4 * threads ? k_norm<T, MX4, C, 4, 1, 1024>
                                               : k_norm<T, MX4, C, 0, 1, 1024>,

@@ -176,6 +176,41 @@ def test_a_row_does_not_depend_on_its_batch(psc):  # noqa: F811
             assert torch.equal(q1[0], q[t]) and torch.equal(s1[0], s[t])
 
 
+@pytest.mark.parametrize("T,K,dtype,residual", [(20000, 72, "bf16", True), (16000, 40, "f32", False), (4001, 4096, "bf16", True),
+                                                (7000, 2048, "bf16", False), (4000, 2056, "f32", True),
+                                                (3000, 8192, "bf16", True), (9000, 1000, "bf16", True)])
+def test_many_rows_are_what_a_few_are(psc, T, K, dtype, residual):  # noqa: F811
+    """A batch that is worked on in turns, rows that need a second pass among it, against the same
+    rows a few at a time; the sum in place of the residual."""
+    rng = np.random.default_rng([T, K])
+    x = _dev(_data(rng, T, K, dtype)).to(DT[dtype])
+    x[5], x[6, 3], x[T - 1] = 0, float("inf"), 0
+    x[7], x[T // 2], x[T // 2 + 1] = x[7] * 1e28, x[T // 2] * 1e-28, float("nan")
+    res = _dev(_data(rng, T, K, dtype)).to(DT[dtype]) if residual else None
+    if residual:
+        res[5:8], res[T // 2:T // 2 + 2], res[T - 1] = 0, 0, 0
+    g, n = _dev(rng.uniform(0.5, 1.5, K).astype(np.float32)), psc.psc_mx4_row_bytes(K)
+
+    def run(lo, hi):
+        rows = hi - lo
+        r8 = None if res is None else res[lo:hi].clone()
+        r4 = None if res is None else res[lo:hi].clone()
+        q8, s8 = torch.zeros(rows, K, dtype=torch.int8, device="cuda"), torch.zeros(rows, device="cuda")
+        q4, s4 = torch.zeros(rows, n, dtype=torch.uint8, device="cuda"), torch.zeros(rows, device="cuda")
+        b = torch.zeros(psc.psc_mx4_block_bytes(rows, K), dtype=torch.uint8, device="cuda")
+        psc.psc_norm_quantize_rows(x[lo:hi], q8, s8, gain=g, residual=r8, sum_out=r8, eps=0.0)
+        psc.psc_norm_quantize_mx4(x[lo:hi], q4, b, s4, gain=g, residual=r4, sum_out=r4, eps=0.0)
+        return [t for t in (q8, s8.view(torch.int32), q4, s4.view(torch.int32), r8, r4) if t is not None], b
+
+    whole, blocks = run(0, T)
+    tiles = blocks.view((T + 127) // 128, -1)
+    for lo in (0, 256, T // 2 // 128 * 128, (T - 1) // 128 * 128):
+        few, b = run(lo, min(T, lo + 128))
+        for u, v in zip(whole, few):
+            assert torch.equal(u[lo:lo + 128].view(torch.uint8), v.view(torch.uint8))
+        assert torch.equal(tiles[lo // 128], b)
+
+
 def test_feeds_the_projections(psc):  # noqa: F811
     """The norm and both projections after it, against the normalised rows in 64 bits: a value of 8 bits
     is off by half a step of its row's largest / 127, one of 4 bits by a quarter of its block's largest."""
