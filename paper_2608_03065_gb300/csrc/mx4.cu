@@ -41,7 +41,8 @@ __global__ void __launch_bounds__(256) k_quantize_mx4(const T* x, int64_t stride
 #pragma unroll
         for (int j = 0; j < AT_ONCE; j++) {
             const uint32_t row = r0 + j * rows_step;
-            quantize8(v[j], largest8(v[j]), l.c, l.there && row < rows ? K : 0, row, q + (size_t)row * q_stride, blocks);
+            quantize8(v[j], largest8(v[j], 0.f), l.c, l.there && row < rows ? K : 0, q + (size_t)row * q_stride,
+                      blocks + block_at(row, 0, n_tiles));
         }
     }
 }

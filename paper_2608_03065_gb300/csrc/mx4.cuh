@@ -166,12 +166,17 @@ inline bool wide_rows(const void* p, int64_t stride, int K) {
     return !p || (K % 8 == 0 && is_aligned(p, stride * (int64_t)sizeof(T), 16));
 }
 
-// The larger of a and |b|; NaN if one is.  As bit patterns magnitudes order as they do as numbers, with
+// The largest of |a|, |b| and |c|; NaN if one is.  As bit patterns magnitudes order as they do as numbers, with
 // infinities and then NaN above all.
-__device__ __forceinline__ float larger(float a, float b) {
+__device__ __forceinline__ float largest(float a, float b, float c) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+__device__ __forceinline__ float largest8(const float v[8], float top) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) top = largest(top, v[j], v[j + 1]);
+    return top;
 }
 constexpr uint32_t INF_BITS = 0x7f800000u;
 
@@ -206,9 +211,10 @@ __device__ __forceinline__ uint32_t codes8(const float v[8], float inverse) {
 
 // A thread's eight columns from 8 c on of a row, to codes and exponents; `top` the largest magnitude of
 // them.  All 32 lanes of a warp call it for neighbouring chunks c (or 16 of one row and 16 of another), lane
-// 0's a multiple of 16; what lies past the row's last tile stores nothing.  Returns whether the block is NaN.
-__device__ __forceinline__ bool quantize8(const float v[8], float top, int c, int K, int row, uint8_t* q_row,
-                                          uint8_t* blocks) {
+// 0's a multiple of 16; what lies past the row's last tile stores nothing.  row_blocks: where the row's first
+// block's exponent is.  Returns whether the block is NaN.
+__device__ __forceinline__ bool quantize8(const float v[8], float top, int c, int K, uint8_t* q_row,
+                                          uint8_t* row_blocks) {
     const int lane = threadIdx.x & 31;
     uint32_t bits = __float_as_uint(top) & 0x7fffffffu;
     bits = max(bits, __shfl_xor_sync(FULL, bits, 1));
@@ -220,18 +226,9 @@ __device__ __forceinline__ bool quantize8(const float v[8], float top, int c, in
     uint32_t word = byte << (8 * ((lane >> 2) & 3));
     word |= __shfl_xor_sync(FULL, word, 4);
     word |= __shfl_xor_sync(FULL, word, 8);
-    const int n_tiles = (K + 127) / 128;
-    if (!(lane & 15) && c < n_tiles * 16)
-        *reinterpret_cast<uint32_t*>(blocks + block_at(row, c / 4, n_tiles)) = word;
+    if (!(lane & 15) && c < (K + 127) / 128 * 16) *reinterpret_cast<uint32_t*>(row_blocks + (int64_t)c * 32) = word;
     return byte == 255;
 }
-__device__ __forceinline__ float largest8(const float v[8]) {
-    float top = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; j++) top = larger(top, v[j]);
-    return top;
-}
-
 inline bool is_mx4(const void* q, int64_t stride, const void* blocks, int K) {
     return is_aligned(q, stride, 16) && (uintptr_t)blocks % 16 == 0 && stride >= ((int64_t)K + 31) / 32 * 16;
 }

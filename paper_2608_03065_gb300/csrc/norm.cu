@@ -223,9 +223,9 @@ __device__ __forceinline__ void unpack_h(const uint32_t (&x)[8], const uint32_t 
 // Many aligned rows: blocks stay and go from row to row, and each thread copies its chunks of the next `stages`
 // rows into shared memory ahead (cp.async; nobody else reads them, so that only their own thread waits).  In k_norm
 // a block's loads all come at its beginning, and half of its time nothing is under way: 16,384 rows of
-// 4,096 bf16 columns with residual 114 us, this way 91.
+// 4,096 bf16 columns with residual 114 us, this way 76.
 template <typename T, bool MX4>
-__global__ void __launch_bounds__(256, 4) k_norm_many(Norm a, int stages) {
+__global__ void __launch_bounds__(256, 3) k_norm_many(Norm a, int stages) {
     constexpr int NV = 4, N = sizeof(T) * 2, PIECES = N / 4;           // words, 16-byte pieces of a chunk
     extern __shared__ uint4 s_ring[];
     const int chunks = a.K / 8, parts = a.residual ? 2 : 1, step = blockDim.x;
@@ -265,6 +265,7 @@ __global__ void __launch_bounds__(256, 4) k_norm_many(Norm a, int stages) {
     int stage = 0, turn = 0;
     for (uint32_t r = blockIdx.x; r < (uint32_t)a.T; r += gridDim.x, stage = stage + 1 == stages ? 0 : stage + 1) {
         const Row<T, WIDE> row(a, r);
+        uint8_t* blocks = MX4 ? a.blocks + block_at(r, 0, (a.K + 127) / 128) : nullptr;
         // this row's copies, the oldest of `stages` groups
         if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
@@ -282,19 +283,18 @@ __global__ void __launch_bounds__(256, 4) k_norm_many(Norm a, int stages) {
                 if (parts == 2) read(stage, 1, i, res);
             }
             unpack_h(x, res, parts == 2, v[i], (const T*)nullptr);
-            float g[8], squares = 0.f, most = 0.f;
+            float g[8], squares = 0.f;
             row.load_gain(c * 8, g);
             row.store_h(c * 8, v[i]);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                float& h = v[i][j];
-                squares = fmaf(h, h, squares);
-                h *= g[j];
-                most = larger(most, h);
+                squares = fmaf(v[i][j], v[i][j], squares);
+                v[i][j] *= g[j];
             }
             s.squares += squares;
-            if (MX4) bad |= quantize8(v[i], most, c, a.K, r, row.q, a.blocks);
-            else top = larger(top, most);
+            const float most = largest8(v[i], top);
+            if (MX4) bad |= quantize8(v[i], most, c, a.K, row.q, blocks);
+            else top = most;
         }
         copy(stage, r + stages * gridDim.x);
         s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
@@ -340,26 +340,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     RowStats s = {0.f, 0u};
     float top = 0.f;
     bool bad = false;
+    uint8_t* blocks = MX4 ? a.blocks + block_at(blockIdx.x, 0, (a.K + 127) / 128) : nullptr;
     auto column = [&](int i) { return row.column(i * blockDim.x + threadIdx.x); };
 #pragma unroll
     for (int i = 0; i < (NV ? NV : 0); i++) row.load_h(column(i), v[i]);       // all on their way before any is used
 #pragma unroll
     for (int i = 0; i < rounds; i++) {
         const int k = column(i), at = NV ? i : 0;
-        float g[8], squares = 0.f, most = 0.f;
+        float g[8], squares = 0.f;
         if (!NV) row.load_h(k, v[0]);
         row.load_gain(k, g);
         row.store_h(k, v[at]);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            float& x = v[at][j];
-            squares = fmaf(x, x, squares);
-            x *= g[j];
-            most = larger(most, x);
+            squares = fmaf(v[at][j], v[at][j], squares);
+            v[at][j] *= g[j];
         }
         s.squares += squares;
-        if (MX4) bad |= quantize8(v[at], most, k / 8, a.K, blockIdx.x, row.q, a.blocks);
-        else top = larger(top, most);
+        const float most = largest8(v[at], top);
+        if (MX4) bad |= quantize8(v[at], most, k / 8, a.K, row.q, blocks);
+        else top = most;
     }
     s.top = MX4 ? (bad ? INF_BITS : 0u) : __float_as_uint(top) & 0x7fffffffu;
     int turn = 0;
@@ -406,9 +406,9 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
         return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
     if (C == WIDE && threads <= 256) {
         // as many blocks as registers leave room for, as many rows ahead as shared memory does
-        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = 1024 / threads;
+        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = 768 / threads;
         const int blocks = std::min(most, RING_BYTES / (2 * stage)), stages = std::min(4, RING_BYTES / (blocks * stage));
-        if (a.T >= 4 * blocks * current_sms())
+        if (a.T >= 2 * blocks * current_sms())
             return ops_launch(k_norm_many<T, MX4>, dim3(blocks * current_sms()), threads, (size_t)stages * stage, 1, cs, me,
                               a, stages);
     }
