@@ -122,6 +122,10 @@ __device__ __forceinline__ void tmem_free(uint32_t tmem) {
 __device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int x, int y) {
     asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
 }
+// A map's own bytes on their way to the TMA.
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 // Lets the copies in flight land: those of the last `slots` of c uses of a ring.
 __device__ __forceinline__ void drain(uint32_t full0, int c, int slots) {
     for (int i = max(0, c - slots); i < c; i++)
@@ -251,6 +255,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     auto acc_empty = [&](int s) { return bars + 8 * (2 * MAX_STAGES + 2 + s); };
     const uint32_t drained = bars + 8 * (2 * MAX_STAGES + 4);
 
+    if (warp == 2 && lane < 4)
+        prefetch_map(lane == 0 ? &w_map : lane == 1 ? &x_map : lane == 2 ? &w_blocks_map : &x_blocks_map);
     if (threadIdx.x == 0) {
         s_failed = 0;
         for (int s = 0; s < p.stages; s++) mbar_init(full(s), 4), mbar_init(empty(s), 1);
@@ -280,6 +286,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
             // a lane per word of a token's four, eight tokens at a time
             const int wi = (blockIdx.x + i * gridDim.x) * 4 + (lane & 3);
             if (wi < h.W)
+#pragma unroll 4
                 for (int t = lane >> 2; t < h.T; t += 8) any |= h.bitmask[(size_t)t * h.W + wi];
             if (__any_sync(FULL, any) && lane == 0) atomicOr(&s_active[i / 32], 1u << (i & 31));
         }
@@ -492,6 +499,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
     const uint32_t drained = bars + 8 * (LAST + 4);
 
+    if (warp == 2 && lane < 4)
+        prefetch_map(lane == 0 ? &w_map : lane == 1 ? &x_map : lane == 2 ? &w_blocks_map : &x_blocks_map);
     if (threadIdx.x == 0) {
         s_failed = 0, s_item = 0;
         for (int s = 0; s < A_SLOTS; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);

@@ -293,3 +293,20 @@ def test_tensors_of_another_device_are_refused(psc, monkeypatch, module):  # noq
                 call()
     finally:
         psc._load_marshal(psc.load())
+
+
+def test_values_back_where_the_factor_leaves_the_normal_numbers(psc):  # noqa: F811
+    """code * 2^e * scale with 2^e * scale above the largest or below the smallest normal number: the power of two
+    first, then one rounding of the product with the scale (and that to the type)."""
+    rng = np.random.default_rng(4)
+    for K in (64, 61):
+        e = np.array([[0, 0], [1, 3], [252, 254], [254, 250], [10, 20], [127, 127], [255, 127], [130, 0]], dtype=np.uint8)
+        scale = np.array([1.3, 1e-3, 2.0, 3e38, 1e-36, 0, 1, np.inf], dtype=np.float32)
+        codes = rng.integers(0, 16, (8, K), dtype=np.uint8)
+        q, blocks = _matrix(psc, codes, e, K)
+        with np.errstate(over="ignore", invalid="ignore", under="ignore"):
+            want = ref.decode(codes, e).astype(np.float32) * scale[:, None]
+        for pad in (0, 3):
+            _, y = _strided(np.zeros((8, K)), torch.float32, pad, 0)
+            psc.psc_dequantize_mx4(q, blocks, y, scale=_dev(scale))
+            np.testing.assert_array_equal(y.cpu().numpy(), want)
