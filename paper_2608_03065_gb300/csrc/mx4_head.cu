@@ -145,6 +145,7 @@ constexpr int VT = 128;                       // vocabulary rows of a tile
 constexpr int W_CODES = VT * KS / 2;
 constexpr int MAX_STAGES = 11;
 constexpr int GROUPS = FEW / 32 / 2;          // a warp's groups of 32 tokens
+constexpr int WARM = 24;                      // stages whose weights are prefetched (1 token over 128,256 x 2048: 28.3 us without, 26.5)
 constexpr int MAX_TILES = 8192;               // of a block, for which masks are looked at beforehand
 
 struct Few {
@@ -271,9 +272,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
     const int n_k = (h.K + KS - 1) / KS;
-    if (!MASKED && warp == 0 && lane == 0)            // the first stages' weights on their way to the L2
-        for (int i = 0; i < min(p.stages, n_k); i++)
-            prefetch_tile(&w_map, i * 128, (int)blockIdx.x * VT);
+    if (!MASKED && warp == 0 && lane == 0)            // the first stages' weights on their way to the L2, while others finish
+        for (int i = 0, k = 0, vt = blockIdx.x; i < WARM && vt < p.n_vt; i++) {
+            prefetch_tile(&w_map, k * 128, vt * VT);
+            if (++k == n_k) k = 0, vt += gridDim.x;
+        }
     dep_wait();
     dep_launch();
     // Of this block's tiles, those in which some token is allowed; the others' weights are not read.
@@ -438,11 +441,13 @@ constexpr int NV = 192;                       // vocabulary rows of a tile
 constexpr int TOGETHER = 4;                   // tiles of tokens that are worked on at the same time
 constexpr int A_CODES = MT / 2 * KS / 2, A_BYTES = A_CODES + 2 * SF;
 constexpr int B_CODES = NV / 2 * KS / 2, B_EXPS = 4 * SF;
-constexpr int A_SLOTS = 8, B_SLOTS = 5;       // (of the weights: their codes, their exponents, TMEM columns for them)
+constexpr int MAX_A = 8, MAX_B = 16;          // slots for the tokens, for the weights' codes
+constexpr int SF_SLOTS = 5;                   // for the weights' exponents, and in TMEM for a stage's
 constexpr int SF_COLS = 24;                   // TMEM columns of a stage's exponents
-static_assert(2 * NV + B_SLOTS * SF_COLS <= 512, "TMEM");
+static_assert(2 * NV + SF_SLOTS * SF_COLS <= 512, "TMEM");
 constexpr int STAGING = 32 * 64;              // a warp's, in the epilogue
-constexpr size_t MANY_SMEM = 1024 + A_SLOTS * A_BYTES + B_SLOTS * (B_CODES + B_EXPS) + EPILOGUE * STAGING;
+constexpr int SLOTS_BYTES = MAX_A * A_BYTES + 5 * B_CODES;            // for the tokens and the weights' codes
+constexpr size_t MANY_SMEM = 1024 + SLOTS_BYTES + SF_SLOTS * B_EXPS + EPILOGUE * STAGING;
 
 // A tile into this block's shared memory; the barrier is the pair's first block's.
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -477,24 +482,29 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                                                              const __grid_constant__ CUtensorMap x_blocks_map, Head h,
                                                              T* logits, int n_mt, int n_vt, bool wide) {
     extern __shared__ uint8_t dyn[];
-    __shared__ __align__(8) uint64_t s_bars[2 * A_SLOTS + 5 * B_SLOTS + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * MAX_A + 2 * MAX_B + 4 * SF_SLOTS + 5];
     __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed, s_item;                  // how many items' weights have begun to be loaded
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = (int)cluster_rank();
     // slots start at multiples of 1024 bytes: the tokens' codes and exponents, the weights' codes, their exponents
-    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, b_base = base + A_SLOTS * A_BYTES;
-    const uint32_t e_base = b_base + B_SLOTS * B_CODES;
+    // Tokens that do not stay come from the L2, weights from memory, which takes longer: most slots are theirs then.
+    const int n_k = (h.K + KS - 1) / KS;
+    const bool stay = n_k <= MAX_A;
+    const int a_slots = stay ? n_k : 4, b_slots = min(MAX_B, (SLOTS_BYTES - a_slots * A_BYTES) / B_CODES);
+    const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, b_base = base + a_slots * A_BYTES;
+    const uint32_t e_base = base + SLOTS_BYTES;
     const uint32_t bars = smem_addr(s_bars);
     auto a_full = [&](int s) { return bars + 8 * s; };
-    auto a_empty = [&](int s) { return bars + 8 * (A_SLOTS + s); };
-    auto b_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + s); };
-    auto b_empty = [&](int s) { return bars + 8 * (2 * A_SLOTS + B_SLOTS + s); };
-    auto e_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 2 * B_SLOTS + s); };
-    auto e_empty = [&](int s) { return bars + 8 * (2 * A_SLOTS + 3 * B_SLOTS + s); };
-    auto sf_full = [&](int s) { return bars + 8 * (2 * A_SLOTS + 4 * B_SLOTS + s); };
-    constexpr int LAST = 2 * A_SLOTS + 5 * B_SLOTS;
+    auto a_empty = [&](int s) { return bars + 8 * (MAX_A + s); };
+    auto b_full = [&](int s) { return bars + 8 * (2 * MAX_A + s); };
+    auto b_empty = [&](int s) { return bars + 8 * (2 * MAX_A + MAX_B + s); };
+    constexpr int SF_BARS = 2 * (MAX_A + MAX_B), LAST = SF_BARS + 4 * SF_SLOTS;
+    auto e_full = [&](int s) { return bars + 8 * (SF_BARS + s); };
+    auto e_empty = [&](int s) { return bars + 8 * (SF_BARS + SF_SLOTS + s); };
+    auto sf_full = [&](int s) { return bars + 8 * (SF_BARS + 2 * SF_SLOTS + s); };
+    auto sf_empty = [&](int s) { return bars + 8 * (SF_BARS + 3 * SF_SLOTS + s); };
     auto acc_full = [&](int s) { return bars + 8 * (LAST + s); };
     auto acc_empty = [&](int s) { return bars + 8 * (LAST + 2 + s); };
     const uint32_t drained = bars + 8 * (LAST + 4);
@@ -503,10 +513,11 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
         prefetch_map(lane == 0 ? &w_map : lane == 1 ? &x_map : lane == 2 ? &w_blocks_map : &x_blocks_map);
     if (threadIdx.x == 0) {
         s_failed = 0, s_item = 0;
-        for (int s = 0; s < A_SLOTS; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
-        for (int s = 0; s < B_SLOTS; s++) {
-            mbar_init(b_full(s), 1), mbar_init(b_empty(s), 1);
-            mbar_init(e_full(s), 1), mbar_init(e_empty(s), 1), mbar_init(sf_full(s), 1);
+        for (int s = 0; s < a_slots; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
+        for (int s = 0; s < b_slots; s++) mbar_init(b_full(s), 1), mbar_init(b_empty(s), 1);
+        for (int s = 0; s < SF_SLOTS; s++) {
+            mbar_init(e_full(s), 1), mbar_init(e_empty(s), 1);
+            mbar_init(sf_full(s), 1), mbar_init(sf_empty(s), 1);
         }
         for (int s = 0; s < 2; s++) mbar_init(acc_full(s), 1), mbar_init(acc_empty(s), EPILOGUE * 2);
         mbar_init(drained, 2);
@@ -520,9 +531,6 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     volatile int* failed = &s_failed;
-    const int n_k = (h.K + KS - 1) / KS;
-    const bool stay = n_k <= A_SLOTS;
-    const int a_slots = stay ? n_k : A_SLOTS;
     dep_wait();
     dep_launch();
     // This pair's items, in order: up to TOGETHER tiles of tokens at a time, a pair staying with one of
@@ -568,9 +576,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
 
     auto codes_row = [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); };
     if (warp == 0) {
-        load_part(&w_map, 128, b_base, B_CODES, B_SLOTS, b_full(0), b_empty(0), B_CODES, false, codes_row);
+        load_part(&w_map, 128, b_base, B_CODES, b_slots, b_full(0), b_empty(0), B_CODES, false, codes_row);
     } else if (warp == 2) {
-        load_part(&w_blocks_map, 256, e_base, B_EXPS, B_SLOTS, e_full(0), e_empty(0), B_EXPS, false, [&](int, int vt) {
+        load_part(&w_blocks_map, 256, e_base, B_EXPS, SF_SLOTS, e_full(0), e_empty(0), B_EXPS, false, [&](int, int vt) {
             *const_cast<volatile int*>(&s_item) = s_item + 1;
             return vt * NV / 128;
         });
@@ -594,17 +602,17 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                   [&](int mt, int) { return mt * 2 + side; });
     } else if (warp == 5 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
-        // issues, for both blocks.  Exponents go to TMEM as soon as the products of B_SLOTS stages before are
+        // issues, for both blocks.  Exponents go to TMEM as soon as the products of SF_SLOTS stages before are
         // done with theirs, while the codes that take those products' place are still on their way.
         const bool issuer = elect_one();
         const uint32_t a_lo = ((base + A_CODES) & 0x3FFFF) >> 4, e_lo = (e_base & 0x3FFFF) >> 4;
         Place unit, at;                               // unit: the first slot of the tile's tokens
         each([&](int, int, bool fresh, bool last) {
             Place at_a = unit;
-            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at.next(B_SLOTS)) {
+            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), e = e_lo + at.s * (B_EXPS / 16);
                 const uint32_t sf = tmem + 2 * NV + at.s * SF_COLS;
-                if (!warp_wait2(e_full(at.s), at.parity, b_empty(at.s), at.parity ^ 1, failed) ||
+                if (!warp_wait2(e_full(at.s), at.parity, sf_empty(at.s), at.parity ^ 1, failed) ||
                     (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed)))
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -620,22 +628,23 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     } else if (warp == 1 && side == 0) {
         const bool issuer = elect_one();
         const uint32_t a_lo = (base & 0x3FFFF) >> 4, b_lo = (b_base & 0x3FFFF) >> 4;
-        Place unit, at_b, acc;
+        Place unit, at_b, at_e, acc;
         bool ok = true;
         each([&](int, int vt, bool fresh, bool last) {
             const uint32_t idesc = instruction(MT, rows_of(vt)), d = tmem + acc.s * NV, shift = vt * NV % 128 / 32;
             Place at_a = unit;
             if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) return false;
-            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(B_SLOTS)) {
+            for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(b_slots), at_e.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_CODES / 16);
-                const uint32_t sf = tmem + 2 * NV + at_b.s * SF_COLS;
-                ok = warp_wait2(sf_full(at_b.s), at_b.parity, b_full(at_b.s), at_b.parity, failed) &&
+                const uint32_t sf = tmem + 2 * NV + at_e.s * SF_COLS;
+                ok = warp_wait2(sf_full(at_e.s), at_e.parity, b_full(at_b.s), at_b.parity, failed) &&
                      (!fresh || warp_wait(a_full(at_a.s), at_a.parity, failed));
                 if (!ok) return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
                     mma_stage<true, 2>(a, b, sf, shift, d, idesc, k);
                     mma_commit<true>(b_empty(at_b.s));
+                    commit_here(sf_empty(at_e.s));
                     if (last) mma_commit<true>(a_empty(at_a.s));
                     if (k + 1 == n_k) mma_commit<true>(acc_full(acc.s));
                 }
@@ -652,7 +661,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     } else if (warp >= FIRST) {
         constexpr int COLS = 64 / sizeof(T);          // logits of a token that go out together
         const int quad = warp & 3, part = (warp - FIRST) >> 2;
-        const uint32_t staging = e_base + B_SLOTS * B_EXPS + (warp - FIRST) * STAGING;
+        const uint32_t staging = e_base + SF_SLOTS * B_EXPS + (warp - FIRST) * STAGING;
         const uint32_t own = staging + lane * 64, own_swap = (lane >> 1) & 3;       // 16-byte pieces change places by rows
         float* scales = s_scale[warp - FIRST];
         Place acc;
