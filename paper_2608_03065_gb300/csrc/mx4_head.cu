@@ -475,6 +475,13 @@ __device__ __forceinline__ void times2(uint32_t& a, uint32_t& b, float x, float 
         : "f"(x), "f"(y));
 }
 
+// The top bit of byte i of a, in all bits of the low half, and that of b in the high half.
+__device__ __forceinline__ uint32_t both_bytes(uint32_t a, uint32_t b, int i) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(0xCC88u + 0x1111u * i));
+    return r;
+}
+
 template <typename T, bool MASKED>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_constant__ CUtensorMap w_map,
                                                              const __grid_constant__ CUtensorMap x_map,
@@ -712,18 +719,26 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                         times2(y[j + 2], y[j + 3], s.z, s.w);
                     }
                 }
-                if (MASKED) {
+                if (MASKED && sizeof(T) == 4) {
 #pragma unroll
                     for (int j = 0; j < 32; j++)
                         if (!((words[i] >> j) & 1)) y[j] = 0xFF800000u;
                 }
+                uint32_t spread[8];                   // bit b of the word as the top bit of byte b / 8 of spread[b % 8]
+#pragma unroll
+                for (int j = 0; j < 8; j++) spread[j] = words[i] << (7 - j);
 #pragma unroll
                 for (int half = 0; half < (int)sizeof(T) / 2; half++) {       // 64 bytes a token
                     uint32_t u[16];
 #pragma unroll
-                    for (int j = 0; j < 16; j++)
+                    for (int j = 0; j < 16; j++) {
                         u[j] = sizeof(T) == 2 ? pack_bf16(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1]))
                                               : y[half * 16 + j];
+                        if (MASKED && sizeof(T) == 2) {
+                            const uint32_t keep = both_bytes(spread[2 * j % 8], spread[2 * j % 8 + 1], j / 4);
+                            u[j] = (u[j] & keep) | (0xFF80FF80u & ~keep);
+                        }
+                    }
                     __syncwarp();
 #pragma unroll
                     for (int j = 0; j < 4; j++)
