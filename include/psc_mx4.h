@@ -18,7 +18,8 @@
  * Conventions, status codes and psc_last_error are those of psc.h, with those that
  * psc_ops.h adds: calls only enqueue work on the stream, may be captured in a CUDA graph,
  * and give the same bits for the same inputs.  Codes start at multiples of 16 bytes with
- * strides that are multiples of 16, blocks at multiples of 16 bytes; other calls are refused.
+ * strides that are multiples of 16, blocks at multiples of 16 bytes, other arrays at multiples of
+ * their elements; other calls are refused.  (Codes at multiples of 128 bytes are read fastest.)
  */
 #ifndef PSC_MX4_H
 #define PSC_MX4_H

@@ -115,9 +115,9 @@ struct Grid {
     dim3 blocks;
 };
 Grid grid_of(int rows, int n_tiles) {
-    const int wave = (current_sms() * 8 * 16 + n_tiles - 1) / n_tiles;
-    const int step = std::max(1, std::min(std::max(wave, rows / (AT_ONCE * TURNS)), (rows + AT_ONCE - 1) / AT_ONCE));
-    return {n_tiles, step, dim3((unsigned)(((int64_t)n_tiles * step + 15) / 16))};
+    const int64_t wave = (current_sms() * 8 * 16 + n_tiles - 1) / n_tiles, most = (1ll << 31) / n_tiles;
+    const int64_t step = std::min({std::max<int64_t>(wave, rows / (AT_ONCE * TURNS)), ((int64_t)rows + AT_ONCE - 1) / AT_ONCE, most});
+    return {n_tiles, (int)step, dim3((unsigned)((n_tiles * step + 15) / 16))};
 }
 
 template <typename T>
@@ -155,6 +155,7 @@ psc_status psc_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_stride
     if (K > MAX_QUANTIZE_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 2^30");
     if (!is_mx4(d_q, q_stride, d_blocks, K))
         return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+    if (!is_whole(d_x, dtype)) return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
     if (T == 0) return PSC_OK;
     if (dtype == PSC_BF16)
         return quantize<__nv_bfloat16>(d_x, row_stride, T, K, d_q, q_stride, d_blocks, (cudaStream_t)stream);
@@ -169,6 +170,8 @@ psc_status psc_dequantize_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_
     if (K > MAX_QUANTIZE_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 2^30");
     if (!is_mx4(d_q, q_stride, d_blocks, K))
         return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+    if (!is_whole(d_y, dtype) || (uintptr_t)d_scale % 4)
+        return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
     if (T == 0) return PSC_OK;
     if (dtype == PSC_BF16)
         return dequantize<__nv_bfloat16>(d_q, q_stride, d_blocks, d_scale, T, K, d_y, row_stride, (cudaStream_t)stream);

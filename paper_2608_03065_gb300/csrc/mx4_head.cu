@@ -828,6 +828,8 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
     if (T > MAX_T || V > MAX_V) return ops_fail(PSC_ERR_LIMIT, ME, "too many rows");
     if (!is_mx4(d_w, w_stride, d_w_blocks, K) || (T && !is_mx4(d_q, q_stride, d_q_blocks, K)))
         return ops_fail(PSC_ERR_ARG, ME, "codes or blocks with a bad stride or alignment");
+    if (!is_whole(d_logits, dtype) || (uintptr_t)d_scale % 4 || (uintptr_t)d_w_scale % 4 || (uintptr_t)d_bitmask % 4)
+        return ops_fail(PSC_ERR_ARG, ME, "an address that is no multiple of its elements' size");
     if (T == 0) return PSC_OK;
     const Head h{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
                  (V + 31) / 32, row_stride};

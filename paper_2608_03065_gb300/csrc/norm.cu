@@ -438,6 +438,9 @@ psc_status norm_entry(const char* me, const Norm& a, psc_dtype dtype, void* stre
     if (a.K > MAX_QUANTIZE_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 2^30");
     if (MX4 ? !is_mx4(a.q, a.q_stride, a.blocks, a.K) : a.q_stride < a.K)
         return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+    if (!is_whole(a.x, dtype) || !is_whole(a.residual, dtype) || !is_whole(a.sum, dtype) || (uintptr_t)a.gain % 4 ||
+        (uintptr_t)a.scale % 4)
+        return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
     if (a.T == 0) return PSC_OK;
     if (dtype == PSC_BF16) return norm<__nv_bfloat16, MX4>(a, me, (cudaStream_t)stream);
     return norm<float, MX4>(a, me, (cudaStream_t)stream);

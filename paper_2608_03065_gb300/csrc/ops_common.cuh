@@ -66,6 +66,8 @@ inline bool is_dtype(psc_dtype d) { return d == PSC_F32 || d == PSC_BF16; }
 inline bool is_aligned(const void* p, int64_t stride_bytes, int64_t to) {
     return (uintptr_t)p % to == 0 && stride_bytes % to == 0;
 }
+// Whether rows of a dtype start at multiples of its size (as torch's do).
+inline bool is_whole(const void* p, psc_dtype d) { return (uintptr_t)p % (d == PSC_BF16 ? 2 : 4) == 0; }
 
 // Launch that may start while the stream's previous kernel finishes (programmatic
 // dependent launch; the kernel waits for its results itself), as clusters of

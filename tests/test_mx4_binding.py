@@ -64,14 +64,16 @@ M = 2 ** 31 - 1
         (dict(q_stride=16), ARG), (dict(T=-1), ARG), (dict(K=0), ARG), (dict(res=P, res_stride=63), ARG),
         (dict(sum_=2 * P, sum_stride=63), ARG), (dict(sum_=P, sum_stride=80), ARG),
         (dict(res=2 * P, res_stride=64, sum_=2 * P, sum_stride=72), ARG), (dict(eps=-1e-9), ARG),
-        (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
+        (dict(x=P + 1), ARG), (dict(res=P + 1, res_stride=64), ARG), (dict(sum_=P + 3, sum_stride=64), ARG),
+        (dict(gain=P + 2), ARG), (dict(scale=P + 1), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
         (dict(K=2 ** 30 + 1, stride=M, q_stride=M // 16 * 16), LIMIT)]
 ] + [
     (_norm("mx4", blocks=None), ARG), (_norm("mx4", q=P + 8), ARG), (_norm("mx4", q_stride=40), ARG),
     (_norm("mx4", blocks=P + 4), ARG),
     (_quantize(x=None), ARG), (_quantize(q=None), ARG), (_quantize(blocks=None), ARG), (_quantize(dtype=-1), ARG),
     (_quantize(stride=63), ARG), (_quantize(q_stride=16), ARG), (_quantize(q_stride=40), ARG), (_quantize(q=P + 4), ARG),
-    (_quantize(blocks=P + 8), ARG), (_quantize(T=-1), ARG), (_quantize(K=0), ARG), (_quantize(K=65, stride=65), ARG),
+    (_quantize(blocks=P + 8), ARG), (_quantize(x=P + 1), ARG), (_quantize(x=P + 2, dtype=0), ARG),
+    (_dequantize(y=P + 1), ARG), (_dequantize(scale=P + 2), ARG), (_head(out=P + 1), ARG), (_head(out=P + 2, dtype=0), ARG), (_quantize(T=-1), ARG), (_quantize(K=0), ARG), (_quantize(K=65, stride=65), ARG),
     (_quantize(K=M, stride=M, q_stride=2 ** 31), LIMIT),
     (_dequantize(q=None), ARG), (_dequantize(y=None), ARG), (_dequantize(blocks=None), ARG), (_dequantize(dtype=5), ARG),
     (_dequantize(stride=63), ARG), (_dequantize(q_stride=16), ARG), (_dequantize(q=P + 1), ARG),
