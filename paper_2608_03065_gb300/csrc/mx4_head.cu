@@ -212,7 +212,8 @@ __device__ __forceinline__ void store_group(T* out, int64_t stride, const uint32
     } else {
 #pragma unroll
         for (int j = 0; j < 32; j++) {
-            if (j < n && left > 0) store_f32(out, logit<MASKED>(y[j], tokens[j].scale, tokens[j].word, sw, bit));
+            if (j >= n) break;
+            if (left > 0) store_f32(out, logit<MASKED>(y[j], tokens[j].scale, tokens[j].word, sw, bit));
             out += stride;
         }
     }

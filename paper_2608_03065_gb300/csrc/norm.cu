@@ -225,7 +225,7 @@ __device__ __forceinline__ void unpack_h(const uint32_t (&x)[8], const uint32_t 
 // a block's loads all come at its beginning, and half of its time nothing is under way: 16,384 rows of
 // 4,096 bf16 columns with residual 114 us, this way 76.
 template <typename T, bool MX4>
-__global__ void __launch_bounds__(256, 3) k_norm_many(Norm a, int stages) {
+__global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
     constexpr int NV = 4, N = sizeof(T) * 2, PIECES = N / 4;           // words, 16-byte pieces of a chunk
     extern __shared__ uint4 s_ring[];
     const int chunks = a.K / 8, parts = a.residual ? 2 : 1, step = blockDim.x;
@@ -404,11 +404,11 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
     if (threads <= 256 && a.T <= 2 * current_sms())
         return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
-    if (C == WIDE && threads <= 256) {
+    if (C == WIDE && threads <= 512) {
         // as many blocks as registers leave room for, as many rows ahead as shared memory does
-        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = 768 / threads;
-        const int blocks = std::min(most, RING_BYTES / (2 * stage)), stages = std::min(4, RING_BYTES / (blocks * stage));
-        if (a.T >= 2 * blocks * current_sms())
+        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = std::max(1, 768 / threads);
+        const int blocks = std::max(1, std::min(most, RING_BYTES / (2 * stage))), stages = std::min(4, RING_BYTES / (blocks * stage));
+        if (stages >= 2 && a.T >= 2 * blocks * current_sms())
             return ops_launch(k_norm_many<T, MX4>, dim3(blocks * current_sms()), threads, (size_t)stages * stage, 1, cs, me,
                               a, stages);
     }

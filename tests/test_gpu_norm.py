@@ -178,7 +178,9 @@ def test_a_row_does_not_depend_on_its_batch(psc):  # noqa: F811
 
 @pytest.mark.parametrize("T,K,dtype,residual", [(20000, 72, "bf16", True), (16000, 40, "f32", False), (4001, 4096, "bf16", True),
                                                 (7000, 2048, "bf16", False), (4000, 2056, "f32", True),
-                                                (3000, 8192, "bf16", True), (9000, 1000, "bf16", True)])
+                                                (3000, 8192, "bf16", True), (9000, 1000, "bf16", True),
+                                                (4001, 4095, "bf16", True), (9000, 1003, "f32", True), (20000, 61, "bf16", False),
+                                                (700, 16384, "bf16", True), (700, 13001, "bf16", True)])
 def test_many_rows_are_what_a_few_are(psc, T, K, dtype, residual):  # noqa: F811
     """A batch that is worked on in turns, rows that need a second pass among it, against the same
     rows a few at a time; the sum in place of the residual."""
