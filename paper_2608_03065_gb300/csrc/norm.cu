@@ -325,8 +325,8 @@ __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
 // A block per row, NV chunks of it in a thread's registers (0: any number, read again for what comes after
 // the sums).  Small blocks whose threads have four chunks each keep most loads under way (16,384 rows of 4,096
 // bf16 columns: 128 threads 111 us, 512 threads 141); where there are too few rows for that, four times as many
-// threads, a chunk each, are done sooner (1 row of 2,048 columns: 4.1 us with 64 threads, 1.9 with 256).  Both add
-// up in the same order (SHARES).
+// threads, a chunk each, are done sooner (2,048 columns with residual: 1 row 4.1 us with 64 threads, 1.9 with 256;
+// 600 rows 5.0 and 3.2).  Both add up in the same order (SHARES).
 template <typename T, bool MX4, Chunks C, int NV, int SHARES, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     dep_wait();
@@ -402,7 +402,8 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     // a thread's share goes by the width alone, and so do the sums' orders
     const int chunks = (a.K + (C == SHIFTED ? 14 : 7)) / 8, quarter = (chunks + 3) / 4;
     const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
-    if (threads <= 256 && a.T <= 2 * current_sms())
+    // a chunk a thread while that fits the GPU at once (1024 threads an SM)
+    if (threads <= 256 && (int64_t)a.T * 4 * threads <= 1024ll * current_sms())
         return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
     if (C == WIDE && threads <= 512) {
         // as many blocks as registers leave room for, as many rows ahead as shared memory does
