@@ -6,7 +6,7 @@
  * Conventions, status codes and psc_last_error are those of psc.h, with those that psc_ops.h
  * adds: calls only enqueue work on the stream, may be captured in a CUDA graph, and give the
  * same bits for the same inputs.  Arrays start at multiples of their elements' size (other calls are
- * refused); rows of whole multiples of 8 elements at multiples of 16 bytes are read fastest.
+ * refused); rows of whole multiples of 8 elements at multiples of 32 bytes are read fastest.
  */
 #ifndef PSC_NORM_H
 #define PSC_NORM_H

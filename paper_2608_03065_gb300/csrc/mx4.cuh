@@ -11,8 +11,8 @@ namespace {
 
 constexpr int MAX_QUANTIZE_K = 1 << 30;
 
-// Eight neighbouring columns (a chunk) of a row go in and out by 16-byte accesses.  Where a row starts
-// elsewhere than at a multiple of 16 bytes, or does not end with a chunk, they still do (WIDE false), but
+// Eight neighbouring columns (a chunk) of a row go in and out by accesses of 16 or 32 bytes.  Where a row starts
+// elsewhere than at a multiple of those, or does not end with a chunk, they still do (WIDE false), but
 // for its ends: what is loaded at aligned addresses is shifted into place, and stores take over the end
 // of the previous lane's chunk.  (Element by element: 16,384 rows of 4,095 bf16 columns through the
 // norm into 8 bits 379 us; 16,384 x 4,096 at aligned addresses 111.)
@@ -40,6 +40,26 @@ __device__ __forceinline__ void pack8(const float v[8], uint32_t (&w)[4], const 
 #pragma unroll
     for (int j = 0; j < 4; j++) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
 }
+// A whole, aligned chunk: eight f32 are a sector of the L2, and go in one access (two of 16 bytes each write half of
+// every sector: 151,936 x 1,024 f32 into 4 bits and back 241 us, 214 this way).
+__device__ __forceinline__ void load_chunk(const float* from, uint32_t (&w)[8]) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(from));
+}
+__device__ __forceinline__ void load_chunk(const __nv_bfloat16* from, uint32_t (&w)[4]) {
+    const uint4 x = *reinterpret_cast<const uint4*>(from);
+    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+}
+__device__ __forceinline__ void store_chunk(float* to, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+__device__ __forceinline__ void store_chunk(__nv_bfloat16* to, const uint32_t (&w)[4]) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // f(std::integral_constant) of a number from 0 to 3 (words' places have to be known to the compiler).
 template <typename F>
 __device__ __forceinline__ void with_place(int i, F f) {
@@ -56,7 +76,9 @@ __device__ __forceinline__ void load8(const T* row, int k, int K, float v[8]) {
     const int off = WIDE ? 0 : (int)((uintptr_t)(row + k) & 15);
     const uint4* at = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row + k) - off);
     uint32_t w[N];
-    if (WIDE || (off == 0 && k + 8 <= K)) {
+    if (WIDE) {
+        load_chunk(row + k, w);
+    } else if (off == 0 && k + 8 <= K) {
 #pragma unroll
         for (int i = 0; i < N / 4; i++) {
             const uint4 x = at[i];
@@ -131,10 +153,7 @@ __device__ __forceinline__ void store8(T* row, int k, int K, const float v[8], b
     uint32_t w[N];
     pack8(v, w, (const T*)nullptr);
     if (WIDE) {
-        if (!there) return;
-#pragma unroll
-        for (int i = 0; i < N / 4; i++)
-            reinterpret_cast<uint4*>(row + k)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        if (there) store_chunk(row + k, w);
     } else {
         store_shifted<N, sizeof(T)>(reinterpret_cast<uint8_t*>(row + k), w, there ? min(8, K - k) : 0, follows);
     }
@@ -160,10 +179,10 @@ __device__ __forceinline__ void store8_at(T* row, int k, int K, bool in_place, c
     for (int j = 0; j < 8; j++)
         if (k + j >= 0 && k + j < K) store_f32(row + k + j, v[j]);
 }
-// Whether rows of these elements (none at all, too) are whole chunks at multiples of 16 bytes.
+// Whether rows of these elements (none at all, too) are whole chunks at multiples of a chunk's size.
 template <typename T>
 inline bool wide_rows(const void* p, int64_t stride, int K) {
-    return !p || (K % 8 == 0 && is_aligned(p, stride * (int64_t)sizeof(T), 16));
+    return !p || (K % 8 == 0 && is_aligned(p, stride * (int64_t)sizeof(T), 8 * sizeof(T)));
 }
 
 // The largest of |a|, |b| and |c|; NaN if one is.  As bit patterns magnitudes order as they do as numbers, with
