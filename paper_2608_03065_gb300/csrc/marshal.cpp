@@ -10,7 +10,7 @@
 
 namespace {
 
-PyObject *s_shape, *s_dtype, *s_is_cuda, *s_stride, *s_data_ptr, *s_numel, *s_is_contiguous, *s_get_device;
+PyObject *s_shape, *s_dtype, *s_stride, *s_data_ptr, *s_numel, *s_is_contiguous, *s_get_device;
 PyObject *t_bf16, *t_f32, *t_i8, *t_u8, *t_i32;
 
 using NormRows = int32_t (*)(const void*, int32_t, int64_t, const void*, int64_t, void*, int64_t, const float*, float,
@@ -43,7 +43,7 @@ bool attribute_is(PyObject* t, PyObject* name, PyObject* value) {
 bool number(PyObject* t, PyObject* method, int64_t* out) {
     const Ref r(PyObject_CallMethodNoArgs(t, method));
     if (!r.p || !PyLong_Check(r.p)) return false;
-    *out = (int64_t)PyLong_AsUnsignedLongLong(r.p);
+    *out = (int64_t)PyLong_AsUnsignedLongLong(r.p);       // addresses may have the top bit; -1 is an error
     return !PyErr_Occurred();
 }
 // The two numbers of a tuple.
@@ -57,40 +57,55 @@ bool size_of(PyObject* t, int64_t* rows, int64_t* cols) {
     const Ref shape(PyObject_GetAttr(t, s_shape));
     return two(shape.p, rows, cols) && *rows >= 0 && *rows <= INT32_MAX && *cols > 0 && *cols <= INT32_MAX;
 }
-bool on_device(PyObject* t, PyObject* dtype) { return attribute_is(t, s_dtype, dtype) && attribute_is(t, s_is_cuda, Py_True); }
+// The current device, by psc.py's _device: every tensor of a call has to be on it (those of the host give -1).
+PyObject* device_function;
+struct Device {
+    int64_t id = -1;
+    bool take() {
+        const Ref here(PyObject_CallNoArgs(device_function));
+        if (!here.p || !PyLong_Check(here.p)) return false;
+        id = PyLong_AsLongLong(here.p);
+        return id >= 0;
+    }
+    bool has(PyObject* t, PyObject* dtype) const {
+        int64_t device;
+        return attribute_is(t, s_dtype, dtype) && number(t, s_get_device, &device) && device == id;
+    }
+};
 
 // A 2-D tensor of `rows` rows and at least `cols` columns, neighbouring in memory.
 struct Matrix {
     int64_t at = 0, stride = 0;
-    bool take(PyObject* t, PyObject* dtype, int64_t rows, int64_t cols) {
+    bool take(const Device& on, PyObject* t, PyObject* dtype, int64_t rows, int64_t cols) {
         int64_t r, c, unit;
-        if (!on_device(t, dtype) || !size_of(t, &r, &c) || r != rows || c < cols) return false;
+        if (!on.has(t, dtype) || !size_of(t, &r, &c) || r != rows || c < cols) return false;
         const Ref strides(PyObject_CallMethodNoArgs(t, s_stride));
         if (!two(strides.p, &stride, &unit) || unit != 1) return false;
         if (rows == 1 && stride < c) stride = c;                // a row of its own may carry any stride
         return number(t, s_data_ptr, &at);
     }
-    bool take_or_none(PyObject* t, PyObject* dtype, int64_t rows, int64_t cols) {
-        return t == Py_None || take(t, dtype, rows, cols);
+    bool take_or_none(const Device& on, PyObject* t, PyObject* dtype, int64_t rows, int64_t cols) {
+        return t == Py_None || take(on, t, dtype, rows, cols);
     }
 };
 // A contiguous tensor of at least n elements.
 struct Vector {
     int64_t at = 0;
-    bool take(PyObject* t, PyObject* dtype, int64_t n) {
+    bool take(const Device& on, PyObject* t, PyObject* dtype, int64_t n) {
         int64_t has;
-        if (!on_device(t, dtype) || !number(t, s_numel, &has) || has < n) return false;
+        if (!on.has(t, dtype) || !number(t, s_numel, &has) || has < n) return false;
         const Ref contiguous(PyObject_CallMethodNoArgs(t, s_is_contiguous));
         return contiguous.p == Py_True && number(t, s_data_ptr, &at);
     }
-    bool take_or_none(PyObject* t, PyObject* dtype, int64_t n) { return t == Py_None || take(t, dtype, n); }
+    bool take_or_none(const Device& on, PyObject* t, PyObject* dtype, int64_t n) { return t == Py_None || take(on, t, dtype, n); }
 };
 // A matrix in 4 bits.
 struct Mx4 {
     Matrix codes;
     Vector blocks;
-    bool take(PyObject* q, PyObject* b, int64_t rows, int64_t K) {
-        return codes.take(q, t_u8, rows, (K + 31) / 32 * 16) && blocks.take(b, t_u8, (rows + 127) / 128 * ((K + 127) / 128) * 512);
+    bool take(const Device& on, PyObject* q, PyObject* b, int64_t rows, int64_t K) {
+        return codes.take(on, q, t_u8, rows, (K + 31) / 32 * 16) &&
+               blocks.take(on, b, t_u8, (rows + 127) / 128 * ((K + 127) / 128) * 512);
     }
 };
 // bf16 or f32, as the library counts them; -1: neither.
@@ -104,13 +119,7 @@ P* at(int64_t a) {
     return reinterpret_cast<P*>(static_cast<uintptr_t>(a));
 }
 // The handle of a stream argument, by psc.py's _stream.
-PyObject *stream_function, *device_function;
-// Whether a tensor is on the current device, by psc.py's _device.
-bool is_here(PyObject* t) {
-    const Ref here(PyObject_CallNoArgs(device_function));
-    int64_t device;
-    return here.p && PyLong_Check(here.p) && number(t, s_get_device, &device) && PyLong_AsLongLong(here.p) == device;
-}
+PyObject* stream_function;
 bool stream_of(PyObject* argument, void** out) {
     const Ref s(PyObject_CallOneArg(stream_function, argument));
     if (!s.p) return false;
@@ -138,23 +147,24 @@ struct NormInputs {
     Matrix x, residual, sum;
     Vector gain;
     float eps = 0;
-    bool take(PyObject* px, PyObject* pgain, PyObject* peps, PyObject* presidual, PyObject* psum) {
+    bool take(const Device& on, PyObject* px, PyObject* pgain, PyObject* peps, PyObject* presidual, PyObject* psum) {
         PyObject* dtype;
         code = code_of(px, &dtype);
         if (code < 0 || !size_of(px, &T, &K)) return false;
         eps = (float)PyFloat_AsDouble(peps);
-        return !PyErr_Occurred() && x.take(px, dtype, T, K) && residual.take_or_none(presidual, dtype, T, K) &&
-               sum.take_or_none(psum, dtype, T, K) && gain.take_or_none(pgain, t_f32, K);
+        return !PyErr_Occurred() && x.take(on, px, dtype, T, K) && residual.take_or_none(on, presidual, dtype, T, K) &&
+               sum.take_or_none(on, psum, dtype, T, K) && gain.take_or_none(on, pgain, t_f32, K);
     }
 };
 
 // norm_rows(x, q, scale, gain, eps, residual, sum_out, stream)
 PyObject* norm_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Device on;
     NormInputs i;
     Matrix q;
     Vector scale;
-    if (n != 8 || !i.take(a[0], a[3], a[4], a[5], a[6]) || !q.take(a[1], t_i8, i.T, i.K) || !scale.take(a[2], t_f32, i.T) ||
-        !is_here(a[0]))
+    if (n != 8 || !on.take() || !i.take(on, a[0], a[3], a[4], a[5], a[6]) || !q.take(on, a[1], t_i8, i.T, i.K) ||
+        !scale.take(on, a[2], t_f32, i.T))
         return not_plain();
     void* stream;
     if (!stream_of(a[7], &stream)) return nullptr;
@@ -167,11 +177,12 @@ PyObject* norm_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // norm_mx4(x, q, blocks, scale, gain, eps, residual, sum_out, stream)
 PyObject* norm_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Device on;
     NormInputs i;
     Mx4 q;
     Vector scale;
-    if (n != 9 || !i.take(a[0], a[4], a[5], a[6], a[7]) || !q.take(a[1], a[2], i.T, i.K) || !scale.take(a[3], t_f32, i.T) ||
-        !is_here(a[0]))
+    if (n != 9 || !on.take() || !i.take(on, a[0], a[4], a[5], a[6], a[7]) || !q.take(on, a[1], a[2], i.T, i.K) ||
+        !scale.take(on, a[3], t_f32, i.T))
         return not_plain();
     void* stream;
     if (!stream_of(a[8], &stream)) return nullptr;
@@ -184,13 +195,14 @@ PyObject* norm_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // quantize_mx4(x, q, blocks, stream)
 PyObject* quantize_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Device on;
     int64_t T, K;
     PyObject* dtype;
     Matrix x;
     Mx4 q;
-    if (n != 4) return not_plain();
+    if (n != 4 || !on.take()) return not_plain();
     const int32_t code = code_of(a[0], &dtype);
-    if (code < 0 || !size_of(a[0], &T, &K) || !x.take(a[0], dtype, T, K) || !q.take(a[1], a[2], T, K) || !is_here(a[0]))
+    if (code < 0 || !size_of(a[0], &T, &K) || !x.take(on, a[0], dtype, T, K) || !q.take(on, a[1], a[2], T, K))
         return not_plain();
     void* stream;
     if (!stream_of(a[3], &stream)) return nullptr;
@@ -202,15 +214,16 @@ PyObject* quantize_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // dequantize_mx4(q, blocks, y, scale, stream)
 PyObject* dequantize_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Device on;
     int64_t T, K;
     PyObject* dtype;
     Matrix y;
     Mx4 q;
     Vector scale;
-    if (n != 5) return not_plain();
+    if (n != 5 || !on.take()) return not_plain();
     const int32_t code = code_of(a[2], &dtype);
-    if (code < 0 || !size_of(a[2], &T, &K) || !y.take(a[2], dtype, T, K) || !q.take(a[0], a[1], T, K) ||
-        !scale.take_or_none(a[3], t_f32, T) || !is_here(a[0]))
+    if (code < 0 || !size_of(a[2], &T, &K) || !y.take(on, a[2], dtype, T, K) || !q.take(on, a[0], a[1], T, K) ||
+        !scale.take_or_none(on, a[3], t_f32, T))
         return not_plain();
     void* stream;
     if (!stream_of(a[4], &stream)) return nullptr;
@@ -222,22 +235,23 @@ PyObject* dequantize_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // head_logits_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask, stream)
 PyObject* head_logits_mx4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    Device on;
     int64_t T, V, c;
     PyObject* dtype;
     Mx4 q, w;
     Matrix logits;
     Vector scale, w_scale, mask;
-    if (n != 10 || !PyLong_Check(a[5])) return not_plain();
+    if (n != 10 || !PyLong_Check(a[5]) || !on.take()) return not_plain();
     const int64_t K = PyLong_AsLongLong(a[5]);
     if (PyErr_Occurred() || K <= 0 || K > INT32_MAX) return not_plain();
     const int32_t code = code_of(a[4], &dtype);
-    if (code < 0 || !size_of(a[0], &T, &c) || !size_of(a[2], &V, &c) || !q.take(a[0], a[1], T, K) ||
-        !w.take(a[2], a[3], V, K) || !logits.take(a[4], dtype, T, V) || !scale.take_or_none(a[6], t_f32, T) ||
-        !w_scale.take_or_none(a[7], t_f32, V) || !is_here(a[0]))
+    if (code < 0 || !size_of(a[0], &T, &c) || !size_of(a[2], &V, &c) || !q.take(on, a[0], a[1], T, K) ||
+        !w.take(on, a[2], a[3], V, K) || !logits.take(on, a[4], dtype, T, V) || !scale.take_or_none(on, a[6], t_f32, T) ||
+        !w_scale.take_or_none(on, a[7], t_f32, V))
         return not_plain();
     if (a[8] != Py_None) {
         int64_t rows, words;
-        if (!size_of(a[8], &rows, &words) || rows != T || words != (V + 31) / 32 || !mask.take(a[8], t_i32, T * words))
+        if (!size_of(a[8], &rows, &words) || rows != T || words != (V + 31) / 32 || !mask.take(on, a[8], t_i32, T * words))
             return not_plain();
     }
     void* stream;
@@ -287,7 +301,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__marshal(void) {
     s_shape = PyUnicode_InternFromString("shape");
     s_dtype = PyUnicode_InternFromString("dtype");
-    s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_stride = PyUnicode_InternFromString("stride");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");

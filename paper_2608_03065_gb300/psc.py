@@ -161,10 +161,11 @@ def _device() -> int:
     return torch.cuda.current_device()
 
 
-def _here(t, name):
+def _here(**tensors):
     """Kernels run on the current device: a tensor of another one is refused."""
-    if t.is_cuda and t.get_device() != _device():
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, and the current device is cuda:{_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.get_device() != _device():
+            raise ValueError(f"{name} is on cuda:{t.get_device()}, and the current device is cuda:{_device()}")
 
 
 _current = None         # of the current device, the current stream's handle
@@ -565,7 +566,7 @@ def psc_quantize_rows(x, q, scale, stream=None):
                                     _stream(stream)))
 
 
-def _norm_inputs(x, residual, sum_out, gain):
+def _norm_inputs(x, residual, sum_out, gain, **outputs):
     """What the two norms share: x's sizes, and the inputs' addresses and strides."""
     import torch
     shape, dtype = x.shape, x.dtype
@@ -573,7 +574,7 @@ def _norm_inputs(x, residual, sum_out, gain):
         raise ValueError("x must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(x)
-    _here(x, "x")
+    _here(x=x, residual=residual, sum_out=sum_out, gain=gain, **outputs)
     px, sx = _at(x, dtype, "x", T, K)
     pr, sr = (None, 0) if residual is None else _at(residual, dtype, "residual", T, K)
     ps, ss = (None, 0) if sum_out is None else _at(sum_out, dtype, "sum_out", T, K)
@@ -590,7 +591,7 @@ def psc_norm_quantize_rows(x, q, scale, gain=None, eps: float = 1e-6, residual=N
         if code is not None:
             return _check(code) if code else None
     import torch
-    T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
+    T, K, inputs = _norm_inputs(x, residual, sum_out, gain, q=q, scale=scale)
     pq, sq = _at(q, torch.int8, "q", T, K)
     _check((_lib or load()).psc_norm_quantize_rows(*inputs, eps, T, K, pq, sq, _ptr(scale, torch.float32, "scale", T),
                                                    _stream(stream)))
@@ -729,7 +730,7 @@ def psc_quantize_mx4(x, q, blocks, stream=None):
         raise ValueError("x must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(x)
-    _here(x, "x")
+    _here(x=x, q=q, blocks=blocks)
     px, sx = _at(x, x.dtype, "x", T, K)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
     _check((_lib or load()).psc_quantize_mx4(px, code, sx, T, K, pq, sq, pb, _stream(stream)))
@@ -747,7 +748,7 @@ def psc_dequantize_mx4(q, blocks, y, scale=None, stream=None):
         raise ValueError("y must be a 2-D tensor")
     T, K = shape
     code = _dtype_code(y)
-    _here(y, "y")
+    _here(y=y, q=q, blocks=blocks, scale=scale)
     py, sy = _at(y, y.dtype, "y", T, K)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
     _check((_lib or load()).psc_dequantize_mx4(pq, sq, pb, _ptr(scale, torch.float32, "scale", T), T, K, py, code, sy,
@@ -762,7 +763,7 @@ def psc_norm_quantize_mx4(x, q, blocks, scale, gain=None, eps: float = 1e-6, res
         if code is not None:
             return _check(code) if code else None
     import torch
-    T, K, inputs = _norm_inputs(x, residual, sum_out, gain)
+    T, K, inputs = _norm_inputs(x, residual, sum_out, gain, q=q, blocks=blocks, scale=scale)
     pq, sq, pb = _mx4(q, blocks, T, K, "q")
     _check((_lib or load()).psc_norm_quantize_mx4(*inputs, eps, T, K, pq, sq, pb, _ptr(scale, torch.float32, "scale", T),
                                                   _stream(stream)))
@@ -782,7 +783,7 @@ def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_
         raise ValueError("q and w must be 2-D tensors")
     T, V = qs[0], ws[0]
     code = _dtype_code(logits)
-    _here(q, "q")
+    _here(q=q, q_blocks=q_blocks, w=w, w_blocks=w_blocks, logits=logits, scale=scale, w_scale=w_scale, bitmask=bitmask)
     pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
     pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
     pl, sl = _at(logits, logits.dtype, "logits", T, V)

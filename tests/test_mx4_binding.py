@@ -139,3 +139,73 @@ def test_the_formats_values_by_hand():
     assert codes[0, :12].tolist() == [7, 9, 0, 2, 2, 4, 4, 6, 6, 8, 6, 15]
     assert codes[0, 32] == 8 + 6                # 1e-3 * 2^12 = 4.096
     assert decode(codes, e)[0, :12].tolist() == [6, -0.5, 0, 1, 1, 2, 2, 4, 4, 0, 4, -6]
+
+
+class _Tensor:
+    """As much of a CUDA tensor as the binding asks for; of an empty batch, so that nothing is launched."""
+
+    def __init__(self, *shape, dtype, device=0):
+        self.shape, self.dtype, self.device, self.is_cuda = shape, dtype, device, True
+
+    def stride(self):
+        return self.shape[1:] + (1,)
+
+    def dim(self):
+        return len(self.shape)
+
+    def data_ptr(self):
+        return P
+
+    def numel(self):
+        return self.shape[0] * (self.shape[1] if len(self.shape) > 1 else 1)
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self.device
+
+
+def _calls(psc):  # noqa: F811
+    """Each entry with the tensors it takes, over no rows."""
+    f32, u8 = torch.float32, torch.uint8
+    x = lambda: _Tensor(0, 64, dtype=f32)  # noqa: E731
+    v = lambda n: _Tensor(n, dtype=f32)  # noqa: E731
+    q, b = (lambda n: _Tensor(n, 32, dtype=u8)), (lambda n: _Tensor(n, dtype=u8))
+    return [(psc.psc_norm_quantize_rows, dict(x=x(), q=_Tensor(0, 64, dtype=torch.int8), scale=v(0), gain=v(64),
+                                              residual=x(), sum_out=x())),
+            (psc.psc_norm_quantize_mx4, dict(x=x(), q=q(0), blocks=b(0), scale=v(0), gain=v(64), residual=x(), sum_out=x())),
+            (psc.psc_quantize_mx4, dict(x=x(), q=q(0), blocks=b(0))),
+            (psc.psc_dequantize_mx4, dict(q=q(0), blocks=b(0), y=x(), scale=v(0))),
+            (psc.psc_head_logits_mx4, dict(q=q(0), q_blocks=b(0), w=q(100), w_blocks=b(512), logits=_Tensor(0, 100, dtype=f32),
+                                           K=64, scale=v(0), w_scale=v(100), bitmask=_Tensor(0, 4, dtype=torch.int32)))]
+
+
+@pytest.mark.parametrize("marshal", [True, False])
+def test_tensors_of_another_device_are_refused(psc, monkeypatch, marshal):  # noqa: F811
+    """Every tensor of a call has to be on the current device (here the binding's idea of it), with the calls taken
+    apart in C and in Python."""
+    lib = psc.load()
+    monkeypatch.setattr(psc, "_device", lambda: 1)
+    if marshal:
+        psc._load_marshal(lib, lambda: 1)
+        if psc._marshal is None:
+            pytest.skip("the module is not built here")
+    else:
+        monkeypatch.setattr(psc, "_marshal", None)
+    try:
+        for entry, tensors in _calls(psc):
+            for t in tensors.values():
+                if isinstance(t, _Tensor):
+                    t.device = 1
+            entry(**tensors, stream=0)
+            for name, t in tensors.items():
+                if not isinstance(t, _Tensor):
+                    continue
+                t.device = 0
+                with pytest.raises(ValueError, match=f"{name} is on cuda:0"):
+                    entry(**tensors, stream=0)
+                t.device = 1
+    finally:
+        if marshal:
+            psc._load_marshal(lib)
