@@ -283,3 +283,34 @@ def test_other_streams_and_graphs(psc):  # noqa: F811
     torch.cuda.synchronize()
     for u, w in zip(a, b):
         assert torch.equal(u, w)
+
+
+@pytest.mark.parametrize("T", [3, 8000])
+def test_sums_of_any_two_bf16(psc, T):  # noqa: F811
+    """x + residual over all bit patterns, subnormal ones among them: the f32 sum, rounded once more."""
+    K, rng = 64, np.random.default_rng(T)
+    bits = rng.integers(-32768, 32768, (2, T, K)).astype(np.int16)
+    bits[1, ::2] = (bits[0, ::2] ^ -32768) + rng.integers(-4, 5, bits[0, ::2].shape)      # nearly -x
+    bits[1, 1::4] = bits[0, 1::4] - rng.integers(0, 1 << 11, bits[0, 1::4].shape)        # a smaller exponent, often
+    x, res = (torch.from_numpy(b).view(torch.bfloat16) for b in bits)
+    out = torch.empty(T, K, dtype=torch.bfloat16, device="cuda")
+    q, s = torch.empty(T, K, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    psc.psc_norm_quantize_rows(x.cuda(), q, s, residual=res.cuda(), sum_out=out)
+    want, got = (x.float() + res.float()).bfloat16(), out.cpu()
+    nan = want.isnan()
+    assert torch.equal(got.isnan(), nan) and (want.float().abs()[~nan] < 2.0 ** -126).any()
+    assert torch.equal(got[~nan].view(torch.int16), want[~nan].view(torch.int16))
+
+
+@pytest.mark.parametrize("K,dtype", [(1001, "bf16"), (4095, "bf16"), (130, "f32")])
+def test_a_row_at_any_address_has_the_same_codes(psc, K, dtype):  # noqa: F811
+    """Rows that start anywhere: the codes are those of the row alone, the scale up to the order of its sum."""
+    rng = np.random.default_rng(K)
+    x = _dev(_data(rng, 9, K, dtype)).to(DT[dtype])
+    q, s = torch.empty(9, K, dtype=torch.int8, device="cuda"), torch.empty(9, device="cuda")
+    psc.psc_norm_quantize_rows(x, q, s)
+    for t in range(9):
+        q1, s1 = torch.empty(1, K, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+        psc.psc_norm_quantize_rows(x[t:t + 1].clone(), q1, s1)
+        assert torch.equal(q1[0], q[t])
+        np.testing.assert_allclose(_f64(s1), _f64(s[t:t + 1]), rtol=2 * _tolerance(K), atol=0)
