@@ -137,6 +137,9 @@ __device__ __forceinline__ void drain(uint32_t full0, int c, int slots) {
 // k_mx4_few: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by all
 // tokens (its N): with few tokens the weights' bytes are all that counts, and tensor cores that give
 // most of their columns away keep up with them.
+// Bound by memory and its beginning and end: 1 token over 128,256 x 2048 takes 27.2 us (140 MB), of which
+// about six are the launch, the first loads' latency and the last tiles; 16 tokens over 151,936 x 1024
+// under masks that leave a few dozen tokens each 15.4 us, mostly that latency and the -inf of the other tiles.
 //   warps 0, 2-4  TMA: the weights' codes (16 KB a stage), the tokens', both sides' exponents
 //   warp 1        the exponents' way to TMEM, the products
 //   warps 8-15    a lane per vocabulary row, two warps for 32 of them: scales, mask, logits
@@ -431,7 +434,9 @@ psc_status head_few(const Head& h, T* logits, cudaStream_t cs) {
 // exponents in both).  Where a tile's tokens fit shared memory (K up to 2048) they stay there, and
 // only the weights are loaded, from memory once and from the L2 for the other tiles of tokens: an SM
 // takes in 64 bytes a cycle, and a stage's 384 cycles of products need 14 KB this way, 31 KB where
-// the tokens come along.  A lane of the epilogue has a token, and 32 neighbouring logits of it with one
+// the tokens come along.  256 tokens over 128,256 x 4096: 61.8 us, at the memory's latency (seven slots, 86 KB of
+// weights an SM); 1024 over 262,144 x 2048, mixed masks: 204 us, 5.4 PFLOP/s, beside 537 MB of logits at
+// the GPU's power limit.  A lane of the epilogue has a token, and 32 neighbouring logits of it with one
 // word of the mask; they go out by way of shared memory, 64 bytes of a token at a time.
 //   warps 0, 2-4  TMA: the weights' codes and exponents, the tokens' codes and exponents
 //   warp 5        the exponents' way to TMEM
