@@ -231,7 +231,8 @@ __device__ __forceinline__ uint32_t codes8(const float v[8], float inverse) {
 // A thread's eight columns from 8 c on of a row, to codes and exponents; `top` the largest magnitude of
 // them.  All 32 lanes of a warp call it for neighbouring chunks c (or 16 of one row and 16 of another), lane
 // 0's a multiple of 16; what lies past the row's last tile stores nothing.  row_blocks: where the row's first
-// block's exponent is.  Returns whether the block is NaN.
+// block's exponent is.  INSIDE: all chunks lie in the row, which is whole tiles.  Returns whether the block is NaN.
+template <bool INSIDE = false>
 __device__ __forceinline__ bool quantize8(const float v[8], float top, int c, int K, uint8_t* q_row,
                                           uint8_t* row_blocks) {
     const int lane = threadIdx.x & 31;
@@ -239,13 +240,13 @@ __device__ __forceinline__ bool quantize8(const float v[8], float top, int c, in
     bits = max(bits, __shfl_xor_sync(FULL, bits, 1));
     bits = max(bits, __shfl_xor_sync(FULL, bits, 2));
     const uint32_t byte = block_byte(bits);
-    if (c < (K + 31) / 32 * 4)
+    if (INSIDE || c < (K + 31) / 32 * 4)
         *reinterpret_cast<uint32_t*>(q_row + c * 4) = byte == 255 ? 0u : codes8(v, block_inverse(byte));
     // the four blocks of a tile's row, by one of its sixteen lanes
     uint32_t word = byte << (8 * ((lane >> 2) & 3));
     word |= __shfl_xor_sync(FULL, word, 4);
     word |= __shfl_xor_sync(FULL, word, 8);
-    if (!(lane & 15) && c < (K + 127) / 128 * 16) *reinterpret_cast<uint32_t*>(row_blocks + (int64_t)c * 32) = word;
+    if (!(lane & 15) && (INSIDE || c < (K + 127) / 128 * 16)) *reinterpret_cast<uint32_t*>(row_blocks + (int64_t)c * 32) = word;
     return byte == 255;
 }
 inline bool is_mx4(const void* q, int64_t stride, const void* blocks, int K) {

@@ -88,11 +88,11 @@ struct Row {
     const float* gain;
     int K, shift;
     bool in_place;
-    __device__ __forceinline__ Row(const Norm& a, int row)
+    __device__ __forceinline__ Row(const Norm& a, int row, int width)
         : x((const T*)a.x + (size_t)row * a.x_stride),
           residual(a.residual ? (const T*)a.residual + (size_t)row * a.residual_stride : nullptr),
           sum(a.sum ? (T*)a.sum + (size_t)row * a.sum_stride : nullptr), q(a.q + (size_t)row * a.q_stride), gain(a.gain),
-          K(a.K), shift(0), in_place(true) {
+          K(width), shift(0), in_place(true) {
         if (C != SHIFTED) return;
         shift = row_shift(x);
         in_place = (!residual || row_shift(residual) == shift) && (!sum || row_shift(sum) == shift) &&
@@ -223,35 +223,38 @@ __device__ __forceinline__ void unpack_h(const uint32_t (&x)[8], const uint32_t 
 // Many aligned rows: blocks stay and go from row to row, and each thread copies its chunks of the next `stages`
 // rows into shared memory ahead (cp.async; nobody else reads them, so that only their own thread waits).  In k_norm
 // a block's loads all come at its beginning, and half of its time nothing is under way: 16,384 rows of
-// 4,096 bf16 columns with residual 114 us, this way 76.
-template <typename T, bool MX4>
+// 4,096 bf16 columns with residual 114 us, this way 75.  FULL_ROWS: every thread has its four chunks (rows of whole
+// multiples of 1,024 columns), which leaves out checks where instructions bound it: without residual
+// 62.0 us with this and the residual known at run time only, 48.9 this way; into 4 bits with residual 111 and 105.
+template <typename T, bool MX4, bool RESIDUAL, bool FULL_ROWS>
 __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
     constexpr int NV = 4, N = sizeof(T) * 2, PIECES = N / 4;           // words, 16-byte pieces of a chunk
+    constexpr int parts = RESIDUAL ? 2 : 1;
     extern __shared__ uint4 s_ring[];
-    const int chunks = a.K / 8, parts = a.residual ? 2 : 1, step = blockDim.x;
+    const int step = blockDim.x, chunks = FULL_ROWS ? NV * step : a.K / 8, K = chunks * 8;
     dep_wait();
     dep_launch();
     // a thread's pieces of a stage, one of each thread after the other
     auto place = [&](int stage, int part, int i, int piece) {
-        return s_ring + (((stage * parts + part) * NV + i) * PIECES + piece) * step + threadIdx.x;
+        return s_ring + stage * (parts * NV * PIECES * step) + threadIdx.x + ((part * NV + i) * PIECES + piece) * step;
     };
     auto copy = [&](int stage, uint32_t r) {
-        if (r < (uint32_t)a.T)
+        if (r < (uint32_t)a.T) {
+            const T* x = (const T*)a.x + (size_t)r * a.x_stride + threadIdx.x * 8;
+            const T* residual = RESIDUAL ? (const T*)a.residual + (size_t)r * a.residual_stride + threadIdx.x * 8 : nullptr;
 #pragma unroll
             for (int i = 0; i < NV; i++) {
-                const int c = i * step + threadIdx.x;
-                if (c >= chunks) break;
-                for (int part = 0; part < parts; part++) {
-                    const T* from = (part ? (const T*)a.residual + (size_t)r * a.residual_stride
-                                          : (const T*)a.x + (size_t)r * a.x_stride) + c * 8;
+                if (!FULL_ROWS && i * step + (int)threadIdx.x >= chunks) break;
+#pragma unroll
+                for (int part = 0; part < parts; part++)
 #pragma unroll
                     for (int piece = 0; piece < PIECES; piece++)
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
                                          (uint32_t)__cvta_generic_to_shared(place(stage, part, i, piece))),
-                                     "l"((const char*)from + 16 * piece)
+                                     "l"((const char*)((part ? residual : x) + i * step * 8) + 16 * piece)
                                      : "memory");
-                }
             }
+        }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     auto read = [&](int stage, int part, int i, uint32_t (&w)[N]) {
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
     for (int i = 0; i < stages; i++) copy(i, blockIdx.x + i * gridDim.x);
     int stage = 0, turn = 0;
     for (uint32_t r = blockIdx.x; r < (uint32_t)a.T; r += gridDim.x, stage = stage + 1 == stages ? 0 : stage + 1) {
-        const Row<T, WIDE> row(a, r);
+        const Row<T, WIDE> row(a, r, K);
         uint8_t* blocks = MX4 ? a.blocks + block_at(r, 0, (a.K + 127) / 128) : nullptr;
         // this row's copies, the oldest of `stages` groups
         if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
         for (int i = 0; i < NV; i++) {
             const int c = i * step + threadIdx.x;
             uint32_t x[N] = {}, res[N] = {};
-            if (c < chunks) {
+            if (FULL_ROWS || c < chunks) {
                 read(stage, 0, i, x);
                 if (parts == 2) read(stage, 1, i, res);
             }
@@ -293,7 +296,7 @@ __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
             }
             s.squares += squares;
             const float most = largest8(v[i], top);
-            if (MX4) bad |= quantize8(v[i], most, c, a.K, row.q, blocks);
+            if (MX4) bad |= quantize8<FULL_ROWS>(v[i], most, c, K, row.q, blocks);
             else top = most;
         }
         copy(stage, r + stages * gridDim.x);
@@ -331,7 +334,7 @@ template <typename T, bool MX4, Chunks C, int NV, int SHARES, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_norm(Norm a) {
     dep_wait();
     dep_launch();
-    const Row<T, C> row(a, blockIdx.x);
+    const Row<T, C> row(a, blockIdx.x, a.K);
     const int chunks = (a.K + row.shift + 7) / 8;
     // whole warps go round together: a warp's lanes share blocks and tiles
     const int rounds = NV ? NV : (chunks + blockDim.x - 1) / blockDim.x;
@@ -406,12 +409,21 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
     if (threads <= 256 && (int64_t)a.T * 4 * threads <= 1024ll * current_sms())
         return ops_launch(k_norm<T, MX4, C, 1, 4, 1024>, dim3(a.T), 4 * threads, 0, 1, cs, me, a);
     if (C == WIDE && threads <= 512) {
-        // as many blocks as registers leave room for, as many rows ahead as shared memory does
-        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1), most = std::max(1, 768 / threads);
+        // as many blocks as registers leave room for, as many rows ahead as shared memory does; into 8 bits with a
+        // residual memory bounds many rows, and fewer blocks with more rows ahead are faster (768 and 512 threads an SM:
+        // 16,384 rows of 4,096 bf16 columns 77.8 and 75.2 us, 65,536 of 2,048 157 and 143; without the residual
+        // 48.9 and 67.0, into 4 bits with it 104.7 and 113.6;
+        // few rows a block: 8,192 of 2,048 with residual 22.2 and 23.1)
+        const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1);
+        const bool fewer = a.residual && !MX4 && a.T >= 8 * (768 / threads) * current_sms();
+        const int most = std::max(1, (fewer ? 512 : 768) / threads);
         const int blocks = std::max(1, std::min(most, RING_BYTES / (2 * stage))), stages = std::min(4, RING_BYTES / (blocks * stage));
         if (stages >= 2 && a.T >= 2 * blocks * current_sms())
-            return ops_launch(k_norm_many<T, MX4>, dim3(blocks * current_sms()), threads, (size_t)stages * stage, 1, cs, me,
-                              a, stages);
+            return ops_launch(!a.residual          ? chunks == 4 * threads ? k_norm_many<T, MX4, false, true>
+                                                                           : k_norm_many<T, MX4, false, false>
+                              : chunks == 4 * threads ? k_norm_many<T, MX4, true, true>
+                                                      : k_norm_many<T, MX4, true, false>,
+                              dim3(blocks * current_sms()), threads, (size_t)stages * stage, 1, cs, me, a, stages);
     }
     return ops_launch(threads <= 256         ? k_norm<T, MX4, C, 4, 1, 256>
                       : chunks <= 4 * threads ? k_norm<T, MX4, C, 4, 1, 1024>
