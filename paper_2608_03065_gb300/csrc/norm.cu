@@ -162,7 +162,9 @@ __device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, in
         return {unit, MX4 ? r : unit * r};
     }
     // the squares, or r, may leave f32 (squares of less than 2^-126 lose bits, but not of a sum from 2^-76
-    // on): once more, with the largest magnitude near 1
+    // on): once more, with the largest magnitude near 1.  It reads the sums again, of which a lane may have stored
+    // another's (store_shifted), and no barrier need have come since in a block of one warp.
+    __syncthreads();
     RowStats t = again(1.f);
     __syncthreads();
     over_block<SHARES>(t, turn++);

@@ -1,0 +1,56 @@
+"""The norms where rows are read a second time, against numpy in 64 bits.  Reference forms and tolerances are those
+of test_gpu_norm."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from tests import _mx4_ref as ref
+from tests.test_gpu_norm import _data, _int8, _tolerance
+from tests.test_gpu_ops import DT, U, _dev, _f64, psc  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("K", [1001, 1003, 250])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("out", ["new", "x", "residual"])
+def test_sums_read_again_by_blocks_of_one_warp(psc, K, dtype, out):  # noqa: F811
+    """Many rows of up to 1024 columns that start anywhere: a warp a row, whose lanes store the ends of each other's sums
+    and read them again in rows whose squares leave f32, and in rows of zeros."""
+    T = 1300
+    rng = np.random.default_rng([K, T])
+    x, res = _data(rng, T, K, dtype), _data(rng, T, K, dtype)
+    x[::5], res[::5] = 0, 0
+    for start, size in ((1, 1e28), (2, 1e-28)):
+        for a in (x, res):
+            scaled = (a[start::5] * np.float32(size)).astype(np.float32)
+            a[start::5] = ref.round_bf16(scaled) if dtype == "bf16" else scaled
+    g = (rng.uniform(0.5, 1.5, K) * rng.choice([-1, 1], K)).astype(np.float32)
+    with np.errstate(divide="ignore"):
+        h, v, r = ref.norm(x, res, g, 0.0, dtype == "bf16")
+    r = np.where((h == 0).all(1), 0, r)                     # a row of zeros has the factor 0
+    codes, e = ref.quantize(v)
+    n = psc.psc_mx4_row_bytes(K)
+
+    def inputs():
+        xd, rd = _dev(x).to(DT[dtype]), _dev(res).to(DT[dtype])
+        return xd, rd, {"new": torch.full((T, K), 7.0, dtype=DT[dtype], device="cuda"), "x": xd, "residual": rd}[out]
+
+    xd, rd, sd = inputs()
+    q, s = torch.zeros(T, n, dtype=torch.uint8, device="cuda"), torch.full((T,), 7.0, device="cuda")
+    b = torch.full((psc.psc_mx4_block_bytes(T, K),), 5, dtype=torch.uint8, device="cuda")
+    psc.psc_norm_quantize_mx4(xd, q, b, s, gain=_dev(g), eps=0.0, residual=rd, sum_out=sd)
+    np.testing.assert_array_equal(_f64(sd), h)
+    np.testing.assert_array_equal(q.cpu().numpy(), ref.pack(codes))
+    np.testing.assert_array_equal(b.cpu().numpy(), ref.tiles(e, K, 5))
+    np.testing.assert_allclose(_f64(s), r, rtol=_tolerance(K), atol=0)
+
+    xd, rd, sd = inputs()
+    q = torch.zeros(T, K, dtype=torch.int8, device="cuda")
+    psc.psc_norm_quantize_rows(xd, q, s, gain=_dev(g), eps=0.0, residual=rd, sum_out=sd)
+    want, scale = _int8(v, r)
+    np.testing.assert_array_equal(_f64(sd), h)
+    np.testing.assert_array_equal(q.cpu().numpy(), want)
+    np.testing.assert_allclose(_f64(s), scale, rtol=_tolerance(K) + U, atol=0)
