@@ -29,6 +29,7 @@ struct Head {
     const uint32_t* bitmask;
     int W;                              // mask words of a row
     int64_t row_stride;
+    int polls;                          // after which a wait gives up
 };
 
 // ------------------------------------------------------------ the tensor-core path
@@ -126,10 +127,17 @@ __device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int x, int
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
-// Lets the copies in flight land: those of the last `slots` of c uses of a ring.
-__device__ __forceinline__ void drain(uint32_t full0, int c, int slots) {
-    for (int i = max(0, c - slots); i < c; i++)
-        for (int it = 0; it < (1 << 20) && !mbar_try(full0 + 8 * (i % slots), (i / slots) & 1); it++) {}
+// After a wait that gave up: blocks end only when nothing is under way to their memory any more.  All warps
+// have left their loops by then, and some may have loaded stages that others did not come to; those arrive without
+// their copies, so that every stage that any warp began completes when its copies have landed.  (A stage begins when
+// the one before it in its slot has been used, so it was complete, and no slot has two stages that are not.)
+__device__ __forceinline__ void drain(uint32_t full0, int stages, int slots) {
+    int left = 1 << 20;
+    for (int i = max(0, stages - slots); i < stages; i++)
+        while (left > 0 && !mbar_try(full0 + 8 * (i % slots), (i / slots) & 1)) left--;
+}
+__device__ __forceinline__ void drain_products(uint32_t bar) {
+    for (int it = 0; it < (1 << 20) && !mbar_try(bar, 0); it++) {}
 }
 
 // -------------------------------------------------------------------- up to 128 tokens
@@ -249,7 +257,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     __shared__ __align__(16) Token s_tokens[EPILOGUE][GROUPS * 32];
     __shared__ uint32_t s_active[MASKED ? MAX_TILES / 32 : 1];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_failed;
+    __shared__ int s_failed, s_loaded[4];             // stages that each loading warp has begun
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // stages start at multiples of 1024 bytes: weights, tokens, the weights' exponents, the tokens'
     const uint32_t base = (smem_addr(dyn) + 1023) & ~1023u, x_codes = p.N * KS / 2;
@@ -302,34 +310,36 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     auto is_active = [&](int i) { return !MASKED || mine > MAX_TILES || (s_active[i / 32] >> (i & 31) & 1); };
     const int vt0 = blockIdx.x, vt_step = gridDim.x;  // tile i of this block
 
-    // Loads one part of every stage: a box at (x, y), x + step, ... of a map; y_step: from tile to tile.
-    auto load_part = [&](const CUtensorMap* map, int step, int y_step, int part, int bytes) {
+    // Loads one part of every stage: a box at (x, y), x + step, ... of a map; y_step: from tile to tile.  All lanes
+    // leave together, by what the warp's wait said (the flag itself may change between two lanes' looks at it).
+    auto load_part = [&](int loader, const CUtensorMap* map, int step, int y_step, int part, int bytes) {
         const bool issuer = elect_one();
         Place at;
         int c = 0;
-        for (int i = 0; i < mine && !*failed; i++) {
+        bool ok = true;
+        for (int i = 0; i < mine && ok; i++) {
             if (!is_active(i)) continue;
             const int vt = vt0 + i * vt_step;
             for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
                 const uint32_t to = base + at.s * p.stage_bytes + part, bar = full(at.s);
-                if (!warp_wait(empty(at.s), at.parity ^ 1, failed)) break;
+                if (!(ok = warp_wait(empty(at.s), at.parity ^ 1, failed, h.polls))) break;
                 if (issuer) {
                     mbar_arrive_tx(bar, bytes);
                     tma_2d(to, map, k * step, vt * y_step, bar);
                 }
             }
         }
-        if (*failed && issuer) drain(full(0), c, p.stages);
+        if (issuer) s_loaded[loader] = c;
     };
 
     if (warp == 0) {
-        load_part(&w_map, 128, VT, 0, W_CODES);
+        load_part(0, &w_map, 128, VT, 0, W_CODES);
     } else if (warp == 2) {
-        load_part(&x_map, 128, 0, W_CODES, x_codes);
+        load_part(1, &x_map, 128, 0, W_CODES, x_codes);
     } else if (warp == 3) {
-        load_part(&w_blocks_map, 256, 1, W_CODES + x_codes, 2 * SF);
+        load_part(2, &w_blocks_map, 256, 1, W_CODES + x_codes, 2 * SF);
     } else if (warp == 4) {
-        load_part(&x_blocks_map, 256, 0, W_CODES + x_codes + 2 * SF, 2 * SF);
+        load_part(3, &x_blocks_map, 256, 0, W_CODES + x_codes + 2 * SF, 2 * SF);
     } else if (warp == 1) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane issues.
         const bool issuer = elect_one();
@@ -338,12 +348,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
         bool ok = true;
         for (int i = 0; i < mine && ok; i++) {
             if (!is_active(i)) continue;
-            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) break;
+            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls))) break;
             const uint32_t d = tmem + acc.s * p.acc;
             for (int k = 0; k < n_k; k++, at.next(p.stages)) {
                 const uint32_t a = lo + at.s * step, b = a + W_CODES / 16, e = b + x_codes / 16;
                 const uint32_t sf = tmem + 2 * p.acc + at.s * 16;
-                if (!(ok = warp_wait(full(at.s), at.parity, failed))) break;
+                if (!(ok = warp_wait(full(at.s), at.parity, failed, h.polls))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
                     copy_stage<false, 1>(e, e + 64, sf);
@@ -353,10 +363,6 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
                 }
             }
             acc.next(2);
-        }
-        if (!ok && issuer) {                          // let the products in flight finish
-            mma_commit<false>(drained);
-            for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
         }
     } else if (warp >= FIRST) {
         const int quad = warp & 3, part = (warp - FIRST) >> 2;      // of every two groups of 32 tokens, this warp's
@@ -381,7 +387,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
                     !MASKED ? FULL : wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u};
             }
             __syncwarp();
-            if (!warp_wait(acc_full(acc.s), acc.parity, failed)) break;
+            if (!warp_wait(acc_full(acc.s), acc.parity, failed, h.polls)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int i = 0; i < GROUPS; i++) {
@@ -404,6 +410,19 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (*failed) {                                    // drain's comment; nobody writes the flag any more
+        const bool issuer = elect_one();              // the lane that issued (it is the same every time)
+        if (warp == 1 && issuer) {
+            mma_commit<false>(drained);
+            drain_products(drained);
+        } else if (warp <= 4 && issuer) {
+            const int most = max(max(s_loaded[0], s_loaded[1]), max(s_loaded[2], s_loaded[3]));
+            for (int i = s_loaded[max(0, warp - 1)]; i < most; i++) mbar_arrive(full(i % p.stages));
+            drain(full(0), most, p.stages);
+        }
+        __syncwarp();
+        __syncthreads();
+    }
     if (warp == 1) tmem_free<false>(tmem);
     if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
@@ -469,6 +488,24 @@ __device__ __forceinline__ uint32_t at_first(uint32_t bar) {
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
     return r;
 }
+// A word of the pair's other block; how to set it.
+__device__ __forceinline__ int read_other(const int* p, int other) {
+    int v;
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %1, %2;\n ld.shared::cluster.s32 %0, [r];\n}"
+                 : "=r"(v)
+                 : "r"(smem_addr(p)), "r"(other)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ void set_other(int* p, int other) {
+    asm volatile("{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n st.shared::cluster.s32 [r], 1;\n}" ::"r"(smem_addr(p)),
+                 "r"(other)
+                 : "memory");
+}
+// Takes `bytes` that do not come off what a barrier of this block waits for.
+__device__ __forceinline__ void forgo_bytes(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 // Arrives at this block's barrier when the pair's copies and products so far are done.
 __device__ __forceinline__ void commit_here(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -499,6 +536,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     __shared__ __align__(16) float s_scale[EPILOGUE][NV / 2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_failed, s_item;                  // how many items' weights have begun to be loaded
+    __shared__ int s_other_failed, s_loaded[4];       // stages that each loading warp has begun
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int side = (int)cluster_rank();
     // slots start at multiples of 1024 bytes: the tokens' codes and exponents, the weights' codes, their exponents
@@ -526,7 +564,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     if (warp == 2 && lane < 4)
         prefetch_map(lane == 0 ? &w_map : lane == 1 ? &x_map : lane == 2 ? &w_blocks_map : &x_blocks_map);
     if (threadIdx.x == 0) {
-        s_failed = 0, s_item = 0;
+        s_failed = 0, s_item = 0, s_other_failed = 0;
         for (int s = 0; s < a_slots; s++) mbar_init(a_full(s), 2), mbar_init(a_empty(s), 1);
         for (int s = 0; s < b_slots; s++) mbar_init(b_full(s), 1), mbar_init(b_empty(s), 1);
         for (int s = 0; s < SF_SLOTS; s++) {
@@ -563,8 +601,9 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     // vocabulary rows of a tile that the products take: both halves in whole sixteens
     auto rows_of = [&](int vt) { return (min(NV, h.V - vt * NV) + 31) / 32 * 32; };
 
-    // Loads one part of every stage (of tokens that stay, of the first item with them).
-    auto load_part = [&](const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
+    // Loads one part of every stage (of tokens that stay, of the first item with them).  All lanes leave together,
+    // by what the warp's wait said.
+    auto load_part = [&](int loader, const CUtensorMap* map, int step, uint32_t to0, int slot_bytes, int slots, uint32_t full0,
                          uint32_t empty0, int bytes, bool tokens, auto row_of) {
         const uint32_t there0 = at_first(full0);
         const bool issuer = elect_one();
@@ -576,23 +615,22 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             int x = 0;
             for (int k = 0; k < n_k; k++, c++, x += step, at.next(slots)) {
                 const uint32_t to = to0 + at.s * slot_bytes, own = full0 + 8 * at.s, bar = there0 + 8 * at.s;
-                if (!warp_wait(empty0 + 8 * at.s, at.parity ^ 1, failed)) return false;
+                if (!warp_wait(empty0 + 8 * at.s, at.parity ^ 1, failed, h.polls)) return false;
                 if (issuer) {
                     if (side == 0) mbar_arrive_tx(own, 2 * bytes);
                     load_tile(to, map, x, y, bar);
                 }
             }
-            return !*failed;
+            return true;
         });
-        // the first block sees both blocks' copies land, and the second does not end before it
-        if (*failed && side == 0 && issuer) drain(full0, c, slots);
+        if (issuer) s_loaded[loader] = c;
     };
 
     auto codes_row = [&](int, int vt) { return vt * NV + side * (rows_of(vt) / 2); };
     if (warp == 0) {
-        load_part(&w_map, 128, b_base, B_CODES, b_slots, b_full(0), b_empty(0), B_CODES, false, codes_row);
+        load_part(0, &w_map, 128, b_base, B_CODES, b_slots, b_full(0), b_empty(0), B_CODES, false, codes_row);
     } else if (warp == 2) {
-        load_part(&w_blocks_map, 256, e_base, B_EXPS, SF_SLOTS, e_full(0), e_empty(0), B_EXPS, false, [&](int, int vt) {
+        load_part(1, &w_blocks_map, 256, e_base, B_EXPS, SF_SLOTS, e_full(0), e_empty(0), B_EXPS, false, [&](int, int vt) {
             *const_cast<volatile int*>(&s_item) = s_item + 1;
             return vt * NV / 128;
         });
@@ -609,10 +647,10 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             return !*failed;
         });
     } else if (warp == 3) {
-        load_part(&x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
+        load_part(2, &x_map, 128, base, A_BYTES, a_slots, a_full(0), a_empty(0), A_CODES, true,
                   [&](int mt, int) { return mt * MT + side * (MT / 2); });
     } else if (warp == 4) {
-        load_part(&x_blocks_map, 256, base + A_CODES, A_BYTES, a_slots, a_full(0), a_empty(0), 2 * SF, true,
+        load_part(3, &x_blocks_map, 256, base + A_CODES, A_BYTES, a_slots, a_full(0), a_empty(0), 2 * SF, true,
                   [&](int mt, int) { return mt * 2 + side; });
     } else if (warp == 5 && side == 0) {
         // The whole warp waits, so that addresses and descriptors stay in uniform registers; one lane
@@ -626,8 +664,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             for (int k = 0; k < n_k; k++, at_a.next(a_slots), at.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), e = e_lo + at.s * (B_EXPS / 16);
                 const uint32_t sf = tmem + 2 * NV + at.s * SF_COLS;
-                if (!warp_wait2(e_full(at.s), at.parity, sf_empty(at.s), at.parity ^ 1, failed) ||
-                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed)))
+                if (!warp_wait2(e_full(at.s), at.parity, sf_empty(at.s), at.parity ^ 1, failed, h.polls) ||
+                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed, h.polls)))
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
@@ -643,17 +681,16 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
         const bool issuer = elect_one();
         const uint32_t a_lo = (base & 0x3FFFF) >> 4, b_lo = (b_base & 0x3FFFF) >> 4;
         Place unit, at_b, at_e, acc;
-        bool ok = true;
         each([&](int, int vt, bool fresh, bool last) {
             const uint32_t idesc = instruction(MT, rows_of(vt)), d = tmem + acc.s * NV, shift = vt * NV % 128 / 32;
             Place at_a = unit;
-            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed))) return false;
+            if (!warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls)) return false;
             for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(b_slots), at_e.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_CODES / 16);
                 const uint32_t sf = tmem + 2 * NV + at_e.s * SF_COLS;
-                ok = warp_wait2(sf_full(at_e.s), at_e.parity, b_full(at_b.s), at_b.parity, failed) &&
-                     (!fresh || warp_wait(a_full(at_a.s), at_a.parity, failed));
-                if (!ok) return false;
+                if (!warp_wait2(sf_full(at_e.s), at_e.parity, b_full(at_b.s), at_b.parity, failed, h.polls) ||
+                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed, h.polls)))
+                    return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
                     mma_stage<true, 2>(a, b, sf, shift, d, idesc, k);
@@ -667,11 +704,6 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             acc.next(2);
             return true;
         });
-        if (!ok && issuer) {                          // let the products in flight finish
-            mma_commit<true>(drained);
-            mma_commit<true>(drained);
-            for (int it = 0; it < (1 << 20) && !mbar_try(drained, 0); it++) {}
-        }
     } else if (warp >= FIRST) {
         constexpr int COLS = 64 / sizeof(T);          // logits of a token that go out together
         const int quad = warp & 3, part = (warp - FIRST) >> 2;
@@ -697,7 +729,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                     if (v0 + i * 32 + lane < h.V) scales[i * 32 + lane] = h.w_scale[v0 + i * 32 + lane];
                 __syncwarp();
             }
-            if (!warp_wait(acc_full(acc.s), acc.parity, failed)) return false;
+            if (!warp_wait(acc_full(acc.s), acc.parity, failed, h.polls)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             T* rows = logits + (size_t)(t0 + (lane >> 2)) * h.row_stride + v0 + (lane & 3) * (COLS / 4);
 #pragma unroll
@@ -791,7 +823,33 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    cluster_sync();                                   // nothing of this block is used by the other any more
+    if (threadIdx.x == 0 && *failed) set_other(&s_other_failed, side ^ 1);
+    cluster_sync();                                   // nothing of this block is used by the other any more, unless
+    if (*failed || *const_cast<volatile int*>(&s_other_failed)) {     // drain's comment; both blocks come here or neither
+        const bool issuer = elect_one();              // the lane that issued (it is the same every time)
+        if (side == 0 && (warp == 1 || warp == 5) && issuer) mma_commit<true>(drained);
+        if (warp == 1 && issuer) drain_products(drained);
+        // both blocks' copies are counted at the first's barriers: there a stage takes an arrival with the bytes of
+        // both, of each of its loaders
+        auto finish = [&](int loader, uint32_t full0, int slots, int bytes, int most) {
+            const int own = s_loaded[loader], theirs = read_other(&s_loaded[loader], 1);
+            for (int i = own; i < most; i++) {
+                if (i < theirs) mbar_arrive_tx(full0 + 8 * (i % slots), bytes);
+                else mbar_arrive(full0 + 8 * (i % slots));
+            }
+            for (int i = theirs; i < own; i++) forgo_bytes(full0 + 8 * (i % slots), bytes);
+            drain(full0, most, slots);
+        };
+        auto begun = [&](int loader) { return max(s_loaded[loader], read_other(&s_loaded[loader], 1)); };
+        if (side == 0 && issuer) {
+            if (warp == 0) finish(0, b_full(0), b_slots, B_CODES, begun(0));
+            if (warp == 2) finish(1, e_full(0), SF_SLOTS, B_EXPS, begun(1));
+            if (warp == 3) finish(2, a_full(0), a_slots, A_CODES, max(begun(2), begun(3)));
+            if (warp == 4) finish(3, a_full(0), a_slots, 2 * SF, max(begun(2), begun(3)));
+        }
+        __syncwarp();
+        cluster_sync();
+    }
     if (warp == 1) tmem_free<true>(tmem);
     if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
@@ -819,6 +877,22 @@ psc_status head(const Head& h, T* logits, cudaStream_t cs) {
     return h.T <= FEW ? head_few(h, logits, cs) : head_many(h, logits, cs);
 }
 
+psc_status head_entry(const char* me, Head h, void* logits, psc_dtype dtype, void* stream) {
+    if (h.T < 0 || h.V <= 0 || h.K <= 0 || h.row_stride < h.V || !is_dtype(dtype) || !h.w || !h.w_blocks ||
+        (h.T && (!h.q || !h.q_blocks || !logits)))
+        return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    if (h.K > MAX_K) return ops_fail(PSC_ERR_LIMIT, me, "K over 131,072");
+    if (h.T > MAX_T || h.V > MAX_V) return ops_fail(PSC_ERR_LIMIT, me, "too many rows");
+    if (!is_mx4(h.w, h.w_stride, h.w_blocks, h.K) || (h.T && !is_mx4(h.q, h.q_stride, h.q_blocks, h.K)))
+        return ops_fail(PSC_ERR_ARG, me, "codes or blocks with a bad stride or alignment");
+    if (!is_whole(logits, dtype) || (uintptr_t)h.scale % 4 || (uintptr_t)h.w_scale % 4 || (uintptr_t)h.bitmask % 4)
+        return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
+    if (h.T == 0) return PSC_OK;
+    h.W = (h.V + 31) / 32;
+    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)logits, (cudaStream_t)stream);
+    return head(h, (float*)logits, (cudaStream_t)stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -827,20 +901,20 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
                                int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                                const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
                                psc_dtype dtype, int64_t row_stride, void* stream) {
-    if (T < 0 || V <= 0 || K <= 0 || row_stride < V || !is_dtype(dtype) || !d_w || !d_w_blocks ||
-        (T && (!d_q || !d_q_blocks || !d_logits)))
-        return ops_fail(PSC_ERR_ARG, ME, "bad arguments");
-    if (K > MAX_K) return ops_fail(PSC_ERR_LIMIT, ME, "K over 131,072");
-    if (T > MAX_T || V > MAX_V) return ops_fail(PSC_ERR_LIMIT, ME, "too many rows");
-    if (!is_mx4(d_w, w_stride, d_w_blocks, K) || (T && !is_mx4(d_q, q_stride, d_q_blocks, K)))
-        return ops_fail(PSC_ERR_ARG, ME, "codes or blocks with a bad stride or alignment");
-    if (!is_whole(d_logits, dtype) || (uintptr_t)d_scale % 4 || (uintptr_t)d_w_scale % 4 || (uintptr_t)d_bitmask % 4)
-        return ops_fail(PSC_ERR_ARG, ME, "an address that is no multiple of its elements' size");
-    if (T == 0) return PSC_OK;
-    const Head h{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
-                 (V + 31) / 32, row_stride};
-    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)d_logits, (cudaStream_t)stream);
-    return head(h, (float*)d_logits, (cudaStream_t)stream);
+    return head_entry(ME, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
+                               0, row_stride, WAIT_POLLS},
+                      d_logits, dtype, stream);
+}
+
+psc_status psc_mx4_check_wait(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
+                              int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
+                              const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
+                              psc_dtype dtype, int64_t row_stride, int32_t limit, void* stream) {
+    const char* me = "psc_mx4_check_wait";
+    if (limit < 0 || limit > WAIT_POLLS) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    return head_entry(me, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
+                               0, row_stride, limit},
+                      d_logits, dtype, stream);
 }
 
 psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream) {

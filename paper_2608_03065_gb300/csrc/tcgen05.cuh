@@ -1,4 +1,4 @@
-// What the tensor-core kernels (head.cu, mx4.cu) share: barriers in shared memory with bounded
+// What the tensor-core kernels (head.cu, mx4_head.cu) share: barriers in shared memory with bounded
 // waits, TMA copies and their maps, operand descriptors, the accumulators' way back.
 #pragma once
 
@@ -32,9 +32,10 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+constexpr int WAIT_POLLS = 1 << 22;
 // Bounded wait: gives up after some seconds, or soon after any other wait of the block did.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-    for (int it = 0; it < (1 << 22); it++) {
+    for (int it = 0; it < WAIT_POLLS; it++) {
         if (mbar_try(bar, parity)) return true;
         if ((it & 1023) == 1023 && *failed) return false;
     }
@@ -43,8 +44,8 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 // The same by a whole warp, with one answer for all lanes; and for two barriers at once
 // (a poll takes about a hundred cycles to answer, so both are asked before either is looked at).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
-    for (int it = 0; it < (1 << 22); it++) {
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed, int polls = WAIT_POLLS) {
+    for (int it = 0; it < polls; it++) {
         if (__all_sync(FULL, mbar_try(bar, parity))) return true;
         if ((it & 1023) == 1023 && __any_sync(FULL, *failed)) return false;
     }
@@ -52,10 +53,10 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return false;
 }
 __device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1,
-                                           volatile int* failed) {
+                                           volatile int* failed, int polls = WAIT_POLLS) {
     const bool a = mbar_try(bar0, parity0), b = mbar_try(bar1, parity1);
     if (__all_sync(FULL, a && b)) return true;
-    return warp_wait(bar0, parity0, failed) && warp_wait(bar1, parity1, failed);
+    return warp_wait(bar0, parity0, failed, polls) && warp_wait(bar1, parity1, failed, polls);
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;

@@ -33,7 +33,7 @@ EXPORTED_OPS = ["psc_quantize_rows", "psc_head_work_bytes", "psc_head_logits", "
                 "psc_sample_work_bytes", "psc_sample"]
 # include/psc_mx4.h: the vocabulary projection in microscaled 4-bit floating point
 EXPORTED_MX4 = ["psc_mx4_block_bytes", "psc_quantize_mx4", "psc_dequantize_mx4", "psc_head_logits_mx4",
-                "psc_mx4_faults"]
+                "psc_mx4_faults", "psc_mx4_check_wait"]
 # include/psc_norm.h: the norm in front of either projection
 EXPORTED_NORM = ["psc_norm_quantize_rows", "psc_norm_quantize_mx4"]
 NOALLOC_MAX_ROWS = 16384
@@ -138,6 +138,7 @@ def load(path: str = LIB_PATH):
         "psc_norm_quantize_mx4": (i32, [vp, i32, i64, vp, i64, vp, i64, vp, f32, i32, i32, vp, i64, vp, vp, vp]),
         "psc_head_logits_mx4": (i32, [vp, i64, vp, vp, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, i64, vp]),
         "psc_mx4_faults": (i32, [vp, i32, vp]),
+        "psc_mx4_check_wait": (i32, [vp, i64, vp, vp, i32, vp, i64, vp, vp, i32, i32, vp, vp, i32, i64, i32, vp]),
         "psc_sample_work_bytes": (i64, [i32]),
         "psc_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
@@ -777,6 +778,12 @@ def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_
         code = _marshal.head_logits_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask, stream)
         if code is not None:
             return _check(code) if code else None
+    _check((_lib or load()).psc_head_logits_mx4(*_head_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask),
+                                                _stream(stream)))
+
+
+def _head_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask):
+    """The library's arguments of the projection, up to the stream."""
     import torch
     qs, ws = q.shape, w.shape
     if len(qs) != 2 or len(ws) != 2:
@@ -787,9 +794,8 @@ def psc_head_logits_mx4(q, q_blocks, w, w_blocks, logits, K: int, scale=None, w_
     pq, sq, pqb = _mx4(q, q_blocks, T, K, "q")
     pw, sw, pwb = _mx4(w, w_blocks, V, K, "w")
     pl, sl = _at(logits, logits.dtype, "logits", T, V)
-    _check((_lib or load()).psc_head_logits_mx4(pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb,
-                                                _ptr(w_scale, torch.float32, "w_scale", V), V, K,
-                                                _mask_ptr(bitmask, T, V), pl, code, sl, _stream(stream)))
+    return (pq, sq, pqb, _ptr(scale, torch.float32, "scale", T), T, pw, sw, pwb, _ptr(w_scale, torch.float32, "w_scale", V),
+            V, K, _mask_ptr(bitmask, T, V), pl, code, sl)
 
 
 def psc_mx4_faults(reset: bool = False, stream=None) -> int:
@@ -798,6 +804,14 @@ def psc_mx4_faults(reset: bool = False, stream=None) -> int:
     out = ctypes.c_int32(0)
     _check(load().psc_mx4_faults(ctypes.byref(out), 1 if reset else 0, _stream(stream)))
     return out.value
+
+
+def psc_mx4_check_wait(q, q_blocks, w, w_blocks, logits, K: int, limit: int, scale=None, w_scale=None, bitmask=None,
+                       stream=None):
+    """Self-test of the fault path: psc_head_logits_mx4 with waits that give up after `limit` polls
+    (some logits are not written; psc_mx4_faults counts the blocks)."""
+    _check(load().psc_mx4_check_wait(*_head_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask), limit,
+                                     _stream(stream)))
 
 
 def psc_sample_work_bytes(B: int) -> int:

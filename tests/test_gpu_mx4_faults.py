@@ -1,0 +1,78 @@
+"""The 4-bit projection where its waits give up, without any fault: psc_mx4_check_wait runs it with waits that are
+too short, and what matters is that it ends, counts the blocks, writes no logit that is not right, and leaves the device
+as it was."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from tests.test_gpu_mx4 import _matrix
+from tests.test_gpu_ops import _mask, _pack, psc  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+# few tokens, with one part of a stage small and with all alike; pairs of blocks whose tokens stay, and whose come along
+SIZES = [(1, 30001, 2048), (16, 25000, 512), (128, 20001, 1024), (300, 30001, 512), (200, 15000, 2304), (600, 9000, 300)]
+
+
+def _call(psc, T, V, K, masked):  # noqa: F811
+    rng = np.random.default_rng([T, V, K])
+    qc, wc = rng.integers(0, 16, (T, K), dtype=np.uint8), rng.integers(0, 16, (V, K), dtype=np.uint8)
+    nb = (K + 31) // 32
+    qe, we = rng.integers(124, 130, (T, nb)).astype(np.uint8), rng.integers(118, 124, (V, nb)).astype(np.uint8)
+    matrices = (*_matrix(psc, qc, qe, K), *_matrix(psc, wc, we, K))
+    bm = _pack(_mask(rng, "mixed", T, V)) if masked else None
+
+    def call(limit=None):
+        big = torch.full((T, V + 3), 7.0, device="cuda")
+        if limit is None:
+            psc.psc_head_logits_mx4(*matrices, big[:, :V], K, bitmask=bm)
+        else:
+            psc.psc_mx4_check_wait(*matrices, big[:, :V], K, limit, bitmask=bm)
+        assert (big[:, V:] == 7).all()
+        return big[:, :V]
+
+    return call
+
+
+@pytest.mark.parametrize("T,V,K", SIZES)
+def test_waits_that_give_up_at_once(psc, T, V, K):  # noqa: F811
+    """Every block gives up, with nothing under way."""
+    call = _call(psc, T, V, K, False)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    tokens, rows = (1, 128) if T <= 128 else (-(-T // 256), 192)
+    tiles = -(-V // rows)
+    blocks = min(tiles, sms) if T <= 128 else 2 * tokens * min(sms // 2 // tokens, tiles)
+    want = call()
+    before = psc.psc_mx4_faults()
+    assert (call(0) == 7).all()
+    assert psc.psc_mx4_faults() - before == blocks
+    assert torch.equal(call(), want)
+    assert psc.psc_mx4_faults() - before == blocks
+
+
+@pytest.mark.parametrize("T,V,K", SIZES)
+@pytest.mark.parametrize("masked", [False, True])
+def test_waits_that_give_up_midway(psc, T, V, K, masked):  # noqa: F811
+    """Blocks give up with copies and products under way: what is written is right, and the calls after it are."""
+    call = _call(psc, T, V, K, masked)
+    want = call()
+    for limit in (1, 2, 3, 5, 8, 13, 20, 32, 50, 100, 300, 1000, 4000):
+        got = call(limit)
+        torch.cuda.synchronize()
+        assert ((got == 7) | (got == want)).all(), limit
+        assert torch.equal(call(), want)
+    before = psc.psc_mx4_faults()
+    assert torch.equal(call(1 << 22), want)                 # as long as the projection itself waits
+    assert psc.psc_mx4_faults() == before
+
+
+def test_counts_are_kept_until_they_are_reset(psc):  # noqa: F811
+    call = _call(psc, 3, 5000, 256, False)
+    psc.psc_mx4_faults(reset=True)
+    assert psc.psc_mx4_faults() == 0
+    call(0), call(0)
+    assert psc.psc_mx4_faults() == 2 * 40
+    assert psc.psc_mx4_faults(reset=True) == 2 * 40
+    assert psc.psc_mx4_faults() == 0
