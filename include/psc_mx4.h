@@ -69,7 +69,8 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
                                psc_dtype dtype, int64_t row_stride, void* stream);
 
 /* Blocks of psc_head_logits_mx4 on the current device in which a bounded wait gave up, since the
- * library was loaded or the last reset; synchronises the stream (not while it is captured). */
+ * library was loaded or the last reset; synchronises the stream (not while it is captured).  reset != 0 takes
+ * off the count what it reports: each fault is in one of several callers' reports, whatever runs beside them. */
 psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream);
 
 /* Self-test of that fault path: psc_head_logits_mx4 with waits that give up after `limit` polls (0 to

@@ -1,6 +1,7 @@
 // psc_head_logits_mx4: the vocabulary projection in microscaled 4-bit floating point, under the
 // grammar's mask.
 #include <algorithm>
+#include <mutex>
 
 #include "mx4.cuh"
 #include "tcgen05.cuh"
@@ -12,8 +13,16 @@ const char* const ME = "psc_head_logits_mx4";
 constexpr int MAX_K = 131072;
 constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, rounded up to tiles, in 32 bits
 
-// Blocks in which a bounded wait gave up.
+// Blocks in which a bounded wait gave up; what a reset takes off it is what it has reported, so that none is lost that
+// another stream adds meanwhile.
 __device__ int g_faults;
+std::mutex g_faults_read;                   // a report and its reset at a time
+
+__global__ void k_take_faults(int reported) {
+    dep_wait();
+    dep_launch();
+    atomicSub(&g_faults, reported);
+}
 
 struct Head {
     const uint8_t* q;
@@ -921,11 +930,12 @@ psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream) {
     const char* me = "psc_mx4_faults";
     if (!h_faults) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
     cudaStream_t cs = (cudaStream_t)stream;
+    std::lock_guard<std::mutex> alone(g_faults_read);
     psc_status s = ops_check(cudaMemcpyFromSymbolAsync(h_faults, g_faults, 4, 0, cudaMemcpyDeviceToHost, cs), me);
     if (s == PSC_OK) s = ops_check(cudaStreamSynchronize(cs), me);
-    if (s == PSC_OK && reset) {
-        static const int none = 0;
-        s = ops_check(cudaMemcpyToSymbolAsync(g_faults, &none, 4, 0, cudaMemcpyHostToDevice, cs), me);
+    if (s == PSC_OK && reset && *h_faults) {
+        s = ops_launch(k_take_faults, dim3(1), 1, 0, 1, cs, me, *h_faults);
+        if (s == PSC_OK) s = ops_check(cudaStreamSynchronize(cs), me);
     }
     return s;
 }

@@ -76,3 +76,42 @@ def test_counts_are_kept_until_they_are_reset(psc):  # noqa: F811
     assert psc.psc_mx4_faults() == 2 * 40
     assert psc.psc_mx4_faults(reset=True) == 2 * 40
     assert psc.psc_mx4_faults() == 0
+
+
+def test_resets_lose_no_fault_of_another_stream(psc):  # noqa: F811
+    """Two threads count and reset while others' projections give up on streams of their own: every fault is reported
+    once."""
+    import threading
+    call = _call(psc, 3, 5000, 256, False)
+    psc.psc_mx4_faults(reset=True)
+    streams, reports, errors = [torch.cuda.Stream() for _ in range(4)], [0, 0], []
+    rounds, done = 150, threading.Event()
+
+    def work(stream):
+        try:
+            with torch.cuda.stream(stream):
+                for _ in range(rounds):
+                    call(0)
+                stream.synchronize()
+        except Exception as e:              # noqa: BLE001
+            errors.append(e)
+
+    def count(i):
+        try:
+            while not done.is_set():
+                reports[i] += psc.psc_mx4_faults(reset=True, stream=streams[2 + i])
+        except Exception as e:              # noqa: BLE001
+            errors.append(e)
+
+    workers = [threading.Thread(target=work, args=(s,)) for s in streams[:2]]
+    counters = [threading.Thread(target=count, args=(i,)) for i in range(2)]
+    for t in workers + counters:
+        t.start()
+    for t in workers:
+        t.join()
+    done.set()
+    for t in counters:
+        t.join()
+    assert not errors
+    assert sum(reports) + psc.psc_mx4_faults(reset=True) == 2 * rounds * 40
+    assert psc.psc_mx4_faults() == 0
