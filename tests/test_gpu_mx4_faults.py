@@ -8,6 +8,7 @@ import pytest
 
 from tests.test_gpu_mx4 import _matrix
 from tests.test_gpu_ops import _mask, _pack, psc  # noqa: F401
+from tests.test_gpu_sampled_decode import example  # noqa: F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -115,3 +116,26 @@ def test_resets_lose_no_fault_of_another_stream(psc):  # noqa: F811
     assert not errors
     assert sum(reports) + psc.psc_mx4_faults(reset=True) == 2 * rounds * 40
     assert psc.psc_mx4_faults() == 0
+
+
+@pytest.mark.parametrize("projection", ["int8", "norm8", "mx4"])
+def test_the_example_counts_its_own_faults(psc, example, projection):  # noqa: F811
+    """What gave up before a run is not the run's; what gives up during a run in 4 bits is."""
+    call = _call(psc, 3, 5000, 256, False)
+    call(0)
+    before = psc.psc_mx4_faults()
+    assert before > 0
+    example.run(3, 4, projection=projection)
+    assert psc.psc_mx4_faults() == before
+    if projection == "mx4":
+        step = example.Decoder.step
+
+        def step_beside_a_fault(self):
+            step(self)
+            call(0)
+
+        with pytest.MonkeyPatch.context() as m:
+            m.setattr(example.Decoder, "step", step_beside_a_fault)
+            with pytest.raises(RuntimeError, match="gave up"):
+                example.run(3, 2, use_graph=False, projection=projection)
+    psc.psc_mx4_faults(reset=True)
