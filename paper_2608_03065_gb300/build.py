@@ -19,7 +19,8 @@ CXX_SOURCES = ["grammar.cpp", "lexer.cpp", "lalr.cpp", "classifier.cpp", "bottom
 CU_SOURCES = ["psc_capi.cu", "process.cu", "sample.cu", "head.cu", "norm.cu", "mx4.cu",
               "mx4_head.cu"]
 GENCODE = "arch=compute_103a,code=sm_103a"
-MARSHAL = os.path.join(HERE, "_marshal.so")      # the binding's Python module (psc.py does without it where Python.h is missing)
+# the binding's Python module, by the interpreter that it is built for (psc.py does without it where Python.h is missing)
+MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def _nvcc() -> str:

@@ -69,7 +69,9 @@ _marshal = None          # csrc/marshal.cpp, where it is built: the small calls'
 
 def _load_marshal(lib, device=None):
     global _marshal
-    path = os.path.join(_HERE, "_marshal.so")
+    import sysconfig
+    # by this interpreter's tag: a module that another one's headers have gone into is not looked at
+    path = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
     if not os.path.exists(path):
         return
     try:
@@ -78,7 +80,7 @@ def _load_marshal(lib, device=None):
         spec = importlib.util.spec_from_file_location("_marshal", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-    except ImportError:                     # no torch, or another Python's module
+    except ImportError:                     # no torch, or a file that is no module
         return
     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
     module.setup((torch.bfloat16, torch.float32, torch.int8, torch.uint8, torch.int32),
