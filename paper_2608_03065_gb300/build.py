@@ -68,11 +68,6 @@ def _build_locked(force: bool, verbose: bool) -> str:
             jobs.append([nvcc, "-gencode", GENCODE, "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
                          "-I", INCLUDE, "-c", s, "-o", o])
 
-    python = sysconfig.get_paths()["include"]
-    marshal = os.path.join(CSRC, "marshal.cpp")
-    if os.path.exists(os.path.join(python, "Python.h")) and (force or _stale(MARSHAL, [marshal])):
-        jobs.append(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", python, marshal, "-o", MARSHAL])
-
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
@@ -81,12 +76,22 @@ def _build_locked(force: bool, verbose: bool) -> str:
             print(r.stdout, r.stderr)
         return r
 
-    with cf.ThreadPoolExecutor(max_workers=len(jobs) or 1) as ex:
-        list(ex.map(run, jobs))
+    def put(target, cmd):
+        """Makes a file that processes may have loaded, or may load meanwhile: beside it, then in its place."""
+        tmp = target + f".{os.getpid()}.tmp"
+        run(cmd + ["-o", tmp])
+        os.replace(tmp, target)
+
+    python = sysconfig.get_paths()["include"]
+    marshal = os.path.join(CSRC, "marshal.cpp")
+    with cf.ThreadPoolExecutor(max_workers=len(jobs) + 1) as ex:
+        waits = [ex.submit(run, cmd) for cmd in jobs]
+        if os.path.exists(os.path.join(python, "Python.h")) and (force or _stale(MARSHAL, [marshal])):
+            waits.append(ex.submit(put, MARSHAL, ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", python, marshal]))
+        for w in waits:
+            w.result()
     if force or jobs or _stale(LIB, objs):
-        tmp = LIB + f".{os.getpid()}.tmp"
-        run([nvcc, "-shared", "-gencode", GENCODE, "-o", tmp] + objs + ["-lpthread", "-ldl"])
-        os.replace(tmp, LIB)
+        put(LIB, [nvcc, "-shared", "-gencode", GENCODE] + objs + ["-lpthread", "-ldl"])
     return LIB
 
 
