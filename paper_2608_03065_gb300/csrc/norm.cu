@@ -28,6 +28,7 @@ struct Norm {
     int64_t q_stride;
     uint8_t* blocks;
     float* scale;
+    float most;                                 // sums of squares up to which their mean with eps stays in f32
 };
 
 struct RowStats {
@@ -157,11 +158,11 @@ template <bool MX4, int SHARES, typename Again>
 __device__ __forceinline__ Factor factor_of(const Norm& a, const RowStats& s, int& turn, Again again) {
     const float unit = s.top >= INF_BITS ? __uint_as_float(0x7fc00000u) : __fmul_rn(__uint_as_float(s.top), 1.f / 127.f);
     if (isnan(unit)) return {unit, unit};
-    if (s.squares >= 0x1p-76f && s.squares <= 0x1p126f) {
+    if (s.squares >= 0x1p-76f && s.squares <= a.most) {
         const float r = __fdiv_rn(1.f, __fsqrt_rn(__fdiv_rn(s.squares, (float)a.K) + a.eps));
         return {unit, MX4 ? r : unit * r};
     }
-    // the squares, or r, may leave f32 (squares of less than 2^-126 lose bits, but not of a sum from 2^-76
+    // the squares, their mean with eps, or r, may leave f32 (squares of less than 2^-126 lose bits, but not of a sum from 2^-76
     // on): once more, with the largest magnitude near 1.  It reads the sums again, of which a lane may have stored
     // another's (store_shifted), and no barrier need have come since in a block of one warp.
     __syncthreads();
@@ -442,7 +443,7 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
 }
 
 template <bool MX4>
-psc_status norm_entry(const char* me, const Norm& a, psc_dtype dtype, void* stream) {
+psc_status norm_entry(const char* me, Norm a, psc_dtype dtype, void* stream) {
     if (a.T < 0 || a.K <= 0 || !is_dtype(dtype) || a.x_stride < a.K || (a.residual && a.residual_stride < a.K) ||
         (a.sum && a.sum_stride < a.K) || !(a.eps >= 0.f && a.eps <= FLT_MAX) ||
         (a.T && (!a.x || !a.q || !a.scale || (MX4 && !a.blocks))))
@@ -457,6 +458,7 @@ psc_status norm_entry(const char* me, const Norm& a, psc_dtype dtype, void* stre
         (uintptr_t)a.scale % 4)
         return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
     if (a.T == 0) return PSC_OK;
+    a.most = a.eps <= 0x1p126f ? 0x1p126f : 0.f;
     if (dtype == PSC_BF16) return norm<__nv_bfloat16, MX4>(a, me, (cudaStream_t)stream);
     return norm<float, MX4>(a, me, (cudaStream_t)stream);
 }
@@ -471,7 +473,7 @@ psc_status psc_norm_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_
                                   void* stream) {
     return norm_entry<false>("psc_norm_quantize_rows",
                              Norm{d_x, row_stride, d_residual, residual_stride, d_sum, sum_stride, d_gain, eps, T, K,
-                                  (uint8_t*)d_q, q_stride, nullptr, d_scale},
+                                  (uint8_t*)d_q, q_stride, nullptr, d_scale, 0.f},
                              dtype, stream);
 }
 
@@ -481,7 +483,7 @@ psc_status psc_norm_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_s
                                  float* d_scale, void* stream) {
     return norm_entry<true>("psc_norm_quantize_mx4",
                             Norm{d_x, row_stride, d_residual, residual_stride, d_sum, sum_stride, d_gain, eps, T, K,
-                                 d_q, q_stride, d_blocks, d_scale},
+                                 d_q, q_stride, d_blocks, d_scale, 0.f},
                             dtype, stream);
 }
 

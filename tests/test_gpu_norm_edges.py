@@ -54,3 +54,23 @@ def test_sums_read_again_by_blocks_of_one_warp(psc, K, dtype, out):  # noqa: F81
     np.testing.assert_array_equal(_f64(sd), h)
     np.testing.assert_array_equal(q.cpu().numpy(), want)
     np.testing.assert_allclose(_f64(s), scale, rtol=_tolerance(K) + U, atol=0)
+
+
+@pytest.mark.parametrize("K", [1, 64, 1001, 4096])
+@pytest.mark.parametrize("T", [2, 3000])
+def test_eps_up_to_the_largest_number(psc, K, T):  # noqa: F811
+    """mean h^2 + eps beyond f32, for squares that are not: the root of it is a number, and so is its inverse."""
+    x = np.full((T, K), 9e18 / np.sqrt(K), dtype=np.float32)          # squares of 8.1e37 in all, below 2^126
+    x[1::2] *= np.float32(1e-3)
+    xd, n = _dev(x), psc.psc_mx4_row_bytes(K)
+    q, s = torch.empty(T, K, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    c, b = torch.empty(T, n, dtype=torch.uint8, device="cuda"), torch.empty(psc.psc_mx4_block_bytes(T, K), dtype=torch.uint8,
+                                                                            device="cuda")
+    for eps in (1e30, 2.0 ** 125, 2.0 ** 126, 2.0 ** 127, float(np.finfo(np.float32).max)):
+        h, v, r = ref.norm(x, None, None, eps, False)
+        psc.psc_norm_quantize_rows(xd, q, s, eps=eps)
+        want, scale = _int8(v, r)
+        np.testing.assert_array_equal(q.cpu().numpy(), want)
+        np.testing.assert_allclose(_f64(s), scale, rtol=_tolerance(K) + U, atol=0)
+        psc.psc_norm_quantize_mx4(xd, c, b, s, eps=eps)
+        np.testing.assert_allclose(_f64(s), r, rtol=_tolerance(K), atol=0)
