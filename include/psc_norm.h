@@ -24,8 +24,9 @@ extern "C" {
  * of the whole row, so it is in the scale alone, and the codes depend on h and gain only.  A
  * row of zeros (or one whose s underflows to zero) gets scale 0 and q 0; a row in which some
  * h or v is an infinity or a NaN gets scale NaN and q 0.  mean_k h^2 neither overflows nor
- * underflows for finite h.  A row's results do not depend on the batch that it is in (where
- * rows do not all start at multiples of 32 bytes, its scale's last bits depend on where it starts).
+ * underflows for finite h.  A row's results do not depend on the batch that it is in, nor on how the
+ * other tensors lie (where rows of x do not all start at multiples of 32 bytes, a scale's last bits
+ * depend on where its row starts).
  *   d_x, d_residual : [T] rows of dtype, K used (d_residual NULL: h = x)
  *   d_sum    : [T] rows of dtype that receive h, or NULL; may be d_x or d_residual (then with the
  *              same stride), otherwise overlaps no input

@@ -405,8 +405,10 @@ constexpr int RING_BYTES = 200 * 1024;            // of an SM's shared memory, f
 
 template <typename T, bool MX4, Chunks C>
 psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
-    // a thread's share goes by the width alone, and so do the sums' orders
-    const int chunks = (a.K + (C == SHIFTED ? 14 : 7)) / 8, quarter = (chunks + 3) / 4;
+    // a thread's share goes by the width and by where x's rows start (a chunk more where those are shifted), and so do
+    // the sums' orders; not by how the other tensors lie
+    const bool shifted = C == SHIFTED && !wide_rows<T>(a.x, a.x_stride, a.K);
+    const int chunks = (a.K + (shifted ? 14 : 7)) / 8, quarter = (chunks + 3) / 4;
     const int threads = quarter < 1024 ? (quarter + 31) / 32 * 32 : 1024;
     // a chunk a thread while that fits the GPU at once (1024 threads an SM)
     if (threads <= 256 && (int64_t)a.T * 4 * threads <= 1024ll * current_sms())

@@ -74,3 +74,36 @@ def test_eps_up_to_the_largest_number(psc, K, T):  # noqa: F811
         np.testing.assert_allclose(_f64(s), scale, rtol=_tolerance(K) + U, atol=0)
         psc.psc_norm_quantize_mx4(xd, c, b, s, eps=eps)
         np.testing.assert_allclose(_f64(s), r, rtol=_tolerance(K), atol=0)
+
+
+@pytest.mark.parametrize("T,K", [(5, 1024), (3000, 1024), (7, 2048), (1500, 2048), (400, 8192)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_do_not_depend_on_how_the_other_tensors_lie(psc, T, K, dtype):  # noqa: F811
+    """Rows of x at aligned addresses: gain, codes, residual and sum may lie anywhere, and every result has the same bits."""
+    rng = np.random.default_rng([T, K])
+    x, res = _dev(_data(rng, T, K, dtype)).to(DT[dtype]), _dev(_data(rng, T, K, dtype)).to(DT[dtype])
+    g = _dev(rng.uniform(0.5, 1.5, K).astype(np.float32))
+
+    def moved(t, by):
+        """The same values, `by` elements off in rows of 8 + by elements more."""
+        if t.dim() == 1:
+            out = torch.empty(K + by, dtype=t.dtype, device="cuda")[by:]
+        else:
+            out = torch.empty(T, K + 8 + by, dtype=t.dtype, device="cuda")[:, by:by + K]
+        out.copy_(t)
+        return out
+
+    def run(gain=g, residual=res, pad=0, sum_by=0):
+        big = torch.zeros(T, K + pad, dtype=torch.int8, device="cuda")
+        h = moved(res, sum_by) if sum_by else torch.empty_like(res)
+        s = torch.empty(T, device="cuda")
+        psc.psc_norm_quantize_rows(x, big[:, :K], s, gain=gain, residual=residual, sum_out=h)
+        q4 = torch.zeros(T, psc.psc_mx4_row_bytes(K), dtype=torch.uint8, device="cuda")
+        b, s4 = torch.zeros(psc.psc_mx4_block_bytes(T, K), dtype=torch.uint8, device="cuda"), torch.empty(T, device="cuda")
+        psc.psc_norm_quantize_mx4(x, q4, b, s4, gain=gain, residual=residual)
+        return big[:, :K], s, h, q4, b, s4
+
+    want = run()
+    for other in (run(gain=moved(g, 1)), run(pad=4), run(residual=moved(res, 3)), run(sum_by=1), run(pad=5, sum_by=2)):
+        for u, v in zip(want, other):
+            assert torch.equal(u, v)
