@@ -55,7 +55,9 @@ psc_status psc_dequantize_mx4(const uint8_t* d_q, int64_t q_stride, const uint8_
  *     logits[t][v] = (sum_k x_t[k] w_v[k]) * scale[t] * w_scale[v]
  * over the values of both matrices, where the mask allows v for row t, -inf elsewhere; rows of
  * w that no token allows need not be read.  Products are exact; sums over K are in f32, in an
- * order that depends on the sizes and the mask.
+ * order that depends on the sizes, and come before the factors: sums of |x_t[k] w_v[k]| from 2^-100 to
+ * 2^127 keep f32's accuracy; from 2^128 on a logit may be infinite or NaN where its formula is not, and
+ * smaller ones lose bits.
  *   d_q, d_q_blocks : the tokens, [T] rows    d_w, d_w_blocks : the weights, [V] rows
  *   d_scale         : float [T], d_w_scale : float [V], each NULL for ones
  *   d_bitmask       : uint32 [T][ceil(V/32)], or NULL (every token allowed)

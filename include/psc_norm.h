@@ -42,7 +42,10 @@ psc_status psc_norm_quantize_rows(const void* d_x, psc_dtype dtype, int64_t row_
 
 /* psc_norm_quantize_rows with an output in the format of psc_mx4.h: h, v and r as there,
  *     the codes and blocks of v as psc_quantize_mx4 makes them      scale = r
- * (scale NaN for a row in which some h or v is not finite; 0 for a row of zeros with eps 0).
+ * (scale NaN for a row in which some h or v is not finite; 0 for a row of zeros with eps 0;
+ * infinity where r is beyond f32, for which eps has to be 0 and the root mean square 2^-128 or less).
+ * As r is in the scale alone, the codes and blocks hold v as it is, and its size goes through the
+ * sums of psc_head_logits_mx4: see there.
  * PSC_ERR_LIMIT: K over 2^30. */
 psc_status psc_norm_quantize_mx4(const void* d_x, psc_dtype dtype, int64_t row_stride, const void* d_residual,
                                  int64_t residual_stride, void* d_sum, int64_t sum_stride, const float* d_gain,

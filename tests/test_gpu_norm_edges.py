@@ -107,3 +107,47 @@ def test_scales_do_not_depend_on_how_the_other_tensors_lie(psc, T, K, dtype):  #
     for other in (run(gain=moved(g, 1)), run(pad=4), run(residual=moved(res, 3)), run(sum_by=1), run(pad=5, sum_by=2)):
         for u, v in zip(want, other):
             assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("T", [3, 140])
+@pytest.mark.parametrize("power", [-106, -60, 0, 60, 112])
+def test_norm_and_projection_in_4_bits_over_the_range_of_rows(psc, T, power):  # noqa: F811
+    """The codes hold h * gain as it is, so that its size goes through the projection's sums: those of magnitudes lie
+    between 2^-100 and 2^127 here, as the header asks for.  Tolerances as in test_gpu_mx4, and the factor's."""
+    rng = np.random.default_rng([T, power + 200])
+    V, K = 500, 512
+    x = np.ldexp(rng.uniform(0.5, 1, (T, K)) * rng.choice([-1, 1], (T, K)), power).astype(np.float32)
+    w = (rng.uniform(0.5, 4, (V, K)) * rng.choice([-1, 1], (V, K))).astype(np.float32)
+    h, v, r = ref.norm(x, None, None, 0.0, False)
+    n = psc.psc_mx4_row_bytes(K)
+    q, b = torch.empty(T, n, dtype=torch.uint8, device="cuda"), torch.empty(psc.psc_mx4_block_bytes(T, K), dtype=torch.uint8,
+                                                                            device="cuda")
+    wq, wb = torch.empty(V, n, dtype=torch.uint8, device="cuda"), torch.empty(psc.psc_mx4_block_bytes(V, K), dtype=torch.uint8,
+                                                                              device="cuda")
+    s, out = torch.empty(T, device="cuda"), torch.empty(T, V, device="cuda")
+    psc.psc_quantize_mx4(_dev(w), wq, wb)
+    psc.psc_norm_quantize_mx4(_dev(x), q, b, s, eps=0.0)
+    psc.psc_head_logits_mx4(q, b, wq, wb, out, K, scale=s)
+    y, m = ref.decode(*ref.quantize(v)), ref.decode(*ref.quantize(w))
+    sums = np.abs(y) @ np.abs(m).T
+    assert 2.0 ** -100 < sums.min() and sums.max() < 2.0 ** 127
+    exact = y @ m.T * r[:, None]
+    tol = 4 * U * (K / 64 + 2) * sums * r[:, None] + (_tolerance(K) + 2 * U) * np.abs(exact)
+    assert (np.abs(_f64(out) - exact) <= tol * 1.0000001).all()
+
+
+def test_the_factor_of_tiny_rows(psc):  # noqa: F811
+    """Beyond f32 only with eps 0 and a root mean square of 2^-128 or less; any eps that is a number of f32 keeps it finite."""
+    x = np.zeros((4, 64), dtype=np.float32)
+    x[0], x[1], x[2] = 1e-42, 2.0 ** -127, 2.0 ** -129
+    n = psc.psc_mx4_row_bytes(64)
+    q, b = torch.empty(4, n, dtype=torch.uint8, device="cuda"), torch.empty(512, dtype=torch.uint8, device="cuda")
+    for eps in (0.0, 2.0 ** -149, 1e-12):
+        psc.psc_norm_quantize_mx4(_dev(x), q, b, s := torch.empty(4, device="cuda"), eps=eps)
+        with np.errstate(divide="ignore"):
+            r = ref.norm(x, None, None, eps, False)[2]
+        r[r > 3.5e38] = np.inf
+        if eps == 0:
+            r[3] = 0
+            assert np.isinf(r).tolist() == [True, False, True, False]
+        np.testing.assert_allclose(_f64(s), r, rtol=_tolerance(64), atol=0)
