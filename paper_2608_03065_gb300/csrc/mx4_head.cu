@@ -255,6 +255,22 @@ __device__ __forceinline__ void forbid_tile(T* out, int64_t stride, int tokens, 
     }
 }
 
+// What drain's comment says, by all warps of the block.  (Not inline, so that the kernel's last instructions do not lie
+// behind it: 79 tokens over 71,701 x 96, 15.1 us, take 0.1 more with it inline.)
+__device__ __noinline__ void settle_few(uint32_t full0, int slots, uint32_t drained, const int* loaded) {
+    const int warp = threadIdx.x >> 5;
+    const bool issuer = elect_one();                  // the lane that issued (it is the same every time)
+    if (warp == 1 && issuer) {
+        mma_commit<false>(drained);
+        drain_products(drained);
+    } else if (warp <= 4 && issuer) {
+        const int most = max(max(loaded[0], loaded[1]), max(loaded[2], loaded[3]));
+        for (int i = loaded[max(0, warp - 1)]; i < most; i++) mbar_arrive(full0 + 8 * (i % slots));
+        drain(full0, most, slots);
+    }
+    __syncwarp();
+}
+
 template <typename T, bool MASKED>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
@@ -419,21 +435,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (*failed) {                                    // drain's comment; nobody writes the flag any more
-        const bool issuer = elect_one();              // the lane that issued (it is the same every time)
-        if (warp == 1 && issuer) {
-            mma_commit<false>(drained);
-            drain_products(drained);
-        } else if (warp <= 4 && issuer) {
-            const int most = max(max(s_loaded[0], s_loaded[1]), max(s_loaded[2], s_loaded[3]));
-            for (int i = s_loaded[max(0, warp - 1)]; i < most; i++) mbar_arrive(full(i % p.stages));
-            drain(full(0), most, p.stages);
-        }
-        __syncwarp();
+    if (*failed) {                                    // nobody writes the flag any more
+        settle_few(bars, p.stages, drained, s_loaded);
+        if (threadIdx.x == 0) atomicAdd(&g_faults, 1);
         __syncthreads();
     }
     if (warp == 1) tmem_free<false>(tmem);
-    if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
 
 template <typename T>
@@ -532,6 +539,34 @@ __device__ __forceinline__ uint32_t both_bytes(uint32_t a, uint32_t b, int i) {
     uint32_t r;
     asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(0xCC88u + 0x1111u * i));
     return r;
+}
+
+// What drain's comment says, by all warps of both blocks (not inline, as settle_few).
+__device__ __noinline__ void settle_many(uint32_t a_full0, int a_slots, uint32_t b_full0, int b_slots, uint32_t e_full0,
+                                         uint32_t drained, const int* loaded) {
+    const int warp = threadIdx.x >> 5, side = (int)cluster_rank();
+    const bool issuer = elect_one();                  // the lane that issued (it is the same every time)
+    if (side == 0 && (warp == 1 || warp == 5) && issuer) mma_commit<true>(drained);
+    if (warp == 1 && issuer) drain_products(drained);
+    // both blocks' copies are counted at the first's barriers: there a stage takes an arrival with the bytes of
+    // both, of each of its loaders
+    auto finish = [&](int loader, uint32_t full0, int slots, int bytes, int most) {
+        const int own = loaded[loader], theirs = read_other(&loaded[loader], 1);
+        for (int i = own; i < most; i++) {
+            if (i < theirs) mbar_arrive_tx(full0 + 8 * (i % slots), bytes);
+            else mbar_arrive(full0 + 8 * (i % slots));
+        }
+        for (int i = theirs; i < own; i++) forgo_bytes(full0 + 8 * (i % slots), bytes);
+        drain(full0, most, slots);
+    };
+    auto begun = [&](int loader) { return max(loaded[loader], read_other(&loaded[loader], 1)); };
+    if (side == 0 && issuer) {
+        if (warp == 0) finish(0, b_full0, b_slots, B_CODES, begun(0));
+        if (warp == 2) finish(1, e_full0, SF_SLOTS, B_EXPS, begun(1));
+        if (warp == 3) finish(2, a_full0, a_slots, A_CODES, max(begun(2), begun(3)));
+        if (warp == 4) finish(3, a_full0, a_slots, 2 * SF, max(begun(2), begun(3)));
+    }
+    __syncwarp();
 }
 
 template <typename T, bool MASKED>
@@ -834,33 +869,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     __syncthreads();
     if (threadIdx.x == 0 && *failed) set_other(&s_other_failed, side ^ 1);
     cluster_sync();                                   // nothing of this block is used by the other any more, unless
-    if (*failed || *const_cast<volatile int*>(&s_other_failed)) {     // drain's comment; both blocks come here or neither
-        const bool issuer = elect_one();              // the lane that issued (it is the same every time)
-        if (side == 0 && (warp == 1 || warp == 5) && issuer) mma_commit<true>(drained);
-        if (warp == 1 && issuer) drain_products(drained);
-        // both blocks' copies are counted at the first's barriers: there a stage takes an arrival with the bytes of
-        // both, of each of its loaders
-        auto finish = [&](int loader, uint32_t full0, int slots, int bytes, int most) {
-            const int own = s_loaded[loader], theirs = read_other(&s_loaded[loader], 1);
-            for (int i = own; i < most; i++) {
-                if (i < theirs) mbar_arrive_tx(full0 + 8 * (i % slots), bytes);
-                else mbar_arrive(full0 + 8 * (i % slots));
-            }
-            for (int i = theirs; i < own; i++) forgo_bytes(full0 + 8 * (i % slots), bytes);
-            drain(full0, most, slots);
-        };
-        auto begun = [&](int loader) { return max(s_loaded[loader], read_other(&s_loaded[loader], 1)); };
-        if (side == 0 && issuer) {
-            if (warp == 0) finish(0, b_full(0), b_slots, B_CODES, begun(0));
-            if (warp == 2) finish(1, e_full(0), SF_SLOTS, B_EXPS, begun(1));
-            if (warp == 3) finish(2, a_full(0), a_slots, A_CODES, max(begun(2), begun(3)));
-            if (warp == 4) finish(3, a_full(0), a_slots, 2 * SF, max(begun(2), begun(3)));
-        }
-        __syncwarp();
+    if (*failed || *const_cast<volatile int*>(&s_other_failed)) {     // both blocks come here or neither
+        settle_many(a_full(0), a_slots, b_full(0), b_slots, e_full(0), drained, s_loaded);
+        if (threadIdx.x == 0 && *failed) atomicAdd(&g_faults, 1);
         cluster_sync();
     }
     if (warp == 1) tmem_free<true>(tmem);
-    if (threadIdx.x == 0 && s_failed) atomicAdd(&g_faults, 1);
 }
 
 template <typename T>
