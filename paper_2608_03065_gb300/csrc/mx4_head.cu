@@ -154,9 +154,10 @@ __device__ __forceinline__ void drain_products(uint32_t bar) {
 // k_mx4_few: a persistent block per SM over tiles of 128 vocabulary rows (the tensor core's M) by all
 // tokens (its N): with few tokens the weights' bytes are all that counts, and tensor cores that give
 // most of their columns away keep up with them.
-// Bound by memory and its beginning and end: 1 token over 128,256 x 2048 takes 27.2 us (140 MB), of which
-// about six are the launch, the first loads' latency and the last tiles; 16 tokens over 151,936 x 1024
-// under masks that leave a few dozen tokens each 15.4 us, mostly that latency and the -inf of the other tiles.
+// Bound by memory and its beginning and end: 1 token over 128,256 x 2048 takes 23.1 us (140 MB, 6.1 TB/s), 64 tokens
+// 24.7; 16 tokens over 151,936 x 1024 under masks that leave a few dozen tokens each 12.1 us, mostly latency (the masks,
+// then the first stages) and the -inf of the other tiles.  Device times of calls that follow each other; behind the
+// norm, which a step has in front, 27.3 and 15.2 with it.
 //   warps 0, 2-4  TMA: the weights' codes (16 KB a stage), the tokens', both sides' exponents
 //   warp 1        the exponents' way to TMEM, the products
 //   warps 8-15    a lane per vocabulary row, two warps for 32 of them: scales, mask, logits
@@ -165,7 +166,7 @@ constexpr int VT = 128;                       // vocabulary rows of a tile
 constexpr int W_CODES = VT * KS / 2;
 constexpr int MAX_STAGES = 11;
 constexpr int GROUPS = FEW / 32 / 2;          // a warp's groups of 32 tokens
-constexpr int WARM = 24;                      // stages whose weights are prefetched (1 token over 128,256 x 2048: 28.3 us without, 26.5)
+constexpr int WARM = 24;                      // stages whose weights are prefetched (1 token over 128,256 x 2048, norm in front: 28.3 us without, 26.5)
 constexpr int MAX_TILES = 8192;               // of a block, for which masks are looked at beforehand
 
 struct Few {
@@ -469,10 +470,12 @@ psc_status head_few(const Head& h, T* logits, cudaStream_t cs) {
 // exponents in both).  Where a tile's tokens fit shared memory (K up to 2048) they stay there, and
 // only the weights are loaded, from memory once and from the L2 for the other tiles of tokens: an SM
 // takes in 64 bytes a cycle, and a stage's 384 cycles of products need 14 KB this way, 31 KB where
-// the tokens come along.  256 tokens over 128,256 x 4096: 61.8 us, at the memory's latency (seven slots, 86 KB of
-// weights an SM); 1024 over 262,144 x 2048, mixed masks: 204 us, 5.4 PFLOP/s, beside 537 MB of logits at
-// the GPU's power limit.  A lane of the epilogue has a token, and 32 neighbouring logits of it with one
-// word of the mask; they go out by way of shared memory, 64 bytes of a token at a time.
+// the tokens come along.  256 tokens over 128,256 x 4096: 58 us, at the memory's latency (seven slots, 86 KB of
+// weights an SM); 1024 over it 192 us, 5.6 PFLOP/s, 1024 over 262,144 x 2048 under mixed masks 183, 6.0 PFLOP/s beside
+// 537 MB of logits, at 2.07 GHz: calls that follow each other for milliseconds.  For seconds the GPU's power cap
+// takes the clock to 1.75 GHz, and the last of these to 218 us.  (With the norm in front 63 and 206 us.)
+// A lane of the epilogue has a token, and 32 neighbouring logits of it with one word of the mask; they go out by
+// way of shared memory, 64 bytes of a token at a time.
 //   warps 0, 2-4  TMA: the weights' codes and exponents, the tokens' codes and exponents
 //   warp 5        the exponents' way to TMEM
 //   warp 1        the products
@@ -585,7 +588,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     const int side = (int)cluster_rank();
     // slots start at multiples of 1024 bytes: the tokens' codes and exponents, the weights' codes, their exponents
     // Tokens that do not stay come from the L2, weights from memory, which takes longer (256 tokens over 128,256 x
-    // 4096: 64.4 us with 4 slots for the tokens and 10 for the weights, 62.8 with 6 and 7, 64.5 with 7 and 6).
+    // 4096, norm in front: 64.4 us with 4 slots for the tokens and 10 for the weights, 62.8 with 6 and 7, 64.5 with 7 and 6).
     const int n_k = (h.K + KS - 1) / KS;
     const bool stay = n_k <= MAX_A;
     const int a_slots = stay ? n_k : 6, b_slots = min(MAX_B, (SLOTS_BYTES - a_slots * A_BYTES) / B_CODES);

@@ -228,7 +228,8 @@ __device__ __forceinline__ void unpack_h(const uint32_t (&x)[8], const uint32_t 
 // a block's loads all come at its beginning, and half of its time nothing is under way: 16,384 rows of
 // 4,096 bf16 columns with residual 114 us, this way 75.  FULL_ROWS: every thread has its four chunks (rows of whole
 // multiples of 1,024 columns), which leaves out checks where instructions bound it: without residual
-// 62.0 us with this and the residual known at run time only, 48.9 this way; into 4 bits with residual 111 and 105.
+// 62.0 us with this and the residual known at run time only, 48.9 this way; into 4 bits with residual, and back, 111 and
+// 105 (there alone 71, with 93 % of its bytes at a copy's rate; without residual 50, half of it instructions).
 template <typename T, bool MX4, bool RESIDUAL, bool FULL_ROWS>
 __global__ void __launch_bounds__(768, 1) k_norm_many(Norm a, int stages) {
     constexpr int NV = 4, N = sizeof(T) * 2, PIECES = N / 4;           // words, 16-byte pieces of a chunk
@@ -417,7 +418,7 @@ psc_status norm(const Norm& a, const char* me, cudaStream_t cs) {
         // as many blocks as registers leave room for, as many rows ahead as shared memory does; into 8 bits with a
         // residual memory bounds many rows, and fewer blocks with more rows ahead are faster (768 and 512 threads an SM:
         // 16,384 rows of 4,096 bf16 columns 77.8 and 75.2 us, 65,536 of 2,048 157 and 143; without the residual
-        // 48.9 and 67.0, into 4 bits with it 104.7 and 113.6;
+        // 48.9 and 67.0, into 4 bits and back with it 104.7 and 113.6;
         // few rows a block: 8,192 of 2,048 with residual 22.2 and 23.1)
         const int stage = threads * 4 * 8 * (int)sizeof(T) * (a.residual ? 2 : 1);
         const bool fewer = a.residual && !MX4 && a.T >= 8 * (768 / threads) * current_sms();
