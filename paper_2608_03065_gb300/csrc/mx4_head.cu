@@ -16,7 +16,7 @@ constexpr int MAX_V = 1 << 30, MAX_T = 1 << 24;     // and numbers of rows, roun
 // Blocks in which a bounded wait gave up; what a reset takes off it is what it has reported, so that none is lost that
 // another stream adds meanwhile.
 __device__ int g_faults;
-std::mutex g_faults_read;                   // a report and its reset at a time
+std::mutex g_faults_read;                   // a report with its reset at a time
 
 __global__ void k_take_faults(int reported) {
     dep_wait();
@@ -947,7 +947,8 @@ psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream) {
     const char* me = "psc_mx4_faults";
     if (!h_faults) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
     cudaStream_t cs = (cudaStream_t)stream;
-    std::lock_guard<std::mutex> alone(g_faults_read);
+    std::unique_lock<std::mutex> alone(g_faults_read, std::defer_lock);
+    if (reset) alone.lock();
     psc_status s = ops_check(cudaMemcpyFromSymbolAsync(h_faults, g_faults, 4, 0, cudaMemcpyDeviceToHost, cs), me);
     if (s == PSC_OK) s = ops_check(cudaStreamSynchronize(cs), me);
     if (s == PSC_OK && reset && *h_faults) {
