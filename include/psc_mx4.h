@@ -75,10 +75,10 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
  * off the count what it reports: each fault is in one of several callers' reports, whatever runs beside them. */
 psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream);
 
-/* Self-test of that fault path: psc_head_logits_mx4 with waits that give up after `limit` polls (0 to
- * 2^22; the projection itself waits for 2^22), 0: without any.  Blocks in which one does leave logits
- * unwritten, wait for what they have under way, end, and are counted; nothing faults, and the device
- * stays usable. */
+/* Self-test of that fault path: psc_head_logits_mx4 into f32 logits, with waits that give up after `limit`
+ * looks (0 to 2^22; some tens of nanoseconds each, where the projection itself waits for seconds).  Blocks
+ * in which one does leave logits unwritten, wait for what they have under way, end, and are counted;
+ * nothing faults, and the device stays usable. */
 psc_status psc_mx4_check_wait(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
                               int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                               const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,

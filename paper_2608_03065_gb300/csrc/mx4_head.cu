@@ -38,7 +38,7 @@ struct Head {
     const uint32_t* bitmask;
     int W;                              // mask words of a row
     int64_t row_stride;
-    int polls;                          // after which a wait gives up
+    int polls;                          // CHECK: looks after which a wait gives up
 };
 
 // ------------------------------------------------------------ the tensor-core path
@@ -272,7 +272,7 @@ __device__ __noinline__ void settle_few(uint32_t full0, int slots, uint32_t drai
     __syncwarp();
 }
 
-template <typename T, bool MASKED>
+template <typename T, bool MASKED, bool CHECK>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constant__ CUtensorMap w_map,
                                                             const __grid_constant__ CUtensorMap x_map,
                                                             const __grid_constant__ CUtensorMap w_blocks_map,
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
             const int vt = vt0 + i * vt_step;
             for (int k = 0; k < n_k; k++, c++, at.next(p.stages)) {
                 const uint32_t to = base + at.s * p.stage_bytes + part, bar = full(at.s);
-                if (!(ok = warp_wait(empty(at.s), at.parity ^ 1, failed, h.polls))) break;
+                if (!(ok = warp_wait<CHECK>(empty(at.s), at.parity ^ 1, failed, h.polls))) break;
                 if (issuer) {
                     mbar_arrive_tx(bar, bytes);
                     tma_2d(to, map, k * step, vt * y_step, bar);
@@ -374,12 +374,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
         bool ok = true;
         for (int i = 0; i < mine && ok; i++) {
             if (!is_active(i)) continue;
-            if (!(ok = warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls))) break;
+            if (!(ok = warp_wait<CHECK>(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls))) break;
             const uint32_t d = tmem + acc.s * p.acc;
             for (int k = 0; k < n_k; k++, at.next(p.stages)) {
                 const uint32_t a = lo + at.s * step, b = a + W_CODES / 16, e = b + x_codes / 16;
                 const uint32_t sf = tmem + 2 * p.acc + at.s * 16;
-                if (!(ok = warp_wait(full(at.s), at.parity, failed, h.polls))) break;
+                if (!(ok = warp_wait<CHECK>(full(at.s), at.parity, failed, h.polls))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
                     copy_stage<false, 1>(e, e + 64, sf);
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
                     !MASKED ? FULL : wi < h.W ? h.bitmask[(size_t)t * h.W + wi] : 0u};
             }
             __syncwarp();
-            if (!warp_wait(acc_full(acc.s), acc.parity, failed, h.polls)) break;
+            if (!warp_wait<CHECK>(acc_full(acc.s), acc.parity, failed, h.polls)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
             for (int i = 0; i < GROUPS; i++) {
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_few(const __grid_constan
     if (warp == 1) tmem_free<false>(tmem);
 }
 
-template <typename T>
+template <typename T, bool CHECK>
 psc_status head_few(const Head& h, T* logits, cudaStream_t cs) {
     const Few p = few_of(h.T, h.V);
     CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
@@ -458,7 +458,7 @@ psc_status head_few(const Head& h, T* logits, cudaStream_t cs) {
         return ops_fail(PSC_ERR_CUDA, ME, "cuTensorMapEncodeTiled failed");
     const int64_t stride = h.row_stride * (int64_t)sizeof(T);
     const bool even = is_aligned(logits, stride, 4), wide = is_aligned(logits, stride, 16);
-    return ops_launch(h.bitmask ? k_mx4_few<T, true> : k_mx4_few<T, false>, dim3(std::min(p.n_vt, current_sms())),
+    return ops_launch(h.bitmask ? k_mx4_few<T, true, CHECK> : k_mx4_few<T, false, CHECK>, dim3(std::min(p.n_vt, current_sms())),
                       MMA_THREADS, p.smem, 1, cs, "k_mx4_few", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, p,
                       even, wide);
 }
@@ -572,7 +572,7 @@ __device__ __noinline__ void settle_many(uint32_t a_full0, int a_slots, uint32_t
     __syncwarp();
 }
 
-template <typename T, bool MASKED>
+template <typename T, bool MASKED, bool CHECK>
 __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_constant__ CUtensorMap w_map,
                                                              const __grid_constant__ CUtensorMap x_map,
                                                              const __grid_constant__ CUtensorMap w_blocks_map,
@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             int x = 0;
             for (int k = 0; k < n_k; k++, c++, x += step, at.next(slots)) {
                 const uint32_t to = to0 + at.s * slot_bytes, own = full0 + 8 * at.s, bar = there0 + 8 * at.s;
-                if (!warp_wait(empty0 + 8 * at.s, at.parity ^ 1, failed, h.polls)) return false;
+                if (!warp_wait<CHECK>(empty0 + 8 * at.s, at.parity ^ 1, failed, h.polls)) return false;
                 if (issuer) {
                     if (side == 0) mbar_arrive_tx(own, 2 * bytes);
                     load_tile(to, map, x, y, bar);
@@ -711,8 +711,8 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
             for (int k = 0; k < n_k; k++, at_a.next(a_slots), at.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), e = e_lo + at.s * (B_EXPS / 16);
                 const uint32_t sf = tmem + 2 * NV + at.s * SF_COLS;
-                if (!warp_wait2(e_full(at.s), at.parity, sf_empty(at.s), at.parity ^ 1, failed, h.polls) ||
-                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed, h.polls)))
+                if (!warp_wait2<CHECK>(e_full(at.s), at.parity, sf_empty(at.s), at.parity ^ 1, failed, h.polls) ||
+                    (fresh && !warp_wait<CHECK>(a_full(at_a.s), at_a.parity, failed, h.polls)))
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
@@ -731,12 +731,12 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
         each([&](int, int vt, bool fresh, bool last) {
             const uint32_t idesc = instruction(MT, rows_of(vt)), d = tmem + acc.s * NV, shift = vt * NV % 128 / 32;
             Place at_a = unit;
-            if (!warp_wait(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls)) return false;
+            if (!warp_wait<CHECK>(acc_empty(acc.s), acc.parity ^ 1, failed, h.polls)) return false;
             for (int k = 0; k < n_k; k++, at_a.next(a_slots), at_b.next(b_slots), at_e.next(SF_SLOTS)) {
                 const uint32_t a = a_lo + at_a.s * (A_BYTES / 16), b = b_lo + at_b.s * (B_CODES / 16);
                 const uint32_t sf = tmem + 2 * NV + at_e.s * SF_COLS;
-                if (!warp_wait2(sf_full(at_e.s), at_e.parity, b_full(at_b.s), at_b.parity, failed, h.polls) ||
-                    (fresh && !warp_wait(a_full(at_a.s), at_a.parity, failed, h.polls)))
+                if (!warp_wait2<CHECK>(sf_full(at_e.s), at_e.parity, b_full(at_b.s), at_b.parity, failed, h.polls) ||
+                    (fresh && !warp_wait<CHECK>(a_full(at_a.s), at_a.parity, failed, h.polls)))
                     return false;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 if (issuer) {
@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
                     if (v0 + i * 32 + lane < h.V) scales[i * 32 + lane] = h.w_scale[v0 + i * 32 + lane];
                 __syncwarp();
             }
-            if (!warp_wait(acc_full(acc.s), acc.parity, failed, h.polls)) return false;
+            if (!warp_wait<CHECK>(acc_full(acc.s), acc.parity, failed, h.polls)) return false;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             T* rows = logits + (size_t)(t0 + (lane >> 2)) * h.row_stride + v0 + (lane & 3) * (COLS / 4);
 #pragma unroll
@@ -880,7 +880,7 @@ __global__ void __launch_bounds__(MMA_THREADS, 1) k_mx4_many(const __grid_consta
     if (warp == 1) tmem_free<true>(tmem);
 }
 
-template <typename T>
+template <typename T, bool CHECK>
 psc_status head_many(const Head& h, T* logits, cudaStream_t cs) {
     CUtensorMap w_map, x_map, w_blocks_map, x_blocks_map;
     const uint64_t row = (h.K + 31) / 32 * 16, n_tiles = (h.K + 127) / 128;
@@ -894,15 +894,17 @@ psc_status head_many(const Head& h, T* logits, cudaStream_t cs) {
     const int n_mt = (h.T + MT - 1) / MT, n_vt = (h.V + NV - 1) / NV;
     const bool wide = is_aligned(logits, h.row_stride * (int64_t)sizeof(T), 16);
     const int pairs = (int)std::min<int64_t>((int64_t)n_mt * n_vt, std::max(1, current_sms() / 2));
-    return ops_launch(h.bitmask ? k_mx4_many<T, true> : k_mx4_many<T, false>, dim3(2 * pairs), MMA_THREADS, MANY_SMEM, 2,
+    return ops_launch(h.bitmask ? k_mx4_many<T, true, CHECK> : k_mx4_many<T, false, CHECK>, dim3(2 * pairs), MMA_THREADS, MANY_SMEM, 2,
                       cs, "k_mx4_many", w_map, x_map, w_blocks_map, x_blocks_map, h, logits, n_mt, n_vt, wide);
 }
 
-template <typename T>
+template <typename T, bool CHECK>
 psc_status head(const Head& h, T* logits, cudaStream_t cs) {
-    return h.T <= FEW ? head_few(h, logits, cs) : head_many(h, logits, cs);
+    return h.T <= FEW ? head_few<T, CHECK>(h, logits, cs) : head_many<T, CHECK>(h, logits, cs);
 }
 
+// CHECK: the kernels that psc_mx4_check_wait runs, the same but for when their waits give up; f32 only.
+template <bool CHECK>
 psc_status head_entry(const char* me, Head h, void* logits, psc_dtype dtype, void* stream) {
     if (h.T < 0 || h.V <= 0 || h.K <= 0 || h.row_stride < h.V || !is_dtype(dtype) || !h.w || !h.w_blocks ||
         (h.T && (!h.q || !h.q_blocks || !logits)))
@@ -915,8 +917,10 @@ psc_status head_entry(const char* me, Head h, void* logits, psc_dtype dtype, voi
         return ops_fail(PSC_ERR_ARG, me, "an address that is no multiple of its elements' size");
     if (h.T == 0) return PSC_OK;
     h.W = (h.V + 31) / 32;
-    if (dtype == PSC_BF16) return head(h, (__nv_bfloat16*)logits, (cudaStream_t)stream);
-    return head(h, (float*)logits, (cudaStream_t)stream);
+    if constexpr (!CHECK) {
+        if (dtype == PSC_BF16) return head<__nv_bfloat16, CHECK>(h, (__nv_bfloat16*)logits, (cudaStream_t)stream);
+    }
+    return head<float, CHECK>(h, (float*)logits, (cudaStream_t)stream);
 }
 
 }  // namespace
@@ -927,9 +931,9 @@ psc_status psc_head_logits_mx4(const uint8_t* d_q, int64_t q_stride, const uint8
                                int32_t T, const uint8_t* d_w, int64_t w_stride, const uint8_t* d_w_blocks,
                                const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
                                psc_dtype dtype, int64_t row_stride, void* stream) {
-    return head_entry(ME, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
-                               0, row_stride, WAIT_POLLS},
-                      d_logits, dtype, stream);
+    return head_entry<false>(ME, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
+                                      0, row_stride, 0},
+                             d_logits, dtype, stream);
 }
 
 psc_status psc_mx4_check_wait(const uint8_t* d_q, int64_t q_stride, const uint8_t* d_q_blocks, const float* d_scale,
@@ -937,10 +941,10 @@ psc_status psc_mx4_check_wait(const uint8_t* d_q, int64_t q_stride, const uint8_
                               const float* d_w_scale, int32_t V, int32_t K, const uint32_t* d_bitmask, void* d_logits,
                               psc_dtype dtype, int64_t row_stride, int32_t limit, void* stream) {
     const char* me = "psc_mx4_check_wait";
-    if (limit < 0 || limit > WAIT_POLLS) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
-    return head_entry(me, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
-                               0, row_stride, limit},
-                      d_logits, dtype, stream);
+    if (limit < 0 || limit > WAIT_POLLS || dtype != PSC_F32) return ops_fail(PSC_ERR_ARG, me, "bad arguments");
+    return head_entry<true>(me, Head{d_q, q_stride, d_q_blocks, d_scale, T, d_w, w_stride, d_w_blocks, d_w_scale, V, K, d_bitmask,
+                                     0, row_stride, limit},
+                            d_logits, dtype, stream);
 }
 
 psc_status psc_mx4_faults(int32_t* h_faults, int32_t reset, void* stream) {

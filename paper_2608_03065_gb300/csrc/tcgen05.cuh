@@ -32,8 +32,18 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+// The same without waiting a while for the answer (mbar_try does for up to 4 us).
+__device__ __forceinline__ bool mbar_look(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 constexpr int WAIT_POLLS = 1 << 22;
-// Bounded wait: gives up after some seconds, or soon after any other wait of the block did.
+// Bounded wait: gives up after some seconds (16), or soon after any other wait of the block did.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
     for (int it = 0; it < WAIT_POLLS; it++) {
         if (mbar_try(bar, parity)) return true;
@@ -44,19 +54,24 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 // The same by a whole warp, with one answer for all lanes; and for two barriers at once
 // (a poll takes about a hundred cycles to answer, so both are asked before either is looked at).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed, int polls = WAIT_POLLS) {
-    for (int it = 0; it < polls; it++) {
-        if (__all_sync(FULL, mbar_try(bar, parity))) return true;
+// CHECK: one that gives up after `polls` looks, for a kernel's self-test.
+template <bool CHECK = false>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* failed, int polls = 0) {
+    for (int it = 0; it < (CHECK ? polls : WAIT_POLLS); it++) {
+        if (__all_sync(FULL, CHECK ? mbar_look(bar, parity) : mbar_try(bar, parity))) return true;
         if ((it & 1023) == 1023 && __any_sync(FULL, *failed)) return false;
     }
     *failed = 1;
     return false;
 }
+template <bool CHECK = false>
 __device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1,
-                                           volatile int* failed, int polls = WAIT_POLLS) {
-    const bool a = mbar_try(bar0, parity0), b = mbar_try(bar1, parity1);
-    if (__all_sync(FULL, a && b)) return true;
-    return warp_wait(bar0, parity0, failed, polls) && warp_wait(bar1, parity1, failed, polls);
+                                           volatile int* failed, int polls = 0) {
+    if (!CHECK) {
+        const bool a = mbar_try(bar0, parity0), b = mbar_try(bar1, parity1);
+        if (__all_sync(FULL, a && b)) return true;
+    }
+    return warp_wait<CHECK>(bar0, parity0, failed, polls) && warp_wait<CHECK>(bar1, parity1, failed, polls);
 }
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;

@@ -810,8 +810,8 @@ def psc_mx4_faults(reset: bool = False, stream=None) -> int:
 
 def psc_mx4_check_wait(q, q_blocks, w, w_blocks, logits, K: int, limit: int, scale=None, w_scale=None, bitmask=None,
                        stream=None):
-    """Self-test of the fault path: psc_head_logits_mx4 with waits that give up after `limit` polls
-    (some logits are not written; psc_mx4_faults counts the blocks)."""
+    """Self-test of the fault path: psc_head_logits_mx4 into f32 logits, with waits that give up after `limit`
+    looks at a barrier (some logits are not written; psc_mx4_faults counts the blocks)."""
     _check(load().psc_mx4_check_wait(*_head_mx4(q, q_blocks, w, w_blocks, logits, K, scale, w_scale, bitmask), limit,
                                      _stream(stream)))
 

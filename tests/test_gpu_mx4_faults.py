@@ -56,16 +56,21 @@ def test_waits_that_give_up_at_once(psc, T, V, K):  # noqa: F811
 @pytest.mark.parametrize("T,V,K", SIZES)
 @pytest.mark.parametrize("masked", [False, True])
 def test_waits_that_give_up_midway(psc, T, V, K, masked):  # noqa: F811
-    """Blocks give up with copies and products under way: what is written is right, and the calls after it are."""
+    """Blocks give up with copies and products under way: what is written is right, and the calls after it are.  A look at
+    once does not find copies that have just been asked for; 4,000 take about a hundred microseconds."""
     call = _call(psc, T, V, K, masked)
     want = call()
-    for limit in (1, 2, 3, 5, 8, 13, 20, 32, 50, 100, 300, 1000, 4000):
+    for limit in (1, 2, 4, 6, 7, 8, 9, 10, 11, 12, 14, 16, 18, 20, 22, 25, 28, 32, 36, 40, 50, 80, 300, 4000):
+        before = psc.psc_mx4_faults()
         got = call(limit)
-        torch.cuda.synchronize()
+        gave_up = psc.psc_mx4_faults() - before
         assert ((got == 7) | (got == want)).all(), limit
+        assert gave_up > 0 or torch.equal(got, want)
+        # (where the masks allow nothing at all, as the one of a single row, there is nothing to wait for)
+        assert gave_up > 0 or limit > 1 or not torch.isfinite(want).any()
         assert torch.equal(call(), want)
     before = psc.psc_mx4_faults()
-    assert torch.equal(call(1 << 22), want)                 # as long as the projection itself waits
+    assert torch.equal(call(1 << 22), want)                 # as many as the projection itself waits for
     assert psc.psc_mx4_faults() == before
 
 

@@ -212,9 +212,10 @@ def test_tensors_of_another_device_are_refused(psc, monkeypatch, marshal):  # no
 
 
 @pytest.mark.parametrize("limit,kw,code", [(-1, {}, ARG), (2 ** 22 + 1, {}, ARG), (5, dict(w=None), ARG), (5, dict(q=P + 8), ARG),
-                                           (5, dict(T=2 ** 24 + 1), LIMIT), (0, dict(q=None, qb=None, out=None, T=0), 0)])
+                                           (5, dict(dtype=1), ARG), (5, dict(dtype=2), ARG), (5, dict(T=2 ** 24 + 1), LIMIT),
+                                           (0, dict(q=None, qb=None, out=None, T=0), 0)])
 def test_the_self_test_of_waits_has_the_projections_checks(psc, limit, kw, code):  # noqa: F811
-    args = _head(**kw)[1]
+    args = _head(**{"dtype": 0, **kw})[1]
     assert psc.load().psc_mx4_check_wait(*args[:-1], limit, None) == code
     if code:
         assert "psc_mx4_check_wait" in psc.load().psc_last_error().decode()
